@@ -10,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -22,6 +23,11 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument", "-Wno-gnu-zero-variadic-macro-arguments",
 ]
+
+# The layers are compiled at -O2: at -O3 one instantiation of the 32-bit
+# per-band product is unrolled until it spills (3.5 KB a lane).
+LAYER_FLAGS = [f if f != "-O3" else "-O2" for f in HIP_FLAGS]
+LAYERS = ["linear", "rotary", "attention", "attention_grad", "step"]
 
 
 def _run(cmd, verbose):
@@ -42,11 +48,16 @@ def build(verbose: bool = False) -> str:
          verbose)
     plan_o = os.path.join(BUILD, "plan.o")
     hip_o = os.path.join(BUILD, "nsgcqt.o")
-    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-c",
-          os.path.join(CSRC, "plan.cpp"), "-o", plan_o], verbose)
-    _run([hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, "nsgcqt.hip"), "-o", hip_o], verbose)
+    jobs = [["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-c", os.path.join(CSRC, "plan.cpp"), "-o", plan_o],
+            [hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, "nsgcqt.hip"), "-o", hip_o]]
+    objects = [plan_o, hip_o]
+    for name in LAYERS:
+        objects.append(os.path.join(BUILD, f"layers_{name}.o"))
+        jobs.append([hipcc, *LAYER_FLAGS, "-c", os.path.join(CSRC, "layers", f"{name}.hip"), "-o", objects[-1]])
+    with ThreadPoolExecutor(min(len(jobs), os.cpu_count() or 1)) as pool:
+        list(pool.map(lambda cmd: _run(cmd, verbose), jobs))
     tmp = LIB + ".tmp"
-    _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, plan_o, hip_o], verbose)
+    _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objects], verbose)
     os.replace(tmp, LIB)
     return LIB
 

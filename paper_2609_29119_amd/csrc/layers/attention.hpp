@@ -1,0 +1,606 @@
+// Windowed attention along the bands: forward and gradient kernels.
+//
+//   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i) over the visible j
+//   dv_j = sum_i p_ij do_i            ds_ij = p_ij (do_i . v_j - do_i . o_i)
+//   dq_i = scale sum_j ds_ij k_j      dk_j = scale sum_i ds_ij q_i
+//
+// visible(i, j): keep_j and j <= i + right and (j >= i - left or j < sinks).
+#pragma once
+#include "tile.hpp"
+
+namespace nsl {
+
+struct AttnArgs {
+    View q, k, v, o, d_o, dq, dk, dv;
+    float* stats;         // [batch][heads][rows]: log2 of the softmax sum of scores times c; +inf for an empty row
+    float* delta;         // [batch][heads][rows]: do . o
+    float* part;          // partial dk, dv of the sinks
+    const uint8_t* keep;
+    int64_t keep_batch;
+    const int64_t* off;
+    int64_t rows;
+    int n_bands, batch, heads, kv_heads, dim;
+    int left, right, sinks;   // at most rows
+    float scale, c;           // c = scale log2(e): exp(scale s) = exp2(c s)
+    bool wide;                // every view takes 16-byte accesses
+};
+
+__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr int kQueries = 128, kQueryShift = 7;   // queries (or keys, in the key gradient) of a workgroup: 4 waves of 32
+template <class T, int DP> constexpr int kv_tile() { return sizeof(T) == 4 && DP > 64 ? 32 : 64; }
+
+template <class T> __device__ inline T* row_of(const View& v, int64_t b, int64_t row, int head) {
+    return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row + head * v.head;
+}
+
+// The window's keys in tiles of BN: first tiles over the sinks that lie
+// before the window of the block's first query, then over the window.
+struct KeyRange {
+    int sink_end, sink_tiles, begin, end, tiles;
+    __device__ KeyRange(const AttnArgs& a, int i_first, int i_last, int len, int bn) {
+        begin = i_first > a.left ? i_first - a.left : 0;
+        end = static_cast<int>(static_cast<int64_t>(i_last) + a.right + 1 < len ? i_last + a.right + 1 : len);
+        sink_end = a.sinks < begin ? a.sinks : begin;
+        sink_tiles = (sink_end + bn - 1) / bn;
+        tiles = sink_tiles + (end - begin + bn - 1) / bn;
+    }
+    // first key of tile t, and the end of the keys it may hold
+    __device__ void tile(int t, int bn, int& j0, int& j_end) const {
+        const bool s = t < sink_tiles;
+        j0 = s ? t * bn : begin + (t - sink_tiles) * bn;
+        j_end = s ? sink_end : end;
+    }
+};
+
+// One tile of BN rows x DP columns of two tensors, through registers: the
+// loads of the next tile are in flight while this one is computed.
+template <class T, int DP, int BN> struct Stage {
+    static constexpr int kChunks = BN * DP / 8, kEach = (kChunks + 255) / 256, kRB = row_bytes<T, DP>();
+    static constexpr int kBytes = BN * kRB;
+    frag<T> x[kEach], y[kEach];
+
+    // rows row0 + (0 .. BN-1) below row_end; others, and those not kept, are zeros
+    __device__ void load(const T* px, int64_t sx, const T* py, int64_t sy, const uint8_t* keep, int row0, int row_end,
+                         int dim, bool wide, int tid) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int c = tid + 256 * e, row = row0 + c / (DP / 8), d = c % (DP / 8) * 8;
+            const bool there = (kChunks % 256 == 0 || c < kChunks) && row < row_end && (!keep || keep[row]);
+            const int n = there ? dim - d : 0;
+            x[e] = load8<T>(px + row * sx + d, n, wide);
+            y[e] = load8<T>(py + row * sy + d, n, wide);
+        }
+    }
+    __device__ void store(char* tx, char* ty, int tid) const {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int c = tid + 256 * e;
+            if (kChunks % 256 == 0 || c < kChunks) {
+                write8<T, kRB>(tx, c / (DP / 8), c % (DP / 8), x[e]);
+                write8<T, kRB>(ty, c / (DP / 8), c % (DP / 8), y[e]);
+            }
+        }
+    }
+};
+
+// 32 rows of a tensor as fragments (A or B): lane l holds row l % 32.
+template <class T, int DP>
+__device__ inline void load_rows(frag<T> (&f)[DP / 16], const T* p, bool there, int dim, bool wide, int lane) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        const int d = 16 * s + 8 * (lane >> 5);
+        f[s] = load8<T>(p + d, there ? dim - d : 0, wide);
+    }
+}
+
+// Zeros for the rows [first, first + 128) of tokens that no band holds.
+template <class T>
+__device__ inline void zero_rows(const View& v, int64_t b, int head, int64_t start, int64_t first, int64_t len, int dim,
+                                 int tid) {
+    for (int64_t r = first; r < first + kQueries && r < len; ++r)
+        for (int d = tid; d < dim; d += 256) row_of<T>(v, b, start + r, head)[d] = static_cast<T>(0.f);
+}
+
+template <class T, int DP>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_attention(AttnArgs a) {
+    constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
+    typedef Stage<T, DP, BN> St;
+    __shared__ __align__(128) char lds[2][2][St::kBytes];
+    __shared__ unsigned kept[2][2];   // a bit for each key of a tile
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+
+    int64_t w = die_order(blockIdx.x, gridDim.x);
+    const int head = static_cast<int>(w % a.heads);
+    w /= a.heads;
+    const int64_t per = tile_count<kQueryShift>(a.n_bands, 1, a.rows), b = w / per;
+    const Tile t = find_tile<kQueryShift>(a.off, a.n_bands, a.rows, 1, w % per, lane);
+    if (!t.live) return;
+    const int len = static_cast<int>(t.len), q0 = static_cast<int>(t.first), kv = head / (a.heads / a.kv_heads);
+    float* stats = a.stats ? a.stats + (b * a.heads + head) * a.rows + t.start : nullptr;
+    if (t.band < 0 || t.band >= a.n_bands) {
+        zero_rows<T>(a.o, b, head, t.start, t.first, t.len, a.dim, tid);
+        if (stats && tid < kQueries && q0 + tid < len) stats[q0 + tid] = INFINITY;
+        return;
+    }
+
+    const int i_lo = q0 + 32 * wave, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
+    const bool mine = i < len, active = i_lo < len;
+    frag<T> qf[DP / 16];
+    load_rows<T, DP>(qf, row_of<T>(a.q, b, t.start + (mine ? i : 0), head), mine, a.dim, a.wide, lane);
+    const T* kp = row_of<T>(a.k, b, t.start, kv);
+    const T* vp = row_of<T>(a.v, b, t.start, kv);
+    const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
+
+    acc16 o[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = zero16();
+    float top = -INFINITY, sum = 0.f;   // running maximum of the raw scores; this half's sum
+
+    const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
+    St st;
+    auto fetch = [&](int n) {
+        int j0, j_end;
+        range.tile(n, BN, j0, j_end);
+        st.load(kp, a.k.row, vp, a.v.row, keep, j0, j_end, a.dim, a.wide, tid);
+    };
+    auto put = [&](int n) {
+        st.store(lds[n & 1][0], lds[n & 1][1], tid);
+        if (keep && tid < BN) {
+            int j0, j_end;
+            range.tile(n, BN, j0, j_end);
+            const uint64_t bits = __ballot(j0 + tid < j_end && keep[j0 + tid] != 0);
+            if (tid < 2) kept[n & 1][tid] = static_cast<unsigned>(bits >> (32 * tid));
+        }
+    };
+    fetch(0);
+    put(0);
+    __syncthreads();
+    for (int n = 0; n < range.tiles; ++n) {
+        if (n + 1 < range.tiles) fetch(n + 1);
+        int j0, j_end;
+        range.tile(n, BN, j0, j_end);
+        const int j_last = min(j0 + BN, j_end) - 1;
+        const bool skip = !active || j0 > i_hi + a.right || (j_last < i_lo - a.left && j0 >= a.sinks);
+        if (!skip) {
+            const char* kt = lds[n & 1][0];
+            const char* vt = lds[n & 1][1];
+            acc16 s[BN / 32];
+#pragma unroll
+            for (int kb = 0; kb < BN / 32; ++kb) {
+                s[kb] = zero16();
+#pragma unroll
+                for (int x = 0; x < DP / 16; ++x) s[kb] = mma(read8<T, RB>(kt, 32 * kb + m, 2 * x + h), qf[x], s[kb]);
+            }
+            const bool all = !keep && j0 + BN <= j_end && j_last <= i_lo + a.right &&
+                             (j0 >= i_hi - a.left || j_last < a.sinks);
+            if (!all) {
+                unsigned ok[BN / 32];
+#pragma unroll
+                for (int kb = 0; kb < BN / 32; ++kb) ok[kb] = keep ? kept[n & 1][kb] : ~0u;
+#pragma unroll
+                for (int kb = 0; kb < BN / 32; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int jj = 8 * (r >> 2) + 4 * h + (r & 3), j = j0 + 32 * kb + jj;
+                        const bool see = j < j_end && j <= i + a.right && (j >= i - a.left || j < a.sinks) &&
+                                         ((ok[kb] >> jj) & 1);
+                        s[kb][r] = see ? s[kb][r] : -INFINITY;
+                    }
+            }
+            float mx = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < BN / 32; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+            const float now = fmaxf(top, half_max(mx));
+            const float base = now == -INFINITY ? 0.f : now * a.c;
+            if (__any(now != top)) {
+                const float alpha = exp2_(fmaf(top, a.c, -base));
+                sum *= alpha;
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
+                top = now;
+            }
+#pragma unroll
+            for (int kb = 0; kb < BN / 32; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[kb][r] = exp2_(fmaf(s[kb][r], a.c, -base));
+                    sum += s[kb][r];
+                }
+#pragma unroll
+            for (int x = 0; x < BN / 16; ++x) {
+                const frag<T> p = narrow<T>(s[x / 2], x % 2);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) o[d] = mma(read_turned<T, RB>(vt, 16 * x, 32 * d, lane), p, o[d]);
+            }
+        }
+        if (n + 1 < range.tiles) put(n + 1);
+        __syncthreads();
+    }
+    const float total = half_sum(sum);
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T* out = mine ? row_of<T>(a.o, b, t.start + i, head) : nullptr;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+        o[d] *= inv;
+        store_column<T>(out, o[d], 32 * d, a.dim, a.wide, lane);
+    }
+    if (stats && mine && h == 0)
+        stats[i] = total == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top * a.c) + __log2f(total);
+}
+
+// --------------------------------------------------------------- gradients
+
+// dq, and delta = do . o for the key gradient. Layout as k_attention: the
+// scores and dp are formed transposed, so ds is the B fragment of dq^T = K^T ds^T.
+template <class T, int DP>
+__global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs a) {
+    constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
+    typedef Stage<T, DP, BN> St;
+    __shared__ __align__(128) char lds[2][2][St::kBytes];
+    __shared__ unsigned kept[2][2];   // a bit for each key of a tile
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+
+    int64_t w = die_order(blockIdx.x, gridDim.x);
+    const int head = static_cast<int>(w % a.heads);
+    w /= a.heads;
+    const int64_t per = tile_count<kQueryShift>(a.n_bands, 1, a.rows), b = w / per;
+    const Tile t = find_tile<kQueryShift>(a.off, a.n_bands, a.rows, 1, w % per, lane);
+    if (!t.live) return;
+    if (t.band < 0 || t.band >= a.n_bands) {
+        zero_rows<T>(a.dq, b, head, t.start, t.first, t.len, a.dim, tid);
+        return;
+    }
+    const int len = static_cast<int>(t.len), q0 = static_cast<int>(t.first), kv = head / (a.heads / a.kv_heads);
+    const int64_t at = (b * a.heads + head) * a.rows + t.start;
+
+    const int i_lo = q0 + 32 * wave, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
+    const bool mine = i < len, active = i_lo < len;
+    const int64_t row = t.start + (mine ? i : 0);
+    frag<T> qf[DP / 16], gf[DP / 16];
+    load_rows<T, DP>(qf, row_of<T>(a.q, b, row, head), mine, a.dim, a.wide, lane);
+    load_rows<T, DP>(gf, row_of<T>(a.d_o, b, row, head), mine, a.dim, a.wide, lane);
+    float delta = 0.f;
+    {
+        frag<T> of[DP / 16];
+        load_rows<T, DP>(of, row_of<T>(a.o, b, row, head), mine, a.dim, a.wide, lane);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                delta = fmaf(static_cast<float>(of[s][j]), static_cast<float>(gf[s][j]), delta);
+    }
+    delta = half_sum(delta);
+    if (mine && h == 0) a.delta[at + i] = delta;
+    const float lse = mine ? a.stats[at + i] : INFINITY;
+
+    const T* kp = row_of<T>(a.k, b, t.start, kv);
+    const T* vp = row_of<T>(a.v, b, t.start, kv);
+    const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
+    acc16 g[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) g[d] = zero16();
+
+    const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
+    St st;
+    auto fetch = [&](int n) {
+        int j0, j_end;
+        range.tile(n, BN, j0, j_end);
+        st.load(kp, a.k.row, vp, a.v.row, keep, j0, j_end, a.dim, a.wide, tid);
+    };
+    auto put = [&](int n) {
+        st.store(lds[n & 1][0], lds[n & 1][1], tid);
+        if (keep && tid < BN) {
+            int j0, j_end;
+            range.tile(n, BN, j0, j_end);
+            const uint64_t bits = __ballot(j0 + tid < j_end && keep[j0 + tid] != 0);
+            if (tid < 2) kept[n & 1][tid] = static_cast<unsigned>(bits >> (32 * tid));
+        }
+    };
+    fetch(0);
+    put(0);
+    __syncthreads();
+    for (int n = 0; n < range.tiles; ++n) {
+        if (n + 1 < range.tiles) fetch(n + 1);
+        int j0, j_end;
+        range.tile(n, BN, j0, j_end);
+        const int j_last = min(j0 + BN, j_end) - 1;
+        const bool skip = !active || j0 > i_hi + a.right || (j_last < i_lo - a.left && j0 >= a.sinks);
+        if (!skip) {
+            const char* kt = lds[n & 1][0];
+            const char* vt = lds[n & 1][1];
+            const bool all = !keep && j0 + BN <= j_end && j_last <= i_lo + a.right &&
+                             (j0 >= i_hi - a.left || j_last < a.sinks);
+#pragma unroll
+            for (int kb = 0; kb < BN / 32; ++kb) {
+                acc16 s = zero16(), dp = zero16();
+#pragma unroll
+                for (int x = 0; x < DP / 16; ++x) {
+                    s = mma(read8<T, RB>(kt, 32 * kb + m, 2 * x + h), qf[x], s);
+                    dp = mma(read8<T, RB>(vt, 32 * kb + m, 2 * x + h), gf[x], dp);
+                }
+                if (all) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
+                } else {
+                    const unsigned ok = keep ? kept[n & 1][kb] : ~0u;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int jj = 8 * (r >> 2) + 4 * h + (r & 3), j = j0 + 32 * kb + jj;
+                        const bool see = j < j_end && j <= i + a.right && (j >= i - a.left || j < a.sinks) &&
+                                         ((ok >> jj) & 1);
+                        const float p = exp2_(fmaf(s[r], a.c, -lse));
+                        s[r] = see ? p * (dp[r] - delta) : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const frag<T> ds = narrow<T>(s, x);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d)
+                        g[d] = mma(read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane), ds, g[d]);
+                }
+            }
+        }
+        if (n + 1 < range.tiles) put(n + 1);
+        __syncthreads();
+    }
+    T* out = mine ? row_of<T>(a.dq, b, t.start + i, head) : nullptr;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+        g[d] *= a.scale;
+        store_column<T>(out, g[d], 32 * d, a.dim, a.wide, lane);
+    }
+}
+
+// The sinks' keys are seen from everywhere. Queries past the window of a key
+// tile's last key ("far" ones) would make one workgroup walk a whole band, so
+// k_attention_far takes them in chunks and leaves partial dk, dv, which the
+// workgroup of the key tile adds up in the chunks' order.
+constexpr int kFarShift = 10;   // queries of a chunk
+__device__ inline int64_t far_begin(const AttnArgs& a, int sink_tile) {   // of 32 keys
+    return static_cast<int64_t>(sink_tile * 32 / kQueries * kQueries) + kQueries + a.left;
+}
+__device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t item, int sink_tile) {
+    const int64_t per = tile_count<kFarShift>(a.n_bands, 1, a.rows);
+    const int n = (a.sinks + 31) / 32;
+    return a.part + (((b * a.kv_heads + kv) * per + item) * n + sink_tile) * (2 * 32 * a.dim);
+}
+
+// One wave's 32 queries (rows of the tiles qt, gt at r0) against its 32 keys:
+// adds to dk^T and dv^T. lse, delta: of the tile's queries, in LDS.
+// see(query row in the tile): whether this lane's key is visible to it.
+template <class T, int DP, class See>
+__device__ inline void key_grad(const char* qt, const char* gt, const float* lse, const float* delta, int r0,
+                                const frag<T> (&kf)[DP / 16], const frag<T> (&vf)[DP / 16], acc16 (&dk)[DP / 32],
+                                acc16 (&dv)[DP / 32], float c, bool all, int lane, See see) {
+    constexpr int RB = row_bytes<T, DP>();
+    const int m = lane & 31, h = lane >> 5;
+    acc16 s = zero16(), dp = zero16();
+#pragma unroll
+    for (int x = 0; x < DP / 16; ++x) {
+        s = mma(read8<T, RB>(qt, r0 + m, 2 * x + h), kf[x], s);
+        dp = mma(read8<T, RB>(gt, r0 + m, 2 * x + h), vf[x], dp);
+    }
+    auto weigh = [&](auto ok) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const f4 l = *reinterpret_cast<const f4*>(lse + r0 + 8 * q + 4 * h);
+            const f4 e = *reinterpret_cast<const f4*>(delta + r0 + 8 * q + 4 * h);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 4 * q + j;
+                const float p = exp2_(fmaf(s[r], c, -l[j])), ds = p * (dp[r] - e[j]);
+                const bool o = ok(r0 + 8 * q + 4 * h + j);
+                s[r] = o ? p : 0.f;
+                dp[r] = o ? ds : 0.f;
+            }
+        }
+    };
+    if (all)
+        weigh([](int) { return true; });
+    else
+        weigh(see);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const frag<T> p = narrow<T>(s, x), ds = narrow<T>(dp, x);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            dv[d] = mma(read_turned<T, RB>(gt, r0 + 16 * x, 32 * d, lane), p, dv[d]);
+            dk[d] = mma(read_turned<T, RB>(qt, r0 + 16 * x, 32 * d, lane), ds, dk[d]);
+        }
+    }
+}
+
+// dk, dv of 128 keys (a wave has 32) over the queries near them.
+template <class T, int DP>
+__global__ __launch_bounds__(256, DP > 32 ? 1 : 2) void k_attention_dkv(AttnArgs a) {
+    constexpr int BQ = kv_tile<T, DP>();
+    typedef Stage<T, DP, BQ> St;
+    __shared__ __align__(128) char lds[2][2][St::kBytes];
+    __shared__ __align__(16) float row_lse[2][BQ], row_delta[2][BQ];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+
+    int64_t w = die_order(blockIdx.x, gridDim.x);
+    const int kv = static_cast<int>(w % a.kv_heads);
+    w /= a.kv_heads;
+    const int64_t per = tile_count<kQueryShift>(a.n_bands, 1, a.rows), b = w / per;
+    const Tile t = find_tile<kQueryShift>(a.off, a.n_bands, a.rows, 1, w % per, lane);
+    if (!t.live) return;
+    if (t.band < 0 || t.band >= a.n_bands) {
+        zero_rows<T>(a.dk, b, kv, t.start, t.first, t.len, a.dim, tid);
+        zero_rows<T>(a.dv, b, kv, t.start, t.first, t.len, a.dim, tid);
+        return;
+    }
+    const int len = static_cast<int>(t.len), k0 = static_cast<int>(t.first), group = a.heads / a.kv_heads;
+    const int j_lo = k0 + 32 * wave, j = j_lo + m, j_hi = min(j_lo + 31, len - 1);
+    const bool mine = j < len, active = j_lo < len;
+    const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
+    const bool kept = mine && (!keep || keep[j]);
+    const int64_t row = t.start + (mine ? j : 0);
+    frag<T> kf[DP / 16], vf[DP / 16];
+    load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, a.wide, lane);
+    load_rows<T, DP>(vf, row_of<T>(a.v, b, row, kv), kept, a.dim, a.wide, lane);
+    acc16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
+
+    const int i_begin = k0 > a.right ? k0 - a.right : 0;
+    const int i_end = static_cast<int64_t>(k0) + kQueries + a.left < len ? k0 + kQueries + a.left : len;
+    const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
+    St st;
+    float next_lse = 0.f, next_delta = 0.f;
+    auto fetch = [&](int n) {
+        const int head = kv * group + n / q_tiles, i0 = i_begin + n % q_tiles * BQ;
+        st.load(row_of<T>(a.q, b, t.start, head), a.q.row, row_of<T>(a.d_o, b, t.start, head), a.d_o.row, nullptr, i0,
+                i_end, a.dim, a.wide, tid);
+        if (tid < BQ) {
+            const int64_t at = (b * a.heads + head) * a.rows + t.start + i0 + tid;
+            const bool there = i0 + tid < i_end;
+            next_lse = there ? a.stats[at] : INFINITY;
+            next_delta = there ? a.delta[at] : 0.f;
+        }
+    };
+    auto put = [&](int n) {
+        st.store(lds[n & 1][0], lds[n & 1][1], tid);
+        if (tid < BQ) {
+            row_lse[n & 1][tid] = next_lse;
+            row_delta[n & 1][tid] = next_delta;
+        }
+    };
+    fetch(0);
+    put(0);
+    __syncthreads();
+    for (int n = 0; n < total; ++n) {
+        if (n + 1 < total) fetch(n + 1);
+        const int i0 = i_begin + n % q_tiles * BQ;
+#pragma unroll
+        for (int qb = 0; qb < BQ / 32; ++qb) {
+            const int i_lo = i0 + 32 * qb, i_hi = min(i_lo + 31, i_end - 1);
+            const bool skip = !active || i_lo >= i_end || j_lo > i_hi + a.right ||
+                              (j_hi < i_lo - a.left && j_lo >= a.sinks);
+            if (!skip) {
+                const bool all = !keep && j_lo + 31 < len && i_lo + 31 < i_end && j_hi <= i_lo + a.right &&
+                                 (j_lo >= i_hi - a.left || j_hi < a.sinks);
+                key_grad<T, DP>(lds[n & 1][0], lds[n & 1][1], row_lse[n & 1], row_delta[n & 1], 32 * qb, kf, vf, dk, dv,
+                                a.c, all, lane, [&](int r) {
+                                    const int i = i0 + r;
+                                    return kept && i < i_end && j <= i + a.right &&
+                                           (j >= i - a.left || j < a.sinks);
+                                });
+            }
+        }
+        if (n + 1 < total) put(n + 1);
+        __syncthreads();
+    }
+    // the far queries' share of the sinks
+    if (j_lo < a.sinks && active) {
+        const int tile = j_lo / 32;
+        const int64_t begin = far_begin(a, tile);
+        const int64_t item0 = (t.start >> kFarShift) + t.band + 1;
+        if (begin < len)
+            for (int64_t ch = begin >> kFarShift; ch <= (len - 1) >> kFarShift; ++ch) {
+                const float* p = far_part(a, b, kv, item0 + ch, tile) + m * a.dim;
+                if (j < a.sinks && mine) {
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int c = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
+                            if (c < a.dim) {
+                                dk[d][r] += p[c];
+                                dv[d][r] += p[32 * a.dim + c];
+                            }
+                        }
+                }
+            }
+    }
+    T* ok = mine ? row_of<T>(a.dk, b, t.start + j, kv) : nullptr;
+    T* ov = mine ? row_of<T>(a.dv, b, t.start + j, kv) : nullptr;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+        dk[d] *= a.scale;
+        store_column<T>(ok, dk[d], 32 * d, a.dim, a.wide, lane);
+        store_column<T>(ov, dv[d], 32 * d, a.dim, a.wide, lane);
+    }
+}
+
+// Partial dk, dv of 32 sink keys over the far queries of one chunk. Every wave
+// has the same keys and takes a quarter of the queries; the four results are
+// added in the waves' order.
+template <class T, int DP>
+__global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
+    constexpr int BQ = sizeof(T) == 4 && DP > 64 ? 64 : 128;
+    typedef Stage<T, DP, BQ> St;
+    __shared__ __align__(128) char lds[2][St::kBytes];
+    __shared__ __align__(16) float row_lse[BQ], row_delta[BQ];
+    __shared__ __align__(16) float joined[2][DP][33];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+
+    const int n_sink = (a.sinks + 31) / 32;
+    int64_t w = die_order(blockIdx.x, gridDim.x);
+    const int tile = static_cast<int>(w % n_sink);
+    w /= n_sink;
+    const int kv = static_cast<int>(w % a.kv_heads);
+    w /= a.kv_heads;
+    const int64_t per = tile_count<kFarShift>(a.n_bands, 1, a.rows), b = w / per, item = w % per;
+    const Tile t = find_tile<kFarShift>(a.off, a.n_bands, a.rows, 1, item, lane);
+    if (!t.live || t.band < 0 || t.band >= a.n_bands) return;
+    const int len = static_cast<int>(t.len), group = a.heads / a.kv_heads, j = 32 * tile + m;
+    const int64_t far = far_begin(a, tile);
+    const int i_end = min(static_cast<int>(t.first) + (1 << kFarShift), len);
+    if (far >= i_end) return;
+    const int i_begin = max(static_cast<int>(t.first), static_cast<int>(far));
+    const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
+    const bool kept = j < a.sinks && j < len && (!keep || keep[j]);
+    const int64_t row = t.start + (j < len ? j : 0);
+    frag<T> kf[DP / 16], vf[DP / 16];
+    load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, a.wide, lane);
+    load_rows<T, DP>(vf, row_of<T>(a.v, b, row, kv), kept, a.dim, a.wide, lane);
+    acc16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
+
+    for (int g = 0; g < group; ++g) {
+        const int head = kv * group + g;
+        const int64_t at = (b * a.heads + head) * a.rows + t.start;
+        for (int i0 = i_begin; i0 < i_end; i0 += BQ) {
+            St st;
+            st.load(row_of<T>(a.q, b, t.start, head), a.q.row, row_of<T>(a.d_o, b, t.start, head), a.d_o.row, nullptr,
+                    i0, i_end, a.dim, a.wide, tid);
+            __syncthreads();   // the previous tile has been read
+            st.store(lds[0], lds[1], tid);
+            if (tid < BQ) {
+                const bool there = i0 + tid < i_end;
+                row_lse[tid] = there ? a.stats[at + i0 + tid] : INFINITY;
+                row_delta[tid] = there ? a.delta[at + i0 + tid] : 0.f;
+            }
+            __syncthreads();
+            if (32 * wave < BQ && i0 + 32 * wave < i_end)
+                key_grad<T, DP>(lds[0], lds[1], row_lse, row_delta, 32 * wave, kf, vf, dk, dv, a.c, false, lane,
+                                [&](int r) { return kept && i0 + r < i_end; });
+        }
+    }
+    for (int v = 0; v < 4; ++v) {
+        if (wave == v) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int c = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
+                    joined[0][c][m] = (v ? joined[0][c][m] : 0.f) + dk[d][r];
+                    joined[1][c][m] = (v ? joined[1][c][m] : 0.f) + dv[d][r];
+                }
+        }
+        __syncthreads();
+    }
+    float* out = far_part(a, b, kv, item, tile);
+    for (int x = tid; x < 2 * 32 * a.dim; x += 256) {
+        const int c = x % a.dim, key = x / a.dim % 32;
+        out[x] = joined[x / (32 * a.dim)][c][key];
+    }
+}
+
+}  // namespace nsl

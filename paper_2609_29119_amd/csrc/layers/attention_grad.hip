@@ -1,0 +1,73 @@
+// C entry of the attention's gradients.
+#include "attention_host.hpp"
+
+using namespace nsl;
+
+namespace {
+
+int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
+
+int64_t delta_bytes(const AttnArgs& a) { return align256(4 * a.rows * a.batch * a.heads); }
+
+int64_t part_bytes(const AttnArgs& a) {
+    return 4 * tile_count<kFarShift>(a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32) * 2 * 32 *
+           a.dim;
+}
+
+// Whether some query lies past the window of some sink's key tile.
+bool has_far(const AttnArgs& a) { return a.sinks > 0 && int64_t(kQueries) + a.left < a.rows; }
+
+}  // namespace
+
+extern "C" int64_t nsgcqt_band_attention_workspace(const nsgcqt_rows* r, const nsgcqt_attention_shape* s) {
+    CHECK_TRY(check_rows(r));
+    CHECK_TRY(check_shape(s));
+    const AttnArgs a = attention_args(r, s);
+    return delta_bytes(a) + (has_far(a) ? part_bytes(a) : 0);
+}
+
+extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_attention_shape* s,
+                                          const nsgcqt_view* q, const nsgcqt_view* k, const nsgcqt_view* v,
+                                          const nsgcqt_view* o, const float* stats, const nsgcqt_view* d_o,
+                                          const nsgcqt_view* dq, const nsgcqt_view* dk, const nsgcqt_view* dv,
+                                          void* ws, size_t ws_bytes, void* stream) {
+    CHECK_TRY(check_dtype(dtype));
+    CHECK_TRY(check_rows(r));
+    CHECK_TRY(check_shape(s));
+    AttnArgs a = attention_args(r, s);
+    a.wide = true;
+    const struct {
+        const nsgcqt_view* v;
+        const char* name;
+        View* to;
+        int64_t heads;
+    } views[] = {{q, "q", &a.q, s->n_heads},       {k, "k", &a.k, s->n_kv_heads},     {v, "v", &a.v, s->n_kv_heads},
+                 {o, "o", &a.o, s->n_heads},       {d_o, "d_o", &a.d_o, s->n_heads},  {dq, "dq", &a.dq, s->n_heads},
+                 {dk, "dk", &a.dk, s->n_kv_heads}, {dv, "dv", &a.dv, s->n_kv_heads}};
+    for (const auto& x : views)
+        CHECK_TRY(check_view(x.v, x.name, dtype, r->batch, r->rows, x.heads, s->head_dim, a.wide));
+    if (r->batch == 0 || r->rows == 0) return NSGCQT_OK;
+    if (!stats || misaligned(stats, 4)) return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 4 bytes");
+    const int64_t need = delta_bytes(a) + (has_far(a) ? part_bytes(a) : 0);
+    if (static_cast<int64_t>(ws_bytes) < need)
+        return set_err(NSGCQT_EWORKSPACE, "workspace of " + std::to_string(ws_bytes) + " bytes, " +
+                                              std::to_string(need) + " required");
+    if (!ws || misaligned(ws, 16)) return set_err(NSGCQT_EINVAL, "workspace is NULL or not aligned to 16 bytes");
+    for (const auto& x : views) *x.to = view_of(x.v);
+    a.stats = const_cast<float*>(stats);
+    a.delta = static_cast<float*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + delta_bytes(a));
+    const int64_t tiles = tile_count<kQueryShift>(a.n_bands, 1, a.rows) * a.batch;
+    const int64_t far = tile_count<kFarShift>(a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32);
+    CHECK_TRY(check_grid(tiles * a.heads));
+    CHECK_TRY(check_grid(far));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_type_and_width(dtype, s->head_dim, [&](auto t, auto dp) -> int {
+        using T = decltype(t);
+        constexpr int DP = decltype(dp)::value;
+        LAUNCH_TRY(k_attention_dq<T, DP>, dim3(static_cast<unsigned>(tiles * a.heads)), dim3(256), 0, st, a);
+        if (has_far(a)) LAUNCH_TRY(k_attention_far<T, DP>, dim3(static_cast<unsigned>(far)), dim3(256), 0, st, a);
+        LAUNCH_TRY(k_attention_dkv<T, DP>, dim3(static_cast<unsigned>(tiles * a.kv_heads)), dim3(256), 0, st, a);
+        return NSGCQT_OK;
+    });
+}

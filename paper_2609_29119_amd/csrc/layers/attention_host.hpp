@@ -1,0 +1,52 @@
+// What the forward and the gradient entry of the attention share on the host.
+#pragma once
+#include <cmath>
+
+#include "attention.hpp"
+#include "checks.hpp"
+
+namespace nsl {
+
+inline int check_shape(const nsgcqt_attention_shape* s) {
+    if (!s) return set_err(NSGCQT_EINVAL, "shape is NULL");
+    if (s->n_heads < 1 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads)
+        return set_err(NSGCQT_EINVAL, "n_kv_heads must divide n_heads, both at least 1");
+    if (s->head_dim < 1) return set_err(NSGCQT_EINVAL, "head_dim must be at least 1");
+    if (s->left < 0 || s->right < 0 || s->sinks < 0)
+        return set_err(NSGCQT_EINVAL, "left, right and sinks must not be negative");
+    if (!(s->scale > 0) || !std::isfinite(s->scale)) return set_err(NSGCQT_EINVAL, "scale must be positive and finite");
+    if (s->head_dim > 128) return set_err(NSGCQT_EUNSUPPORTED, "head_dim above 128");
+    if (s->n_heads > 65536) return set_err(NSGCQT_EUNSUPPORTED, "more than 65,536 heads");
+    return NSGCQT_OK;
+}
+
+inline AttnArgs attention_args(const nsgcqt_rows* r, const nsgcqt_attention_shape* s) {
+    AttnArgs a{};
+    a.keep = s->keep;
+    a.keep_batch = s->keep_batch;
+    a.off = r->offsets;
+    a.rows = r->rows;
+    a.n_bands = static_cast<int>(r->n_bands);
+    a.batch = static_cast<int>(r->batch);
+    a.heads = static_cast<int>(s->n_heads);
+    a.kv_heads = static_cast<int>(s->n_kv_heads);
+    a.dim = static_cast<int>(s->head_dim);
+    auto cut = [&](int64_t v) { return static_cast<int>(v < r->rows ? v : r->rows); };
+    a.left = cut(s->left);
+    a.right = cut(s->right);
+    a.sinks = cut(s->sinks);
+    a.scale = static_cast<float>(s->scale);
+    a.c = static_cast<float>(s->scale * 1.4426950408889634);
+    return a;
+}
+
+// f(T(), DP) with the head width's padded size as an integral constant
+template <class F> int by_type_and_width(int dtype, int64_t dim, F f) {
+    return by_type(dtype, [&](auto t) {
+        if (dim <= 32) return f(t, std::integral_constant<int, 32>());
+        if (dim <= 64) return f(t, std::integral_constant<int, 64>());
+        return f(t, std::integral_constant<int, 128>());
+    });
+}
+
+}  // namespace nsl

@@ -1,0 +1,126 @@
+// C entries of the per-band products.
+#include "checks.hpp"
+#include "linear.hpp"
+
+using namespace nsl;
+
+namespace {
+
+int check_linear(int dtype, const nsgcqt_rows* r, int64_t n_in, int64_t n_out) {
+    CHECK_TRY(check_dtype(dtype));
+    CHECK_TRY(check_rows(r));
+    if (n_in < 0 || n_out < 0) return set_err(NSGCQT_EINVAL, "a width is negative");
+    if (n_in > kMaxWidth || n_out > kMaxWidth) return set_err(NSGCQT_EUNSUPPORTED, "a width above 65,536");
+    return NSGCQT_OK;
+}
+
+LinearArgs linear_args(const nsgcqt_rows* r, int64_t n_in, int64_t n_out) {
+    LinearArgs a{};
+    a.off = r->offsets;
+    a.rows = r->rows;
+    a.n_bands = static_cast<int>(r->n_bands);
+    a.batch = static_cast<int>(r->batch);
+    a.n_in = static_cast<int>(n_in);
+    a.n_out = static_cast<int>(n_out);
+    a.x_wide = a.y_wide = true;
+    return a;
+}
+
+int check_weights(const void* w, const char* name, int dtype, int64_t count) {
+    if (count && !w) return set_err(NSGCQT_EINVAL, std::string(name) + " is NULL");
+    if (misaligned(w, elem_bytes(dtype))) return set_err(NSGCQT_EINVAL, std::string(name) + " is not aligned to its element");
+    return NSGCQT_OK;
+}
+
+// y = W x, or with BACK dx = W^T dy: in has n_red columns, out n_col.
+template <bool BACK>
+int run_linear(int dtype, const nsgcqt_rows* r, const nsgcqt_view* in, const void* w, const void* bias,
+               const nsgcqt_view* out, int64_t n_in, int64_t n_out, void* stream) {
+    CHECK_TRY(check_linear(dtype, r, n_in, n_out));
+    LinearArgs a = linear_args(r, n_in, n_out);
+    const int64_t n_red = BACK ? n_out : n_in, n_col = BACK ? n_in : n_out;
+    CHECK_TRY(check_view(in, BACK ? "dy" : "x", dtype, r->batch, r->rows, 1, n_red, a.x_wide));
+    CHECK_TRY(check_view(out, BACK ? "dx" : "y", dtype, r->batch, r->rows, 1, n_col, a.y_wide));
+    CHECK_TRY(check_weights(w, "w", dtype, r->n_bands * n_in * n_out));
+    CHECK_TRY(check_weights(bias, "bias", dtype, 0));
+    if (r->batch == 0 || r->rows == 0 || n_col == 0) return NSGCQT_OK;
+    a.x = view_of(in);
+    a.y = view_of(out);
+    a.w = w;
+    a.bias = bias;
+    a.w_wide = n_in % 8 == 0 && !misaligned(w, 16);
+    const int64_t tiles = tile_count<kRowShift>(a.n_bands, a.batch, a.rows);
+    return by_type(dtype, [&](auto t) -> int {
+        using T = decltype(t);
+        auto go = [&](auto nb) -> int {
+            constexpr int NB = decltype(nb)::value;
+            const int64_t blocks = tiles * ((n_col + 32 * NB - 1) / (32 * NB));
+            CHECK_TRY(check_grid(blocks));
+            LAUNCH_TRY(k_linear<T, NB, BACK>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), a);
+            return NSGCQT_OK;
+        };
+        if (n_col <= 32) return go(std::integral_constant<int, 1>());
+        if (n_col <= 64) return go(std::integral_constant<int, 2>());
+        return go(std::integral_constant<int, 4>());
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int nsgcqt_band_linear(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const void* w, const void* bias,
+                       const nsgcqt_view* y, int64_t n_in, int64_t n_out, void* stream) {
+    return run_linear<false>(dtype, r, x, w, bias, y, n_in, n_out, stream);
+}
+
+int nsgcqt_band_linear_grad_input(int dtype, const nsgcqt_rows* r, const nsgcqt_view* dy, const void* w,
+                                  const nsgcqt_view* dx, int64_t n_in, int64_t n_out, void* stream) {
+    return run_linear<true>(dtype, r, dy, w, nullptr, dx, n_in, n_out, stream);
+}
+
+int64_t nsgcqt_band_linear_workspace(int64_t n_bands, int64_t batch, int64_t rows, int64_t n_in, int64_t n_out) {
+    static const int64_t none = 0;
+    const nsgcqt_rows r{&none, n_bands, batch, rows};
+    CHECK_TRY(check_linear(NSGCQT_F32, &r, n_in, n_out));
+    return 4 * tile_count<kChunkShift>(n_bands, batch, rows) * (n_in * n_out + n_out);
+}
+
+int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const nsgcqt_view* dy,
+                                   void* dw, void* db, int64_t n_in, int64_t n_out, void* ws, size_t ws_bytes,
+                                   void* stream) {
+    CHECK_TRY(check_linear(dtype, r, n_in, n_out));
+    LinearArgs a = linear_args(r, n_in, n_out);
+    CHECK_TRY(check_view(x, "x", dtype, r->batch, r->rows, 1, n_in, a.x_wide));
+    CHECK_TRY(check_view(dy, "dy", dtype, r->batch, r->rows, 1, n_out, a.y_wide));
+    CHECK_TRY(check_weights(dw, "dw", dtype, r->n_bands * n_in * n_out));
+    CHECK_TRY(check_weights(db, "db", dtype, 0));
+    if (r->n_bands == 0 || n_out == 0 || (n_in == 0 && !db)) return NSGCQT_OK;
+    const int64_t need = nsgcqt_band_linear_workspace(r->n_bands, r->batch, r->rows, n_in, n_out);
+    if (static_cast<int64_t>(ws_bytes) < need)
+        return set_err(NSGCQT_EWORKSPACE, "workspace of " + std::to_string(ws_bytes) + " bytes, " +
+                                              std::to_string(need) + " required");
+    if (!ws || misaligned(ws, 16)) return set_err(NSGCQT_EINVAL, "workspace is NULL or not aligned to 16 bytes");
+    a.x = view_of(x);
+    a.y = view_of(dy);
+    a.dw = dw;
+    a.db = db;
+    a.part = static_cast<float*>(ws);
+    // with no inputs there is still the sum of dy
+    const int64_t ot = (n_out + 127) / 128, it = n_in ? (n_in + 127) / 128 : 1;
+    const int64_t blocks = tile_count<kChunkShift>(a.n_bands, a.batch, a.rows) * ot * it;
+    const int64_t join = (n_in * n_out + n_out + 255) / 256;
+    CHECK_TRY(check_grid(blocks));
+    if (r->n_bands > 65535) return set_err(NSGCQT_EUNSUPPORTED, "more than 65,535 bands in a gradient of weights");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_type(dtype, [&](auto t) -> int {
+        using T = decltype(t);
+        LAUNCH_TRY(k_linear_dw<T>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
+        LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64), static_cast<unsigned>(a.n_bands)),
+                   dim3(256), 0, st, a);
+        return NSGCQT_OK;
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,104 @@
+// Rotary positions over several axes.
+//
+//   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = +- positions[axis(p)] freqs[p]
+#pragma once
+#include "tile.hpp"
+
+namespace nsl {
+
+struct RotaryArgs {
+    View in[2], out[2];      // q and k
+    int heads[2];
+    const void* positions;
+    int64_t pos_axis, pos_batch;
+    const float* freqs;
+    int64_t rows, tokens;    // tokens = batch * rows
+    int pos_type, dim, pairs, ends[4];   // ends[x]: first pair past axis x
+    int chunks, each;        // work items of a head; heads an item takes
+    bool interleaved, inverse;
+};
+
+// cos and sin of +-position * freq. The product and its reduction to turns
+// are in 64 bits (a 32-bit product of a position near 10^5 is off by 10^-2
+// rad); the reduced angle in 32 bits is exact to 2^-25 of a turn.
+__device__ inline void turn_of(const RotaryArgs& a, int64_t at, int p, float& cs, float& sn) {
+    const int axis = (p >= a.ends[0]) + (p >= a.ends[1]) + (p >= a.ends[2]);
+    const int64_t i = axis * a.pos_axis + at;
+    double x;
+    if (a.pos_type == 0)
+        x = static_cast<const float*>(a.positions)[i];
+    else if (a.pos_type == 1)
+        x = static_cast<const double*>(a.positions)[i];
+    else
+        x = static_cast<double>(static_cast<const int64_t*>(a.positions)[i]);
+    double turns = x * static_cast<double>(a.freqs[p]) * 0.15915494309189535;
+    turns -= rint(turns);
+    sincospif(2.f * static_cast<float>(turns), &sn, &cs);
+    if (a.inverse) sn = -sn;
+}
+
+// One item: V pairs (or V values past the pairs, which are copied) of one
+// token, for `each` heads: the angles are formed once and serve them all.
+// V = 8 takes 16-byte accesses.
+template <class T, int V>
+__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, token = id / a.chunks;
+    if (token >= a.tokens) return;
+    const int chunk = static_cast<int>(id - token * a.chunks);
+    const int64_t b = token / a.rows, row = token - b * a.rows;
+    const int turned = a.pairs / V, h0 = blockIdx.y * a.each, h1 = min(h0 + a.each, a.heads[0] + a.heads[1]);
+    float cs[V], sn[V];
+    int d0, d1;   // where the item's first and second V values lie
+    const bool pairs = chunk < turned;
+    if (pairs) {
+        const int64_t at = b * a.pos_batch + row;
+#pragma unroll
+        for (int j = 0; j < V; ++j) turn_of(a, at, chunk * V + j, cs[j], sn[j]);
+        d0 = a.interleaved ? 2 * V * chunk : V * chunk;
+        d1 = a.interleaved ? d0 + V : a.pairs + d0;
+    } else {
+        d0 = 2 * a.pairs + V * (chunk - turned);
+        d1 = d0;
+    }
+    for (int hh = h0; hh < h1; ++hh) {
+        const int which = hh >= a.heads[0], head = which ? hh - a.heads[0] : hh;
+        const View &in = a.in[which], &out = a.out[which];
+        const T* x = reinterpret_cast<const T*>(in.data) + b * in.batch + row * in.row + head * in.head;
+        T* y = reinterpret_cast<T*>(out.data) + b * out.batch + row * out.row + head * out.head;
+        if constexpr (V == 8) {
+            frag<T> u = *reinterpret_cast<const frag<T>*>(x + d0), v = *reinterpret_cast<const frag<T>*>(x + d1);
+            if (pairs) {
+                float f[16], g[16];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    f[j] = static_cast<float>(u[j]);
+                    f[8 + j] = static_cast<float>(v[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float m = a.interleaved ? f[2 * j] : f[j], n = a.interleaved ? f[2 * j + 1] : f[8 + j];
+                    const float r = fmaf(m, cs[j], -n * sn[j]), s = fmaf(m, sn[j], n * cs[j]);
+                    g[j] = r;
+                    g[8 + j] = s;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    u[j] = static_cast<T>(a.interleaved ? g[(j & 1) * 8 + (j >> 1)] : g[j]);
+                    v[j] = static_cast<T>(a.interleaved ? g[(j & 1) * 8 + 4 + (j >> 1)] : g[8 + j]);
+                }
+                *reinterpret_cast<frag<T>*>(y + d1) = v;
+            }
+            *reinterpret_cast<frag<T>*>(y + d0) = u;
+        } else {
+            if (pairs) {
+                const float m = static_cast<float>(x[d0]), n = static_cast<float>(x[d1]);
+                y[d0] = static_cast<T>(fmaf(m, cs[0], -n * sn[0]));
+                y[d1] = static_cast<T>(fmaf(m, sn[0], n * cs[0]));
+            } else {
+                y[d0] = x[d0];
+            }
+        }
+    }
+}
+
+}  // namespace nsl

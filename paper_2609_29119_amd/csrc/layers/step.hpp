@@ -1,0 +1,218 @@
+// Attention of one new token a stream over its ring cache, and the cache's fill.
+//
+// The cache's valid slots are a prefix (the window's order does not matter to
+// a softmax), so a step reads slots 0 .. min(pos + 1, sinks + window) - 1.
+#pragma once
+#include "attention.hpp"
+
+namespace nsl {
+
+struct StepArgs {
+    View q, k, v, o;           // batch stride: from stream to stream
+    void *k_cache, *v_cache;   // [streams][kv_heads][slots][dim]
+    const int64_t* pos;
+    float* part;               // [streams][heads][splits][dim + 2]: sum p v, maximum, sum p
+    int64_t streams;
+    int heads, kv_heads, dim, group, head_blocks, splits;
+    int slots, sinks, window;
+    float c;
+    bool wide;
+};
+
+__device__ inline int ring_slot(int64_t t, int sinks, int window) {
+    return static_cast<int>(t < sinks ? t : sinks + (t - sinks) % window);
+}
+
+// A workgroup takes one stream, one kv head with up to 32 of its query heads
+// (the columns of S^T = K Q^T), and one of `splits` stretches of the slots;
+// its waves take every fourth tile of 32 slots. K goes from memory to
+// fragments; V goes through a stretch of LDS of the wave's own to be turned.
+template <class T, int DP>
+__global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
+    constexpr int RB = row_bytes<T, DP>(), kEach = 32 * DP / 8 / 64;
+    __shared__ __align__(128) char vt[4][32 * RB];
+    __shared__ float tops[4][32], sums[4][32];
+    __shared__ float joined[DP][33];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    const int64_t id = die_order(blockIdx.x, gridDim.x);
+    const int split = static_cast<int>(id % a.splits);
+    const int64_t rest = id / a.splits;
+    const int hb = static_cast<int>(rest % a.head_blocks);
+    const int64_t sk = rest / a.head_blocks, stream = sk / a.kv_heads;
+    const int kv = static_cast<int>(sk % a.kv_heads);
+    const int h_first = 32 * hb, h_count = min(32, a.group - h_first);
+
+    const int64_t pos = a.pos[stream];
+    const int n = pos < 0 ? 0 : static_cast<int>(pos + 1 < a.slots ? pos + 1 : a.slots);
+    const int fresh = pos < 0 ? -1 : ring_slot(pos, a.sinks, a.window);
+    const T* kn = reinterpret_cast<T*>(a.k.data) + stream * a.k.batch + kv * a.k.head;
+    const T* vn = reinterpret_cast<T*>(a.v.data) + stream * a.v.batch + kv * a.v.head;
+    T* kc = static_cast<T*>(a.k_cache) + sk * a.slots * a.dim;
+    T* vc = static_cast<T*>(a.v_cache) + sk * a.slots * a.dim;
+    const int tiles = (n + 31) / 32;
+    const int t0 = static_cast<int>(static_cast<int64_t>(tiles) * split / a.splits);
+    const int t1 = static_cast<int>(static_cast<int64_t>(tiles) * (split + 1) / a.splits);
+
+    // the new token's row is taken from the arguments, by every workgroup
+    // that needs it; only one of them writes it to the cache
+    if (hb == 0 && fresh >= 32 * t0 && fresh < 32 * t1) {
+        for (int d = tid; d < a.dim; d += 256) {
+            kc[static_cast<int64_t>(fresh) * a.dim + d] = kn[d];
+            vc[static_cast<int64_t>(fresh) * a.dim + d] = vn[d];
+        }
+    }
+    const bool mine = m < h_count;
+    const T* qp = reinterpret_cast<T*>(a.q.data) + stream * a.q.batch +
+                  static_cast<int64_t>(kv * a.group + h_first + (mine ? m : 0)) * a.q.head;
+    frag<T> qf[DP / 16], kf[DP / 16], vr[kEach];
+    load_rows<T, DP>(qf, qp, mine && n > 0, a.dim, a.wide, lane);
+    acc16 o[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = zero16();
+    float top = -INFINITY, sum = 0.f;
+
+    auto fetch = [&](int t) {
+        const int key = 32 * t + m;
+        load_rows<T, DP>(kf, key == fresh ? kn : kc + static_cast<int64_t>(key) * a.dim, key < n, a.dim, a.wide, lane);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int c = lane + 64 * e, slot = 32 * t + c / (DP / 8), d = c % (DP / 8) * 8;
+            vr[e] = load8<T>((slot == fresh ? vn : vc + static_cast<int64_t>(slot) * a.dim) + d,
+                             slot < n ? a.dim - d : 0, a.wide);
+        }
+    };
+    if (t0 + wave < t1) fetch(t0 + wave);
+    for (int t = t0 + wave; t < t1; t += 4) {
+        acc16 s = zero16();
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x) s = mma(kf[x], qf[x], s);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int c = lane + 64 * e;
+            write8<T, RB>(vt[wave], c / (DP / 8), c % (DP / 8), vr[e]);
+        }
+        if (t + 4 < t1) fetch(t + 4);
+        if (32 * t + 32 > n) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = 32 * t + 8 * (r >> 2) + 4 * h + (r & 3) < n ? s[r] : -INFINITY;
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        const float now = fmaxf(top, half_max(mx)), base = now == -INFINITY ? 0.f : now * a.c;
+        if (__any(now != top)) {
+            const float alpha = exp2_(fmaf(top, a.c, -base));
+            sum *= alpha;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
+            top = now;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = exp2_(fmaf(s[r], a.c, -base));
+            sum += s[r];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const frag<T> p = narrow<T>(s, x);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) o[d] = mma(read_turned<T, RB>(vt[wave], 16 * x, 32 * d, lane), p, o[d]);
+        }
+    }
+    // the four waves' results, in the waves' order
+    sum = half_sum(sum);
+    if (h == 0) {
+        tops[wave][m] = top;
+        sums[wave][m] = sum;
+    }
+    __syncthreads();
+    const float all = fmaxf(fmaxf(tops[0][m], tops[1][m]), fmaxf(tops[2][m], tops[3][m]));
+    const float base = all == -INFINITY ? 0.f : all * a.c, share = exp2_(fmaf(top, a.c, -base));
+    for (int v = 0; v < 4; ++v) {
+        if (wave == v) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
+                    joined[row][m] = (v ? joined[row][m] : 0.f) + o[d][r] * share;
+                }
+        }
+        __syncthreads();
+    }
+    for (int x = tid; x < h_count * a.dim; x += 256) {
+        const int hd = x / a.dim, d = x - hd * a.dim;
+        const int head = kv * a.group + h_first + hd;
+        const float am = fmaxf(fmaxf(tops[0][hd], tops[1][hd]), fmaxf(tops[2][hd], tops[3][hd]));
+        const float bm = am == -INFINITY ? 0.f : am * a.c;
+        float total = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) total += sums[v][hd] * exp2_(fmaf(tops[v][hd], a.c, -bm));
+        const float val = joined[d][hd];
+        if (a.splits == 1) {
+            reinterpret_cast<T*>(a.o.data)[stream * a.o.batch + head * a.o.head + d] =
+                static_cast<T>(total == 0.f ? 0.f : val / total);
+        } else {
+            float* p = a.part + ((stream * a.heads + head) * a.splits + split) * (a.dim + 2);
+            p[d] = val;
+            if (d == 0) {
+                p[a.dim] = am;
+                p[a.dim + 1] = total;
+            }
+        }
+    }
+}
+
+// Joins the stretches of one head of one stream.
+template <class T>
+__global__ __launch_bounds__(128) void k_step_join(StepArgs a) {
+    const int64_t sh = blockIdx.x, stream = sh / a.heads;
+    const int head = static_cast<int>(sh % a.heads), d = threadIdx.x;
+    const float* p = a.part + sh * a.splits * (a.dim + 2);
+    float top = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, p[s * (a.dim + 2) + a.dim]);
+    const float base = top == -INFINITY ? 0.f : top * a.c;
+    float total = 0.f, val = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float* x = p + s * (a.dim + 2);
+        const float w = exp2_(fmaf(x[a.dim], a.c, -base));
+        total = fmaf(x[a.dim + 1], w, total);
+        if (d < a.dim) val = fmaf(x[d], w, val);
+    }
+    if (d < a.dim)
+        reinterpret_cast<T*>(a.o.data)[stream * a.o.batch + head * a.o.head + d] =
+            static_cast<T>(total == 0.f ? 0.f : val / total);
+}
+
+struct FillArgs {
+    View k, v;
+    void *k_cache, *v_cache;
+    const int64_t* off;
+    int64_t rows;
+    int n_bands, kv_heads, dim, slots, sinks, window;
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void k_fill(FillArgs a) {
+    const int64_t stream = blockIdx.y;
+    const int64_t b = stream / a.n_bands;
+    const int band = static_cast<int>(stream % a.n_bands);
+    const int64_t start = band_bound(a.off, a.n_bands, a.rows, band + 1);
+    const int64_t last = band_bound(a.off, a.n_bands, a.rows, band + 2) - start - 1;
+    const int64_t n = static_cast<int64_t>(a.kv_heads) * a.slots * a.dim;
+    for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
+        const int d = static_cast<int>(e % a.dim), slot = static_cast<int>(e / a.dim % a.slots);
+        const int kv = static_cast<int>(e / a.dim / a.slots);
+        int64_t t = slot;
+        if (slot >= a.sinks) {   // the last token that went to this slot
+            const int64_t since = last - a.sinks - (slot - a.sinks);
+            t = since < 0 ? -1 : slot + since / a.window * a.window;
+        }
+        if (t >= 0 && t <= last) {
+            static_cast<T*>(a.k_cache)[stream * n + e] = row_of<T>(a.k, b, start + t, kv)[d];
+            static_cast<T*>(a.v_cache)[stream * n + e] = row_of<T>(a.v, b, start + t, kv)[d];
+        }
+    }
+}
+
+}  // namespace nsl

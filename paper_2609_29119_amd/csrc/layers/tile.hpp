@@ -1,0 +1,294 @@
+// Matrix fragments, LDS tiles and the search for a block's band: what the
+// layer kernels share.
+//
+// Fragments. Every product is built from 32 x 32 tiles of the matrix cores
+// with 16 reduction steps a call. A lane l = 32 h + m holds 8 consecutive
+// reduction steps (8 h .. 8 h + 7) of row m of A, or of column m of B. In 16
+// bits that is one v_mfma_f32_32x32x16; in 32 bits it is eight
+// v_mfma_f32_32x32x2, call j taking step j of either half: the order in which
+// a reduction's steps are taken is free as long as A and B agree. So one code
+// serves all three types. The result's register r of lane l is element
+// (row 8 (r / 4) + 4 h + r % 4, column m).
+//
+// Chains without a trip through LDS. With the scores formed as S^T = K Q^T
+// (row: key, column: query), registers 8 s .. 8 s + 7 of a lane hold keys
+// 16 s + 4 h + {0..3} and 16 s + 8 + 4 h + {0..3} of its query. Taken as they
+// are, they are a B fragment of the next product's 16 steps, if its A
+// fragment takes its steps in that same order (`read_turned`).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace nsl {
+
+typedef float acc16 __attribute__((ext_vector_type(16)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef short s8 __attribute__((ext_vector_type(8)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Type;
+template <> struct Type<float> { typedef f8 v8; typedef f4 v4; };
+template <> struct Type<_Float16> { typedef h8 v8; typedef h4 v4; };
+template <> struct Type<__bf16> { typedef b8 v8; typedef b4 v4; };
+template <class T> using frag = typename Type<T>::v8;
+template <class T> using quad = typename Type<T>::v4;
+
+__device__ inline acc16 mma(h8 a, h8 b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ inline acc16 mma(b8 a, b8 b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline acc16 mma(f8 a, f8 b, acc16 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+template <class T> __device__ inline frag<T> zero8() {
+    frag<T> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = static_cast<T>(0.f);
+    return f;
+}
+
+__device__ inline acc16 zero16() {
+    acc16 c;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) c[r] = 0.f;
+    return c;
+}
+
+// Registers 8 s .. 8 s + 7 of c, rounded to T: the next product's B fragment.
+template <class T> __device__ inline frag<T> narrow(const acc16& c, int s) {
+    frag<T> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = static_cast<T>(c[8 * s + j]);
+    return f;
+}
+
+// 8 values at p, of which the first n are there (n may be <= 0 or past 8).
+// wide: p is 16-byte aligned and n is never between 0 and 8.
+template <class T> __device__ inline frag<T> load8(const T* p, int n, bool wide) {
+    frag<T> f = zero8<T>();
+    if (wide) {
+        if (n > 0) f = *reinterpret_cast<const frag<T>*>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) f[j] = p[j];
+    }
+    return f;
+}
+
+// The values of lane l % 32 and lane l % 32 + 32, in every lane.
+__device__ inline void halves(float x, float& low, float& high) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const u2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];   // (a bit cast of a vector's element reads element 0)
+    low = __builtin_bit_cast(float, a);
+    high = __builtin_bit_cast(float, b);
+}
+__device__ inline float half_max(float x) {
+    float a, b;
+    halves(x, a, b);
+    return fmaxf(a, b);
+}
+__device__ inline float half_sum(float x) {
+    float a, b;
+    halves(x, a, b);
+    return a + b;
+}
+
+// ------------------------------------------------------------------ LDS tiles
+
+// A tile's row takes 128 bytes or a multiple; its 16-byte chunks lie at
+// chunk ^ turn(row). Both ways of reading are then free of bank conflicts:
+// `read8` (eight lanes on eight consecutive rows, one chunk: eight different
+// turns) and the transposed read (16 lanes on four rows, two chunks: the
+// turns of four rows differ in their upper two bits).
+template <class T, int D> constexpr int row_bytes() { return (D * static_cast<int>(sizeof(T)) + 127) / 128 * 128; }
+__device__ inline int turn(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+// Columns 8 c8 .. 8 c8 + 7 of `row`.
+template <class T, int RB> __device__ inline frag<T> read8(const char* tile, int row, int c8) {
+    const char* r = tile + row * RB;
+    const int t = turn(row);
+    if constexpr (sizeof(T) == 2) {
+        return *reinterpret_cast<const frag<T>*>(r + ((c8 ^ t) << 4));
+    } else {
+        const f4 a = *reinterpret_cast<const f4*>(r + (((2 * c8) ^ t) << 4));
+        const f4 b = *reinterpret_cast<const f4*>(r + (((2 * c8 + 1) ^ t) << 4));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+template <class T, int RB> __device__ inline void write8(char* tile, int row, int c8, frag<T> f) {
+    char* r = tile + row * RB;
+    const int t = turn(row);
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<frag<T>*>(r + ((c8 ^ t) << 4)) = f;
+    } else {
+        *reinterpret_cast<f4*>(r + (((2 * c8) ^ t) << 4)) = __builtin_shufflevector(f, f, 0, 1, 2, 3);
+        *reinterpret_cast<f4*>(r + (((2 * c8 + 1) ^ t) << 4)) = __builtin_shufflevector(f, f, 4, 5, 6, 7);
+    }
+}
+
+typedef __attribute__((address_space(3))) s4 lds_s4;
+
+// A fragment of the tile's transpose: for column col0 + (lane % 32), rows
+// row0 + 4 h + {0..3} and row0 + 8 + 4 h + {0..3}, h = lane / 32 (row0 and
+// col0 multiples of 16 and 32). In 16 bits ds_read_b64_tr_b16 turns 4 x 16
+// blocks on the way out of LDS.
+template <class T, int RB> __device__ inline frag<T> read_turned(const char* tile, int row0, int col0, int lane) {
+    const int h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        const int l16 = lane & 15, row = row0 + 4 * h + (l16 >> 2);
+        const int c = ((col0 + (lane & 16)) >> 3) + ((l16 & 3) >> 1);
+        const char* a = tile + row * RB + ((c ^ turn(row)) << 4) + ((l16 & 1) << 3);
+        const char* b = tile + (row + 8) * RB + ((c ^ turn(row + 8)) << 4) + ((l16 & 1) << 3);
+        const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)a);
+        const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)b);
+        const s8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(frag<T>, z);
+    } else {
+        const int col = col0 + (lane & 31);
+        frag<T> f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = row0 + 4 * h + (j & 3) + 8 * (j >> 2);
+            f[j] = *reinterpret_cast<const T*>(tile + row * RB + (((col >> 2) ^ turn(row)) << 4) + ((col & 3) << 2));
+        }
+        return f;
+    }
+}
+
+// As read_turned, with rows row0 + 8 h + {0..7}: the order in which `load8`
+// and `read8` hold a reduction's steps.
+template <class T, int RB> __device__ inline frag<T> read_turned8(const char* tile, int row0, int col0, int lane) {
+    const int h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        const int l16 = lane & 15, row = row0 + 8 * h + (l16 >> 2);
+        const int c = ((col0 + (lane & 16)) >> 3) + ((l16 & 3) >> 1);
+        const char* a = tile + row * RB + ((c ^ turn(row)) << 4) + ((l16 & 1) << 3);
+        const char* b = tile + (row + 4) * RB + ((c ^ turn(row + 4)) << 4) + ((l16 & 1) << 3);
+        const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)a);
+        const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)b);
+        const s8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(frag<T>, z);
+    } else {
+        const int col = col0 + (lane & 31);
+        frag<T> f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = row0 + 8 * h + j;
+            f[j] = *reinterpret_cast<const T*>(tile + row * RB + (((col >> 2) ^ turn(row)) << 4) + ((col & 3) << 2));
+        }
+        return f;
+    }
+}
+
+// ---------------------------------------------------------------------- stores
+
+// Stores rows 0 .. 31 of a result tile, held as registers of column m = one
+// token: element d0 + row of the token's row p (NULL: nothing), d below n.
+// wide: 16-byte aligned rows and n a multiple of 8. In 16 bits the halves of
+// the wave exchange quads, so that each lane stores 8 consecutive values.
+template <class T> __device__ inline void store_column(T* p, const acc16& c, int d0, int n, bool wide, int lane) {
+    const int h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        if (wide) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const frag<T> f = narrow<T>(c, s);
+                const u4 u = __builtin_bit_cast(u4, f);
+                const u2 x = __builtin_amdgcn_permlane32_swap(u[0], u[2], false, false);
+                const u2 y = __builtin_amdgcn_permlane32_swap(u[1], u[3], false, false);
+                const u4 out = {x[0], y[0], x[1], y[1]};
+                const int d = d0 + 16 * s + 8 * h;
+                if (p && d < n) *reinterpret_cast<u4*>(p + d) = out;
+            }
+            return;
+        }
+    } else {
+        if (wide) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int d = d0 + 8 * q + 4 * h;
+                const f4 v = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+                if (p && d < n) *reinterpret_cast<f4*>(p + d) = v;
+            }
+            return;
+        }
+    }
+    if (p) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int d = d0 + 8 * (r >> 2) + 4 * h + (r & 3);
+            if (d < n) p[d] = static_cast<T>(c[r]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- work items
+
+// Which of n work items block `id` takes: blocks go to the 8 compute dies in
+// turn, so each die gets one contiguous stretch and neighbours share its L2.
+__device__ inline int64_t die_order(int64_t id, int64_t n) {
+    const int64_t q = n >> 3, r = n & 7, x = id & 7;
+    return x * q + (x < r ? x : r) + (id >> 3);
+}
+
+struct Tile {
+    int band;        // -1: tokens before the first band, n_bands: after the last
+    int64_t start;   // the band's first token
+    int64_t len;     // and its number of tokens
+    int64_t first;   // the tile's first row of the band's mult * len rows
+    bool live;       // false: nothing to do
+};
+
+// Tiles of 2^SHIFT rows of the bands' mult * len rows each, without a table:
+// band i's tiles begin at item floor(mult start_i / 2^SHIFT) + i, which
+// leaves room for each band's ragged last tile, so tile_count() items hold
+// them all and some items are empty. The band of item p is found by a search
+// over the offsets, 64 at a time: one or two rounds of loads.
+template <int SHIFT> __host__ __device__ inline int64_t tile_count(int64_t n_bands, int64_t mult, int64_t rows) {
+    return ((mult * rows) >> SHIFT) + n_bands + 2;
+}
+
+__device__ inline int64_t band_bound(const int64_t* off, int n_bands, int64_t rows, int i) {
+    if (i <= 0) return 0;
+    if (i >= n_bands + 2) return rows;
+    const int64_t o = off[i - 1];
+    return o < 0 ? 0 : o > rows ? rows : o;
+}
+
+template <int SHIFT>
+__device__ inline Tile find_tile(const int64_t* off, int n_bands, int64_t rows, int64_t mult, int64_t p, int lane) {
+    int lo = 0, hi = n_bands + 2;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+        const bool below = i < hi && ((mult * band_bound(off, n_bands, rows, i)) >> SHIFT) + i <= p;
+        const int count = __popcll(__ballot(below));
+        lo += (count > 1 ? count - 1 : 0) * step;
+        hi = lo + step < hi ? lo + step : hi;
+    }
+    Tile t;
+    const int64_t a = band_bound(off, n_bands, rows, lo), b = band_bound(off, n_bands, rows, lo + 1);
+    t.band = lo - 1;
+    t.start = a;
+    t.len = b > a ? b - a : 0;
+    t.first = (p - (((mult * a) >> SHIFT) + lo)) << SHIFT;
+    t.live = t.first >= 0 && t.first < mult * t.len;
+    return t;
+}
+
+struct View {
+    char* data;
+    int64_t batch, row, head;   // strides in elements
+};
+
+}  // namespace nsl

@@ -212,6 +212,12 @@ class Plan:
     def bands(self):
         return [self.band(i) for i in range(self.n_bands)]
 
+    def band_offsets(self, device="cuda"):
+        """First coefficient of each band and, last, C: int64 [n_bands + 1],
+        the offsets of the layers (layers.py)."""
+        import torch
+        return torch.tensor([b.offset for b in self.bands()] + [self.n_coeffs], dtype=torch.int64, device=device)
+
     def weights(self, which):
         import numpy as np
         out = np.empty(self.n_coeffs, dtype=np.float32)

@@ -1,0 +1,564 @@
+"""GPU tests of the layers on the band layout against plain fp64 forms.
+
+Bounds. u is the unit roundoff of the data's type (2^-24, 2^-11, 2^-8). A
+product with 32-bit sums is off by its one rounding, u in the 2-norm, and by
+the sums' own 2^-24 sqrt(K) or so. A rotation adds one rounded multiply-add.
+Attention rounds the probabilities (u) and the result (u); in 32 bits the
+scores' error, 2^-24 times |q| |k| and the growth of the sum (below 64 for
+D <= 128), passes through the exponential. Gradients chain three rounded
+factors (probabilities, their gradients, the forward result in delta) before
+their own rounding. The bounds below are those counts with a factor of two.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2609_29119_amd as nc  # noqa: E402
+from paper_2609_29119_amd import layers  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    nc.lib()
+
+
+def product_bound(dtype, k):
+    return 2 * (U[dtype] + 2.0 ** -24 * max(k, 1) ** 0.5)
+
+
+def attention_bound(dtype, grad=False):
+    return 2 * ((4 if grad else 2) * U[dtype] + 64 * 2.0 ** -24)
+
+
+def close(got, ref, bound, what, size=None):
+    """2-norm within the bound, and each value within 8 bounds of the larger of itself and the root mean square
+    (rounding errors of single values, each a sum of many, stay within 8 standard deviations). `size`: the result
+    with every term's magnitude in the place of its value; 2^-22 of it is what 32-bit sums leave where terms cancel."""
+    got, ref = got.detach().double().cpu(), ref.detach().double().cpu()
+    assert got.shape == ref.shape, what
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    if ref.numel() == 0:
+        return
+    norm = ref.norm().item()
+    err = (got - ref).norm().item()
+    noise = 0.0 if size is None else 2.0 ** -22 * size.norm().item()
+    assert err <= bound * norm + noise + 1e-30, f"{what}: {err / max(norm, 1e-300):.3g} over {bound:.3g}"
+    rms = norm / ref.numel() ** 0.5
+    worst = (((got - ref).abs() - 8 * noise).clamp(min=0) / ref.abs().clamp(min=rms + 1e-30)).max().item()
+    assert worst <= 8 * bound, f"{what}: a value is off by {worst:.3g}"
+
+
+def offsets_of(lengths, first=0):
+    return torch.tensor(np.concatenate([[first], first + np.cumsum(lengths)]).astype(np.int64), device="cuda")
+
+
+def randn(seed, *shape, dtype=torch.float32, by=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g, dtype=torch.float64) * by).to(dtype).cuda()
+
+
+# ------------------------------------------------------------------ band_linear
+
+LINEAR = [
+    # lengths, batch, n_in, n_out, bias
+    ([1], 1, 1, 1, True),
+    ([5, 0, 3], 2, 2, 32, True),
+    ([130, 1, 257], 3, 8, 8, False),
+    ([64, 200], 1, 33, 77, True),
+    ([300, 7, 0, 0, 129], 2, 128, 128, True),
+    ([150], 2, 72, 200, True),
+    ([40, 90], 1, 200, 40, False),
+    ([31, 33], 2, 257, 65, True),
+    ([1500, 600], 3, 24, 16, True),       # several chunks of the weights' gradient
+    ([3] * 150 + [0, 1], 1, 16, 24, True),  # more bands than one round of the search
+    ([0, 0], 2, 4, 4, True),
+    ([12], 1, 0, 8, True),                # nothing but the bias
+    ([12, 4], 1, 8, 0, False),
+]
+
+
+def linear_reference(x, w, b, lengths, first, dy):
+    x, w = x.detach().double().cpu(), w.detach().double().cpu()
+    dy = dy.double().cpu()
+    y = torch.zeros(*x.shape[:2], w.shape[1], dtype=torch.float64)
+    dx, dw = torch.zeros_like(x), torch.zeros_like(w)
+    db = torch.zeros(w.shape[:2], dtype=torch.float64)
+    at = first
+    for g, n in enumerate(lengths):
+        s = slice(at, at + n)
+        y[:, s] = x[:, s] @ w[g].T + (b[g].detach().double().cpu() if b is not None else 0)
+        dx[:, s] = dy[:, s] @ w[g]
+        dw[g] = torch.einsum("bro,bri->oi", dy[:, s], x[:, s])
+        db[g] = dy[:, s].sum((0, 1))
+        at += n
+    return y, dx, dw, db
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(LINEAR)))
+def test_band_linear(case, dtype):
+    lengths, batch, n_in, n_out, bias = LINEAR[case]
+    rows, G = sum(lengths), len(lengths)
+    x = randn(case, batch, rows, n_in, dtype=dtype).requires_grad_()
+    w = randn(case + 50, G, n_out, n_in, dtype=dtype, by=max(n_in, 1) ** -0.5).requires_grad_()
+    b = randn(case + 90, G, n_out, dtype=dtype).requires_grad_() if bias else None
+    dy = randn(case + 70, batch, rows, n_out, dtype=dtype)
+    y = layers.band_linear(x, w, offsets_of(lengths), b)
+    grads = torch.autograd.grad(y, [x, w] + ([b] if bias else []), dy)
+    ry, rdx, rdw, rdb = linear_reference(x, w, b, lengths, 0, dy)
+    close(y, ry, product_bound(dtype, n_in), "y")
+    close(grads[0], rdx, product_bound(dtype, n_out), "dx")
+    close(grads[1], rdw, product_bound(dtype, rows * batch), "dw")
+    if bias:
+        close(grads[2], rdb, product_bound(dtype, rows * batch), "db")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_band_linear_strides_and_uncovered_tokens(dtype):
+    """Rows and batches with strides, a base off by one element, tokens before
+    the first band and after the last: zeros there, in the gradient too."""
+    lengths, first, rows, batch, n_in, n_out = [17, 150], 9, 190, 2, 48, 40
+    big = randn(3, batch, rows + 3, 2 * n_in + 1, dtype=dtype)
+    for lo in (0, 1):
+        x = big[:, 1:rows + 1, lo:lo + n_in].detach().requires_grad_()
+        w = randn(4, 2, n_out, n_in, dtype=dtype).requires_grad_()
+        dy = randn(5, rows, batch, n_out, dtype=dtype).transpose(0, 1)
+        off = offsets_of(lengths, first)
+        y = layers.band_linear(x, w, off)
+        dx, dw = torch.autograd.grad(y, [x, w], dy)
+        ry, rdx, rdw, _ = linear_reference(x, w, None, lengths, first, dy)
+        close(y, ry, product_bound(dtype, n_in), "y")
+        close(dx, rdx, product_bound(dtype, n_out), "dx")
+        close(dw, rdw, product_bound(dtype, rows * batch), "dw")
+        assert y[:, :first].abs().max() == 0 and y[:, first + 167:].abs().max() == 0
+        assert dx[:, :first].abs().max() == 0 and dx[:, first + 167:].abs().max() == 0
+
+
+def test_band_linear_matches_plan_layout():
+    """The transform's own coefficients through a product and back: one matrix a band."""
+    plan = nc.Plan(22050.0, 110.0, 11025.0, 12, 16384, batch=2)
+    c = plan.analyse(randn(1, 2, 16384))
+    x = torch.view_as_real(c)
+    off = plan.band_offsets()
+    assert off.tolist() == [b.offset for b in plan.bands()] + [plan.n_coeffs]
+    w = randn(2, plan.n_bands, 6, 2)
+    y = layers.band_linear(x, w, off)
+    ref, _, _, _ = linear_reference(x, w, None, [b.length for b in plan.bands()], 0, y)
+    close(y, ref, product_bound(torch.float32, 2), "y")
+
+
+# ----------------------------------------------------------------------- rotary
+
+
+def rotary_reference(x, positions, freqs, sections, interleaved, sign=1.0):
+    x = x.detach().double().cpu()
+    pos, freqs = positions.double().cpu(), freqs.double().cpu()
+    if pos.dim() == 2:
+        pos = pos[:, None].expand(-1, x.shape[0], -1)
+    y, P, p = x.clone(), sum(sections), 0
+    for axis, n in enumerate(sections):
+        for _ in range(n):
+            t = pos[axis] * freqs[p] * sign
+            c, s = t.cos()[:, :, None], t.sin()[:, :, None]
+            i, j = (2 * p, 2 * p + 1) if interleaved else (p, p + P)
+            y[..., i], y[..., j] = x[..., i] * c - x[..., j] * s, x[..., i] * s + x[..., j] * c
+            p += 1
+    return y
+
+
+ROTARY = [
+    # batch, rows, heads, kv_heads, dim, sections, interleaved, positions per signal, type of positions
+    (1, 1, 1, 1, 2, [1], False, False, torch.int64),
+    (2, 37, 8, 2, 64, [16, 16], False, False, torch.float64),
+    (2, 37, 8, 2, 64, [16, 16], True, True, torch.float32),
+    (3, 20, 3, 1, 80, [8, 8, 16], True, False, torch.float64),
+    (1, 300, 2, 2, 128, [5, 20, 3, 4], False, True, torch.int64),
+    (2, 19, 5, 3, 7, [1, 0, 2], False, False, torch.float32),
+    (2, 19, 5, 0, 9, [2, 2], True, False, torch.float64),
+    (1, 2000, 4, 4, 32, [16], False, False, torch.int64),
+    (1, 9, 2, 1, 16, [0], False, False, torch.float64),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(ROTARY)))
+def test_rotary(case, dtype):
+    batch, rows, h, hk, d, sections, inter, per_signal, kind = ROTARY[case]
+    both = randn(case, batch, rows, h + hk, d + 8, dtype=dtype)
+    q = both[:, :, :h, :d].detach().requires_grad_()
+    k = both[:, :, h:, :d].detach().requires_grad_() if hk else None
+    shape = (len(sections),) + ((batch,) if per_signal else ()) + (rows,)
+    g = torch.Generator().manual_seed(case)
+    pos = (torch.rand(shape, generator=g, dtype=torch.float64) * 2e6 - 1e6).to(kind).cuda()
+    freqs = layers.rotary_frequencies(sections)
+    got = layers.rotary(q, k, pos, freqs, sections, inter)
+    dq, dk = randn(case + 9, batch, rows, h, d, dtype=dtype), randn(case + 8, batch, rows, max(hk, 1), d, dtype=dtype)
+    # one rounded multiply-add on top of the result's rounding; angles exact to 2^-24 of a turn
+    bound = 2 * (U[dtype] + 2.0 ** -22)
+    if hk:
+        close(got[0], rotary_reference(q, pos, freqs, sections, inter), bound, "q")
+        close(got[1], rotary_reference(k, pos, freqs, sections, inter), bound, "k")
+        gq, gk = torch.autograd.grad(got, [q, k], [dq, dk])
+        close(gk, rotary_reference(dk, pos, freqs, sections, inter, -1.0), bound, "dk")
+    else:
+        close(got, rotary_reference(q, pos, freqs, sections, inter), bound, "q")
+        (gq,) = torch.autograd.grad(got, [q], dq)
+    close(gq, rotary_reference(dq, pos, freqs, sections, inter, -1.0), bound, "dq")
+    rest = 2 * sum(sections)
+    q_out = got[0] if hk else got
+    assert torch.equal(q_out[..., rest:], q[..., rest:])
+
+
+# --------------------------------------------------------------- band_attention
+
+
+def visible(n, left, right, sinks, keep):
+    i, j = torch.arange(n)[:, None], torch.arange(n)[None]
+    see = (j <= i + right) & ((j >= i - left) | (j < sinks))
+    return see if keep is None else see & keep[None]
+
+
+def attention_reference(q, k, v, lengths, first, left, right, sinks, scale, keep, do):
+    """Dense, in 64 bits, the gradients from the formulas; what is not seen is never used."""
+    q, k, v, do = (t.detach().double().cpu() for t in (q, k, v, do))
+    h, hk = q.shape[2], k.shape[2]
+    o, dq, dk, dv = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    sq, sk = torch.zeros_like(q), torch.zeros_like(k)     # sizes of dq and dk's terms
+    big = 1 << 40
+    for b in range(q.shape[0]):
+        at = first
+        for n in lengths:
+            s = slice(at, at + n)
+            kp = None if keep is None else keep[b, s].cpu()
+            see = visible(n, big if left is None else left, big if right is None else right, sinks, kp)
+            for a in range(h if n else 0):
+                c = a // (h // hk)
+                kk, vv = k[b, s, c], v[b, s, c]
+                if kp is not None:
+                    kk, vv = torch.where(kp[:, None], kk, 0.0), torch.where(kp[:, None], vv, 0.0)
+                p = (q[b, s, a] @ kk.T * scale).masked_fill(~see, float("-inf")).softmax(-1)
+                p = torch.where(see.any(-1)[:, None], p, 0.0)
+                o[b, s, a] = p @ vv
+                dp = do[b, s, a] @ vv.T
+                ds = p * (dp - (do[b, s, a] * o[b, s, a]).sum(-1, keepdim=True)) * scale
+                dq[b, s, a] = ds @ kk
+                dk[b, s, c] += ds.T @ q[b, s, a]
+                dv[b, s, c] += p.T @ do[b, s, a]
+                size = p * (do[b, s, a].abs() @ vv.abs().T + (do[b, s, a] * o[b, s, a]).abs().sum(-1, keepdim=True)) * scale
+                sq[b, s, a] = size @ kk.abs()
+                sk[b, s, c] += size.T @ q[b, s, a].abs()
+            at += n
+    return o, dq, dk, dv, sq, sk
+
+
+ATTENTION = [
+    # lengths, batch, heads, kv_heads, dim, left, right, sinks
+    ([1], 1, 1, 1, 1, 0, 0, 0),
+    ([1, 2, 3], 2, 2, 1, 8, 1, 0, 1),
+    ([70, 0, 33], 1, 4, 2, 32, 16, 0, 0),
+    ([300], 1, 2, 2, 64, 63, 0, 4),
+    ([129, 257], 2, 4, 1, 64, 40, 25, 3),
+    ([500, 5], 1, 3, 3, 40, 7, 0, 40),       # the sinks pass one tile
+    ([400], 1, 2, 1, 128, None, 0, 0),       # causal
+    ([150, 31], 1, 2, 1, 96, None, None, 0),  # every token sees every token
+    ([260], 1, 2, 2, 17, 100, 3, 2),
+    ([640], 1, 2, 1, 32, 0, 0, 2),           # itself and the sinks
+    ([2700], 1, 2, 1, 16, 30, 0, 5),         # several chunks of far queries
+    ([900], 1, 1, 1, 24, 10, 0, 200),        # sinks over two key tiles
+    ([3] * 140, 1, 2, 2, 16, 5, 0, 1),
+]
+
+
+def attention_inputs(case, dtype):
+    lengths, batch, h, hk, d, left, right, sinks = ATTENTION[case]
+    rows = sum(lengths)
+    qkv = randn(case, batch, rows, h + 2 * hk, d, dtype=dtype)
+    q, k, v = (t.detach().requires_grad_() for t in (qkv[:, :, :h], qkv[:, :, h:h + hk], qkv[:, :, h + hk:]))
+    return q, k, v, randn(case + 30, batch, rows, h, d, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("case", range(len(ATTENTION)))
+def test_band_attention(case, masked, dtype):
+    lengths, batch, h, hk, d, left, right, sinks = ATTENTION[case]
+    q, k, v, do = attention_inputs(case, dtype)
+    keep = None
+    if masked:
+        g = torch.Generator().manual_seed(case)
+        keep = torch.rand(batch, sum(lengths), generator=g) > 0.3
+        keep[:, : sum(lengths) // 3] = False    # whole windows, and the sinks, without a kept token
+        keep = keep.cuda()
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, right, sinks, keep=keep)
+    dq, dk, dv = torch.autograd.grad(o, [q, k, v], do)
+    ref = attention_reference(q, k, v, lengths, 0, left, right, sinks, d ** -0.5, keep, do)
+    close(o, ref[0], attention_bound(dtype), "o")
+    for got, r, name, size in zip((dq, dk, dv), ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+        close(got, r, attention_bound(dtype, True), name, size)
+    if masked:
+        assert not dk[~keep].any() and not dv[~keep].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_band_attention_never_uses_what_is_not_kept(dtype):
+    lengths = [200, 90]
+    q, k, v, do = (randn(i, 2, 290, n, 32, dtype=dtype) for i, n in ((1, 4), (2, 2), (3, 2), (4, 4)))
+    keep = torch.rand(2, 290, generator=torch.Generator().manual_seed(0)) > 0.4
+    keep[:, 100:200] = False
+    keep = keep.cuda()
+    want = layers.band_attention(q, k, v, offsets_of(lengths), 30, 5, 3, keep=keep)
+    for bad in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).min):
+        k2, v2 = (torch.where(keep[..., None, None], t, bad).to(dtype).requires_grad_() for t in (k, v))
+        q2 = q.detach().requires_grad_()
+        o = layers.band_attention(q2, k2, v2, offsets_of(lengths), 30, 5, 3, keep=keep)
+        assert torch.equal(o, want)
+        for g in torch.autograd.grad(o, [q2, k2, v2], do):
+            assert torch.isfinite(g).all()
+    # no kept token at all: zeros, and no gradient
+    none = torch.zeros_like(keep)
+    q2 = q.detach().requires_grad_()
+    o = layers.band_attention(q2, k, v, offsets_of(lengths), 30, 5, 3, keep=none)
+    (dq,) = torch.autograd.grad(o, [q2], do)
+    assert o.abs().max() == 0 and dq.abs().max() == 0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_band_attention_strides_scale_and_uncovered_tokens(dtype):
+    lengths, first, rows, d = [50, 140], 7, 200, 20
+    off = offsets_of(lengths, first)
+    base = randn(1, 3, rows + 1, 6, d + 1, dtype=dtype)
+    q = base[::2, 1:, 1:5, 1:].detach().requires_grad_()        # odd strides, a base off by one
+    k = randn(2, rows, 2, 2, d, dtype=dtype).transpose(0, 1).detach().requires_grad_()
+    v = randn(3, 2, 2, rows, d, dtype=dtype).transpose(1, 2).detach().requires_grad_()
+    do = randn(4, 2, 4, rows, d, dtype=dtype).transpose(1, 2)
+    o = layers.band_attention(q, k, v, off, 25, 10, 2, scale=0.4)
+    grads = torch.autograd.grad(o, [q, k, v], do)
+    ref = attention_reference(q, k, v, lengths, first, 25, 10, 2, 0.4, None, do)
+    close(o, ref[0], attention_bound(dtype), "o")
+    for got, r, name, size in zip(grads, ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+        close(got, r, attention_bound(dtype, True), name, size)
+    for t in (o,) + grads:
+        assert t[:, :first].abs().max() == 0 and t[:, first + 190:].abs().max() == 0
+
+
+def test_gradients_against_differences():
+    """Directional central differences of a scalar loss in 32 bits: truncation
+    is of the order of h^2 = 1e-4, cancellation 2^-24 / h = 6e-6 of the loss' terms."""
+    lengths, off = [90, 40], offsets_of([90, 40])
+    q, k, v, do = (randn(i, 1, 130, n, 16).requires_grad_(i < 4) for i, n in ((1, 4), (2, 2), (3, 2), (4, 4)))
+    x = randn(6, 1, 130, 12).requires_grad_()
+    w = randn(7, 2, 64, 12, by=0.3).requires_grad_()
+    pos = torch.arange(130, dtype=torch.float64, device="cuda")[None]
+    freqs = layers.rotary_frequencies([8])
+
+    def loss(q, k, v, x, w):
+        a, b = layers.rotary(q + layers.band_linear(x, w, off).view(1, 130, 4, 16), k, pos, freqs, [8])
+        return (layers.band_attention(a, b, v, off, 20, 4, 2).double() * do.double()).sum()
+
+    args = [q, k, v, x, w]
+    grads = torch.autograd.grad(loss(*args), args)
+    h = 1e-2
+    for n, (t, g) in enumerate(zip(args, grads)):
+        u = randn(20 + n, *t.shape)
+        u /= u.norm() / t.numel() ** 0.25
+        with torch.no_grad():
+            hi, lo = (loss(*[a + s * h * u if m == n else a for m, a in enumerate(args)]) for s in (1, -1))
+        want = ((hi - lo) / (2 * h)).item()
+        have = (g.double() * u.double()).sum().item()
+        assert abs(have - want) <= 5e-3 * (g.norm() * u.norm()).item() / t.numel() ** 0.5 * 8 + 2e-3 * abs(want), n
+
+
+def test_results_do_not_vary():
+    lengths = [1000, 70, 300]
+    off = offsets_of(lengths)
+    q, k, v, do = (randn(i, 2, 1370, n, 64, dtype=torch.bfloat16).requires_grad_(i < 4)
+                   for i, n in ((1, 4), (2, 1), (3, 1), (4, 4)))
+    x = randn(5, 2, 1370, 64, dtype=torch.bfloat16).requires_grad_()
+    w = randn(6, 3, 32, 64, dtype=torch.bfloat16).requires_grad_()
+
+    def once():
+        o = layers.band_attention(q, k, v, off, 100, 0, 4)
+        y = layers.band_linear(x, w, off)
+        return [o, y, *torch.autograd.grad(o, [q, k, v], do), *torch.autograd.grad(y, [x, w], torch.ones_like(y))]
+
+    first = once()
+    for _ in range(3):
+        for a, b in zip(first, once()):
+            assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------- single-token step
+
+
+def step_reference(q, ks, vs, upto, sinks, window, scale):
+    """One stream: q [heads][D] over its first `upto` tokens."""
+    see = torch.tensor([t for t in range(upto) if t < sinks or t >= max(sinks, upto - window)])
+    h, hk = q.shape[0], ks.shape[1]
+    out = torch.zeros(q.shape, dtype=torch.float64)
+    for a in range(h):
+        c = a // (h // hk)
+        p = (ks[see, c].double() @ q[a].double() * scale).softmax(-1)
+        out[a] = p @ vs[see, c].double()
+    return out
+
+
+STEP = [
+    # streams, heads, kv_heads, dim, window, sinks, tokens
+    (1, 1, 1, 1, 1, 0, 3),
+    (3, 4, 2, 64, 5, 2, 14),
+    (2, 8, 1, 32, 40, 0, 50),
+    (5, 3, 3, 40, 33, 31, 70),
+    (2, 2, 1, 128, 16, 4, 25),
+    (2, 6, 2, 7, 9, 1, 20),
+    (1, 40, 1, 16, 20, 3, 26),     # more than 32 query heads of one key head
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(STEP)))
+def test_attention_step_from_the_first_token(case, dtype):
+    n, h, hk, d, window, sinks, tokens = STEP[case]
+    cache = layers.StreamCache(n, hk, d, window, sinks, dtype=dtype)
+    cache.k.fill_(float("nan"))      # what no token has been written to is never used
+    cache.v.fill_(float("nan"))
+    qkv = randn(case, tokens, n, h + 2 * hk, d, dtype=dtype)
+    ref = qkv.cpu()
+    for t in range(tokens):
+        o = cache.step(qkv[t][:, :h], qkv[t][:, h:h + hk], qkv[t][:, h + hk:])
+        want = torch.stack([step_reference(ref[t, s, :h], ref[:, s, h:h + hk], ref[:, s, h + hk:], t + 1, sinks, window,
+                                           d ** -0.5) for s in range(n)])
+        close(o, want, attention_bound(dtype), f"token {t}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_step_continues_what_attention_began(dtype):
+    """Caches filled from whole bands, then steps: the same rows as the attention over the longer bands."""
+    lengths, more, left, sinks = [37, 0, 3, 90], 6, 20, 3
+    h, hk, d, batch = 4, 2, 32, 2
+    full = [n + more for n in lengths]
+    qkv = randn(1, batch, sum(full), h + 2 * hk, d, dtype=dtype)
+    q, k, v = qkv[:, :, :h], qkv[:, :, h:h + hk], qkv[:, :, h + hk:]
+    whole = layers.band_attention(q, k, v, offsets_of(full), left, 0, sinks)
+    ends = np.cumsum(full)
+    head = torch.cat([torch.arange(e - n - more, e - more) for e, n in zip(ends, lengths)]).cuda()
+    cache = layers.StreamCache(batch * len(lengths), hk, d, left + 1, sinks, dtype=dtype)
+    cache.fill(k[:, head], v[:, head], offsets_of(lengths))
+    assert cache.pos.tolist() == lengths * batch
+    for t in range(more):
+        at = torch.tensor([e - more + t for e in ends]).cuda()
+        o = cache.step(*(x[:, at].reshape(batch * len(lengths), -1, d) for x in (q, k, v)))
+        close(o.view(batch, len(lengths), h, d), whole[:, at].double(), 2 * attention_bound(dtype), f"token {t}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("slots,d", [(5000, 64), (1301, 40), (3000, 128)])
+def test_attention_step_split_caches(slots, d, dtype):
+    """Long caches (split and joined), streams of every age, one without a token; only its slot is written."""
+    n, h, hk, sinks = 4, 4, 2, 4
+    window = slots - sinks
+    kc, vc = randn(1, n, hk, slots, d, dtype=dtype), randn(2, n, hk, slots, d, dtype=dtype)
+    q, k, v = randn(3, n, h, d, dtype=dtype), randn(4, n, hk, d, dtype=dtype), randn(5, n, hk, d, dtype=dtype)
+    pos = torch.tensor([0, 700, -1, 3 * slots + 11], device="cuda")
+    k0, v0 = kc.clone(), vc.clone()
+    o = layers.attention_step(q, k, v, kc, vc, pos, sinks)
+    for s, p in enumerate(pos.tolist()):
+        if p >= 0:
+            at = p if p < sinks else sinks + (p - sinks) % window
+            k0[s, :, at], v0[s, :, at] = k[s], v[s]
+            seen = min(p + 1, slots)
+            want = step_reference(q[s].cpu(), k0[s, :, :seen].transpose(0, 1).cpu(),
+                                  v0[s, :, :seen].transpose(0, 1).cpu(), seen, seen, 1, d ** -0.5)
+            close(o[s], want, attention_bound(dtype), f"stream {s}")
+        else:
+            assert o[s].abs().max() == 0
+    assert torch.equal(kc, k0) and torch.equal(vc, v0)
+
+
+def test_step_in_a_graph_and_on_another_stream():
+    n, h, hk, d, window, sinks = 8, 8, 2, 64, 2000, 4
+    cache = layers.StreamCache(n, hk, d, window, sinks)
+    eager = layers.StreamCache(n, hk, d, window, sinks)
+    freqs = layers.rotary_frequencies([16, 16])
+    qkv = randn(0, n, h + 2 * hk, d, dtype=torch.bfloat16)
+    pos = torch.zeros(2, n, dtype=torch.int64, device="cuda")
+
+    def token(c):
+        pos[0] = c.pos
+        q, k = layers.rotary(qkv[None, :, :h], qkv[None, :, h:h + hk], pos, freqs, [16, 16])
+        return c.step(q[0], k[0], qkv[:, h + hk:])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            token(cache)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = token(cache)
+    for c in (cache, eager):
+        for t in (c.k, c.v, c.pos):
+            t.zero_()
+    for t in range(6):
+        qkv.copy_(randn(t, n, h + 2 * hk, d, dtype=torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, token(eager)), t
+        assert torch.equal(cache.k, eager.k) and torch.equal(cache.v, eager.v) and torch.equal(cache.pos, eager.pos)
+
+
+def test_refusals():
+    off = offsets_of([4, 4])
+    x, w = randn(0, 1, 8, 3), randn(1, 2, 5, 3)
+    q = randn(2, 1, 8, 4, 16)
+    with pytest.raises(ValueError):
+        layers.band_linear(x.cpu(), w, off)
+    with pytest.raises(ValueError):
+        layers.band_linear(x, w.half(), off)
+    with pytest.raises(ValueError):
+        layers.band_linear(x, w[:1], off)
+    with pytest.raises(ValueError):
+        layers.band_linear(x, w, off.int())
+    with pytest.raises(ValueError):
+        layers.band_linear(x.double(), w.double(), off)
+    with pytest.raises(ValueError):
+        layers.band_linear(x.transpose(1, 2).contiguous().transpose(1, 2), w, off)
+    with pytest.raises(ValueError):
+        layers.band_attention(q, q[:, :4], q, off, 3)
+    with pytest.raises(ValueError):
+        layers.band_attention(q, q, q, off, 3, keep=torch.ones(1, 8, device="cuda"))
+    for bad in (dict(left=-1), dict(left=3, right=-2), dict(left=3, sinks=-1), dict(left=3, scale=0.0),
+                dict(left=3, scale=float("nan"))):
+        with pytest.raises(nc.NsgcqtError) as e:
+            layers.band_attention(q, q, q, off, **bad)
+        assert e.value.status == nc.EINVAL
+    with pytest.raises(nc.NsgcqtError) as e:
+        layers.band_attention(q, q[:, :, :3], q[:, :, :3], off, 3)
+    assert e.value.status == nc.EINVAL
+    wide = randn(3, 1, 8, 1, 129)
+    with pytest.raises(nc.NsgcqtError) as e:
+        layers.band_attention(wide, wide, wide, off, 3)
+    assert e.value.status == nc.EUNSUPPORTED
+    pos = torch.zeros(2, 8, dtype=torch.float64, device="cuda")
+    with pytest.raises(ValueError):
+        layers.rotary(q, None, pos, layers.rotary_frequencies([6, 6]), [6, 6])
+    with pytest.raises(ValueError):
+        layers.rotary(q, None, pos[:1], layers.rotary_frequencies([2, 2]), [2, 2])
+    with pytest.raises(ValueError):
+        layers.rotary(q, None, pos.float().half(), layers.rotary_frequencies([2, 2]), [2, 2])
+    c = layers.StreamCache(2, 1, 16, 8, 2, dtype=torch.float32)
+    with pytest.raises(ValueError):
+        c.step(q[0, :2], q[0, :2, :1], q[0, :2, :1].half())
+    with pytest.raises(ValueError):
+        layers.attention_step(q[0, :2], q[0, :2, :1], q[0, :2, :1], c.k, c.v[:, :, :4], c.pos, 2)
+    with pytest.raises(nc.NsgcqtError):
+        layers.attention_step(q[0, :2], q[0, :2, :1], q[0, :2, :1], c.k, c.v, c.pos, 10)
+    with pytest.raises(ValueError):
+        layers.attention_step(q[0, :2].requires_grad_(), q[0, :2, :1], q[0, :2, :1], c.k, c.v, c.pos, 2)
