@@ -54,22 +54,28 @@ struct KeyRange {
 };
 
 // One tile of BN rows x DP columns of two tensors, through registers: the
-// loads of the next tile are in flight while this one is computed.
+// loads of the next tile are in flight while this one is computed. Rows that
+// are not kept are loaded like others and become zeros on their way to LDS,
+// so that no load waits for a mask.
 template <class T, int DP, int BN> struct Stage {
     static constexpr int kChunks = BN * DP / 8, kEach = (kChunks + 255) / 256, kRB = row_bytes<T, DP>();
     static constexpr int kBytes = BN * kRB;
     frag<T> x[kEach], y[kEach];
+    bool kept[kEach];
 
-    // rows row0 + (0 .. BN-1) below row_end; others, and those not kept, are zeros
+    // rows row0 + (0 .. BN-1) below row_end; others are zeros
     __device__ void load(const T* px, int64_t sx, const T* py, int64_t sy, const uint8_t* keep, int row0, int row_end,
                          int dim, bool wide, int tid) {
+        px += row0 * sx;
+        py += row0 * sy;
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int c = tid + 256 * e, row = row0 + c / (DP / 8), d = c % (DP / 8) * 8;
-            const bool there = (kChunks % 256 == 0 || c < kChunks) && row < row_end && (!keep || keep[row]);
+            const int c = tid + 256 * e, row = c / (DP / 8), d = c % (DP / 8) * 8;
+            const bool there = (kChunks % 256 == 0 || c < kChunks) && row0 + row < row_end;
             const int n = there ? dim - d : 0;
             x[e] = load8<T>(px + row * sx + d, n, wide);
             y[e] = load8<T>(py + row * sy + d, n, wide);
+            kept[e] = !keep || (there && keep[row0 + row]);
         }
     }
     __device__ void store(char* tx, char* ty, int tid) const {
@@ -77,12 +83,45 @@ template <class T, int DP, int BN> struct Stage {
         for (int e = 0; e < kEach; ++e) {
             const int c = tid + 256 * e;
             if (kChunks % 256 == 0 || c < kChunks) {
-                write8<T, kRB>(tx, c / (DP / 8), c % (DP / 8), x[e]);
-                write8<T, kRB>(ty, c / (DP / 8), c % (DP / 8), y[e]);
+                write8<T, kRB>(tx, c / (DP / 8), c % (DP / 8), kept[e] ? x[e] : zero8<T>());
+                write8<T, kRB>(ty, c / (DP / 8), c % (DP / 8), kept[e] ? y[e] : zero8<T>());
             }
         }
     }
 };
+
+// Where a wave's scores start: 0 for a key that is there and kept, -inf for
+// others. The masked keys' rows are zeros, so their scores stay -inf.
+__device__ inline acc16 start_scores(const float* bias, int kb, int h) {
+    acc16 s;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f4 b = *reinterpret_cast<const f4*>(bias + 32 * kb + 8 * q + 4 * h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * q + j] = b[j];
+    }
+    return s;
+}
+
+// The window's edges, for tiles that cross one: hides the scores (column:
+// query i, rows: keys j0 + 32 kb + ...) of keys outside [i - left, i + right]
+// that are not sinks.
+__device__ inline void hide_edges(acc16& s, const AttnArgs& a, int i, int j0, int kb, int h) {
+    const int at = j0 + 32 * kb + 4 * h, lo = i - a.left - at;
+    const unsigned span = static_cast<unsigned>(a.left) + a.right;
+    if (j0 >= a.sinks) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[r] = static_cast<unsigned>(8 * (r >> 2) + (r & 3) - lo) <= span ? s[r] : -INFINITY;
+    } else {
+        const int hi = i + a.right - at, sink = a.sinks - at;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int e = 8 * (r >> 2) + (r & 3);
+            s[r] = e <= hi && (e >= lo || e < sink) ? s[r] : -INFINITY;
+        }
+    }
+}
 
 // 32 rows of a tensor as fragments (A or B): lane l holds row l % 32.
 template <class T, int DP>
@@ -107,7 +146,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
     constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
     typedef Stage<T, DP, BN> St;
     __shared__ __align__(128) char lds[2][2][St::kBytes];
-    __shared__ unsigned kept[2][2];   // a bit for each key of a tile
+    __shared__ __align__(16) float bias[2][BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
 
     int64_t w = die_order(blockIdx.x, gridDim.x);
@@ -139,19 +178,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
 
     const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
     St st;
+    float next_bias = 0.f;
     auto fetch = [&](int n) {
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
         st.load(kp, a.k.row, vp, a.v.row, keep, j0, j_end, a.dim, a.wide, tid);
+        if (tid < BN) next_bias = j0 + tid < j_end && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
     };
     auto put = [&](int n) {
         st.store(lds[n & 1][0], lds[n & 1][1], tid);
-        if (keep && tid < BN) {
-            int j0, j_end;
-            range.tile(n, BN, j0, j_end);
-            const uint64_t bits = __ballot(j0 + tid < j_end && keep[j0 + tid] != 0);
-            if (tid < 2) kept[n & 1][tid] = static_cast<unsigned>(bits >> (32 * tid));
-        }
+        if (tid < BN) bias[n & 1][tid] = next_bias;
     };
     fetch(0);
     put(0);
@@ -165,28 +201,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
         if (!skip) {
             const char* kt = lds[n & 1][0];
             const char* vt = lds[n & 1][1];
+            const bool whole = !keep && j0 + BN <= j_end;
+            const bool edge = j_last > i_lo + a.right || (j0 < i_hi - a.left && j_last >= a.sinks);
             acc16 s[BN / 32];
 #pragma unroll
             for (int kb = 0; kb < BN / 32; ++kb) {
-                s[kb] = zero16();
+                s[kb] = whole ? zero16() : start_scores(bias[n & 1], kb, h);
 #pragma unroll
                 for (int x = 0; x < DP / 16; ++x) s[kb] = mma(read8<T, RB>(kt, 32 * kb + m, 2 * x + h), qf[x], s[kb]);
             }
-            const bool all = !keep && j0 + BN <= j_end && j_last <= i_lo + a.right &&
-                             (j0 >= i_hi - a.left || j_last < a.sinks);
-            if (!all) {
-                unsigned ok[BN / 32];
+            if (edge) {
 #pragma unroll
-                for (int kb = 0; kb < BN / 32; ++kb) ok[kb] = keep ? kept[n & 1][kb] : ~0u;
-#pragma unroll
-                for (int kb = 0; kb < BN / 32; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int jj = 8 * (r >> 2) + 4 * h + (r & 3), j = j0 + 32 * kb + jj;
-                        const bool see = j < j_end && j <= i + a.right && (j >= i - a.left || j < a.sinks) &&
-                                         ((ok[kb] >> jj) & 1);
-                        s[kb][r] = see ? s[kb][r] : -INFINITY;
-                    }
+                for (int kb = 0; kb < BN / 32; ++kb) hide_edges(s[kb], a, i, j0, kb, h);
             }
             float mx = s[0][0];
 #pragma unroll
@@ -240,7 +266,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
     constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
     typedef Stage<T, DP, BN> St;
     __shared__ __align__(128) char lds[2][2][St::kBytes];
-    __shared__ unsigned kept[2][2];   // a bit for each key of a tile
+    __shared__ __align__(16) float bias[2][BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
 
     int64_t w = die_order(blockIdx.x, gridDim.x);
@@ -285,19 +311,16 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
 
     const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
     St st;
+    float next_bias = 0.f;
     auto fetch = [&](int n) {
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
         st.load(kp, a.k.row, vp, a.v.row, keep, j0, j_end, a.dim, a.wide, tid);
+        if (tid < BN) next_bias = j0 + tid < j_end && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
     };
     auto put = [&](int n) {
         st.store(lds[n & 1][0], lds[n & 1][1], tid);
-        if (keep && tid < BN) {
-            int j0, j_end;
-            range.tile(n, BN, j0, j_end);
-            const uint64_t bits = __ballot(j0 + tid < j_end && keep[j0 + tid] != 0);
-            if (tid < 2) kept[n & 1][tid] = static_cast<unsigned>(bits >> (32 * tid));
-        }
+        if (tid < BN) bias[n & 1][tid] = next_bias;
     };
     fetch(0);
     put(0);
@@ -311,29 +334,22 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
         if (!skip) {
             const char* kt = lds[n & 1][0];
             const char* vt = lds[n & 1][1];
-            const bool all = !keep && j0 + BN <= j_end && j_last <= i_lo + a.right &&
-                             (j0 >= i_hi - a.left || j_last < a.sinks);
+            const bool whole = !keep && j0 + BN <= j_end;
+            const bool edge = j_last > i_lo + a.right || (j0 < i_hi - a.left && j_last >= a.sinks);
 #pragma unroll
             for (int kb = 0; kb < BN / 32; ++kb) {
-                acc16 s = zero16(), dp = zero16();
+                acc16 s = whole ? zero16() : start_scores(bias[n & 1], kb, h), dp = zero16();
 #pragma unroll
                 for (int x = 0; x < DP / 16; ++x) {
                     s = mma(read8<T, RB>(kt, 32 * kb + m, 2 * x + h), qf[x], s);
                     dp = mma(read8<T, RB>(vt, 32 * kb + m, 2 * x + h), gf[x], dp);
                 }
-                if (all) {
+                if (edge) hide_edges(s, a, i, j0, kb, h);
+                // p is 0 for hidden keys; what dp holds there must not turn it into NaN
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
-                } else {
-                    const unsigned ok = keep ? kept[n & 1][kb] : ~0u;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int jj = 8 * (r >> 2) + 4 * h + (r & 3), j = j0 + 32 * kb + jj;
-                        const bool see = j < j_end && j <= i + a.right && (j >= i - a.left || j < a.sinks) &&
-                                         ((ok >> jj) & 1);
-                        const float p = exp2_(fmaf(s[r], a.c, -lse));
-                        s[r] = see ? p * (dp[r] - delta) : 0.f;
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const float p = exp2_(fmaf(s[r], a.c, -lse));
+                    s[r] = p == 0.f ? 0.f : p * (dp[r] - delta);
                 }
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -370,12 +386,14 @@ __device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t 
 }
 
 // One wave's 32 queries (rows of the tiles qt, gt at r0) against its 32 keys:
-// adds to dk^T and dv^T. lse, delta: of the tile's queries, in LDS.
-// see(query row in the tile): whether this lane's key is visible to it.
-template <class T, int DP, class See>
+// adds to dk^T and dv^T. lse, delta: of the tile's queries, in LDS (+inf for a
+// query that is not there: its probabilities are 0). With edge, this lane's
+// key is visible to the rows r0 + lo .. r0 + lo + span only. A key that is
+// not there or not kept only spoils its own column, which its lane drops.
+template <class T, int DP>
 __device__ inline void key_grad(const char* qt, const char* gt, const float* lse, const float* delta, int r0,
                                 const frag<T> (&kf)[DP / 16], const frag<T> (&vf)[DP / 16], acc16 (&dk)[DP / 32],
-                                acc16 (&dv)[DP / 32], float c, bool all, int lane, See see) {
+                                acc16 (&dv)[DP / 32], float c, bool edge, int lo, unsigned span, int lane) {
     constexpr int RB = row_bytes<T, DP>();
     const int m = lane & 31, h = lane >> 5;
     acc16 s = zero16(), dp = zero16();
@@ -384,25 +402,22 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
         s = mma(read8<T, RB>(qt, r0 + m, 2 * x + h), kf[x], s);
         dp = mma(read8<T, RB>(gt, r0 + m, 2 * x + h), vf[x], dp);
     }
-    auto weigh = [&](auto ok) {
+    if (edge) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f4 l = *reinterpret_cast<const f4*>(lse + r0 + 8 * q + 4 * h);
-            const f4 e = *reinterpret_cast<const f4*>(delta + r0 + 8 * q + 4 * h);
+        for (int r = 0; r < 16; ++r)
+            s[r] = static_cast<unsigned>(8 * (r >> 2) + 4 * h + (r & 3) - lo) <= span ? s[r] : -INFINITY;
+    }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = 4 * q + j;
-                const float p = exp2_(fmaf(s[r], c, -l[j])), ds = p * (dp[r] - e[j]);
-                const bool o = ok(r0 + 8 * q + 4 * h + j);
-                s[r] = o ? p : 0.f;
-                dp[r] = o ? ds : 0.f;
-            }
+    for (int q = 0; q < 4; ++q) {
+        const f4 l = *reinterpret_cast<const f4*>(lse + r0 + 8 * q + 4 * h);
+        const f4 e = *reinterpret_cast<const f4*>(delta + r0 + 8 * q + 4 * h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = 4 * q + j;
+            s[r] = exp2_(fmaf(s[r], c, -l[j]));
+            dp[r] = s[r] == 0.f ? 0.f : s[r] * (dp[r] - e[j]);
         }
-    };
-    if (all)
-        weigh([](int) { return true; });
-    else
-        weigh(see);
+    }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const frag<T> p = narrow<T>(s, x), ds = narrow<T>(dp, x);
@@ -416,7 +431,7 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 
 // dk, dv of 128 keys (a wave has 32) over the queries near them.
 template <class T, int DP>
-__global__ __launch_bounds__(256, DP > 32 ? 1 : 2) void k_attention_dkv(AttnArgs a) {
+__global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2) void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = kv_tile<T, DP>();
     typedef Stage<T, DP, BQ> St;
     __shared__ __align__(128) char lds[2][2][St::kBytes];
@@ -450,6 +465,7 @@ __global__ __launch_bounds__(256, DP > 32 ? 1 : 2) void k_attention_dkv(AttnArgs
     const int i_begin = k0 > a.right ? k0 - a.right : 0;
     const int i_end = static_cast<int64_t>(k0) + kQueries + a.left < len ? k0 + kQueries + a.left : len;
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
+    const unsigned span = j < a.sinks ? 0x7fffffffu : static_cast<unsigned>(a.left) + a.right;
     St st;
     float next_lse = 0.f, next_delta = 0.f;
     auto fetch = [&](int n) {
@@ -482,14 +498,9 @@ __global__ __launch_bounds__(256, DP > 32 ? 1 : 2) void k_attention_dkv(AttnArgs
             const bool skip = !active || i_lo >= i_end || j_lo > i_hi + a.right ||
                               (j_hi < i_lo - a.left && j_lo >= a.sinks);
             if (!skip) {
-                const bool all = !keep && j_lo + 31 < len && i_lo + 31 < i_end && j_hi <= i_lo + a.right &&
-                                 (j_lo >= i_hi - a.left || j_hi < a.sinks);
+                const bool edge = j_hi > i_lo + a.right || (j_lo < i_hi - a.left && j_hi >= a.sinks);
                 key_grad<T, DP>(lds[n & 1][0], lds[n & 1][1], row_lse[n & 1], row_delta[n & 1], 32 * qb, kf, vf, dk, dv,
-                                a.c, all, lane, [&](int r) {
-                                    const int i = i0 + r;
-                                    return kept && i < i_end && j <= i + a.right &&
-                                           (j >= i - a.left || j < a.sinks);
-                                });
+                                a.c, edge, j - a.right - i_lo, span, lane);
             }
         }
         if (n + 1 < total) put(n + 1);
@@ -521,7 +532,11 @@ __global__ __launch_bounds__(256, DP > 32 ? 1 : 2) void k_attention_dkv(AttnArgs
     T* ov = mine ? row_of<T>(a.dv, b, t.start + j, kv) : nullptr;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-        dk[d] *= a.scale;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            dk[d][r] = kept ? dk[d][r] * a.scale : 0.f;
+            dv[d][r] = kept ? dv[d][r] : 0.f;
+        }
         store_column<T>(ok, dk[d], 32 * d, a.dim, a.wide, lane);
         store_column<T>(ov, dv[d], 32 * d, a.dim, a.wide, lane);
     }
@@ -579,8 +594,7 @@ __global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
             }
             __syncthreads();
             if (32 * wave < BQ && i0 + 32 * wave < i_end)
-                key_grad<T, DP>(lds[0], lds[1], row_lse, row_delta, 32 * wave, kf, vf, dk, dv, a.c, false, lane,
-                                [&](int r) { return kept && i0 + r < i_end; });
+                key_grad<T, DP>(lds[0], lds[1], row_lse, row_delta, 32 * wave, kf, vf, dk, dv, a.c, false, 0, 0, lane);
         }
     }
     for (int v = 0; v < 4; ++v) {

@@ -19,7 +19,9 @@ strides are free. Calls run on the current stream.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import struct
 
 import torch
 
@@ -39,19 +41,10 @@ EXPORTS = [
 ]
 
 
-class View(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("row", ctypes.c_int64),
-                ("head", ctypes.c_int64)]
-
-
-class Rows(ctypes.Structure):
-    _fields_ = [("offsets", ctypes.c_void_p), ("n_bands", ctypes.c_int64), ("batch", ctypes.c_int64),
-                ("rows", ctypes.c_int64)]
-
-
-class AttentionShape(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int64) for n in ("n_heads", "n_kv_heads", "head_dim", "left", "right", "sinks")] + [
-        ("scale", ctypes.c_double), ("keep", ctypes.c_void_p), ("keep_batch", ctypes.c_int64)]
+# The structs of the header, packed: a call passes their bytes.
+_view = struct.Struct("=4q").pack                # nsgcqt_view: data, strides of batch, row, head
+_rows = struct.Struct("=4q").pack                # nsgcqt_rows: offsets, n_bands, batch, rows
+_shape = struct.Struct("=6qd2q").pack            # nsgcqt_attention_shape
 
 
 _fns = None
@@ -92,6 +85,14 @@ def _bytes(n):
     return _check(int(n)) if n < 0 else n
 
 
+_here = contextlib.nullcontext()
+
+
+def _on(t):
+    """A context with t's device current."""
+    return _here if t.get_device() == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
 def _stream(t):
     return torch.cuda.current_stream(t.device).cuda_stream
 
@@ -103,11 +104,11 @@ def _tensor(t, name, like=None, shape=None):
     if like is None:
         if t.dtype not in _DTYPES:
             raise ValueError(f"{name} is {t.dtype}: float32, float16 or bfloat16 is expected")
-    elif t.dtype != like.dtype or t.device != like.device:
+    elif t.dtype != like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name} is {t.dtype} on {t.device}: {like.dtype} on {like.device} is expected")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is expected")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"the last axis of {name} has to be contiguous")
     return t
 
@@ -115,31 +116,32 @@ def _tensor(t, name, like=None, shape=None):
 def _offsets(offsets, like):
     if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
         raise ValueError("offsets has to be a contiguous int64 vector of n_bands + 1 values")
-    if offsets.device != like.device:
+    if offsets.get_device() != like.get_device():
         raise ValueError(f"offsets is on {offsets.device}: {like.device} is expected")
     return offsets
 
 
-def _rows(offsets, batch, rows):
-    return Rows(offsets.data_ptr(), offsets.numel() - 1, batch, rows)
+def _ragged(offsets, batch, rows):
+    return _rows(offsets.data_ptr(), offsets.shape[0] - 1, batch, rows)
 
 
 def _view3(t):
     s = t.stride()
-    return View(t.data_ptr(), s[0], s[1], 0)
+    return _view(t.data_ptr(), s[0], s[1], 0)
 
 
 def _view4(t):
     s = t.stride()
-    return View(t.data_ptr(), s[0], s[1], s[2])
+    return _view(t.data_ptr(), s[0], s[1], s[2])
+
+
+def _trains(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 def _last(t):
     """t with a contiguous last axis (a gradient may come in any layout)."""
     return t if t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
-
-
-_ref = ctypes.byref
 
 
 # ------------------------------------------------------------------ band_linear
@@ -164,10 +166,10 @@ def _linear_forward(x, weight, offsets, bias):
     batch, rows, n_in = x.shape
     n_out = weight.shape[1]
     y = torch.empty((batch, rows, n_out), dtype=x.dtype, device=x.device)
-    with torch.cuda.device(x.device):
+    with _on(x):
         _check(_lib().nsgcqt_band_linear(
-            _DTYPES[x.dtype], _ref(_rows(offsets, batch, rows)), _ref(_view3(x)), weight.data_ptr(),
-            None if bias is None else bias.data_ptr(), _ref(_view3(y)), n_in, n_out, _stream(x)))
+            _DTYPES[x.dtype], _ragged(offsets, batch, rows), _view3(x), weight.data_ptr(),
+            None if bias is None else bias.data_ptr(), _view3(y), n_in, n_out, _stream(x)))
     return y
 
 
@@ -175,10 +177,10 @@ def _linear_grad_input(dy, weight, offsets):
     batch, rows, n_out = dy.shape
     n_in = weight.shape[2]
     dx = torch.empty((batch, rows, n_in), dtype=dy.dtype, device=dy.device)
-    with torch.cuda.device(dy.device):
+    with _on(dy):
         _check(_lib().nsgcqt_band_linear_grad_input(
-            _DTYPES[dy.dtype], _ref(_rows(offsets, batch, rows)), _ref(_view3(dy)), weight.data_ptr(),
-            _ref(_view3(dx)), n_in, n_out, _stream(dy)))
+            _DTYPES[dy.dtype], _ragged(offsets, batch, rows), _view3(dy), weight.data_ptr(),
+            _view3(dx), n_in, n_out, _stream(dy)))
     return dx
 
 
@@ -190,9 +192,9 @@ def _linear_grad_weight(x, dy, offsets, with_bias):
     L = _lib()
     n = _bytes(L.nsgcqt_band_linear_workspace(bands, batch, rows, n_in, n_out))
     ws = torch.empty(max(n, 1), dtype=torch.uint8, device=x.device)
-    with torch.cuda.device(x.device):
+    with _on(x):
         _check(L.nsgcqt_band_linear_grad_weight(
-            _DTYPES[x.dtype], _ref(_rows(offsets, batch, rows)), _ref(_view3(x)), _ref(_view3(dy)), dw.data_ptr(),
+            _DTYPES[x.dtype], _ragged(offsets, batch, rows), _view3(x), _view3(dy), dw.data_ptr(),
             None if db is None else db.data_ptr(), n_in, n_out, ws.data_ptr(), n, _stream(x)))
     return dw, db
 
@@ -225,6 +227,8 @@ def band_linear(x, weight, offsets, bias=None):
     x, weight and bias.
     """
     _linear_checks(x, weight, offsets, bias)
+    if not _trains(x, weight, bias):
+        return _linear_forward(x, weight, offsets, bias)
     return _BandLinear.apply(x, weight, bias, offsets)
 
 
@@ -249,6 +253,9 @@ def rotary_frequencies(sections, base=10000.0, device="cuda"):
     return torch.cat([base ** (-torch.arange(s, dtype=torch.float64) / max(s, 1)) for s in sections]).float().to(device)
 
 
+_sections = [struct.Struct(f"={n}i").pack for n in range(5)]
+
+
 def _rotary_call(q, k, positions, freqs, sections, interleaved, inverse):
     outs, views, heads = [], [], []
     for t in (q, k):
@@ -259,17 +266,21 @@ def _rotary_call(q, k, positions, freqs, sections, interleaved, inverse):
         else:
             o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
             outs.append(o)
-            views += [_ref(_view4(t)), _ref(_view4(o))]
+            views += [_view4(t), _view4(o)]
             heads.append(t.shape[2])
     t = q if q is not None else k
     batch, rows, _, dim = t.shape
     s = positions.stride()
-    with torch.cuda.device(t.device):
+    with _on(t):
         _check(_lib().nsgcqt_rotary(
             _DTYPES[t.dtype], views[0], views[1], heads[0], views[2], views[3], heads[1], batch, rows, dim,
             positions.data_ptr(), _POS[positions.dtype], s[0], s[1] if positions.dim() == 3 else 0, freqs.data_ptr(),
-            sections, len(sections), int(interleaved), int(inverse), _stream(t)))
+            sections, len(sections) // 4, int(interleaved), int(inverse), _stream(t)))
     return outs
+
+
+def _rotary_forward(q, k, positions, freqs, sections, interleaved):
+    return tuple(_rotary_call(q, k, positions, freqs, sections, interleaved, False))
 
 
 class _Rotary(torch.autograd.Function):
@@ -278,7 +289,7 @@ class _Rotary(torch.autograd.Function):
         ctx.save_for_backward(positions, freqs)
         ctx.how = sections, interleaved
         ctx.set_materialize_grads(False)
-        return tuple(_rotary_call(q, k, positions, freqs, sections, interleaved, False))
+        return _rotary_forward(q, k, positions, freqs, sections, interleaved)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -315,39 +326,42 @@ def rotary(q, k, positions, freqs, sections, interleaved=False):
         raise ValueError("sections has to hold 1 to 4 counts of at most D / 2 pairs in all")
     if positions.dtype not in _POS or positions.device != q.device:
         raise ValueError("positions has to be float32, float64 or int64 on the device of q")
-    if tuple(positions.shape) not in ((len(sections), rows), (len(sections), batch, rows)) or (
+    if positions.shape not in ((len(sections), rows), (len(sections), batch, rows)) or (
             rows > 1 and positions.stride(-1) != 1):
         raise ValueError("positions has to be [axes][rows] or [axes][batch][rows], its rows contiguous")
-    if freqs.dtype != torch.float32 or freqs.device != q.device or tuple(freqs.shape) != (pairs,) or not freqs.is_contiguous():
+    if freqs.dtype != torch.float32 or freqs.device != q.device or freqs.shape != (pairs,) or not freqs.is_contiguous():
         raise ValueError(f"freqs has to be a float32 vector of {pairs} values on the device of q")
-    sec = (ctypes.c_int32 * len(sections))(*sections)
-    if k is None:
-        return _Rotary.apply(q, None, positions, freqs, sec, interleaved)[0]
-    return _Rotary.apply(q, k, positions, freqs, sec, interleaved)
+    sec = _sections[len(sections)](*sections)
+    call = _Rotary.apply if _trains(q, k) else _rotary_forward
+    out = call(q, k, positions, freqs, sec, interleaved)
+    return out[0] if k is None else out
 
 
 # --------------------------------------------------------------- band_attention
 
 
 def _shape_of(q, k, left, right, sinks, scale, keep):
-    return AttentionShape(q.shape[2], k.shape[2], q.shape[3], left, right, sinks, scale,
-                          None if keep is None else keep.data_ptr(), 0 if keep is None else keep.stride(0))
+    return _shape(q.shape[2], k.shape[2], q.shape[3], left, right, sinks, scale,
+                          0 if keep is None else keep.data_ptr(), 0 if keep is None else keep.stride(0))
+
+
+def _attention_forward(q, k, v, offsets, keep, left, right, sinks, scale, stats=None):
+    batch, rows, heads, dim = q.shape
+    o = torch.empty((batch, rows, heads, dim), dtype=q.dtype, device=q.device)
+    with _on(q):
+        _check(_lib().nsgcqt_band_attention(
+            _DTYPES[q.dtype], _ragged(offsets, batch, rows), _shape_of(q, k, left, right, sinks, scale, keep),
+            _view4(q), _view4(k), _view4(v), _view4(o), None if stats is None else stats.data_ptr(), _stream(q)))
+    return o
 
 
 class _BandAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, offsets, keep, left, right, sinks, scale, train):
-        batch, rows, heads, dim = q.shape
-        o = torch.empty((batch, rows, heads, dim), dtype=q.dtype, device=q.device)
-        stats = torch.empty((batch, heads, rows), dtype=torch.float32, device=q.device) if train else None
-        shape = _shape_of(q, k, left, right, sinks, scale, keep)
-        with torch.cuda.device(q.device):
-            _check(_lib().nsgcqt_band_attention(
-                _DTYPES[q.dtype], _ref(_rows(offsets, batch, rows)), _ref(shape), _ref(_view4(q)), _ref(_view4(k)),
-                _ref(_view4(v)), _ref(_view4(o)), None if stats is None else stats.data_ptr(), _stream(q)))
-        if train:
-            ctx.save_for_backward(q, k, v, o, stats, offsets, keep)
-            ctx.how = left, right, sinks, scale
+    def forward(ctx, q, k, v, offsets, keep, left, right, sinks, scale):
+        stats = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        o = _attention_forward(q, k, v, offsets, keep, left, right, sinks, scale, stats)
+        ctx.save_for_backward(q, k, v, o, stats, offsets, keep)
+        ctx.how = left, right, sinks, scale
         return o
 
     @staticmethod
@@ -356,16 +370,16 @@ class _BandAttention(torch.autograd.Function):
         q, k, v, o, stats, offsets, keep = ctx.saved_tensors
         do = _last(do)
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        shape, r = _shape_of(q, k, *ctx.how, keep), _rows(offsets, q.shape[0], q.shape[1])
+        shape, r = _shape_of(q, k, *ctx.how, keep), _ragged(offsets, q.shape[0], q.shape[1])
         L = _lib()
-        n = _bytes(L.nsgcqt_band_attention_workspace(_ref(r), _ref(shape)))
+        n = _bytes(L.nsgcqt_band_attention_workspace(r, shape))
         ws = torch.empty(max(n, 1), dtype=torch.uint8, device=q.device)
-        with torch.cuda.device(q.device):
+        with _on(q):
             _check(L.nsgcqt_band_attention_grad(
-                _DTYPES[q.dtype], _ref(r), _ref(shape), _ref(_view4(q)), _ref(_view4(k)), _ref(_view4(v)),
-                _ref(_view4(o)), stats.data_ptr(), _ref(_view4(do)), _ref(_view4(dq)), _ref(_view4(dk)),
-                _ref(_view4(dv)), ws.data_ptr(), n, _stream(q)))
-        return dq, dk, dv, None, None, None, None, None, None, None
+                _DTYPES[q.dtype], r, shape, _view4(q), _view4(k), _view4(v),
+                _view4(o), stats.data_ptr(), _view4(do), _view4(dq), _view4(dk),
+                _view4(dv), ws.data_ptr(), n, _stream(q)))
+        return dq, dk, dv, None, None, None, None, None, None
 
 
 def band_attention(q, k, v, offsets, left, right=0, sinks=0, scale=None, keep=None):
@@ -387,14 +401,13 @@ def band_attention(q, k, v, offsets, left, right=0, sinks=0, scale=None, keep=No
     _tensor(v, "v", q, k.shape)
     _offsets(offsets, q)
     if keep is not None:
-        if keep.dtype != torch.bool or keep.device != q.device or tuple(keep.shape) != (batch, rows) or (
+        if keep.dtype != torch.bool or keep.device != q.device or keep.shape != (batch, rows) or (
                 rows > 1 and keep.stride(1) != 1):
             raise ValueError("keep has to be bool [batch][rows] on the device of q, its rows contiguous")
     far = 1 << 40
-    train = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)
-    return _BandAttention.apply(q, k, v, offsets, keep, far if left is None else int(left),
-                                far if right is None else int(right), int(sinks),
-                                dim ** -0.5 if scale is None else float(scale), train)
+    call = _BandAttention.apply if _trains(q, k, v) else _attention_forward
+    return call(q, k, v, offsets, keep, far if left is None else int(left), far if right is None else int(right),
+                int(sinks), dim ** -0.5 if scale is None else float(scale))
 
 
 # ------------------------------------------------------------- single-token step
@@ -429,9 +442,9 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
     _tensor(k, "k", q, (streams, kv_heads, dim))
     _tensor(v, "v", q, k.shape)
     slots = _caches(k_cache, v_cache, q, streams, kv_heads, dim)
-    if pos.dtype != torch.int64 or pos.device != q.device or tuple(pos.shape) != (streams,) or not pos.is_contiguous():
+    if pos.dtype != torch.int64 or pos.device != q.device or pos.shape != (streams,) or not pos.is_contiguous():
         raise ValueError("pos has to be int64 [streams] on the device of q")
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+    if _trains(q, k, v):
         raise ValueError("attention_step has no gradient: call it under torch.no_grad()")
     o = torch.empty((streams, heads, dim), dtype=q.dtype, device=q.device) if out is None else out
     _tensor(o, "out", q, (streams, heads, dim))
@@ -439,12 +452,11 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
     sinks = int(sinks)
     n = _bytes(L.nsgcqt_attention_step_workspace(streams, heads, kv_heads, dim, slots - sinks, sinks))
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    views = [View(t.data_ptr(), t.stride(0), 0, t.stride(1)) for t in (q, k, v, o)]
-    with torch.cuda.device(q.device):
+    views = [_view(t.data_ptr(), t.stride(0), 0, t.stride(1)) for t in (q, k, v, o)]
+    with _on(q):
         _check(L.nsgcqt_attention_step(
             _DTYPES[q.dtype], streams, heads, kv_heads, dim, slots - sinks, sinks,
-            dim ** -0.5 if scale is None else float(scale), _ref(views[0]), _ref(views[1]), _ref(views[2]),
-            _ref(views[3]), k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(),
+            dim ** -0.5 if scale is None else float(scale), *views, k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(),
             ws.data_ptr() if n else None, n, _stream(q)))
     return o
 
@@ -463,10 +475,10 @@ def cache_fill(k, v, offsets, k_cache, v_cache, sinks=0):
     _tensor(v, "v", k, k.shape)
     _offsets(offsets, k)
     slots = _caches(k_cache, v_cache, k, batch * (offsets.numel() - 1), kv_heads, dim)
-    with torch.cuda.device(k.device):
+    with _on(k):
         _check(_lib().nsgcqt_cache_fill(
-            _DTYPES[k.dtype], _ref(_rows(offsets, batch, rows)), kv_heads, dim, slots - int(sinks), int(sinks),
-            _ref(_view4(k)), _ref(_view4(v)), k_cache.data_ptr(), v_cache.data_ptr(), _stream(k)))
+            _DTYPES[k.dtype], _ragged(offsets, batch, rows), kv_heads, dim, slots - int(sinks), int(sinks),
+            _view4(k), _view4(v), k_cache.data_ptr(), v_cache.data_ptr(), _stream(k)))
 
 
 class StreamCache:

@@ -30,20 +30,35 @@ def test_every_declared_symbol_is_exported(L):
         assert hasattr(L, n), n
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("n_bands", ctypes.c_int64), ("batch", ctypes.c_int64),
+                ("rows", ctypes.c_int64)]
+
+
+class View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("row", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
+class Shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_heads", "n_kv_heads", "head_dim", "left", "right", "sinks")] + [
+        ("scale", ctypes.c_double), ("keep", ctypes.c_void_p), ("keep_batch", ctypes.c_int64)]
+
+
 def ref(x):
     return ctypes.byref(x)
 
 
 def rows(offsets=FAKE, bands=2, batch=1, n=8):
-    return layers.Rows(offsets, bands, batch, n)
+    return Rows(offsets, bands, batch, n)
 
 
 def view(data=FAKE, batch=64, row=8, head=8):
-    return layers.View(data, batch, row, head)
+    return View(data, batch, row, head)
 
 
 def shape(heads=2, kv=1, dim=8, left=3, right=0, sinks=0, scale=1.0):
-    return layers.AttentionShape(heads, kv, dim, left, right, sinks, scale, None, 0)
+    return Shape(heads, kv, dim, left, right, sinks, scale, None, 0)
 
 
 def refused(status, code, word):
