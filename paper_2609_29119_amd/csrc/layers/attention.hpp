@@ -45,6 +45,14 @@ struct KeyRange {
         sink_tiles = (sink_end + bn - 1) / bn;
         tiles = sink_tiles + (end - begin + bn - 1) / bn;
     }
+    // Of 32 keys j .. of a tile and a wave's queries i_lo .. i_hi: whether no
+    // query sees any of them, and whether some see only some of them.
+    __device__ static bool hidden(const AttnArgs& a, int j, int j_end, int i_lo, int i_hi) {
+        return j >= j_end || j > i_hi + a.right || (j + 31 < i_lo - a.left && j >= a.sinks);
+    }
+    __device__ static bool edge(const AttnArgs& a, int j, int i_lo, int i_hi) {
+        return j + 31 > i_lo + a.right || (j < i_hi - a.left && j + 31 >= a.sinks);
+    }
     // first key of tile t, and the end of the keys it may hold
     __device__ void tile(int t, int bn, int& j0, int& j_end) const {
         const bool s = t < sink_tiles;
@@ -53,61 +61,93 @@ struct KeyRange {
     }
 };
 
-// One tile of BN rows x DP columns of two tensors, through registers: the
-// loads of the next tile are in flight while this one is computed. Rows that
-// are not kept are loaded like others and become zeros on their way to LDS,
-// so that no load waits for a mask.
-template <class T, int DP, int BN> struct Stage {
-    static constexpr int kChunks = BN * DP / 8, kEach = (kChunks + 255) / 256, kRB = row_bytes<T, DP>();
-    static constexpr int kBytes = BN * kRB;
-    frag<T> x[kEach], y[kEach];
-    bool kept[kEach];
+typedef __attribute__((address_space(3))) void lds_void;
 
-    // rows row0 + (0 .. BN-1) below row_end; others are zeros
-    __device__ void load(const T* px, int64_t sx, const T* py, int64_t sy, const uint8_t* keep, int row0, int row_end,
-                         int dim, bool wide, int tid) {
+// One tile of BN rows x DP columns of two tensors into LDS. Wide tensors go
+// there directly, 16 bytes a lane (a wave fills 1 KB of consecutive LDS, so
+// the lanes fetch the chunks that belong to their places): no registers, no
+// stores, and the next tile is on its way while this one is computed. Lanes
+// whose row or column is not there aim past the buffer's end, which reads as
+// zero. Other tensors take element loads and are stored from registers.
+template <class T, int DP, int BN> struct Loader {
+    static constexpr int kRB = row_bytes<T, DP>(), kBytes = BN * kRB;
+    static constexpr int kEach = kBytes / 4096;          // wide: loads of a thread for each tensor
+    static constexpr int kChunks = BN * DP / 8;          // else: chunks of 8 values of a tile
+    static constexpr unsigned kPast = 0x80000000u;       // the buffers' size: tiles span less
+
+    // place of load e of this thread in a tile
+    static __device__ int row(int e, int wave, int lane) { return ((wave * kEach + e) * 1024 + lane * 16) / kRB; }
+    static __device__ int col(int e, int wave, int lane) {
+        const int r = row(e, wave, lane), slot = (wave * kEach + e) * 1024 % kRB / 16 + lane % (kRB / 16 < 64 ? kRB / 16 : 64);
+        return (slot ^ turn(r)) * (16 / static_cast<int>(sizeof(T)));
+    }
+
+    // kept: for each load, whether its row may be used (wide only)
+    static __device__ void load(char* tx, char* ty, const T* px, int64_t sx, const T* py, int64_t sy, int row0,
+                                int row_end, int dim, bool wide, const uint8_t* keep, const bool (&kept)[kEach], int tid) {
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         px += row0 * sx;
         py += row0 * sy;
+        if (wide) {
+            const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(px), 0, kPast, 0x00020000);
+            const auto ry = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(py), 0, kPast, 0x00020000);
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int c = tid + 256 * e, row = c / (DP / 8), d = c % (DP / 8) * 8;
-            const bool there = (kChunks % 256 == 0 || c < kChunks) && row0 + row < row_end;
-            const int n = there ? dim - d : 0;
-            x[e] = load8<T>(px + row * sx + d, n, wide);
-            y[e] = load8<T>(py + row * sy + d, n, wide);
-            kept[e] = !keep || (there && keep[row0 + row]);
-        }
-    }
-    __device__ void store(char* tx, char* ty, int tid) const {
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int c = tid + 256 * e;
-            if (kChunks % 256 == 0 || c < kChunks) {
-                write8<T, kRB>(tx, c / (DP / 8), c % (DP / 8), kept[e] ? x[e] : zero8<T>());
-                write8<T, kRB>(ty, c / (DP / 8), c % (DP / 8), kept[e] ? y[e] : zero8<T>());
+            for (int e = 0; e < kEach; ++e) {
+                const int r = row(e, wave, lane), d = col(e, wave, lane);
+                const bool there = row0 + r < row_end && d < dim && kept[e];
+                const unsigned ox = (r * static_cast<unsigned>(sx) + d) * sizeof(T);
+                const unsigned oy = (r * static_cast<unsigned>(sy) + d) * sizeof(T);
+                const int at = (wave * kEach + e) * 1024;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(tx + at), 16, there ? ox : kPast, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_void*)(ty + at), 16, there ? oy : kPast, 0, 0, 0);
+            }
+        } else {
+            for (int c = tid; c < kChunks; c += 256) {
+                const int r = c / (DP / 8), d = c % (DP / 8) * 8;
+                const int n = row0 + r < row_end && (!keep || keep[row0 + r]) ? dim - d : 0;
+                write8<T, kRB>(tx, r, c % (DP / 8), load8<T>(px + r * sx + d, n, false));
+                write8<T, kRB>(ty, r, c % (DP / 8), load8<T>(py + r * sy + d, n, false));
             }
         }
     }
 };
 
-// Where a wave's scores start: 0 for a key that is there and kept, -inf for
-// others. The masked keys' rows are zeros, so their scores stay -inf.
-__device__ inline acc16 start_scores(const float* bias, int kb, int h) {
+// Every LDS write of this wave, the direct ones too, is done; then all waves'.
+__device__ inline void tile_barrier() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// S^T of 32 keys (rows row0 .. of a tile) and 32 queries. With a bias (of the
+// tile's keys: 0, or -inf for one that is not there or not kept; its row is
+// zeros) the sums start there, so that masking costs no instruction.
+template <class T, int DP>
+__device__ inline acc16 scores(const char* tile, int row0, const frag<T> (&f)[DP / 16], const float* bias, int lane) {
+    constexpr int RB = row_bytes<T, DP>();
+    const int m = lane & 31, h = lane >> 5;
+    if (!bias) {
+        acc16 s = zero16();
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x) s = mma(read8<T, RB>(tile, row0 + m, 2 * x + h), f[x], s);
+        return s;
+    }
     acc16 s;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const f4 b = *reinterpret_cast<const f4*>(bias + 32 * kb + 8 * q + 4 * h);
+        const f4 b = *reinterpret_cast<const f4*>(bias + row0 + 8 * q + 4 * h);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[4 * q + j] = b[j];
     }
+#pragma unroll
+    for (int x = 0; x < DP / 16; ++x) s = mma(read8<T, RB>(tile, row0 + m, 2 * x + h), f[x], s);
     return s;
 }
 
 // The window's edges, for tiles that cross one: hides the scores (column:
-// query i, rows: keys j0 + 32 kb + ...) of keys outside [i - left, i + right]
+// query i, rows: keys j0 ..) of keys outside [i - left, i + right]
 // that are not sinks.
-__device__ inline void hide_edges(acc16& s, const AttnArgs& a, int i, int j0, int kb, int h) {
-    const int at = j0 + 32 * kb + 4 * h, lo = i - a.left - at;
+__device__ inline void hide_edges(acc16& s, const AttnArgs& a, int i, int j0, int h) {
+    const int at = j0 + 4 * h, lo = i - a.left - at;
     const unsigned span = static_cast<unsigned>(a.left) + a.right;
     if (j0 >= a.sinks) {
 #pragma unroll
@@ -144,8 +184,8 @@ __device__ inline void zero_rows(const View& v, int64_t b, int head, int64_t sta
 template <class T, int DP>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_attention(AttnArgs a) {
     constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
-    typedef Stage<T, DP, BN> St;
-    __shared__ __align__(128) char lds[2][2][St::kBytes];
+    typedef Loader<T, DP, BN> Ld;
+    __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float bias[2][BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
 
@@ -174,76 +214,76 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
     acc16 o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) o[d] = zero16();
-    float top = -INFINITY, sum = 0.f;   // running maximum of the raw scores; this half's sum
+    float top = -INFINITY, sum = 0.f;   // running maximum of the raw scores (up to slack); this half's sum
+    const float slack = 8.f / a.c;
 
     const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
-    St st;
+    // what masks tile n is fetched a tile earlier than the tile itself
+    bool kept[Ld::kEach];
     float next_bias = 0.f;
+    auto fetch_masks = [&](int n) {
+        int j0 = 0, j_end = 0;
+        if (n < range.tiles) range.tile(n, BN, j0, j_end);
+#pragma unroll
+        for (int e = 0; e < Ld::kEach; ++e) {
+            const int j = j0 + Ld::row(e, wave, lane);
+            kept[e] = !keep || (j < j_end && keep[j]);
+        }
+        next_bias = j0 + tid < j_end && tid < BN && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
+    };
     auto fetch = [&](int n) {
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
-        st.load(kp, a.k.row, vp, a.v.row, keep, j0, j_end, a.dim, a.wide, tid);
-        if (tid < BN) next_bias = j0 + tid < j_end && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
-    };
-    auto put = [&](int n) {
-        st.store(lds[n & 1][0], lds[n & 1][1], tid);
+        Ld::load(lds[n & 1][0], lds[n & 1][1], kp, a.k.row, vp, a.v.row, j0, j_end, a.dim, a.wide, keep, kept, tid);
         if (tid < BN) bias[n & 1][tid] = next_bias;
     };
+    fetch_masks(0);
     fetch(0);
-    put(0);
-    __syncthreads();
+    fetch_masks(1);
+    tile_barrier();
     for (int n = 0; n < range.tiles; ++n) {
-        if (n + 1 < range.tiles) fetch(n + 1);
+        if (n + 1 < range.tiles) {
+            fetch(n + 1);
+            fetch_masks(n + 2);
+        }
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
-        const int j_last = min(j0 + BN, j_end) - 1;
-        const bool skip = !active || j0 > i_hi + a.right || (j_last < i_lo - a.left && j0 >= a.sinks);
-        if (!skip) {
-            const char* kt = lds[n & 1][0];
-            const char* vt = lds[n & 1][1];
-            const bool whole = !keep && j0 + BN <= j_end;
-            const bool edge = j_last > i_lo + a.right || (j0 < i_hi - a.left && j_last >= a.sinks);
-            acc16 s[BN / 32];
+        const char* kt = lds[n & 1][0];
+        const char* vt = lds[n & 1][1];
 #pragma unroll
-            for (int kb = 0; kb < BN / 32; ++kb) {
-                s[kb] = whole ? zero16() : start_scores(bias[n & 1], kb, h);
+        for (int kb = 0; kb < BN / 32; ++kb) {
+            const int j = j0 + 32 * kb;
+            if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
+            acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[n & 1] : nullptr, lane);
+            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges(s, a, i, j, h);
+            float mx = s[0];
 #pragma unroll
-                for (int x = 0; x < DP / 16; ++x) s[kb] = mma(read8<T, RB>(kt, 32 * kb + m, 2 * x + h), qf[x], s[kb]);
-            }
-            if (edge) {
-#pragma unroll
-                for (int kb = 0; kb < BN / 32; ++kb) hide_edges(s[kb], a, i, j0, kb, h);
-            }
-            float mx = s[0][0];
-#pragma unroll
-            for (int kb = 0; kb < BN / 32; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-            const float now = fmaxf(top, half_max(mx));
-            const float base = now == -INFINITY ? 0.f : now * a.c;
-            if (__any(now != top)) {
-                const float alpha = exp2_(fmaf(top, a.c, -base));
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+            mx = half_max(mx);
+            // the maximum may lag by 8 powers of two: sums and outputs are
+            // rescaled when it grows by more, which is rare after the first keys
+            if (__any(mx > top + slack)) {
+                const float now = fmaxf(top, mx), alpha = now == -INFINITY ? 1.f : exp2_((top - now) * a.c);
                 sum *= alpha;
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
                 top = now;
             }
+            const float base = top == -INFINITY ? 0.f : top * a.c;
 #pragma unroll
-            for (int kb = 0; kb < BN / 32; ++kb)
+            for (int r = 0; r < 16; ++r) {
+                s[r] = exp2_(fmaf(s[r], a.c, -base));
+                sum += s[r];
+            }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[kb][r] = exp2_(fmaf(s[kb][r], a.c, -base));
-                    sum += s[kb][r];
-                }
+            for (int x = 0; x < 2; ++x) {
+                const frag<T> p = narrow<T>(s, x);
 #pragma unroll
-            for (int x = 0; x < BN / 16; ++x) {
-                const frag<T> p = narrow<T>(s[x / 2], x % 2);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) o[d] = mma(read_turned<T, RB>(vt, 16 * x, 32 * d, lane), p, o[d]);
+                for (int d = 0; d < DP / 32; ++d)
+                    o[d] = mma(read_turned<T, RB>(vt, 32 * kb + 16 * x, 32 * d, lane), p, o[d]);
             }
         }
-        if (n + 1 < range.tiles) put(n + 1);
-        __syncthreads();
+        tile_barrier();
     }
     const float total = half_sum(sum);
     const float inv = total == 0.f ? 0.f : 1.f / total;
@@ -264,8 +304,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
 template <class T, int DP>
 __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs a) {
     constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
-    typedef Stage<T, DP, BN> St;
-    __shared__ __align__(128) char lds[2][2][St::kBytes];
+    typedef Loader<T, DP, BN> Ld;
+    __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float bias[2][BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
 
@@ -310,58 +350,60 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
     for (int d = 0; d < DP / 32; ++d) g[d] = zero16();
 
     const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
-    St st;
+    // what masks tile n is fetched a tile earlier than the tile itself
+    bool kept[Ld::kEach];
     float next_bias = 0.f;
+    auto fetch_masks = [&](int n) {
+        int j0 = 0, j_end = 0;
+        if (n < range.tiles) range.tile(n, BN, j0, j_end);
+#pragma unroll
+        for (int e = 0; e < Ld::kEach; ++e) {
+            const int j = j0 + Ld::row(e, wave, lane);
+            kept[e] = !keep || (j < j_end && keep[j]);
+        }
+        next_bias = j0 + tid < j_end && tid < BN && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
+    };
     auto fetch = [&](int n) {
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
-        st.load(kp, a.k.row, vp, a.v.row, keep, j0, j_end, a.dim, a.wide, tid);
-        if (tid < BN) next_bias = j0 + tid < j_end && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
-    };
-    auto put = [&](int n) {
-        st.store(lds[n & 1][0], lds[n & 1][1], tid);
+        Ld::load(lds[n & 1][0], lds[n & 1][1], kp, a.k.row, vp, a.v.row, j0, j_end, a.dim, a.wide, keep, kept, tid);
         if (tid < BN) bias[n & 1][tid] = next_bias;
     };
+    fetch_masks(0);
     fetch(0);
-    put(0);
-    __syncthreads();
+    fetch_masks(1);
+    tile_barrier();
     for (int n = 0; n < range.tiles; ++n) {
-        if (n + 1 < range.tiles) fetch(n + 1);
+        if (n + 1 < range.tiles) {
+            fetch(n + 1);
+            fetch_masks(n + 2);
+        }
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
-        const int j_last = min(j0 + BN, j_end) - 1;
-        const bool skip = !active || j0 > i_hi + a.right || (j_last < i_lo - a.left && j0 >= a.sinks);
-        if (!skip) {
-            const char* kt = lds[n & 1][0];
-            const char* vt = lds[n & 1][1];
-            const bool whole = !keep && j0 + BN <= j_end;
-            const bool edge = j_last > i_lo + a.right || (j0 < i_hi - a.left && j_last >= a.sinks);
+        const char* kt = lds[n & 1][0];
+        const char* vt = lds[n & 1][1];
 #pragma unroll
-            for (int kb = 0; kb < BN / 32; ++kb) {
-                acc16 s = whole ? zero16() : start_scores(bias[n & 1], kb, h), dp = zero16();
+        for (int kb = 0; kb < BN / 32; ++kb) {
+            const int j = j0 + 32 * kb;
+            if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
+            acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[n & 1] : nullptr, lane);
+            const acc16 dp = scores<T, DP>(vt, 32 * kb, gf, nullptr, lane);
+            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges(s, a, i, j, h);
+            // p is 0 for hidden keys; what dp holds there must not turn it into NaN
 #pragma unroll
-                for (int x = 0; x < DP / 16; ++x) {
-                    s = mma(read8<T, RB>(kt, 32 * kb + m, 2 * x + h), qf[x], s);
-                    dp = mma(read8<T, RB>(vt, 32 * kb + m, 2 * x + h), gf[x], dp);
-                }
-                if (edge) hide_edges(s, a, i, j0, kb, h);
-                // p is 0 for hidden keys; what dp holds there must not turn it into NaN
+            for (int r = 0; r < 16; ++r) {
+                const float p = exp2_(fmaf(s[r], a.c, -lse));
+                s[r] = p == 0.f ? 0.f : p * (dp[r] - delta);
+            }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float p = exp2_(fmaf(s[r], a.c, -lse));
-                    s[r] = p == 0.f ? 0.f : p * (dp[r] - delta);
-                }
+            for (int x = 0; x < 2; ++x) {
+                const frag<T> ds = narrow<T>(s, x);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const frag<T> ds = narrow<T>(s, x);
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d)
-                        g[d] = mma(read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane), ds, g[d]);
-                }
+                for (int d = 0; d < DP / 32; ++d)
+                    g[d] = mma(read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane), ds, g[d]);
             }
         }
-        if (n + 1 < range.tiles) put(n + 1);
-        __syncthreads();
+        tile_barrier();
     }
     T* out = mine ? row_of<T>(a.dq, b, t.start + i, head) : nullptr;
 #pragma unroll
@@ -433,8 +475,8 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 template <class T, int DP>
 __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2) void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = kv_tile<T, DP>();
-    typedef Stage<T, DP, BQ> St;
-    __shared__ __align__(128) char lds[2][2][St::kBytes];
+    typedef Loader<T, DP, BQ> Ld;
+    __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float row_lse[2][BQ], row_delta[2][BQ];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
 
@@ -466,31 +508,36 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     const int i_end = static_cast<int64_t>(k0) + kQueries + a.left < len ? k0 + kQueries + a.left : len;
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
     const unsigned span = j < a.sinks ? 0x7fffffffu : static_cast<unsigned>(a.left) + a.right;
-    St st;
     float next_lse = 0.f, next_delta = 0.f;
-    auto fetch = [&](int n) {
-        const int head = kv * group + n / q_tiles, i0 = i_begin + n % q_tiles * BQ;
-        st.load(row_of<T>(a.q, b, t.start, head), a.q.row, row_of<T>(a.d_o, b, t.start, head), a.d_o.row, nullptr, i0,
-                i_end, a.dim, a.wide, tid);
-        if (tid < BQ) {
-            const int64_t at = (b * a.heads + head) * a.rows + t.start + i0 + tid;
-            const bool there = i0 + tid < i_end;
-            next_lse = there ? a.stats[at] : INFINITY;
-            next_delta = there ? a.delta[at] : 0.f;
+    bool every[Ld::kEach];
+#pragma unroll
+    for (int e = 0; e < Ld::kEach; ++e) every[e] = true;
+    auto fetch_stats = [&](int n) {
+        if (n < total && tid < BQ) {
+            const int head = kv * group + n / q_tiles, i = i_begin + n % q_tiles * BQ + tid;
+            const int64_t at = (b * a.heads + head) * a.rows + t.start + i;
+            next_lse = i < i_end ? a.stats[at] : INFINITY;
+            next_delta = i < i_end ? a.delta[at] : 0.f;
         }
     };
-    auto put = [&](int n) {
-        st.store(lds[n & 1][0], lds[n & 1][1], tid);
+    auto fetch = [&](int n) {
+        const int head = kv * group + n / q_tiles, i0 = i_begin + n % q_tiles * BQ;
+        Ld::load(lds[n & 1][0], lds[n & 1][1], row_of<T>(a.q, b, t.start, head), a.q.row,
+                 row_of<T>(a.d_o, b, t.start, head), a.d_o.row, i0, i_end, a.dim, a.wide, nullptr, every, tid);
         if (tid < BQ) {
             row_lse[n & 1][tid] = next_lse;
             row_delta[n & 1][tid] = next_delta;
         }
     };
+    fetch_stats(0);
     fetch(0);
-    put(0);
-    __syncthreads();
+    fetch_stats(1);
+    tile_barrier();
     for (int n = 0; n < total; ++n) {
-        if (n + 1 < total) fetch(n + 1);
+        if (n + 1 < total) {
+            fetch(n + 1);
+            fetch_stats(n + 2);
+        }
         const int i0 = i_begin + n % q_tiles * BQ;
 #pragma unroll
         for (int qb = 0; qb < BQ / 32; ++qb) {
@@ -503,8 +550,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
                                 a.c, edge, j - a.right - i_lo, span, lane);
             }
         }
-        if (n + 1 < total) put(n + 1);
-        __syncthreads();
+        tile_barrier();
     }
     // the far queries' share of the sinks
     if (j_lo < a.sinks && active) {
@@ -548,8 +594,8 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
 template <class T, int DP>
 __global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
     constexpr int BQ = sizeof(T) == 4 && DP > 64 ? 64 : 128;
-    typedef Stage<T, DP, BQ> St;
-    __shared__ __align__(128) char lds[2][St::kBytes];
+    typedef Loader<T, DP, BQ> Ld;
+    __shared__ __align__(1024) char lds[2][Ld::kBytes];
     __shared__ __align__(16) float row_lse[BQ], row_delta[BQ];
     __shared__ __align__(16) float joined[2][DP][33];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
@@ -582,17 +628,18 @@ __global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
         const int head = kv * group + g;
         const int64_t at = (b * a.heads + head) * a.rows + t.start;
         for (int i0 = i_begin; i0 < i_end; i0 += BQ) {
-            St st;
-            st.load(row_of<T>(a.q, b, t.start, head), a.q.row, row_of<T>(a.d_o, b, t.start, head), a.d_o.row, nullptr,
-                    i0, i_end, a.dim, a.wide, tid);
+            bool every[Ld::kEach];
+#pragma unroll
+            for (int e = 0; e < Ld::kEach; ++e) every[e] = true;
             __syncthreads();   // the previous tile has been read
-            st.store(lds[0], lds[1], tid);
+            Ld::load(lds[0], lds[1], row_of<T>(a.q, b, t.start, head), a.q.row, row_of<T>(a.d_o, b, t.start, head),
+                     a.d_o.row, i0, i_end, a.dim, a.wide, nullptr, every, tid);
             if (tid < BQ) {
                 const bool there = i0 + tid < i_end;
                 row_lse[tid] = there ? a.stats[at + i0 + tid] : INFINITY;
                 row_delta[tid] = there ? a.delta[at + i0 + tid] : 0.f;
             }
-            __syncthreads();
+            tile_barrier();
             if (32 * wave < BQ && i0 + 32 * wave < i_end)
                 key_grad<T, DP>(lds[0], lds[1], row_lse, row_delta, 32 * wave, kf, vf, dk, dv, a.c, false, 0, 0, lane);
         }
