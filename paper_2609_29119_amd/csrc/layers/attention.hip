@@ -22,7 +22,7 @@ extern "C" int nsgcqt_band_attention(int dtype, const nsgcqt_rows* r, const nsgc
     a.v = view_of(v);
     a.o = view_of(o);
     a.stats = stats;
-    const int64_t blocks = tile_count<kQueryShift>(a.n_bands, 1, a.rows) * a.batch * a.heads;
+    const int64_t blocks = query_blocks(a);
     CHECK_TRY(check_grid(blocks));
     return by_type_and_width(dtype, s->head_dim, [&](auto t, auto dp) -> int {
         LAUNCH_TRY(k_attention<decltype(t), decltype(dp)::value>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0,

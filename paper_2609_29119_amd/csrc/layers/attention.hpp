@@ -18,8 +18,8 @@ struct AttnArgs {
     const uint8_t* keep;
     int64_t keep_batch;
     const int64_t* off;
-    int64_t rows;
-    int n_bands, batch, heads, kv_heads, dim;
+    int rows, n_bands, batch, heads, kv_heads, dim;
+    int share;            // heads of one kv head that a workgroup takes: 1, 2 or 4
     int left, right, sinks;   // at most rows
     float scale, c;           // c = scale log2(e): exp(scale s) = exp2(c s)
     bool wide;                // every view takes 16-byte accesses
@@ -27,7 +27,12 @@ struct AttnArgs {
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-constexpr int kQueries = 128, kQueryShift = 7;   // queries (or keys, in the key gradient) of a workgroup: 4 waves of 32
+// A workgroup has four waves of 32 rows each. Forward and dq: `share` heads of
+// one kv head, 128 / share queries of each, so that the waves need (nearly)
+// the same keys: with a window of 256 and four heads a workgroup walks 287
+// keys and not 383. The key gradient: 128 keys of one kv head.
+constexpr int kKeys = 128, kKeyShift = 7;
+__host__ __device__ inline int query_shift(int share) { return share == 4 ? 5 : share == 2 ? 6 : 7; }
 template <class T, int DP> constexpr int kv_tile() { return sizeof(T) == 4 && DP > 64 ? 32 : 64; }
 
 template <class T> __device__ inline T* row_of(const View& v, int64_t b, int64_t row, int head) {
@@ -85,7 +90,7 @@ template <class T, int DP, int BN> struct Loader {
     // kept: for each load, whether its row may be used (wide only)
     static __device__ void load(char* tx, char* ty, const T* px, int64_t sx, const T* py, int64_t sy, int row0,
                                 int row_end, int dim, bool wide, const uint8_t* keep, const bool (&kept)[kEach], int tid) {
-        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int lane = tid & 63, wave = wave_number();
         px += row0 * sx;
         py += row0 * sy;
         if (wide) {
@@ -173,13 +178,31 @@ __device__ inline void load_rows(frag<T> (&f)[DP / 16], const T* p, bool there, 
     }
 }
 
-// Zeros for the rows [first, first + 128) of tokens that no band holds.
+// Zeros for `count` rows from `first` on (below len) of tokens that no band holds.
 template <class T>
-__device__ inline void zero_rows(const View& v, int64_t b, int head, int64_t start, int64_t first, int64_t len, int dim,
+__device__ inline void zero_rows(const View& v, int64_t b, int head, int start, int first, int count, int len, int dim,
                                  int tid) {
-    for (int64_t r = first; r < first + kQueries && r < len; ++r)
+    for (int r = first; r < first + count && r < len; ++r)
         for (int d = tid; d < dim; d += 256) row_of<T>(v, b, start + r, head)[d] = static_cast<T>(0.f);
 }
+
+// What a workgroup of the forward or the dq kernel works on.
+struct QueryWork {
+    int b, kv, head0, head, i_lo, queries;
+    Tile<int> t;
+    __device__ QueryWork(const AttnArgs& a, int wave, int lane) {
+        const int group = a.heads / a.kv_heads, parts = group / a.share, shift = query_shift(a.share);
+        const unsigned id = die_order(blockIdx.x, gridDim.x), units = a.kv_heads * parts, unit = id % units, rest = id / units;
+        const unsigned per = static_cast<unsigned>(tile_count(shift, a.n_bands, 1, a.rows));
+        b = rest / per;
+        kv = unit / parts;
+        head0 = kv * group + unit % parts * a.share;
+        queries = 1 << shift;
+        t = find_tile<int>(a.off, a.n_bands, a.rows, 1, shift, rest - b * per, lane);
+        head = head0 + (wave & (a.share - 1));
+        i_lo = t.first + 32 * (wave >> (7 - shift));
+    }
+};
 
 template <class T, int DP>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_attention(AttnArgs a) {
@@ -187,24 +210,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
     typedef Loader<T, DP, BN> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float bias[2][BN];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
-    int64_t w = die_order(blockIdx.x, gridDim.x);
-    const int head = static_cast<int>(w % a.heads);
-    w /= a.heads;
-    const int64_t per = tile_count<kQueryShift>(a.n_bands, 1, a.rows), b = w / per;
-    const Tile t = find_tile<kQueryShift>(a.off, a.n_bands, a.rows, 1, w % per, lane);
+    const QueryWork w(a, wave, lane);
+    const Tile<int>& t = w.t;
     if (!t.live) return;
-    const int len = static_cast<int>(t.len), q0 = static_cast<int>(t.first), kv = head / (a.heads / a.kv_heads);
+    const int64_t b = w.b;
+    const int len = t.len, q0 = t.first, kv = w.kv, head = w.head;
     float* stats = a.stats ? a.stats + (b * a.heads + head) * a.rows + t.start : nullptr;
+    const int i_lo = w.i_lo, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
+    const bool mine = i < len, active = i_lo < len;
     if (t.band < 0 || t.band >= a.n_bands) {
-        zero_rows<T>(a.o, b, head, t.start, t.first, t.len, a.dim, tid);
-        if (stats && tid < kQueries && q0 + tid < len) stats[q0 + tid] = INFINITY;
+        for (int x = 0; x < a.share; ++x)
+            zero_rows<T>(a.o, b, w.head0 + x, t.start, q0, w.queries, len, a.dim, tid);
+        if (stats && mine && h == 0) stats[i] = INFINITY;
         return;
     }
-
-    const int i_lo = q0 + 32 * wave, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
-    const bool mine = i < len, active = i_lo < len;
     frag<T> qf[DP / 16];
     load_rows<T, DP>(qf, row_of<T>(a.q, b, t.start + (mine ? i : 0), head), mine, a.dim, a.wide, lane);
     const T* kp = row_of<T>(a.k, b, t.start, kv);
@@ -217,7 +238,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
     float top = -INFINITY, sum = 0.f;   // running maximum of the raw scores (up to slack); this half's sum
     const float slack = 8.f / a.c;
 
-    const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
+    const KeyRange range(a, q0, min(q0 + w.queries, len) - 1, len, BN);
     // what masks tile n is fetched a tile earlier than the tile itself
     bool kept[Ld::kEach];
     float next_bias = 0.f;
@@ -307,22 +328,20 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
     typedef Loader<T, DP, BN> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float bias[2][BN];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
-    int64_t w = die_order(blockIdx.x, gridDim.x);
-    const int head = static_cast<int>(w % a.heads);
-    w /= a.heads;
-    const int64_t per = tile_count<kQueryShift>(a.n_bands, 1, a.rows), b = w / per;
-    const Tile t = find_tile<kQueryShift>(a.off, a.n_bands, a.rows, 1, w % per, lane);
+    const QueryWork w(a, wave, lane);
+    const Tile<int>& t = w.t;
     if (!t.live) return;
+    const int64_t b = w.b;
+    const int len = t.len, q0 = t.first, kv = w.kv, head = w.head;
     if (t.band < 0 || t.band >= a.n_bands) {
-        zero_rows<T>(a.dq, b, head, t.start, t.first, t.len, a.dim, tid);
+        for (int x = 0; x < a.share; ++x)
+            zero_rows<T>(a.dq, b, w.head0 + x, t.start, q0, w.queries, len, a.dim, tid);
         return;
     }
-    const int len = static_cast<int>(t.len), q0 = static_cast<int>(t.first), kv = head / (a.heads / a.kv_heads);
     const int64_t at = (b * a.heads + head) * a.rows + t.start;
-
-    const int i_lo = q0 + 32 * wave, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
+    const int i_lo = w.i_lo, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
     const bool mine = i < len, active = i_lo < len;
     const int64_t row = t.start + (mine ? i : 0);
     frag<T> qf[DP / 16], gf[DP / 16];
@@ -349,7 +368,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) g[d] = zero16();
 
-    const KeyRange range(a, q0, min(q0 + kQueries, len) - 1, len, BN);
+    const KeyRange range(a, q0, min(q0 + w.queries, len) - 1, len, BN);
     // what masks tile n is fetched a tile earlier than the tile itself
     bool kept[Ld::kEach];
     float next_bias = 0.f;
@@ -417,12 +436,12 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
 // tile's last key ("far" ones) would make one workgroup walk a whole band, so
 // k_attention_far takes them in chunks and leaves partial dk, dv, which the
 // workgroup of the key tile adds up in the chunks' order.
-constexpr int kFarShift = 10;   // queries of a chunk
-__device__ inline int64_t far_begin(const AttnArgs& a, int sink_tile) {   // of 32 keys
-    return static_cast<int64_t>(sink_tile * 32 / kQueries * kQueries) + kQueries + a.left;
+constexpr int kFarShift = 9;   // queries of a chunk
+__device__ inline int far_begin(const AttnArgs& a, int sink_tile) {   // of 32 keys
+    return sink_tile * 32 / kKeys * kKeys + kKeys + a.left;
 }
 __device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t item, int sink_tile) {
-    const int64_t per = tile_count<kFarShift>(a.n_bands, 1, a.rows);
+    const int64_t per = tile_count(kFarShift, a.n_bands, 1, a.rows);
     const int n = (a.sinks + 31) / 32;
     return a.part + (((b * a.kv_heads + kv) * per + item) * n + sink_tile) * (2 * 32 * a.dim);
 }
@@ -478,20 +497,21 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     typedef Loader<T, DP, BQ> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float row_lse[2][BQ], row_delta[2][BQ];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
-    int64_t w = die_order(blockIdx.x, gridDim.x);
-    const int kv = static_cast<int>(w % a.kv_heads);
-    w /= a.kv_heads;
-    const int64_t per = tile_count<kQueryShift>(a.n_bands, 1, a.rows), b = w / per;
-    const Tile t = find_tile<kQueryShift>(a.off, a.n_bands, a.rows, 1, w % per, lane);
+    const unsigned id = die_order(blockIdx.x, gridDim.x), rest = id / a.kv_heads;
+    const unsigned per = static_cast<unsigned>(tile_count(kKeyShift, a.n_bands, 1, a.rows));
+    const int kv = id - rest * a.kv_heads;
+    const int64_t b = rest / per;
+    const Tile<int> t =
+        find_tile<int>(a.off, a.n_bands, a.rows, 1, kKeyShift, rest - static_cast<unsigned>(b) * per, lane);
     if (!t.live) return;
+    const int len = t.len, k0 = t.first, group = a.heads / a.kv_heads;
     if (t.band < 0 || t.band >= a.n_bands) {
-        zero_rows<T>(a.dk, b, kv, t.start, t.first, t.len, a.dim, tid);
-        zero_rows<T>(a.dv, b, kv, t.start, t.first, t.len, a.dim, tid);
+        zero_rows<T>(a.dk, b, kv, t.start, k0, kKeys, len, a.dim, tid);
+        zero_rows<T>(a.dv, b, kv, t.start, k0, kKeys, len, a.dim, tid);
         return;
     }
-    const int len = static_cast<int>(t.len), k0 = static_cast<int>(t.first), group = a.heads / a.kv_heads;
     const int j_lo = k0 + 32 * wave, j = j_lo + m, j_hi = min(j_lo + 31, len - 1);
     const bool mine = j < len, active = j_lo < len;
     const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
@@ -505,7 +525,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
 
     const int i_begin = k0 > a.right ? k0 - a.right : 0;
-    const int i_end = static_cast<int64_t>(k0) + kQueries + a.left < len ? k0 + kQueries + a.left : len;
+    const int i_end = min(k0 + kKeys + a.left, len);
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
     const unsigned span = j < a.sinks ? 0x7fffffffu : static_cast<unsigned>(a.left) + a.right;
     float next_lse = 0.f, next_delta = 0.f;
@@ -555,10 +575,10 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     // the far queries' share of the sinks
     if (j_lo < a.sinks && active) {
         const int tile = j_lo / 32;
-        const int64_t begin = far_begin(a, tile);
+        const int begin = far_begin(a, tile);
         const int64_t item0 = (t.start >> kFarShift) + t.band + 1;
         if (begin < len)
-            for (int64_t ch = begin >> kFarShift; ch <= (len - 1) >> kFarShift; ++ch) {
+            for (int ch = begin >> kFarShift; ch <= (len - 1) >> kFarShift; ++ch) {
                 const float* p = far_part(a, b, kv, item0 + ch, tile) + m * a.dim;
                 if (j < a.sinks && mine) {
 #pragma unroll
@@ -592,28 +612,25 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
 // has the same keys and takes a quarter of the queries; the four results are
 // added in the waves' order.
 template <class T, int DP>
-__global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
+__global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2) void k_attention_far(AttnArgs a) {
     constexpr int BQ = sizeof(T) == 4 && DP > 64 ? 64 : 128;
     typedef Loader<T, DP, BQ> Ld;
-    __shared__ __align__(1024) char lds[2][Ld::kBytes];
-    __shared__ __align__(16) float row_lse[BQ], row_delta[BQ];
-    __shared__ __align__(16) float joined[2][DP][33];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    __shared__ __align__(1024) char lds[2][2 * Ld::kBytes];
+    __shared__ __align__(16) float row_lse[2][BQ], row_delta[2][BQ];
+    static_assert(sizeof(lds) >= 2 * DP * 33 * 4, "the tiles' room also serves to add up the waves");
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
-    const int n_sink = (a.sinks + 31) / 32;
-    int64_t w = die_order(blockIdx.x, gridDim.x);
-    const int tile = static_cast<int>(w % n_sink);
-    w /= n_sink;
-    const int kv = static_cast<int>(w % a.kv_heads);
-    w /= a.kv_heads;
-    const int64_t per = tile_count<kFarShift>(a.n_bands, 1, a.rows), b = w / per, item = w % per;
-    const Tile t = find_tile<kFarShift>(a.off, a.n_bands, a.rows, 1, item, lane);
+    const unsigned n_sink = (a.sinks + 31) / 32, id = die_order(blockIdx.x, gridDim.x);
+    const int tile = id % n_sink, kv = id / n_sink % a.kv_heads;
+    const unsigned rest = id / n_sink / a.kv_heads;
+    const unsigned per = static_cast<unsigned>(tile_count(kFarShift, a.n_bands, 1, a.rows));
+    const int64_t b = rest / per;
+    const int item = rest - static_cast<unsigned>(b) * per;
+    const Tile<int> t = find_tile<int>(a.off, a.n_bands, a.rows, 1, kFarShift, item, lane);
     if (!t.live || t.band < 0 || t.band >= a.n_bands) return;
-    const int len = static_cast<int>(t.len), group = a.heads / a.kv_heads, j = 32 * tile + m;
-    const int64_t far = far_begin(a, tile);
-    const int i_end = min(static_cast<int>(t.first) + (1 << kFarShift), len);
-    if (far >= i_end) return;
-    const int i_begin = max(static_cast<int>(t.first), static_cast<int>(far));
+    const int len = t.len, group = a.heads / a.kv_heads, j = 32 * tile + m, far = far_begin(a, tile);
+    const int i_begin = max(t.first, far), i_end = min(t.first + (1 << kFarShift), len);
+    if (i_begin >= i_end) return;
     const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
     const bool kept = j < a.sinks && j < len && (!keep || keep[j]);
     const int64_t row = t.start + (j < len ? j : 0);
@@ -624,26 +641,31 @@ __global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
 
-    for (int g = 0; g < group; ++g) {
-        const int head = kv * group + g;
-        const int64_t at = (b * a.heads + head) * a.rows + t.start;
-        for (int i0 = i_begin; i0 < i_end; i0 += BQ) {
-            bool every[Ld::kEach];
+    const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
+    bool every[Ld::kEach];
 #pragma unroll
-            for (int e = 0; e < Ld::kEach; ++e) every[e] = true;
-            __syncthreads();   // the previous tile has been read
-            Ld::load(lds[0], lds[1], row_of<T>(a.q, b, t.start, head), a.q.row, row_of<T>(a.d_o, b, t.start, head),
-                     a.d_o.row, i0, i_end, a.dim, a.wide, nullptr, every, tid);
-            if (tid < BQ) {
-                const bool there = i0 + tid < i_end;
-                row_lse[tid] = there ? a.stats[at + i0 + tid] : INFINITY;
-                row_delta[tid] = there ? a.delta[at + i0 + tid] : 0.f;
-            }
-            tile_barrier();
-            if (32 * wave < BQ && i0 + 32 * wave < i_end)
-                key_grad<T, DP>(lds[0], lds[1], row_lse, row_delta, 32 * wave, kf, vf, dk, dv, a.c, false, 0, 0, lane);
+    for (int e = 0; e < Ld::kEach; ++e) every[e] = true;
+    auto fetch = [&](int n) {
+        const int head = kv * group + n / q_tiles, i0 = i_begin + n % q_tiles * BQ;
+        Ld::load(lds[n & 1], lds[n & 1] + Ld::kBytes, row_of<T>(a.q, b, t.start, head), a.q.row,
+                 row_of<T>(a.d_o, b, t.start, head), a.d_o.row, i0, i_end, a.dim, a.wide, nullptr, every, tid);
+        if (tid < BQ) {
+            const int64_t at = (b * a.heads + head) * a.rows + t.start + i0 + tid;
+            const bool there = i0 + tid < i_end;
+            row_lse[n & 1][tid] = there ? a.stats[at] : INFINITY;
+            row_delta[n & 1][tid] = there ? a.delta[at] : 0.f;
         }
+    };
+    fetch(0);
+    tile_barrier();
+    for (int n = 0; n < total; ++n) {
+        if (n + 1 < total) fetch(n + 1);
+        if (32 * wave < BQ && i_begin + n % q_tiles * BQ + 32 * wave < i_end)
+            key_grad<T, DP>(lds[n & 1], lds[n & 1] + Ld::kBytes, row_lse[n & 1], row_delta[n & 1], 32 * wave, kf, vf, dk,
+                            dv, a.c, false, 0, 0, lane);
+        tile_barrier();
     }
+    float(*joined)[DP][33] = reinterpret_cast<float(*)[DP][33]>(&lds[0][0]);
     for (int v = 0; v < 4; ++v) {
         if (wave == v) {
 #pragma unroll
@@ -657,10 +679,11 @@ __global__ __launch_bounds__(256, 1) void k_attention_far(AttnArgs a) {
         }
         __syncthreads();
     }
+    const int keys = min(32, a.sinks - 32 * tile);
     float* out = far_part(a, b, kv, item, tile);
     for (int x = tid; x < 2 * 32 * a.dim; x += 256) {
         const int c = x % a.dim, key = x / a.dim % 32;
-        out[x] = joined[x / (32 * a.dim)][c][key];
+        if (key < keys) out[x] = joined[x / (32 * a.dim)][c][key];
     }
 }
 

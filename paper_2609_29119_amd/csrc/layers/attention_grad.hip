@@ -7,15 +7,15 @@ namespace {
 
 int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
-int64_t delta_bytes(const AttnArgs& a) { return align256(4 * a.rows * a.batch * a.heads); }
+int64_t delta_bytes(const AttnArgs& a) { return align256(int64_t(4) * a.rows * a.batch * a.heads); }
 
 int64_t part_bytes(const AttnArgs& a) {
-    return 4 * tile_count<kFarShift>(a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32) * 2 * 32 *
+    return int64_t(4) * tile_count(kFarShift, a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32) * 2 * 32 *
            a.dim;
 }
 
 // Whether some query lies past the window of some sink's key tile.
-bool has_far(const AttnArgs& a) { return a.sinks > 0 && int64_t(kQueries) + a.left < a.rows; }
+bool has_far(const AttnArgs& a) { return a.sinks > 0 && kKeys + a.left < a.rows; }
 
 }  // namespace
 
@@ -57,17 +57,18 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
     a.stats = const_cast<float*>(stats);
     a.delta = static_cast<float*>(ws);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + delta_bytes(a));
-    const int64_t tiles = tile_count<kQueryShift>(a.n_bands, 1, a.rows) * a.batch;
-    const int64_t far = tile_count<kFarShift>(a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32);
-    CHECK_TRY(check_grid(tiles * a.heads));
+    const int64_t queries = query_blocks(a), keys = tile_count(kKeyShift, a.n_bands, 1, a.rows) * a.batch * a.kv_heads;
+    const int64_t far = tile_count(kFarShift, a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32);
+    CHECK_TRY(check_grid(queries));
+    CHECK_TRY(check_grid(keys));
     CHECK_TRY(check_grid(far));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_type_and_width(dtype, s->head_dim, [&](auto t, auto dp) -> int {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
-        LAUNCH_TRY(k_attention_dq<T, DP>, dim3(static_cast<unsigned>(tiles * a.heads)), dim3(256), 0, st, a);
+        LAUNCH_TRY(k_attention_dq<T, DP>, dim3(static_cast<unsigned>(queries)), dim3(256), 0, st, a);
         if (has_far(a)) LAUNCH_TRY(k_attention_far<T, DP>, dim3(static_cast<unsigned>(far)), dim3(256), 0, st, a);
-        LAUNCH_TRY(k_attention_dkv<T, DP>, dim3(static_cast<unsigned>(tiles * a.kv_heads)), dim3(256), 0, st, a);
+        LAUNCH_TRY(k_attention_dkv<T, DP>, dim3(static_cast<unsigned>(keys)), dim3(256), 0, st, a);
         return NSGCQT_OK;
     });
 }

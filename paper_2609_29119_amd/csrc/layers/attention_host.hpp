@@ -25,12 +25,14 @@ inline AttnArgs attention_args(const nsgcqt_rows* r, const nsgcqt_attention_shap
     a.keep = s->keep;
     a.keep_batch = s->keep_batch;
     a.off = r->offsets;
-    a.rows = r->rows;
+    a.rows = static_cast<int>(r->rows);
     a.n_bands = static_cast<int>(r->n_bands);
     a.batch = static_cast<int>(r->batch);
     a.heads = static_cast<int>(s->n_heads);
     a.kv_heads = static_cast<int>(s->n_kv_heads);
     a.dim = static_cast<int>(s->head_dim);
+    const int group = a.heads / a.kv_heads;
+    a.share = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
     auto cut = [&](int64_t v) { return static_cast<int>(v < r->rows ? v : r->rows); };
     a.left = cut(s->left);
     a.right = cut(s->right);
@@ -38,6 +40,11 @@ inline AttnArgs attention_args(const nsgcqt_rows* r, const nsgcqt_attention_shap
     a.scale = static_cast<float>(s->scale);
     a.c = static_cast<float>(s->scale * 1.4426950408889634);
     return a;
+}
+
+// Workgroups of the kernels that go by queries.
+inline int64_t query_blocks(const AttnArgs& a) {
+    return tile_count(query_shift(a.share), a.n_bands, 1, a.rows) * a.batch * (a.heads / a.share);
 }
 
 // f(T(), DP) with the head width's padded size as an integral constant

@@ -17,7 +17,7 @@ int check_linear(int dtype, const nsgcqt_rows* r, int64_t n_in, int64_t n_out) {
 LinearArgs linear_args(const nsgcqt_rows* r, int64_t n_in, int64_t n_out) {
     LinearArgs a{};
     a.off = r->offsets;
-    a.rows = r->rows;
+    a.rows = static_cast<int>(r->rows);
     a.n_bands = static_cast<int>(r->n_bands);
     a.batch = static_cast<int>(r->batch);
     a.n_in = static_cast<int>(n_in);
@@ -49,7 +49,7 @@ int run_linear(int dtype, const nsgcqt_rows* r, const nsgcqt_view* in, const voi
     a.w = w;
     a.bias = bias;
     a.w_wide = n_in % 8 == 0 && !misaligned(w, 16);
-    const int64_t tiles = tile_count<kRowShift>(a.n_bands, a.batch, a.rows);
+    const int64_t tiles = tile_count(kRowShift, a.n_bands, a.batch, a.rows);
     return by_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
         auto go = [&](auto nb) -> int {
@@ -84,7 +84,7 @@ int64_t nsgcqt_band_linear_workspace(int64_t n_bands, int64_t batch, int64_t row
     static const int64_t none = 0;
     const nsgcqt_rows r{&none, n_bands, batch, rows};
     CHECK_TRY(check_linear(NSGCQT_F32, &r, n_in, n_out));
-    return 4 * tile_count<kChunkShift>(n_bands, batch, rows) * (n_in * n_out + n_out);
+    return 4 * tile_count(kChunkShift, n_bands, batch, rows) * (n_in * n_out + n_out);
 }
 
 int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const nsgcqt_view* dy,
@@ -109,7 +109,7 @@ int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt
     a.part = static_cast<float*>(ws);
     // with no inputs there is still the sum of dy
     const int64_t ot = (n_out + 127) / 128, it = n_in ? (n_in + 127) / 128 : 1;
-    const int64_t blocks = tile_count<kChunkShift>(a.n_bands, a.batch, a.rows) * ot * it;
+    const int64_t blocks = tile_count(kChunkShift, a.n_bands, a.batch, a.rows) * ot * it;
     const int64_t join = (n_in * n_out + n_out + 255) / 256;
     CHECK_TRY(check_grid(blocks));
     if (r->n_bands > 65535) return set_err(NSGCQT_EUNSUPPORTED, "more than 65,535 bands in a gradient of weights");

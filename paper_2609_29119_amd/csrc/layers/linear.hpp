@@ -17,8 +17,7 @@ struct LinearArgs {
     void* db;
     float* part;          // partial dW (and db) of bands of several chunks
     const int64_t* off;
-    int64_t rows;
-    int n_bands, batch;
+    int rows, n_bands, batch;
     int n_in, n_out;      // of the layer, whichever direction is computed
     bool x_wide, y_wide, w_wide;
 };
@@ -26,7 +25,7 @@ struct LinearArgs {
 constexpr int kRowShift = 7;   // rows of a workgroup: 4 waves of 32
 template <class T> constexpr int step_width() { return 128 / static_cast<int>(sizeof(T)); }   // reduction of one LDS tile
 
-template <class T> __device__ inline T* band_row(const View& v, const Tile& t, int64_t r) {
+template <class T> __device__ inline T* band_row(const View& v, const Tile<int64_t>& t, int64_t r) {
     const int64_t b = r / t.len, c = r - b * t.len;
     return reinterpret_cast<T*>(v.data) + b * v.batch + (t.start + c) * v.row;
 }
@@ -41,14 +40,14 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinearArgs a) {
     constexpr int WR = BACK ? BK : BN, WC = BACK ? BN : BK;           // rows and columns of the tile of W
     constexpr int RB = row_bytes<T, WC>(), kChunks = WR * WC / 8, kEach = (kChunks + 255) / 256;
     __shared__ __align__(128) char lds[2][WR * RB];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int n_red = BACK ? a.n_out : a.n_in, n_col = BACK ? a.n_in : a.n_out, cols = (n_col + BN - 1) / BN;
 
-    const int64_t id = die_order(blockIdx.x, gridDim.x), p = id / cols;
-    const int c0 = static_cast<int>(id - p * cols) * BN;
-    const Tile t = find_tile<kRowShift>(a.off, a.n_bands, a.rows, a.batch, p, lane);
+    const unsigned id = die_order(blockIdx.x, gridDim.x), p = id / cols;
+    const int c0 = (id - p * cols) * BN;
+    const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, kRowShift, p, lane);
     if (!t.live) return;
-    const int64_t n_rows = t.len * a.batch, r = t.first + 32 * wave + m;
+    const int64_t n_rows = static_cast<int64_t>(t.len) * a.batch, r = t.first + 32 * wave + m;
     const bool mine = r < n_rows;
     T* out = mine ? band_row<T>(a.y, t, r) : nullptr;
     if (t.band < 0 || t.band >= a.n_bands) {
@@ -147,13 +146,13 @@ __global__ __launch_bounds__(256, 2) void k_linear_dw(LinearArgs a) {
     constexpr int kEach = BR * 16 / 256;
     __shared__ __align__(128) char lds[2][BR * RB];
     __shared__ float sums[16][128 + 4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int ot = (a.n_out + 127) / 128, it = max(1, (a.n_in + 127) / 128);
-    const int64_t id = die_order(blockIdx.x, gridDim.x), p = id / (ot * it);
-    const int o0 = static_cast<int>(id % (ot * it)) / it * 128, i0 = static_cast<int>(id % (ot * it)) % it * 128;
-    const Tile t = find_tile<kChunkShift>(a.off, a.n_bands, a.rows, a.batch, p, lane);
+    const unsigned id = die_order(blockIdx.x, gridDim.x), p = id / (ot * it), at2 = id - p * (ot * it);
+    const int o0 = at2 / it * 128, i0 = at2 % it * 128;
+    const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, kChunkShift, p, lane);
     if (!t.live || t.band < 0 || t.band >= a.n_bands) return;
-    const int64_t n_rows = t.len * a.batch;
+    const int64_t n_rows = static_cast<int64_t>(t.len) * a.batch;
     const int64_t r_end = min(t.first + (int64_t(1) << kChunkShift), n_rows);
     const int wo = wave >> 1 << 6, wi = (wave & 1) << 6;
 

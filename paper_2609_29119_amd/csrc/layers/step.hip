@@ -95,7 +95,7 @@ int nsgcqt_attention_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t
         using T = decltype(t);
         LAUNCH_TRY(k_step<T, decltype(dp)::value>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
         if (a.splits > 1)
-            LAUNCH_TRY(k_step_join<T>, dim3(static_cast<unsigned>(n_streams * n_heads)), dim3(128), 0, st, a);
+            LAUNCH_TRY(k_step_join<T>, dim3(static_cast<unsigned>(n_streams * n_heads)), dim3(256), 0, st, a);
         return NSGCQT_OK;
     });
 }
@@ -121,7 +121,7 @@ int nsgcqt_cache_fill(int dtype, const nsgcqt_rows* r, int64_t n_kv_heads, int64
     a.k_cache = k_cache;
     a.v_cache = v_cache;
     a.off = r->offsets;
-    a.rows = r->rows;
+    a.rows = static_cast<int>(r->rows);
     a.n_bands = static_cast<int>(r->n_bands);
     a.kv_heads = static_cast<int>(n_kv_heads);
     a.dim = static_cast<int>(head_dim);

@@ -33,12 +33,12 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     __shared__ __align__(128) char vt[4][32 * RB];
     __shared__ float tops[4][32], sums[4][32];
     __shared__ float joined[DP][33];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, h = lane >> 5;
-    const int64_t id = die_order(blockIdx.x, gridDim.x);
-    const int split = static_cast<int>(id % a.splits);
-    const int64_t rest = id / a.splits;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
+    const unsigned id = die_order(blockIdx.x, gridDim.x), rest = id / a.splits;
+    const int split = id - rest * a.splits;
     const int hb = static_cast<int>(rest % a.head_blocks);
-    const int64_t sk = rest / a.head_blocks, stream = sk / a.kv_heads;
+    const unsigned sk = rest / a.head_blocks;
+    const int64_t stream = sk / a.kv_heads;
     const int kv = static_cast<int>(sk % a.kv_heads);
     const int h_first = 32 * hb, h_count = min(32, a.group - h_first);
 
@@ -47,8 +47,8 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     const int fresh = pos < 0 ? -1 : ring_slot(pos, a.sinks, a.window);
     const T* kn = reinterpret_cast<T*>(a.k.data) + stream * a.k.batch + kv * a.k.head;
     const T* vn = reinterpret_cast<T*>(a.v.data) + stream * a.v.batch + kv * a.v.head;
-    T* kc = static_cast<T*>(a.k_cache) + sk * a.slots * a.dim;
-    T* vc = static_cast<T*>(a.v_cache) + sk * a.slots * a.dim;
+    T* kc = static_cast<T*>(a.k_cache) + static_cast<int64_t>(sk) * a.slots * a.dim;
+    T* vc = static_cast<T*>(a.v_cache) + static_cast<int64_t>(sk) * a.slots * a.dim;
     const int tiles = (n + 31) / 32;
     const int t0 = static_cast<int>(static_cast<int64_t>(tiles) * split / a.splits);
     const int t1 = static_cast<int>(static_cast<int64_t>(tiles) * (split + 1) / a.splits);
@@ -163,33 +163,52 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     }
 }
 
-// Joins the stretches of one head of one stream.
+// Joins the stretches (at most 256) of one head of one stream: their weights
+// first, then each wave adds up every fourth stretch and the four sums are added.
 template <class T>
-__global__ __launch_bounds__(128) void k_step_join(StepArgs a) {
-    const int64_t sh = blockIdx.x, stream = sh / a.heads;
-    const int head = static_cast<int>(sh % a.heads), d = threadIdx.x;
-    const float* p = a.part + sh * a.splits * (a.dim + 2);
-    float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, p[s * (a.dim + 2) + a.dim]);
-    const float base = top == -INFINITY ? 0.f : top * a.c;
-    float total = 0.f, val = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float* x = p + s * (a.dim + 2);
-        const float w = exp2_(fmaf(x[a.dim], a.c, -base));
-        total = fmaf(x[a.dim + 1], w, total);
-        if (d < a.dim) val = fmaf(x[d], w, val);
+__global__ __launch_bounds__(256) void k_step_join(StepArgs a) {
+    __shared__ float tops[4], totals[4], weight[256], sums[4][128];
+    const int64_t stream = blockIdx.x / a.heads, stride = a.dim + 2;
+    const int head = blockIdx.x % a.heads, tid = threadIdx.x, lane = tid & 63, wave = wave_number();
+    const float* p = a.part + static_cast<int64_t>(blockIdx.x) * a.splits * stride;
+    const bool there = tid < a.splits;
+    const float mine = there ? p[tid * stride + a.dim] : -INFINITY;
+    float top = mine;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const float base = top == -INFINITY ? 0.f : top * a.c, w = exp2_(fmaf(mine, a.c, -base));
+    weight[tid] = w;
+    float total = there ? p[tid * stride + a.dim + 1] * w : 0.f;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) total += __shfl_xor(total, x);
+    if (lane == 0) totals[wave] = total;
+    __syncthreads();
+    total = totals[0] + totals[1] + totals[2] + totals[3];
+    float x0 = 0.f, x1 = 0.f;
+#pragma unroll 8
+    for (int s = wave; s < a.splits; s += 4) {
+        const float* q = p + s * stride;
+        x0 = fmaf(lane < a.dim ? q[lane] : 0.f, weight[s], x0);
+        x1 = fmaf(lane + 64 < a.dim ? q[lane + 64] : 0.f, weight[s], x1);
     }
-    if (d < a.dim)
-        reinterpret_cast<T*>(a.o.data)[stream * a.o.batch + head * a.o.head + d] =
+    sums[wave][lane] = x0;
+    sums[wave][lane + 64] = x1;
+    __syncthreads();
+    if (tid < a.dim) {
+        const float val = sums[0][tid] + sums[1][tid] + sums[2][tid] + sums[3][tid];
+        reinterpret_cast<T*>(a.o.data)[stream * a.o.batch + head * a.o.head + tid] =
             static_cast<T>(total == 0.f ? 0.f : val / total);
+    }
 }
 
 struct FillArgs {
     View k, v;
     void *k_cache, *v_cache;
     const int64_t* off;
-    int64_t rows;
-    int n_bands, kv_heads, dim, slots, sinks, window;
+    int rows, n_bands, kv_heads, dim, slots, sinks, window;
 };
 
 template <class T>

@@ -237,54 +237,60 @@ template <class T> __device__ inline void store_column(T* p, const acc16& c, int
 
 // Which of n work items block `id` takes: blocks go to the 8 compute dies in
 // turn, so each die gets one contiguous stretch and neighbours share its L2.
-__device__ inline int64_t die_order(int64_t id, int64_t n) {
-    const int64_t q = n >> 3, r = n & 7, x = id & 7;
+__device__ inline unsigned die_order(unsigned id, unsigned n) {
+    const unsigned q = n >> 3, r = n & 7, x = id & 7;
     return x * q + (x < r ? x : r) + (id >> 3);
 }
 
-struct Tile {
-    int band;        // -1: tokens before the first band, n_bands: after the last
-    int64_t start;   // the band's first token
-    int64_t len;     // and its number of tokens
-    int64_t first;   // the tile's first row of the band's mult * len rows
-    bool live;       // false: nothing to do
+// I: int where a band's mult * len rows stay below 2^30, else int64_t.
+template <class I> struct Tile {
+    int band;    // -1: tokens before the first band, n_bands: after the last
+    int start;   // the band's first token
+    int len;     // and its number of tokens
+    I first;     // the tile's first row of the band's mult * len rows
+    bool live;   // false: nothing to do
 };
 
-// Tiles of 2^SHIFT rows of the bands' mult * len rows each, without a table:
-// band i's tiles begin at item floor(mult start_i / 2^SHIFT) + i, which
+// Tiles of 2^shift rows of the bands' mult * len rows each, without a table:
+// band i's tiles begin at item floor(mult start_i / 2^shift) + i, which
 // leaves room for each band's ragged last tile, so tile_count() items hold
 // them all and some items are empty. The band of item p is found by a search
 // over the offsets, 64 at a time: one or two rounds of loads.
-template <int SHIFT> __host__ __device__ inline int64_t tile_count(int64_t n_bands, int64_t mult, int64_t rows) {
-    return ((mult * rows) >> SHIFT) + n_bands + 2;
+inline __host__ __device__ int64_t tile_count(int shift, int64_t n_bands, int64_t mult, int64_t rows) {
+    return ((mult * rows) >> shift) + n_bands + 2;
 }
 
-__device__ inline int64_t band_bound(const int64_t* off, int n_bands, int64_t rows, int i) {
+__device__ inline int band_bound(const int64_t* off, int n_bands, int rows, int i) {
     if (i <= 0) return 0;
     if (i >= n_bands + 2) return rows;
     const int64_t o = off[i - 1];
-    return o < 0 ? 0 : o > rows ? rows : o;
+    return o < 0 ? 0 : o > rows ? rows : static_cast<int>(o);
 }
 
-template <int SHIFT>
-__device__ inline Tile find_tile(const int64_t* off, int n_bands, int64_t rows, int64_t mult, int64_t p, int lane) {
+template <class I>
+__device__ inline Tile<I> find_tile(const int64_t* off, int n_bands, int rows, I mult, int shift, I p, int lane) {
     int lo = 0, hi = n_bands + 2;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        const bool below = i < hi && ((mult * band_bound(off, n_bands, rows, i)) >> SHIFT) + i <= p;
+        const bool below = i < hi && ((mult * band_bound(off, n_bands, rows, i)) >> shift) + i <= p;
         const int count = __popcll(__ballot(below));
         lo += (count > 1 ? count - 1 : 0) * step;
         hi = lo + step < hi ? lo + step : hi;
     }
-    Tile t;
-    const int64_t a = band_bound(off, n_bands, rows, lo), b = band_bound(off, n_bands, rows, lo + 1);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    Tile<I> t;
+    const int a = band_bound(off, n_bands, rows, lo), b = band_bound(off, n_bands, rows, lo + 1);
     t.band = lo - 1;
     t.start = a;
     t.len = b > a ? b - a : 0;
-    t.first = (p - (((mult * a) >> SHIFT) + lo)) << SHIFT;
+    t.first = (p - (((mult * a) >> shift) + lo)) << shift;
     t.live = t.first >= 0 && t.first < mult * t.len;
     return t;
 }
+
+// The number of this thread's wave, in a scalar register: what follows from
+// it (a wave's range of rows, what it skips) is then scalar work.
+__device__ inline int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 struct View {
     char* data;
