@@ -110,8 +110,8 @@ template <class T, int DP, int BN> struct Loader {
             for (int c = tid; c < kChunks; c += 256) {
                 const int r = c / (DP / 8), d = c % (DP / 8) * 8;
                 const int n = row0 + r < row_end && (!keep || keep[row0 + r]) ? dim - d : 0;
-                write8<T, kRB>(tx, r, c % (DP / 8), load8<T>(px + r * sx + d, n, false));
-                write8<T, kRB>(ty, r, c % (DP / 8), load8<T>(py + r * sy + d, n, false));
+                write8<T, kRB>(tx, r, c % (DP / 8), load8<T, false>(px + r * sx + d, n, d > 0));
+                write8<T, kRB>(ty, r, c % (DP / 8), load8<T, false>(py + r * sy + d, n, d > 0));
             }
         }
     }
@@ -171,11 +171,13 @@ __device__ inline void hide_edges(acc16& s, const AttnArgs& a, int i, int j0, in
 // 32 rows of a tensor as fragments (A or B): lane l holds row l % 32.
 template <class T, int DP>
 __device__ inline void load_rows(frag<T> (&f)[DP / 16], const T* p, bool there, int dim, bool wide, int lane) {
+    by_width(wide, [&](auto w) {
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-        const int d = 16 * s + 8 * (lane >> 5);
-        f[s] = load8<T>(p + d, there ? dim - d : 0, wide);
-    }
+        for (int s = 0; s < DP / 16; ++s) {
+            const int d = 16 * s + 8 * (lane >> 5);
+            f[s] = load8<T, w.value>(p + d, there ? dim - d : 0, d > 0);
+        }
+    });
 }
 
 // Zeros for `count` rows from `first` on (below len) of tokens that no band holds.

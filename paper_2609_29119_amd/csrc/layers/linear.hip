@@ -26,6 +26,30 @@ LinearArgs linear_args(const nsgcqt_rows* r, int64_t n_in, int64_t n_out) {
     return a;
 }
 
+// Rows of a chunk of the weights' gradient: as many as leave three workgroups
+// for each of the 256 compute units, 256 to 4096.
+int chunk_shift_of(int64_t batch, int64_t rows, int64_t n_in, int64_t n_out) {
+    const int64_t tiles = ((n_out + 127) / 128) * (n_in ? (n_in + 127) / 128 : 1);
+    int shift = 12;
+    while (shift > 8 && ((batch * rows) >> shift) * tiles < 768) --shift;
+    return shift;
+}
+
+// LDS of k_linear_kept for W.
+template <class T, bool BACK> int kept_bytes(int64_t n_red, int64_t n_col, int nb) {
+    if (n_red > 4096) return kKeptLds;
+    return kept_rows<BACK>(static_cast<int>(n_red), static_cast<int>(n_col), nb) *
+           kept_row_bytes<T, BACK>(static_cast<int>(n_red), nb);
+}
+
+// Rows of a workgroup of k_linear_kept: up to 1024 for each copy of W into
+// LDS, but not so many that fewer than 4 workgroups fall on a compute unit.
+int kept_shift(int64_t batch, int64_t rows, int64_t cols) {
+    int shift = 10;
+    while (shift > 7 && ((batch * rows) >> shift) * cols < 1024) --shift;
+    return shift;
+}
+
 int check_weights(const void* w, const char* name, int dtype, int64_t count) {
     if (count && !w) return set_err(NSGCQT_EINVAL, std::string(name) + " is NULL");
     if (misaligned(w, elem_bytes(dtype))) return set_err(NSGCQT_EINVAL, std::string(name) + " is not aligned to its element");
@@ -49,19 +73,29 @@ int run_linear(int dtype, const nsgcqt_rows* r, const nsgcqt_view* in, const voi
     a.w = w;
     a.bias = bias;
     a.w_wide = n_in % 8 == 0 && !misaligned(w, 16);
-    const int64_t tiles = tile_count(kRowShift, a.n_bands, a.batch, a.rows);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
         auto go = [&](auto nb) -> int {
             constexpr int NB = decltype(nb)::value;
-            const int64_t blocks = tiles * ((n_col + 32 * NB - 1) / (32 * NB));
+            const int64_t cols = (n_col + 32 * NB - 1) / (32 * NB);
+            const int lds = kKeptRest + kept_bytes<T, BACK>(n_red, n_col, NB);
+            if (n_red > 0 && lds <= kKeptLds) {
+                a.chunk_shift = kept_shift(a.batch, a.rows, cols);
+                const int64_t blocks = tile_count(a.chunk_shift, a.n_bands, a.batch, a.rows) * cols;
+                CHECK_TRY(check_grid(blocks));
+                LAUNCH_TRY(k_linear_kept<T, NB, BACK>, dim3(static_cast<unsigned>(blocks)), dim3(256),
+                           static_cast<size_t>(lds), st, a);
+                return NSGCQT_OK;
+            }
+            const int64_t blocks = tile_count(kRowShift, a.n_bands, a.batch, a.rows) * cols;
             CHECK_TRY(check_grid(blocks));
-            LAUNCH_TRY(k_linear<T, NB, BACK>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), a);
+            LAUNCH_TRY(k_linear<T, NB, BACK>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
             return NSGCQT_OK;
         };
         if (n_col <= 32) return go(std::integral_constant<int, 1>());
         if (n_col <= 64) return go(std::integral_constant<int, 2>());
+        if (n_col <= 96) return go(std::integral_constant<int, 3>());
         return go(std::integral_constant<int, 4>());
     });
 }
@@ -84,7 +118,7 @@ int64_t nsgcqt_band_linear_workspace(int64_t n_bands, int64_t batch, int64_t row
     static const int64_t none = 0;
     const nsgcqt_rows r{&none, n_bands, batch, rows};
     CHECK_TRY(check_linear(NSGCQT_F32, &r, n_in, n_out));
-    return 4 * tile_count(kChunkShift, n_bands, batch, rows) * (n_in * n_out + n_out);
+    return 4 * tile_count(chunk_shift_of(batch, rows, n_in, n_out), n_bands, batch, rows) * (n_in * n_out + n_out);
 }
 
 int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const nsgcqt_view* dy,
@@ -107,9 +141,10 @@ int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt
     a.dw = dw;
     a.db = db;
     a.part = static_cast<float*>(ws);
+    a.chunk_shift = chunk_shift_of(r->batch, r->rows, n_in, n_out);
     // with no inputs there is still the sum of dy
     const int64_t ot = (n_out + 127) / 128, it = n_in ? (n_in + 127) / 128 : 1;
-    const int64_t blocks = tile_count(kChunkShift, a.n_bands, a.batch, a.rows) * ot * it;
+    const int64_t blocks = tile_count(a.chunk_shift, a.n_bands, a.batch, a.rows) * ot * it;
     const int64_t join = (n_in * n_out + n_out + 255) / 256;
     CHECK_TRY(check_grid(blocks));
     if (r->n_bands > 65535) return set_err(NSGCQT_EUNSUPPORTED, "more than 65,535 bands in a gradient of weights");

@@ -65,8 +65,9 @@ extern "C" int nsgcqt_rotary(int dtype, const nsgcqt_view* q, const nsgcqt_view*
     a.pairs = static_cast<int>(pairs);
     a.interleaved = interleaved != 0;
     a.inverse = inverse != 0;
-    const bool eight = wide && pairs % 8 == 0;
-    const int v = eight ? 8 : 1;
+    // the most values an item can take that divide both parts of a head
+    const int64_t both = pairs | (head_dim - 2 * pairs);
+    const int v = both % 8 == 0 ? 8 : both % 4 == 0 ? 4 : both % 2 == 0 ? 2 : 1;
     a.chunks = static_cast<int>(pairs / v + (head_dim - 2 * pairs) / v);
     const int64_t blocks = (a.tokens * a.chunks + 255) / 256, heads = n_q_heads + n_k_heads;
     CHECK_TRY(check_grid(blocks));
@@ -77,10 +78,15 @@ extern "C" int nsgcqt_rotary(int dtype, const nsgcqt_view* q, const nsgcqt_view*
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>((heads + a.each - 1) / a.each));
     return by_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
-        if (eight)
-            LAUNCH_TRY(k_rotary<T, 8>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
-        else
-            LAUNCH_TRY(k_rotary<T, 1>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
-        return NSGCQT_OK;
+        auto go = [&](auto width) -> int {
+            LAUNCH_TRY(k_rotary<T, decltype(width)::value>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+            return NSGCQT_OK;
+        };
+        switch (v) {
+            case 8: return go(std::integral_constant<int, 8>());
+            case 4: return go(std::integral_constant<int, 4>());
+            case 2: return go(std::integral_constant<int, 2>());
+            default: return go(std::integral_constant<int, 1>());
+        }
     });
 }

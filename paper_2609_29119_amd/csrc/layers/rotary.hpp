@@ -39,7 +39,7 @@ __device__ inline void turn_of(const RotaryArgs& a, int64_t at, int p, float& cs
 
 // One item: V pairs (or V values past the pairs, which are copied) of one
 // token, for `each` heads: the angles are formed once and serve them all.
-// V = 8 takes 16-byte accesses.
+// Rows need no more alignment than their element's.
 template <class T, int V>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, token = id / a.chunks;
@@ -48,14 +48,14 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
     const int64_t b = token / a.rows, row = token - b * a.rows;
     const int turned = a.pairs / V, h0 = blockIdx.y * a.each, h1 = min(h0 + a.each, a.heads[0] + a.heads[1]);
     float cs[V], sn[V];
-    int d0, d1;   // where the item's first and second V values lie
+    int d0, d1;   // where the item's values lie (interleaved pairs: 2 V from d0 on)
     const bool pairs = chunk < turned;
     if (pairs) {
         const int64_t at = b * a.pos_batch + row;
 #pragma unroll
         for (int j = 0; j < V; ++j) turn_of(a, at, chunk * V + j, cs[j], sn[j]);
         d0 = a.interleaved ? 2 * V * chunk : V * chunk;
-        d1 = a.interleaved ? d0 + V : a.pairs + d0;
+        d1 = a.pairs + d0;
     } else {
         d0 = 2 * a.pairs + V * (chunk - turned);
         d1 = d0;
@@ -65,38 +65,32 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         const View &in = a.in[which], &out = a.out[which];
         const T* x = reinterpret_cast<const T*>(in.data) + b * in.batch + row * in.row + head * in.head;
         T* y = reinterpret_cast<T*>(out.data) + b * out.batch + row * out.row + head * out.head;
-        if constexpr (V == 8) {
-            frag<T> u = *reinterpret_cast<const frag<T>*>(x + d0), v = *reinterpret_cast<const frag<T>*>(x + d1);
-            if (pairs) {
-                float f[16], g[16];
+        T u[2 * V];
+        if (!pairs) {
+            __builtin_memcpy(u, x + d0, V * sizeof(T));
+            __builtin_memcpy(y + d0, u, V * sizeof(T));
+            continue;
+        }
+        if (a.interleaved) {
+            __builtin_memcpy(u, x + d0, 2 * V * sizeof(T));
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    f[j] = static_cast<float>(u[j]);
-                    f[8 + j] = static_cast<float>(v[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float m = a.interleaved ? f[2 * j] : f[j], n = a.interleaved ? f[2 * j + 1] : f[8 + j];
-                    const float r = fmaf(m, cs[j], -n * sn[j]), s = fmaf(m, sn[j], n * cs[j]);
-                    g[j] = r;
-                    g[8 + j] = s;
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    u[j] = static_cast<T>(a.interleaved ? g[(j & 1) * 8 + (j >> 1)] : g[j]);
-                    v[j] = static_cast<T>(a.interleaved ? g[(j & 1) * 8 + 4 + (j >> 1)] : g[8 + j]);
-                }
-                *reinterpret_cast<frag<T>*>(y + d1) = v;
+            for (int j = 0; j < V; ++j) {
+                const float m = static_cast<float>(u[2 * j]), n = static_cast<float>(u[2 * j + 1]);
+                u[2 * j] = static_cast<T>(fmaf(m, cs[j], -n * sn[j]));
+                u[2 * j + 1] = static_cast<T>(fmaf(m, sn[j], n * cs[j]));
             }
-            *reinterpret_cast<frag<T>*>(y + d0) = u;
+            __builtin_memcpy(y + d0, u, 2 * V * sizeof(T));
         } else {
-            if (pairs) {
-                const float m = static_cast<float>(x[d0]), n = static_cast<float>(x[d1]);
-                y[d0] = static_cast<T>(fmaf(m, cs[0], -n * sn[0]));
-                y[d1] = static_cast<T>(fmaf(m, sn[0], n * cs[0]));
-            } else {
-                y[d0] = x[d0];
+            __builtin_memcpy(u, x + d0, V * sizeof(T));
+            __builtin_memcpy(u + V, x + d1, V * sizeof(T));
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float m = static_cast<float>(u[j]), n = static_cast<float>(u[V + j]);
+                u[j] = static_cast<T>(fmaf(m, cs[j], -n * sn[j]));
+                u[V + j] = static_cast<T>(fmaf(m, sn[j], n * cs[j]));
             }
+            __builtin_memcpy(y + d0, u, V * sizeof(T));
+            __builtin_memcpy(y + d1, u + V, V * sizeof(T));
         }
     }
 }

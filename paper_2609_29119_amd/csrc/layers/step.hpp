@@ -73,13 +73,18 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
 
     auto fetch = [&](int t) {
         const int key = 32 * t + m;
-        load_rows<T, DP>(kf, key == fresh ? kn : kc + static_cast<int64_t>(key) * a.dim, key < n, a.dim, a.wide, lane);
+        const T* kr = key == fresh ? kn : kc + static_cast<int64_t>(key) * a.dim;
+        by_width(a.wide, [&](auto wide) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int c = lane + 64 * e, slot = 32 * t + c / (DP / 8), d = c % (DP / 8) * 8;
-            vr[e] = load8<T>((slot == fresh ? vn : vc + static_cast<int64_t>(slot) * a.dim) + d,
-                             slot < n ? a.dim - d : 0, a.wide);
-        }
+            for (int s = 0; s < DP / 16; ++s)
+                kf[s] = load8<T, wide.value>(kr + 16 * s + 8 * h, key < n ? a.dim - 16 * s - 8 * h : 0, s + h > 0);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int c = lane + 64 * e, slot = 32 * t + c / (DP / 8), d = c % (DP / 8) * 8;
+                vr[e] = load8<T, wide.value>((slot == fresh ? vn : vc + static_cast<int64_t>(slot) * a.dim) + d,
+                                             slot < n ? a.dim - d : 0, d > 0);
+            }
+        });
     };
     if (t0 + wave < t1) fetch(t0 + wave);
     for (int t = t0 + wave; t < t1; t += 4) {

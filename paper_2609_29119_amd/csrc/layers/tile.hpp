@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace nsl {
 
 typedef float acc16 __attribute__((ext_vector_type(16)));
@@ -71,17 +73,52 @@ template <class T> __device__ inline frag<T> narrow(const acc16& c, int s) {
 }
 
 // 8 values at p, of which the first n are there (n may be <= 0 or past 8).
-// wide: p is 16-byte aligned and n is never between 0 and 8.
-template <class T> __device__ inline frag<T> load8(const T* p, int n, bool wide) {
+// WIDE: p is 16-byte aligned and n is never between 0 and 8. Else p is
+// aligned to its element only, which the memory pipeline takes too; a row's
+// last values come from the 8 that end it (before: 8 values lie in front of
+// p) and are shifted down. Callers branch on the alignment around a group of
+// loads, not at each one, which would keep them from being in flight together.
+template <class T, bool WIDE> __device__ inline frag<T> load8(const T* p, int n, bool before = false) {
     frag<T> f = zero8<T>();
-    if (wide) {
+    if constexpr (WIDE) {
         if (n > 0) f = *reinterpret_cast<const frag<T>*>(p);
-    } else {
+    } else if (n >= 8) {
+        __builtin_memcpy(&f, p, sizeof(f));
+    } else if (n > 0) {
+        if constexpr (sizeof(T) == 2) {
+            if (before) {
+                uint64_t u[2];
+                __builtin_memcpy(u, p + n - 8, 16);
+                const int s = 16 * (8 - n);
+                const uint64_t lo = s >= 64 ? u[1] >> (s - 64) : (u[0] >> s) | (u[1] << (64 - s));
+                const uint64_t hi = s >= 64 ? 0 : u[1] >> s;
+                const u4 w = {static_cast<unsigned>(lo), static_cast<unsigned>(lo >> 32), static_cast<unsigned>(hi),
+                              static_cast<unsigned>(hi >> 32)};
+                return __builtin_bit_cast(frag<T>, w);
+            }
+        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 7; ++j)
             if (j < n) f[j] = p[j];
     }
     return f;
+}
+
+// f(0), ..., f(N - 1) with integral constants: a loop over an array that has to
+// stay in registers where the code around it is too large for the unroller.
+template <int N, int I = 0, class F> __device__ __attribute__((always_inline)) inline void each(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each<N, I + 1>(f);
+    }
+}
+
+// f(true_type or false_type)
+template <class F> __device__ inline void by_width(bool wide, F f) {
+    if (wide)
+        f(std::true_type());
+    else
+        f(std::false_type());
 }
 
 // The values of lane l % 32 and lane l % 32 + 32, in every lane.
@@ -114,8 +151,8 @@ template <class T, int D> constexpr int row_bytes() { return (D * static_cast<in
 __device__ inline int turn(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
 
 // Columns 8 c8 .. 8 c8 + 7 of `row`.
-template <class T, int RB> __device__ inline frag<T> read8(const char* tile, int row, int c8) {
-    const char* r = tile + row * RB;
+template <class T> __device__ inline frag<T> read8(const char* tile, int rb, int row, int c8) {
+    const char* r = tile + row * rb;
     const int t = turn(row);
     if constexpr (sizeof(T) == 2) {
         return *reinterpret_cast<const frag<T>*>(r + ((c8 ^ t) << 4));
@@ -126,8 +163,12 @@ template <class T, int RB> __device__ inline frag<T> read8(const char* tile, int
     }
 }
 
-template <class T, int RB> __device__ inline void write8(char* tile, int row, int c8, frag<T> f) {
-    char* r = tile + row * RB;
+template <class T, int RB> __device__ inline frag<T> read8(const char* tile, int row, int c8) {
+    return read8<T>(tile, RB, row, c8);
+}
+
+template <class T> __device__ inline void write8(char* tile, int rb, int row, int c8, frag<T> f) {
+    char* r = tile + row * rb;
     const int t = turn(row);
     if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<frag<T>*>(r + ((c8 ^ t) << 4)) = f;
@@ -135,6 +176,10 @@ template <class T, int RB> __device__ inline void write8(char* tile, int row, in
         *reinterpret_cast<f4*>(r + (((2 * c8) ^ t) << 4)) = __builtin_shufflevector(f, f, 0, 1, 2, 3);
         *reinterpret_cast<f4*>(r + (((2 * c8 + 1) ^ t) << 4)) = __builtin_shufflevector(f, f, 4, 5, 6, 7);
     }
+}
+
+template <class T, int RB> __device__ inline void write8(char* tile, int row, int c8, frag<T> f) {
+    write8<T>(tile, RB, row, c8, f);
 }
 
 typedef __attribute__((address_space(3))) s4 lds_s4;
@@ -195,51 +240,62 @@ template <class T, int RB> __device__ inline frag<T> read_turned8(const char* ti
 
 // Stores rows 0 .. 31 of a result tile, held as registers of column m = one
 // token: element d0 + row of the token's row p (NULL: nothing), d below n.
-// wide: 16-byte aligned rows and n a multiple of 8. In 16 bits the halves of
-// the wave exchange quads, so that each lane stores 8 consecutive values.
+// wide: 16-byte aligned rows and n a multiple of 8; else rows are aligned to
+// their element only. In 16 bits the halves of the wave exchange quads, so
+// that each lane stores 8 consecutive values.
 template <class T> __device__ inline void store_column(T* p, const acc16& c, int d0, int n, bool wide, int lane) {
     const int h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
-        if (wide) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const frag<T> f = narrow<T>(c, s);
-                const u4 u = __builtin_bit_cast(u4, f);
-                const u2 x = __builtin_amdgcn_permlane32_swap(u[0], u[2], false, false);
-                const u2 y = __builtin_amdgcn_permlane32_swap(u[1], u[3], false, false);
-                const u4 out = {x[0], y[0], x[1], y[1]};
-                const int d = d0 + 16 * s + 8 * h;
-                if (p && d < n) *reinterpret_cast<u4*>(p + d) = out;
+        for (int s = 0; s < 2; ++s) {
+            const frag<T> f = narrow<T>(c, s);
+            const u4 u = __builtin_bit_cast(u4, f);
+            const u2 x = __builtin_amdgcn_permlane32_swap(u[0], u[2], false, false);
+            const u2 y = __builtin_amdgcn_permlane32_swap(u[1], u[3], false, false);
+            const u4 out = {x[0], y[0], x[1], y[1]};
+            const int d = d0 + 16 * s + 8 * h;
+            if (!p || d >= n) continue;
+            if (wide) {
+                *reinterpret_cast<u4*>(p + d) = out;
+            } else if (d + 8 <= n) {
+                __builtin_memcpy(p + d, &out, 16);
+            } else {
+                const frag<T> g = __builtin_bit_cast(frag<T>, out);
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (d + j < n) p[d + j] = g[j];
             }
-            return;
         }
     } else {
-        if (wide) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int d = d0 + 8 * q + 4 * h;
-                const f4 v = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-                if (p && d < n) *reinterpret_cast<f4*>(p + d) = v;
+        for (int q = 0; q < 4; ++q) {
+            const int d = d0 + 8 * q + 4 * h;
+            const f4 v = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+            if (!p || d >= n) continue;
+            if (wide) {
+                *reinterpret_cast<f4*>(p + d) = v;
+            } else if (d + 4 <= n) {
+                __builtin_memcpy(p + d, &v, 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (d + j < n) p[d + j] = v[j];
             }
-            return;
-        }
-    }
-    if (p) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int d = d0 + 8 * (r >> 2) + 4 * h + (r & 3);
-            if (d < n) p[d] = static_cast<T>(c[r]);
         }
     }
 }
 
 // ---------------------------------------------------------------- work items
 
-// Which of n work items block `id` takes: blocks go to the 8 compute dies in
-// turn, so each die gets one contiguous stretch and neighbours share its L2.
+// Which of n work items block `id` takes. Blocks go to the 8 compute dies in
+// turn; each die gets stretches of 16 neighbouring items, which share its L2,
+// and stretches from everywhere: bands grow along the row, and with one eighth
+// of it for each die the last die has most of the work.
 __device__ inline unsigned die_order(unsigned id, unsigned n) {
-    const unsigned q = n >> 3, r = n & 7, x = id & 7;
-    return x * q + (x < r ? x : r) + (id >> 3);
+    constexpr unsigned kStretch = 16;
+    if (id >= n / (8 * kStretch) * (8 * kStretch)) return id;
+    const unsigned die = id & 7, k = id >> 3;
+    return (k / kStretch * 8 + die) * kStretch + k % kStretch;
 }
 
 // I: int where a band's mult * len rows stay below 2^30, else int64_t.

@@ -21,6 +21,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import struct
 
 import torch
@@ -86,15 +87,17 @@ def _bytes(n):
 
 
 _here = contextlib.nullcontext()
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
 def _on(t):
     """A context with t's device current."""
-    return _here if t.get_device() == torch.cuda.current_device() else torch.cuda.device(t.device)
+    return _here if t.get_device() == _current_device() else torch.cuda.device(t.device)
 
 
 def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
+    """The raw handle of t's device's current stream."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _tensor(t, name, like=None, shape=None):
@@ -135,8 +138,17 @@ def _view4(t):
     return _view(t.data_ptr(), s[0], s[1], s[2])
 
 
+def _view_step(t):
+    s = t.stride()
+    return _view(t.data_ptr(), s[0], 0, s[1])
+
+
 def _trains(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _last(t):
@@ -165,7 +177,7 @@ def _linear_checks(x, weight, offsets, bias):
 def _linear_forward(x, weight, offsets, bias):
     batch, rows, n_in = x.shape
     n_out = weight.shape[1]
-    y = torch.empty((batch, rows, n_out), dtype=x.dtype, device=x.device)
+    y = x.new_empty((batch, rows, n_out))
     with _on(x):
         _check(_lib().nsgcqt_band_linear(
             _DTYPES[x.dtype], _ragged(offsets, batch, rows), _view3(x), weight.data_ptr(),
@@ -176,7 +188,7 @@ def _linear_forward(x, weight, offsets, bias):
 def _linear_grad_input(dy, weight, offsets):
     batch, rows, n_out = dy.shape
     n_in = weight.shape[2]
-    dx = torch.empty((batch, rows, n_in), dtype=dy.dtype, device=dy.device)
+    dx = dy.new_empty((batch, rows, n_in))
     with _on(dy):
         _check(_lib().nsgcqt_band_linear_grad_input(
             _DTYPES[dy.dtype], _ragged(offsets, batch, rows), _view3(dy), weight.data_ptr(),
@@ -253,7 +265,13 @@ def rotary_frequencies(sections, base=10000.0, device="cuda"):
     return torch.cat([base ** (-torch.arange(s, dtype=torch.float64) / max(s, 1)) for s in sections]).float().to(device)
 
 
-_sections = [struct.Struct(f"={n}i").pack for n in range(5)]
+@functools.lru_cache(maxsize=256)
+def _sections(sections, dim):
+    """The packed sections of a head of dim values, and their number of pairs."""
+    pairs = sum(sections)
+    if not 1 <= len(sections) <= 4 or min(sections) < 0 or 2 * pairs > dim:
+        raise ValueError("sections has to hold 1 to 4 counts of at most D / 2 pairs in all")
+    return struct.pack(f"={len(sections)}i", *sections), pairs
 
 
 def _rotary_call(q, k, positions, freqs, sections, interleaved, inverse):
@@ -264,7 +282,7 @@ def _rotary_call(q, k, positions, freqs, sections, interleaved, inverse):
             views += [None, None]
             heads.append(0)
         else:
-            o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+            o = torch.empty_like(t, memory_format=torch.contiguous_format)
             outs.append(o)
             views += [_view4(t), _view4(o)]
             heads.append(t.shape[2])
@@ -321,17 +339,15 @@ def rotary(q, k, positions, freqs, sections, interleaved=False):
         if k.dim() != 4:
             raise ValueError("k has to be [batch][rows][heads][D]")
         _tensor(k, "k", q, (batch, rows, k.shape[2], dim))
-    pairs = sum(sections)
-    if not 1 <= len(sections) <= 4 or min(sections) < 0 or 2 * pairs > dim:
-        raise ValueError("sections has to hold 1 to 4 counts of at most D / 2 pairs in all")
+    sec, pairs = _sections(tuple(sections), dim)
+    axes = len(sections)
     if positions.dtype not in _POS or positions.device != q.device:
         raise ValueError("positions has to be float32, float64 or int64 on the device of q")
-    if positions.shape not in ((len(sections), rows), (len(sections), batch, rows)) or (
-            rows > 1 and positions.stride(-1) != 1):
+    if (positions.shape != (axes, rows) and positions.shape != (axes, batch, rows)) or (
+            positions.stride(-1) != 1 and rows > 1):
         raise ValueError("positions has to be [axes][rows] or [axes][batch][rows], its rows contiguous")
     if freqs.dtype != torch.float32 or freqs.device != q.device or freqs.shape != (pairs,) or not freqs.is_contiguous():
         raise ValueError(f"freqs has to be a float32 vector of {pairs} values on the device of q")
-    sec = _sections[len(sections)](*sections)
     call = _Rotary.apply if _trains(q, k) else _rotary_forward
     out = call(q, k, positions, freqs, sec, interleaved)
     return out[0] if k is None else out
@@ -347,7 +363,7 @@ def _shape_of(q, k, left, right, sinks, scale, keep):
 
 def _attention_forward(q, k, v, offsets, keep, left, right, sinks, scale, stats=None):
     batch, rows, heads, dim = q.shape
-    o = torch.empty((batch, rows, heads, dim), dtype=q.dtype, device=q.device)
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
     with _on(q):
         _check(_lib().nsgcqt_band_attention(
             _DTYPES[q.dtype], _ragged(offsets, batch, rows), _shape_of(q, k, left, right, sinks, scale, keep),
@@ -369,7 +385,7 @@ class _BandAttention(torch.autograd.Function):
     def backward(ctx, do):
         q, k, v, o, stats, offsets, keep = ctx.saved_tensors
         do = _last(do)
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
         shape, r = _shape_of(q, k, *ctx.how, keep), _ragged(offsets, q.shape[0], q.shape[1])
         L = _lib()
         n = _bytes(L.nsgcqt_band_attention_workspace(r, shape))
@@ -424,6 +440,11 @@ def _caches(k_cache, v_cache, like, streams, kv_heads, dim):
     return k_cache.shape[2]
 
 
+@functools.lru_cache(maxsize=256)
+def _step_workspace(*sizes):
+    return _bytes(_lib().nsgcqt_attention_step_workspace(*sizes))
+
+
 def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None):
     """Attention of one new token of each stream over its ring cache.
 
@@ -446,17 +467,14 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
         raise ValueError("pos has to be int64 [streams] on the device of q")
     if _trains(q, k, v):
         raise ValueError("attention_step has no gradient: call it under torch.no_grad()")
-    o = torch.empty((streams, heads, dim), dtype=q.dtype, device=q.device) if out is None else out
-    _tensor(o, "out", q, (streams, heads, dim))
-    L = _lib()
+    o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else _tensor(out, "out", q, q.shape)
     sinks = int(sinks)
-    n = _bytes(L.nsgcqt_attention_step_workspace(streams, heads, kv_heads, dim, slots - sinks, sinks))
+    n = _step_workspace(streams, heads, kv_heads, dim, slots - sinks, sinks)
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    views = [_view(t.data_ptr(), t.stride(0), 0, t.stride(1)) for t in (q, k, v, o)]
     with _on(q):
-        _check(L.nsgcqt_attention_step(
+        _check(_lib().nsgcqt_attention_step(
             _DTYPES[q.dtype], streams, heads, kv_heads, dim, slots - sinks, sinks,
-            dim ** -0.5 if scale is None else float(scale), *views, k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(),
+            dim ** -0.5 if scale is None else float(scale), _view_step(q), _view_step(k), _view_step(v), _view_step(o), k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(),
             ws.data_ptr() if n else None, n, _stream(q)))
     return o
 

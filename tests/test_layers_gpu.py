@@ -79,6 +79,9 @@ LINEAR = [
     ([1500, 600], 3, 24, 16, True),       # several chunks of the weights' gradient
     ([3] * 150 + [0, 1], 1, 16, 24, True),  # more bands than one round of the search
     ([0, 0], 2, 4, 4, True),
+    ([70, 131], 2, 520, 130, True),       # W does not fit LDS
+    ([90, 40], 1, 130, 600, False),
+    ([300, 700], 2, 96, 96, True),
     ([12], 1, 0, 8, True),                # nothing but the bias
     ([12, 4], 1, 8, 0, False),
 ]
