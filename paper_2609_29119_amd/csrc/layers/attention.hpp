@@ -149,21 +149,27 @@ __device__ inline acc16 scores(const char* tile, int row0, const frag<T> (&f)[DP
 }
 
 // The window's edges, for tiles that cross one: hides the scores (column:
-// query i, rows: keys j0 ..) of keys outside [i - left, i + right]
-// that are not sinks.
-__device__ inline void hide_edges(acc16& s, const AttnArgs& a, int i, int j0, int h) {
+// query i, rows: keys j0 ..) of keys outside [i - left, i + right] that are
+// not sinks, and with GRAD drops what dp holds there (0 * inf would be NaN).
+template <bool GRAD>
+__device__ inline void hide_edges(acc16& s, acc16& dp, const AttnArgs& a, int i, int j0, int h) {
     const int at = j0 + 4 * h, lo = i - a.left - at;
     const unsigned span = static_cast<unsigned>(a.left) + a.right;
     if (j0 >= a.sinks) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[r] = static_cast<unsigned>(8 * (r >> 2) + (r & 3) - lo) <= span ? s[r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) {
+            const bool see = static_cast<unsigned>(8 * (r >> 2) + (r & 3) - lo) <= span;
+            s[r] = see ? s[r] : -INFINITY;
+            if (GRAD) dp[r] = see ? dp[r] : 0.f;
+        }
     } else {
         const int hi = i + a.right - at, sink = a.sinks - at;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int e = 8 * (r >> 2) + (r & 3);
-            s[r] = e <= hi && (e >= lo || e < sink) ? s[r] : -INFINITY;
+            const bool see = e <= hi && (e >= lo || e < sink);
+            s[r] = see ? s[r] : -INFINITY;
+            if (GRAD) dp[r] = see ? dp[r] : 0.f;
         }
     }
 }
@@ -278,7 +284,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
             const int j = j0 + 32 * kb;
             if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
             acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[n & 1] : nullptr, lane);
-            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges(s, a, i, j, h);
+            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<false>(s, s, a, i, j, h);
             float mx = s[0];
 #pragma unroll
             for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
@@ -325,7 +331,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
 // dq, and delta = do . o for the key gradient. Layout as k_attention: the
 // scores and dp are formed transposed, so ds is the B fragment of dq^T = K^T ds^T.
 template <class T, int DP>
-__global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs a) {
+__global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 4 ? 2 : 3) void k_attention_dq(AttnArgs a) {
     constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
     typedef Loader<T, DP, BN> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
@@ -408,14 +414,10 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void k_attention_dq(AttnArgs 
             const int j = j0 + 32 * kb;
             if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
             acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[n & 1] : nullptr, lane);
-            const acc16 dp = scores<T, DP>(vt, 32 * kb, gf, nullptr, lane);
-            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges(s, a, i, j, h);
-            // p is 0 for hidden keys; what dp holds there must not turn it into NaN
+            acc16 dp = scores<T, DP>(vt, 32 * kb, gf, nullptr, lane);
+            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<true>(s, dp, a, i, j, h);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = exp2_(fmaf(s[r], a.c, -lse));
-                s[r] = p == 0.f ? 0.f : p * (dp[r] - delta);
-            }
+            for (int r = 0; r < 16; ++r) s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const frag<T> ds = narrow<T>(s, x);
@@ -467,8 +469,11 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
     }
     if (edge) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[r] = static_cast<unsigned>(8 * (r >> 2) + 4 * h + (r & 3) - lo) <= span ? s[r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) {
+            const bool see = static_cast<unsigned>(8 * (r >> 2) + (r & 3) - (lo - 4 * h)) <= span;
+            s[r] = see ? s[r] : -INFINITY;
+            dp[r] = see ? dp[r] : 0.f;
+        }
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -478,7 +483,7 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
         for (int j = 0; j < 4; ++j) {
             const int r = 4 * q + j;
             s[r] = exp2_(fmaf(s[r], c, -l[j]));
-            dp[r] = s[r] == 0.f ? 0.f : s[r] * (dp[r] - e[j]);
+            dp[r] = s[r] * (dp[r] - e[j]);
         }
     }
 #pragma unroll

@@ -31,7 +31,7 @@ LinearArgs linear_args(const nsgcqt_rows* r, int64_t n_in, int64_t n_out) {
 int chunk_shift_of(int64_t batch, int64_t rows, int64_t n_in, int64_t n_out) {
     const int64_t tiles = ((n_out + 127) / 128) * (n_in ? (n_in + 127) / 128 : 1);
     int shift = 12;
-    while (shift > 8 && ((batch * rows) >> shift) * tiles < 768) --shift;
+    while (shift > 8 && ((batch * rows) >> shift) * tiles < 400) --shift;
     return shift;
 }
 
@@ -80,7 +80,7 @@ int run_linear(int dtype, const nsgcqt_rows* r, const nsgcqt_view* in, const voi
             constexpr int NB = decltype(nb)::value;
             const int64_t cols = (n_col + 32 * NB - 1) / (32 * NB);
             const int lds = kKeptRest + kept_bytes<T, BACK>(n_red, n_col, NB);
-            if (n_red > 0 && lds <= kKeptLds) {
+            if (!a.x_wide && n_red > 0 && lds <= kKeptLds) {
                 a.chunk_shift = kept_shift(a.batch, a.rows, cols);
                 const int64_t blocks = tile_count(a.chunk_shift, a.n_bands, a.batch, a.rows) * cols;
                 CHECK_TRY(check_grid(blocks));

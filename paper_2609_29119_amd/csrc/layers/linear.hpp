@@ -31,75 +31,16 @@ template <class T> __device__ inline T* band_row(const View& v, const Tile<int64
     return reinterpret_cast<T*>(v.data) + b * v.batch + (t.start + c) * v.row;
 }
 
-// Lane l's pointer.
-template <class P> __device__ inline P from_lane(P p, int l) {
-    return reinterpret_cast<P>(__shfl(reinterpret_cast<unsigned long long>(p), l));
-}
-
-// Stores a wave's result, 128 bytes of each of its rows at a time, through
-// 4 KB of LDS of its own: lane l's column is row l % 32, whose pointer is out;
-// the first `there` rows exist.
-template <class T, int NB>
-__device__ inline void store_rows(char* slab, const acc16 (&acc)[NB], T* out, int there, int c0, int n_col, bool y_wide,
-                                  int lane) {
-    constexpr int kSlab = 128 / (32 * static_cast<int>(sizeof(T)));   // tiles of 32 columns in 128 bytes
-    constexpr int kIn16 = 16 / static_cast<int>(sizeof(T));
-    const int m = lane & 31, h = lane >> 5;
-    T* row_out[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) row_out[e] = from_lane(out, lane / 8 + 8 * e);
-    each<(NB + kSlab - 1) / kSlab>([&](auto z) __attribute__((always_inline)) {
-        constexpr int n0 = decltype(z)::value * kSlab;
-        each<kSlab>([&](auto x) __attribute__((always_inline)) {
-            constexpr int nb = n0 + decltype(x)::value;
-            if constexpr (nb < NB) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    quad<T> v;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = static_cast<T>(acc[nb][4 * q + j]);
-                    const int byte = (32 * decltype(x)::value + 8 * q + 4 * h) * static_cast<int>(sizeof(T));
-                    *reinterpret_cast<quad<T>*>(slab + m * 128 + (((byte >> 4) ^ turn(m)) << 4) + (byte & 15)) = v;
-                }
-            }
-        });
-        const int d = c0 + 32 * n0 + lane % 8 * kIn16;
-        by_width(y_wide, [&](auto wide) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = lane / 8 + 8 * e;
-                const u4 v = *reinterpret_cast<const u4*>(slab + row * 128 + ((lane % 8 ^ turn(row)) << 4));
-                if (row >= there || d >= n_col || 32 * n0 + lane % 8 * kIn16 >= 32 * NB) continue;
-                if (wide.value) {
-                    *reinterpret_cast<u4*>(row_out[e] + d) = v;
-                } else if (d + kIn16 <= n_col) {
-                    __builtin_memcpy(row_out[e] + d, &v, 16);
-                } else {
-                    T x[kIn16];
-                    __builtin_memcpy(x, &v, 16);
-#pragma unroll
-                    for (int j = 0; j < kIn16 - 1; ++j)
-                        if (d + j < n_col) row_out[e][d + j] = x[j];
-                }
-            }
-        });
-    });
-}
-
 // y (BACK: dx). The product is formed transposed, y^T = W x^T: a lane's column
-// is a row of x and the result's registers run along y. W's tile is shared by
-// the four waves (BACK reads it turned); a wave's 32 rows of x go through LDS
-// of its own, and so does its result, because memory is then read and written
-// in runs of 128 bytes a row. Straight to fragments (32 bytes a row and load)
-// the addresses, not the bytes, were the limit.
+// is a row of x, whose 8 consecutive values are its B fragment straight from
+// memory, and the result's registers run along y. Only W goes through LDS,
+// where the four waves share it; BACK reads it turned.
 template <class T, int NB, bool BACK>
 __global__ __launch_bounds__(256, 2) void k_linear(LinearArgs a) {
     constexpr int BK = step_width<T>(), BN = 32 * NB, KS = BK / 16;
     constexpr int WR = BACK ? BK : BN, WC = BACK ? BN : BK;           // rows and columns of the tile of W
     constexpr int RB = row_bytes<T, WC>(), kChunks = WR * WC / 8, kEach = (kChunks + 255) / 256;
-    constexpr int XB = 32 * 128, kRowEach = 32 * BK / 8 / 64;         // a wave's rows: 128 bytes each
     __shared__ __align__(128) char lds[2][WR * RB];
-    __shared__ __align__(128) char rows[4][2][XB];
     __shared__ __align__(16) float start[BN];   // where the sums start: the bias
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int n_red = BACK ? a.n_out : a.n_in, n_col = BACK ? a.n_in : a.n_out, cols = (n_col + BN - 1) / BN;
@@ -110,7 +51,6 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinearArgs a) {
     if (!t.live) return;
     const int64_t n_rows = static_cast<int64_t>(t.len) * a.batch, r = t.first + 32 * wave + m;
     const bool mine = r < n_rows;
-    const int there = static_cast<int>(min(n_rows - t.first - 32 * wave, int64_t(32)));   // rows of this wave
     T* out = mine ? band_row<T>(a.y, t, r) : nullptr;
     if (t.band < 0 || t.band >= a.n_bands) {
 #pragma unroll
@@ -119,47 +59,44 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinearArgs a) {
     }
     const T* in = mine ? band_row<T>(a.x, t, r) : nullptr;
     const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(t.band) * a.n_out * a.n_in;
-    const T* row_in[kRowEach];   // this lane's part of the wave's rows: chunk lane % (BK / 8) of these
-#pragma unroll
-    for (int e = 0; e < kRowEach; ++e) row_in[e] = from_lane(in, (lane + 64 * e) / (BK / 8));
 
-    frag<T> wr[kEach], xr[kRowEach];
-    auto fetch = [&](int k0) {
-        by_width(a.x_wide, [&](auto wide) {
-#pragma unroll
-            for (int e = 0; e < kRowEach; ++e) {
-                const int k = k0 + lane % (BK / 8) * 8;
-                xr[e] = load8<T, wide.value>(row_in[e] + k, (lane + 64 * e) / (BK / 8) < there ? n_red - k : 0, k > 0);
-            }
-        });
+    frag<T> wr[kEach], xf[KS], xn[KS];
+    auto fetch_w = [&](int k0) {
         by_width(a.w_wide, [&](auto wide) {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 const int c = tid + 256 * e, row = c / (WC / 8) + (BACK ? k0 : c0);
                 const int col = c % (WC / 8) * 8 + (BACK ? c0 : k0);
-                const bool ok = (kChunks % 256 == 0 || c < kChunks) && row < a.n_out;
-                wr[e] = load8<T, wide.value>(w + static_cast<int64_t>(row) * a.n_in + col, ok ? a.n_in - col : 0,
+                const bool there = (kChunks % 256 == 0 || c < kChunks) && row < a.n_out;
+                wr[e] = load8<T, wide.value>(w + static_cast<int64_t>(row) * a.n_in + col, there ? a.n_in - col : 0,
                                              col > 0);
             }
         });
     };
-    auto put = [&](int n) {
-#pragma unroll
-        for (int e = 0; e < kRowEach; ++e)
-            write8<T, 128>(rows[wave][n & 1], (lane + 64 * e) / (BK / 8), lane % (BK / 8), xr[e]);
+    auto put_w = [&](int n) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const int c = tid + 256 * e;
             if (kChunks % 256 == 0 || c < kChunks) write8<T, RB>(lds[n & 1], c / (WC / 8), c % (WC / 8), wr[e]);
         }
     };
+    auto fetch_x = [&](frag<T>(&f)[KS], int k0) {
+        by_width(a.x_wide, [&](auto wide) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int k = k0 + 16 * s + 8 * h;
+                f[s] = load8<T, wide.value>(in + k, mine ? n_red - k : 0, k > 0);
+            }
+        });
+    };
     const int steps = (n_red + BK - 1) / BK;
-    fetch(0);
+    fetch_w(0);
+    fetch_x(xf, 0);
     if (a.bias && tid < BN)
         start[tid] = c0 + tid < n_col ? static_cast<float>(static_cast<const T*>(
                                             a.bias)[static_cast<int64_t>(t.band) * a.n_out + c0 + tid])
                                       : 0.f;
-    put(0);
+    put_w(0);
     __syncthreads();
     acc16 acc[NB];
 #pragma unroll
@@ -176,31 +113,44 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinearArgs a) {
     }
 #pragma unroll 1
     for (int n = 0; n < steps; ++n) {
-        if (n + 1 < steps) fetch((n + 1) * BK);
+        if (n + 1 < steps) {
+            fetch_w((n + 1) * BK);
+            fetch_x(xn, (n + 1) * BK);
+        }
         const char* tile = lds[n & 1];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             if (n * BK + 16 * s < n_red) {
-                const frag<T> xf = read8<T, 128>(rows[wave][n & 1], m, 2 * s + h);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     if constexpr (BACK)
-                        acc[nb] = mma(read_turned8<T, RB>(tile, 16 * s, 32 * nb, lane), xf, acc[nb]);
+                        acc[nb] = mma(read_turned8<T, RB>(tile, 16 * s, 32 * nb, lane), xf[s], acc[nb]);
                     else
-                        acc[nb] = mma(read8<T, RB>(tile, 32 * nb + m, 2 * s + h), xf, acc[nb]);
+                        acc[nb] = mma(read8<T, RB>(tile, 32 * nb + m, 2 * s + h), xf[s], acc[nb]);
                 }
             }
         }
-        if (n + 1 < steps) put(n + 1);
+        if (n + 1 < steps) {
+            put_w(n + 1);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) xf[s] = xn[s];
+        }
         __syncthreads();
     }
-    store_rows<T, NB>(rows[wave][0], acc, out, there, c0, n_col, a.y_wide, lane);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) store_column<T>(out, acc[nb], c0 + 32 * nb, n_col, a.y_wide, lane);
 }
 
-// The same product where a band's whole W (or 32 NB of its output columns)
-// fits LDS beside 4 KB for each wave: W is loaded once and each wave walks
-// through its share of the workgroup's 2^chunk_shift rows on its own, without
-// a barrier, the next 8 KB of x on their way while it computes.
+// The same product for rows of odd widths or strides, where a band's whole W
+// (or 32 NB of its output columns) fits LDS beside 4 KB for each wave: W is
+// loaded once, and each wave walks through its share of the workgroup's
+// 2^chunk_shift rows on its own, without a barrier. Its rows go through LDS in
+// slabs of 128 bytes a row, two on their way while one is computed, and so
+// does its result: memory is read and written in runs of 128 bytes a row.
+// Straight to fragments, 32 unaligned bytes of each of 32 rows a load, the
+// addresses are the limit (193 -> 77 columns, 710,680 rows, float16: 205 us,
+// here 149); aligned rows are faster that way, which keeps more waves
+// resident (128 -> 128, 446,932 rows, bfloat16: 60 us, here 70).
 constexpr int kKeptLds = 65536, kKeptRest = 4 * 4096 + 512;   // rows of the waves, bias
 template <class T, bool BACK> __host__ __device__ inline int kept_row_bytes(int n_red, int nb) {
     return ((BACK ? 32 * nb : n_red) * static_cast<int>(sizeof(T)) + 127) / 128 * 128;
@@ -322,7 +272,10 @@ __global__ __launch_bounds__(256, 2) void k_linear_kept(LinearArgs a) {
                 }
                 if (++step >= steps || outside) {
                     T* out = r0 + m < r_end ? band_row<T>(a.y, t, r0 + m) : nullptr;
-                    store_rows<T, NB>(slab, acc, out, static_cast<int>(min(r_end - r0, int64_t(32))), c0, n_col, a.y_wide, lane);
+                    T* row_out[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) row_out[e] = from_lane(out, lane / 8 + 8 * e);
+            store_rows<T, NB>(slab, acc, row_out, static_cast<int>(min(r_end - r0, int64_t(32))), c0, n_col, a.y_wide, lane);
                     r0 += 128;
                     step = 0;
                 }
@@ -452,6 +405,7 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
     const int64_t item = ((b0 * a.batch) >> a.chunk_shift) + band + 1;
     for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
         float s = 0.f;
+#pragma unroll 8
         for (int64_t c = 0; c < chunks; ++c) s += dw_part(a, item + c)[e];
         if (e < n_w)
             static_cast<T*>(a.dw)[band * n_w + e] = static_cast<T>(s);

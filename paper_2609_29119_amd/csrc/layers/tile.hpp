@@ -285,6 +285,58 @@ template <class T> __device__ inline void store_column(T* p, const acc16& c, int
     }
 }
 
+// Lane l's pointer.
+template <class P> __device__ inline P from_lane(P p, int l) {
+    return reinterpret_cast<P>(__shfl(reinterpret_cast<unsigned long long>(p), l));
+}
+
+// Stores a wave's result, 128 bytes of each of its rows at a time, through
+// 4 KB of LDS of its own: lane l's column is row l % 32; row_out: the rows
+// lane / 8 + {0, 8, 16, 24}, of which those below `there` exist.
+template <class T, int NB>
+__device__ inline void store_rows(char* slab, const acc16 (&acc)[NB], T* const (&row_out)[4], int there, int c0,
+                                  int n_col, bool y_wide, int lane) {
+    constexpr int kSlab = 128 / (32 * static_cast<int>(sizeof(T)));   // tiles of 32 columns in 128 bytes
+    constexpr int kIn16 = 16 / static_cast<int>(sizeof(T));
+    const int m = lane & 31, h = lane >> 5;
+    each<(NB + kSlab - 1) / kSlab>([&](auto z) __attribute__((always_inline)) {
+        constexpr int n0 = decltype(z)::value * kSlab;
+        each<kSlab>([&](auto x) __attribute__((always_inline)) {
+            constexpr int nb = n0 + decltype(x)::value;
+            if constexpr (nb < NB) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    quad<T> v;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = static_cast<T>(acc[nb][4 * q + j]);
+                    const int byte = (32 * decltype(x)::value + 8 * q + 4 * h) * static_cast<int>(sizeof(T));
+                    *reinterpret_cast<quad<T>*>(slab + m * 128 + (((byte >> 4) ^ turn(m)) << 4) + (byte & 15)) = v;
+                }
+            }
+        });
+        const int d = c0 + 32 * n0 + lane % 8 * kIn16;
+        by_width(y_wide, [&](auto wide) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = lane / 8 + 8 * e;
+                const u4 v = *reinterpret_cast<const u4*>(slab + row * 128 + ((lane % 8 ^ turn(row)) << 4));
+                if (row >= there || d >= n_col || 32 * n0 + lane % 8 * kIn16 >= 32 * NB) continue;
+                if (wide.value) {
+                    *reinterpret_cast<u4*>(row_out[e] + d) = v;
+                } else if (d + kIn16 <= n_col) {
+                    __builtin_memcpy(row_out[e] + d, &v, 16);
+                } else {
+                    T x[kIn16];
+                    __builtin_memcpy(x, &v, 16);
+#pragma unroll
+                    for (int j = 0; j < kIn16 - 1; ++j)
+                        if (d + j < n_col) row_out[e][d + j] = x[j];
+                }
+            }
+        });
+    });
+}
+
 // ---------------------------------------------------------------- work items
 
 // Which of n work items block `id` takes. Blocks go to the 8 compute dies in
@@ -325,17 +377,22 @@ __device__ inline int band_bound(const int64_t* off, int n_bands, int rows, int 
 
 template <class I>
 __device__ inline Tile<I> find_tile(const int64_t* off, int n_bands, int rows, I mult, int shift, I p, int lane) {
-    int lo = 0, hi = n_bands + 2;
+    int lo = 0, hi = n_bands + 2, bound = 0, at = 0;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        const bool below = i < hi && ((mult * band_bound(off, n_bands, rows, i)) >> shift) + i <= p;
+        bound = band_bound(off, n_bands, rows, i);
+        const bool below = i < hi && ((mult * bound) >> shift) + i <= p;
         const int count = __popcll(__ballot(below));
-        lo += (count > 1 ? count - 1 : 0) * step;
+        at = count > 1 ? count - 1 : 0;
+        lo += at * step;
         hi = lo + step < hi ? lo + step : hi;
     }
+    // the last round went in steps of one: its lanes hold the bounds
     lo = __builtin_amdgcn_readfirstlane(lo);
+    at = __builtin_amdgcn_readfirstlane(at);
     Tile<I> t;
-    const int a = band_bound(off, n_bands, rows, lo), b = band_bound(off, n_bands, rows, lo + 1);
+    const int a = __builtin_amdgcn_readlane(bound, at);
+    const int b = at < 63 ? __builtin_amdgcn_readlane(bound, at + 1) : band_bound(off, n_bands, rows, lo + 1);
     t.band = lo - 1;
     t.start = a;
     t.len = b > a ? b - a : 0;
