@@ -10,11 +10,11 @@ extern "C" int nsgcqt_band_attention(int dtype, const nsgcqt_rows* r, const nsgc
     CHECK_TRY(check_rows(r));
     CHECK_TRY(check_shape(s));
     AttnArgs a = attention_args(r, s);
-    a.wide = true;
-    CHECK_TRY(check_view(q, "q", dtype, r->batch, r->rows, s->n_heads, s->head_dim, a.wide));
-    CHECK_TRY(check_view(k, "k", dtype, r->batch, r->rows, s->n_kv_heads, s->head_dim, a.wide));
-    CHECK_TRY(check_view(v, "v", dtype, r->batch, r->rows, s->n_kv_heads, s->head_dim, a.wide));
-    CHECK_TRY(check_view(o, "o", dtype, r->batch, r->rows, s->n_heads, s->head_dim, a.wide));
+    bool wide = true;
+    CHECK_TRY(check_view(q, "q", dtype, r->batch, r->rows, s->n_heads, s->head_dim, wide));
+    CHECK_TRY(check_view(k, "k", dtype, r->batch, r->rows, s->n_kv_heads, s->head_dim, wide));
+    CHECK_TRY(check_view(v, "v", dtype, r->batch, r->rows, s->n_kv_heads, s->head_dim, wide));
+    CHECK_TRY(check_view(o, "o", dtype, r->batch, r->rows, s->n_heads, s->head_dim, wide));
     if (misaligned(stats, 4)) return set_err(NSGCQT_EINVAL, "stats is not aligned to 4 bytes");
     if (r->batch == 0 || r->rows == 0) return NSGCQT_OK;
     a.q = view_of(q);
@@ -24,8 +24,8 @@ extern "C" int nsgcqt_band_attention(int dtype, const nsgcqt_rows* r, const nsgc
     a.stats = stats;
     const int64_t blocks = query_blocks(a);
     CHECK_TRY(check_grid(blocks));
-    return by_type_and_width(dtype, s->head_dim, [&](auto t, auto dp) -> int {
-        LAUNCH_TRY(k_attention<decltype(t), decltype(dp)::value>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0,
+    return by_shape(dtype, s->head_dim, wide, [&](auto t, auto dp, auto w) -> int {
+        LAUNCH_TRY(k_attention<decltype(t), decltype(dp)::value, decltype(w)::value>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0,
                    static_cast<hipStream_t>(stream), a);
         return NSGCQT_OK;
     });

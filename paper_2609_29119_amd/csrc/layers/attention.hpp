@@ -10,6 +10,7 @@
 
 namespace nsl {
 
+// The kernels' WIDE: every view takes 16-byte accesses.
 struct AttnArgs {
     View q, k, v, o, d_o, dq, dk, dv;
     float* stats;         // [batch][heads][rows]: log2 of the softmax sum of scores times c; +inf for an empty row
@@ -71,45 +72,60 @@ typedef __attribute__((address_space(3))) void lds_void;
 // One tile of BN rows x DP columns of two tensors into LDS. Wide tensors go
 // there directly, 16 bytes a lane (a wave fills 1 KB of consecutive LDS, so
 // the lanes fetch the chunks that belong to their places): no registers, no
-// stores, and the next tile is on its way while this one is computed. Lanes
-// whose row or column is not there aim past the buffer's end, which reads as
-// zero. Other tensors take element loads and are stored from registers.
-template <class T, int DP, int BN> struct Loader {
+// stores, and the next tile is on its way while this one is computed. The
+// buffer ends with the tile's last row, and reads past its end give zeros:
+// rows that are not there cost nothing; lanes whose column or row is not there
+// or not kept aim past the end. Other tensors take element loads and are
+// stored from registers.
+template <class T, int DP, int BN, bool WIDE> struct Loader {
     static constexpr int kRB = row_bytes<T, DP>(), kBytes = BN * kRB;
     static constexpr int kEach = kBytes / 4096;          // wide: loads of a thread for each tensor
     static constexpr int kChunks = BN * DP / 8;          // else: chunks of 8 values of a tile
-    static constexpr unsigned kPast = 0x80000000u;       // the buffers' size: tiles span less
+    static constexpr unsigned kPast = 0x80000000u;       // past every tile
+    unsigned ox[kEach], oy[kEach];                       // wide: this lane's offsets in bytes
+    int64_t sx, sy;
+    int dim;
 
-    // place of load e of this thread in a tile
+    // row of load e of this thread in a tile
     static __device__ int row(int e, int wave, int lane) { return ((wave * kEach + e) * 1024 + lane * 16) / kRB; }
-    static __device__ int col(int e, int wave, int lane) {
-        const int r = row(e, wave, lane), slot = (wave * kEach + e) * 1024 % kRB / 16 + lane % (kRB / 16 < 64 ? kRB / 16 : 64);
-        return (slot ^ turn(r)) * (16 / static_cast<int>(sizeof(T)));
+
+    __device__ Loader(int64_t stride_x, int64_t stride_y, int width, int wave, int lane)
+        : sx(stride_x), sy(stride_y), dim(width) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int r = row(e, wave, lane), slot = lane % (kRB / 16 < 64 ? kRB / 16 : 64);
+            const unsigned d = (slot ^ turn(r)) * (16 / sizeof(T));
+            ox[e] = d < static_cast<unsigned>(dim) ? (r * static_cast<unsigned>(sx) + d) * sizeof(T) : kPast;
+            oy[e] = d < static_cast<unsigned>(dim) ? (r * static_cast<unsigned>(sy) + d) * sizeof(T) : kPast;
+        }
     }
 
-    // kept: for each load, whether its row may be used (wide only)
-    static __device__ void load(char* tx, char* ty, const T* px, int64_t sx, const T* py, int64_t sy, int row0,
-                                int row_end, int dim, bool wide, const uint8_t* keep, const bool (&kept)[kEach], int tid) {
-        const int lane = tid & 63, wave = wave_number();
+    // rows row0 .. of px, py (below row_end) into tx, ty; kept: for each load
+    // of a wide tensor, whether its row may be used (with keep)
+    __device__ void load(char* tx, char* ty, const T* px, const T* py, int row0, int row_end, const uint8_t* keep,
+                         const bool (&kept)[kEach], int tid) const {
         px += row0 * sx;
         py += row0 * sy;
-        if (wide) {
-            const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(px), 0, kPast, 0x00020000);
-            const auto ry = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(py), 0, kPast, 0x00020000);
+        const int rows = min(row_end - row0, BN);
+        if constexpr (WIDE) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass does not know a buffer's type
+            const int wave = wave_number();
+            const auto rx = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<T*>(px), 0, rows * static_cast<unsigned>(sx) * static_cast<unsigned>(sizeof(T)), 0x00020000);
+            const auto ry = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<T*>(py), 0, rows * static_cast<unsigned>(sy) * static_cast<unsigned>(sizeof(T)), 0x00020000);
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
-                const int r = row(e, wave, lane), d = col(e, wave, lane);
-                const bool there = row0 + r < row_end && d < dim && kept[e];
-                const unsigned ox = (r * static_cast<unsigned>(sx) + d) * sizeof(T);
-                const unsigned oy = (r * static_cast<unsigned>(sy) + d) * sizeof(T);
                 const int at = (wave * kEach + e) * 1024;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(tx + at), 16, there ? ox : kPast, 0, 0, 0);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_void*)(ty + at), 16, there ? oy : kPast, 0, 0, 0);
+                const unsigned x = keep && !kept[e] ? kPast : ox[e], y = keep && !kept[e] ? kPast : oy[e];
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(tx + at), 16, x, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_void*)(ty + at), 16, y, 0, 0, 0);
             }
+#endif
         } else {
             for (int c = tid; c < kChunks; c += 256) {
                 const int r = c / (DP / 8), d = c % (DP / 8) * 8;
-                const int n = row0 + r < row_end && (!keep || keep[row0 + r]) ? dim - d : 0;
+                const int n = r < rows && (!keep || keep[row0 + r]) ? dim - d : 0;
                 write8<T, kRB>(tx, r, c % (DP / 8), load8<T, false>(px + r * sx + d, n, d > 0));
                 write8<T, kRB>(ty, r, c % (DP / 8), load8<T, false>(py + r * sy + d, n, d > 0));
             }
@@ -145,6 +161,18 @@ __device__ inline acc16 scores(const char* tile, int row0, const frag<T> (&f)[DP
     }
 #pragma unroll
     for (int x = 0; x < DP / 16; ++x) s = mma(read8<T, RB>(tile, row0 + m, 2 * x + h), f[x], s);
+    return s;
+}
+
+// The product of 32 rows (from row0 on) of two tiles, transposed: rows of a, columns of b.
+template <class T, int DP>
+__device__ inline acc16 rows_product(const char* a, int row_a, const char* b, int row_b, int lane) {
+    constexpr int RB = row_bytes<T, DP>();
+    const int m = lane & 31, h = lane >> 5;
+    acc16 s = zero16();
+#pragma unroll
+    for (int x = 0; x < DP / 16; ++x)
+        s = mma(read8<T, RB>(a, row_a + m, 2 * x + h), read8<T, RB>(b, row_b + m, 2 * x + h), s);
     return s;
 }
 
@@ -194,6 +222,18 @@ __device__ inline void zero_rows(const View& v, int64_t b, int head, int start, 
         for (int d = tid; d < dim; d += 256) row_of<T>(v, b, start + r, head)[d] = static_cast<T>(0.f);
 }
 
+// The same 32 rows in LDS of the wave's own, to be read as fragments when they
+// are needed: registers, and with them the waves on a SIMD, are what the
+// gradient kernels are short of (dq of 5 s clips: 890 us with three waves,
+// 1104 with two).
+template <class T, int DP>
+__device__ inline void keep_rows(char* to, const T* p, bool there, int dim, bool wide, int lane) {
+    frag<T> f[DP / 16];
+    load_rows<T, DP>(f, p, there, dim, wide, lane);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) write8<T, row_bytes<T, DP>()>(to, lane & 31, 2 * s + (lane >> 5), f[s]);
+}
+
 // What a workgroup of the forward or the dq kernel works on.
 struct QueryWork {
     int b, kv, head0, head, i_lo, queries;
@@ -212,10 +252,10 @@ struct QueryWork {
     }
 };
 
-template <class T, int DP>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_attention(AttnArgs a) {
-    constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
-    typedef Loader<T, DP, BN> Ld;
+template <class T, int DP, bool WIDE>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : sizeof(T) == 2 && WIDE ? 3 : 2) void k_attention(AttnArgs a) {
+    constexpr int BN = DP > 64 ? 32 : 64, RB = row_bytes<T, DP>();
+    typedef Loader<T, DP, BN, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float bias[2][BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
@@ -235,7 +275,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
         return;
     }
     frag<T> qf[DP / 16];
-    load_rows<T, DP>(qf, row_of<T>(a.q, b, t.start + (mine ? i : 0), head), mine, a.dim, a.wide, lane);
+    load_rows<T, DP>(qf, row_of<T>(a.q, b, t.start + (mine ? i : 0), head), mine, a.dim, WIDE, lane);
     const T* kp = row_of<T>(a.k, b, t.start, kv);
     const T* vp = row_of<T>(a.v, b, t.start, kv);
     const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
@@ -247,6 +287,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
     const float slack = 8.f / a.c;
 
     const KeyRange range(a, q0, min(q0 + w.queries, len) - 1, len, BN);
+    const Ld ld(a.k.row, a.v.row, a.dim, wave, lane);
     // what masks tile n is fetched a tile earlier than the tile itself
     bool kept[Ld::kEach];
     float next_bias = 0.f;
@@ -260,59 +301,64 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
         }
         next_bias = j0 + tid < j_end && tid < BN && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
     };
-    auto fetch = [&](int n) {
+    auto fetch = [&](int n, int u) {
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
-        Ld::load(lds[n & 1][0], lds[n & 1][1], kp, a.k.row, vp, a.v.row, j0, j_end, a.dim, a.wide, keep, kept, tid);
-        if (tid < BN) bias[n & 1][tid] = next_bias;
+        ld.load(lds[u][0], lds[u][1], kp, vp, j0, j_end, keep, kept, tid);
+        if (tid < BN) bias[u][tid] = next_bias;
     };
     fetch_masks(0);
-    fetch(0);
+    fetch(0, 0);
     fetch_masks(1);
     tile_barrier();
-    for (int n = 0; n < range.tiles; ++n) {
-        if (n + 1 < range.tiles) {
-            fetch(n + 1);
-            fetch_masks(n + 2);
+    for (int n0 = 0; n0 < range.tiles; n0 += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {   // by two, so that a tile's place in LDS is a constant
+            const int n = n0 + u;
+            if (n >= range.tiles) continue;
+            if (n + 1 < range.tiles) {
+                fetch(n + 1, u ^ 1);
+                fetch_masks(n + 2);
+            }
+            int j0, j_end;
+            range.tile(n, BN, j0, j_end);
+            const char* kt = lds[u][0];
+            const char* vt = lds[u][1];
+#pragma unroll
+            for (int kb = 0; kb < BN / 32; ++kb) {
+                const int j = j0 + 32 * kb;
+                if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
+                acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[u] : nullptr, lane);
+                if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<false>(s, s, a, i, j, h);
+                float mx = s[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+                mx = half_max(mx);
+                // the maximum may lag by 8 powers of two: sums and outputs are
+                // rescaled when it grows by more, which is rare after the first keys
+                if (__any(mx > top + slack)) {
+                    const float now = fmaxf(top, mx), alpha = now == -INFINITY ? 1.f : exp2_((top - now) * a.c);
+                    sum *= alpha;
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
+                    top = now;
+                }
+                const float base = top == -INFINITY ? 0.f : top * a.c;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = exp2_(fmaf(s[r], a.c, -base));
+                    sum += s[r];
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const frag<T> p = narrow<T>(s, x);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d)
+                        o[d] = mma(read_turned<T, RB>(vt, 32 * kb + 16 * x, 32 * d, lane), p, o[d]);
+                }
+            }
+            tile_barrier();
         }
-        int j0, j_end;
-        range.tile(n, BN, j0, j_end);
-        const char* kt = lds[n & 1][0];
-        const char* vt = lds[n & 1][1];
-#pragma unroll
-        for (int kb = 0; kb < BN / 32; ++kb) {
-            const int j = j0 + 32 * kb;
-            if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
-            acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[n & 1] : nullptr, lane);
-            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<false>(s, s, a, i, j, h);
-            float mx = s[0];
-#pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-            mx = half_max(mx);
-            // the maximum may lag by 8 powers of two: sums and outputs are
-            // rescaled when it grows by more, which is rare after the first keys
-            if (__any(mx > top + slack)) {
-                const float now = fmaxf(top, mx), alpha = now == -INFINITY ? 1.f : exp2_((top - now) * a.c);
-                sum *= alpha;
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
-                top = now;
-            }
-            const float base = top == -INFINITY ? 0.f : top * a.c;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = exp2_(fmaf(s[r], a.c, -base));
-                sum += s[r];
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const frag<T> p = narrow<T>(s, x);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-                    o[d] = mma(read_turned<T, RB>(vt, 32 * kb + 16 * x, 32 * d, lane), p, o[d]);
-            }
-        }
-        tile_barrier();
     }
     const float total = half_sum(sum);
     const float inv = total == 0.f ? 0.f : 1.f / total;
@@ -320,7 +366,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
         o[d] *= inv;
-        store_column<T>(out, o[d], 32 * d, a.dim, a.wide, lane);
+        store_column<T>(out, o[d], 32 * d, a.dim, WIDE, lane);
     }
     if (stats && mine && h == 0)
         stats[i] = total == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top * a.c) + __log2f(total);
@@ -330,11 +376,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : 2) void k_atte
 
 // dq, and delta = do . o for the key gradient. Layout as k_attention: the
 // scores and dp are formed transposed, so ds is the B fragment of dq^T = K^T ds^T.
-template <class T, int DP>
-__global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 4 ? 2 : 3) void k_attention_dq(AttnArgs a) {
-    constexpr int BN = kv_tile<T, DP>(), RB = row_bytes<T, DP>();
-    typedef Loader<T, DP, BN> Ld;
+template <class T, int DP, bool WIDE>
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 || !WIDE ? 2 : 3) void k_attention_dq(AttnArgs a) {
+    constexpr int BN = DP > 64 ? 32 : 64, RB = row_bytes<T, DP>();
+    typedef Loader<T, DP, BN, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
+    __shared__ __align__(128) char grads[4][32 * RB];   // each wave's rows of do
     __shared__ __align__(16) float bias[2][BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
@@ -352,18 +399,21 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 4 ? 2 : 3) void k_a
     const int i_lo = w.i_lo, i = i_lo + m, i_hi = min(i_lo + 31, len - 1);
     const bool mine = i < len, active = i_lo < len;
     const int64_t row = t.start + (mine ? i : 0);
-    frag<T> qf[DP / 16], gf[DP / 16];
-    load_rows<T, DP>(qf, row_of<T>(a.q, b, row, head), mine, a.dim, a.wide, lane);
-    load_rows<T, DP>(gf, row_of<T>(a.d_o, b, row, head), mine, a.dim, a.wide, lane);
+    frag<T> qf[DP / 16];
+    load_rows<T, DP>(qf, row_of<T>(a.q, b, row, head), mine, a.dim, WIDE, lane);
+    char* own = grads[wave];
     float delta = 0.f;
     {
-        frag<T> of[DP / 16];
-        load_rows<T, DP>(of, row_of<T>(a.o, b, row, head), mine, a.dim, a.wide, lane);
+        frag<T> of[DP / 16], gf[DP / 16];
+        load_rows<T, DP>(gf, row_of<T>(a.d_o, b, row, head), mine, a.dim, WIDE, lane);
+        load_rows<T, DP>(of, row_of<T>(a.o, b, row, head), mine, a.dim, WIDE, lane);
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s)
+        for (int s = 0; s < DP / 16; ++s) {
+            write8<T, RB>(own, m, 2 * s + h, gf[s]);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 delta = fmaf(static_cast<float>(of[s][j]), static_cast<float>(gf[s][j]), delta);
+        }
     }
     delta = half_sum(delta);
     if (mine && h == 0) a.delta[at + i] = delta;
@@ -377,6 +427,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 4 ? 2 : 3) void k_a
     for (int d = 0; d < DP / 32; ++d) g[d] = zero16();
 
     const KeyRange range(a, q0, min(q0 + w.queries, len) - 1, len, BN);
+    const Ld ld(a.k.row, a.v.row, a.dim, wave, lane);
     // what masks tile n is fetched a tile earlier than the tile itself
     bool kept[Ld::kEach];
     float next_bias = 0.f;
@@ -390,49 +441,54 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 4 ? 2 : 3) void k_a
         }
         next_bias = j0 + tid < j_end && tid < BN && (!keep || keep[j0 + tid]) ? 0.f : -INFINITY;
     };
-    auto fetch = [&](int n) {
+    auto fetch = [&](int n, int u) {
         int j0, j_end;
         range.tile(n, BN, j0, j_end);
-        Ld::load(lds[n & 1][0], lds[n & 1][1], kp, a.k.row, vp, a.v.row, j0, j_end, a.dim, a.wide, keep, kept, tid);
-        if (tid < BN) bias[n & 1][tid] = next_bias;
+        ld.load(lds[u][0], lds[u][1], kp, vp, j0, j_end, keep, kept, tid);
+        if (tid < BN) bias[u][tid] = next_bias;
     };
     fetch_masks(0);
-    fetch(0);
+    fetch(0, 0);
     fetch_masks(1);
     tile_barrier();
-    for (int n = 0; n < range.tiles; ++n) {
-        if (n + 1 < range.tiles) {
-            fetch(n + 1);
-            fetch_masks(n + 2);
-        }
-        int j0, j_end;
-        range.tile(n, BN, j0, j_end);
-        const char* kt = lds[n & 1][0];
-        const char* vt = lds[n & 1][1];
+    for (int n0 = 0; n0 < range.tiles; n0 += 2) {
 #pragma unroll
-        for (int kb = 0; kb < BN / 32; ++kb) {
-            const int j = j0 + 32 * kb;
-            if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
-            acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[n & 1] : nullptr, lane);
-            acc16 dp = scores<T, DP>(vt, 32 * kb, gf, nullptr, lane);
-            if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<true>(s, dp, a, i, j, h);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const frag<T> ds = narrow<T>(s, x);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-                    g[d] = mma(read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane), ds, g[d]);
+        for (int u = 0; u < 2; ++u) {   // by two, so that a tile's place in LDS is a constant
+            const int n = n0 + u;
+            if (n >= range.tiles) continue;
+            if (n + 1 < range.tiles) {
+                fetch(n + 1, u ^ 1);
+                fetch_masks(n + 2);
             }
+            int j0, j_end;
+            range.tile(n, BN, j0, j_end);
+            const char* kt = lds[u][0];
+            const char* vt = lds[u][1];
+#pragma unroll
+            for (int kb = 0; kb < BN / 32; ++kb) {
+                const int j = j0 + 32 * kb;
+                if (!active || KeyRange::hidden(a, j, j_end, i_lo, i_hi)) continue;
+                acc16 s = scores<T, DP>(kt, 32 * kb, qf, keep || j + 32 > j_end ? bias[u] : nullptr, lane);
+                acc16 dp = rows_product<T, DP>(vt, 32 * kb, own, 0, lane);
+                if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<true>(s, dp, a, i, j, h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const frag<T> ds = narrow<T>(s, x);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d)
+                        g[d] = mma(read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane), ds, g[d]);
+                }
+            }
+            tile_barrier();
         }
-        tile_barrier();
     }
     T* out = mine ? row_of<T>(a.dq, b, t.start + i, head) : nullptr;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
         g[d] *= a.scale;
-        store_column<T>(out, g[d], 32 * d, a.dim, a.wide, lane);
+        store_column<T>(out, g[d], 32 * d, a.dim, WIDE, lane);
     }
 }
 
@@ -451,22 +507,17 @@ __device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t 
 }
 
 // One wave's 32 queries (rows of the tiles qt, gt at r0) against its 32 keys:
-// adds to dk^T and dv^T. lse, delta: of the tile's queries, in LDS (+inf for a
+// adds to dk^T and dv^T. kf, vt: the keys' k as fragments and v in LDS. lse, delta: of the tile's queries, in LDS (+inf for a
 // query that is not there: its probabilities are 0). With edge, this lane's
 // key is visible to the rows r0 + lo .. r0 + lo + span only. A key that is
 // not there or not kept only spoils its own column, which its lane drops.
 template <class T, int DP>
 __device__ inline void key_grad(const char* qt, const char* gt, const float* lse, const float* delta, int r0,
-                                const frag<T> (&kf)[DP / 16], const frag<T> (&vf)[DP / 16], acc16 (&dk)[DP / 32],
+                                const frag<T> (&kf)[DP / 16], const char* vt, acc16 (&dk)[DP / 32],
                                 acc16 (&dv)[DP / 32], float c, bool edge, int lo, unsigned span, int lane) {
     constexpr int RB = row_bytes<T, DP>();
-    const int m = lane & 31, h = lane >> 5;
-    acc16 s = zero16(), dp = zero16();
-#pragma unroll
-    for (int x = 0; x < DP / 16; ++x) {
-        s = mma(read8<T, RB>(qt, r0 + m, 2 * x + h), kf[x], s);
-        dp = mma(read8<T, RB>(gt, r0 + m, 2 * x + h), vf[x], dp);
-    }
+    const int h = lane >> 5;
+    acc16 s = scores<T, DP>(qt, r0, kf, nullptr, lane), dp = rows_product<T, DP>(gt, r0, vt, 0, lane);
     if (edge) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -498,11 +549,12 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 }
 
 // dk, dv of 128 keys (a wave has 32) over the queries near them.
-template <class T, int DP>
-__global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2) void k_attention_dkv(AttnArgs a) {
+template <class T, int DP, bool WIDE>
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 32 ? 1 : 2) : DP > 64 ? 1 : WIDE ? 3 : 2) void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = kv_tile<T, DP>();
-    typedef Loader<T, DP, BQ> Ld;
+    typedef Loader<T, DP, BQ, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
+    __shared__ __align__(128) char values[4][32 * Ld::kRB];   // each wave's rows of v
     __shared__ __align__(16) float row_lse[2][BQ], row_delta[2][BQ];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
@@ -524,9 +576,9 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
     const bool kept = mine && (!keep || keep[j]);
     const int64_t row = t.start + (mine ? j : 0);
-    frag<T> kf[DP / 16], vf[DP / 16];
-    load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, a.wide, lane);
-    load_rows<T, DP>(vf, row_of<T>(a.v, b, row, kv), kept, a.dim, a.wide, lane);
+    frag<T> kf[DP / 16];
+    load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, WIDE, lane);
+    keep_rows<T, DP>(values[wave], row_of<T>(a.v, b, row, kv), kept, a.dim, WIDE, lane);
     acc16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
@@ -536,6 +588,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
     const unsigned span = j < a.sinks ? 0x7fffffffu : static_cast<unsigned>(a.left) + a.right;
     float next_lse = 0.f, next_delta = 0.f;
+    const Ld ld(a.q.row, a.d_o.row, a.dim, wave, lane);
     bool every[Ld::kEach];
 #pragma unroll
     for (int e = 0; e < Ld::kEach; ++e) every[e] = true;
@@ -547,37 +600,42 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
             next_delta = i < i_end ? a.delta[at] : 0.f;
         }
     };
-    auto fetch = [&](int n) {
+    auto fetch = [&](int n, int u) {
         const int head = kv * group + n / q_tiles, i0 = i_begin + n % q_tiles * BQ;
-        Ld::load(lds[n & 1][0], lds[n & 1][1], row_of<T>(a.q, b, t.start, head), a.q.row,
-                 row_of<T>(a.d_o, b, t.start, head), a.d_o.row, i0, i_end, a.dim, a.wide, nullptr, every, tid);
+        ld.load(lds[u][0], lds[u][1], row_of<T>(a.q, b, t.start, head), row_of<T>(a.d_o, b, t.start, head), i0,
+                i_end, nullptr, every, tid);
         if (tid < BQ) {
-            row_lse[n & 1][tid] = next_lse;
-            row_delta[n & 1][tid] = next_delta;
+            row_lse[u][tid] = next_lse;
+            row_delta[u][tid] = next_delta;
         }
     };
     fetch_stats(0);
-    fetch(0);
+    fetch(0, 0);
     fetch_stats(1);
     tile_barrier();
-    for (int n = 0; n < total; ++n) {
-        if (n + 1 < total) {
-            fetch(n + 1);
-            fetch_stats(n + 2);
-        }
-        const int i0 = i_begin + n % q_tiles * BQ;
+    for (int n0 = 0; n0 < total; n0 += 2) {
 #pragma unroll
-        for (int qb = 0; qb < BQ / 32; ++qb) {
-            const int i_lo = i0 + 32 * qb, i_hi = min(i_lo + 31, i_end - 1);
-            const bool skip = !active || i_lo >= i_end || j_lo > i_hi + a.right ||
-                              (j_hi < i_lo - a.left && j_lo >= a.sinks);
-            if (!skip) {
-                const bool edge = j_hi > i_lo + a.right || (j_lo < i_hi - a.left && j_hi >= a.sinks);
-                key_grad<T, DP>(lds[n & 1][0], lds[n & 1][1], row_lse[n & 1], row_delta[n & 1], 32 * qb, kf, vf, dk, dv,
-                                a.c, edge, j - a.right - i_lo, span, lane);
+        for (int u = 0; u < 2; ++u) {
+            const int n = n0 + u;
+            if (n >= total) continue;
+            if (n + 1 < total) {
+                fetch(n + 1, u ^ 1);
+                fetch_stats(n + 2);
             }
+            const int i0 = i_begin + n % q_tiles * BQ;
+#pragma unroll 1
+            for (int qb = 0; qb < BQ / 32; ++qb) {
+                const int i_lo = i0 + 32 * qb, i_hi = min(i_lo + 31, i_end - 1);
+                const bool skip = !active || i_lo >= i_end || j_lo > i_hi + a.right ||
+                                  (j_hi < i_lo - a.left && j_lo >= a.sinks);
+                if (!skip) {
+                    const bool edge = j_hi > i_lo + a.right || (j_lo < i_hi - a.left && j_hi >= a.sinks);
+                    key_grad<T, DP>(lds[u][0], lds[u][1], row_lse[u], row_delta[u], 32 * qb, kf, values[wave], dk, dv,
+                                    a.c, edge, j - a.right - i_lo, span, lane);
+                }
+            }
+            tile_barrier();
         }
-        tile_barrier();
     }
     // the far queries' share of the sinks
     if (j_lo < a.sinks && active) {
@@ -589,7 +647,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
                 const float* p = far_part(a, b, kv, item0 + ch, tile) + m * a.dim;
                 if (j < a.sinks && mine) {
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d)
+                    for (int d = 0; d < DP / 32; ++d) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const int c = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
@@ -597,7 +655,9 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
                                 dk[d][r] += p[c];
                                 dv[d][r] += p[32 * a.dim + c];
                             }
+                            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // few loads at a time: registers
                         }
+                    }
                 }
             }
     }
@@ -610,19 +670,20 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
             dk[d][r] = kept ? dk[d][r] * a.scale : 0.f;
             dv[d][r] = kept ? dv[d][r] : 0.f;
         }
-        store_column<T>(ok, dk[d], 32 * d, a.dim, a.wide, lane);
-        store_column<T>(ov, dv[d], 32 * d, a.dim, a.wide, lane);
+        store_column<T>(ok, dk[d], 32 * d, a.dim, WIDE, lane);
+        store_column<T>(ov, dv[d], 32 * d, a.dim, WIDE, lane);
     }
 }
 
 // Partial dk, dv of 32 sink keys over the far queries of one chunk. Every wave
 // has the same keys and takes a quarter of the queries; the four results are
 // added in the waves' order.
-template <class T, int DP>
+template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2) void k_attention_far(AttnArgs a) {
     constexpr int BQ = sizeof(T) == 4 && DP > 64 ? 64 : 128;
-    typedef Loader<T, DP, BQ> Ld;
+    typedef Loader<T, DP, BQ, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2 * Ld::kBytes];
+    __shared__ __align__(128) char values[32 * Ld::kRB];   // the keys' rows of v
     __shared__ __align__(16) float row_lse[2][BQ], row_delta[2][BQ];
     static_assert(sizeof(lds) >= 2 * DP * 33 * 4, "the tiles' room also serves to add up the waves");
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
@@ -641,21 +702,22 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
     const bool kept = j < a.sinks && j < len && (!keep || keep[j]);
     const int64_t row = t.start + (j < len ? j : 0);
-    frag<T> kf[DP / 16], vf[DP / 16];
-    load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, a.wide, lane);
-    load_rows<T, DP>(vf, row_of<T>(a.v, b, row, kv), kept, a.dim, a.wide, lane);
+    frag<T> kf[DP / 16];
+    load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, WIDE, lane);
+    if (wave == 0) keep_rows<T, DP>(values, row_of<T>(a.v, b, row, kv), kept, a.dim, WIDE, lane);
     acc16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
 
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
+    const Ld ld(a.q.row, a.d_o.row, a.dim, wave, lane);
     bool every[Ld::kEach];
 #pragma unroll
     for (int e = 0; e < Ld::kEach; ++e) every[e] = true;
     auto fetch = [&](int n) {
         const int head = kv * group + n / q_tiles, i0 = i_begin + n % q_tiles * BQ;
-        Ld::load(lds[n & 1], lds[n & 1] + Ld::kBytes, row_of<T>(a.q, b, t.start, head), a.q.row,
-                 row_of<T>(a.d_o, b, t.start, head), a.d_o.row, i0, i_end, a.dim, a.wide, nullptr, every, tid);
+        ld.load(lds[n & 1], lds[n & 1] + Ld::kBytes, row_of<T>(a.q, b, t.start, head), row_of<T>(a.d_o, b, t.start, head),
+                i0, i_end, nullptr, every, tid);
         if (tid < BQ) {
             const int64_t at = (b * a.heads + head) * a.rows + t.start + i0 + tid;
             const bool there = i0 + tid < i_end;
@@ -668,8 +730,8 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     for (int n = 0; n < total; ++n) {
         if (n + 1 < total) fetch(n + 1);
         if (32 * wave < BQ && i_begin + n % q_tiles * BQ + 32 * wave < i_end)
-            key_grad<T, DP>(lds[n & 1], lds[n & 1] + Ld::kBytes, row_lse[n & 1], row_delta[n & 1], 32 * wave, kf, vf, dk,
-                            dv, a.c, false, 0, 0, lane);
+            key_grad<T, DP>(lds[n & 1], lds[n & 1] + Ld::kBytes, row_lse[n & 1], row_delta[n & 1], 32 * wave, kf,
+                            values, dk, dv, a.c, false, 0, 0, lane);
         tile_barrier();
     }
     float(*joined)[DP][33] = reinterpret_cast<float(*)[DP][33]>(&lds[0][0]);

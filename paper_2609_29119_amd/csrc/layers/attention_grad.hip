@@ -35,7 +35,7 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
     CHECK_TRY(check_rows(r));
     CHECK_TRY(check_shape(s));
     AttnArgs a = attention_args(r, s);
-    a.wide = true;
+    bool wide = true;
     const struct {
         const nsgcqt_view* v;
         const char* name;
@@ -45,7 +45,7 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
                  {o, "o", &a.o, s->n_heads},       {d_o, "d_o", &a.d_o, s->n_heads},  {dq, "dq", &a.dq, s->n_heads},
                  {dk, "dk", &a.dk, s->n_kv_heads}, {dv, "dv", &a.dv, s->n_kv_heads}};
     for (const auto& x : views)
-        CHECK_TRY(check_view(x.v, x.name, dtype, r->batch, r->rows, x.heads, s->head_dim, a.wide));
+        CHECK_TRY(check_view(x.v, x.name, dtype, r->batch, r->rows, x.heads, s->head_dim, wide));
     if (r->batch == 0 || r->rows == 0) return NSGCQT_OK;
     if (!stats || misaligned(stats, 4)) return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 4 bytes");
     const int64_t need = delta_bytes(a) + (has_far(a) ? part_bytes(a) : 0);
@@ -63,12 +63,13 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
     CHECK_TRY(check_grid(keys));
     CHECK_TRY(check_grid(far));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return by_type_and_width(dtype, s->head_dim, [&](auto t, auto dp) -> int {
+    return by_shape(dtype, s->head_dim, wide, [&](auto t, auto dp, auto w) -> int {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
-        LAUNCH_TRY(k_attention_dq<T, DP>, dim3(static_cast<unsigned>(queries)), dim3(256), 0, st, a);
-        if (has_far(a)) LAUNCH_TRY(k_attention_far<T, DP>, dim3(static_cast<unsigned>(far)), dim3(256), 0, st, a);
-        LAUNCH_TRY(k_attention_dkv<T, DP>, dim3(static_cast<unsigned>(keys)), dim3(256), 0, st, a);
+        constexpr bool WIDE = decltype(w)::value;
+        LAUNCH_TRY(k_attention_dq<T, DP, WIDE>, dim3(static_cast<unsigned>(queries)), dim3(256), 0, st, a);
+        if (has_far(a)) LAUNCH_TRY(k_attention_far<T, DP, WIDE>, dim3(static_cast<unsigned>(far)), dim3(256), 0, st, a);
+        LAUNCH_TRY(k_attention_dkv<T, DP, WIDE>, dim3(static_cast<unsigned>(keys)), dim3(256), 0, st, a);
         return NSGCQT_OK;
     });
 }

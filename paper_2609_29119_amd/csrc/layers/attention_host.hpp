@@ -56,4 +56,11 @@ template <class F> int by_type_and_width(int dtype, int64_t dim, F f) {
     });
 }
 
+// f(T(), DP, true_type or false_type)
+template <class F> int by_shape(int dtype, int64_t dim, bool wide, F f) {
+    return by_type_and_width(dtype, dim, [&](auto t, auto dp) {
+        return wide ? f(t, dp, std::true_type()) : f(t, dp, std::false_type());
+    });
+}
+
 }  // namespace nsl

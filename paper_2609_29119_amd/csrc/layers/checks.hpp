@@ -33,8 +33,8 @@ inline int check_rows(const nsgcqt_rows* r) {
 }
 
 // A tensor [batch][rows][heads][width]: its pointer and alignment; `wide`
-// stays true if it takes 16-byte accesses, and a tile of up to 128 rows spans
-// less than the 2^31 bytes that a buffer access reaches.
+// stays true if it takes 16-byte accesses, its rows do not overlap, and a tile
+// of up to 128 rows spans less than the 2^31 bytes that a buffer access reaches.
 inline int check_view(const nsgcqt_view* v, const char* name, int dtype, int64_t batch, int64_t rows, int64_t heads,
                       int64_t width, bool& wide) {
     if (!v) return set_err(NSGCQT_EINVAL, std::string(name) + " is NULL");
@@ -46,7 +46,8 @@ inline int check_view(const nsgcqt_view* v, const char* name, int dtype, int64_t
         return set_err(NSGCQT_EINVAL, std::string(name) + " has a negative stride");
     const int64_t step = 16 / e;
     if (misaligned(v->data, 16) || width % 8 || (batch > 1 && v->batch % step) || (rows > 1 && v->row % step) ||
-        (heads > 1 && v->head % step) || v->row * e >= (int64_t(1) << 23))
+        (heads > 1 && v->head % step) || v->row * e >= (int64_t(1) << 23) ||
+        (rows > 1 && v->row < width))
         wide = false;
     return NSGCQT_OK;
 }
