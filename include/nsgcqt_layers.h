@@ -111,7 +111,9 @@ int nsgcqt_rotary(int dtype, const nsgcqt_view* q, const nsgcqt_view* q_out, int
  * band and signal when keep[b][j] is not 0 (keep NULL: always),
  * j <= i + right, and j >= i - left or j < sinks (numbers within the band).
  * A token that sees none gets a zero row and passes no gradient. What a
- * token that is not kept holds in k and v is never used, whatever it is. */
+ * token that is not kept holds in k and v is never used, whatever it is; an
+ * infinity or NaN of a kept token may, with weight zero, reach tokens of its
+ * band near it that do not see it. */
 typedef struct {
     int64_t n_heads, n_kv_heads;   /* n_kv_heads divides n_heads; head h reads kv head h / (n_heads / n_kv_heads) */
     int64_t head_dim;              /* 1 .. 128 */

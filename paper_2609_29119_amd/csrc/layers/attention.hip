@@ -10,7 +10,7 @@ extern "C" int nsgcqt_band_attention(int dtype, const nsgcqt_rows* r, const nsgc
     CHECK_TRY(check_rows(r));
     CHECK_TRY(check_shape(s));
     AttnArgs a = attention_args(r, s);
-    bool wide = true;
+    bool wide = r->rows > 1;   // (a lone row's stride may be anything)
     CHECK_TRY(check_view(q, "q", dtype, r->batch, r->rows, s->n_heads, s->head_dim, wide));
     CHECK_TRY(check_view(k, "k", dtype, r->batch, r->rows, s->n_kv_heads, s->head_dim, wide));
     CHECK_TRY(check_view(v, "v", dtype, r->batch, r->rows, s->n_kv_heads, s->head_dim, wide));

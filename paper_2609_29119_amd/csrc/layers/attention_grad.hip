@@ -35,7 +35,7 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
     CHECK_TRY(check_rows(r));
     CHECK_TRY(check_shape(s));
     AttnArgs a = attention_args(r, s);
-    bool wide = true;
+    bool wide = r->rows > 1;   // (a lone row's stride may be anything)
     const struct {
         const nsgcqt_view* v;
         const char* name;

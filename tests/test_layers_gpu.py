@@ -517,6 +517,47 @@ def test_step_in_a_graph_and_on_another_stream():
         assert torch.equal(cache.k, eager.k) and torch.equal(cache.v, eager.v) and torch.equal(cache.pos, eager.pos)
 
 
+def test_example_trains_and_streams(repo_root):
+    import importlib.util
+    import os
+    spec = importlib.util.spec_from_file_location("band_model", os.path.join(repo_root, "examples", "band_model.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    losses = m.train(25)
+    assert np.isfinite(losses).all() and losses[-1] < 0.7 * losses[0]
+    o = m.stream()
+    assert torch.isfinite(o).all() and o.abs().max() > 0
+
+
+def test_lone_tokens_with_any_stride():
+    """One token a signal: its row stride may be anything, zero or below the width."""
+    off = offsets_of([1])
+    base = randn(0, 3, 2, 64, dtype=torch.bfloat16)
+    q = base[:, None].expand(3, 1, 2, 64).as_strided((3, 1, 2, 64), (128, 0, 64, 1))
+    o = layers.band_attention(q, q, q, off, 5)
+    assert torch.equal(o[:, 0], base)
+    x = randn(1, 3, 64).as_strided((3, 1, 64), (64, 1, 1))
+    w = randn(2, 1, 8, 64)
+    close(layers.band_linear(x, w, off)[:, 0], x[:, 0].double() @ w[0].double().T, product_bound(torch.float32, 64), "y")
+
+
+def test_broadcast_inputs():
+    """Expanded inputs (stride 0) and gradients that come expanded."""
+    off = offsets_of([30, 20])
+    q = randn(0, 1, 1, 2, 32).requires_grad_()
+    k = randn(1, 2, 50, 1, 32).requires_grad_()
+    o = layers.band_attention(q.expand(2, 50, 2, 32), k, k, off, 7, 2, 1)
+    ref = attention_reference(q.expand(2, 50, 2, 32), k, k, [30, 20], 0, 7, 2, 1, 32 ** -0.5, None, torch.ones(2, 50, 2, 32))
+    close(o, ref[0], attention_bound(torch.float32), "o")
+    gq, gk = torch.autograd.grad(o.sum(), [q, k])
+    close(gq, ref[1].sum((0, 1), keepdim=True), attention_bound(torch.float32, True), "dq", ref[4].sum((0, 1), keepdim=True))
+    close(gk, ref[2] + ref[3], attention_bound(torch.float32, True), "dk", ref[5])
+    x = randn(2, 1, 1, 24).expand(2, 50, 24)
+    w = randn(3, 2, 16, 24)
+    y, _, _, _ = linear_reference(x, w, None, [30, 20], 0, torch.zeros(2, 50, 16))
+    close(layers.band_linear(x, w, off), y, product_bound(torch.float32, 24), "y")
+
+
 def test_refusals():
     off = offsets_of([4, 4])
     x, w = randn(0, 1, 8, 3), randn(1, 2, 5, 3)
