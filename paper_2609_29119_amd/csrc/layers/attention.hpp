@@ -374,7 +374,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : sizeof(T) == 2
 
 // --------------------------------------------------------------- gradients
 
-// dq, and delta = do . o for the key gradient. Layout as k_attention: the
+// dq, and delta = do . o for the key gradient. In 16 bits ds goes into its
+// product as two numbers, the rounded one and what the rounding left: with one
+// alone dq is off by 0.0025 in the 2-norm (bfloat16; 0.0017 is its own
+// rounding). delta comes from the rounded o; a row of ds sums to zero with the
+// exact one, so the sum that is found is delta's error, and the key gradient
+// gets the corrected value. Layout as k_attention: the
 // scores and dp are formed transposed, so ds is the B fragment of dq^T = K^T ds^T.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 || !WIDE ? 2 : 3) void k_attention_dq(AttnArgs a) {
@@ -416,7 +421,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
         }
     }
     delta = half_sum(delta);
-    if (mine && h == 0) a.delta[at + i] = delta;
+    float rest = 0.f;   // the sum of this row's ds: 0 but for delta's error
     const float lse = mine ? a.stats[at + i] : INFINITY;
 
     const T* kp = row_of<T>(a.k, b, t.start, kv);
@@ -472,18 +477,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
                 acc16 dp = rows_product<T, DP>(vt, 32 * kb, own, 0, lane);
                 if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<true>(s, dp, a, i, j, h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
+                    rest += s[r];
+                }
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const frag<T> ds = narrow<T>(s, x);
+                    frag<T> low;
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d)
-                        g[d] = mma(read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane), ds, g[d]);
+                    for (int e = 0; e < 8; ++e) low[e] = static_cast<T>(s[8 * x + e] - static_cast<float>(ds[e]));
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        const frag<T> kd = read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane);
+                        g[d] = mma(kd, ds, g[d]);
+                        if constexpr (sizeof(T) == 2) g[d] = mma(kd, low, g[d]);
+                    }
                 }
             }
             tile_barrier();
         }
     }
+    rest = half_sum(rest);
+    if (mine && h == 0) a.delta[at + i] = delta + rest;
     T* out = mine ? row_of<T>(a.dq, b, t.start + i, head) : nullptr;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
