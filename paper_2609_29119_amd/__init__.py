@@ -3,7 +3,9 @@
 The transform runs in hand-written HIP kernels behind the C ABI declared in
 include/nsgcqt.h (libnsgcqt.so, built in-tree by ``build.py``); this package
 is its Python binding. ``paper_2609_29119_amd.autograd`` makes analysis and
-synthesis differentiable through their explicit adjoints.
+synthesis differentiable through their explicit adjoints, and
+``paper_2609_29119_amd.layers`` holds layers that work on the ragged band
+layout (per-band products, rotary positions, windowed attention).
 """
 from .nsgcqt import (Plan, NsgcqtError, Info, BandInfo, BandSpec, lib, LIB_PATH, table1_layout, erb_layout,
                      BAND_DC, BAND_POSITIVE, BAND_NYQUIST,

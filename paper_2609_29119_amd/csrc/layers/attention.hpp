@@ -23,7 +23,6 @@ struct AttnArgs {
     int share;            // heads of one kv head that a workgroup takes: 1, 2 or 4
     int left, right, sinks;   // at most rows
     float scale, c;           // c = scale log2(e): exp(scale s) = exp2(c s)
-    bool wide;                // every view takes 16-byte accesses
 };
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -252,6 +251,20 @@ struct QueryWork {
     }
 };
 
+// Forward. One pass over the visible keys with a running maximum and sum. The
+// scores are formed transposed (a lane has one query), so a row's maximum and
+// sum need one exchange between the wave's halves, and the probabilities are
+// the B fragment of o^T = V^T p^T without leaving the registers. p is rounded
+// to the data's type for that product (16 bits: o is off by 0.0022 in the
+// 2-norm in bfloat16, its own rounding is 0.0017); sums take it unrounded.
+//
+// 131,072 tokens, 8 heads of 128 over 2, window 1024: 667 us, 826 TFLOP/s of
+// visible pairs (457 us at the rate of a large product): the matrix cores wait
+// for the exponentials (a quarter of the vector rate) and the maxima. Tiles of
+// 32 keys there, three waves a SIMD: with 64 and two waves 760 us.
+// 446,932 tokens in 221 bands, 8 heads of 64 over 2, window 256: 600 us, of
+// which 300 are reading and writing (232 at the rate of a large copy) and 25
+// go to each 32 keys of the window.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : sizeof(T) == 2 && WIDE ? 3 : 2) void k_attention(AttnArgs a) {
     constexpr int BN = DP > 64 ? 32 : 64, RB = row_bytes<T, DP>();
@@ -564,7 +577,13 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
     }
 }
 
-// dk, dv of 128 keys (a wave has 32) over the queries near them.
+// dk, dv of 128 keys (a wave has 32) over the queries near them, for all heads
+// of their kv head: no atomics and no partial sums but the sinks'. Scores and
+// dp are formed the other way round than in dq (a lane has one key), so p and
+// ds are B fragments again. p and ds are rounded to the data's type.
+// 446,932 tokens, 8 heads of 64 over 2, window 256, bfloat16: 800 us (dq 980,
+// far queries 180): 2.3 ms with the forward, 324 TFLOP/s of the formulas' work.
+// Bound by waiting: three waves a SIMD, half their cycles.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 32 ? 1 : 2) : DP > 64 ? 1 : WIDE ? 3 : 2) void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = kv_tile<T, DP>();

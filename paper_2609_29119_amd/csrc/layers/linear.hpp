@@ -34,7 +34,10 @@ template <class T> __device__ inline T* band_row(const View& v, const Tile<int64
 // y (BACK: dx). The product is formed transposed, y^T = W x^T: a lane's column
 // is a row of x, whose 8 consecutive values are its B fragment straight from
 // memory, and the result's registers run along y. Only W goes through LDS,
-// where the four waves share it; BACK reads it turned.
+// where the four waves share it; BACK reads it turned. Bound by memory and by
+// what each workgroup waits for in turn (the search, its rows, W):
+// 446,932 rows, 128 -> 128, bfloat16, 221 bands: y 58 us (4.1 TB/s), dx 61 us,
+// of 48 at the rate of a large copy.
 template <class T, int NB, bool BACK>
 __global__ __launch_bounds__(256, 2) void k_linear(LinearArgs a) {
     constexpr int BK = step_width<T>(), BN = 32 * NB, KS = BK / 16;
@@ -286,7 +289,10 @@ __global__ __launch_bounds__(256, 2) void k_linear_kept(LinearArgs a) {
 // dW over chunks of 2^chunk_shift rows: 128 outputs x 128 inputs a workgroup, its
 // waves 64 x 64 each. Both operands run along the rows, so both are read
 // turned from LDS. A band of one chunk is written at once, one of several as
-// 32-bit partial sums that k_linear_join adds in order.
+// 32-bit partial sums that k_linear_join adds in order: no atomics, so the sums
+// do not vary. 446,932 rows, 128 x 128, bfloat16: 65 us and 17 us for the join
+// (chunks of 512 rows: 71 and 23; of 2048: 98 and 13), of 48 at the rate of a
+// large copy; bound by waiting for loads, three waves a SIMD.
 __device__ inline float* dw_part(const LinearArgs& a, int64_t item) {
     return a.part + item * (static_cast<int64_t>(a.n_out) * a.n_in + a.n_out);
 }

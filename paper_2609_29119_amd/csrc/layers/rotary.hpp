@@ -39,7 +39,10 @@ __device__ inline void turn_of(const RotaryArgs& a, int64_t at, int p, float& cs
 
 // One item: V pairs (or V values past the pairs, which are copied) of one
 // token, for `each` heads: the angles are formed once and serve them all.
-// Rows need no more alignment than their element's.
+// Rows need no more alignment than their element's. Bound by memory:
+// 446,932 tokens of 8 + 2 heads of 64, bfloat16: 250 us (4.6 TB/s, 232 at the
+// rate of a large copy); 88,835 of 6 + 3 heads of 80 with 30 pairs, float32
+// (V = 2): 136 us (3.8 TB/s, 104).
 template <class T, int V>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, token = id / a.chunks;

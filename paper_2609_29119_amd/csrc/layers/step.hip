@@ -26,7 +26,8 @@ int check_step(int64_t streams, int64_t heads, int64_t kv_heads, int64_t dim, in
 int64_t head_blocks(int64_t heads, int64_t kv_heads) { return (heads / kv_heads + 31) / 32; }
 
 // Stretches of a cache: enough workgroups for four on each of the 256 compute
-// units, none shorter than 256 slots (two tiles for each wave).
+// units, none shorter than 256 slots (two tiles for each wave; a shorter cache
+// is one workgroup's and needs no join, which costs 6.5 us).
 int64_t splits_of(int64_t streams, int64_t heads, int64_t kv_heads, int64_t slots) {
     const int64_t blocks = std::max<int64_t>(1, streams * kv_heads * head_blocks(heads, kv_heads));
     return std::max<int64_t>(1, std::min<int64_t>({1024 / blocks, slots / 256, 256}));
