@@ -7,6 +7,14 @@
 
 namespace nsl {
 
+// The scores' factor in 32 bits, with and without log2(e), has to be a number.
+inline int check_scale(double scale) {
+    const float c = static_cast<float>(scale * 1.4426950408889634);
+    if (!(scale > 0) || !std::isfinite(c) || c < 1e-37f)
+        return set_err(NSGCQT_EINVAL, "scale must be positive and finite in 32 bits");
+    return NSGCQT_OK;
+}
+
 inline int check_shape(const nsgcqt_attention_shape* s) {
     if (!s) return set_err(NSGCQT_EINVAL, "shape is NULL");
     if (s->n_heads < 1 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads)
@@ -14,7 +22,7 @@ inline int check_shape(const nsgcqt_attention_shape* s) {
     if (s->head_dim < 1) return set_err(NSGCQT_EINVAL, "head_dim must be at least 1");
     if (s->left < 0 || s->right < 0 || s->sinks < 0)
         return set_err(NSGCQT_EINVAL, "left, right and sinks must not be negative");
-    if (!(s->scale > 0) || !std::isfinite(s->scale)) return set_err(NSGCQT_EINVAL, "scale must be positive and finite");
+    CHECK_TRY(check_scale(s->scale));
     if (s->head_dim > 128) return set_err(NSGCQT_EUNSUPPORTED, "head_dim above 128");
     if (s->n_heads > 65536) return set_err(NSGCQT_EUNSUPPORTED, "more than 65,536 heads");
     return NSGCQT_OK;

@@ -50,7 +50,7 @@ int nsgcqt_attention_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t
                           const int64_t* pos, void* ws, size_t ws_bytes, void* stream) {
     CHECK_TRY(check_dtype(dtype));
     CHECK_TRY(check_step(n_streams, n_heads, n_kv_heads, head_dim, window, sinks));
-    if (!(scale > 0) || !std::isfinite(scale)) return set_err(NSGCQT_EINVAL, "scale must be positive and finite");
+    CHECK_TRY(check_scale(scale));
     StepArgs a{};
     a.wide = true;
     CHECK_TRY(check_view(q, "q", dtype, n_streams, 1, n_heads, head_dim, a.wide));
@@ -129,11 +129,15 @@ int nsgcqt_cache_fill(int dtype, const nsgcqt_rows* r, int64_t n_kv_heads, int64
     a.slots = static_cast<int>(window + sinks);
     a.sinks = static_cast<int>(sinks);
     a.window = static_cast<int>(window);
-    const int64_t blocks = std::min<int64_t>((n_kv_heads * head_dim * (window + sinks) + 255) / 256,
-                                             std::max<int64_t>(1, 16384 / streams));
+    const int each = head_dim % 8 ? 1 : 8;
+    const int64_t blocks = std::min<int64_t>((n_kv_heads * head_dim / each * (window + sinks) + 255) / 256,
+                                             std::max<int64_t>(1, 65536 / streams));
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(streams));
     return by_type(dtype, [&](auto t) -> int {
-        LAUNCH_TRY(k_fill<decltype(t)>, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(streams)), dim3(256),
-                   0, static_cast<hipStream_t>(stream), a);
+        if (each == 8)
+            LAUNCH_TRY(k_fill<decltype(t), 8>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+        else
+            LAUNCH_TRY(k_fill<decltype(t), 1>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
         return NSGCQT_OK;
     });
 }

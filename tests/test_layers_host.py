@@ -103,7 +103,7 @@ def test_attention_refusals(L):
     refused(call(s=shape(dim=0)), nb.EINVAL, "head_dim")
     refused(call(s=shape(dim=129)), nb.EUNSUPPORTED, "128")
     refused(call(s=shape(left=-1)), nb.EINVAL, "negative")
-    for bad in (0.0, -1.0, float("inf"), float("nan")):
+    for bad in (0.0, -1.0, float("inf"), float("nan"), 1e300, 1e-300):
         refused(call(s=shape(scale=bad)), nb.EINVAL, "scale")
     refused(call(q=view(data=FAKE + 1)), nb.EINVAL, "aligned")
     assert call(r=rows(n=0)) == nb.OK
