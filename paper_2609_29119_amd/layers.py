@@ -474,8 +474,8 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
     with _on(q):
         _check(_lib().nsgcqt_attention_step(
             _DTYPES[q.dtype], streams, heads, kv_heads, dim, slots - sinks, sinks,
-            dim ** -0.5 if scale is None else float(scale), _view_step(q), _view_step(k), _view_step(v), _view_step(o), k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(),
-            ws.data_ptr() if n else None, n, _stream(q)))
+            dim ** -0.5 if scale is None else float(scale), _view_step(q), _view_step(k), _view_step(v), _view_step(o),
+            k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(), ws.data_ptr() if n else None, n, _stream(q)))
     return o
 
 
@@ -500,7 +500,11 @@ def cache_fill(k, v, offsets, k_cache, v_cache, sinks=0):
 
 
 class StreamCache:
-    """Ring caches of many streams: the first `sinks` tokens and the last `window` others of each."""
+    """Ring caches of many streams: the first `sinks` tokens and the last `window` others of each.
+
+    `pos` holds the number of each stream's next token; a stream whose pos is
+    below 0 is idle: its cache and its pos stay as they are.
+    """
 
     def __init__(self, streams, kv_heads, head_dim, window, sinks=0, dtype=torch.bfloat16, device="cuda"):
         if window < 1 or sinks < 0:
@@ -509,7 +513,7 @@ class StreamCache:
         shape = (streams, kv_heads, sinks + window, head_dim)
         self.k = torch.zeros(shape, dtype=dtype, device=device)
         self.v = torch.zeros(shape, dtype=dtype, device=device)
-        self.pos = torch.zeros(streams, dtype=torch.int64, device=device)   # number of each stream's next token
+        self.pos = torch.zeros(streams, dtype=torch.int64, device=device)
 
     def fill(self, k, v, offsets):
         """Starts the streams with whole bands (`cache_fill`)."""
@@ -517,7 +521,7 @@ class StreamCache:
         self.pos.copy_((offsets[1:] - offsets[:-1]).repeat(k.shape[0]))
 
     def step(self, q, k, v, scale=None):
-        """`attention_step` of every stream's next token."""
+        """`attention_step` of every stream's next token (zeros for an idle one)."""
         o = attention_step(q, k, v, self.k, self.v, self.pos, self.sinks, scale)
-        self.pos += 1
+        self.pos += self.pos >= 0
         return o

@@ -517,6 +517,18 @@ def test_step_in_a_graph_and_on_another_stream():
         assert torch.equal(cache.k, eager.k) and torch.equal(cache.v, eager.v) and torch.equal(cache.pos, eager.pos)
 
 
+def test_idle_stream_stays_idle():
+    """A stream without a token keeps its cache and its number over many steps, beside one that runs."""
+    cache = layers.StreamCache(2, 1, 16, 3, 1, dtype=torch.float32)
+    cache.pos[0] = -1
+    qkv = randn(0, 6, 2, 3, 16, dtype=torch.float32)
+    for t in range(6):
+        o = cache.step(qkv[t][:, :1], qkv[t][:, 1:2], qkv[t][:, 2:])
+        assert o[0].abs().max() == 0 and o[1].abs().max() > 0
+        assert cache.pos.tolist() == [-1, t + 1]
+    assert cache.k[0].abs().max() == 0 and cache.v[0].abs().max() == 0
+
+
 def test_example_trains_and_streams(repo_root):
     import importlib.util
     import os
