@@ -33,7 +33,12 @@ __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 // keys and not 383. The key gradient: 128 keys of one kv head.
 constexpr int kKeys = 128, kKeyShift = 7;
 __host__ __device__ inline int query_shift(int share) { return share == 4 ? 5 : share == 2 ? 6 : 7; }
-template <class T, int DP> constexpr int kv_tile() { return sizeof(T) == 4 && DP > 64 ? 32 : 64; }
+// Rows of a tile of keys (forward, dq) and of queries (key gradient): short
+// enough for two workgroups' tiles in a compute unit's LDS. 223,466 tokens,
+// 4 heads of 64 over 2, window 128, float32: 437 us forward and 2263 with
+// gradients; with tiles of 64 there 468 and 2799.
+template <class T, int DP> constexpr int key_tile() { return row_bytes<T, DP>() > 128 ? 32 : 64; }
+template <class T, int DP> constexpr int query_tile() { return sizeof(T) == 4 && DP > 32 ? 32 : 64; }
 
 template <class T> __device__ inline T* row_of(const View& v, int64_t b, int64_t row, int head) {
     return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row + head * v.head;
@@ -266,8 +271,8 @@ struct QueryWork {
 // which 300 are reading and writing (232 at the rate of a large copy) and 25
 // go to each 32 keys of the window.
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : sizeof(T) == 2 && WIDE ? 3 : 2) void k_attention(AttnArgs a) {
-    constexpr int BN = DP > 64 ? 32 : 64, RB = row_bytes<T, DP>();
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) void k_attention(AttnArgs a) {
+    constexpr int BN = key_tile<T, DP>(), RB = row_bytes<T, DP>();
     typedef Loader<T, DP, BN, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(16) float bias[2][BN];
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : sizeof(T) == 2
 // scores and dp are formed transposed, so ds is the B fragment of dq^T = K^T ds^T.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 || !WIDE ? 2 : 3) void k_attention_dq(AttnArgs a) {
-    constexpr int BN = DP > 64 ? 32 : 64, RB = row_bytes<T, DP>();
+    constexpr int BN = key_tile<T, DP>(), RB = row_bytes<T, DP>();
     typedef Loader<T, DP, BN, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(128) char grads[4][32 * RB];   // each wave's rows of do
@@ -585,8 +590,8 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 // far queries 180): 2.3 ms with the forward, 324 TFLOP/s of the formulas' work.
 // Bound by waiting: three waves a SIMD, half their cycles.
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 32 ? 1 : 2) : DP > 64 ? 1 : WIDE ? 3 : 2) void k_attention_dkv(AttnArgs a) {
-    constexpr int BQ = kv_tile<T, DP>();
+__global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 2 && WIDE ? 3 : 2) void k_attention_dkv(AttnArgs a) {
+    constexpr int BQ = query_tile<T, DP>();
     typedef Loader<T, DP, BQ, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
     __shared__ __align__(128) char values[4][32 * Ld::kRB];   // each wave's rows of v
