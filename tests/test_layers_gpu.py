@@ -351,6 +351,22 @@ def test_band_attention_strides_scale_and_uncovered_tokens(dtype):
         assert t[:, :first].abs().max() == 0 and t[:, first + 190:].abs().max() == 0
 
 
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("left,right,sinks,d", [(1, 0, 0, 64), (3, 0, 1, 128), (1, 1, 0, 30), (20, 0, 2, 32)])
+def test_query_gradient_of_few_keys(left, right, sinks, d, dtype):
+    """With few keys do . v - do . o is small beside do . o, whose error must not reach dq: what is left is dq's own
+    rounding (uniform in half a unit of the last place: u / sqrt(3) of the 2-norm at most) and 32-bit sums. With
+    the widest window here delta's error adds less to it than that bound, taken at its largest, has to spare."""
+    lengths = [600, 3, 45]
+    q, k, v, do = (randn(i, 1, sum(lengths), n, d, dtype=dtype).requires_grad_(i < 4)
+                   for i, n in ((1, 4), (2, 2), (3, 2), (4, 4)))
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, right, sinks)
+    (dq,) = torch.autograd.grad(o, [q], do)
+    want = attention_reference(q, k, v, lengths, 0, left, right, sinks, d ** -0.5, None, do)[1]
+    err = ((dq.double().cpu() - want).norm() / want.norm()).item()
+    assert err <= U[dtype] / 3 ** 0.5 + 64 * 2.0 ** -24, err
+
+
 def test_gradients_against_differences():
     """Directional central differences of a scalar loss in 32 bits: truncation
     is of the order of h^2 = 1e-4, cancellation 2^-24 / h = 6e-6 of the loss' terms."""
