@@ -17,8 +17,9 @@
  *   - Data are float32, float16 or bfloat16 (nsgcqt_dtype), one type a call.
  *     Products, sums, softmax statistics and angles are held in 32 bits or
  *     more; each result is rounded once. In 16-bit attention the
- *     probabilities and their gradients are rounded to the data's type
- *     before their products.
+ *     probabilities enter their product as two numbers of the data's type,
+ *     the rounded one and what the rounding left; in the single-token step
+ *     and in the key gradient (where ds does too) as the rounded one alone.
  *   - A tensor is an nsgcqt_view: a device pointer and the strides, in
  *     elements, of its batch, row (token) and head axes; the last axis is
  *     contiguous. Pointers are aligned to their element. 16-byte aligned

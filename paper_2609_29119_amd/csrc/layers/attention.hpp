@@ -259,17 +259,16 @@ struct QueryWork {
 // Forward. One pass over the visible keys with a running maximum and sum. The
 // scores are formed transposed (a lane has one query), so a row's maximum and
 // sum need one exchange between the wave's halves, and the probabilities are
-// the B fragment of o^T = V^T p^T without leaving the registers. p is rounded
-// to the data's type for that product (16 bits: o is off by 0.0022 in the
-// 2-norm in bfloat16, its own rounding is 0.0017); sums take it unrounded.
+// the B fragment of o^T = V^T p^T without leaving the registers. In 16 bits p
+// goes into that product as two numbers, the rounded one and what the rounding
+// left: with one alone o is off by 0.0022 in the 2-norm in bfloat16, with two
+// by its own rounding, 0.0016. Sums take p unrounded.
 //
-// 131,072 tokens, 8 heads of 128 over 2, window 1024: 667 us, 826 TFLOP/s of
-// visible pairs (457 us at the rate of a large product): the matrix cores wait
-// for the exponentials (a quarter of the vector rate) and the maxima. Tiles of
-// 32 keys there, three waves a SIMD: with 64 and two waves 760 us.
-// 446,932 tokens in 221 bands, 8 heads of 64 over 2, window 256: 600 us, of
-// which 300 are reading and writing (232 at the rate of a large copy) and 25
-// go to each 32 keys of the window.
+// 131,072 tokens, 8 heads of 128 over 2, window 1024: 913 us (667 with p as
+// one number; 457 at the rate of a large product, of which p's second number
+// takes half as much again): the matrix cores wait for the exponentials (a
+// quarter of the vector rate) and the maxima. Tiles of 32 keys there, three
+// waves a SIMD.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) void k_attention(AttnArgs a) {
     constexpr int BN = key_tile<T, DP>(), RB = row_bytes<T, DP>();
@@ -369,10 +368,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) 
                 }
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const frag<T> p = narrow<T>(s, x);
+                    const frag<T> p = narrow<T>(s, x), low = rest_of<T>(s, x, p);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d)
-                        o[d] = mma(read_turned<T, RB>(vt, 32 * kb + 16 * x, 32 * d, lane), p, o[d]);
+                    for (int d = 0; d < DP / 32; ++d) {
+                        const frag<T> vd = read_turned<T, RB>(vt, 32 * kb + 16 * x, 32 * d, lane);
+                        o[d] = mma(vd, p, o[d]);
+                        if constexpr (sizeof(T) == 2) o[d] = mma(vd, low, o[d]);
+                    }
                 }
             }
             tile_barrier();
@@ -516,10 +518,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
                     if (pass == 0) continue;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const frag<T> ds = narrow<T>(s, x);
-                        frag<T> low;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) low[e] = static_cast<T>(s[8 * x + e] - static_cast<float>(ds[e]));
+                        const frag<T> ds = narrow<T>(s, x), low = rest_of<T>(s, x, ds);
 #pragma unroll
                         for (int d = 0; d < DP / 32; ++d) {
                             const frag<T> kd = read_turned<T, RB>(kt, 32 * kb + 16 * x, 32 * d, lane);

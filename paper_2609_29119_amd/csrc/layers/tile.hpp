@@ -72,6 +72,15 @@ template <class T> __device__ inline frag<T> narrow(const acc16& c, int s) {
     return f;
 }
 
+// What `narrow` left of them, rounded to T in turn. The two fragments together
+// hold 16 bits of each value in bfloat16 and 22 in float16.
+template <class T> __device__ inline frag<T> rest_of(const acc16& c, int s, const frag<T>& f) {
+    frag<T> low;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) low[j] = static_cast<T>(c[8 * s + j] - static_cast<float>(f[j]));
+    return low;
+}
+
 // 8 values at p, of which the first n are there (n may be <= 0 or past 8).
 // WIDE: p is 16-byte aligned and n is never between 0 and 8. Else p is
 // aligned to its element only, which the memory pipeline takes too; a row's

@@ -634,3 +634,30 @@ def test_refusals():
         layers.attention_step(q[0, :2], q[0, :2, :1], q[0, :2, :1], c.k, c.v, c.pos, 10)
     with pytest.raises(ValueError):
         layers.attention_step(q[0, :2].requires_grad_(), q[0, :2, :1], q[0, :2, :1], c.k, c.v, c.pos, 2)
+
+
+# --------------------------------------------- 16-bit results: their own rounding
+
+
+def beyond_rounding(got, exact, eps, what):
+    """A 16-bit result that is off by its own rounding only. A value whose 32-bit form is off by eps of itself rounds
+    to another neighbour of the exact one with probability eps / u at most, and is then 2 u away: 2 sqrt(eps u) in the
+    2-norm, here with a factor of two."""
+    u, exact = U[got.dtype], exact.detach().double().cpu()
+    err = (got.detach().cpu().double() - exact.to(got.dtype).double()).norm().item() / exact.norm().item()
+    assert err <= 4 * (eps * u) ** 0.5, f"{what}: {err:.3g} over {4 * (eps * u) ** 0.5:.3g}"
+
+
+# Of the probabilities' two numbers (16 bits of each in bfloat16, 22 in float16) and of scores up to 16 in 32 bits.
+ATTENTION_EPS = {torch.bfloat16: 2.0 ** -17 + 2.0 ** -20, torch.float16: 2.0 ** -19}
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("d,left,right,sinks", [(64, 300, 0, 4), (128, 200, 0, 0), (30, None, None, 0), (33, 90, 20, 3)])
+def test_attention_rounds_once(d, left, right, sinks, dtype):
+    """The probabilities' rounding does not reach the result: it rounds once, at the end."""
+    lengths = [700, 45]
+    q, k, v = (randn(i, 1, sum(lengths), n, d, dtype=dtype) for i, n in ((1, 4), (2, 2), (3, 2)))
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, right, sinks)
+    want = attention_reference(q, k, v, lengths, 0, left, right, sinks, d ** -0.5, None, torch.zeros_like(q))[0]
+    beyond_rounding(o, want, ATTENTION_EPS[dtype], "o")
