@@ -18,8 +18,8 @@
  *     Products, sums, softmax statistics and angles are held in 32 bits or
  *     more; each result is rounded once. In 16-bit attention the
  *     probabilities enter their product as two numbers of the data's type,
- *     the rounded one and what the rounding left; in the single-token step
- *     and in the key gradient (where ds does too) as the rounded one alone.
+ *     the rounded one and what the rounding left; in the key gradient they
+ *     and ds enter as the rounded one alone.
  *   - A tensor is an nsgcqt_view: a device pointer and the strides, in
  *     elements, of its batch, row (token) and head axes; the last axis is
  *     contiguous. Pointers are aligned to their element. 16-byte aligned

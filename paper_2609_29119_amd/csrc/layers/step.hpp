@@ -27,6 +27,7 @@ __device__ inline int ring_slot(int64_t t, int sinks, int window) {
 // (the columns of S^T = K Q^T), and one of `splits` stretches of the slots;
 // its waves take every fourth tile of 32 slots. K goes from memory to
 // fragments; V goes through a stretch of LDS of the wave's own to be turned.
+// In 16 bits p enters its product as two numbers, as in k_attention.
 // Bound by reading the cache: 3,536 streams of 260 slots, 8 heads of 64 over 2,
 // bfloat16: 107 us (4.1 TB/s, 90 at the rate of a large copy); 4 streams of
 // 131,076 slots of 128, float16: 100 us and 6.5 for the join (5.1 TB/s, 109).
@@ -122,9 +123,13 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const frag<T> p = narrow<T>(s, x);
+            const frag<T> p = narrow<T>(s, x), low = rest_of<T>(s, x, p);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) o[d] = mma(read_turned<T, RB>(vt[wave], 16 * x, 32 * d, lane), p, o[d]);
+            for (int d = 0; d < DP / 32; ++d) {
+                const frag<T> vd = read_turned<T, RB>(vt[wave], 16 * x, 32 * d, lane);
+                o[d] = mma(vd, p, o[d]);
+                if constexpr (sizeof(T) == 2) o[d] = mma(vd, low, o[d]);
+            }
         }
     }
     // the four waves' results, in the waves' order

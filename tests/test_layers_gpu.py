@@ -661,3 +661,17 @@ def test_attention_rounds_once(d, left, right, sinks, dtype):
     o = layers.band_attention(q, k, v, offsets_of(lengths), left, right, sinks)
     want = attention_reference(q, k, v, lengths, 0, left, right, sinks, d ** -0.5, None, torch.zeros_like(q))[0]
     beyond_rounding(o, want, ATTENTION_EPS[dtype], "o")
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("slots,d", [(260, 64), (5000, 64), (301, 40), (3000, 128)])
+def test_step_rounds_once(slots, d, dtype):
+    """As test_attention_rounds_once, for the single-token form: one workgroup a cache, and split ones."""
+    n, h, hk = 5, 8, 2
+    kc, vc = randn(1, n, hk, slots, d, dtype=dtype), randn(2, n, hk, slots, d, dtype=dtype)
+    q, k, v = randn(3, n, h, d, dtype=dtype), randn(4, n, hk, d, dtype=dtype), randn(5, n, hk, d, dtype=dtype)
+    pos = torch.full((n,), 3 * slots, dtype=torch.int64, device="cuda")
+    o = layers.attention_step(q, k, v, kc, vc, pos, 4)
+    want = torch.stack([step_reference(q[s].cpu(), kc[s].transpose(0, 1).cpu(), vc[s].transpose(0, 1).cpu(), slots,
+                                       slots, 1, d ** -0.5) for s in range(n)])
+    beyond_rounding(o, want, ATTENTION_EPS[dtype], "o")
