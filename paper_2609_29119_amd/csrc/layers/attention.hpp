@@ -10,6 +10,10 @@
 
 namespace nsl {
 
+struct AttnScale {
+    float c, unit;   // scale log2(e): exp(scale s) = exp2(c s); the scores' difference of one power of two, 1 / c
+};
+
 // The kernels' WIDE: every view takes 16-byte accesses.
 struct AttnArgs {
     View q, k, v, o, d_o, dq, dk, dv;
@@ -22,10 +26,43 @@ struct AttnArgs {
     int rows, n_bands, batch, heads, kv_heads, dim;
     int share;            // heads of one kv head that a workgroup takes: 1, 2 or 4
     int left, right, sinks;   // at most rows
-    float scale, c;           // c = scale log2(e): exp(scale s) = exp2(c s)
+    float scale;
+    AttnScale by;
 };
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The base of a running softmax: what is subtracted from the scores before
+// the exponential. It is the maximum, but may lag by LAG powers of two: sums
+// and outputs are rescaled when it moves by more, which is rare after the
+// first keys. Float16 has no numbers between 0 and 2^-24, and keys of smaller
+// probabilities may add up to a result: there the base also follows the scores
+// of the last 32 keys down where they lie kDown powers of two below it (sums
+// and outputs, in 32 bits, then grow; by 2^kDeep at most), and probabilities
+// are formed times 2^kLift: the largest of 32 keys lies in 2^-1 .. 2^15.
+template <class T, int LAG> struct Base {
+    static constexpr bool kHalf = std::is_same<T, _Float16>::value;
+    static constexpr float kDown = 8.f, kDeep = 48.f, kLift = kHalf ? 15.f - LAG : 0.f;
+    float top = -INFINITY, peak = -INFINITY;   // the base's score; the largest score yet (float16)
+
+    // Takes the largest score of the next keys: true if `factor` has to be
+    // applied to what was summed before.
+    __device__ bool move(float mx, const AttnScale& by, float& factor) {
+        bool far = LAG ? mx > top + LAG * by.unit : mx > top;
+        if constexpr (kHalf) {
+            peak = fmaxf(peak, mx);
+            far |= mx < top - kDown * by.unit && mx > -INFINITY && top > peak - kDeep * by.unit;
+        }
+        if (!__any(far)) return false;
+        float now = fmaxf(top, mx);
+        if constexpr (kHalf) now = mx > -INFINITY ? fmaxf(mx, peak - kDeep * by.unit) : top;
+        factor = now == -INFINITY ? 1.f : exp2_((top - now) * by.c);
+        top = now;
+        return true;
+    }
+    // in powers of two: a key's probability is exp2(c score - of(c))
+    __device__ float of(const AttnScale& by) const { return top == -INFINITY ? 0.f : fmaf(top, by.c, -kLift); }
+};
 
 // A workgroup has four waves of 32 rows each. Forward and dq: `share` heads of
 // one kv head, 128 / share queries of each, so that the waves need (nearly)
@@ -300,8 +337,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) 
     acc16 o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) o[d] = zero16();
-    float top = -INFINITY, sum = 0.f;   // running maximum of the raw scores (up to slack); this half's sum
-    const float slack = 8.f / a.c;
+    float sum = 0.f;   // this half's
+    Base<T, 8> base;
 
     const KeyRange range(a, q0, min(q0 + w.queries, len) - 1, len, BN);
     const Ld ld(a.k.row, a.v.row, a.dim, wave, lane);
@@ -351,19 +388,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) 
 #pragma unroll
                 for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
                 mx = half_max(mx);
-                // the maximum may lag by 8 powers of two: sums and outputs are
-                // rescaled when it grows by more, which is rare after the first keys
-                if (__any(mx > top + slack)) {
-                    const float now = fmaxf(top, mx), alpha = now == -INFINITY ? 1.f : exp2_((top - now) * a.c);
-                    sum *= alpha;
+                float factor;
+                if (base.move(mx, a.by, factor)) {
+                    sum *= factor;
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
-                    top = now;
+                    for (int d = 0; d < DP / 32; ++d) o[d] *= factor;
                 }
-                const float base = top == -INFINITY ? 0.f : top * a.c;
+                const float zero = base.of(a.by);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[r] = exp2_(fmaf(s[r], a.c, -base));
+                    s[r] = exp2_(fmaf(s[r], a.by.c, -zero));
                     sum += s[r];
                 }
 #pragma unroll
@@ -389,7 +423,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) 
         store_column<T>(out, o[d], 32 * d, a.dim, WIDE, lane);
     }
     if (stats && mine && h == 0)
-        stats[i] = total == 0.f ? INFINITY : (top == -INFINITY ? 0.f : top * a.c) + __log2f(total);
+        stats[i] = total == 0.f ? INFINITY : base.of(a.by) + __log2f(total);
 }
 
 // --------------------------------------------------------------- gradients
@@ -512,7 +546,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
                     if (KeyRange::edge(a, j, i_lo, i_hi)) hide_edges<true>(s, dp, a, i, j, h);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        s[r] = exp2_(fmaf(s[r], a.c, -lse)) * (dp[r] - delta);
+                        s[r] = exp2_(fmaf(s[r], a.by.c, -lse)) * (dp[r] - delta);
                         rest += s[r];
                     }
                     if (pass == 0) continue;
@@ -690,7 +724,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 2 && WIDE ? 3 : 2) 
                 if (!skip) {
                     const bool edge = j_hi > i_lo + a.right || (j_lo < i_hi - a.left && j_hi >= a.sinks);
                     key_grad<T, DP>(lds[u][0], lds[u][1], row_lse[u], row_delta[u], 32 * qb, kf, values[wave], dk, dv,
-                                    a.c, edge, j - a.right - i_lo, span, lane);
+                                    a.by.c, edge, j - a.right - i_lo, span, lane);
                 }
             }
             tile_barrier();
@@ -790,7 +824,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
         if (n + 1 < total) fetch(n + 1);
         if (32 * wave < BQ && i_begin + n % q_tiles * BQ + 32 * wave < i_end)
             key_grad<T, DP>(lds[n & 1], lds[n & 1] + Ld::kBytes, row_lse[n & 1], row_delta[n & 1], 32 * wave, kf,
-                            values, dk, dv, a.c, false, 0, 0, lane);
+                            values, dk, dv, a.by.c, false, 0, 0, lane);
         tile_barrier();
     }
     float(*joined)[DP][33] = reinterpret_cast<float(*)[DP][33]>(&lds[0][0]);

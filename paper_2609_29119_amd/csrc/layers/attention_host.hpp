@@ -15,6 +15,11 @@ inline int check_scale(double scale) {
     return NSGCQT_OK;
 }
 
+inline AttnScale scale_of(double scale) {
+    const double c = scale * 1.4426950408889634;
+    return {static_cast<float>(c), static_cast<float>(1.0 / c)};
+}
+
 inline int check_shape(const nsgcqt_attention_shape* s) {
     if (!s) return set_err(NSGCQT_EINVAL, "shape is NULL");
     if (s->n_heads < 1 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads)
@@ -46,7 +51,7 @@ inline AttnArgs attention_args(const nsgcqt_rows* r, const nsgcqt_attention_shap
     a.right = cut(s->right);
     a.sinks = cut(s->sinks);
     a.scale = static_cast<float>(s->scale);
-    a.c = static_cast<float>(s->scale * 1.4426950408889634);
+    a.by = scale_of(s->scale);
     return a;
 }
 

@@ -52,17 +52,17 @@ int nsgcqt_attention_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t
     CHECK_TRY(check_step(n_streams, n_heads, n_kv_heads, head_dim, window, sinks));
     CHECK_TRY(check_scale(scale));
     StepArgs a{};
-    a.wide = true;
-    CHECK_TRY(check_view(q, "q", dtype, n_streams, 1, n_heads, head_dim, a.wide));
-    CHECK_TRY(check_view(k, "k", dtype, n_streams, 1, n_kv_heads, head_dim, a.wide));
-    CHECK_TRY(check_view(v, "v", dtype, n_streams, 1, n_kv_heads, head_dim, a.wide));
-    CHECK_TRY(check_view(o, "o", dtype, n_streams, 1, n_heads, head_dim, a.wide));
+    bool wide = true;
+    CHECK_TRY(check_view(q, "q", dtype, n_streams, 1, n_heads, head_dim, wide));
+    CHECK_TRY(check_view(k, "k", dtype, n_streams, 1, n_kv_heads, head_dim, wide));
+    CHECK_TRY(check_view(v, "v", dtype, n_streams, 1, n_kv_heads, head_dim, wide));
+    CHECK_TRY(check_view(o, "o", dtype, n_streams, 1, n_heads, head_dim, wide));
     if (n_streams == 0) return NSGCQT_OK;
     const size_t e = elem_bytes(dtype);
     if (!k_cache || !v_cache || misaligned(k_cache, e) || misaligned(v_cache, e))
         return set_err(NSGCQT_EINVAL, "a cache is NULL or not aligned to its element");
     if (!pos || misaligned(pos, 8)) return set_err(NSGCQT_EINVAL, "pos is NULL or not aligned to 8 bytes");
-    a.wide = a.wide && !misaligned(k_cache, 16) && !misaligned(v_cache, 16);
+    wide = wide && !misaligned(k_cache, 16) && !misaligned(v_cache, 16);
     a.splits = static_cast<int>(splits_of(n_streams, n_heads, n_kv_heads, window + sinks));
     const int64_t need = nsgcqt_attention_step_workspace(n_streams, n_heads, n_kv_heads, head_dim, window, sinks);
     if (static_cast<int64_t>(ws_bytes) < need)
@@ -87,14 +87,14 @@ int nsgcqt_attention_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t
     a.slots = static_cast<int>(window + sinks);
     a.sinks = static_cast<int>(sinks);
     a.window = static_cast<int>(window);
-    a.c = static_cast<float>(scale * 1.4426950408889634);
+    a.by = scale_of(scale);
     const int64_t blocks = n_streams * n_kv_heads * a.head_blocks * a.splits;
     CHECK_TRY(check_grid(blocks));
     CHECK_TRY(check_grid(n_streams * n_heads));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return by_type_and_width(dtype, head_dim, [&](auto t, auto dp) -> int {
+    return by_shape(dtype, head_dim, wide, [&](auto t, auto dp, auto w) -> int {
         using T = decltype(t);
-        LAUNCH_TRY(k_step<T, decltype(dp)::value>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
+        LAUNCH_TRY(k_step<T, decltype(dp)::value, decltype(w)::value>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
         if (a.splits > 1)
             LAUNCH_TRY(k_step_join<T>, dim3(static_cast<unsigned>(n_streams * n_heads)), dim3(256), 0, st, a);
         return NSGCQT_OK;

@@ -15,8 +15,7 @@ struct StepArgs {
     int64_t streams;
     int heads, kv_heads, dim, group, head_blocks, splits;
     int slots, sinks, window;
-    float c;
-    bool wide;
+    AttnScale by;
 };
 
 __device__ inline int ring_slot(int64_t t, int sinks, int window) {
@@ -31,7 +30,7 @@ __device__ inline int ring_slot(int64_t t, int sinks, int window) {
 // Bound by reading the cache: 3,536 streams of 260 slots, 8 heads of 64 over 2,
 // bfloat16: 107 us (4.1 TB/s, 90 at the rate of a large copy); 4 streams of
 // 131,076 slots of 128, float16: 100 us and 6.5 for the join (5.1 TB/s, 109).
-template <class T, int DP>
+template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     constexpr int RB = row_bytes<T, DP>(), kEach = 32 * DP / 8 / 64;
     __shared__ __align__(128) char vt[4][32 * RB];
@@ -69,26 +68,25 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     const T* qp = reinterpret_cast<T*>(a.q.data) + stream * a.q.batch +
                   static_cast<int64_t>(kv * a.group + h_first + (mine ? m : 0)) * a.q.head;
     frag<T> qf[DP / 16], kf[DP / 16], vr[kEach];
-    load_rows<T, DP>(qf, qp, mine && n > 0, a.dim, a.wide, lane);
+    load_rows<T, DP>(qf, qp, mine && n > 0, a.dim, WIDE, lane);
     acc16 o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) o[d] = zero16();
-    float top = -INFINITY, sum = 0.f;
+    float sum = 0.f;
+    Base<T, 0> base;
 
     auto fetch = [&](int t) {
         const int key = 32 * t + m;
         const T* kr = key == fresh ? kn : kc + static_cast<int64_t>(key) * a.dim;
-        by_width(a.wide, [&](auto wide) {
 #pragma unroll
-            for (int s = 0; s < DP / 16; ++s)
-                kf[s] = load8<T, wide.value>(kr + 16 * s + 8 * h, key < n ? a.dim - 16 * s - 8 * h : 0, s + h > 0);
+        for (int s = 0; s < DP / 16; ++s)
+            kf[s] = load8<T, WIDE>(kr + 16 * s + 8 * h, key < n ? a.dim - 16 * s - 8 * h : 0, s + h > 0);
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) {
-                const int c = lane + 64 * e, slot = 32 * t + c / (DP / 8), d = c % (DP / 8) * 8;
-                vr[e] = load8<T, wide.value>((slot == fresh ? vn : vc + static_cast<int64_t>(slot) * a.dim) + d,
-                                             slot < n ? a.dim - d : 0, d > 0);
-            }
-        });
+        for (int e = 0; e < kEach; ++e) {
+            const int c = lane + 64 * e, slot = 32 * t + c / (DP / 8), d = c % (DP / 8) * 8;
+            vr[e] = load8<T, WIDE>((slot == fresh ? vn : vc + static_cast<int64_t>(slot) * a.dim) + d,
+                                   slot < n ? a.dim - d : 0, d > 0);
+        }
     };
     if (t0 + wave < t1) fetch(t0 + wave);
     for (int t = t0 + wave; t < t1; t += 4) {
@@ -108,17 +106,16 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
         float mx = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        const float now = fmaxf(top, half_max(mx)), base = now == -INFINITY ? 0.f : now * a.c;
-        if (__any(now != top)) {
-            const float alpha = exp2_(fmaf(top, a.c, -base));
-            sum *= alpha;
+        float factor;
+        if (base.move(half_max(mx), a.by, factor)) {
+            sum *= factor;
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
-            top = now;
+            for (int d = 0; d < DP / 32; ++d) o[d] *= factor;
         }
+        const float zero = base.of(a.by);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            s[r] = exp2_(fmaf(s[r], a.c, -base));
+            s[r] = exp2_(fmaf(s[r], a.by.c, -zero));
             sum += s[r];
         }
 #pragma unroll
@@ -135,12 +132,12 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     // the four waves' results, in the waves' order
     sum = half_sum(sum);
     if (h == 0) {
-        tops[wave][m] = top;
+        tops[wave][m] = base.top;
         sums[wave][m] = sum;
     }
     __syncthreads();
     const float all = fmaxf(fmaxf(tops[0][m], tops[1][m]), fmaxf(tops[2][m], tops[3][m]));
-    const float base = all == -INFINITY ? 0.f : all * a.c, share = exp2_(fmaf(top, a.c, -base));
+    const float share = exp2_(fmaf(base.top, a.by.c, all == -INFINITY ? 0.f : -all * a.by.c));
     for (int v = 0; v < 4; ++v) {
         if (wave == v) {
 #pragma unroll
@@ -157,10 +154,10 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
         const int hd = x / a.dim, d = x - hd * a.dim;
         const int head = kv * a.group + h_first + hd;
         const float am = fmaxf(fmaxf(tops[0][hd], tops[1][hd]), fmaxf(tops[2][hd], tops[3][hd]));
-        const float bm = am == -INFINITY ? 0.f : am * a.c;
+        const float bm = am == -INFINITY ? 0.f : am * a.by.c;
         float total = 0.f;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) total += sums[v][hd] * exp2_(fmaf(tops[v][hd], a.c, -bm));
+        for (int v = 0; v < 4; ++v) total += sums[v][hd] * exp2_(fmaf(tops[v][hd], a.by.c, -bm));
         const float val = joined[d][hd];
         if (a.splits == 1) {
             reinterpret_cast<T*>(a.o.data)[stream * a.o.batch + head * a.o.head + d] =
@@ -192,7 +189,7 @@ __global__ __launch_bounds__(256) void k_step_join(StepArgs a) {
     if (lane == 0) tops[wave] = top;
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float base = top == -INFINITY ? 0.f : top * a.c, w = exp2_(fmaf(mine, a.c, -base));
+    const float base = top == -INFINITY ? 0.f : top * a.by.c, w = exp2_(fmaf(mine, a.by.c, -base));
     weight[tid] = w;
     float total = there ? p[tid * stride + a.dim + 1] * w : 0.f;
 #pragma unroll

@@ -675,3 +675,26 @@ def test_step_rounds_once(slots, d, dtype):
     want = torch.stack([step_reference(q[s].cpu(), kc[s].transpose(0, 1).cpu(), vc[s].transpose(0, 1).cpu(), slots,
                                        slots, 1, d ** -0.5) for s in range(n)])
     beyond_rounding(o, want, ATTENTION_EPS[dtype], "o")
+
+
+def test_float16_sums_small_probabilities():
+    """Many keys of a probability near 2^-25.5 beside one near 1: float16's smallest number is 2^-24, yet they are a
+    part of the sum, and all of the result where the one key's value is zero."""
+    n, d, a = 4096, 16, 4.2
+    q = torch.zeros(1, n, 1, d, dtype=torch.float16, device="cuda")
+    k, v = torch.zeros_like(q), torch.ones_like(q)
+    q[..., 0], k[:, 0, :, 0], v[:, 0] = a, a, 0.0
+    s = float(q[0, 0, 0, 0]) ** 2
+    want = (n - 1) * np.exp(-s) / (1 + (n - 1) * np.exp(-s))
+    # the result's rounding (its value is normal: above 2^-14), and a score of 18 in 32 bits through the exponential
+    bound = 2 * (U[torch.float16] + 18 * 2.0 ** -23)
+    assert want > 2.0 ** -14
+    o = layers.band_attention(q, k, v, offsets_of([n]), None, None, scale=1.0)
+    assert (o.double() / want - 1).abs().max().item() <= bound
+    for slots in (n, 200):     # split and joined, and one workgroup
+        kc, vc = k[:, :slots].transpose(1, 2).contiguous(), v[:, :slots].transpose(1, 2).contiguous()
+        pos = torch.full((1,), slots - 1, dtype=torch.int64, device="cuda")
+        o = layers.attention_step(q[:, 1], k[:, 1], v[:, 1], kc, vc, pos, scale=1.0)
+        want = (slots - 1) * np.exp(-s) / (1 + (slots - 1) * np.exp(-s))
+        # below 2^-14 the result is a multiple of 2^-24
+        assert (o.double() - want).abs().max().item() <= bound * want + 2.0 ** -25
