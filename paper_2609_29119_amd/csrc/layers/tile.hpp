@@ -378,37 +378,62 @@ inline __host__ __device__ int64_t tile_count(int shift, int64_t n_bands, int64_
     return ((mult * rows) >> shift) + n_bands + 2;
 }
 
-__device__ inline int band_bound(const int64_t* off, int n_bands, int rows, int i) {
+inline __host__ __device__ int band_bound(const int64_t* off, int n_bands, int rows, int i) {
     if (i <= 0) return 0;
     if (i >= n_bands + 2) return rows;
     const int64_t o = off[i - 1];
     return o < 0 ? 0 : o > rows ? rows : static_cast<int>(o);
 }
 
-template <class I>
-__device__ inline Tile<I> find_tile(const int64_t* off, int n_bands, int rows, I mult, int shift, I p, int lane) {
-    int lo = 0, hi = n_bands + 2, bound = 0, at = 0;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        bound = band_bound(off, n_bands, rows, i);
-        const bool below = i < hi && ((mult * bound) >> shift) + i <= p;
-        const int count = __popcll(__ballot(below));
+// The band of item p among the bounds lo .. hi - 1, in rounds of 64 bounds
+// that are `step` apart: a round's `count` is how many of them, from lo on,
+// begin at or before p. At the end `lo` is the band's bound, which lane `at`
+// of the last round held; its next lane held the next bound only if that
+// round went in steps of one (a round in larger steps may end the search too:
+// when its last bound is the only one left).
+struct BandSearch {
+    int lo = 0, hi, step = 0, at = 0;
+    __host__ __device__ explicit BandSearch(int n_bands) : hi(n_bands + 2) {}
+    __host__ __device__ bool more() const { return hi - lo > 1; }
+    __host__ __device__ void open() { step = (hi - lo + 63) >> 6; }
+    __host__ __device__ void close(int count) {
         at = count > 1 ? count - 1 : 0;
         lo += at * step;
         hi = lo + step < hi ? lo + step : hi;
     }
-    // the last round went in steps of one: its lanes hold the bounds
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    at = __builtin_amdgcn_readfirstlane(at);
+    __host__ __device__ bool next_held() const { return step == 1 && at < 63; }
+};
+
+// Whether item p lies at or behind the first item of bound i, token `bound`.
+template <class I> __host__ __device__ inline bool item_from(I mult, int bound, int shift, int i, I p) {
+    return ((mult * bound) >> shift) + i <= p;
+}
+
+// The tile of item p, between the bounds a (of band lo - 1) and b.
+template <class I> __host__ __device__ inline Tile<I> tile_of(int lo, int a, int b, I mult, int shift, I p) {
     Tile<I> t;
-    const int a = __builtin_amdgcn_readlane(bound, at);
-    const int b = at < 63 ? __builtin_amdgcn_readlane(bound, at + 1) : band_bound(off, n_bands, rows, lo + 1);
     t.band = lo - 1;
     t.start = a;
     t.len = b > a ? b - a : 0;
     t.first = (p - (((mult * a) >> shift) + lo)) << shift;
     t.live = t.first >= 0 && t.first < mult * t.len;
     return t;
+}
+
+template <class I>
+__device__ inline Tile<I> find_tile(const int64_t* off, int n_bands, int rows, I mult, int shift, I p, int lane) {
+    BandSearch s(n_bands);
+    int bound = 0;
+    while (s.more()) {
+        s.open();
+        const int i = s.lo + lane * s.step;
+        bound = band_bound(off, n_bands, rows, i);
+        s.close(__popcll(__ballot(i < s.hi && item_from(mult, bound, shift, i, p))));
+    }
+    const int lo = __builtin_amdgcn_readfirstlane(s.lo), at = __builtin_amdgcn_readfirstlane(s.at);
+    const int a = __builtin_amdgcn_readlane(bound, at);
+    const int b = s.next_held() ? __builtin_amdgcn_readlane(bound, at + 1) : band_bound(off, n_bands, rows, lo + 1);
+    return tile_of(lo, a, b, mult, shift, p);
 }
 
 // The number of this thread's wave, in a scalar register: what follows from

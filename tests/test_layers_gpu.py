@@ -698,3 +698,23 @@ def test_float16_sums_small_probabilities():
         want = (slots - 1) * np.exp(-s) / (1 + (slots - 1) * np.exp(-s))
         # below 2^-14 the result is a multiple of 2^-24
         assert (o.double() - want).abs().max().item() <= bound * want + 2.0 ** -25
+
+
+@pytest.mark.parametrize("bands,batch", [(4095, 3), (5000, 1)])
+def test_thousands_of_bands(bands, batch):
+    """More bands than two rounds of the search cover in steps of one: products and attention with their gradients."""
+    lengths = np.random.default_rng(bands).integers(0, 12, bands)
+    lengths[:: bands // 7] += 60
+    rows, off = int(lengths.sum()), offsets_of(lengths)
+    x, w = randn(1, batch, rows, 6).requires_grad_(), randn(2, bands, 5, 6).requires_grad_()
+    b, dy = randn(3, bands, 5).requires_grad_(), randn(4, batch, rows, 5)
+    y = layers.band_linear(x, w, off, b)
+    ref = linear_reference(x, w, b, lengths, 0, dy)
+    for got, r, name in zip((y, *torch.autograd.grad(y, [x, w, b], dy)), ref, ("y", "dx", "dw", "db")):
+        close(got, r, product_bound(torch.float32, 6 if name == "y" else 200), name)
+    q, k, v, do = (randn(i, 1, rows, 1, 8).requires_grad_(i < 8) for i in (5, 6, 7, 8))
+    o = layers.band_attention(q, k, v, off, 20, 0, 2)
+    ref = attention_reference(q, k, v, lengths, 0, 20, 0, 2, 8 ** -0.5, None, do)
+    close(o, ref[0], attention_bound(torch.float32), "o")
+    for got, r, name, size in zip(torch.autograd.grad(o, [q, k, v], do), ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+        close(got, r, attention_bound(torch.float32, True), name, size)
