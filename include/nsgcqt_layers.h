@@ -17,9 +17,9 @@
  *   - Data are float32, float16 or bfloat16 (nsgcqt_dtype), one type a call.
  *     Products, sums, softmax statistics and angles are held in 32 bits or
  *     more; each result is rounded once. In 16-bit attention the
- *     probabilities enter their product as two numbers of the data's type,
- *     the rounded one and what the rounding left; in the key gradient they
- *     and ds enter as the rounded one alone.
+ *     probabilities and their gradients enter the matrix products as two
+ *     numbers of the data's type, the rounded one and what the rounding
+ *     left; an infinity in v, k, q or d_o may therefore come out as NaN.
  *   - A tensor is an nsgcqt_view: a device pointer and the strides, in
  *     elements, of its batch, row (token) and head axes; the last axis is
  *     contiguous. Pointers are aligned to their element. 16-byte aligned

@@ -616,21 +616,34 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const f4 l = *reinterpret_cast<const f4*>(lse + r0 + 8 * q + 4 * h);
-        const f4 e = *reinterpret_cast<const f4*>(delta + r0 + 8 * q + 4 * h);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = 4 * q + j;
-            s[r] = exp2_(fmaf(s[r], c, -l[j]));
-            dp[r] = s[r] * (dp[r] - e[j]);
-        }
+        for (int j = 0; j < 4; ++j) s[4 * q + j] = exp2_(fmaf(s[4 * q + j], c, -l[j]));
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        const frag<T> p = narrow<T>(s, x), ds = narrow<T>(dp, x);
+        const frag<T> p = narrow<T>(s, x), low = rest_of<T>(s, x, p);
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d) {
-            dv[d] = mma(read_turned<T, RB>(gt, r0 + 16 * x, 32 * d, lane), p, dv[d]);
-            dk[d] = mma(read_turned<T, RB>(qt, r0 + 16 * x, 32 * d, lane), ds, dk[d]);
+            const frag<T> g = read_turned<T, RB>(gt, r0 + 16 * x, 32 * d, lane);
+            dv[d] = mma(g, p, dv[d]);
+            if constexpr (sizeof(T) == 2) dv[d] = mma(g, low, dv[d]);
+        }
+    }
+    if (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);   // p's fragments are gone before ds' are made: registers
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f4 e = *reinterpret_cast<const f4*>(delta + r0 + 8 * q + 4 * h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dp[4 * q + j] = s[4 * q + j] * (dp[4 * q + j] - e[j]);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const frag<T> ds = narrow<T>(dp, x), low = rest_of<T>(dp, x, ds);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            const frag<T> q = read_turned<T, RB>(qt, r0 + 16 * x, 32 * d, lane);
+            dk[d] = mma(q, ds, dk[d]);
+            if constexpr (sizeof(T) == 2) dk[d] = mma(q, low, dk[d]);
         }
     }
 }
@@ -638,12 +651,15 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 // dk, dv of 128 keys (a wave has 32) over the queries near them, for all heads
 // of their kv head: no atomics and no partial sums but the sinks'. Scores and
 // dp are formed the other way round than in dq (a lane has one key), so p and
-// ds are B fragments again. p and ds are rounded to the data's type.
+// ds are B fragments again. In 16 bits each goes into its product as two
+// numbers: with one, dk and dv are off by 0.0026 and 0.0023 in the 2-norm in
+// bfloat16, with two by their own rounding, 0.0016.
 // 446,932 tokens, 8 heads of 64 over 2, window 256, bfloat16: 800 us (dq 980,
 // far queries 180): 2.3 ms with the forward, 324 TFLOP/s of the formulas' work.
 // Bound by waiting: three waves a SIMD, half their cycles.
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 2 && WIDE ? 3 : 2) void k_attention_dkv(AttnArgs a) {
+__global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 2 && WIDE && (DP == 32 || std::is_same<T, __bf16>::value) ? 3 : 2)
+void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = query_tile<T, DP>();
     typedef Loader<T, DP, BQ, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];

@@ -718,3 +718,22 @@ def test_thousands_of_bands(bands, batch):
     close(o, ref[0], attention_bound(torch.float32), "o")
     for got, r, name, size in zip(torch.autograd.grad(o, [q, k, v], do), ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
         close(got, r, attention_bound(torch.float32, True), name, size)
+
+
+# As ATTENTION_EPS, with the differences of 32-bit sums that ds is formed of.
+GRADIENT_EPS = {torch.bfloat16: 2.0 ** -16, torch.float16: 2.0 ** -18}
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("d,left,right,sinks,h,hk", [(64, 255, 0, 4, 4, 2), (128, 100, 0, 0, 2, 1), (24, 80, 30, 2, 4, 4),
+                                                     (61, 120, 0, 40, 2, 1)])
+def test_key_gradients_round_once(d, left, right, sinks, h, hk, dtype):
+    """The rounding of p and ds does not reach dk and dv: they round once, at the end (far queries of the sinks too)."""
+    lengths = [1500, 45]
+    q, k, v, do = (randn(i, 1, sum(lengths), n, d, dtype=dtype).requires_grad_(i < 4)
+                   for i, n in ((1, h), (2, hk), (3, hk), (4, h)))
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, right, sinks)
+    dk, dv = torch.autograd.grad(o, [k, v], do)
+    ref = attention_reference(q, k, v, lengths, 0, left, right, sinks, d ** -0.5, None, do)
+    beyond_rounding(dk, ref[2], GRADIENT_EPS[dtype], "dk")
+    beyond_rounding(dv, ref[3], GRADIENT_EPS[dtype], "dv")
