@@ -428,6 +428,51 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) 
 
 // --------------------------------------------------------------- gradients
 
+// Float16's range in a product summed over blocks: a lane's 16 values x of a
+// block belong to one column of the sums (with those of the lane 32 away), and
+// are multiplied by a power of two of the column's that brings the largest of
+// a block to 2^-1 .. 2^15: probabilities' gradients pass 65,504 under a scaled
+// loss, and lie below 2^-24 under a small one, where dq, dk and dv are float16
+// numbers. When the power changes the sums, in 32 bits, change with it; they
+// grow by 2^48 at most. In the other types there is nothing to do. (446,932
+// tokens, 8 heads of 64 over 2, window 256, forward and gradients: 3524 us in
+// float16, 2687 in bfloat16: the powers' registers leave two waves a SIMD.)
+template <class T> struct InRange {
+    static constexpr bool kHalf = std::is_same<T, _Float16>::value;
+    static constexpr float kGrow = 0x1p48f;
+    float by = 0.f, least = INFINITY;   // the column's power (0: none yet), and the smallest yet
+
+    template <int N> __device__ void take(acc16& x, acc16 (&sums)[N]) {
+        if constexpr (kHalf) {
+            float mx = fabsf(x[0]);
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fabsf(x[r]));
+            mx = half_max(mx);
+            const float at = mx * by;
+            if (__any(at > 0x1p15f || (at < 0.5f && mx > 0.f && by < least * kGrow))) {
+                float to = by > 0.f ? by : 1.f;
+                if (mx > 0.f && mx < INFINITY)
+                    to = fminf(fminf(ldexpf(1.f, 14 - __builtin_amdgcn_frexp_expf(mx)), 0x1p100f), least * kGrow);
+                const float change = by > 0.f ? to / by : 1.f;
+#pragma unroll
+                for (int d = 0; d < N; ++d) sums[d] *= change;
+                by = to;
+                if (mx > 0.f) least = fminf(least, to);
+            }
+            x *= by;
+        }
+    }
+    // what takes the sums back
+    __device__ float undo() const { return kHalf && by > 0.f ? 1.f / by : 1.f; }
+};
+
+// Waves a SIMD of dq and the key gradient, by what their registers allow:
+// `large` at heads above 64.
+template <class T, int DP, bool WIDE> constexpr int grad_waves(int large) {
+    if (DP > 64) return large;
+    return sizeof(T) == 2 && WIDE && (DP <= 32 || !InRange<T>::kHalf) ? 3 : 2;
+}
+
 // dq, and delta = do . o for the key gradient. In 16 bits ds goes into its
 // product as two numbers, the rounded one and what the rounding left: with one
 // alone dq is off by 0.0025 in the 2-norm (bfloat16; 0.0017 is its own
@@ -443,7 +488,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) 
 // fragment of dq^T = K^T ds^T.
 constexpr int kFewKeys = 16;
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 || !WIDE ? 2 : 3) void k_attention_dq(AttnArgs a) {
+__global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(sizeof(T) == 4 ? 1 : 2))) void k_attention_dq(AttnArgs a) {
     constexpr int BN = key_tile<T, DP>(), RB = row_bytes<T, DP>();
     typedef Loader<T, DP, BN, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
@@ -483,6 +528,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
     }
     delta = half_sum(delta);
     float rest = 0.f;   // the sum of this row's ds: 0 but for delta's error
+    InRange<T> range_ds;
     const float lse = mine ? a.stats[at + i] : INFINITY;
 
     const T* kp = row_of<T>(a.k, b, t.start, kv);
@@ -550,6 +596,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
                         rest += s[r];
                     }
                     if (pass == 0) continue;
+                    range_ds.take(s, g);
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const frag<T> ds = narrow<T>(s, x), low = rest_of<T>(s, x, ds);
@@ -574,7 +621,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? (DP > 64 ? 1 : 2) : DP > 64 |
     T* out = mine ? row_of<T>(a.dq, b, t.start + i, head) : nullptr;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-        g[d] *= a.scale;
+        g[d] *= a.scale * range_ds.undo();
         store_column<T>(out, g[d], 32 * d, a.dim, WIDE, lane);
     }
 }
@@ -601,7 +648,8 @@ __device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t 
 template <class T, int DP>
 __device__ inline void key_grad(const char* qt, const char* gt, const float* lse, const float* delta, int r0,
                                 const frag<T> (&kf)[DP / 16], const char* vt, acc16 (&dk)[DP / 32],
-                                acc16 (&dv)[DP / 32], float c, bool edge, int lo, unsigned span, int lane) {
+                                acc16 (&dv)[DP / 32], InRange<T>& range_ds, InRange<T>& range_p, float c, bool edge,
+                                int lo, unsigned span, int lane) {
     constexpr int RB = row_bytes<T, DP>();
     const int h = lane >> 5;
     acc16 s = scores<T, DP>(qt, r0, kf, nullptr, lane), dp = rows_product<T, DP>(gt, r0, vt, 0, lane);
@@ -619,9 +667,11 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[4 * q + j] = exp2_(fmaf(s[4 * q + j], c, -l[j]));
     }
+    acc16 pr = s;
+    range_p.take(pr, dv);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        const frag<T> p = narrow<T>(s, x), low = rest_of<T>(s, x, p);
+        const frag<T> p = narrow<T>(pr, x), low = rest_of<T>(pr, x, p);
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d) {
             const frag<T> g = read_turned<T, RB>(gt, r0 + 16 * x, 32 * d, lane);
@@ -636,6 +686,7 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 #pragma unroll
         for (int j = 0; j < 4; ++j) dp[4 * q + j] = s[4 * q + j] * (dp[4 * q + j] - e[j]);
     }
+    range_ds.take(dp, dk);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const frag<T> ds = narrow<T>(dp, x), low = rest_of<T>(dp, x, ds);
@@ -658,8 +709,7 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
 // far queries 180): 2.3 ms with the forward, 324 TFLOP/s of the formulas' work.
 // Bound by waiting: three waves a SIMD, half their cycles.
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(256, DP > 64 ? 1 : sizeof(T) == 2 && WIDE && (DP == 32 || std::is_same<T, __bf16>::value) ? 3 : 2)
-void k_attention_dkv(AttnArgs a) {
+__global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(1))) void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = query_tile<T, DP>();
     typedef Loader<T, DP, BQ, WIDE> Ld;
     __shared__ __align__(1024) char lds[2][2][Ld::kBytes];
@@ -691,6 +741,7 @@ void k_attention_dkv(AttnArgs a) {
     acc16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
+    InRange<T> range_ds, range_p;
 
     const int i_begin = k0 > a.right ? k0 - a.right : 0;
     const int i_end = min(k0 + kKeys + a.left, len);
@@ -740,10 +791,17 @@ void k_attention_dkv(AttnArgs a) {
                 if (!skip) {
                     const bool edge = j_hi > i_lo + a.right || (j_lo < i_hi - a.left && j_hi >= a.sinks);
                     key_grad<T, DP>(lds[u][0], lds[u][1], row_lse[u], row_delta[u], 32 * qb, kf, values[wave], dk, dv,
-                                    a.by.c, edge, j - a.right - i_lo, span, lane);
+                                    range_ds, range_p, a.by.c, edge, j - a.right - i_lo, span, lane);
                 }
             }
             tile_barrier();
+        }
+    }
+    if constexpr (InRange<T>::kHalf) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            dk[d] *= range_ds.undo();
+            dv[d] *= range_p.undo();
         }
     }
     // the far queries' share of the sinks
@@ -817,6 +875,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     acc16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zero16();
+    InRange<T> range_ds, range_p;
 
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
     const Ld ld(a.q.row, a.d_o.row, a.dim, wave, lane);
@@ -840,8 +899,15 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
         if (n + 1 < total) fetch(n + 1);
         if (32 * wave < BQ && i_begin + n % q_tiles * BQ + 32 * wave < i_end)
             key_grad<T, DP>(lds[n & 1], lds[n & 1] + Ld::kBytes, row_lse[n & 1], row_delta[n & 1], 32 * wave, kf,
-                            values, dk, dv, a.by.c, false, 0, 0, lane);
+                            values, dk, dv, range_ds, range_p, a.by.c, false, 0, 0, lane);
         tile_barrier();
+    }
+    if constexpr (InRange<T>::kHalf) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            dk[d] *= range_ds.undo();
+            dv[d] *= range_p.undo();
+        }
     }
     float(*joined)[DP][33] = reinterpret_cast<float(*)[DP][33]>(&lds[0][0]);
     for (int v = 0; v < 4; ++v) {

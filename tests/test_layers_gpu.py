@@ -737,3 +737,48 @@ def test_key_gradients_round_once(d, left, right, sinks, h, hk, dtype):
     ref = attention_reference(q, k, v, lengths, 0, left, right, sinks, d ** -0.5, None, do)
     beyond_rounding(dk, ref[2], GRADIENT_EPS[dtype], "dk")
     beyond_rounding(dv, ref[3], GRADIENT_EPS[dtype], "dv")
+
+
+@pytest.mark.parametrize("d", [16, 64, 128, 41])
+def test_float16_gradients_of_large_loss(d):
+    """A scaled loss: p (do . v - do . o) passes 65,504 while dq, dk, dv are float16 numbers."""
+    lengths, dtype, left, sinks = [300, 40], torch.float16, 1, 1
+    # do . v has a standard deviation of 163,840
+    q, k, v, do = (randn(i, 1, 340, n, d, dtype=dtype, by=by).requires_grad_(i < 4)
+                   for i, n, by in ((1, 4, 0.02), (2, 2, 0.02), (3, 2, 160.0 / d ** 0.5), (4, 4, 1024.0)))
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, 0, sinks)
+    grads = torch.autograd.grad(o, [q, k, v], do)
+    ref = attention_reference(q, k, v, lengths, 0, left, 0, sinks, d ** -0.5, None, do)
+    for got, r, name, size in zip(grads, ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+        assert r.abs().max() < 60000
+        close(got, r, attention_bound(dtype, True), name, size)
+
+
+@pytest.mark.parametrize("left", [255, None])
+@pytest.mark.parametrize("name,q_by,k_by", [("dq", 2.0 ** -8, 2.0 ** 8), ("dk", 2.0 ** 8, 2.0 ** -8)])
+def test_float16_gradients_of_small_loss(name, q_by, k_by, left):
+    """do near 2^-16: p (do . v - do . o) lies below float16's normal numbers, dq (or dk) does not."""
+    n, d, dtype = 600, 64, torch.float16
+    q, k, v, do = (randn(i, 1, n, m, d, dtype=dtype, by=by).requires_grad_(i < 4)
+                   for i, m, by in ((1, 2, q_by), (2, 1, k_by), (3, 1, 1.0), (4, 2, 2.0 ** -14)))
+    o = layers.band_attention(q, k, v, offsets_of([n]), left)
+    got = torch.autograd.grad(o, [q, k, v], do)
+    ref = attention_reference(q, k, v, [n], 0, left, 0, 0, d ** -0.5, None, do)
+    at = {"dq": 0, "dk": 1}[name]
+    assert ref[1 + at].pow(2).mean().sqrt() > 2.0 ** -13
+    # single values below 2^-14 are multiples of 2^-24: their rounding is at most 2^-25
+    noise = torch.full_like(ref[1 + at], 2.0 ** -3)   # times 2^-22
+    close(got[at], ref[1 + at], attention_bound(dtype, True), name, noise)
+
+
+def test_float16_value_gradient_of_unlikely_keys():
+    """Keys whose probabilities lie near 2^-26, under gradients of 2^10: their dv is a normal float16 number."""
+    n, d, dtype = 256, 32, torch.float16
+    q, k, v, do = (randn(i, 1, n, 1, d, dtype=dtype, by=by) for i, by in ((1, 0.3), (2, 0.3), (3, 1.0), (4, 1024.0)))
+    q[..., 0], k[:, 1::2, :, 0] = 4.0, -16.0
+    q, k, v = q.requires_grad_(), k.requires_grad_(), v.requires_grad_()
+    o = layers.band_attention(q, k, v, offsets_of([n]), None, None)
+    (dv,) = torch.autograd.grad(o, [v], do)
+    want = attention_reference(q, k, v, [n], 0, None, None, 0, d ** -0.5, None, do)[3][:, 1::2]
+    assert want.pow(2).mean().sqrt() > 2.0 ** -13
+    close(dv[:, 1::2], want, attention_bound(dtype, True), "dv", torch.full_like(want, 2.0 ** -3))
