@@ -122,8 +122,11 @@ template <class T, int DP, int BN, bool WIDE> struct Loader {
     static constexpr int kRB = row_bytes<T, DP>(), kBytes = BN * kRB;
     static constexpr int kEach = kBytes / 4096;          // wide: loads of a thread for each tensor
     static constexpr int kChunks = BN * DP / 8;          // else: chunks of 8 values of a tile
-    static constexpr unsigned kPast = 0x80000000u;       // past every tile
-    unsigned ox[kEach], oy[kEach];                       // wide: this lane's offsets in bytes
+    static constexpr unsigned kPast = 0x80000000u;       // past every tile, and less than 2^30 from its end
+    // Wide: this lane's offsets in bytes. In rows of 128 bytes a wave's loads
+    // are 8 rows apart, where the chunks' order repeats: one offset serves all.
+    static constexpr int kOffsets = kRB == 128 ? 1 : kEach;
+    unsigned ox[kOffsets], oy[kOffsets];
     int64_t sx, sy;
     int dim;
 
@@ -133,12 +136,16 @@ template <class T, int DP, int BN, bool WIDE> struct Loader {
     __device__ Loader(int64_t stride_x, int64_t stride_y, int width, int wave, int lane)
         : sx(stride_x), sy(stride_y), dim(width) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
+        for (int e = 0; e < kOffsets; ++e) {
             const int r = row(e, wave, lane), slot = lane % (kRB / 16 < 64 ? kRB / 16 : 64);
             const unsigned d = (slot ^ turn(r)) * (16 / sizeof(T));
             ox[e] = d < static_cast<unsigned>(dim) ? (r * static_cast<unsigned>(sx) + d) * sizeof(T) : kPast;
             oy[e] = d < static_cast<unsigned>(dim) ? (r * static_cast<unsigned>(sy) + d) * sizeof(T) : kPast;
         }
+    }
+
+    static __device__ unsigned offset(const unsigned (&o)[kOffsets], int e, int64_t stride) {
+        return kOffsets > 1 ? o[e] : o[0] + e * 8 * static_cast<unsigned>(stride) * static_cast<unsigned>(sizeof(T));
     }
 
     // rows row0 .. of px, py (below row_end) into tx, ty; kept: for each load
@@ -158,7 +165,8 @@ template <class T, int DP, int BN, bool WIDE> struct Loader {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 const int at = (wave * kEach + e) * 1024;
-                const unsigned x = keep && !kept[e] ? kPast : ox[e], y = keep && !kept[e] ? kPast : oy[e];
+                const bool drop = keep && !kept[e];
+                const unsigned x = drop ? kPast : offset(ox, e, sx), y = drop ? kPast : offset(oy, e, sy);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(tx + at), 16, x, 0, 0, 0);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_void*)(ty + at), 16, y, 0, 0, 0);
             }
@@ -478,15 +486,17 @@ template <class T, int DP, bool WIDE> constexpr int grad_waves(int large) {
 // alone dq is off by 0.0025 in the 2-norm (bfloat16; 0.0017 is its own
 // rounding). delta comes from the rounded o; a row of ds sums to zero with the
 // exact one, so the sum that is found is delta's error, and the key gradient
-// gets the corrected value. Where queries see few keys, dp - delta is small
-// beside delta, whose error then shows in dq (two keys, bfloat16: 0.0034 in the
-// 2-norm): with at most kFewKeys a first pass over them, without the product
-// with K, finds that sum and corrects delta beforehand (0.0017, all of it dq's
-// own rounding; 446,932 tokens, window of 2, forward and gradients: 1157 us
-// instead of 1088). With 17 keys dq is at 0.0019 without it. Layout as
-// k_attention: the scores and dp are formed transposed, so ds is the B
-// fragment of dq^T = K^T ds^T.
-constexpr int kFewKeys = 16;
+// gets the corrected value. Where few keys have a weight (few are seen, or one
+// outweighs the others), dp - delta is small beside delta, whose error then
+// shows in dq (two keys, bfloat16: 0.0034 in the 2-norm). So a workgroup in
+// which that sum passes a quarter of u of the row's sum of |ds| anywhere goes
+// through its keys once more with the corrected delta (0.0017). With random
+// scores that happens below some 30 keys and at a band's first tokens:
+// 446,932 tokens, forward and gradients, window of 2, everywhere: 1388 us;
+// window of 256, hardly anywhere: 4 % of the whole, for the sums of |ds|.
+// Layout as k_attention: the scores and dp are formed transposed, so ds is the
+// B fragment of dq^T = K^T ds^T.
+template <class T> constexpr float kRest = std::is_same<T, _Float16>::value ? 0x1p-13f : 0x1p-10f;
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(sizeof(T) == 4 ? 1 : 2))) void k_attention_dq(AttnArgs a) {
     constexpr int BN = key_tile<T, DP>(), RB = row_bytes<T, DP>();
@@ -559,11 +569,10 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(sizeof(T) == 4 ? 1 : 
         ld.load(lds[u][0], lds[u][1], kp, vp, j0, j_end, keep, kept, tid);
         if (tid < BN) bias[u][tid] = next_bias;
     };
-    const int64_t seen = static_cast<int64_t>(a.left) + a.right + 1 + a.sinks;   // by a query, at most
-    const bool few = sizeof(T) == 2 && min(seen, static_cast<int64_t>(len)) <= kFewKeys;
+    float size = 0.f;   // the sum of |ds|
 #pragma unroll 1
-    for (int pass = few ? 0 : 1; pass < 2; ++pass) {
-        const bool load = pass == 0 || !few || range.tiles > 2;   // else both tiles are still in LDS
+    for (int pass = 0; pass < 2; ++pass) {
+        const bool load = pass == 0 || range.tiles > 2;   // else both tiles are still in LDS
         if (load) {
             fetch_masks(0);
             fetch(0, 0);
@@ -594,8 +603,8 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(sizeof(T) == 4 ? 1 : 
                     for (int r = 0; r < 16; ++r) {
                         s[r] = exp2_(fmaf(s[r], a.by.c, -lse)) * (dp[r] - delta);
                         rest += s[r];
+                        if (sizeof(T) == 2) size += fabsf(s[r]);
                     }
-                    if (pass == 0) continue;
                     range_ds.take(s, g);
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
@@ -612,10 +621,13 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(sizeof(T) == 4 ? 1 : 
             }
         }
         rest = half_sum(rest);
-        if (pass == 0) {
-            delta += rest;
-            rest = 0.f;
-        }
+        if (sizeof(T) == 4 || pass == 1) break;
+        if (!__syncthreads_or(fabsf(rest) > kRest<T> * half_sum(size))) break;
+        delta += rest;
+        rest = 0.f;
+        range_ds = InRange<T>();
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) g[d] = zero16();
     }
     if (mine && h == 0) a.delta[at + i] = delta + rest;
     T* out = mine ? row_of<T>(a.dq, b, t.start + i, head) : nullptr;

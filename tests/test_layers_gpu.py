@@ -782,3 +782,27 @@ def test_float16_value_gradient_of_unlikely_keys():
     want = attention_reference(q, k, v, [n], 0, None, None, 0, d ** -0.5, None, do)[3][:, 1::2]
     assert want.pow(2).mean().sqrt() > 2.0 ** -13
     close(dv[:, 1::2], want, attention_bound(dtype, True), "dv", torch.full_like(want, 2.0 ** -3))
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("case", ["sparse", "peaked", "first", "sinks"])
+def test_query_gradient_where_few_keys_weigh(case, dtype):
+    """Wide windows in which few keys have a weight: few are kept, one outweighs the others, or the band has just
+    begun. What the error of do . o (from the rounded o) may leave in a row of ds is a quarter of u; with dq's own
+    rounding, u / sqrt(3) at most, that is u sqrt(1/3 + 1/16), and 32-bit sums."""
+    lengths, d, left, sinks, by, keep = [900, 70], 64, 255, 0, 1.0, None
+    if case == "sparse":
+        keep = (torch.arange(970) % 100 < 2)[None].cuda()
+    elif case == "peaked":
+        by = 5.0
+    elif case == "first":
+        lengths = [20] * 30 + [17, 33, 2]
+    else:
+        left, sinks, by = 0, 17, 3.0
+    q, k, v, do = (randn(i, 1, sum(lengths), n, d, dtype=dtype, by=b).requires_grad_(i < 4)
+                   for i, n, b in ((1, 4, by), (2, 2, 1.0), (3, 2, 1.0), (4, 4, 1.0)))
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, 0, sinks, keep=keep)
+    (dq,) = torch.autograd.grad(o, [q], do)
+    want = attention_reference(q, k, v, lengths, 0, left, 0, sinks, d ** -0.5, keep, do)[1]
+    err = ((dq.double().cpu() - want).norm() / want.norm()).item()
+    assert err <= U[dtype] * (1 / 3 + 1 / 16) ** 0.5 + 64 * 2.0 ** -24, err
