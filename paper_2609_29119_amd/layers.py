@@ -25,6 +25,7 @@ import functools
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from .nsgcqt import EINVAL, NsgcqtError, _check, lib
 
@@ -144,11 +145,22 @@ def _view_step(t):
 
 
 def _trains(*tensors):
+    """Whether a result has to carry a derivative: an input requires grad, or
+    has a forward-mode tangent (which no operator here has a rule for: the
+    autograd functions then raise NotImplementedError)."""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
                 return True
+    if _dual_level() >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                return True
     return False
+
+
+def _dual_level():
+    return getattr(forward_ad, "_current_level", 0)   # -1: no forward-mode level is open
 
 
 def _last(t):

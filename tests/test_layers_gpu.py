@@ -806,3 +806,22 @@ def test_query_gradient_where_few_keys_weigh(case, dtype):
     want = attention_reference(q, k, v, lengths, 0, left, 0, sinks, d ** -0.5, keep, do)[1]
     err = ((dq.double().cpu() - want).norm() / want.norm()).item()
     assert err <= U[dtype] * (1 / 3 + 1 / 16) ** 0.5 + 64 * 2.0 ** -24, err
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_forward_mode_is_refused(grad):
+    """No operator has a forward-mode rule: a tangent raises instead of vanishing."""
+    off = offsets_of([5, 3])
+    x, w, q = randn(0, 1, 8, 4), randn(1, 2, 3, 4), randn(2, 1, 8, 2, 16)
+    pos, freqs = torch.zeros(1, 8, dtype=torch.float64, device="cuda"), layers.rotary_frequencies([8])
+    cache = layers.StreamCache(8, 2, 16, 4, dtype=torch.float32)
+    with torch.set_grad_enabled(grad), torch.autograd.forward_ad.dual_level():
+        def dual(t):
+            return torch.autograd.forward_ad.make_dual(t, torch.ones_like(t))
+        for call in (lambda: layers.band_linear(dual(x), w, off), lambda: layers.band_linear(x, dual(w), off),
+                     lambda: layers.rotary(dual(q), q, pos, freqs, [8]),
+                     lambda: layers.band_attention(q, q, dual(q), off, 3)):
+            with pytest.raises(NotImplementedError):
+                call()
+        with pytest.raises(ValueError):
+            cache.step(dual(q)[0], q[0], q[0])
