@@ -341,7 +341,8 @@ def rotary(q, k, positions, freqs, sections, interleaved=False):
     float32 [sum(sections)], sections: the number of pairs of each of the 1
     to 4 axes. Pairs are values (p, p + P), P = sum(sections), or (2p, 2p + 1)
     with interleaved=True; values past 2 P are copied. Angles are formed in
-    64 bits. Gradients for q and k. Returns (q, k), or q alone if k is None.
+    64 bits. Gradients for q and k; positions and freqs have none and are
+    refused where they would need one. Returns (q, k), or q alone if k is None.
     """
     _tensor(q, "q")
     if q.dim() != 4:
@@ -360,6 +361,8 @@ def rotary(q, k, positions, freqs, sections, interleaved=False):
         raise ValueError("positions has to be [axes][rows] or [axes][batch][rows], its rows contiguous")
     if freqs.dtype != torch.float32 or freqs.device != q.device or freqs.shape != (pairs,) or not freqs.is_contiguous():
         raise ValueError(f"freqs has to be a float32 vector of {pairs} values on the device of q")
+    if _trains(positions, freqs):
+        raise ValueError("rotary has no gradient for positions and freqs: detach them")
     call = _Rotary.apply if _trains(q, k) else _rotary_forward
     out = call(q, k, positions, freqs, sec, interleaved)
     return out[0] if k is None else out

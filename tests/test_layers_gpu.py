@@ -825,3 +825,16 @@ def test_forward_mode_is_refused(grad):
                 call()
         with pytest.raises(ValueError):
             cache.step(dual(q)[0], q[0], q[0])
+
+
+def test_rotary_refuses_gradients_of_angles():
+    """positions and freqs get no gradient: asking for one raises, without one (or without grad mode) they are data."""
+    q = randn(0, 1, 8, 2, 16)
+    pos, freqs = torch.zeros(1, 8, dtype=torch.float64, device="cuda"), layers.rotary_frequencies([8])
+    want = layers.rotary(q, None, pos, freqs, [8])
+    for p, f in ((pos.clone().requires_grad_(), freqs), (pos, freqs.clone().requires_grad_())):
+        for x in (q, q.clone().requires_grad_()):
+            with pytest.raises(ValueError):
+                layers.rotary(x, None, p, f, [8])
+        with torch.no_grad():
+            assert torch.equal(layers.rotary(q, None, p, f, [8]), want)
