@@ -163,6 +163,12 @@ def _dual_level():
     return getattr(forward_ad, "_current_level", 0)   # -1: no forward-mode level is open
 
 
+def _written(*tensors):
+    """Tells autograd that a kernel wrote to these: a graph that saved one
+    then refuses to run backward with the new values."""
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _last(t):
     """t with a contiguous last axis (a gradient may come in any layout)."""
     return t if t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
@@ -480,7 +486,7 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
     slots = _caches(k_cache, v_cache, q, streams, kv_heads, dim)
     if pos.dtype != torch.int64 or pos.device != q.device or pos.shape != (streams,) or not pos.is_contiguous():
         raise ValueError("pos has to be int64 [streams] on the device of q")
-    if _trains(q, k, v):
+    if _trains(q, k, v, k_cache, v_cache, out):
         raise ValueError("attention_step has no gradient: call it under torch.no_grad()")
     o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else _tensor(out, "out", q, q.shape)
     sinks = int(sinks)
@@ -491,6 +497,7 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
             _DTYPES[q.dtype], streams, heads, kv_heads, dim, slots - sinks, sinks,
             dim ** -0.5 if scale is None else float(scale), _view_step(q), _view_step(k), _view_step(v), _view_step(o),
             k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(), ws.data_ptr() if n else None, n, _stream(q)))
+    _written(k_cache, v_cache, *(() if out is None else (out,)))
     return o
 
 
@@ -499,7 +506,8 @@ def cache_fill(k, v, offsets, k_cache, v_cache, sinks=0):
 
     k and v [batch][rows][kv_heads][D]; the caches are those of
     `attention_step`. Afterwards a stream's next token is number
-    offsets[g + 1] - offsets[g]. Slots without a token are left alone.
+    offsets[g + 1] - offsets[g]. Slots without a token are left alone. Not
+    differentiable.
     """
     _tensor(k, "k")
     if k.dim() != 4:
@@ -508,10 +516,13 @@ def cache_fill(k, v, offsets, k_cache, v_cache, sinks=0):
     _tensor(v, "v", k, k.shape)
     _offsets(offsets, k)
     slots = _caches(k_cache, v_cache, k, batch * (offsets.numel() - 1), kv_heads, dim)
+    if _trains(k, v, k_cache, v_cache):
+        raise ValueError("cache_fill has no gradient: call it under torch.no_grad()")
     with _on(k):
         _check(_lib().nsgcqt_cache_fill(
             _DTYPES[k.dtype], _ragged(offsets, batch, rows), kv_heads, dim, slots - int(sinks), int(sinks),
             _view4(k), _view4(v), k_cache.data_ptr(), v_cache.data_ptr(), _stream(k)))
+    _written(k_cache, v_cache)
 
 
 class StreamCache:

@@ -838,3 +838,36 @@ def test_rotary_refuses_gradients_of_angles():
                 layers.rotary(x, None, p, f, [8])
         with torch.no_grad():
             assert torch.equal(layers.rotary(q, None, p, f, [8]), want)
+
+
+def test_writes_to_caches_are_seen_by_autograd():
+    """The kernels' writes count as in-place changes: a graph that saved a cache (or `out`) refuses its backward pass,
+    and tensors that require grad are refused."""
+    n, h, d = 2, 2, 16
+    q, off = randn(0, n, h, d), offsets_of([3, 1])
+    k = randn(1, 1, 4, h, d)
+    pos = torch.zeros(n, dtype=torch.int64, device="cuda")
+    for write in (lambda c, o: layers.attention_step(q, q, q, c, c.clone(), pos, out=o),
+                  lambda c, o: layers.attention_step(q, q, q, c.clone(), c, pos, out=o),
+                  lambda c, o: layers.cache_fill(k, k, off, c, c.clone()),
+                  lambda c, o: layers.cache_fill(k, k, off, c.clone(), c)):
+        x, cache, out = randn(2, n, h, 5, d).requires_grad_(), randn(3, n, h, 5, d), randn(4, n, h, d)
+        loss = (x * cache).sum()
+        with torch.no_grad():
+            write(cache, out)
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+        with pytest.raises(ValueError):
+            write(randn(5, n, h, 5, d).requires_grad_(), out)
+    x, out = randn(6, n, h, d).requires_grad_(), randn(7, n, h, d)
+    loss = (x * out).sum()
+    layers.attention_step(q, q, q, randn(8, n, h, 5, d), randn(9, n, h, 5, d), pos, out=out)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    with pytest.raises(ValueError):
+        layers.attention_step(q, q, q, randn(8, n, h, 5, d), randn(9, n, h, 5, d), pos, out=out.requires_grad_())
+    with pytest.raises(ValueError):
+        layers.cache_fill(k.clone().requires_grad_(), k, off, randn(8, n, h, 5, d), randn(9, n, h, 5, d))
+    with torch.inference_mode():
+        cache = layers.StreamCache(n, h, d, 4, dtype=torch.float32)
+        assert torch.isfinite(cache.step(q, q, q)).all()
