@@ -20,7 +20,8 @@ struct RotaryArgs {
 
 // cos and sin of +-position * freq. The product and its reduction to turns
 // are in 64 bits (a 32-bit product of a position near 10^5 is off by 10^-2
-// rad); the reduced angle in 32 bits is exact to 2^-25 of a turn.
+// rad). Sine and cosine are taken of the reduced angle in 32 bits, which is
+// off by up to 2^-26 of a turn; what that rounding left enters to first order.
 __device__ inline void turn_of(const RotaryArgs& a, int64_t at, int p, float& cs, float& sn) {
     const int axis = (p >= a.ends[0]) + (p >= a.ends[1]) + (p >= a.ends[2]);
     const int64_t i = axis * a.pos_axis + at;
@@ -33,7 +34,12 @@ __device__ inline void turn_of(const RotaryArgs& a, int64_t at, int p, float& cs
         x = static_cast<double>(static_cast<const int64_t*>(a.positions)[i]);
     double turns = x * static_cast<double>(a.freqs[p]) * 0.15915494309189535;
     turns -= rint(turns);
-    sincospif(2.f * static_cast<float>(turns), &sn, &cs);
+    const float near = static_cast<float>(turns);
+    const float left = static_cast<float>(turns - static_cast<double>(near)) * 6.2831853f;
+    float s0, c0;
+    sincospif(2.f * near, &s0, &c0);
+    sn = fmaf(c0, left, s0);
+    cs = fmaf(-s0, left, c0);
     if (a.inverse) sn = -sn;
 }
 

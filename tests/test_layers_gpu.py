@@ -871,3 +871,15 @@ def test_writes_to_caches_are_seen_by_autograd():
     with torch.inference_mode():
         cache = layers.StreamCache(n, h, d, 4, dtype=torch.float32)
         assert torch.isfinite(cache.step(q, q, q)).all()
+
+
+def test_rotary_angles_near_half_turns():
+    """Positions near odd multiples of pi: the sine is small and the reduced angle is not, so the angle's 32-bit
+    rounding (2^-26 of a turn) must not reach it. Sine, its correction and the result: 16 units of 2^-24 in all."""
+    p = [3, 22, 44, 333, 355, 710]
+    pos = torch.tensor([p], dtype=torch.int64, device="cuda")
+    q = torch.zeros(1, len(p), 1, 2, device="cuda")
+    q[..., 0] = 1.0
+    got = layers.rotary(q, None, pos, torch.ones(1, device="cuda"), [1])[0, :, 0].double().cpu()
+    want = torch.tensor([[np.cos(float(x)), np.sin(float(x))] for x in p], dtype=torch.float64)
+    assert ((got - want).abs() <= 2.0 ** -20 * want.abs()).all(), (got - want) / want
