@@ -1,4 +1,6 @@
 // C entries of the per-band products.
+#include <algorithm>
+
 #include "checks.hpp"
 #include "linear.hpp"
 
@@ -150,12 +152,11 @@ int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt
     const int64_t blocks = tile_count(a.chunk_shift, a.n_bands, a.batch, a.rows) * ot * it;
     const int64_t join = (n_in * n_out + n_out + 255) / 256;
     CHECK_TRY(check_grid(blocks));
-    if (r->n_bands > 65535) return set_err(NSGCQT_EUNSUPPORTED, "more than 65,535 bands in a gradient of weights");
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
         LAUNCH_TRY(k_linear_dw<T>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
-        LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64), static_cast<unsigned>(a.n_bands)),
+        LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64), static_cast<unsigned>(std::min(a.n_bands, 65535))),
                    dim3(256), 0, st, a);
         return NSGCQT_OK;
     });

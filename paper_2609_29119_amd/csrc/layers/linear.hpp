@@ -402,21 +402,22 @@ __global__ __launch_bounds__(256, 2) void k_linear_dw(LinearArgs a) {
 // Adds the partial sums of bands of several chunks, and writes zeros for empty bands.
 template <class T>
 __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
-    const int band = blockIdx.y;
-    const int64_t b0 = band_bound(a.off, a.n_bands, a.rows, band + 1), b1 = band_bound(a.off, a.n_bands, a.rows, band + 2);
-    const int64_t n_rows = b1 > b0 ? (b1 - b0) * a.batch : 0;
-    if (n_rows > 0 && n_rows <= (int64_t(1) << a.chunk_shift)) return;
     const int64_t n_w = static_cast<int64_t>(a.n_out) * a.n_in, n = n_w + (a.db ? a.n_out : 0);
-    const int64_t chunks = (n_rows + (int64_t(1) << a.chunk_shift) - 1) >> a.chunk_shift;
-    const int64_t item = ((b0 * a.batch) >> a.chunk_shift) + band + 1;
-    for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
-        float s = 0.f;
+    for (int band = blockIdx.y; band < a.n_bands; band += gridDim.y) {
+        const int64_t b0 = band_bound(a.off, a.n_bands, a.rows, band + 1), b1 = band_bound(a.off, a.n_bands, a.rows, band + 2);
+        const int64_t n_rows = b1 > b0 ? (b1 - b0) * a.batch : 0;
+        if (n_rows > 0 && n_rows <= (int64_t(1) << a.chunk_shift)) continue;
+        const int64_t chunks = (n_rows + (int64_t(1) << a.chunk_shift) - 1) >> a.chunk_shift;
+        const int64_t item = ((b0 * a.batch) >> a.chunk_shift) + band + 1;
+        for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
+            float s = 0.f;
 #pragma unroll 8
-        for (int64_t c = 0; c < chunks; ++c) s += dw_part(a, item + c)[e];
-        if (e < n_w)
-            static_cast<T*>(a.dw)[band * n_w + e] = static_cast<T>(s);
-        else
-            static_cast<T*>(a.db)[static_cast<int64_t>(band) * a.n_out + e - n_w] = static_cast<T>(s);
+            for (int64_t c = 0; c < chunks; ++c) s += dw_part(a, item + c)[e];
+            if (e < n_w)
+                static_cast<T*>(a.dw)[band * n_w + e] = static_cast<T>(s);
+            else
+                static_cast<T*>(a.db)[static_cast<int64_t>(band) * a.n_out + e - n_w] = static_cast<T>(s);
+        }
     }
 }
 

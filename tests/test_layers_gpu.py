@@ -883,3 +883,19 @@ def test_rotary_angles_near_half_turns():
     got = layers.rotary(q, None, pos, torch.ones(1, device="cuda"), [1])[0, :, 0].double().cpu()
     want = torch.tensor([[np.cos(float(x)), np.sin(float(x))] for x in p], dtype=torch.float64)
     assert ((got - want).abs() <= 2.0 ** -20 * want.abs()).all(), (got - want) / want
+
+
+def test_weights_gradient_of_many_bands():
+    """More bands than a grid's second axis holds: empty ones, one of several chunks and a last one among them."""
+    bands = 70000
+    lengths = np.random.default_rng(0).integers(0, 3, bands)
+    lengths[[5, bands - 1]] = 9000
+    rows, off = int(lengths.sum()), offsets_of(lengths)
+    x, w = randn(1, 1, rows, 2), randn(2, bands, 3, 2).requires_grad_()
+    b, dy = randn(3, bands, 3).requires_grad_(), randn(4, 1, rows, 3)
+    y = layers.band_linear(x, w, off, b)
+    dw, db = torch.autograd.grad(y, [w, b], dy)
+    ry, _, rdw, rdb = linear_reference(x, w, b, lengths, 0, dy)
+    close(y, ry, product_bound(torch.float32, 2), "y")
+    close(dw, rdw, product_bound(torch.float32, 9000), "dw")
+    close(db, rdb, product_bound(torch.float32, 9000), "db")
