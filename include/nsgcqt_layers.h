@@ -40,6 +40,14 @@
  *     nsgcqt_last_error(). EINVAL for null or misaligned pointers, negative
  *     sizes, an unknown type; EUNSUPPORTED for head_dim above 128 and sizes
  *     beyond the stated limits; EWORKSPACE for a workspace below its size.
+ *   - Limits: below 2^30 rows, 2^24 bands, 2^30 signals, 2^40 tokens in all,
+ *     widths of 65,536, 65,536 heads; and 16,777,215 workgroups a launch,
+ *     which comes first for many signals or short bands: with tiles of R
+ *     tokens a signal has rows / R + n_bands + 2 of them (R = 128 for the
+ *     products and the key gradient, which counts in kv heads; 128 / s with
+ *     s = 4, 2 or 1 heads a workgroup, the largest that divides n_heads /
+ *     n_kv_heads, for the attention). The step takes a workgroup for each
+ *     stream, kv head and 32 query heads of it, and one for each stream and head.
  */
 #ifndef NSGCQT_LAYERS_H
 #define NSGCQT_LAYERS_H
@@ -164,7 +172,7 @@ int64_t nsgcqt_attention_step_workspace(int64_t n_streams, int64_t n_heads, int6
 /* Fills ring caches from whole bands: stream b n_bands + g holds the tokens
  * of band g of signal b, numbered from 0; what its cache would hold after
  * steps over all of them is copied, slots without a token are left alone.
- * k, v: [batch][rows][n_kv_heads][head_dim]. */
+ * k, v: [batch][rows][n_kv_heads][head_dim]. At most 65,535 streams a call. */
 int nsgcqt_cache_fill(int dtype, const nsgcqt_rows* r, int64_t n_kv_heads, int64_t head_dim, int64_t window,
                       int64_t sinks, const nsgcqt_view* k, const nsgcqt_view* v, void* k_cache, void* v_cache,
                       void* stream);

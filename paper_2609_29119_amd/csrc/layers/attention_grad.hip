@@ -9,13 +9,20 @@ int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
 int64_t delta_bytes(const AttnArgs& a) { return align256(int64_t(4) * a.rows * a.batch * a.heads); }
 
-int64_t part_bytes(const AttnArgs& a) {
-    return int64_t(4) * tile_count(kFarShift, a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32) * 2 * 32 *
-           a.dim;
+// Workgroups of the far queries: for each chunk, kv head and 32 sinks.
+int64_t far_blocks(const AttnArgs& a) {
+    return product(tile_count(kFarShift, a.n_bands, 1, a.rows), a.batch, a.kv_heads, (a.sinks + 31) / 32);
 }
+
+int64_t part_bytes(const AttnArgs& a) { return product(far_blocks(a), 4 * 2 * 32 * a.dim); }
 
 // Whether some query lies past the window of some sink's key tile.
 bool has_far(const AttnArgs& a) { return a.sinks > 0 && kKeys + a.left < a.rows; }
+
+int64_t grad_bytes(const AttnArgs& a) {
+    const int64_t part = has_far(a) ? workspace_of(part_bytes(a)) : 0;
+    return part < 0 ? part : delta_bytes(a) + part;
+}
 
 }  // namespace
 
@@ -23,7 +30,7 @@ extern "C" int64_t nsgcqt_band_attention_workspace(const nsgcqt_rows* r, const n
     CHECK_TRY(check_rows(r));
     CHECK_TRY(check_shape(s));
     const AttnArgs a = attention_args(r, s);
-    return delta_bytes(a) + (has_far(a) ? part_bytes(a) : 0);
+    return grad_bytes(a);
 }
 
 extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_attention_shape* s,
@@ -48,7 +55,8 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
         CHECK_TRY(check_view(x.v, x.name, dtype, r->batch, r->rows, x.heads, s->head_dim, wide));
     if (r->batch == 0 || r->rows == 0) return NSGCQT_OK;
     if (!stats || misaligned(stats, 4)) return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 4 bytes");
-    const int64_t need = delta_bytes(a) + (has_far(a) ? part_bytes(a) : 0);
+    const int64_t need = grad_bytes(a);
+    if (need < 0) return static_cast<int>(need);
     if (static_cast<int64_t>(ws_bytes) < need)
         return set_err(NSGCQT_EWORKSPACE, "workspace of " + std::to_string(ws_bytes) + " bytes, " +
                                               std::to_string(need) + " required");
@@ -57,11 +65,11 @@ extern "C" int nsgcqt_band_attention_grad(int dtype, const nsgcqt_rows* r, const
     a.stats = const_cast<float*>(stats);
     a.delta = static_cast<float*>(ws);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + delta_bytes(a));
-    const int64_t queries = query_blocks(a), keys = tile_count(kKeyShift, a.n_bands, 1, a.rows) * a.batch * a.kv_heads;
-    const int64_t far = tile_count(kFarShift, a.n_bands, 1, a.rows) * a.batch * a.kv_heads * ((a.sinks + 31) / 32);
+    const int64_t queries = query_blocks(a), far = far_blocks(a);
+    const int64_t keys = product(tile_count(kKeyShift, a.n_bands, 1, a.rows), a.batch, a.kv_heads);
     CHECK_TRY(check_grid(queries));
     CHECK_TRY(check_grid(keys));
-    CHECK_TRY(check_grid(far));
+    if (has_far(a)) CHECK_TRY(check_grid(far));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_shape(dtype, s->head_dim, wide, [&](auto t, auto dp, auto w) -> int {
         using T = decltype(t);

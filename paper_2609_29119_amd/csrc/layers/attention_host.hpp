@@ -57,7 +57,7 @@ inline AttnArgs attention_args(const nsgcqt_rows* r, const nsgcqt_attention_shap
 
 // Workgroups of the kernels that go by queries.
 inline int64_t query_blocks(const AttnArgs& a) {
-    return tile_count(query_shift(a.share), a.n_bands, 1, a.rows) * a.batch * (a.heads / a.share);
+    return product(tile_count(query_shift(a.share), a.n_bands, 1, a.rows), a.batch, a.heads / a.share);
 }
 
 // f(T(), DP) with the head width's padded size as an integral constant

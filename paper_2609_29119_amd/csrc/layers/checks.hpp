@@ -10,7 +10,7 @@ using nsg::launch_kernel;
 using nsg::set_err;
 
 constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxCount = int64_t(1) << 30, kMaxBands = int64_t(1) << 24,
-                  kMaxWidth = 65536, kMaxGrid = 0x7fffffff;
+                  kMaxWidth = 65536, kMaxGrid = 0xffffffffll / 256;   // a launch takes less than 2^32 threads
 
 inline int elem_bytes(int dtype) { return dtype == NSGCQT_F32 ? 4 : 2; }
 
@@ -59,9 +59,24 @@ inline View view_of(const nsgcqt_view* v) { return View{static_cast<char*>(v->da
         if (int r_ = (expr); r_ != NSGCQT_OK) return r_; \
     } while (0)
 
+// The product of counts that are not negative, or the largest number.
+template <class... N> inline int64_t product(int64_t a, N... rest) {
+    if constexpr (sizeof...(rest) > 0) {
+        int64_t all;
+        return __builtin_mul_overflow(a, product(rest...), &all) ? INT64_MAX : all;
+    }
+    return a;
+}
+
 inline int check_grid(int64_t blocks) {
-    if (blocks > kMaxGrid) return set_err(NSGCQT_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
+    if (blocks > kMaxGrid) return set_err(NSGCQT_EUNSUPPORTED, "more than 16,777,215 workgroups");
     return NSGCQT_OK;
+}
+
+// A workspace's size in bytes.
+inline int64_t workspace_of(int64_t bytes) {
+    if (bytes > (int64_t(1) << 60)) return set_err(NSGCQT_EUNSUPPORTED, "a workspace above 2^60 bytes");
+    return bytes;
 }
 
 // f(T()) for the element type of dtype

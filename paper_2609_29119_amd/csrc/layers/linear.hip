@@ -123,7 +123,8 @@ int64_t nsgcqt_band_linear_workspace(int64_t n_bands, int64_t batch, int64_t row
     static const int64_t none = 0;
     const nsgcqt_rows r{&none, n_bands, batch, rows};
     CHECK_TRY(check_linear(NSGCQT_F32, &r, n_in, n_out));
-    return 4 * tile_count(chunk_shift_of(batch, rows, n_in, n_out), n_bands, batch, rows) * (n_in * n_out + n_out);
+    return workspace_of(
+        product(4, tile_count(chunk_shift_of(batch, rows, n_in, n_out), n_bands, batch, rows), n_in * n_out + n_out));
 }
 
 int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const nsgcqt_view* dy,
@@ -137,6 +138,7 @@ int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt
     CHECK_TRY(check_weights(db, "db", dtype, 0));
     if (r->n_bands == 0 || n_out == 0 || (n_in == 0 && !db)) return NSGCQT_OK;
     const int64_t need = nsgcqt_band_linear_workspace(r->n_bands, r->batch, r->rows, n_in, n_out);
+    if (need < 0) return static_cast<int>(need);
     if (static_cast<int64_t>(ws_bytes) < need)
         return set_err(NSGCQT_EWORKSPACE, "workspace of " + std::to_string(ws_bytes) + " bytes, " +
                                               std::to_string(need) + " required");

@@ -202,3 +202,32 @@ def test_band_search(seed, tmp_path):
                     os.path.join(ROOT, "tests", "c", "band_search.cpp"), "-o", str(exe)], check=True, timeout=300)
     r = subprocess.run([str(exe), str(seed)], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stdout
+
+
+def test_sizes_past_what_a_launch_takes(L):
+    """Sizes that one launch cannot take are refused as such before anything is launched, also where their product
+    passes 64 bits; so are workspaces."""
+    v = view()
+    step = lambda n, heads, kv: L.nsgcqt_attention_step(  # noqa: E731
+        0, n, heads, kv, 8, 8, 0, 1.0, *[ref(v)] * 4, FAKE, FAKE, FAKE, None, 0, None)
+    refused(step(1 << 22, 4, 4), nb.EUNSUPPORTED, "workgroups")        # 2^24 workgroups of 256 threads
+    refused(step(1 << 20, 16, 1), nb.EUNSUPPORTED, "workgroups")       # outputs
+    attend = lambda r, s: L.nsgcqt_band_attention(0, ref(r), ref(s), *[ref(v)] * 4, None, None)  # noqa: E731
+    refused(attend(rows(bands=1 << 20, batch=16, n=1 << 20), shape(heads=8, kv=2)), nb.EUNSUPPORTED, "workgroups")
+    # 2^24 tiles of 2^30 signals and 2^16 heads: the product is 0 in 64 bits
+    wraps = rows(bands=(1 << 24) - 2 - 8, batch=1 << 30, n=1024)
+    refused(attend(wraps, shape(heads=65536, kv=65536)), nb.EUNSUPPORTED, "workgroups")
+    refused(L.nsgcqt_band_attention_workspace(ref(rows(bands=(1 << 24) - 4, batch=1 << 30, n=1024)),
+                                              ref(shape(heads=65536, kv=65536, sinks=4))), nb.EUNSUPPORTED, "workspace")
+    refused(L.nsgcqt_band_attention_grad(0, ref(rows(bands=1 << 20, batch=16, n=1 << 20)), ref(shape(heads=8, kv=8)),
+                                         *[ref(v)] * 4, FAKE, *[ref(v)] * 4, FAKE, 1 << 60, None),
+            nb.EUNSUPPORTED, "workgroups")
+    refused(L.nsgcqt_band_linear(0, ref(rows(bands=1 << 24, batch=1, n=1024)), ref(v), FAKE, None, ref(v), 8, 8, None),
+            nb.EUNSUPPORTED, "workgroups")
+    refused(L.nsgcqt_rotary(0, ref(v), ref(v), 1, None, None, 0, 1 << 20, 1 << 10, 64, FAKE, 1, 8, 0, FAKE,
+                            (ctypes.c_int32 * 4)(32, 0, 0, 0), 1, 0, 0, None), nb.EUNSUPPORTED, "workgroups")
+    # 2^34 tiles of 2^32 weights, 4 bytes each: 0 in 64 bits
+    n = L.nsgcqt_band_linear_workspace(2, 1 << 30, 1 << 10, 65536, 65535)
+    refused(n, nb.EUNSUPPORTED, "workspace")
+    refused(L.nsgcqt_band_linear_grad_weight(0, ref(rows(batch=1 << 30, n=1 << 10)), ref(v), ref(v), FAKE, FAKE, 65536,
+                                             65535, FAKE, 1 << 60, None), nb.EUNSUPPORTED, "workspace")
