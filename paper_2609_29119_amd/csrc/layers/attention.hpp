@@ -26,6 +26,7 @@ struct AttnArgs {
     int rows, n_bands, batch, heads, kv_heads, dim;
     int share;            // heads of one kv head that a workgroup takes: 1, 2 or 4
     int left, right, sinks;   // at most rows
+    int far;                  // of the sinks, those whose far queries have partial sums (gradient)
     float scale;
     AttnScale by;
 };
@@ -641,14 +642,19 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(sizeof(T) == 4 ? 1 : 
 // The sinks' keys are seen from everywhere. Queries past the window of a key
 // tile's last key ("far" ones) would make one workgroup walk a whole band, so
 // k_attention_far takes them in chunks and leaves partial dk, dv, which the
-// workgroup of the key tile adds up in the chunks' order.
+// workgroup of the key tile adds up in the chunks' order. The partial sums
+// take 64 dim floats for each 512 tokens and 32 sinks: with kFarSinks twice
+// what dk and dv take in 16 bits. Key tiles past those sinks walk the whole
+// band after all.
 constexpr int kFarShift = 9;   // queries of a chunk
+constexpr int kFarSinks = 512;
+static_assert(kFarSinks % kKeys == 0, "a key tile is on one side");
 __device__ inline int far_begin(const AttnArgs& a, int sink_tile) {   // of 32 keys
     return sink_tile * 32 / kKeys * kKeys + kKeys + a.left;
 }
 __device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t item, int sink_tile) {
     const int64_t per = tile_count(kFarShift, a.n_bands, 1, a.rows);
-    const int n = (a.sinks + 31) / 32;
+    const int n = (a.far + 31) / 32;
     return a.part + (((b * a.kv_heads + kv) * per + item) * n + sink_tile) * (2 * 32 * a.dim);
 }
 
@@ -756,7 +762,7 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(1))) void k_attention
     InRange<T> range_ds, range_p;
 
     const int i_begin = k0 > a.right ? k0 - a.right : 0;
-    const int i_end = min(k0 + kKeys + a.left, len);
+    const int i_end = k0 >= a.far && k0 < a.sinks ? len : min(k0 + kKeys + a.left, len);
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
     const unsigned span = j < a.sinks ? 0x7fffffffu : static_cast<unsigned>(a.left) + a.right;
     float next_lse = 0.f, next_delta = 0.f;
@@ -817,14 +823,14 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(1))) void k_attention
         }
     }
     // the far queries' share of the sinks
-    if (j_lo < a.sinks && active) {
+    if (j_lo < a.far && active) {
         const int tile = j_lo / 32;
         const int begin = far_begin(a, tile);
         const int64_t item0 = (t.start >> kFarShift) + t.band + 1;
         if (begin < len)
             for (int ch = begin >> kFarShift; ch <= (len - 1) >> kFarShift; ++ch) {
                 const float* p = far_part(a, b, kv, item0 + ch, tile) + m * a.dim;
-                if (j < a.sinks && mine) {
+                if (j < a.far && mine) {
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) {
 #pragma unroll
@@ -867,7 +873,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     static_assert(sizeof(lds) >= 2 * DP * 33 * 4, "the tiles' room also serves to add up the waves");
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
 
-    const unsigned n_sink = (a.sinks + 31) / 32, id = die_order(blockIdx.x, gridDim.x);
+    const unsigned n_sink = (a.far + 31) / 32, id = die_order(blockIdx.x, gridDim.x);
     const int tile = id % n_sink, kv = id / n_sink % a.kv_heads;
     const unsigned rest = id / n_sink / a.kv_heads;
     const unsigned per = static_cast<unsigned>(tile_count(kFarShift, a.n_bands, 1, a.rows));
@@ -879,7 +885,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
     const int i_begin = max(t.first, far), i_end = min(t.first + (1 << kFarShift), len);
     if (i_begin >= i_end) return;
     const uint8_t* keep = a.keep ? a.keep + b * a.keep_batch + t.start : nullptr;
-    const bool kept = j < a.sinks && j < len && (!keep || keep[j]);
+    const bool kept = j < a.far && j < len && (!keep || keep[j]);
     const int64_t row = t.start + (j < len ? j : 0);
     frag<T> kf[DP / 16];
     load_rows<T, DP>(kf, row_of<T>(a.k, b, row, kv), kept, a.dim, WIDE, lane);
@@ -935,7 +941,7 @@ __global__ __launch_bounds__(256, DP > 64 || (sizeof(T) == 4 && DP > 32) ? 1 : 2
         }
         __syncthreads();
     }
-    const int keys = min(32, a.sinks - 32 * tile);
+    const int keys = min(32, a.far - 32 * tile);
     float* out = far_part(a, b, kv, item, tile);
     for (int x = tid; x < 2 * 32 * a.dim; x += 256) {
         const int c = x % a.dim, key = x / a.dim % 32;

@@ -11,7 +11,7 @@ int64_t delta_bytes(const AttnArgs& a) { return align256(int64_t(4) * a.rows * a
 
 // Workgroups of the far queries: for each chunk, kv head and 32 sinks.
 int64_t far_blocks(const AttnArgs& a) {
-    return product(tile_count(kFarShift, a.n_bands, 1, a.rows), a.batch, a.kv_heads, (a.sinks + 31) / 32);
+    return product(tile_count(kFarShift, a.n_bands, 1, a.rows), a.batch, a.kv_heads, (a.far + 31) / 32);
 }
 
 int64_t part_bytes(const AttnArgs& a) { return product(far_blocks(a), 4 * 2 * 32 * a.dim); }

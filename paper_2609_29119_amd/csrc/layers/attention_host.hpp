@@ -50,6 +50,7 @@ inline AttnArgs attention_args(const nsgcqt_rows* r, const nsgcqt_attention_shap
     a.left = cut(s->left);
     a.right = cut(s->right);
     a.sinks = cut(s->sinks);
+    a.far = a.sinks < kFarSinks ? a.sinks : kFarSinks;
     a.scale = static_cast<float>(s->scale);
     a.by = scale_of(s->scale);
     return a;

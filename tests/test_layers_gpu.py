@@ -899,3 +899,19 @@ def test_weights_gradient_of_many_bands():
     close(y, ry, product_bound(torch.float32, 2), "y")
     close(dw, rdw, product_bound(torch.float32, 9000), "dw")
     close(db, rdb, product_bound(torch.float32, 9000), "db")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_sinks_than_have_partial_sums(dtype):
+    """Sinks past the 512 whose far queries are summed in parts: their key tiles walk the band."""
+    lengths, h, hk, d = [1500, 700], 2, 1, 16
+    q, k, v, do = (randn(i, 1, 2200, n, d, dtype=dtype).requires_grad_(i < 4)
+                   for i, n in ((1, h), (2, hk), (3, hk), (4, h)))
+    keep = (torch.rand(1, 2200, generator=torch.Generator().manual_seed(0)) > 0.2).cuda()
+    for sinks, kp in ((700, None), (600, keep), (512, None)):
+        o = layers.band_attention(q, k, v, offsets_of(lengths), 10, 2, sinks, keep=kp)
+        grads = torch.autograd.grad(o, [q, k, v], do)
+        ref = attention_reference(q, k, v, lengths, 0, 10, 2, sinks, d ** -0.5, kp, do)
+        close(o, ref[0], attention_bound(dtype), "o")
+        for got, r, name, size in zip(grads, ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+            close(got, r, attention_bound(dtype, True), name, size)

@@ -231,3 +231,9 @@ def test_sizes_past_what_a_launch_takes(L):
     refused(n, nb.EUNSUPPORTED, "workspace")
     refused(L.nsgcqt_band_linear_grad_weight(0, ref(rows(batch=1 << 30, n=1 << 10)), ref(v), ref(v), FAKE, FAKE, 65536,
                                              65535, FAKE, 1 << 60, None), nb.EUNSUPPORTED, "workspace")
+
+
+def test_gradient_workspace_with_many_sinks(L):
+    """The partial sums of the sinks are bounded: 131,072 tokens, every one a sink, 2 kv heads of 128."""
+    s, r = shape(heads=8, kv=2, dim=128, left=1023, sinks=131072), rows(bands=1, n=131072)
+    assert L.nsgcqt_band_attention_workspace(ref(r), ref(s)) <= 4 * 131072 * 8 + 2 * (2 * 2 * 131072 * 2 * 128) * 1.05
