@@ -717,6 +717,13 @@ __device__ inline void key_grad(const char* qt, const char* gt, const float* lse
     }
 }
 
+// Past the last query near 128 keys from k0 on. (Their sum passes 31 bits in
+// the longest rows.)
+__host__ __device__ inline int queries_end(int k0, int left, int len) {
+    const int64_t end = static_cast<int64_t>(k0) + kKeys + left;
+    return static_cast<int>(end < len ? end : len);
+}
+
 // dk, dv of 128 keys (a wave has 32) over the queries near them, for all heads
 // of their kv head: no atomics and no partial sums but the sinks'. Scores and
 // dp are formed the other way round than in dq (a lane has one key), so p and
@@ -762,7 +769,7 @@ __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(1))) void k_attention
     InRange<T> range_ds, range_p;
 
     const int i_begin = k0 > a.right ? k0 - a.right : 0;
-    const int i_end = k0 >= a.far && k0 < a.sinks ? len : min(k0 + kKeys + a.left, len);
+    const int i_end = k0 >= a.far && k0 < a.sinks ? len : queries_end(k0, a.left, len);
     const int q_tiles = (i_end - i_begin + BQ - 1) / BQ, total = q_tiles * group;
     const unsigned span = j < a.sinks ? 0x7fffffffu : static_cast<unsigned>(a.left) + a.right;
     float next_lse = 0.f, next_delta = 0.f;

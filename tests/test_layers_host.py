@@ -190,18 +190,27 @@ def test_no_kernel_spills(name, tmp_path):
     assert not [(n, s) for n, s in zip(names, scratch) if s]
 
 
+def run_on_the_host(name, tmp_path, *args):
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("hipcc not available")
+    exe = tmp_path / name
+    subprocess.run([hipcc, "-x", "hip", "--offload-host-only", "-O2", "-fwrapv", "-std=c++17", "-w",
+                    os.path.join(ROOT, "tests", "c", name + ".cpp"), "-o", str(exe)], check=True, timeout=300)
+    r = subprocess.run([str(exe), *args], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout
+
+
 @pytest.mark.parametrize("seed", [0, 1])
 def test_band_search(seed, tmp_path):
     """The search for a work item's band against a plain scan, on the host: 0 to 20,000 bands, among them those where
     its last round goes in steps of more than one; offsets in any order keep every tile and chunk in range."""
-    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
-    if not os.path.exists(hipcc):
-        pytest.skip("hipcc not available")
-    exe = tmp_path / "band_search"
-    subprocess.run([hipcc, "-x", "hip", "--offload-host-only", "-O2", "-std=c++17", "-w",
-                    os.path.join(ROOT, "tests", "c", "band_search.cpp"), "-o", str(exe)], check=True, timeout=300)
-    r = subprocess.run([str(exe), str(seed)], capture_output=True, text=True, timeout=120)
-    assert r.returncode == 0, r.stdout
+    run_on_the_host("band_search", tmp_path, str(seed))
+
+
+def test_attention_range_of_the_longest_rows(tmp_path):
+    """The end of a key tile's queries, with a window as long as the longest row."""
+    run_on_the_host("attention_range", tmp_path)
 
 
 def test_sizes_past_what_a_launch_takes(L):
