@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     const int h_first = 32 * hb, h_count = min(32, a.group - h_first);
 
     const int64_t pos = a.pos[stream];
-    const int n = pos < 0 ? 0 : static_cast<int>(pos + 1 < a.slots ? pos + 1 : a.slots);
+    const int n = pos < 0 ? 0 : pos < a.slots ? static_cast<int>(pos) + 1 : a.slots;
     const int fresh = pos < 0 ? -1 : ring_slot(pos, a.sinks, a.window);
     const T* kn = reinterpret_cast<T*>(a.k.data) + stream * a.k.batch + kv * a.k.head;
     const T* vn = reinterpret_cast<T*>(a.v.data) + stream * a.v.batch + kv * a.v.head;

@@ -915,3 +915,17 @@ def test_more_sinks_than_have_partial_sums(dtype):
         close(o, ref[0], attention_bound(dtype), "o")
         for got, r, name, size in zip(grads, ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
             close(got, r, attention_bound(dtype, True), name, size)
+
+
+def test_step_numbers_up_to_the_last():
+    """The largest token numbers: the cache is full, whatever the number."""
+    n, d, slots = 3, 16, 9
+    q, k, v = (randn(i, n, 1, d) for i in range(3))
+    kc, vc = randn(3, n, 1, slots, d), randn(4, n, 1, slots, d)
+    pos = torch.tensor([(1 << 63) - 1, (1 << 40) + 5, (1 << 31) - 1], device="cuda")
+    o = layers.attention_step(q, k, v, kc, vc, pos, 2)
+    for s, p in enumerate(pos.tolist()):
+        at = 2 + (p - 2) % 7
+        assert torch.equal(kc[s, 0, at], k[s, 0]) and torch.equal(vc[s, 0, at], v[s, 0])
+        want = step_reference(q[s].cpu(), kc[s].transpose(0, 1).cpu(), vc[s].transpose(0, 1).cpu(), slots, slots, 1, 0.25)
+        close(o[s], want, attention_bound(torch.float32), f"stream {s}")
