@@ -544,7 +544,8 @@ class StreamCache:
     def fill(self, k, v, offsets):
         """Starts the streams with whole bands (`cache_fill`)."""
         cache_fill(k, v, offsets, self.k, self.v, self.sinks)
-        self.pos.copy_((offsets[1:] - offsets[:-1]).repeat(k.shape[0]))
+        ends = offsets.clamp(0, k.shape[1])     # bands are cut to the row, as the kernels cut them
+        self.pos.copy_((ends[1:] - ends[:-1]).repeat(k.shape[0]))
 
     def step(self, q, k, v, scale=None):
         """`attention_step` of every stream's next token (zeros for an idle one)."""

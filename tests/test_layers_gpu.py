@@ -929,3 +929,14 @@ def test_step_numbers_up_to_the_last():
         assert torch.equal(kc[s, 0, at], k[s, 0]) and torch.equal(vc[s, 0, at], v[s, 0])
         want = step_reference(q[s].cpu(), kc[s].transpose(0, 1).cpu(), vc[s].transpose(0, 1).cpu(), slots, slots, 1, 0.25)
         close(o[s], want, attention_bound(torch.float32), f"stream {s}")
+
+
+def test_fill_numbers_the_tokens_that_exist():
+    """Bands that reach past the row (or begin before it) are cut to it: the next token's number counts those held."""
+    k = randn(0, 2, 12, 1, 8)
+    cache = layers.StreamCache(6, 1, 8, 20, dtype=torch.float32)
+    cache.fill(k, k, torch.tensor([-3, 4, 9, 30], device="cuda"))
+    assert cache.pos.tolist() == [4, 5, 3] * 2
+    for s in range(6):
+        a, b = [(0, 4), (4, 9), (9, 12)][s % 3]
+        assert torch.equal(cache.k[s, 0, :b - a], k[s // 3, a:b, 0]) and not cache.k[s, 0, b - a:].any()
