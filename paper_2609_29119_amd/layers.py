@@ -101,8 +101,10 @@ def _stream(t):
     return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
-def _tensor(t, name, like=None, shape=None):
+def _tensor(t, name, like=None, shape=None, dims=None):
     """Checks one tensor of a call: its device, type, shape and last stride."""
+    if dims is not None and t.dim() != dims.count("["):
+        raise ValueError(f"{name} has {t.dim()} axes: {dims} is expected")
     if not t.is_cuda:
         raise ValueError(f"{name} is on {t.device}: a cuda tensor is expected")
     if like is None:
@@ -144,6 +146,11 @@ def _view_step(t):
     return _view(t.data_ptr(), s[0], 0, s[1])
 
 
+def _scale(scale, dim):
+    """The scores' factor as given, or D^-1/2 (the call refuses a width of 0)."""
+    return float(scale) if scale is not None else dim ** -0.5 if dim else 1.0
+
+
 def _trains(*tensors):
     """Whether a result has to carry a derivative: an input requires grad, or
     has a forward-mode tangent (which no operator here has a rule for: the
@@ -178,9 +185,9 @@ def _last(t):
 
 
 def _linear_checks(x, weight, offsets, bias):
-    _tensor(x, "x")
-    if x.dim() != 3 or weight.dim() != 3:
-        raise ValueError("x has to be [batch][rows][n_in] and weight [n_bands][n_out][n_in]")
+    _tensor(x, "x", dims="[batch][rows][n_in]")
+    if weight.dim() != 3:
+        raise ValueError("weight has to be [n_bands][n_out][n_in]")
     _offsets(offsets, x)
     bands = offsets.numel() - 1
     _tensor(weight, "weight", x, (bands, weight.shape[1], x.shape[2]))
@@ -350,9 +357,7 @@ def rotary(q, k, positions, freqs, sections, interleaved=False):
     64 bits. Gradients for q and k; positions and freqs have none and are
     refused where they would need one. Returns (q, k), or q alone if k is None.
     """
-    _tensor(q, "q")
-    if q.dim() != 4:
-        raise ValueError("q has to be [batch][rows][heads][D]")
+    _tensor(q, "q", dims="[batch][rows][heads][D]")
     batch, rows, _, dim = q.shape
     if k is not None:
         if k.dim() != 4:
@@ -430,9 +435,9 @@ def band_attention(q, k, v, offsets, left, right=0, sinks=0, scale=None, keep=No
     token that sees none gets zeros and passes no gradient, and what k and v
     hold at tokens that are not kept is never used. Gradients for q, k, v.
     """
-    _tensor(q, "q")
-    if q.dim() != 4 or k.dim() != 4:
-        raise ValueError("q and k have to be [batch][rows][heads][D]")
+    _tensor(q, "q", dims="[batch][rows][heads][D]")
+    if k.dim() != 4:
+        raise ValueError("k has to be [batch][rows][kv_heads][D]")
     batch, rows, heads, dim = q.shape
     _tensor(k, "k", q, (batch, rows, k.shape[2], dim))
     _tensor(v, "v", q, k.shape)
@@ -444,7 +449,7 @@ def band_attention(q, k, v, offsets, left, right=0, sinks=0, scale=None, keep=No
     far = 1 << 40
     call = _BandAttention.apply if _trains(q, k, v) else _attention_forward
     return call(q, k, v, offsets, keep, far if left is None else int(left), far if right is None else int(right),
-                int(sinks), dim ** -0.5 if scale is None else float(scale))
+                int(sinks), _scale(scale, dim))
 
 
 # ------------------------------------------------------------- single-token step
@@ -476,9 +481,9 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
     attends over all tokens held. pos < 0: the stream has no token in this
     step, its cache stays as it is and its row is zero. Not differentiable.
     """
-    _tensor(q, "q")
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q and k have to be [streams][heads][D]")
+    _tensor(q, "q", dims="[streams][heads][D]")
+    if k.dim() != 3:
+        raise ValueError("k has to be [streams][kv_heads][D]")
     streams, heads, dim = q.shape
     kv_heads = k.shape[1]
     _tensor(k, "k", q, (streams, kv_heads, dim))
@@ -495,7 +500,7 @@ def attention_step(q, k, v, k_cache, v_cache, pos, sinks=0, scale=None, out=None
     with _on(q):
         _check(_lib().nsgcqt_attention_step(
             _DTYPES[q.dtype], streams, heads, kv_heads, dim, slots - sinks, sinks,
-            dim ** -0.5 if scale is None else float(scale), _view_step(q), _view_step(k), _view_step(v), _view_step(o),
+            _scale(scale, dim), _view_step(q), _view_step(k), _view_step(v), _view_step(o),
             k_cache.data_ptr(), v_cache.data_ptr(), pos.data_ptr(), ws.data_ptr() if n else None, n, _stream(q)))
     _written(k_cache, v_cache, *(() if out is None else (out,)))
     return o
@@ -509,9 +514,7 @@ def cache_fill(k, v, offsets, k_cache, v_cache, sinks=0):
     offsets[g + 1] - offsets[g]. Slots without a token are left alone. Not
     differentiable.
     """
-    _tensor(k, "k")
-    if k.dim() != 4:
-        raise ValueError("k has to be [batch][rows][kv_heads][D]")
+    _tensor(k, "k", dims="[batch][rows][kv_heads][D]")
     batch, rows, kv_heads, dim = k.shape
     _tensor(v, "v", k, k.shape)
     _offsets(offsets, k)

@@ -940,3 +940,25 @@ def test_fill_numbers_the_tokens_that_exist():
     for s in range(6):
         a, b = [(0, 4), (4, 9), (9, 12)][s % 3]
         assert torch.equal(cache.k[s, 0, :b - a], k[s // 3, a:b, 0]) and not cache.k[s, 0, b - a:].any()
+
+
+def test_refusals_of_shapes_without_axes_or_width():
+    """Tensors of other dimensions and heads of width 0 get the calls' own errors."""
+    off, one, x = offsets_of([4]), randn(0), randn(1, 1, 4, 2, 16)
+    w, pos, freqs = randn(2, 1, 3, 16), torch.zeros(1, 4, dtype=torch.float64, device="cuda"), layers.rotary_frequencies([8])
+    c = layers.StreamCache(4, 2, 16, 8, dtype=torch.float32)
+    for t in (one, x[0, 0, 0], x[None]):
+        for call in (lambda: layers.band_linear(t, w, off), lambda: layers.band_linear(x[:, :, 0], t, off),
+                     lambda: layers.rotary(t, None, pos, freqs, [8]), lambda: layers.rotary(x, t, pos, freqs, [8]),
+                     lambda: layers.band_attention(t, x, x, off, 3), lambda: layers.band_attention(x, t, x, off, 3),
+                     lambda: layers.band_attention(x, x, t, off, 3), lambda: layers.cache_fill(t, x, off, c.k, c.v),
+                     lambda: c.step(t, x[0], x[0]), lambda: c.step(x[0], t, x[0])):
+            with pytest.raises(ValueError):
+                call()
+    none = x[..., :0]
+    for call in (lambda: layers.band_attention(none, none, none, off, 3),
+                 lambda: layers.attention_step(none[0], none[0], none[0], c.k[..., :0].contiguous(),
+                                               c.v[..., :0].contiguous(), c.pos)):
+        with pytest.raises(nc.NsgcqtError) as e:
+            call()
+        assert e.value.status == nc.EINVAL
