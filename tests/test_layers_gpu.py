@@ -944,7 +944,7 @@ def test_fill_numbers_the_tokens_that_exist():
 
 def test_refusals_of_shapes_without_axes_or_width():
     """Tensors of other dimensions and heads of width 0 get the calls' own errors."""
-    off, one, x = offsets_of([4]), randn(0), randn(1, 1, 4, 2, 16)
+    off, one, x = offsets_of([4]), randn(0, 1)[0], randn(1, 1, 4, 2, 16)
     w, pos, freqs = randn(2, 1, 3, 16), torch.zeros(1, 4, dtype=torch.float64, device="cuda"), layers.rotary_frequencies([8])
     c = layers.StreamCache(4, 2, 16, 8, dtype=torch.float32)
     for t in (one, x[0, 0, 0], x[None]):
