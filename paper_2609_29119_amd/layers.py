@@ -114,8 +114,11 @@ def _tensor(t, name, like=None, shape=None, dims=None):
         raise ValueError(f"{name} is {t.dtype} on {t.device}: {like.dtype} on {like.device} is expected")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is expected")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"the last axis of {name} has to be contiguous")
+    if t.shape[-1] > 1:
+        if t.stride(-1) != 1:
+            raise ValueError(f"the last axis of {name} has to be contiguous")
+    elif t.is_neg():   # (of the imaginary part of a conjugate: its other strides are even, never 1)
+        raise ValueError(f"{name} is a lazy negative: call resolve_neg()")
     return t
 
 
@@ -177,7 +180,8 @@ def _written(*tensors):
 
 
 def _last(t):
-    """t with a contiguous last axis (a gradient may come in any layout)."""
+    """t with a contiguous last axis and no lazy sign (a gradient may come in any layout)."""
+    t = t.resolve_neg()
     return t if t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
 
 
@@ -368,7 +372,7 @@ def rotary(q, k, positions, freqs, sections, interleaved=False):
     if positions.dtype not in _POS or positions.device != q.device:
         raise ValueError("positions has to be float32, float64 or int64 on the device of q")
     if (positions.shape != (axes, rows) and positions.shape != (axes, batch, rows)) or (
-            positions.stride(-1) != 1 and rows > 1):
+            positions.stride(-1) != 1 if rows > 1 else positions.is_neg()):
         raise ValueError("positions has to be [axes][rows] or [axes][batch][rows], its rows contiguous")
     if freqs.dtype != torch.float32 or freqs.device != q.device or freqs.shape != (pairs,) or not freqs.is_contiguous():
         raise ValueError(f"freqs has to be a float32 vector of {pairs} values on the device of q")

@@ -962,3 +962,21 @@ def test_refusals_of_shapes_without_axes_or_width():
         with pytest.raises(nc.NsgcqtError) as e:
             call()
         assert e.value.status == nc.EINVAL
+
+
+def test_lazy_negatives():
+    """The imaginary part of a conjugate is stored with the other sign: such a tensor is refused, such a gradient is
+    taken with its sign."""
+    off, w = offsets_of([4, 2]), randn(0, 2, 1, 1)
+    z = torch.complex(randn(1, 1, 6), randn(2, 1, 6))
+    lazy = z.conj().imag.unsqueeze(-1)
+    assert lazy.is_neg()
+    with pytest.raises(ValueError, match="negative"):
+        layers.band_linear(lazy, w, off)
+    with pytest.raises(ValueError, match="negative"):
+        layers.band_attention(lazy[..., None], lazy[..., None], lazy[..., None], off, 3)
+    x = z.imag.unsqueeze(-1).clone().requires_grad_()
+    y = layers.band_linear(x, w, off)
+    (dx,) = torch.autograd.grad(y, [x], lazy)
+    (want,) = torch.autograd.grad(layers.band_linear(x, w, off), [x], lazy.resolve_neg())
+    assert torch.equal(dx, want)
