@@ -980,3 +980,59 @@ def test_lazy_negatives():
     (dx,) = torch.autograd.grad(y, [x], lazy)
     (want,) = torch.autograd.grad(layers.band_linear(x, w, off), [x], lazy.resolve_neg())
     assert torch.equal(dx, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("d,left,sinks", [(96, 20, 5), (128, 20, 40), (100, 30, 5), (125, 0, 70)])
+def test_far_queries_of_wide_heads(d, left, sinks, masked, dtype):
+    """Sinks over several chunks of far queries at heads above 64, aligned and not."""
+    lengths, h, hk = [1400, 60], 4, 1
+    q, k, v, do = (randn(i, 1, 1460, n, d, dtype=dtype).requires_grad_(i < 4)
+                   for i, n in ((1, h), (2, hk), (3, hk), (4, h)))
+    keep = (torch.rand(1, 1460, generator=torch.Generator().manual_seed(d)) > 0.3).cuda() if masked else None
+    o = layers.band_attention(q, k, v, offsets_of(lengths), left, 0, sinks, keep=keep)
+    grads = torch.autograd.grad(o, [q, k, v], do)
+    ref = attention_reference(q, k, v, lengths, 0, left, 0, sinks, d ** -0.5, keep, do)
+    close(o, ref[0], attention_bound(dtype), "o")
+    for got, r, name, size in zip(grads, ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+        close(got, r, attention_bound(dtype, True), name, size)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("h,hk", [(12, 1), (6, 1), (10, 2), (24, 3)])
+def test_large_groups_of_query_heads(h, hk, dtype):
+    """More query heads a key head than a workgroup takes."""
+    lengths, d = [130, 0, 77], 24
+    q, k, v, do = (randn(i, 2, 207, n, d, dtype=dtype).requires_grad_(i < 4)
+                   for i, n in ((1, h), (2, hk), (3, hk), (4, h)))
+    o = layers.band_attention(q, k, v, offsets_of(lengths), 30, 3, 2)
+    grads = torch.autograd.grad(o, [q, k, v], do)
+    ref = attention_reference(q, k, v, lengths, 0, 30, 3, 2, d ** -0.5, None, do)
+    close(o, ref[0], attention_bound(dtype), "o")
+    for got, r, name, size in zip(grads, ref[1:4], ("dq", "dk", "dv"), (*ref[4:], None)):
+        close(got, r, attention_bound(dtype, True), name, size)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [1, 7, 20, 24])
+def test_cache_fill_holds_what_steps_would(d, dtype):
+    """Each slot has the last token that goes to it; the others, and slots without a token, are left alone."""
+    lengths, hk, window, sinks = [0, 3, 9, 40], 2, 6, 2
+    base = randn(0, 2, 52, 2 * hk + 1, d + 1, dtype=dtype)
+    k, v = base[:, :, 1:1 + hk, 1:], base[:, :, 1 + hk:, 1:]      # strides that no 16-byte access fits
+    cache = layers.StreamCache(8, hk, d, window, sinks, dtype=dtype)
+    cache.k.fill_(-7.0)
+    cache.v.fill_(-8.0)
+    cache.fill(k, v, offsets_of(lengths))
+    assert cache.pos.tolist() == lengths * 2
+    for got, x, none in ((cache.k, k, -7.0), (cache.v, v, -8.0)):
+        want = torch.full_like(got, none)
+        for b in range(2):
+            at = 0
+            for g, n in enumerate(lengths):
+                for t in range(n):
+                    slot = t if t < sinks else sinks + (t - sinks) % window
+                    want[b * 4 + g, :, slot] = x[b, at + t]
+                at += n
+        assert torch.equal(got, want)
