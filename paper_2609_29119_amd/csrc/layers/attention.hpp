@@ -659,8 +659,9 @@ __device__ inline float* far_part(const AttnArgs& a, int64_t b, int kv, int64_t 
 }
 
 // One wave's 32 queries (rows of the tiles qt, gt at r0) against its 32 keys:
-// adds to dk^T and dv^T. kf, vt: the keys' k as fragments and v in LDS. lse, delta: of the tile's queries, in LDS (+inf for a
-// query that is not there: its probabilities are 0). With edge, this lane's
+// adds to dk^T and dv^T, each times its column's power of two. kf, vt: the
+// keys' k as fragments and v in LDS. lse, delta: of the tile's queries, in LDS
+// (+inf for a query that is not there: its probabilities are 0). With edge, this lane's
 // key is visible to the rows r0 + lo .. r0 + lo + span only. A key that is
 // not there or not kept only spoils its own column, which its lane drops.
 template <class T, int DP>

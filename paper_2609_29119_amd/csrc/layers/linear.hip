@@ -158,8 +158,10 @@ int nsgcqt_band_linear_grad_weight(int dtype, const nsgcqt_rows* r, const nsgcqt
     return by_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
         LAUNCH_TRY(k_linear_dw<T>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
-        LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64), static_cast<unsigned>(std::min(a.n_bands, 65535))),
-                   dim3(256), 0, st, a);
+        for (; a.first_band < a.n_bands; a.first_band += 65535)   // the most that a grid's second axis holds
+            LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64),
+                                              static_cast<unsigned>(std::min(a.n_bands - a.first_band, 65535))),
+                       dim3(256), 0, st, a);
         return NSGCQT_OK;
     });
 }

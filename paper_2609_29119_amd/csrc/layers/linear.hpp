@@ -19,6 +19,7 @@ struct LinearArgs {
     const int64_t* off;
     int rows, n_bands, batch;
     int n_in, n_out;      // of the layer, whichever direction is computed
+    int first_band;       // of a launch of k_linear_join
     int chunk_shift;      // rows of a workgroup of the weights' gradient, or of k_linear_kept
     bool x_wide, y_wide, w_wide;
 };
@@ -239,49 +240,51 @@ __global__ __launch_bounds__(256, 2) void k_linear_kept(LinearArgs a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {   // one slab; its registers are then free for the one after the next
             if (r0 >= r_end) continue;
-                if (step == 0) {
-                    each<NB>([&](auto nb) __attribute__((always_inline)) {
-                        acc16 v = zero16();
-                        if (a.bias && !outside) {
-        #pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const f4 u = *reinterpret_cast<const f4*>(start + 32 * nb.value + 8 * q + 4 * h);
-        #pragma unroll
-                                for (int j = 0; j < 4; ++j) v[4 * q + j] = u[j];
-                            }
-                        }
-                        acc[nb.value] = v;
-                    });
-                }
-                if (!outside) {
-        #pragma unroll
-                    for (int e = 0; e < kRowEach; ++e) write8<T, 128>(slab, (lane + 64 * e) / (BK / 8), lane % (BK / 8), xr[u][e]);
-                    fetch(xr[u]);
-                    each<KS>([&](auto s) __attribute__((always_inline)) {
-                        if (step * BK + 16 * s.value < n_red) {
-                            const frag<T> xf = read8<T, 128>(slab, m, 2 * s.value + h);
-                            each<NB>([&](auto nb) __attribute__((always_inline)) {
-                                if constexpr (BACK)
-                                    acc[nb.value] = mma(
-                                        read_turned8<T, row_bytes<T, BN>()>(wt, step * BK + 16 * s.value, 32 * nb.value, lane),
-                                        xf, acc[nb.value]);
-                                else
-                                    acc[nb.value] = mma(read8<T>(wt, RB, min(32 * nb.value + m, w_rows - 1),
-                                                                 step * (BK / 8) + 2 * s.value + h),
-                                                        xf, acc[nb.value]);
-                            });
-                        }
-                    });
-                }
-                if (++step >= steps || outside) {
-                    T* out = r0 + m < r_end ? band_row<T>(a.y, t, r0 + m) : nullptr;
-                    T* row_out[4];
+            if (step == 0) {
+                each<NB>([&](auto nb) __attribute__((always_inline)) {
+                    acc16 v = zero16();
+                    if (a.bias && !outside) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) row_out[e] = from_lane(out, lane / 8 + 8 * e);
-            store_rows<T, NB>(slab, acc, row_out, static_cast<int>(min(r_end - r0, int64_t(32))), c0, n_col, a.y_wide, lane);
-                    r0 += 128;
-                    step = 0;
-                }
+                        for (int q = 0; q < 4; ++q) {
+                            const f4 u = *reinterpret_cast<const f4*>(start + 32 * nb.value + 8 * q + 4 * h);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[4 * q + j] = u[j];
+                        }
+                    }
+                    acc[nb.value] = v;
+                });
+            }
+            if (!outside) {
+#pragma unroll
+                for (int e = 0; e < kRowEach; ++e)
+                    write8<T, 128>(slab, (lane + 64 * e) / (BK / 8), lane % (BK / 8), xr[u][e]);
+                fetch(xr[u]);
+                each<KS>([&](auto s) __attribute__((always_inline)) {
+                    if (step * BK + 16 * s.value < n_red) {
+                        const frag<T> xf = read8<T, 128>(slab, m, 2 * s.value + h);
+                        each<NB>([&](auto nb) __attribute__((always_inline)) {
+                            if constexpr (BACK)
+                                acc[nb.value] = mma(read_turned8<T, row_bytes<T, BN>()>(wt, step * BK + 16 * s.value,
+                                                                                        32 * nb.value, lane),
+                                                    xf, acc[nb.value]);
+                            else
+                                acc[nb.value] = mma(read8<T>(wt, RB, min(32 * nb.value + m, w_rows - 1),
+                                                             step * (BK / 8) + 2 * s.value + h),
+                                                    xf, acc[nb.value]);
+                        });
+                    }
+                });
+            }
+            if (++step >= steps || outside) {
+                T* out = r0 + m < r_end ? band_row<T>(a.y, t, r0 + m) : nullptr;
+                T* row_out[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) row_out[e] = from_lane(out, lane / 8 + 8 * e);
+                store_rows<T, NB>(slab, acc, row_out, static_cast<int>(min(r_end - r0, int64_t(32))), c0, n_col,
+                                  a.y_wide, lane);
+                r0 += 128;
+                step = 0;
+            }
         }
     }
 }
@@ -399,25 +402,24 @@ __global__ __launch_bounds__(256, 2) void k_linear_dw(LinearArgs a) {
     }
 }
 
-// Adds the partial sums of bands of several chunks, and writes zeros for empty bands.
+// Adds the partial sums of bands of several chunks, and writes zeros for empty bands: bands first_band on.
 template <class T>
 __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
+    const int band = a.first_band + static_cast<int>(blockIdx.y);
+    const int64_t b0 = band_bound(a.off, a.n_bands, a.rows, band + 1), b1 = band_bound(a.off, a.n_bands, a.rows, band + 2);
+    const int64_t n_rows = b1 > b0 ? (b1 - b0) * a.batch : 0;
+    if (n_rows > 0 && n_rows <= (int64_t(1) << a.chunk_shift)) return;
     const int64_t n_w = static_cast<int64_t>(a.n_out) * a.n_in, n = n_w + (a.db ? a.n_out : 0);
-    for (int band = blockIdx.y; band < a.n_bands; band += gridDim.y) {
-        const int64_t b0 = band_bound(a.off, a.n_bands, a.rows, band + 1), b1 = band_bound(a.off, a.n_bands, a.rows, band + 2);
-        const int64_t n_rows = b1 > b0 ? (b1 - b0) * a.batch : 0;
-        if (n_rows > 0 && n_rows <= (int64_t(1) << a.chunk_shift)) continue;
-        const int64_t chunks = (n_rows + (int64_t(1) << a.chunk_shift) - 1) >> a.chunk_shift;
-        const int64_t item = ((b0 * a.batch) >> a.chunk_shift) + band + 1;
-        for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
-            float s = 0.f;
+    const int64_t chunks = (n_rows + (int64_t(1) << a.chunk_shift) - 1) >> a.chunk_shift;
+    const int64_t item = ((b0 * a.batch) >> a.chunk_shift) + band + 1;
+    for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
+        float s = 0.f;
 #pragma unroll 8
-            for (int64_t c = 0; c < chunks; ++c) s += dw_part(a, item + c)[e];
-            if (e < n_w)
-                static_cast<T*>(a.dw)[band * n_w + e] = static_cast<T>(s);
-            else
-                static_cast<T*>(a.db)[static_cast<int64_t>(band) * a.n_out + e - n_w] = static_cast<T>(s);
-        }
+        for (int64_t c = 0; c < chunks; ++c) s += dw_part(a, item + c)[e];
+        if (e < n_w)
+            static_cast<T*>(a.dw)[band * n_w + e] = static_cast<T>(s);
+        else
+            static_cast<T*>(a.db)[static_cast<int64_t>(band) * a.n_out + e - n_w] = static_cast<T>(s);
     }
 }
 

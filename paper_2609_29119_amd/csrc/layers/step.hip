@@ -107,9 +107,9 @@ int nsgcqt_cache_fill(int dtype, const nsgcqt_rows* r, int64_t n_kv_heads, int64
     CHECK_TRY(check_dtype(dtype));
     CHECK_TRY(check_rows(r));
     CHECK_TRY(check_step(r->batch * r->n_bands, n_kv_heads, n_kv_heads, head_dim, window, sinks));
-    bool wide = true;
-    CHECK_TRY(check_view(k, "k", dtype, r->batch, r->rows, n_kv_heads, head_dim, wide));
-    CHECK_TRY(check_view(v, "v", dtype, r->batch, r->rows, n_kv_heads, head_dim, wide));
+    bool any = true;   // the copies take rows of every alignment
+    CHECK_TRY(check_view(k, "k", dtype, r->batch, r->rows, n_kv_heads, head_dim, any));
+    CHECK_TRY(check_view(v, "v", dtype, r->batch, r->rows, n_kv_heads, head_dim, any));
     const int64_t streams = r->batch * r->n_bands;
     if (streams == 0 || r->rows == 0) return NSGCQT_OK;
     const size_t e = elem_bytes(dtype);
