@@ -274,8 +274,9 @@ __device__ inline void zero_rows(const View& v, int64_t b, int head, int start, 
 
 // The same 32 rows in LDS of the wave's own, to be read as fragments when they
 // are needed: registers, and with them the waves on a SIMD, are what the
-// gradient kernels are short of (dq of 5 s clips: 890 us with three waves,
-// 1104 with two).
+// gradient kernels are short of (446,932 tokens, 8 heads of 64 over 2, window
+// 256, bfloat16: dq 1065 us with three waves, 1292 with two; the key gradient
+// 1044 and 1167).
 template <class T, int DP>
 __device__ inline void keep_rows(char* to, const T* p, bool there, int dim, bool wide, int lane) {
     frag<T> f[DP / 16];
@@ -310,11 +311,13 @@ struct QueryWork {
 // left: with one alone o is off by 0.0022 in the 2-norm in bfloat16, with two
 // by its own rounding, 0.0016. Sums take p unrounded.
 //
-// 131,072 tokens, 8 heads of 128 over 2, window 1024: 913 us (667 with p as
-// one number; 457 at the rate of a large product, of which p's second number
-// takes half as much again): the matrix cores wait for the exponentials (a
-// quarter of the vector rate) and the maxima. Tiles of 32 keys there, three
-// waves a SIMD.
+// 131,072 tokens, 8 heads of 128 over 2, window 1024: 850 us (667 with p as
+// one number), 648 TFLOP/s of visible pairs; 457 at the rate of a large
+// product, 685 with p's second number, which is half as many products again.
+// The matrix cores wait for the exponentials (a quarter of the vector rate),
+// the maxima and the rounding. Tiles of 32 keys there, three waves a SIMD.
+// 446,932 tokens in 221 bands, 8 heads of 64 over 2, window 256: 690 us (600
+// with p as one number), 232 for reading and writing at the rate of a large copy.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP > 64 ? 1 : WIDE ? 3 : 2) void k_attention(AttnArgs a) {
     constexpr int BN = key_tile<T, DP>(), RB = row_bytes<T, DP>();
@@ -492,9 +495,10 @@ template <class T, int DP, bool WIDE> constexpr int grad_waves(int large) {
 // shows in dq (two keys, bfloat16: 0.0034 in the 2-norm). So a workgroup in
 // which that sum passes a quarter of u of the row's sum of |ds| anywhere goes
 // through its keys once more with the corrected delta (0.0017). With random
-// scores that happens below some 30 keys and at a band's first tokens:
-// 446,932 tokens, forward and gradients, window of 2, everywhere: 1388 us;
-// window of 256, hardly anywhere: 4 % of the whole, for the sums of |ds|.
+// scores that happens below some 30 keys, at a band's first tokens and where
+// few are kept: 446,932 tokens, window of 256, one key in eight and a long
+// stretch dropped: 11 % of the workgroups, 1070 us instead of 970; window of 2,
+// everywhere: forward and gradients 1390 us instead of 1290.
 // Layout as k_attention: the scores and dp are formed transposed, so ds is the
 // B fragment of dq^T = K^T ds^T.
 template <class T> constexpr float kRest = std::is_same<T, _Float16>::value ? 0x1p-13f : 0x1p-10f;
@@ -731,9 +735,10 @@ __host__ __device__ inline int queries_end(int k0, int left, int len) {
 // ds are B fragments again. In 16 bits each goes into its product as two
 // numbers: with one, dk and dv are off by 0.0026 and 0.0023 in the 2-norm in
 // bfloat16, with two by their own rounding, 0.0016.
-// 446,932 tokens, 8 heads of 64 over 2, window 256, bfloat16: 800 us (dq 980,
-// far queries 180): 2.3 ms with the forward, 324 TFLOP/s of the formulas' work.
-// Bound by waiting: three waves a SIMD, half their cycles.
+// 446,932 tokens, 8 heads of 64 over 2, window 256, bfloat16: 1044 us (820 with
+// p and ds as one number; dq 1070, far queries 190): 2.8 ms with the forward,
+// 273 TFLOP/s of the formulas' work. Bound by waiting: three waves a SIMD,
+// half their cycles.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, (grad_waves<T, DP, WIDE>(1))) void k_attention_dkv(AttnArgs a) {
     constexpr int BQ = query_tile<T, DP>();

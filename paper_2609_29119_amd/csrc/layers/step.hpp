@@ -28,8 +28,10 @@ __device__ inline int ring_slot(int64_t t, int sinks, int window) {
 // fragments; V goes through a stretch of LDS of the wave's own to be turned.
 // In 16 bits p enters its product as two numbers, as in k_attention.
 // Bound by reading the cache: 3,536 streams of 260 slots, 8 heads of 64 over 2,
-// bfloat16: 107 us (4.1 TB/s, 90 at the rate of a large copy); 4 streams of
+// bfloat16: 103 us (4.3 TB/s, 90 at the rate of a large copy); 4 streams of
 // 131,076 slots of 128, float16: 100 us and 6.5 for the join (5.1 TB/s, 109).
+// WIDE: every view and the caches take 16-byte accesses (one kernel for both
+// spilled at heads above 64: 142 us on the long streams).
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     constexpr int RB = row_bytes<T, DP>(), kEach = 32 * DP / 8 / 64;
