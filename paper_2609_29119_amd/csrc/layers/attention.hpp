@@ -57,8 +57,11 @@ template <class T, int LAG> struct Base {
         if (!__any(far)) return false;
         float now = fmaxf(top, mx);
         if constexpr (kHalf) now = mx > -INFINITY ? fmaxf(mx, peak - kDeep * by.unit) : top;
-        factor = now == -INFINITY ? 1.f : exp2_((top - now) * by.c);
+        // the difference of the bases as the exponentials take them, rounded
+        const float before = of(by);
+        const bool first = top == -INFINITY;   // nothing was summed yet
         top = now;
+        factor = first ? 1.f : exp2_(before - of(by));
         return true;
     }
     // in powers of two: a key's probability is exp2(c score - of(c))

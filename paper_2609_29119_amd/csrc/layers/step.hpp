@@ -11,7 +11,7 @@ struct StepArgs {
     View q, k, v, o;           // batch stride: from stream to stream
     void *k_cache, *v_cache;   // [streams][kv_heads][slots][dim]
     const int64_t* pos;
-    float* part;               // [streams][heads][splits][dim + 2]: sum p v, maximum, sum p
+    float* part;               // [streams][heads][splits][dim + 2]: sum p v, base, sum p
     int64_t streams;
     int heads, kv_heads, dim, group, head_blocks, splits;
     int slots, sinks, window;
@@ -21,6 +21,9 @@ struct StepArgs {
 __device__ inline int ring_slot(int64_t t, int sinks, int window) {
     return static_cast<int>(t < sinks ? t : sinks + (t - sinks) % window);
 }
+
+// What a part whose base is `base` weighs beside one of base `all`, the largest (-inf: nothing was seen).
+__device__ inline float weight_of(float base, float all) { return base == -INFINITY ? 0.f : exp2_(base - all); }
 
 // A workgroup takes one stream, one kv head with up to 32 of its query heads
 // (the columns of S^T = K Q^T), and one of `splits` stretches of the slots;
@@ -134,12 +137,13 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
     // the four waves' results, in the waves' order
     sum = half_sum(sum);
     if (h == 0) {
-        tops[wave][m] = base.top;
+        tops[wave][m] = base.top == -INFINITY ? -INFINITY : base.of(a.by);
         sums[wave][m] = sum;
     }
     __syncthreads();
+    // weights are differences of the bases as the exponentials took them
     const float all = fmaxf(fmaxf(tops[0][m], tops[1][m]), fmaxf(tops[2][m], tops[3][m]));
-    const float share = exp2_(fmaf(base.top, a.by.c, all == -INFINITY ? 0.f : -all * a.by.c));
+    const float share = weight_of(tops[wave][m], all);
     for (int v = 0; v < 4; ++v) {
         if (wave == v) {
 #pragma unroll
@@ -156,10 +160,9 @@ __global__ __launch_bounds__(256, 2) void k_step(StepArgs a) {
         const int hd = x / a.dim, d = x - hd * a.dim;
         const int head = kv * a.group + h_first + hd;
         const float am = fmaxf(fmaxf(tops[0][hd], tops[1][hd]), fmaxf(tops[2][hd], tops[3][hd]));
-        const float bm = am == -INFINITY ? 0.f : am * a.by.c;
         float total = 0.f;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) total += sums[v][hd] * exp2_(fmaf(tops[v][hd], a.by.c, -bm));
+        for (int v = 0; v < 4; ++v) total += sums[v][hd] * weight_of(tops[v][hd], am);
         const float val = joined[d][hd];
         if (a.splits == 1) {
             reinterpret_cast<T*>(a.o.data)[stream * a.o.batch + head * a.o.head + d] =
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(256) void k_step_join(StepArgs a) {
     if (lane == 0) tops[wave] = top;
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float base = top == -INFINITY ? 0.f : top * a.by.c, w = exp2_(fmaf(mine, a.by.c, -base));
+    const float w = weight_of(mine, top);
     weight[tid] = w;
     float total = there ? p[tid * stride + a.dim + 1] * w : 0.f;
 #pragma unroll

@@ -1036,3 +1036,29 @@ def test_cache_fill_holds_what_steps_would(d, dtype):
                     want[b * 4 + g, :, slot] = x[b, at + t]
                 at += n
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rescaling_uses_the_bases_as_rounded(dtype):
+    """Large scores (exact ones here) whose level changes by many powers of two every 32 keys: what was summed before
+    is rescaled by the difference of the bases as the exponentials used them, so that their rounding (2^-13 at scores
+    of 1000) does not add up from block to block. 16-bit results round once (the bound is of a mean: 1,024 values, of
+    which a few lie at a tie and may round the other way); in 32 bits sums of 6,400 terms remain."""
+    n, h, d = 6400, 8, 128
+    level = torch.randint(-160, 1, (n // 32,), generator=torch.Generator().manual_seed(3)).double() / 8 - 0.125
+    q, k = torch.zeros(1, n, h, d, dtype=dtype), torch.zeros(1, n, h, d, dtype=dtype)
+    q[..., 0], k[..., 0] = 32.0, 32.0                       # 1024
+    q[..., 1], k[..., 1] = 1.0, level.repeat_interleave(32)[None, :, None].to(dtype)
+    q, k, v = q.cuda(), k.cuda(), randn(1, 1, n, h, d, dtype=dtype)
+    p = (k[0, :, 0, 1].double().cpu()).softmax(0)
+    want = torch.einsum("n,nhd->hd", p, v[0].double().cpu())
+    eps = 2.0 ** -24 * 6400 ** 0.5 if dtype == torch.float32 else ATTENTION_EPS[dtype]
+    kc, vc = k.transpose(1, 2).contiguous(), v.transpose(1, 2).contiguous()
+    got = [layers.band_attention(q, k, v, offsets_of([n]), None, None, scale=1.0)[0, 0]]
+    pos = torch.full((1,), n - 1, dtype=torch.int64, device="cuda")
+    got.append(layers.attention_step(q[:, 0], k[:, -1], v[:, -1], kc, vc, pos, scale=1.0)[0])
+    for o in got:
+        if dtype == torch.float32:
+            assert ((o.double().cpu() - want).norm() / want.norm()).item() <= 2 * eps
+        else:
+            beyond_rounding(o, want, eps, "o")
