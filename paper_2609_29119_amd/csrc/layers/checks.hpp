@@ -42,12 +42,12 @@ inline int check_view(const nsgcqt_view* v, const char* name, int dtype, int64_t
     const int e = elem_bytes(dtype);
     if (!v->data) return set_err(NSGCQT_EINVAL, std::string(name) + " has a NULL pointer");
     if (misaligned(v->data, e)) return set_err(NSGCQT_EINVAL, std::string(name) + " is not aligned to its element");
-    if (v->batch < 0 || v->row < 0 || v->head < 0)
+    // the stride of an axis of one element is not read
+    if ((batch > 1 && v->batch < 0) || (rows > 1 && v->row < 0) || (heads > 1 && v->head < 0))
         return set_err(NSGCQT_EINVAL, std::string(name) + " has a negative stride");
     const int64_t step = 16 / e;
-    if (misaligned(v->data, 16) || width % 8 || (batch > 1 && v->batch % step) || (rows > 1 && v->row % step) ||
-        (heads > 1 && v->head % step) || v->row * e >= (int64_t(1) << 23) ||
-        (rows > 1 && v->row < width))
+    if (misaligned(v->data, 16) || width % 8 || (batch > 1 && v->batch % step) || (heads > 1 && v->head % step) ||
+        (rows > 1 && (v->row % step || v->row >= (int64_t(1) << 23) / e || v->row < width)))
         wide = false;
     return NSGCQT_OK;
 }

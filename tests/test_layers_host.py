@@ -246,3 +246,16 @@ def test_gradient_workspace_with_many_sinks(L):
     """The partial sums of the sinks are bounded: 131,072 tokens, every one a sink, 2 kv heads of 128."""
     s, r = shape(heads=8, kv=2, dim=128, left=1023, sinks=131072), rows(bands=1, n=131072)
     assert L.nsgcqt_band_attention_workspace(ref(r), ref(s)) <= 4 * 131072 * 8 + 2 * (2 * 2 * 131072 * 2 * 128) * 1.05
+
+
+def test_strides_of_axes_of_one_element_are_not_read(L):
+    """What is not read may hold anything: both calls below are refused for their workspace, later than for strides."""
+    v = view(row=-(1 << 62))
+    refused(L.nsgcqt_attention_step(0, 2, 2, 1, 8, 100000, 0, 1.0, *[ref(v)] * 4, FAKE, FAKE, FAKE, FAKE, 16, None),
+            nb.EWORKSPACE, "required")
+    v = view(batch=-3, head=-5)
+    refused(L.nsgcqt_band_linear_grad_weight(0, ref(rows(batch=1)), ref(v), ref(v), FAKE, None, 8, 8, FAKE, 16, None),
+            nb.EWORKSPACE, "required")
+    v = view(batch=-3)
+    refused(L.nsgcqt_band_linear_grad_weight(0, ref(rows(batch=2)), ref(v), ref(v), FAKE, None, 8, 8, FAKE, 16, None),
+            nb.EINVAL, "negative stride")
