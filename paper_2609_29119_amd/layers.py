@@ -162,21 +162,20 @@ def _trains(*tensors):
         for t in tensors:
             if t is not None and t.requires_grad:
                 return True
-    if _dual_level() >= 0:
+    if getattr(forward_ad, "_current_level", 0) >= 0:   # (-1: no forward-mode level is open)
         for t in tensors:
             if t is not None and forward_ad.unpack_dual(t).tangent is not None:
                 return True
     return False
 
 
-def _dual_level():
-    return getattr(forward_ad, "_current_level", 0)   # -1: no forward-mode level is open
+_increment = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
 
 
 def _written(*tensors):
     """Tells autograd that a kernel wrote to these: a graph that saved one
     then refuses to run backward with the new values."""
-    torch.autograd.graph.increment_version(tensors)
+    _increment(tensors)
 
 
 def _last(t):
