@@ -12,6 +12,9 @@
  *                           and first tokens that stay visible (sinks)
  *   nsgcqt_attention_step   the same attention for one new token of each of
  *                           many streams, over a ring cache; _cache_fill
+ *   nsgcqt_decay_attention* linear attention along each band with a decay for
+ *                           each head, from and into a state
+ *   nsgcqt_decay_step       the same for one new token of each of many streams
  *
  * Conventions
  *   - Data are float32, float16 or bfloat16 (nsgcqt_dtype), one type a call.
@@ -176,6 +179,50 @@ int64_t nsgcqt_attention_step_workspace(int64_t n_streams, int64_t n_heads, int6
 int nsgcqt_cache_fill(int dtype, const nsgcqt_rows* r, int64_t n_kv_heads, int64_t head_dim, int64_t window,
                       int64_t sinks, const nsgcqt_view* k, const nsgcqt_view* v, void* k_cache, void* v_cache,
                       void* stream);
+
+/* Shape of a decayed linear attention. Head h of q and o reads key head
+ * n = h / (n_heads / n_kv_heads) of k and v, whose decay is
+ * exp(log_decay[n]); with keep not NULL, tokens with keep[b][j] = 0 add
+ * nothing (what k and v hold there is never used), but count as distance. */
+typedef struct {
+    int64_t n_heads, n_kv_heads;   /* n_kv_heads divides n_heads */
+    int64_t head_dim;              /* 1 .. 128 */
+    double scale;                  /* of the results, finite */
+    const float* log_decay;        /* device, [n_kv_heads]; a decay of at most 1, log_decay <= 0, is meant */
+    const uint8_t* keep;           /* device, [batch][rows] with batch stride keep_batch, or NULL */
+    int64_t keep_batch;
+} nsgcqt_decay_shape;
+
+/* o_t = scale (decay^(t + 1) q_t S + sum over tokens s <= t of the band of
+ * decay^(t - s) (q_t . k_s) v_s), t counted within the band. S is state
+ * [batch * n_bands][n_kv_heads][head_dim][head_dim] float32, contiguous, stream
+ * b n_bands + g that of band g of signal b; the call leaves in its place
+ * decay^len S + sum_s decay^(len - 1 - s) k_s v_s^T (of a band without tokens:
+ * S itself). state NULL: S = 0. q, o: [batch][rows][n_heads][head_dim]; k, v
+ * with n_kv_heads. Sums whose terms pass 16 bits enter the products of 16-bit
+ * data as two numbers of 8 bits, those of the state as three; an infinity or
+ * NaN may, with weight zero, reach the 31 tokens before it, and come out as NaN. */
+int nsgcqt_decay_attention(int dtype, const nsgcqt_rows* r, const nsgcqt_decay_shape* s, const nsgcqt_view* q,
+                           const nsgcqt_view* k, const nsgcqt_view* v, const nsgcqt_view* o, float* state, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* dq, dk, dv of a loss with gradient d_o at o, for state NULL. */
+int nsgcqt_decay_attention_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_decay_shape* s, const nsgcqt_view* q,
+                                const nsgcqt_view* k, const nsgcqt_view* v, const nsgcqt_view* d_o,
+                                const nsgcqt_view* dq, const nsgcqt_view* dk, const nsgcqt_view* dv, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/* Workspace bytes of nsgcqt_decay_attention (grad 0) or its gradient, or a negative status. */
+int64_t nsgcqt_decay_attention_workspace(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, int grad);
+
+/* One new token of each of n_streams streams: S <- decay S + k v^T,
+ * o = scale q S, with S in state [n_streams][n_kv_heads][head_dim][head_dim]
+ * float32, contiguous. pos[s] (device int64) above 0: the stream goes on; 0: it
+ * begins, what its state holds is not used; below 0: it has no token, its
+ * state stays as it is and its row is zero. Views as in nsgcqt_attention_step. */
+int nsgcqt_decay_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, double scale,
+                      const nsgcqt_view* q, const nsgcqt_view* k, const nsgcqt_view* v, const nsgcqt_view* o,
+                      float* state, const int64_t* pos, const float* log_decay, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,548 @@
+// Linear attention along the bands with a decay for each head, and its step.
+//
+//   o_t = sum over s <= t of g^(t - s) (q_t . k_s) v_s        (times scale)
+//
+// Forward and gradients are one operator with its arguments in other places:
+//   W(a, b, c)_t = sum_{s <= t} g^(t - s) (a_t . b_s) c_s     W' the same over s >= t
+//   o = W(q, k, v)   dq = W(do, v, k)   dk = sum_heads W'(v, do, q)   dv = sum_heads W'(k, q, do)
+// and W' is W with a band's tokens numbered from its end.
+//
+// In tiles of 32 tokens, with S = sum of g^(first - 1 - s) b_s c_s^T over the tokens before the tile:
+//   out_i = g^(i + 1) a_i S + sum_{j <= i} g^(i - j) (a_i . b_j) c_j
+//   S <- g^32 S + sum_j g^(31 - j) b_j c_j^T
+// Every power's exponent is a distance: nothing grows, however fast a head forgets.
+#pragma once
+#include "tile.hpp"
+
+namespace nsl {
+
+constexpr int kDecayTile = 32;
+
+// One sum W or W' of a launch. Result head h belongs to key head h / per and
+// takes the sources (key head) * many + {0 .. many - 1}.
+struct DecayJob {
+    View a, b, c, out;
+    float* part;         // states of segments of long bands, [batch][slots][kv_heads][dim][dim]
+    int heads, per, many;
+    bool reverse;        // W'
+    bool turned;         // the states are those of the job with b and c exchanged
+    bool keep_result;    // keep takes out results (else sources)
+};
+
+struct DecayArgs {
+    DecayJob job[3];
+    const float* log_decay;   // [kv_heads]
+    float* state;             // [batch * n_bands][kv_heads][dim][dim] or NULL
+    const uint8_t* keep;
+    int64_t keep_batch;
+    const int64_t* off;
+    int rows, n_bands, kv_heads, dim;
+    int units;                // result heads of all jobs
+    int shift;                // of a segment's length
+    unsigned items;           // work items of a signal
+    int64_t first_block;      // of a launch of k_decay_scan
+    bool single;              // k_decay_sum: bands of one segment, into `state`
+    float scale;
+};
+
+template <class T> __device__ inline T* decay_row(const View& v, int64_t b, int64_t row, int head) {
+    return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row + head * v.head;
+}
+
+// The states of segments of bands of several segments have slots of their
+// own: a band of more than T tokens that starts at token `start` has those
+// from floor(2 start / T) on, of which its ceil(len / T) segments do not reach
+// the next such band's.
+inline __host__ __device__ int64_t decay_slots(int64_t rows, int shift) { return ((2 * rows) >> shift) + 1; }
+inline __host__ __device__ int64_t decay_slot(int64_t start, int64_t segment, int shift) {
+    return ((2 * start) >> shift) + segment;
+}
+
+// decay^n of a head, l2 the decay's base-2 logarithm. The product is formed in
+// 64 bits and only its fraction enters the exponential: the power is right to
+// the last bits of 32 however long the distance.
+__device__ inline float decay_power(double l2, int64_t n) {
+    if (n == 0) return 1.f;
+    const double x = fmin(fmax(l2 * static_cast<double>(n), -400.0), 400.0);
+    if (l2 != l2) return __builtin_nanf("");
+    const double whole = floor(x);
+    return ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), static_cast<int>(whole));
+}
+
+// A fragment as a sum of fragments of the matrix cores' type, the largest
+// first. bfloat16 and float32 data are one piece, float16 data (whose range
+// the sums would leave) two of bfloat16, without loss; 32-bit values that meet
+// 16-bit data are N pieces of bfloat16, 8 bits each. Products leave out what
+// is below the last piece's rounding.
+template <class F, int N> struct Pieces { F p[N]; };
+template <class T> constexpr int data_pieces() { return std::is_same<T, _Float16>::value ? 2 : 1; }
+template <class T> using piece = std::conditional_t<std::is_same<T, float>::value, f8, b8>;
+
+template <int N> __device__ inline Pieces<b8, N> cut(f8 x) {
+    Pieces<b8, N> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            r.p[i][j] = static_cast<__bf16>(x[j]);
+            x[j] -= static_cast<float>(r.p[i][j]);
+        }
+    }
+    return r;
+}
+__device__ inline f8 wide_of(f8 f) { return f; }
+template <class F> __device__ inline f8 wide_of(F f) {
+    f8 x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = static_cast<float>(f[j]);
+    return x;
+}
+__device__ inline Pieces<f8, 1> data_of(f8 f) { return {{f}}; }
+__device__ inline Pieces<b8, 1> data_of(b8 f) { return {{f}}; }
+__device__ inline Pieces<b8, 2> data_of(h8 f) { return cut<2>(wide_of(f)); }
+template <class T, int N> __device__ inline auto sum_of(f8 x) {
+    if constexpr (sizeof(T) == 4)
+        return Pieces<f8, 1>{{x}};
+    else
+        return cut<N>(x);
+}
+
+template <class F, int NA, int NB>
+__device__ inline acc16 product(const Pieces<F, NA>& a, const Pieces<F, NB>& b, acc16 c) {
+    constexpr int kLast = NA > NB ? NA : NB;
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (i + j < kLast) c = mma(a.p[i], b.p[j], c);
+    return c;
+}
+
+__device__ inline f8 octet(const acc16& c, int s) {
+    f8 x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = c[8 * s + j];
+    return x;
+}
+
+// As read_turned, with bits 2 and 3 of the column's number exchanged: a
+// product's result whose rows are these columns then holds, in registers
+// 8 s .. 8 s + 7 of a lane, the columns 16 s + 8 h + {0 .. 7}, which is the
+// order in which `load8` holds a reduction's steps. So a state whose rows are
+// b's columns is a fragment for the product with a as it is loaded.
+template <class T, int RB> __device__ inline frag<T> read_turned_state(const char* tile, int row0, int col0, int lane) {
+    const int h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        const int l16 = lane & 15, row = row0 + 4 * h + (l16 >> 2);
+        const int c = ((col0 + (lane & 16)) >> 3) + (l16 & 1), at = (l16 & 2) << 2;
+        const char* a = tile + row * RB + ((c ^ turn(row)) << 4) + at;
+        const char* b = tile + (row + 8) * RB + ((c ^ turn(row + 8)) << 4) + at;
+        const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)a);
+        const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)b);
+        const s8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(frag<T>, z);
+    } else {
+        const int m = lane & 31, col = col0 + ((m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1));
+        frag<T> f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = row0 + 4 * h + (j & 3) + 8 * (j >> 2);
+            f[j] = *reinterpret_cast<const T*>(tile + row * RB + (((col >> 2) ^ turn(row)) << 4) + ((col & 3) << 2));
+        }
+        return f;
+    }
+}
+
+// What a workgroup of either kernel works on.
+struct DecayPlace {
+    int job, head, kv;
+    int64_t b;
+    Tile<int> seg;
+    int n;          // the segment's tokens
+    bool outside;   // tokens that no band holds
+    bool several;   // the band has more than one segment
+    __device__ DecayPlace(const DecayArgs& a, int lane) {
+        const unsigned id = die_order(blockIdx.x, gridDim.x), rest = id / a.units;
+        head = static_cast<int>(id - rest * a.units);
+        job = 0;
+        while (head >= a.job[job].heads) head -= a.job[job++].heads;
+        kv = head / a.job[job].per;
+        b = rest / a.items;
+        seg = find_tile<int>(a.off, a.n_bands, a.rows, 1, a.shift, static_cast<int>(rest % a.items), lane);
+        n = min(seg.len - seg.first, 1 << a.shift);
+        outside = seg.band < 0 || seg.band >= a.n_bands;
+        several = seg.len > 1 << a.shift;
+    }
+    __device__ int64_t token(int t, bool reverse) const {   // the row's token of the segment's t-th
+        return seg.start + (reverse ? seg.len - 1 - seg.first - t : seg.first + t);
+    }
+};
+
+// 32 tokens of b and c of one head, as registers on their way to LDS: 2 chunks of a thread each.
+template <class T, int DP, bool WIDE> struct DecaySources {
+    static constexpr int kThreads = 2 * DP, RB = row_bytes<T, DP>();
+    frag<T> fb[2], fc[2];
+    __device__ void fetch(const DecayArgs& a, const DecayJob& j, const DecayPlace& p, int t0, int head, int tid) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = tid + kThreads * e, t = t0 + c / (DP / 8), d = c % (DP / 8) * 8;
+            bool there = t < p.n;
+            const int64_t row = p.token(there ? t : 0, j.reverse);
+            if (a.keep && !j.keep_result) there = there && a.keep[p.b * a.keep_batch + row];
+            const int n = there ? a.dim - d : 0;
+            fb[e] = load8<T, WIDE>(decay_row<T>(j.b, p.b, row, head) + d, n, d > 0);
+            fc[e] = load8<T, WIDE>(decay_row<T>(j.c, p.b, row, head) + d, n, d > 0);
+        }
+    }
+    __device__ void put(char* tb, char* tc, int tid) const {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = tid + kThreads * e;
+            write8<T, RB>(tb, c / (DP / 8), c % (DP / 8), fb[e]);
+            write8<T, RB>(tc, c / (DP / 8), c % (DP / 8), fc[e]);
+        }
+    }
+};
+
+// S += b^T (w c): the wave's 32 columns of c, N pieces of w c.
+template <class T, int DP, int N>
+__device__ inline void decay_add(acc16 (&s)[DP / 32], const char* tb, frag<T> cf, f8 w, int step, int lane) {
+    const auto cw = sum_of<T, N>(wide_of(cf) * w);
+    each<DP / 32>([&](auto d) __attribute__((always_inline)) {
+        const auto bf = data_of(read_turned_state<T, row_bytes<T, DP>()>(tb, 16 * step, 32 * d.value, lane));
+        s[d.value] = product(bf, cw, s[d.value]);
+    });
+}
+
+// 8 weights decay^(last - token), for the tokens of reduction step `step` in read_turned's order.
+__device__ inline f8 decay_weights(const float* power, int last, int step, int h) {
+    f8 w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = power[max(last - (16 * step + 4 * h + (j & 3) + 8 * (j >> 2)), 0)];
+    return w;
+}
+
+// The state that a segment starts with, or the place of one: element [d][e] of the job's own order.
+__device__ inline float* decay_state_of(const DecayArgs& a, const DecayJob& j, const DecayPlace& p, bool& there) {
+    const int64_t size = static_cast<int64_t>(a.dim) * a.dim;
+    there = true;
+    if (p.several)
+        return j.part + ((p.b * decay_slots(a.rows, a.shift) + decay_slot(p.seg.start, p.seg.first >> a.shift, a.shift)) *
+                             a.kv_heads + p.kv) * size;
+    if (a.state) return a.state + ((p.b * a.n_bands + p.seg.band) * a.kv_heads + p.kv) * size;
+    there = false;
+    return nullptr;
+}
+
+// out of one segment of one result head. The workgroup's waves hold 32 columns
+// of the state each, in registers for the whole segment; the score tile, which
+// all of them need, is formed by each (8 of 44 products at heads of 128). All
+// products are formed transposed, so that the scores, the state and the result
+// go from one to the next without a trip through LDS; only b and c do, to be
+// turned.
+template <class T, int DP, bool WIDE>
+__global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
+    constexpr int RB = row_bytes<T, DP>(), ND = DP / 32, NK = DP / 16;
+    constexpr bool kHold = sizeof(T) == 2 || DP <= 64;   // a's fragments stay in registers between their two uses
+    constexpr bool kEarly = kHold || DP <= 96 || WIDE;   // the next sources are on their way while these are computed
+    __shared__ __align__(128) char tiles[2][2][kDecayTile * RB];
+    __shared__ float power[kDecayTile + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
+    const DecayPlace p(a, lane);
+    if (!p.seg.live) return;
+    const DecayJob& j = a.job[p.job];
+    if (p.outside) {
+        for (int t = m; t < p.n; t += 32)
+            store_column<T>(decay_row<T>(j.out, p.b, p.token(t, j.reverse), p.head), zero16(), 32 * wave, a.dim, WIDE, lane);
+        return;
+    }
+    DecaySources<T, DP, WIDE> next;
+    next.fetch(a, j, p, 0, p.kv * j.many, tid);
+    frag<T> af[kHold ? NK : 1];
+    const T* ap;      // this lane's row of a, and whether it is there and kept
+    bool mine, kept;
+    auto a_row = [&](int t0) {
+        mine = t0 + m < p.n;
+        const int64_t row = p.token(mine ? t0 + m : 0, j.reverse);
+        kept = mine && !(a.keep && j.keep_result && !a.keep[p.b * a.keep_batch + row]);
+        ap = decay_row<T>(j.a, p.b, row, p.head);
+    };
+    auto a_at = [&](int x) {
+        return load8<T, WIDE>(ap + 16 * x + 8 * h, kept ? a.dim - 16 * x - 8 * h : 0, x + h > 0);
+    };
+    auto fetch_a = [&]() {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int x = 0; x < NK; ++x) af[x] = a_at(x);
+        }
+    };
+    a_row(0);
+    fetch_a();
+    const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
+    if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
+    acc16 s[ND];
+    bool some;    // there is a state
+    const float* from = decay_state_of(a, j, p, some);
+    const int col = 32 * wave + m;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) s[d] = zero16();
+    if (some) {
+        const int64_t sd = j.turned ? 1 : a.dim, sc = j.turned ? a.dim : 1;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = 32 * d + 16 * (r >> 3) + 8 * h + (r & 7);
+                if (row < a.dim && col < a.dim) s[d][r] = from[row * sd + col * sc];
+            }
+    }
+    next.put(tiles[0][0], tiles[0][1], tid);
+    __syncthreads();
+    float fade[16];   // decay^(i - j) where j <= i
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int lag = m - (8 * (r >> 2) + 4 * h + (r & 3));
+        fade[r] = lag < 0 ? 0.f : power[lag];
+    }
+    const float up = power[m + 1], across = power[kDecayTile];
+    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
+    acc16 out;
+    int tile = 0, g = 0;
+    for (int stage = 0; stage < stages; ++stage) {
+        const bool more = stage + 1 < stages, end = g + 1 == j.many, last = tile + 1 == count;
+        const char *tb = tiles[stage & 1][0], *tc = tiles[stage & 1][1];
+        const int next_t = kDecayTile * (end ? tile + 1 : tile), next_head = p.kv * j.many + (end ? 0 : g + 1);
+        if (kEarly && more) next.fetch(a, j, p, next_t, next_head, tid);
+        if (g == 0) {
+            out = zero16();
+            if (some) {
+                each<NK>([&](auto x) __attribute__((always_inline)) {
+                    const auto af_x = data_of(kHold ? af[kHold ? x.value : 0] : a_at(x.value));
+                    out = product(sum_of<T, 2>(octet(s[x.value / 2], x.value % 2)), af_x, out);
+                });
+                out *= up;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) s[d] *= across;
+            }
+        }
+        acc16 q = zero16();
+        each<NK>([&](auto x) __attribute__((always_inline)) {
+            const frag<T> af_x = kHold ? af[kHold ? x.value : 0] : a_at(x.value);
+            q = mma(read8<T, RB>(tb, m, 2 * x.value + h), af_x, q);
+        });
+        T* to = mine ? decay_row<T>(j.out, p.b, p.token(kDecayTile * tile + m, j.reverse), p.head) : nullptr;
+        const bool drop = mine && !kept;
+        if (end && !last) {
+            a_row(kDecayTile * (tile + 1));
+            fetch_a();
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) q[r] *= fade[r];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const frag<T> cf = read_turned<T, RB>(tc, 16 * x, 32 * wave, lane);
+            out = product(data_of(cf), sum_of<T, 2>(octet(q, x)), out);
+            if (!last) decay_add<T, DP, 2>(s, tb, cf, decay_weights(power, kDecayTile - 1, x, h), x, lane);
+        }
+        if (end) {
+            out *= a.scale;
+            if (drop) out = zero16();
+            store_column<T>(to, out, 32 * wave, a.dim, WIDE, lane);
+            some = true;
+            g = 0;
+            ++tile;
+        } else {
+            ++g;
+        }
+        if (!kEarly && more) next.fetch(a, j, p, next_t, next_head, tid);
+        if (more) next.put(tiles[(stage + 1) & 1][0], tiles[(stage + 1) & 1][1], tid);
+        __syncthreads();
+    }
+}
+
+// What a segment adds to the state, sum_s g^(n - 1 - s) b_s c_s^T, into its
+// slot: for bands of several segments (the last one's only where a state is
+// kept). single: bands of one segment, whose state in `state` goes on. Three
+// pieces of w c: the states are 32-bit results.
+template <class T, int DP, bool WIDE>
+__global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
+    constexpr int RB = row_bytes<T, DP>(), ND = DP / 32;
+    __shared__ __align__(128) char tiles[2][2][kDecayTile * RB];
+    __shared__ float power[kDecayTile + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
+    const DecayPlace p(a, lane);
+    if (!p.seg.live || p.outside || p.several == a.single) return;
+    const DecayJob& j = a.job[p.job];
+    if (!a.state && p.seg.first + p.n == p.seg.len) return;
+    DecaySources<T, DP, WIDE> next;
+    next.fetch(a, j, p, 0, p.kv * j.many, tid);
+    const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
+    if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
+    bool there;
+    float* to = decay_state_of(a, j, p, there);
+    const int col = 32 * wave + m;
+    acc16 s[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = 32 * d + 16 * (r >> 3) + 8 * h + (r & 7);
+            s[d][r] = a.single && row < a.dim && col < a.dim ? to[row * a.dim + col] : 0.f;
+        }
+    next.put(tiles[0][0], tiles[0][1], tid);
+    __syncthreads();
+    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
+    int tile = 0, g = 0;
+    for (int stage = 0; stage < stages; ++stage) {
+        const bool more = stage + 1 < stages, end = g + 1 == j.many;
+        const char *tb = tiles[stage & 1][0], *tc = tiles[stage & 1][1];
+        const int n = min(p.n - kDecayTile * tile, kDecayTile);
+        if (more) next.fetch(a, j, p, kDecayTile * (end ? tile + 1 : tile), p.kv * j.many + (end ? 0 : g + 1), tid);
+        if (g == 0) {
+            const float across = power[n];
+#pragma unroll
+            for (int d = 0; d < ND; ++d) s[d] *= across;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            decay_add<T, DP, 3>(s, tb, read_turned<T, RB>(tc, 16 * x, 32 * wave, lane),
+                                decay_weights(power, n - 1, x, h), x, lane);
+        if (end) {
+            g = 0;
+            ++tile;
+        } else {
+            ++g;
+        }
+        if (more) next.put(tiles[(stage + 1) & 1][0], tiles[(stage + 1) & 1][1], tid);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = 32 * d + 16 * (r >> 3) + 8 * h + (r & 7);
+            if (row < a.dim && col < a.dim) to[row * a.dim + col] = s[d][r];
+        }
+}
+
+// From what each segment adds to the state that each starts with, in place,
+// along the segments of every band of several; `state` goes to the band's end.
+// A thread takes one element.
+__global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
+    const int size = a.dim * a.dim, parts = (size + 255) / 256;
+    int64_t id = a.first_block + blockIdx.x;
+    const int e = static_cast<int>(id % parts) * 256 + static_cast<int>(threadIdx.x);
+    id /= parts;
+    const int u = static_cast<int>(id % a.units), job = u / a.kv_heads, kv = u % a.kv_heads;
+    id /= a.units;
+    const int band = static_cast<int>(id % a.n_bands);
+    const int64_t b = id / a.n_bands;
+    const int start = band_bound(a.off, a.n_bands, a.rows, band + 1), len = band_bound(a.off, a.n_bands, a.rows, band + 2) - start;
+    if (len <= 1 << a.shift || e >= size) return;
+    const double l2 = static_cast<double>(a.log_decay[kv]) * 1.4426950408889634;
+    const float across = decay_power(l2, int64_t(1) << a.shift);
+    const int count = (len + (1 << a.shift) - 1) >> a.shift;
+    const int64_t step = static_cast<int64_t>(a.kv_heads) * size;
+    float* x = a.job[job].part + ((b * decay_slots(a.rows, a.shift) + decay_slot(start, 0, a.shift)) * a.kv_heads + kv) * size + e;
+    float* st = a.state ? a.state + ((b * a.n_bands + band) * a.kv_heads + kv) * size + e : nullptr;
+    float s = st ? *st : 0.f;
+    constexpr int kAhead = 16;
+    for (int i = 0; i + 1 < count; i += kAhead) {
+        float add[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) add[k] = i + k + 1 < count ? x[(i + k) * step] : 0.f;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k + 1 < count) {
+                x[(i + k) * step] = s;
+                s = fmaf(across, s, add[k]);
+            }
+    }
+    const float add = st ? x[(count - 1) * step] : 0.f;
+    x[(count - 1) * step] = s;
+    if (st) *st = fmaf(decay_power(l2, len - (static_cast<int64_t>(count - 1) << a.shift)), s, add);
+}
+
+// ------------------------------------------------------------- single tokens
+
+struct DecayStepArgs {
+    View q, k, v, o;   // batch stride: from stream to stream
+    float* state;      // [streams][kv_heads][dim][dim]
+    const int64_t* pos;
+    const float* log_decay;
+    int heads, kv_heads, dim, group;
+    float scale;
+};
+
+// S <- g S + k v^T, o = scale q S for the query heads of one key head of one
+// stream. A thread holds V neighbouring columns of every kRows-th row of the
+// state in registers; the rows' sums meet in LDS.
+template <class T, int DP, int V>
+__global__ __launch_bounds__(256) void k_decay_step(DecayStepArgs a) {
+    constexpr int kCols = DP / V, kRows = 256 / kCols, kEach = DP / kRows, kHeads = 4;
+    __shared__ float sums[kHeads][kRows][DP + 4];
+    __shared__ float ks[DP], qs[kHeads][DP];
+    typedef float vec __attribute__((ext_vector_type(V)));
+    const int tid = threadIdx.x, c0 = tid % kCols * V, r0 = tid / kCols;
+    const int64_t stream = blockIdx.x / a.kv_heads;
+    const int kv = static_cast<int>(blockIdx.x % a.kv_heads);
+    const int64_t pos = a.pos[stream];
+    auto q_of = [&](int g) { return reinterpret_cast<const T*>(a.q.data) + stream * a.q.batch + static_cast<int64_t>(kv * a.group + g) * a.q.head; };
+    auto o_of = [&](int g) { return reinterpret_cast<T*>(a.o.data) + stream * a.o.batch + static_cast<int64_t>(kv * a.group + g) * a.o.head; };
+    if (pos < 0) {
+        for (int e = tid; e < a.group * a.dim; e += 256) o_of(e / a.dim)[e % a.dim] = static_cast<T>(0.f);
+        return;
+    }
+    const T* kp = reinterpret_cast<const T*>(a.k.data) + stream * a.k.batch + kv * a.k.head;
+    const T* vp = reinterpret_cast<const T*>(a.v.data) + stream * a.v.batch + kv * a.v.head;
+    float* st = a.state + static_cast<int64_t>(blockIdx.x) * a.dim * a.dim;
+    vec s[kEach], v = 0.f;
+    if (pos > 0) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int r = r0 + kRows * i;
+            s[i] = r < a.dim && c0 < a.dim ? *reinterpret_cast<const vec*>(st + r * a.dim + c0) : vec(0.f);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) s[i] = 0.f;
+    }
+    if (c0 < a.dim)
+#pragma unroll
+        for (int x = 0; x < V; ++x) v[x] = static_cast<float>(vp[c0 + x]);
+    const float fade = decay_power(static_cast<double>(a.log_decay[kv]) * 1.4426950408889634, 1);
+    if (tid < DP) ks[tid] = tid < a.dim ? static_cast<float>(kp[tid]) : 0.f;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = r0 + kRows * i;
+        const float kr = ks[r];
+#pragma unroll
+        for (int x = 0; x < V; ++x) s[i][x] = fmaf(pos > 0 ? fade : 0.f, s[i][x], kr * v[x]);
+        if (r < a.dim && c0 < a.dim) *reinterpret_cast<vec*>(st + r * a.dim + c0) = s[i];
+    }
+    for (int g0 = 0; g0 < a.group; g0 += kHeads) {
+        const int n = min(a.group - g0, kHeads);
+        __syncthreads();
+        for (int e = tid; e < n * DP; e += 256)
+            qs[e / DP][e % DP] = e % DP < a.dim ? static_cast<float>(q_of(g0 + e / DP)[e % DP]) : 0.f;
+        __syncthreads();
+        for (int g = 0; g < n; ++g) {
+            vec sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) sum += s[i] * qs[g][r0 + kRows * i];
+#pragma unroll
+            for (int x = 0; x < V; ++x) sums[g][r0][c0 + x] = sum[x];
+        }
+        __syncthreads();
+        for (int e = tid; e < n * DP; e += 256) {
+            const int g = e / DP, c = e % DP;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) sum += sums[g][r][c];
+            if (c < a.dim) o_of(g0 + g)[c] = static_cast<T>(sum * a.scale);
+        }
+    }
+}
+
+}  // namespace nsl

@@ -12,8 +12,12 @@ include/nsgcqt_layers.h:
   attention_step   the same attention for one new token of each of many
                    streams, over a ring cache; `cache_fill` starts the caches,
                    `StreamCache` holds them
+  decay_attention  linear attention along each band, whose past decays at a
+                   rate of each head's own; from and into a state
+  decay_step       the same for one new token of each of many streams;
+                   `DecayState` holds the streams' states
 
-The first three are differentiable. Data are float32, float16 or bfloat16
+All but the steps and fills are differentiable. Data are float32, float16 or bfloat16
 CUDA tensors, one type a call; the last axis has to be contiguous, other
 strides are free. Calls run on the current stream.
 """
@@ -39,7 +43,8 @@ EXPORTS = [
     "nsgcqt_band_linear", "nsgcqt_band_linear_grad_input", "nsgcqt_band_linear_grad_weight",
     "nsgcqt_band_linear_workspace", "nsgcqt_rotary", "nsgcqt_band_attention", "nsgcqt_band_attention_grad",
     "nsgcqt_band_attention_workspace", "nsgcqt_attention_step", "nsgcqt_attention_step_workspace",
-    "nsgcqt_cache_fill",
+    "nsgcqt_cache_fill", "nsgcqt_decay_attention", "nsgcqt_decay_attention_grad", "nsgcqt_decay_attention_workspace",
+    "nsgcqt_decay_step",
 ]
 
 
@@ -47,6 +52,7 @@ EXPORTS = [
 _view = struct.Struct("=4q").pack                # nsgcqt_view: data, strides of batch, row, head
 _rows = struct.Struct("=4q").pack                # nsgcqt_rows: offsets, n_bands, batch, rows
 _shape = struct.Struct("=6qd2q").pack            # nsgcqt_attention_shape
+_decay_shape = struct.Struct("=3qd3q").pack      # nsgcqt_decay_shape
 
 
 _fns = None
@@ -70,6 +76,10 @@ def _lib():
             "nsgcqt_attention_step": [I, I64, I64, I64, I64, I64, I64, D, V, V, V, V, V, V, V, V, Z, V],
             "nsgcqt_attention_step_workspace": [I64] * 6,
             "nsgcqt_cache_fill": [I, V, I64, I64, I64, I64, V, V, V, V, V],
+            "nsgcqt_decay_attention": [I] + [V] * 8 + [Z, V],
+            "nsgcqt_decay_attention_grad": [I] + [V] * 10 + [Z, V],
+            "nsgcqt_decay_attention_workspace": [V, V, I],
+            "nsgcqt_decay_step": [I, I64, I64, I64, I64, D] + [V] * 8,
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -427,6 +437,12 @@ class _BandAttention(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None, None
 
 
+def _keep(keep, like, batch, rows):
+    if keep is not None and (keep.dtype != torch.bool or keep.device != like.device or keep.shape != (batch, rows) or (
+            rows > 1 and keep.stride(1) != 1)):
+        raise ValueError("keep has to be bool [batch][rows] on the device of q, its rows contiguous")
+
+
 def band_attention(q, k, v, offsets, left, right=0, sinks=0, scale=None, keep=None):
     """Attention along each band of each signal.
 
@@ -445,10 +461,7 @@ def band_attention(q, k, v, offsets, left, right=0, sinks=0, scale=None, keep=No
     _tensor(k, "k", q, (batch, rows, k.shape[2], dim))
     _tensor(v, "v", q, k.shape)
     _offsets(offsets, q)
-    if keep is not None:
-        if keep.dtype != torch.bool or keep.device != q.device or keep.shape != (batch, rows) or (
-                rows > 1 and keep.stride(1) != 1):
-            raise ValueError("keep has to be bool [batch][rows] on the device of q, its rows contiguous")
+    _keep(keep, q, batch, rows)
     far = 1 << 40
     call = _BandAttention.apply if _trains(q, k, v) else _attention_forward
     return call(q, k, v, offsets, keep, far if left is None else int(left), far if right is None else int(right),
@@ -556,5 +569,159 @@ class StreamCache:
     def step(self, q, k, v, scale=None):
         """`attention_step` of every stream's next token (zeros for an idle one)."""
         o = attention_step(q, k, v, self.k, self.v, self.pos, self.sinks, scale)
+        self.pos += self.pos >= 0
+        return o
+
+
+# -------------------------------------------------------------- decay_attention
+
+
+def _decay_of(log_decay, like, kv_heads):
+    if log_decay.dtype != torch.float32 or log_decay.device != like.device or log_decay.shape != (kv_heads,) or (
+            not log_decay.is_contiguous()):
+        raise ValueError(f"log_decay has to be a float32 vector of {kv_heads} values on the device of q")
+
+
+def _states(state, like, streams, kv_heads, dim):
+    if state.dtype != torch.float32 or state.device != like.device or (
+            state.shape != (streams, kv_heads, dim, dim)) or not state.is_contiguous():
+        raise ValueError(f"state has to be contiguous float32 {[streams, kv_heads, dim, dim]} on the device of q")
+
+
+def _decay_shape_of(q, k, log_decay, keep, scale):
+    return _decay_shape(q.shape[2], k.shape[2], q.shape[3], scale, log_decay.data_ptr(),
+                        0 if keep is None else keep.data_ptr(), 0 if keep is None else keep.stride(0))
+
+
+def _decay_workspace(r, shape, grad, like):
+    n = _bytes(_lib().nsgcqt_decay_attention_workspace(r, shape, grad))
+    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None, n
+
+
+def _decay_forward(q, k, v, offsets, log_decay, keep, state, scale):
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    shape, r = _decay_shape_of(q, k, log_decay, keep, scale), _ragged(offsets, q.shape[0], q.shape[1])
+    with _on(q):
+        ws, n = _decay_workspace(r, shape, 0, q)
+        _check(_lib().nsgcqt_decay_attention(
+            _DTYPES[q.dtype], r, shape, _view4(q), _view4(k), _view4(v), _view4(o),
+            None if state is None else state.data_ptr(), ws.data_ptr() if n else None, n, _stream(q)))
+    return o
+
+
+class _DecayAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, log_decay, keep, state, scale):
+        ctx.save_for_backward(q, k, v, offsets, log_decay, keep)
+        ctx.scale = scale
+        return _decay_forward(q, k, v, offsets, log_decay, keep, state, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do):
+        q, k, v, offsets, log_decay, keep = ctx.saved_tensors
+        do = _last(do)
+        dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
+        shape, r = _decay_shape_of(q, k, log_decay, keep, ctx.scale), _ragged(offsets, q.shape[0], q.shape[1])
+        with _on(q):
+            ws, n = _decay_workspace(r, shape, 1, q)
+            _check(_lib().nsgcqt_decay_attention_grad(
+                _DTYPES[q.dtype], r, shape, _view4(q), _view4(k), _view4(v), _view4(do), _view4(dq), _view4(dk),
+                _view4(dv), ws.data_ptr() if n else None, n, _stream(q)))
+        return dq, dk, dv, None, None, None, None, None
+
+
+def decay_attention(q, k, v, offsets, log_decay, scale=None, keep=None, state=None):
+    """Linear attention along each band, the past decaying by exp(log_decay) a token.
+
+    o_t = scale * sum over s <= t of exp(log_decay (t - s)) (q_t . k_s) v_s,
+    within token t's band. q [batch][rows][heads][D], k and v with kv_heads
+    heads, a divisor of heads (D at most 128); log_decay float32 [kv_heads], at
+    most 0. scale: D^-1/2 by default. keep (bool [batch][rows] or None): tokens
+    that add nothing, though they count as distance; what k and v hold there is
+    never used. state (float32 [batch * n_bands][kv_heads][D][D] or None): the
+    sum of exp(..) k_s v_s^T over what came before each band, row b * n_bands +
+    g for band g of signal b; it is replaced by that sum at the band's end.
+    Gradients for q, k and v, where no state is given; log_decay has none.
+    """
+    _tensor(q, "q", dims="[batch][rows][heads][D]")
+    if k.dim() != 4:
+        raise ValueError("k has to be [batch][rows][kv_heads][D]")
+    batch, rows, _, dim = q.shape
+    kv_heads = k.shape[2]
+    _tensor(k, "k", q, (batch, rows, kv_heads, dim))
+    _tensor(v, "v", q, k.shape)
+    _offsets(offsets, q)
+    _keep(keep, q, batch, rows)
+    _decay_of(log_decay, q, kv_heads)
+    if _trains(log_decay):
+        raise ValueError("decay_attention has no gradient for log_decay: detach it")
+    trains = _trains(q, k, v)
+    if state is not None:
+        _states(state, q, batch * (offsets.numel() - 1), kv_heads, dim)
+        if trains or _trains(state):
+            raise ValueError("decay_attention has no gradient from or into a state: call it under torch.no_grad()")
+    o = (_DecayAttention.apply if trains else _decay_forward)(q, k, v, offsets, log_decay, keep, state,
+                                                              _scale(scale, dim))
+    if state is not None:
+        _written(state)
+    return o
+
+
+def decay_step(q, k, v, state, pos, log_decay, scale=None, out=None):
+    """`decay_attention` of one new token of each stream.
+
+    q [streams][heads][D], k and v [streams][kv_heads][D]; state float32
+    [streams][kv_heads][D][D] takes the token in place, then q meets it. pos
+    int64 [streams] numbers the token: 0 starts a stream, whatever its state
+    holds; below 0 the stream has no token in this step, its state stays as it
+    is and its row is zero. Not differentiable.
+    """
+    _tensor(q, "q", dims="[streams][heads][D]")
+    if k.dim() != 3:
+        raise ValueError("k has to be [streams][kv_heads][D]")
+    streams, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    _tensor(k, "k", q, (streams, kv_heads, dim))
+    _tensor(v, "v", q, k.shape)
+    _decay_of(log_decay, q, kv_heads)
+    _states(state, q, streams, kv_heads, dim)
+    if pos.dtype != torch.int64 or pos.device != q.device or pos.shape != (streams,) or not pos.is_contiguous():
+        raise ValueError("pos has to be int64 [streams] on the device of q")
+    if _trains(q, k, v, state, log_decay, out):
+        raise ValueError("decay_step has no gradient: call it under torch.no_grad()")
+    o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else _tensor(out, "out", q, q.shape)
+    with _on(q):
+        _check(_lib().nsgcqt_decay_step(
+            _DTYPES[q.dtype], streams, heads, kv_heads, dim, _scale(scale, dim), _view_step(q), _view_step(k),
+            _view_step(v), _view_step(o), state.data_ptr(), pos.data_ptr(), log_decay.data_ptr(), _stream(q)))
+    _written(state, *(() if out is None else (out,)))
+    return o
+
+
+class DecayState:
+    """The states of many streams of `decay_attention`: one matrix a key head, however long a stream is.
+
+    `pos` holds the number of each stream's next token; a stream whose pos is
+    below 0 is idle: its state and its pos stay as they are.
+    """
+
+    def __init__(self, streams, kv_heads, head_dim, device="cuda"):
+        self.state = torch.zeros((streams, kv_heads, head_dim, head_dim), dtype=torch.float32, device=device)
+        self.pos = torch.zeros(streams, dtype=torch.int64, device=device)
+
+    def read(self, q, k, v, offsets, log_decay, scale=None, keep=None):
+        """`decay_attention` of whole bands: band g of signal b continues stream b * n_bands + g, or begins it where
+        its pos is 0 or below."""
+        self.pos.clamp_(min=0)
+        self.state.masked_fill_((self.pos == 0)[:, None, None, None], 0.0)
+        o = decay_attention(q, k, v, offsets, log_decay, scale, keep, self.state)
+        ends = offsets.clamp(0, k.shape[1])     # bands are cut to the row, as the kernels cut them
+        self.pos += (ends[1:] - ends[:-1]).repeat(k.shape[0])
+        return o
+
+    def step(self, q, k, v, log_decay, scale=None):
+        """`decay_step` of every stream's next token (zeros for an idle one)."""
+        o = decay_step(q, k, v, self.state, self.pos, log_decay, scale)
         self.pos += self.pos >= 0
         return o
