@@ -15,6 +15,7 @@
  *   nsgcqt_decay_attention* linear attention along each band with a decay for
  *                           each head, from and into a state
  *   nsgcqt_decay_step       the same for one new token of each of many streams
+ *   nsgcqt_band_norm*       group norm of each band with an activation
  *
  * Conventions
  *   - Data are float32, float16 or bfloat16 (nsgcqt_dtype), one type a call.
@@ -223,6 +224,39 @@ int64_t nsgcqt_decay_attention_workspace(const nsgcqt_rows* r, const nsgcqt_deca
 int nsgcqt_decay_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, double scale,
                       const nsgcqt_view* q, const nsgcqt_view* k, const nsgcqt_view* v, const nsgcqt_view* o,
                       float* state, const int64_t* pos, const float* log_decay, void* stream);
+
+/* none: z; silu: z / (1 + exp(-z)); gelu: z Phi(z), Phi the normal
+ * distribution's; sigmoid: 1 / (1 + exp(-z)). */
+typedef enum {
+    NSGCQT_ACT_NONE = 0, NSGCQT_ACT_SILU = 1, NSGCQT_ACT_GELU = 2, NSGCQT_ACT_SIGMOID = 3
+} nsgcqt_act;
+
+/* Shape and parameters of a group norm. */
+typedef struct {
+    int64_t channels, groups;   /* groups divides channels; at most 4,096 and 1,024 */
+    double eps;                 /* 1e-30 .. 1e30 */
+    const void *w, *b;          /* device, element [g][c] at [g w_band + c]; NULL: ones, zeros */
+    int64_t w_band, b_band;     /* strides in elements, not negative; 0 shares a row among bands */
+    int act;                    /* nsgcqt_act */
+} nsgcqt_norm_shape;
+
+/* y = act(w (x - mean) / sqrt(var + eps) + b), mean and (biased) variance over
+ * the channels of a group and all tokens of a band of one signal. x, y:
+ * [batch][rows][channels]. stats: [batch][n_bands][groups][2] float64, 16-byte
+ * aligned, receives mean and 1 / sqrt(var + eps) of bands that have tokens. y
+ * may be x itself. */
+int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, const nsgcqt_view* x,
+                     const nsgcqt_view* y, double* stats, void* ws, size_t ws_bytes, void* stream);
+
+/* dx, and with dw or db not NULL the gradients of w and b as
+ * [n_bands][channels] contiguous (whatever their strides), of a loss with
+ * gradient dy at y; stats as the forward call wrote them. dx may be NULL. */
+int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, const nsgcqt_view* x,
+                          const double* stats, const nsgcqt_view* dy, const nsgcqt_view* dx, void* dw, void* db,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of nsgcqt_band_norm (grad 0) or its gradient (weights: with dw or db), or a negative status. */
+int64_t nsgcqt_band_norm_workspace(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, int grad, int weights);
 
 #ifdef __cplusplus
 }

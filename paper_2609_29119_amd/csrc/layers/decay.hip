@@ -41,7 +41,7 @@ int segment_shift(int64_t batch, int64_t rows, int64_t heads) {
 // Bytes of the segments' states, `sums` of them a slot and key head.
 int64_t states_bytes(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, int shift, int sums) {
     if (r->rows <= int64_t(1) << shift) return 0;   // no band has several segments
-    return workspace_of(product(4 * sums, r->batch, decay_slots(r->rows, shift), s->n_kv_heads, s->head_dim * s->head_dim));
+    return workspace_of(product(4 * sums, r->batch, slot_count(r->rows, shift), s->n_kv_heads, s->head_dim * s->head_dim));
 }
 
 int64_t decay_workspace(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, bool grad) {

@@ -49,15 +49,6 @@ template <class T> __device__ inline T* decay_row(const View& v, int64_t b, int6
     return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row + head * v.head;
 }
 
-// The states of segments of bands of several segments have slots of their
-// own: a band of more than T tokens that starts at token `start` has those
-// from floor(2 start / T) on, of which its ceil(len / T) segments do not reach
-// the next such band's.
-inline __host__ __device__ int64_t decay_slots(int64_t rows, int shift) { return ((2 * rows) >> shift) + 1; }
-inline __host__ __device__ int64_t decay_slot(int64_t start, int64_t segment, int shift) {
-    return ((2 * start) >> shift) + segment;
-}
-
 // decay^n of a head, l2 the decay's base-2 logarithm. The product is formed in
 // 64 bits and only its fraction enters the exponential: the power is right to
 // the last bits of 32 however long the distance.
@@ -227,7 +218,7 @@ __device__ inline float* decay_state_of(const DecayArgs& a, const DecayJob& j, c
     const int64_t size = static_cast<int64_t>(a.dim) * a.dim;
     there = true;
     if (p.several)
-        return j.part + ((p.b * decay_slots(a.rows, a.shift) + decay_slot(p.seg.start, p.seg.first >> a.shift, a.shift)) *
+        return j.part + ((p.b * slot_count(a.rows, a.shift) + slot_of(p.seg.start, p.seg.first >> a.shift, a.shift)) *
                              a.kv_heads + p.kv) * size;
     if (a.state) return a.state + ((p.b * a.n_bands + p.seg.band) * a.kv_heads + p.kv) * size;
     there = false;
@@ -443,7 +434,7 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
     const float across = decay_power(l2, int64_t(1) << a.shift);
     const int count = (len + (1 << a.shift) - 1) >> a.shift;
     const int64_t step = static_cast<int64_t>(a.kv_heads) * size;
-    float* x = a.job[job].part + ((b * decay_slots(a.rows, a.shift) + decay_slot(start, 0, a.shift)) * a.kv_heads + kv) * size + e;
+    float* x = a.job[job].part + ((b * slot_count(a.rows, a.shift) + slot_of(start, 0, a.shift)) * a.kv_heads + kv) * size + e;
     float* st = a.state ? a.state + ((b * a.n_bands + band) * a.kv_heads + kv) * size + e : nullptr;
     float s = st ? *st : 0.f;
     constexpr int kAhead = 16;

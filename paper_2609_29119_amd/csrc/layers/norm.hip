@@ -1,0 +1,206 @@
+// C entries of the group norm on ragged rows.
+#include <algorithm>
+
+#include "checks.hpp"
+#include "norm.hpp"
+
+using namespace nsl;
+
+namespace {
+
+int check_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s) {
+    CHECK_TRY(check_dtype(dtype));
+    CHECK_TRY(check_rows(r));
+    if (!s) return set_err(NSGCQT_EINVAL, "shape is NULL");
+    if (s->groups < 1 || s->channels < 0 || s->channels % s->groups)
+        return set_err(NSGCQT_EINVAL, "groups must divide channels, and be at least 1");
+    if (!(s->eps >= 1e-30 && s->eps <= 1e30)) return set_err(NSGCQT_EINVAL, "eps must lie between 1e-30 and 1e30");
+    if (s->act < NSGCQT_ACT_NONE || s->act > NSGCQT_ACT_SIGMOID)
+        return set_err(NSGCQT_EINVAL, "unknown activation " + std::to_string(s->act));
+    if (s->w_band < 0 || s->b_band < 0) return set_err(NSGCQT_EINVAL, "a stride of w or b is negative");
+    if (misaligned(s->w, elem_bytes(dtype)) || misaligned(s->b, elem_bytes(dtype)))
+        return set_err(NSGCQT_EINVAL, "w or b is not aligned to its element");
+    if (s->channels > kNormChannels || s->groups > kNormGroups)
+        return set_err(NSGCQT_EUNSUPPORTED, "more than 4,096 channels or 1,024 groups");
+    return NSGCQT_OK;
+}
+
+// Tokens of a chunk: what a workgroup's registers hold, `held` octets a thread
+// (64 KB a workgroup).
+void set_chunk(NormArgs& a, int held) {
+    a.octets = (a.channels + 7) / 8;
+    a.together = kNormThreads / a.octets;
+    a.shift = 0;
+    while ((2 << a.shift) <= a.together * held) ++a.shift;
+    a.items = static_cast<unsigned>(tile_count(a.shift, a.n_bands, 1, a.rows));
+}
+
+// Rows of an item of the weights' gradient, 64 to 4096: the most that leave 1024 items.
+int weight_shift_of(int64_t batch, int64_t rows) {
+    int shift = 12;
+    while (shift > 6 && product(batch, rows) >> shift < 1024) --shift;
+    return shift;
+}
+
+NormArgs norm_args(const nsgcqt_rows* r, const nsgcqt_norm_shape* s) {
+    NormArgs a{};
+    a.w = s->w;
+    a.b = s->b;
+    a.w_band = s->w_band;
+    a.b_band = s->b_band;
+    a.off = r->offsets;
+    a.rows = static_cast<int>(r->rows);
+    a.n_bands = static_cast<int>(r->n_bands);
+    a.batch = static_cast<int>(r->batch);
+    a.channels = static_cast<int>(s->channels);
+    a.groups = static_cast<int>(s->groups);
+    a.cg = a.channels / a.groups;
+    a.act = s->act;
+    a.eps = s->eps;
+    return a;
+}
+
+int held_of(int dtype, bool grad) { return (dtype == NSGCQT_F32 ? norm_held<float>() : norm_held<__bf16>()) / (grad ? 2 : 1); }
+
+// Bytes of the workspace, whose parts begin at 16-byte boundaries: chunks'
+// statistics, then the weights' partial sums.
+struct NormSpace { int64_t part, sums; };
+NormSpace norm_space(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, bool grad, bool weights) {
+    NormArgs a = norm_args(r, s);
+    if (a.channels == 0) return {0, 0};
+    set_chunk(a, held_of(dtype, grad));
+    NormSpace n{0, 0};
+    if (r->rows > int64_t(1) << a.shift) n.part = product(16, r->batch, slot_count(r->rows, a.shift), a.groups);
+    if (grad && weights)
+        n.sums = product(8, tile_count(weight_shift_of(r->batch, r->rows), r->n_bands, r->batch, r->rows), a.channels);
+    return n;
+}
+int64_t norm_bytes(const NormSpace& n) {
+    int64_t all;
+    return workspace_of(__builtin_add_overflow(n.part, n.sums, &all) ? INT64_MAX : all);
+}
+
+int check_space(const void* ws, size_t have, int64_t need) {
+    if (need < 0) return static_cast<int>(need);
+    if (static_cast<int64_t>(have) < need)
+        return set_err(NSGCQT_EWORKSPACE, "workspace of " + std::to_string(have) + " bytes, " + std::to_string(need) +
+                                              " required");
+    if (need > 0 && (!ws || misaligned(ws, 16)))
+        return set_err(NSGCQT_EINVAL, "workspace is NULL or not aligned to 16 bytes");
+    return NSGCQT_OK;
+}
+
+template <class K> int launch_all(K kernel, NormArgs a, int64_t threads, hipStream_t st) {
+    const int64_t blocks = (threads + 255) / 256;
+    for (; a.first_block < blocks; a.first_block += kMaxGrid)
+        LAUNCH_TRY(kernel, dim3(static_cast<unsigned>(std::min(blocks - a.first_block, kMaxGrid))), dim3(256), 0, st, a);
+    return NSGCQT_OK;
+}
+
+// f(T(), true_type or false_type)
+template <class F> int by_width_of(int dtype, bool wide, F f) {
+    return by_type(dtype, [&](auto t) { return wide ? f(t, std::true_type()) : f(t, std::false_type()); });
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t nsgcqt_band_norm_workspace(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, int grad, int weights) {
+    CHECK_TRY(check_norm(dtype, r, s));
+    return norm_bytes(norm_space(dtype, r, s, grad != 0, weights != 0));
+}
+
+int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, const nsgcqt_view* x,
+                     const nsgcqt_view* y, double* stats, void* ws, size_t ws_bytes, void* stream) {
+    CHECK_TRY(check_norm(dtype, r, s));
+    bool wide = true;
+    CHECK_TRY(check_view(x, "x", dtype, r->batch, r->rows, 1, s->channels, wide));
+    CHECK_TRY(check_view(y, "y", dtype, r->batch, r->rows, 1, s->channels, wide));
+    if (r->batch == 0 || r->rows == 0 || s->channels == 0) return NSGCQT_OK;
+    if (!stats || misaligned(stats, 16)) return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 16 bytes");
+    const NormSpace space = norm_space(dtype, r, s, false, false);
+    CHECK_TRY(check_space(ws, ws_bytes, norm_bytes(space)));
+    NormArgs a = norm_args(r, s);
+    set_chunk(a, held_of(dtype, false));
+    a.x = view_of(x);
+    a.y = view_of(y);
+    a.stats = reinterpret_cast<double2*>(stats);
+    a.part = static_cast<double2*>(ws);
+    const int64_t blocks = product(r->batch, static_cast<int64_t>(a.items));
+    CHECK_TRY(check_grid(blocks));
+    const int64_t groups = product(r->batch, r->n_bands, a.groups);
+    if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
+    const dim3 grid(static_cast<unsigned>(blocks)), block(kNormThreads);
+    const size_t lds = sizeof(double) * 8 * a.octets * a.together;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
+        using T = decltype(t);
+        constexpr bool kWide = decltype(w)::value;
+        LAUNCH_TRY((k_norm<T, kWide>), grid, block, lds, st, a);
+        if (space.part) {
+            CHECK_TRY(launch_all(k_norm_join<false>, a, groups, st));
+            LAUNCH_TRY((k_norm_apply<T, kWide>), grid, block, 0, st, a);
+        }
+        return NSGCQT_OK;
+    });
+}
+
+int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, const nsgcqt_view* x,
+                          const double* stats, const nsgcqt_view* dy, const nsgcqt_view* dx, void* dw, void* db,
+                          void* ws, size_t ws_bytes, void* stream) {
+    CHECK_TRY(check_norm(dtype, r, s));
+    bool wide = true;
+    CHECK_TRY(check_view(x, "x", dtype, r->batch, r->rows, 1, s->channels, wide));
+    CHECK_TRY(check_view(dy, "dy", dtype, r->batch, r->rows, 1, s->channels, wide));
+    if (dx) CHECK_TRY(check_view(dx, "dx", dtype, r->batch, r->rows, 1, s->channels, wide));
+    if (misaligned(dw, elem_bytes(dtype)) || misaligned(db, elem_bytes(dtype)))
+        return set_err(NSGCQT_EINVAL, "dw or db is not aligned to its element");
+    const bool weights = dw || db;
+    if (s->channels == 0 || (!dx && !weights)) return NSGCQT_OK;
+    const bool rows = r->batch > 0 && r->rows > 0;
+    if (rows && (!stats || misaligned(stats, 16)))
+        return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 16 bytes");
+    const NormSpace space = norm_space(dtype, r, s, true, weights);
+    CHECK_TRY(check_space(ws, ws_bytes, norm_bytes(space)));
+    NormArgs a = norm_args(r, s);
+    set_chunk(a, held_of(dtype, true));
+    a.weight_shift = weight_shift_of(r->batch, r->rows);
+    a.x = view_of(x);
+    a.dy = view_of(dy);
+    if (dx) a.y = view_of(dx);
+    a.stats = reinterpret_cast<double2*>(const_cast<double*>(stats));
+    a.part = static_cast<double2*>(ws);
+    a.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + space.part);
+    a.dw = dw;
+    a.db = db;
+    const int64_t blocks = product(r->batch, static_cast<int64_t>(a.items));
+    const int64_t items = tile_count(a.weight_shift, r->n_bands, r->batch, r->rows);
+    const int64_t groups = product(r->batch, r->n_bands, a.groups);
+    if (dx) CHECK_TRY(check_grid(blocks));
+    if (weights) CHECK_TRY(check_grid(items));
+    if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
+    const dim3 block(kNormThreads);
+    const size_t lds = sizeof(double) * 8 * a.octets * a.together;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
+        using T = decltype(t);
+        constexpr bool kWide = decltype(w)::value;
+        if (dx && rows) {
+            const dim3 grid(static_cast<unsigned>(blocks));
+            LAUNCH_TRY((k_norm_grad<T, kWide, false>), grid, block, lds, st, a);
+            if (space.part) {
+                CHECK_TRY(launch_all(k_norm_join<true>, a, groups, st));
+                LAUNCH_TRY((k_norm_grad<T, kWide, true>), grid, block, 0, st, a);
+            }
+        }
+        if (weights) {
+            if (rows)
+                LAUNCH_TRY((k_norm_weight<T, kWide>), dim3(static_cast<unsigned>(items)), block, lds, st, a);
+            CHECK_TRY(launch_all(k_norm_weight_join<T>, a, r->n_bands * s->channels, st));
+        }
+        return NSGCQT_OK;
+    });
+}
+
+}  // extern "C"

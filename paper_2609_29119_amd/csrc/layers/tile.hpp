@@ -436,6 +436,15 @@ __device__ inline Tile<I> find_tile(const int64_t* off, int n_bands, int rows, I
     return tile_of(lo, a, b, mult, shift, p);
 }
 
+// Slots for the segments of 2^shift = T tokens of those bands that have
+// several, without a table: a band of more than T tokens that starts at token
+// `start` has those from floor(2 start / T) on, and its ceil(len / T) segments
+// end before the next such band's first, as floor(2 len / T) is no less.
+inline __host__ __device__ int64_t slot_count(int64_t rows, int shift) { return ((2 * rows) >> shift) + 1; }
+inline __host__ __device__ int64_t slot_of(int64_t start, int64_t segment, int shift) {
+    return ((2 * start) >> shift) + segment;
+}
+
 // The number of this thread's wave, in a scalar register: what follows from
 // it (a wave's range of rows, what it skips) is then scalar work.
 __device__ inline int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }

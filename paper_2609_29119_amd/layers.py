@@ -16,6 +16,7 @@ include/nsgcqt_layers.h:
                    rate of each head's own; from and into a state
   decay_step       the same for one new token of each of many streams;
                    `DecayState` holds the streams' states
+  band_norm        group norm of each band, with an activation
 
 All but the steps and fills are differentiable. Data are float32, float16 or bfloat16
 CUDA tensors, one type a call; the last axis has to be contiguous, other
@@ -37,6 +38,7 @@ F32, F16, BF16 = 0, 1, 2
 POS_F32, POS_F64, POS_I64 = 0, 1, 2
 
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_ACTS = {None: 0, "silu": 1, "gelu": 2, "sigmoid": 3}
 _POS = {torch.float32: POS_F32, torch.float64: POS_F64, torch.int64: POS_I64}
 
 EXPORTS = [
@@ -44,7 +46,7 @@ EXPORTS = [
     "nsgcqt_band_linear_workspace", "nsgcqt_rotary", "nsgcqt_band_attention", "nsgcqt_band_attention_grad",
     "nsgcqt_band_attention_workspace", "nsgcqt_attention_step", "nsgcqt_attention_step_workspace",
     "nsgcqt_cache_fill", "nsgcqt_decay_attention", "nsgcqt_decay_attention_grad", "nsgcqt_decay_attention_workspace",
-    "nsgcqt_decay_step",
+    "nsgcqt_decay_step", "nsgcqt_band_norm", "nsgcqt_band_norm_grad", "nsgcqt_band_norm_workspace",
 ]
 
 
@@ -53,6 +55,7 @@ _view = struct.Struct("=4q").pack                # nsgcqt_view: data, strides of
 _rows = struct.Struct("=4q").pack                # nsgcqt_rows: offsets, n_bands, batch, rows
 _shape = struct.Struct("=6qd2q").pack            # nsgcqt_attention_shape
 _decay_shape = struct.Struct("=3qd3q").pack      # nsgcqt_decay_shape
+_norm_shape = struct.Struct("=2qd4qi4x").pack    # nsgcqt_norm_shape
 
 
 _fns = None
@@ -80,6 +83,9 @@ def _lib():
             "nsgcqt_decay_attention_grad": [I] + [V] * 10 + [Z, V],
             "nsgcqt_decay_attention_workspace": [V, V, I],
             "nsgcqt_decay_step": [I, I64, I64, I64, I64, D] + [V] * 8,
+            "nsgcqt_band_norm": [I] + [V] * 6 + [Z, V],
+            "nsgcqt_band_norm_grad": [I] + [V] * 9 + [Z, V],
+            "nsgcqt_band_norm_workspace": [I, V, V, I, I],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -725,3 +731,100 @@ class DecayState:
         o = decay_step(q, k, v, self.state, self.pos, log_decay, scale)
         self.pos += self.pos >= 0
         return o
+
+
+# -------------------------------------------------------------------- band_norm
+
+
+def _act(activation):
+    if activation not in _ACTS:
+        raise ValueError(f"activation is {activation!r}: None, 'silu', 'gelu' or 'sigmoid' is expected")
+    return _ACTS[activation]
+
+
+def _norm_shape_of(x, weight, bias, groups, act, eps):
+    w, b = ((0, 0) if t is None else (t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0) for t in (weight, bias))
+    return _norm_shape(x.shape[2], groups, eps, w[0], b[0], w[1], b[1], act)
+
+
+def _norm_workspace(x, r, shape, grad, weights):
+    n = _bytes(_lib().nsgcqt_band_norm_workspace(_DTYPES[x.dtype], r, shape, grad, weights))
+    return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None, n
+
+
+def _norm_call(x, offsets, weight, bias, groups, act, eps):
+    batch, rows, channels = x.shape
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    stats = torch.empty((batch, offsets.numel() - 1, groups, 2), dtype=torch.float64, device=x.device)
+    shape, r = _norm_shape_of(x, weight, bias, groups, act, eps), _ragged(offsets, batch, rows)
+    with _on(x):
+        ws, n = _norm_workspace(x, r, shape, 0, 0)
+        _check(_lib().nsgcqt_band_norm(_DTYPES[x.dtype], r, shape, _view3(x), _view3(y), stats.data_ptr(),
+                                       ws.data_ptr() if n else None, n, _stream(x)))
+    return y, stats
+
+
+def _norm_forward(x, weight, bias, offsets, groups, act, eps):
+    return _norm_call(x, offsets, weight, bias, groups, act, eps)[0]
+
+
+class _BandNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, offsets, groups, act, eps):
+        y, stats = _norm_call(x, offsets, weight, bias, groups, act, eps)
+        ctx.save_for_backward(x, weight, bias, offsets, stats)
+        ctx.how = groups, act, eps
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, offsets, stats = ctx.saved_tensors
+        dy = _last(dy)
+        need = ctx.needs_input_grad
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need[0] else None
+        dw, db = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if n else None
+                  for t, n in ((weight, need[1]), (bias, need[2])))
+        shape, r = _norm_shape_of(x, weight, bias, *ctx.how), _ragged(offsets, x.shape[0], x.shape[1])
+        with _on(x):
+            ws, n = _norm_workspace(x, r, shape, 1, dw is not None or db is not None)
+            _check(_lib().nsgcqt_band_norm_grad(
+                _DTYPES[x.dtype], r, shape, _view3(x), stats.data_ptr(), _view3(dy),
+                None if dx is None else _view3(dx), None if dw is None else dw.data_ptr(),
+                None if db is None else db.data_ptr(), ws.data_ptr() if n else None, n, _stream(x)))
+        return dx, dw, db, None, None, None, None
+
+
+def band_norm(x, offsets, weight=None, bias=None, groups=1, activation=None, eps=1e-5):
+    """Group norm of each band of each signal, with an activation.
+
+    x [batch][rows][channels]: mean and (biased) variance go over the channels
+    of one of `groups` equal groups and all tokens of one band. weight and bias
+    [n_bands][channels] or None: y = act(weight * (x - mean) / sqrt(var + eps)
+    + bias); a row shared by the bands may be expanded to them. activation:
+    None, "silu", "gelu" (by the normal distribution) or "sigmoid". Tokens that
+    no band holds get zeros. Tokens are normalised each by itself as rows of one
+    token: x [tokens][1][channels], offsets [0, 1]. At most 4,096 channels and
+    1,024 groups. Gradients for x, weight and bias.
+    """
+    _tensor(x, "x", dims="[batch][rows][channels]")
+    _offsets(offsets, x)
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _tensor(t, name, x, (offsets.numel() - 1, x.shape[2]))
+    act = _act(activation)
+    call = _BandNorm.apply if _trains(x, weight, bias) else _norm_forward
+    return call(x, weight, bias, offsets, int(groups), act, float(eps))
+
+
+class BandNorm(torch.nn.Module):
+    """band_norm with its own weights (ones and zeros at the start)."""
+
+    def __init__(self, n_bands, channels, groups=1, activation=None, eps=1e-5, device="cuda", dtype=torch.float32):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(n_bands, channels, device=device, dtype=dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(n_bands, channels, device=device, dtype=dtype))
+        self.groups, self.activation, self.eps = groups, activation, eps
+
+    def forward(self, x, offsets):
+        return band_norm(x, offsets, self.weight, self.bias, self.groups, self.activation, self.eps)

@@ -211,3 +211,123 @@ def test_decay_step_from_the_first_token(case, dtype):
     ref, size = decay_reference(q, k, v, [tokens], 0, lam, d ** -0.5, state=zero)
     close(torch.stack(rows, 1), ref[0], size[0], "o", 2.0 ** -20, 2.0 ** -25)
     close(held.state[:streams], ref[4], size[4], "state", 2.0 ** -20)
+
+
+# -------------------------------------------------------------------- band_norm
+
+ACTS = [None, "silu", "gelu", "sigmoid"]
+
+
+def act_reference(z, how):
+    """act(z) and act'(z), in 64 bits."""
+    if how is None:
+        return z, torch.ones_like(z)
+    if how == "gelu":
+        phi = 0.5 * torch.special.erfc(-z / 2 ** 0.5)
+        return z * phi, phi + z * (-z * z / 2).exp() / (2 * np.pi) ** 0.5
+    s = torch.sigmoid(z)
+    return (s, s * torch.sigmoid(-z)) if how == "sigmoid" else (z * s, s + z * s * torch.sigmoid(-z))
+
+
+def norm_reference(x, lengths, first, w, b, groups, act, eps, dy):
+    """(y, dx, dw, db) in 64 bits, and the sizes of their terms: a value's own magnitude, the mean's and the shift's
+    stand in z, and each sum has its terms' magnitudes."""
+    x, dy = x.detach().double(), dy.detach().double()
+    B, _, ch = x.shape
+    G = len(lengths)
+    w = torch.ones(G, ch, device="cuda").double() if w is None else w.detach().double()
+    b = torch.zeros(G, ch, device="cuda").double() if b is None else b.detach().double()
+    ref = [torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(w), torch.zeros_like(w)]
+    size = [torch.zeros_like(t) for t in ref]
+    at = first
+    for g, n in enumerate(lengths):
+        s = slice(at, at + n)
+        at += n
+        if n == 0:
+            continue
+        split = lambda t: t.reshape(*t.shape[:-1], groups, -1)  # noqa: E731
+        t = split(x[:, s])
+        mean, var = t.mean((1, 3), keepdim=True), t.var((1, 3), correction=0, keepdim=True)
+        r = (var + eps) ** -0.5
+        hat, hat_size = (t - mean) * r, (t.abs() + mean.abs()) * r
+        wg, bg = split(w[g]), split(b[g])
+        z, z_size = wg * hat + bg, wg.abs() * hat_size + bg.abs()
+        y, slope = act_reference(z, act)
+        ref[0][:, s], size[0][:, s] = y.flatten(2), (y.abs() + (slope.abs() + 0.4) * z_size).flatten(2)
+        d0 = split(dy[:, s])
+        dz, dz_size = d0 * slope, d0.abs() * (slope.abs() + z_size)
+        d, d_size = dz * wg, dz_size * wg.abs()
+        mean2 = lambda v: v.mean((1, 3), keepdim=True)  # noqa: E731
+        ref[1][:, s] = (r * (d - mean2(d) - hat * mean2(d * hat))).flatten(2)
+        size[1][:, s] = (r * (d_size + mean2(d_size) + hat_size * mean2(d_size * hat_size))).flatten(2)
+        ref[2][g], size[2][g] = (dz * hat).sum((0, 1)).flatten(), (dz_size * hat_size).sum((0, 1)).flatten()
+        ref[3][g], size[3][g] = dz.sum((0, 1)).flatten(), dz_size.sum((0, 1)).flatten()
+    return ref, size
+
+
+NORM = [
+    # lengths, batch, channels, groups, affine
+    ([1], 1, 1, 1, True),
+    ([1], 5, 24, 3, True),                  # single tokens
+    ([5, 0, 3], 2, 8, 8, True),
+    ([130, 1, 257], 3, 12, 4, True),
+    ([300, 7, 0, 0, 129], 2, 128, 8, True),
+    ([64, 200], 1, 77, 7, True),
+    ([700, 900], 1, 64, 1, True),           # several chunks
+    ([6000], 2, 9, 1, False),
+    ([31, 33], 2, 1000, 10, True),
+    ([9, 20], 1, 4096, 4, True),
+    ([40], 1, 2600, 2, False),
+    ([3] * 150 + [0, 1], 1, 16, 2, True),
+    ([0, 0], 2, 4, 2, True),
+    ([17, 5], 40, 33, 33, True),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(NORM)))
+def test_band_norm(case, dtype):
+    lengths, batch, ch, groups, affine = NORM[case]
+    rows, G, act = sum(lengths), len(lengths), ACTS[case % 4]
+    x = (randn(case, batch, rows, ch) + 2 * randn(case + 1, ch)).to(dtype).requires_grad_()
+    w, b = (((randn(case + n, G, ch, by=0.4) + 1).to(dtype).requires_grad_() if affine else None) for n in (50, 60))
+    dy = randn(case + 70, batch, rows, ch, dtype=dtype)
+    y = layers.band_norm(x, offsets_of(lengths), w, b, groups, act, 1e-3)
+    got = [y, *torch.autograd.grad(y, [t for t in (x, w, b) if t is not None], dy)]
+    ref, size = norm_reference(x, lengths, 0, w, b, groups, act, 1e-3, dy)
+    for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
+        close(t, r, z, name, 2.0 ** -20, 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+def test_band_norm_strides_uncovered_tokens_and_shared_weights(act, dtype):
+    """Odd strides, tokens of no band, one row of weights for all bands, whose gradients are then its sum."""
+    lengths, first, rows, batch, ch = [17, 1150], 9, 1190, 2, 40
+    big = randn(3, batch, rows + 3, 2 * ch + 1, dtype=dtype)
+    w, b = (randn(n, ch, dtype=dtype).requires_grad_() for n in (4, 5))
+    dy = randn(6, rows, batch, ch, dtype=dtype).transpose(0, 1)
+    for lo in (0, 1):
+        x = big[:, 1:rows + 1, lo:lo + ch].detach().requires_grad_()
+        y = layers.band_norm(x, offsets_of(lengths, first), w.expand(2, -1), b.expand(2, -1), 5, act)
+        got = torch.autograd.grad(y, [x, w, b], dy)
+        ref, size = norm_reference(x, lengths, first, w.expand(2, -1), b.expand(2, -1), 5, act, 1e-5, dy)
+        close(y, ref[0], size[0], "y", 2.0 ** -20, 2.0 ** -25)
+        close(got[0], ref[1], size[1], "dx", 2.0 ** -20, 2.0 ** -25)
+        # autograd adds the two bands' rows, each rounded: one rounding of each row, and one of the sum
+        for t, r, z, name in zip(got[1:], ref[2:], size[2:], ("dw", "db")):
+            u = U[dtype]
+            assert ((t.double() - r.sum(0)).abs() <= 2.0 ** -20 * z.sum(0) + u * (r.abs().sum(0) + 1.01 * r.sum(0).abs()) * 1.01 + 2.0 ** -24).all(), name
+        for t in (y, got[0]):
+            assert t[:, :first].abs().max() == 0 and t[:, first + 1167:].abs().max() == 0
+
+
+def test_band_norm_far_from_zero():
+    """A mean of 10^4 standard deviations: the statistics are differences from the mean, not of squares."""
+    for n in (40, 5000):
+        x = 1e4 + randn(1, 2, n, 16)
+        y = layers.band_norm(x, offsets_of([n]), groups=2)
+        ref, _ = norm_reference(x, [n], 0, None, None, 2, None, 1e-5, x)
+        assert (y.double() - ref[0]).abs().max() < 2.0 ** -20
+        same = layers.band_norm(torch.full((1, n, 16), 3e4, device="cuda"), offsets_of([n]), activation="silu")
+        assert not same.any()
