@@ -16,6 +16,8 @@
  *                           each head, from and into a state
  *   nsgcqt_decay_step       the same for one new token of each of many streams
  *   nsgcqt_band_norm*       group norm of each band with an activation
+ *   nsgcqt_band_gated*      two projections of each band, an activation and
+ *                           their product
  *
  * Conventions
  *   - Data are float32, float16 or bfloat16 (nsgcqt_dtype), one type a call.
@@ -257,6 +259,25 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
 
 /* Workspace bytes of nsgcqt_band_norm (grad 0) or its gradient (weights: with dw or db), or a negative status. */
 int64_t nsgcqt_band_norm_workspace(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, int grad, int weights);
+
+/* y[b][c][:] = act(Wa x + ba) (Wu x + bu), elementwise, with Wa, Wu = w[g][0],
+ * w[g][1] and ba, bu = bias[g][0], bias[g][1], g the band of token c. x:
+ * [batch][rows][n_in], w: [n_bands][2][n_out][n_in] contiguous, bias:
+ * [n_bands][2][n_out] contiguous or NULL, y: [batch][rows][n_out]; act an
+ * nsgcqt_act. n_in at most 65,536, n_out 32,768. */
+int nsgcqt_band_gated(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const void* w, const void* bias,
+                      const nsgcqt_view* y, int64_t n_in, int64_t n_out, int act, void* stream);
+
+/* dx, dw and db (as w and bias) of a loss with gradient dy at y. dx may be
+ * NULL, and so may db, or dw and db; the workspace is for dw and db. The
+ * gradients at the two projections enter the products of 16-bit data as two
+ * numbers of 8 bits. */
+int nsgcqt_band_gated_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, const void* w, const void* bias,
+                           const nsgcqt_view* dy, const nsgcqt_view* dx, void* dw, void* db, int64_t n_in,
+                           int64_t n_out, int act, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of nsgcqt_band_gated_grad, or a negative status. */
+int64_t nsgcqt_band_gated_workspace(const nsgcqt_rows* r, int64_t n_in, int64_t n_out);
 
 #ifdef __cplusplus
 }

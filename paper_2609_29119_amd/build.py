@@ -27,7 +27,7 @@ HIP_FLAGS = [
 # The layers are compiled at -O2: at -O3 one instantiation of the 32-bit
 # per-band product is unrolled until it spills (3.5 KB a lane).
 LAYER_FLAGS = [f if f != "-O3" else "-O2" for f in HIP_FLAGS]
-LAYERS = ["linear", "rotary", "attention", "attention_grad", "step", "decay", "norm"]
+LAYERS = ["linear", "rotary", "attention", "attention_grad", "step", "decay", "norm", "gated"]
 
 
 def _run(cmd, verbose):

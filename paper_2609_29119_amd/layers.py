@@ -17,6 +17,7 @@ include/nsgcqt_layers.h:
   decay_step       the same for one new token of each of many streams;
                    `DecayState` holds the streams' states
   band_norm        group norm of each band, with an activation
+  band_gated       two projections of each band, an activation, their product
 
 All but the steps and fills are differentiable. Data are float32, float16 or bfloat16
 CUDA tensors, one type a call; the last axis has to be contiguous, other
@@ -47,6 +48,7 @@ EXPORTS = [
     "nsgcqt_band_attention_workspace", "nsgcqt_attention_step", "nsgcqt_attention_step_workspace",
     "nsgcqt_cache_fill", "nsgcqt_decay_attention", "nsgcqt_decay_attention_grad", "nsgcqt_decay_attention_workspace",
     "nsgcqt_decay_step", "nsgcqt_band_norm", "nsgcqt_band_norm_grad", "nsgcqt_band_norm_workspace",
+    "nsgcqt_band_gated", "nsgcqt_band_gated_grad", "nsgcqt_band_gated_workspace",
 ]
 
 
@@ -86,6 +88,9 @@ def _lib():
             "nsgcqt_band_norm": [I] + [V] * 6 + [Z, V],
             "nsgcqt_band_norm_grad": [I] + [V] * 9 + [Z, V],
             "nsgcqt_band_norm_workspace": [I, V, V, I, I],
+            "nsgcqt_band_gated": [I, V, V, V, V, V, I64, I64, I, V],
+            "nsgcqt_band_gated_grad": [I] + [V] * 8 + [I64, I64, I, V, Z, V],
+            "nsgcqt_band_gated_workspace": [V, I64, I64],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -828,3 +833,87 @@ class BandNorm(torch.nn.Module):
 
     def forward(self, x, offsets):
         return band_norm(x, offsets, self.weight, self.bias, self.groups, self.activation, self.eps)
+
+
+# ------------------------------------------------------------------- band_gated
+
+
+def _gated_forward(x, weight, bias, offsets, act):
+    batch, rows, n_in = x.shape
+    n_out = weight.shape[2]
+    y = x.new_empty((batch, rows, n_out))
+    with _on(x):
+        _check(_lib().nsgcqt_band_gated(
+            _DTYPES[x.dtype], _ragged(offsets, batch, rows), _view3(x), weight.data_ptr(),
+            None if bias is None else bias.data_ptr(), _view3(y), n_in, n_out, act, _stream(x)))
+    return y
+
+
+class _BandGated(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, offsets, act):
+        ctx.save_for_backward(x, weight, bias, offsets)
+        ctx.act = act
+        return _gated_forward(x, weight, bias, offsets, act)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, offsets = ctx.saved_tensors
+        dy = _last(dy)
+        batch, rows, n_in = x.shape
+        n_out = weight.shape[2]
+        need = ctx.needs_input_grad
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need[0] else None
+        dw = torch.empty_like(weight) if need[1] or need[2] else None
+        db = torch.empty_like(bias) if need[2] else None
+        L, r = _lib(), _ragged(offsets, batch, rows)
+        n = _bytes(L.nsgcqt_band_gated_workspace(r, n_in, n_out)) if dw is not None else 0
+        ws = torch.empty(max(n, 1), dtype=torch.uint8, device=x.device)
+        with _on(x):
+            _check(L.nsgcqt_band_gated_grad(
+                _DTYPES[x.dtype], r, _view3(x), weight.data_ptr(), None if bias is None else bias.data_ptr(), _view3(dy),
+                None if dx is None else _view3(dx), None if dw is None else dw.data_ptr(),
+                None if db is None else db.data_ptr(), n_in, n_out, ctx.act, ws.data_ptr(), n, _stream(x)))
+        return dx, dw if need[1] else None, db, None, None
+
+
+def band_gated(x, weight, offsets, bias=None, activation="silu"):
+    """y[b, c] = act(weight[g, 0] @ x[b, c] + bias[g, 0]) * (weight[g, 1] @ x[b, c] + bias[g, 1]), g the band of token c.
+
+    x [batch][rows][n_in], weight [n_bands][2][n_out][n_in], bias
+    [n_bands][2][n_out] or None, offsets int64 [n_bands + 1]; activation None,
+    "silu", "gelu" (by the normal distribution) or "sigmoid"; returns
+    [batch][rows][n_out]. Tokens that no band holds get zeros. Gradients for
+    x, weight and bias; they form both projections again.
+    """
+    _tensor(x, "x", dims="[batch][rows][n_in]")
+    if weight.dim() != 4:
+        raise ValueError("weight has to be [n_bands][2][n_out][n_in]")
+    _offsets(offsets, x)
+    bands, n_out = offsets.numel() - 1, weight.shape[2]
+    _tensor(weight, "weight", x, (bands, 2, n_out, x.shape[2]))
+    if not weight.is_contiguous():
+        raise ValueError("weight has to be contiguous")
+    if bias is not None:
+        _tensor(bias, "bias", x, (bands, 2, n_out))
+        if not bias.is_contiguous():
+            raise ValueError("bias has to be contiguous")
+    act = _act(activation)
+    call = _BandGated.apply if _trains(x, weight, bias) else _gated_forward
+    return call(x, weight, bias, offsets, act)
+
+
+class BandGated(torch.nn.Module):
+    """band_gated with its own weights (uniform in +-n_in^-1/2 at the start)."""
+
+    def __init__(self, n_bands, n_in, n_out, activation="silu", bias=True, device="cuda", dtype=torch.float32):
+        super().__init__()
+        k = n_in ** -0.5 if n_in else 0.0
+        self.weight = torch.nn.Parameter(
+            torch.empty(n_bands, 2, n_out, n_in, device=device, dtype=dtype).uniform_(-k, k))
+        self.bias = torch.nn.Parameter(torch.zeros(n_bands, 2, n_out, device=device, dtype=dtype)) if bias else None
+        self.activation = activation
+
+    def forward(self, x, offsets):
+        return band_gated(x, self.weight, offsets, self.bias, self.activation)

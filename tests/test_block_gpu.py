@@ -331,3 +331,91 @@ def test_band_norm_far_from_zero():
         assert (y.double() - ref[0]).abs().max() < 2.0 ** -20
         same = layers.band_norm(torch.full((1, n, 16), 3e4, device="cuda"), offsets_of([n]), activation="silu")
         assert not same.any()
+
+
+# ------------------------------------------------------------------- band_gated
+
+
+def gated_reference(x, w, b, lengths, first, act, dy):
+    """(y, dx, dw, db) in 64 bits, and their sizes: projections' errors, 2^-20 of their terms, pass through the
+    activation and its slope (both change by at most their argument's change, 0.8 of it for the slope)."""
+    x, w, dy = (t.detach().double() for t in (x, w, dy))
+    b = torch.zeros(*w.shape[:3], device="cuda").double() if b is None else b.detach().double()
+    ref = [torch.zeros(*x.shape[:2], w.shape[2], device="cuda").double(), torch.zeros_like(x), torch.zeros_like(w),
+           torch.zeros_like(b)]
+    size = [torch.zeros_like(t) for t in ref]
+    at = first
+    for g, n in enumerate(lengths):
+        s = slice(at, at + n)
+        at += n
+        if n == 0:
+            continue
+        xs, d = x[:, s], dy[:, s]
+        a, u = (torch.matmul(xs, w[g, i].T.contiguous()) + b[g, i] for i in (0, 1))
+        za, zu = (torch.matmul(xs.abs(), w[g, i].T.abs().contiguous()) + b[g, i].abs() for i in (0, 1))
+        f, slope = act_reference(a, act)
+        fz, sz = f.abs() + slope.abs() * za + za * 2.0 ** -20, slope.abs() + za
+        ref[0][:, s], size[0][:, s] = f * u, fz * zu
+        da, du, da_z, du_z = d * u * slope, d * f, d.abs() * zu * sz, d.abs() * fz
+        ref[1][:, s] = torch.matmul(da, w[g, 0]) + torch.matmul(du, w[g, 1])
+        size[1][:, s] = torch.matmul(da_z, w[g, 0].abs()) + torch.matmul(du_z, w[g, 1].abs())
+        for i, (t, z) in enumerate(((da, da_z), (du, du_z))):
+            ref[2][g, i] = torch.matmul(t.flatten(0, 1).T.contiguous(), xs.flatten(0, 1))
+            size[2][g, i] = torch.matmul(z.flatten(0, 1).T.contiguous(), xs.flatten(0, 1).abs())
+            ref[3][g, i], size[3][g, i] = t.sum((0, 1)), z.sum((0, 1))
+    return ref, size
+
+
+GATED = [
+    # lengths, batch, n_in, n_out, bias
+    ([1], 1, 1, 1, True),
+    ([5, 0, 3], 2, 2, 32, True),
+    ([130, 1, 257], 3, 8, 8, False),
+    ([64, 200], 1, 33, 77, True),
+    ([300, 7, 0, 0, 129], 2, 128, 128, True),
+    ([150], 2, 72, 200, True),
+    ([40, 90], 1, 200, 40, False),
+    ([31, 33], 2, 257, 65, True),
+    ([1500, 600], 3, 24, 16, True),        # several chunks of the weights' gradient
+    ([3] * 150 + [0, 1], 1, 16, 24, True),
+    ([0, 0], 2, 4, 4, True),
+    ([70, 131], 2, 520, 130, True),
+    ([1] * 40, 5, 64, 96, True),
+    ([12], 1, 0, 8, True),                 # nothing but the bias
+    ([12, 4], 1, 8, 0, False),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(GATED)))
+def test_band_gated(case, dtype):
+    lengths, batch, n_in, n_out, bias = GATED[case]
+    rows, G, act = sum(lengths), len(lengths), ACTS[(case + 1) % 4]
+    x = randn(case, batch, rows, n_in, dtype=dtype).requires_grad_()
+    w = randn(case + 50, G, 2, n_out, n_in, dtype=dtype, by=max(n_in, 1) ** -0.5).requires_grad_()
+    b = randn(case + 90, G, 2, n_out, dtype=dtype).requires_grad_() if bias else None
+    dy = randn(case + 70, batch, rows, n_out, dtype=dtype)
+    y = layers.band_gated(x, w, offsets_of(lengths), b, act)
+    got = [y, *torch.autograd.grad(y, [t for t in (x, w, b) if t is not None], dy)]
+    ref, size = gated_reference(x, w, b, lengths, 0, act, dy)
+    close(y, ref[0], size[0], "y", 2.0 ** -20, 2.0 ** -25)
+    for t, r, z, name in zip(got[1:], ref[1:], size[1:], ("dx", "dw", "db")):
+        close(t, r, z, name, 2.0 ** -20 if name == "db" else sums_of(dtype), 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_band_gated_strides_and_uncovered_tokens(dtype):
+    lengths, first, rows, batch, n_in, n_out = [17, 150], 9, 190, 2, 48, 40
+    big = randn(3, batch, rows + 3, 2 * n_in + 1, dtype=dtype)
+    for lo in (0, 1):
+        x = big[:, 1:rows + 1, lo:lo + n_in].detach().requires_grad_()
+        w = randn(4, 2, 2, n_out, n_in, dtype=dtype, by=0.2).requires_grad_()
+        dy = randn(5, rows, batch, n_out, dtype=dtype).transpose(0, 1)
+        y = layers.band_gated(x, w, offsets_of(lengths, first), activation="gelu")
+        dx, dw = torch.autograd.grad(y, [x, w], dy)
+        ref, size = gated_reference(x, w, None, lengths, first, "gelu", dy)
+        close(y, ref[0], size[0], "y", 2.0 ** -20, 2.0 ** -25)
+        close(dx, ref[1], size[1], "dx", sums_of(dtype), 2.0 ** -25)
+        close(dw, ref[2], size[2], "dw", sums_of(dtype), 2.0 ** -25)
+        for t in (y, dx):
+            assert t[:, :first].abs().max() == 0 and t[:, first + 167:].abs().max() == 0
