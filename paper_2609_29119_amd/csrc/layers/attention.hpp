@@ -112,8 +112,6 @@ struct KeyRange {
     }
 };
 
-typedef __attribute__((address_space(3))) void lds_void;
-
 // One tile of BN rows x DP columns of two tensors into LDS. Wide tensors go
 // there directly, 16 bytes a lane (a wave fills 1 KB of consecutive LDS, so
 // the lanes fetch the chunks that belong to their places): no registers, no
@@ -185,12 +183,6 @@ template <class T, int DP, int BN, bool WIDE> struct Loader {
         }
     }
 };
-
-// Every LDS write of this wave, the direct ones too, is done; then all waves'.
-__device__ inline void tile_barrier() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
-}
 
 // S^T of 32 keys (rows row0 .. of a tile) and 32 queries. With a bias (of the
 // tile's keys: 0, or -inf for one that is not there or not kept; its row is

@@ -67,6 +67,7 @@ DecayArgs decay_args(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, int64_t 
     a.off = r->offsets;
     a.rows = static_cast<int>(r->rows);
     a.n_bands = static_cast<int>(r->n_bands);
+    a.batch = static_cast<int>(r->batch);
     a.kv_heads = static_cast<int>(s->n_kv_heads);
     a.dim = static_cast<int>(s->head_dim);
     a.units = static_cast<int>(heads);
@@ -93,7 +94,10 @@ int run_decay(int dtype, const nsgcqt_rows* r, const DecayArgs& a, DecayArgs sum
     sums.units = n_sums * a.kv_heads;
     const int64_t items = product(r->batch, static_cast<int64_t>(a.items)), walk = product(items, a.units),
                   sum = product(items, sums.units);
-    const int64_t parts = (static_cast<int64_t>(a.dim) * a.dim + 255) / 256;
+    // four elements of a state at once where both kinds of states are aligned for it
+    const bool quads = a.dim % 2 == 0 && !misaligned(a.state, 16) && !misaligned(a.job[0].part, 16) && !misaligned(a.job[1].part, 16);
+    const int64_t part = quads ? decay_scan_part<4>() : decay_scan_part<1>();
+    const int64_t parts = (static_cast<int64_t>(a.dim) * a.dim + part - 1) / part;
     const int64_t scan = product(r->batch, r->n_bands, sums.units, parts);
     CHECK_TRY(check_grid(walk));
     CHECK_TRY(check_grid(sum));
@@ -106,7 +110,7 @@ int run_decay(int dtype, const nsgcqt_rows* r, const DecayArgs& a, DecayArgs sum
         if (several) {
             LAUNCH_TRY(k_decay_sum<T, DP, kWide>, dim3(static_cast<unsigned>(sum)), block, 0, st, sums);
             for (; sums.first_block < scan; sums.first_block += kMaxGrid)
-                LAUNCH_TRY(k_decay_scan, dim3(static_cast<unsigned>(std::min(scan - sums.first_block, kMaxGrid))),
+                LAUNCH_TRY(quads ? k_decay_scan<4> : k_decay_scan<1>, dim3(static_cast<unsigned>(std::min(scan - sums.first_block, kMaxGrid))),
                            dim3(256), 0, st, sums);
         }
         LAUNCH_TRY(k_decay<T, DP, kWide>, dim3(static_cast<unsigned>(walk)), block, 0, st, a);

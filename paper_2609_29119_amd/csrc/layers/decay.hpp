@@ -36,7 +36,7 @@ struct DecayArgs {
     const uint8_t* keep;
     int64_t keep_batch;
     const int64_t* off;
-    int rows, n_bands, kv_heads, dim;
+    int rows, n_bands, batch, kv_heads, dim;
     int units;                // result heads of all jobs
     int shift;                // of a segment's length
     unsigned items;           // work items of a signal
@@ -88,7 +88,8 @@ template <class T, int RB> __device__ inline frag<T> read_turned_state(const cha
     }
 }
 
-// What a workgroup of either kernel works on.
+// What a workgroup of either kernel works on. Blocks begin at the end of the
+// row: where bands grow along it, the longest segments come first.
 struct DecayPlace {
     int job, head, kv;
     int64_t b;
@@ -97,13 +98,13 @@ struct DecayPlace {
     bool outside;   // tokens that no band holds
     bool several;   // the band has more than one segment
     __device__ DecayPlace(const DecayArgs& a, int lane) {
-        const unsigned id = die_order(blockIdx.x, gridDim.x), rest = id / a.units;
+        const unsigned id = gridDim.x - 1 - die_order(blockIdx.x, gridDim.x), rest = id / a.units;
         head = static_cast<int>(id - rest * a.units);
         job = 0;
         while (head >= a.job[job].heads) head -= a.job[job++].heads;
         kv = head / a.job[job].per;
-        b = rest / a.items;
-        seg = find_tile<int>(a.off, a.n_bands, a.rows, 1, a.shift, static_cast<int>(rest % a.items), lane);
+        b = rest % a.batch;
+        seg = find_tile<int>(a.off, a.n_bands, a.rows, 1, a.shift, static_cast<int>(rest / a.batch), lane);
         n = min(seg.len - seg.first, 1 << a.shift);
         outside = seg.band < 0 || seg.band >= a.n_bands;
         several = seg.len > 1 << a.shift;
@@ -111,30 +112,58 @@ struct DecayPlace {
     __device__ int64_t token(int t, bool reverse) const {   // the row's token of the segment's t-th
         return seg.start + (reverse ? seg.len - 1 - seg.first - t : seg.first + t);
     }
+    // keep of tile `tile`, a bit for each of its tokens (all set without keep)
+    __device__ unsigned kept(const DecayArgs& a, bool reverse, int tile, int lane) const {
+        const int t = kDecayTile * tile + (lane & 31);
+        const bool k = t < n && (!a.keep || a.keep[b * a.keep_batch + token(t, reverse)]);
+        return static_cast<unsigned>(__ballot(k));
+    }
 };
 
-// 32 tokens of b and c of one head, as registers on their way to LDS: 2 chunks of a thread each.
-template <class T, int DP, bool WIDE> struct DecaySources {
-    static constexpr int kThreads = 2 * DP, RB = row_bytes<T, DP>();
-    frag<T> fb[2], fc[2];
-    __device__ void fetch(const DecayArgs& a, const DecayJob& j, const DecayPlace& p, int t0, int head, int tid) {
+// 32 tokens of one head of one tensor on their way into an LDS tile. Wide
+// tensors go there directly: a wave's load fills 1 KB of it, its lanes fetch
+// the chunks that belong there, and those whose token or column is not there
+// or not kept aim past the buffer's end, which gives zeros. Other tensors go
+// through registers, two chunks a thread.
+template <class T, int DP, bool WIDE> struct DecayLoad {
+    static constexpr int kThreads = 2 * DP, RB = row_bytes<T, DP>(), kLoads = kDecayTile * RB / 1024,
+                         kEach = (kLoads + DP / 32 - 1) / (DP / 32);
+    static constexpr unsigned kPast = 0x80000000u;   // past every tile, and less than 2^30 from its end
+    frag<T> f[WIDE ? 1 : 2];
+    __device__ void fetch(char* tile, const DecayArgs& a, const View& v, const DecayPlace& p, int t0, int head, bool reverse,
+                          unsigned kept, int tid) {
+        const int n = min(p.n - t0, kDecayTile);
+        const T* base = decay_row<T>(v, p.b, p.token(reverse ? t0 + n - 1 : t0, reverse), head);
+        if constexpr (WIDE) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass does not know a buffer's type
+            const unsigned row = static_cast<unsigned>(v.row) * sizeof(T);
+            const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, n * row, 0x00020000);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int c = tid + kThreads * e, t = t0 + c / (DP / 8), d = c % (DP / 8) * 8;
-            bool there = t < p.n;
-            const int64_t row = p.token(there ? t : 0, j.reverse);
-            if (a.keep && !j.keep_result) there = there && a.keep[p.b * a.keep_batch + row];
-            const int n = there ? a.dim - d : 0;
-            fb[e] = load8<T, WIDE>(decay_row<T>(j.b, p.b, row, head) + d, n, d > 0);
-            fc[e] = load8<T, WIDE>(decay_row<T>(j.c, p.b, row, head) + d, n, d > 0);
+            for (int e = 0; e < kEach; ++e) {
+                const int load = wave_number() * kEach + e;
+                if (kLoads % (DP / 32) && load >= kLoads) break;
+                const int byte = load * 1024 + (tid & 63) * 16, r = byte / RB;
+                const unsigned d = ((byte % RB / 16) ^ turn(r)) * 16;
+                const bool there = (kept >> r & 1) && d < a.dim * sizeof(T);   // (tokens that are not there are not kept)
+                const unsigned at = there ? static_cast<unsigned>(reverse ? n - 1 - r : r) * row + d : kPast;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(tile + load * 1024), 16, at, 0, 0, 0);
+            }
+#endif
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c = tid + kThreads * e, r = c / (DP / 8), d = c % (DP / 8) * 8;
+                f[e] = load8<T, false>(base + (reverse ? n - 1 - r : r) * v.row + d, kept >> r & 1 ? a.dim - d : 0, d > 0);
+            }
         }
     }
-    __device__ void put(char* tb, char* tc, int tid) const {
+    __device__ void put(char* tile, int tid) const {
+        if constexpr (!WIDE) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int c = tid + kThreads * e;
-            write8<T, RB>(tb, c / (DP / 8), c % (DP / 8), fb[e]);
-            write8<T, RB>(tc, c / (DP / 8), c % (DP / 8), fc[e]);
+            for (int e = 0; e < 2; ++e) {
+                const int c = tid + kThreads * e;
+                write8<T, RB>(tile, c / (DP / 8), c % (DP / 8), f[e]);
+            }
         }
     }
 };
@@ -173,46 +202,39 @@ __device__ inline float* decay_state_of(const DecayArgs& a, const DecayJob& j, c
 // of the state each, in registers for the whole segment; the score tile, which
 // all of them need, is formed by each (8 of 44 products at heads of 128). All
 // products are formed transposed, so that the scores, the state and the result
-// go from one to the next without a trip through LDS; only b and c do, to be
-// turned.
+// go from one to the next without a trip through LDS.
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
+__global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_decay(DecayArgs a) {
     constexpr int RB = row_bytes<T, DP>(), ND = DP / 32, NK = DP / 16;
-    constexpr bool kHold = sizeof(T) == 2 || DP <= 64;   // a's fragments stay in registers between their two uses
-    constexpr bool kEarly = kHold || DP <= 96 || WIDE;   // the next sources are on their way while these are computed
-    __shared__ __align__(128) char tiles[2][2][kDecayTile * RB];
+    constexpr bool kEarly = WIDE || sizeof(T) == 2;   // the next tiles are on their way while these are computed
+    __shared__ __align__(128) char ta[2][kDecayTile * RB], tb[2][kDecayTile * RB], tc[2][kDecayTile * RB];
     __shared__ float power[kDecayTile + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const DecayPlace p(a, lane);
     if (!p.seg.live) return;
     const DecayJob& j = a.job[p.job];
+    const bool reverse = j.reverse;
     if (p.outside) {
         for (int t = m; t < p.n; t += 32)
-            store_column<T>(decay_row<T>(j.out, p.b, p.token(t, j.reverse), p.head), zero16(), 32 * wave, a.dim, WIDE, lane);
+            store_column<T>(decay_row<T>(j.out, p.b, p.token(t, reverse), p.head), zero16(), 32 * wave, a.dim, WIDE, lane);
         return;
     }
-    DecaySources<T, DP, WIDE> next;
-    next.fetch(a, j, p, 0, p.kv * j.many, tid);
-    frag<T> af[kHold ? NK : 1];
-    const T* ap;      // this lane's row of a, and whether it is there and kept
-    bool mine, kept;
-    auto a_row = [&](int t0) {
-        mine = t0 + m < p.n;
-        const int64_t row = p.token(mine ? t0 + m : 0, j.reverse);
-        kept = mine && !(a.keep && j.keep_result && !a.keep[p.b * a.keep_batch + row]);
-        ap = decay_row<T>(j.a, p.b, row, p.head);
+    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
+    unsigned kept = p.kept(a, reverse, 0, lane), kept_next = 0;
+    DecayLoad<T, DP, WIDE> la, lb, lc;
+    // (where keep takes out results, the sources are all those that exist)
+    auto exist = [&](int tile) { return p.n - kDecayTile * tile >= kDecayTile ? ~0u : (1u << (p.n - kDecayTile * tile)) - 1; };
+    auto fetch_a = [&](int tile, unsigned k) {
+        la.fetch(ta[tile & 1], a, j.a, p, kDecayTile * tile, p.head, reverse, j.keep_result ? k : exist(tile), tid);
     };
-    auto a_at = [&](int x) {
-        return load8<T, WIDE>(ap + 16 * x + 8 * h, kept ? a.dim - 16 * x - 8 * h : 0, x + h > 0);
+    auto fetch_bc = [&](int stage, int tile, int g, unsigned k) {
+        const unsigned use = j.keep_result ? exist(tile) : k;
+        lb.fetch(tb[stage & 1], a, j.b, p, kDecayTile * tile, p.kv * j.many + g, reverse, use, tid);
+        lc.fetch(tc[stage & 1], a, j.c, p, kDecayTile * tile, p.kv * j.many + g, reverse, use, tid);
     };
-    auto fetch_a = [&]() {
-        if constexpr (kHold) {
-#pragma unroll
-            for (int x = 0; x < NK; ++x) af[x] = a_at(x);
-        }
-    };
-    a_row(0);
-    fetch_a();
+    fetch_a(0, kept);
+    fetch_bc(0, 0, 0, kept);
+    if (count > 1) kept_next = p.kept(a, reverse, 1, lane);
     const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
     if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
     acc16 s[ND];
@@ -231,8 +253,10 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
                 if (row < a.dim && col < a.dim) s[d][r] = from[row * sd + col * sc];
             }
     }
-    next.put(tiles[0][0], tiles[0][1], tid);
-    __syncthreads();
+    la.put(ta[0], tid);
+    lb.put(tb[0], tid);
+    lc.put(tc[0], tid);
+    tile_barrier();
     float fade[16];   // decay^(i - j) where j <= i
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -240,20 +264,27 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
         fade[r] = lag < 0 ? 0.f : power[lag];
     }
     const float up = power[m + 1], across = power[kDecayTile];
-    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
     acc16 out;
     int tile = 0, g = 0;
     for (int stage = 0; stage < stages; ++stage) {
         const bool more = stage + 1 < stages, end = g + 1 == j.many, last = tile + 1 == count;
-        const char *tb = tiles[stage & 1][0], *tc = tiles[stage & 1][1];
-        const int next_t = kDecayTile * (end ? tile + 1 : tile), next_head = p.kv * j.many + (end ? 0 : g + 1);
-        if (kEarly && more) next.fetch(a, j, p, next_t, next_head, tid);
+        const char *xa = ta[tile & 1], *xb = tb[stage & 1], *xc = tc[stage & 1];
+        const unsigned kept_now = kept;
+        if (end) kept = kept_next;
+        const int next_tile = end ? tile + 1 : tile, next_g = end ? 0 : g + 1;
+        auto fetch = [&]() __attribute__((always_inline)) {
+            if (!more) return;
+            if (end) fetch_a(next_tile, kept);
+            fetch_bc(stage + 1, next_tile, next_g, kept);
+        };
+        if (kEarly) fetch();
+        if (end && tile + 2 < count) kept_next = a.keep ? p.kept(a, reverse, tile + 2, lane) : exist(tile + 2);
         if (g == 0) {
             out = zero16();
             if (some) {
                 each<NK>([&](auto x) __attribute__((always_inline)) {
-                    const auto af_x = data_of(kHold ? af[kHold ? x.value : 0] : a_at(x.value));
-                    out = product(sum_of<T, 2>(octet(s[x.value / 2], x.value % 2)), af_x, out);
+                    const auto af = data_of(read8<T, RB>(xa, m, 2 * x.value + h));
+                    out = product(sum_of<T, 2>(octet(s[x.value / 2], x.value % 2)), af, out);
                 });
                 out *= up;
 #pragma unroll
@@ -262,26 +293,21 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
         }
         acc16 q = zero16();
         each<NK>([&](auto x) __attribute__((always_inline)) {
-            const frag<T> af_x = kHold ? af[kHold ? x.value : 0] : a_at(x.value);
-            q = mma(read8<T, RB>(tb, m, 2 * x.value + h), af_x, q);
+            q = mma(read8<T, RB>(xb, m, 2 * x.value + h), read8<T, RB>(xa, m, 2 * x.value + h), q);
         });
-        T* to = mine ? decay_row<T>(j.out, p.b, p.token(kDecayTile * tile + m, j.reverse), p.head) : nullptr;
-        const bool drop = mine && !kept;
-        if (end && !last) {
-            a_row(kDecayTile * (tile + 1));
-            fetch_a();
-        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) q[r] *= fade[r];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const frag<T> cf = read_turned<T, RB>(tc, 16 * x, 32 * wave, lane);
+            const frag<T> cf = read_turned<T, RB>(xc, 16 * x, 32 * wave, lane);
             out = product(data_of(cf), sum_of<T, 2>(octet(q, x)), out);
-            if (!last) decay_add<T, DP, 2>(s, tb, cf, decay_weights(power, kDecayTile - 1, x, h), x, lane);
+            if (!last) decay_add<T, DP, 2>(s, xb, cf, decay_weights(power, kDecayTile - 1, x, h), x, lane);
         }
         if (end) {
+            const int t = kDecayTile * tile + m;
+            T* to = t < p.n ? decay_row<T>(j.out, p.b, p.token(t, reverse), p.head) : nullptr;
             out *= a.scale;
-            if (drop) out = zero16();
+            if (j.keep_result && !(kept_now >> m & 1)) out = zero16();
             store_column<T>(to, out, 32 * wave, a.dim, WIDE, lane);
             some = true;
             g = 0;
@@ -289,9 +315,13 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
         } else {
             ++g;
         }
-        if (!kEarly && more) next.fetch(a, j, p, next_t, next_head, tid);
-        if (more) next.put(tiles[(stage + 1) & 1][0], tiles[(stage + 1) & 1][1], tid);
-        __syncthreads();
+        if (more) {
+            if (!kEarly) fetch();
+            if (end) la.put(ta[tile & 1], tid);
+            lb.put(tb[(stage + 1) & 1], tid);
+            lc.put(tc[(stage + 1) & 1], tid);
+        }
+        tile_barrier();
     }
 }
 
@@ -302,15 +332,26 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay(DecayArgs a) {
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
     constexpr int RB = row_bytes<T, DP>(), ND = DP / 32;
-    __shared__ __align__(128) char tiles[2][2][kDecayTile * RB];
+    __shared__ __align__(128) char tb[2][kDecayTile * RB], tc[2][kDecayTile * RB];
     __shared__ float power[kDecayTile + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const DecayPlace p(a, lane);
     if (!p.seg.live || p.outside || p.several == a.single) return;
     const DecayJob& j = a.job[p.job];
     if (!a.state && p.seg.first + p.n == p.seg.len) return;
-    DecaySources<T, DP, WIDE> next;
-    next.fetch(a, j, p, 0, p.kv * j.many, tid);
+    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
+    DecayLoad<T, DP, WIDE> lb, lc;
+    auto use = [&](int tile) {
+        if (a.keep && !j.keep_result) return p.kept(a, j.reverse, tile, lane);
+        return p.n - kDecayTile * tile >= kDecayTile ? ~0u : (1u << (p.n - kDecayTile * tile)) - 1;
+    };
+    auto fetch = [&](int stage, int tile, int g, unsigned k) {
+        lb.fetch(tb[stage & 1], a, j.b, p, kDecayTile * tile, p.kv * j.many + g, j.reverse, k, tid);
+        lc.fetch(tc[stage & 1], a, j.c, p, kDecayTile * tile, p.kv * j.many + g, j.reverse, k, tid);
+    };
+    unsigned kept = use(0), kept_next = 0;
+    fetch(0, 0, 0, kept);
+    if (count > 1) kept_next = use(1);
     const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
     if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
     bool there;
@@ -324,15 +365,17 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
             const int row = 32 * d + 16 * (r >> 3) + 8 * h + (r & 7);
             s[d][r] = a.single && row < a.dim && col < a.dim ? to[row * a.dim + col] : 0.f;
         }
-    next.put(tiles[0][0], tiles[0][1], tid);
-    __syncthreads();
-    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
+    lb.put(tb[0], tid);
+    lc.put(tc[0], tid);
+    tile_barrier();
     int tile = 0, g = 0;
     for (int stage = 0; stage < stages; ++stage) {
         const bool more = stage + 1 < stages, end = g + 1 == j.many;
-        const char *tb = tiles[stage & 1][0], *tc = tiles[stage & 1][1];
+        const char *xb = tb[stage & 1], *xc = tc[stage & 1];
         const int n = min(p.n - kDecayTile * tile, kDecayTile);
-        if (more) next.fetch(a, j, p, kDecayTile * (end ? tile + 1 : tile), p.kv * j.many + (end ? 0 : g + 1), tid);
+        if (end) kept = kept_next;
+        if (more) fetch(stage + 1, end ? tile + 1 : tile, end ? 0 : g + 1, kept);
+        if (end && tile + 2 < count) kept_next = use(tile + 2);
         if (g == 0) {
             const float across = power[n];
 #pragma unroll
@@ -340,7 +383,7 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-            decay_add<T, DP, 3>(s, tb, read_turned<T, RB>(tc, 16 * x, 32 * wave, lane),
+            decay_add<T, DP, 3>(s, xb, read_turned<T, RB>(xc, 16 * x, 32 * wave, lane),
                                 decay_weights(power, n - 1, x, h), x, lane);
         if (end) {
             g = 0;
@@ -348,8 +391,11 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
         } else {
             ++g;
         }
-        if (more) next.put(tiles[(stage + 1) & 1][0], tiles[(stage + 1) & 1][1], tid);
-        __syncthreads();
+        if (more) {
+            lb.put(tb[(stage + 1) & 1], tid);
+            lc.put(tc[(stage + 1) & 1], tid);
+        }
+        tile_barrier();
     }
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -362,11 +408,13 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
 
 // From what each segment adds to the state that each starts with, in place,
 // along the segments of every band of several; `state` goes to the band's end.
-// A thread takes one element.
-__global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
-    const int size = a.dim * a.dim, parts = (size + 255) / 256;
+// A thread takes V neighbouring elements.
+template <int V> constexpr int decay_scan_part() { return 256 * V; }   // elements of a workgroup
+template <int V> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
+    typedef float vec __attribute__((ext_vector_type(V)));
+    const int size = a.dim * a.dim, parts = (size + decay_scan_part<V>() - 1) / decay_scan_part<V>();
     int64_t id = a.first_block + blockIdx.x;
-    const int e = static_cast<int>(id % parts) * 256 + static_cast<int>(threadIdx.x);
+    const int e = (static_cast<int>(id % parts) * 256 + static_cast<int>(threadIdx.x)) * V;
     id /= parts;
     const int u = static_cast<int>(id % a.units), job = u / a.kv_heads, kv = u % a.kv_heads;
     id /= a.units;
@@ -380,22 +428,23 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
     const int64_t step = static_cast<int64_t>(a.kv_heads) * size;
     float* x = a.job[job].part + ((b * slot_count(a.rows, a.shift) + slot_of(start, 0, a.shift)) * a.kv_heads + kv) * size + e;
     float* st = a.state ? a.state + ((b * a.n_bands + band) * a.kv_heads + kv) * size + e : nullptr;
-    float s = st ? *st : 0.f;
-    constexpr int kAhead = 16;
+    auto at = [&](int i) -> vec& { return *reinterpret_cast<vec*>(x + i * step); };
+    vec s = st ? *reinterpret_cast<vec*>(st) : vec(0.f);
+    constexpr int kAhead = V == 1 ? 16 : 8;
     for (int i = 0; i + 1 < count; i += kAhead) {
-        float add[kAhead];
+        vec add[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) add[k] = i + k + 1 < count ? x[(i + k) * step] : 0.f;
+        for (int k = 0; k < kAhead; ++k) add[k] = i + k + 1 < count ? at(i + k) : vec(0.f);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
             if (i + k + 1 < count) {
-                x[(i + k) * step] = s;
-                s = fmaf(across, s, add[k]);
+                at(i + k) = s;
+                s = across * s + add[k];
             }
     }
-    const float add = st ? x[(count - 1) * step] : 0.f;
-    x[(count - 1) * step] = s;
-    if (st) *st = fmaf(decay_power(l2, len - (static_cast<int64_t>(count - 1) << a.shift)), s, add);
+    const vec add = st ? at(count - 1) : vec(0.f);
+    at(count - 1) = s;
+    if (st) *reinterpret_cast<vec*>(st) = decay_power(l2, len - (static_cast<int64_t>(count - 1) << a.shift)) * s + add;
 }
 
 // ------------------------------------------------------------- single tokens

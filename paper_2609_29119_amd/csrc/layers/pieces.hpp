@@ -13,16 +13,25 @@ template <class F, int N> struct Pieces { F p[N]; };
 template <class T> constexpr int data_pieces() { return std::is_same<T, _Float16>::value ? 2 : 1; }
 template <class T> using piece = std::conditional_t<std::is_same<T, float>::value, f8, b8>;
 
+// All but the last piece are the value's next 8 bits as they are (two values'
+// upper halves are one instruction), the last one is rounded.
 template <int N> __device__ inline Pieces<b8, N> cut(f8 x) {
     Pieces<b8, N> r;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i + 1 < N; ++i) {
+        u4 u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            r.p[i][j] = static_cast<__bf16>(x[j]);
-            x[j] -= static_cast<float>(r.p[i][j]);
+        for (int j = 0; j < 4; ++j) {
+            const float even = x[2 * j], odd = x[2 * j + 1];
+            const unsigned e = __builtin_bit_cast(unsigned, even), o = __builtin_bit_cast(unsigned, odd);
+            u[j] = __builtin_amdgcn_perm(o, e, 0x07060302u);
+            x[2 * j] = even - __builtin_bit_cast(float, e & 0xffff0000u);
+            x[2 * j + 1] = odd - __builtin_bit_cast(float, o & 0xffff0000u);
         }
+        r.p[i] = __builtin_bit_cast(b8, u);
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.p[N - 1][j] = static_cast<__bf16>(x[j]);
     return r;
 }
 __device__ inline f8 wide_of(f8 f) { return f; }

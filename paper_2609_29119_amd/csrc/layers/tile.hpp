@@ -193,6 +193,13 @@ template <class T, int RB> __device__ inline void write8(char* tile, int row, in
 }
 
 typedef __attribute__((address_space(3))) s4 lds_s4;
+typedef __attribute__((address_space(3))) void lds_void;   // where a direct load into LDS goes
+
+// Every LDS write of this wave, the direct ones too, is done; then all waves'.
+__device__ inline void tile_barrier() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+}
 
 // A fragment of the tile's transpose: for column col0 + (lane % 32), rows
 // row0 + 4 h + {0..3} and row0 + 8 + 4 h + {0..3}, h = lane / 32 (row0 and
