@@ -124,36 +124,58 @@ struct DecayPlace {
 // tensors go there directly: a wave's load fills 1 KB of it, its lanes fetch
 // the chunks that belong there, and those whose token or column is not there
 // or not kept aim past the buffer's end, which gives zeros. Other tensors go
-// through registers, two chunks a thread.
+// through registers, two chunks a thread. W' numbers tokens from the band's
+// end: its buffers begin at the tile's last token.
 template <class T, int DP, bool WIDE> struct DecayLoad {
     static constexpr int kThreads = 2 * DP, RB = row_bytes<T, DP>(), kLoads = kDecayTile * RB / 1024,
-                         kEach = (kLoads + DP / 32 - 1) / (DP / 32);
+                         kEach = WIDE ? (kLoads + DP / 32 - 1) / (DP / 32) : 2;
     static constexpr unsigned kPast = 0x80000000u;   // past every tile, and less than 2^30 from its end
+    const char* base;    // of the first tile's buffer
+    int64_t step, head;  // bytes from tile to tile, from head to head
+    unsigned row;        // and from token to token
+    bool reverse;
+    unsigned at[WIDE ? kEach : 1];
     frag<T> f[WIDE ? 1 : 2];
-    __device__ void fetch(char* tile, const DecayArgs& a, const View& v, const DecayPlace& p, int t0, int head, bool reverse,
-                          unsigned kept, int tid) {
-        const int n = min(p.n - t0, kDecayTile);
-        const T* base = decay_row<T>(v, p.b, p.token(reverse ? t0 + n - 1 : t0, reverse), head);
+
+    static __device__ int token_of(int e, int tid) {   // of the thread's e-th chunk in a tile
+        return WIDE ? ((wave_number() * kEach + e) * 1024 + (tid & 63) * 16) / RB : (tid + kThreads * e) / (DP / 8);
+    }
+    __device__ DecayLoad(const DecayArgs& a, const View& v, const DecayPlace& p, int first_head, bool rev, int tid) {
+        reverse = rev;
+        row = static_cast<unsigned>(v.row) * sizeof(T);
+        step = (rev ? -v.row : v.row) * static_cast<int64_t>(kDecayTile * sizeof(T));
+        head = v.head * static_cast<int64_t>(sizeof(T));
+        base = reinterpret_cast<const char*>(decay_row<T>(v, p.b, p.token(rev ? kDecayTile - 1 : 0, rev), first_head));
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int byte = (wave_number() * kEach + e) * 1024 + (tid & 63) * 16, r = byte / RB;
+                const unsigned d = ((byte % RB / 16) ^ turn(r)) * 16;
+                at[e] = d < a.dim * sizeof(T) ? (rev ? kDecayTile - 1 - r : r) * row + d : kPast;
+            }
+        }
+    }
+    // kept: a bit for each of the tile's tokens that are there and kept
+    __device__ void fetch(char* tile, const DecayArgs& a, int number, int g, unsigned kept, int tid) {
+        const char* from = base + number * step + g * head;
         if constexpr (WIDE) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass does not know a buffer's type
-            const unsigned row = static_cast<unsigned>(v.row) * sizeof(T);
-            const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, n * row, 0x00020000);
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, kDecayTile * row, 0x00020000);
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 const int load = wave_number() * kEach + e;
                 if (kLoads % (DP / 32) && load >= kLoads) break;
-                const int byte = load * 1024 + (tid & 63) * 16, r = byte / RB;
-                const unsigned d = ((byte % RB / 16) ^ turn(r)) * 16;
-                const bool there = (kept >> r & 1) && d < a.dim * sizeof(T);   // (tokens that are not there are not kept)
-                const unsigned at = there ? static_cast<unsigned>(reverse ? n - 1 - r : r) * row + d : kPast;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(tile + load * 1024), 16, at, 0, 0, 0);
+                unsigned x = at[e];
+                if (kept != ~0u && !(kept >> token_of(e, tid) & 1)) x = kPast;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lds_void*)(tile + load * 1024), 16, x, 0, 0, 0);
             }
 #endif
         } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int c = tid + kThreads * e, r = c / (DP / 8), d = c % (DP / 8) * 8;
-                f[e] = load8<T, false>(base + (reverse ? n - 1 - r : r) * v.row + d, kept >> r & 1 ? a.dim - d : 0, d > 0);
+                const int r = token_of(e, tid), d = (tid + kThreads * e) % (DP / 8) * 8;
+                const T* p = reinterpret_cast<const T*>(from + static_cast<int64_t>(reverse ? kDecayTile - 1 - r : r) * row);
+                f[e] = load8<T, false>(p + d, kept >> r & 1 ? a.dim - d : 0, d > 0);
             }
         }
     }
@@ -219,26 +241,26 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
             store_column<T>(decay_row<T>(j.out, p.b, p.token(t, reverse), p.head), zero16(), 32 * wave, a.dim, WIDE, lane);
         return;
     }
-    const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
-    unsigned kept = p.kept(a, reverse, 0, lane), kept_next = 0;
-    DecayLoad<T, DP, WIDE> la, lb, lc;
+    const int count = (p.n + kDecayTile - 1) / kDecayTile;
+    DecayLoad<T, DP, WIDE> la(a, j.a, p, p.head, reverse, tid), lb(a, j.b, p, p.kv * j.many, reverse, tid),
+        lc(a, j.c, p, p.kv * j.many, reverse, tid);
     // (where keep takes out results, the sources are all those that exist)
     auto exist = [&](int tile) { return p.n - kDecayTile * tile >= kDecayTile ? ~0u : (1u << (p.n - kDecayTile * tile)) - 1; };
-    auto fetch_a = [&](int tile, unsigned k) {
-        la.fetch(ta[tile & 1], a, j.a, p, kDecayTile * tile, p.head, reverse, j.keep_result ? k : exist(tile), tid);
-    };
+    auto kept_of = [&](int tile) { return a.keep ? p.kept(a, reverse, tile, lane) : exist(tile); };
+    auto fetch_a = [&](int tile, unsigned k) { la.fetch(ta[tile & 1], a, tile, 0, j.keep_result ? k : exist(tile), tid); };
     auto fetch_bc = [&](int stage, int tile, int g, unsigned k) {
         const unsigned use = j.keep_result ? exist(tile) : k;
-        lb.fetch(tb[stage & 1], a, j.b, p, kDecayTile * tile, p.kv * j.many + g, reverse, use, tid);
-        lc.fetch(tc[stage & 1], a, j.c, p, kDecayTile * tile, p.kv * j.many + g, reverse, use, tid);
+        lb.fetch(tb[stage & 1], a, tile, g, use, tid);
+        lc.fetch(tc[stage & 1], a, tile, g, use, tid);
     };
+    unsigned kept = kept_of(0), kept_next = 0;
     fetch_a(0, kept);
     fetch_bc(0, 0, 0, kept);
-    if (count > 1) kept_next = p.kept(a, reverse, 1, lane);
+    if (count > 1) kept_next = kept_of(1);
     const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
     if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
     acc16 s[ND];
-    bool some;    // there is a state
+    bool some;
     const float* from = decay_state_of(a, j, p, some);
     const int col = 32 * wave + m;
 #pragma unroll
@@ -257,31 +279,34 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
     lb.put(tb[0], tid);
     lc.put(tc[0], tid);
     tile_barrier();
-    float fade[16];   // decay^(i - j) where j <= i
+    float fade[16];   // scale decay^(i - j) where j <= i
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int lag = m - (8 * (r >> 2) + 4 * h + (r & 3));
-        fade[r] = lag < 0 ? 0.f : power[lag];
+        fade[r] = lag < 0 ? 0.f : power[lag] * a.scale;
     }
-    const float up = power[m + 1], across = power[kDecayTile];
-    acc16 out;
-    int tile = 0, g = 0;
-    for (int stage = 0; stage < stages; ++stage) {
-        const bool more = stage + 1 < stages, end = g + 1 == j.many, last = tile + 1 == count;
-        const char *xa = ta[tile & 1], *xb = tb[stage & 1], *xc = tc[stage & 1];
+    const float up = power[m + 1] * a.scale, across = power[kDecayTile];
+    T* to = decay_row<T>(j.out, p.b, p.token(m, reverse), p.head);   // (of the last tile, perhaps past the segment: not used)
+    const int64_t to_step = (reverse ? -j.out.row : j.out.row) * kDecayTile;
+    int stage = 0;
+    for (int tile = 0; tile < count; ++tile) {
+        const bool last = tile + 1 == count;
+        const char* xa = ta[tile & 1];
         const unsigned kept_now = kept;
-        if (end) kept = kept_next;
-        const int next_tile = end ? tile + 1 : tile, next_g = end ? 0 : g + 1;
-        auto fetch = [&]() __attribute__((always_inline)) {
-            if (!more) return;
-            if (end) fetch_a(next_tile, kept);
-            fetch_bc(stage + 1, next_tile, next_g, kept);
-        };
-        if (kEarly) fetch();
-        if (end && tile + 2 < count) kept_next = a.keep ? p.kept(a, reverse, tile + 2, lane) : exist(tile + 2);
-        if (g == 0) {
-            out = zero16();
-            if (some) {
+        acc16 out = zero16();
+        for (int g = 0; g < j.many; ++g, ++stage) {
+            const bool end = g + 1 == j.many, more = !(end && last);
+            const char *xb = tb[stage & 1], *xc = tc[stage & 1];
+            const int next_tile = end ? tile + 1 : tile;
+            if (end) kept = kept_next;
+            auto fetch = [&]() __attribute__((always_inline)) {
+                if (!more) return;
+                if (end) fetch_a(next_tile, kept);
+                fetch_bc(stage + 1, next_tile, end ? 0 : g + 1, kept);
+            };
+            if (kEarly) fetch();
+            if (end && tile + 2 < count) kept_next = kept_of(tile + 2);
+            if (g == 0) {
                 each<NK>([&](auto x) __attribute__((always_inline)) {
                     const auto af = data_of(read8<T, RB>(xa, m, 2 * x.value + h));
                     out = product(sum_of<T, 2>(octet(s[x.value / 2], x.value % 2)), af, out);
@@ -290,38 +315,31 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
 #pragma unroll
                 for (int d = 0; d < ND; ++d) s[d] *= across;
             }
-        }
-        acc16 q = zero16();
-        each<NK>([&](auto x) __attribute__((always_inline)) {
-            q = mma(read8<T, RB>(xb, m, 2 * x.value + h), read8<T, RB>(xa, m, 2 * x.value + h), q);
-        });
+            acc16 q = zero16();
+            each<NK>([&](auto x) __attribute__((always_inline)) {
+                q = mma(read8<T, RB>(xb, m, 2 * x.value + h), read8<T, RB>(xa, m, 2 * x.value + h), q);
+            });
 #pragma unroll
-        for (int r = 0; r < 16; ++r) q[r] *= fade[r];
+            for (int r = 0; r < 16; ++r) q[r] *= fade[r];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const frag<T> cf = read_turned<T, RB>(xc, 16 * x, 32 * wave, lane);
-            out = product(data_of(cf), sum_of<T, 2>(octet(q, x)), out);
-            if (!last) decay_add<T, DP, 2>(s, xb, cf, decay_weights(power, kDecayTile - 1, x, h), x, lane);
+            for (int x = 0; x < 2; ++x) {
+                const frag<T> cf = read_turned<T, RB>(xc, 16 * x, 32 * wave, lane);
+                out = product(data_of(cf), sum_of<T, 2>(octet(q, x)), out);
+                if (!last) decay_add<T, DP, 2>(s, xb, cf, decay_weights(power, kDecayTile - 1, x, h), x, lane);
+            }
+            if (more) {
+                if (!kEarly) fetch();
+                if (end) la.put(ta[next_tile & 1], tid);
+                lb.put(tb[(stage + 1) & 1], tid);
+                lc.put(tc[(stage + 1) & 1], tid);
+            }
+            if (end) {
+                if (a.keep && j.keep_result && !(kept_now >> m & 1)) out = zero16();
+                store_column<T>(kDecayTile * tile + m < p.n ? to : nullptr, out, 32 * wave, a.dim, WIDE, lane);
+                to += to_step;
+            }
+            tile_barrier();
         }
-        if (end) {
-            const int t = kDecayTile * tile + m;
-            T* to = t < p.n ? decay_row<T>(j.out, p.b, p.token(t, reverse), p.head) : nullptr;
-            out *= a.scale;
-            if (j.keep_result && !(kept_now >> m & 1)) out = zero16();
-            store_column<T>(to, out, 32 * wave, a.dim, WIDE, lane);
-            some = true;
-            g = 0;
-            ++tile;
-        } else {
-            ++g;
-        }
-        if (more) {
-            if (!kEarly) fetch();
-            if (end) la.put(ta[tile & 1], tid);
-            lb.put(tb[(stage + 1) & 1], tid);
-            lc.put(tc[(stage + 1) & 1], tid);
-        }
-        tile_barrier();
     }
 }
 
@@ -340,14 +358,14 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
     const DecayJob& j = a.job[p.job];
     if (!a.state && p.seg.first + p.n == p.seg.len) return;
     const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
-    DecayLoad<T, DP, WIDE> lb, lc;
+    DecayLoad<T, DP, WIDE> lb(a, j.b, p, p.kv * j.many, j.reverse, tid), lc(a, j.c, p, p.kv * j.many, j.reverse, tid);
     auto use = [&](int tile) {
         if (a.keep && !j.keep_result) return p.kept(a, j.reverse, tile, lane);
         return p.n - kDecayTile * tile >= kDecayTile ? ~0u : (1u << (p.n - kDecayTile * tile)) - 1;
     };
     auto fetch = [&](int stage, int tile, int g, unsigned k) {
-        lb.fetch(tb[stage & 1], a, j.b, p, kDecayTile * tile, p.kv * j.many + g, j.reverse, k, tid);
-        lc.fetch(tc[stage & 1], a, j.c, p, kDecayTile * tile, p.kv * j.many + g, j.reverse, k, tid);
+        lb.fetch(tb[stage & 1], a, tile, g, k, tid);
+        lc.fetch(tc[stage & 1], a, tile, g, k, tid);
     };
     unsigned kept = use(0), kept_next = 0;
     fetch(0, 0, 0, kept);
