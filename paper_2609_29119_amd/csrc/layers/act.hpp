@@ -14,9 +14,17 @@ __device__ inline float exp_neg(float z) {
     return __builtin_amdgcn_exp2f(y) * fmaf(rest, 0.69314718f, 1.f);
 }
 
-__device__ inline float logistic(float z) {
+// 1 / (1 + exp(-z)), and into `other` the same of -z (their sum is 1, but the
+// smaller one's last bits are not in the larger one).
+__device__ inline float logistic(float z, float& other) {
     // (past 80 the correction would meet an infinity; 1 / (1 + e^80) is below what any result shows beside it)
-    return __builtin_amdgcn_rcpf(1.f + exp_neg(fmaxf(z, -80.f)));
+    const float e = exp_neg(fmaxf(z, -80.f)), s = __builtin_amdgcn_rcpf(1.f + e);
+    other = e * s;
+    return s;
+}
+__device__ inline float logistic(float z) {
+    float other;
+    return logistic(z, other);
 }
 
 // The normal distribution's Phi(z), and exp(-z^2 / 2) into `bell`. With w =
@@ -54,8 +62,9 @@ template <int ACT> __device__ inline float act_of(float z) {
 // act(z), and its derivative into slope.
 template <int ACT> __device__ inline float act_of(float z, float& slope) {
     if constexpr (ACT == kSilu) {
-        const float s = logistic(z);
-        slope = fmaf(z * s, logistic(-z), s);   // (1 - s would lose what s has beyond 1/2)
+        float other;
+        const float s = logistic(z, other);
+        slope = fmaf(z * s, other, s);
         return z * s;
     } else if constexpr (ACT == kGelu) {
         float bell;
@@ -63,8 +72,9 @@ template <int ACT> __device__ inline float act_of(float z, float& slope) {
         slope = fmaf(0.39894228f * z, bell, phi);
         return z * phi;
     } else if constexpr (ACT == kSigmoid) {
-        const float s = logistic(z);
-        slope = s * logistic(-z);
+        float other;
+        const float s = logistic(z, other);
+        slope = s * other;
         return s;
     } else {
         slope = 1.f;

@@ -30,23 +30,29 @@ int check_state(const float* p) {
     return NSGCQT_OK;
 }
 
-// Tokens of a segment, 128 to 4096: the most that leave 1024 workgroups of one
-// head each, four on a compute unit.
-int segment_shift(int64_t batch, int64_t rows, int64_t heads) {
-    int shift = 12;
-    while (shift > 7 && product(batch, rows >> shift, heads) < 1024) --shift;
+// Tokens of a segment, 128 to 4096 (2048 for the gradients, where some heads
+// walk through them several times): the most that leave 1536 workgroups of one
+// result head each; and of a part of it, at most 1024, as many of one key head
+// (few of a ragged row's tokens lie in bands of several segments). A part's
+// state costs as much to write, join and read as 4 head_dim of its tokens: parts
+// of less than 8 head_dim tokens only below 1024 workgroups. 131,072 tokens, 8
+// heads of 128, bfloat16: 1024 tokens 445 us, 512 tokens 480, 2048 560.
+int shift_of(int64_t batch, int64_t rows, int64_t heads, int64_t dim, int shift) {
+    while (shift > 7 && product(batch, rows >> shift, heads) < (1 << shift > 8 * dim ? 1536 : 1024)) --shift;
     return shift;
 }
-
-// Bytes of the segments' states, `sums` of them a slot and key head.
-int64_t states_bytes(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, int shift, int sums) {
-    if (r->rows <= int64_t(1) << shift) return 0;   // no band has several segments
-    return workspace_of(product(4 * sums, r->batch, slot_count(r->rows, shift), s->n_kv_heads, s->head_dim * s->head_dim));
+struct DecayCut { int shift, fine; };
+DecayCut cut_of(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, bool grad) {
+    const int64_t heads = grad ? s->n_heads + 2 * s->n_kv_heads : s->n_heads;
+    const int shift = shift_of(r->batch, r->rows, heads, s->head_dim, grad ? 11 : 12);
+    return {shift, shift_of(r->batch, r->rows, (grad ? 2 : 1) * s->n_kv_heads, s->head_dim, std::min(shift, 10))};
 }
 
+// Bytes of the states within bands of several segments.
 int64_t decay_workspace(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, bool grad) {
-    const int64_t heads = grad ? s->n_heads + 2 * s->n_kv_heads : s->n_heads;
-    return states_bytes(r, s, segment_shift(r->batch, r->rows, heads), grad ? 2 : 1);
+    const DecayCut cut = cut_of(r, s, grad);
+    if (r->rows <= int64_t(1) << cut.shift) return 0;   // no band has several segments
+    return workspace_of(product(grad ? 8 : 4, r->batch, slot_count(r->rows, cut.fine), s->n_kv_heads, s->head_dim * s->head_dim));
 }
 
 int check_workspace(const void* ws, size_t have, int64_t need) {
@@ -59,7 +65,7 @@ int check_workspace(const void* ws, size_t have, int64_t need) {
     return NSGCQT_OK;
 }
 
-DecayArgs decay_args(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, int64_t heads) {
+DecayArgs decay_args(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, bool grad) {
     DecayArgs a{};
     a.log_decay = s->log_decay;
     a.keep = s->keep;
@@ -70,9 +76,10 @@ DecayArgs decay_args(const nsgcqt_rows* r, const nsgcqt_decay_shape* s, int64_t 
     a.batch = static_cast<int>(r->batch);
     a.kv_heads = static_cast<int>(s->n_kv_heads);
     a.dim = static_cast<int>(s->head_dim);
-    a.units = static_cast<int>(heads);
-    a.shift = segment_shift(r->batch, r->rows, heads);
-    a.items = static_cast<unsigned>(tile_count(a.shift, r->n_bands, 1, r->rows));
+    a.units = static_cast<int>(grad ? s->n_heads + 2 * s->n_kv_heads : s->n_heads);
+    const DecayCut cut = cut_of(r, s, grad);
+    a.shift = cut.shift;
+    a.fine = cut.fine;
     a.scale = static_cast<float>(s->scale);
     return a;
 }
@@ -92,15 +99,16 @@ template <class F> int by_decay_shape(int dtype, int64_t dim, bool wide, F f) {
 int run_decay(int dtype, const nsgcqt_rows* r, const DecayArgs& a, DecayArgs sums, int n_sums, bool wide, hipStream_t st) {
     const bool several = r->rows > int64_t(1) << a.shift;
     sums.units = n_sums * a.kv_heads;
-    const int64_t items = product(r->batch, static_cast<int64_t>(a.items)), walk = product(items, a.units),
-                  sum = product(items, sums.units);
+    const int64_t items = product(r->batch, tile_count(a.shift, a.n_bands, 1, a.rows));
+    const int64_t walk = product(items, a.units), single = product(items, sums.units);
+    const int64_t sum = product(r->batch, tile_count(a.fine, a.n_bands, 1, a.rows), sums.units);
     // four elements of a state at once where both kinds of states are aligned for it
     const bool quads = a.dim % 2 == 0 && !misaligned(a.state, 16) && !misaligned(a.job[0].part, 16) && !misaligned(a.job[1].part, 16);
     const int64_t part = quads ? decay_scan_part<4>() : decay_scan_part<1>();
     const int64_t parts = (static_cast<int64_t>(a.dim) * a.dim + part - 1) / part;
     const int64_t scan = product(r->batch, r->n_bands, sums.units, parts);
     CHECK_TRY(check_grid(walk));
-    CHECK_TRY(check_grid(sum));
+    CHECK_TRY(check_grid(std::max(single, several ? sum : 0)));
     if (several && scan == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more workgroups than 64 bits count");
     return by_decay_shape(dtype, a.dim, wide, [&](auto t, auto dp, auto w) -> int {
         using T = decltype(t);
@@ -116,7 +124,7 @@ int run_decay(int dtype, const nsgcqt_rows* r, const DecayArgs& a, DecayArgs sum
         LAUNCH_TRY(k_decay<T, DP, kWide>, dim3(static_cast<unsigned>(walk)), block, 0, st, a);
         if (a.state) {
             sums.single = true;
-            LAUNCH_TRY(k_decay_sum<T, DP, kWide>, dim3(static_cast<unsigned>(sum)), block, 0, st, sums);
+            LAUNCH_TRY(k_decay_sum<T, DP, kWide>, dim3(static_cast<unsigned>(single)), block, 0, st, sums);
         }
         return NSGCQT_OK;
     });
@@ -165,7 +173,7 @@ int nsgcqt_decay_attention(int dtype, const nsgcqt_rows* r, const nsgcqt_decay_s
     if (r->batch == 0 || r->rows == 0) return NSGCQT_OK;
     CHECK_TRY(check_log_decay(s->log_decay));
     CHECK_TRY(check_workspace(ws, ws_bytes, decay_workspace(r, s, false)));
-    DecayArgs a = decay_args(r, s, s->n_heads);
+    DecayArgs a = decay_args(r, s, false);
     a.state = state;
     a.job[0] = job_of(q, k, v, o, static_cast<float*>(ws), a, s->n_heads, false, false);
     DecayArgs sums = a;
@@ -191,7 +199,7 @@ int nsgcqt_decay_attention_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_de
     CHECK_TRY(check_log_decay(s->log_decay));
     const int64_t need = decay_workspace(r, s, true);
     CHECK_TRY(check_workspace(ws, ws_bytes, need));
-    DecayArgs a = decay_args(r, s, s->n_heads + 2 * s->n_kv_heads);
+    DecayArgs a = decay_args(r, s, true);
     float* before = static_cast<float*>(ws);   // states of what came before, k v^T, and of what follows, q do^T
     float* after = need ? before + need / 8 : before;
     a.job[0] = job_of(d_o, v, k, dq, before, a, s->n_heads, false, true);

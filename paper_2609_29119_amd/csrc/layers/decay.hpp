@@ -22,7 +22,7 @@ constexpr int kDecayTile = 32;
 // takes the sources (key head) * many + {0 .. many - 1}.
 struct DecayJob {
     View a, b, c, out;
-    float* part;         // states of segments of long bands, [batch][slots][kv_heads][dim][dim]
+    float* part;         // states within long bands, [batch][slots][kv_heads][dim][dim]
     int heads, per, many;
     bool reverse;        // W'
     bool turned;         // the states are those of the job with b and c exchanged
@@ -38,8 +38,8 @@ struct DecayArgs {
     const int64_t* off;
     int rows, n_bands, batch, kv_heads, dim;
     int units;                // result heads of all jobs
-    int shift;                // of a segment's length
-    unsigned items;           // work items of a signal
+    int shift;                // of a segment's length: what k_decay's workgroups walk through
+    int fine;                 // of a part's: what k_decay_sum's do, in bands of several segments
     int64_t first_block;      // of a launch of k_decay_scan
     bool single;              // k_decay_sum: bands of one segment, into `state`
     float scale;
@@ -94,18 +94,18 @@ struct DecayPlace {
     int job, head, kv;
     int64_t b;
     Tile<int> seg;
-    int n;          // the segment's tokens
+    int n;          // the segment's (or part's) tokens
     bool outside;   // tokens that no band holds
     bool several;   // the band has more than one segment
-    __device__ DecayPlace(const DecayArgs& a, int lane) {
+    __device__ DecayPlace(const DecayArgs& a, int shift, int lane) {
         const unsigned id = gridDim.x - 1 - die_order(blockIdx.x, gridDim.x), rest = id / a.units;
         head = static_cast<int>(id - rest * a.units);
         job = 0;
         while (head >= a.job[job].heads) head -= a.job[job++].heads;
         kv = head / a.job[job].per;
         b = rest % a.batch;
-        seg = find_tile<int>(a.off, a.n_bands, a.rows, 1, a.shift, static_cast<int>(rest / a.batch), lane);
-        n = min(seg.len - seg.first, 1 << a.shift);
+        seg = find_tile<int>(a.off, a.n_bands, a.rows, 1, shift, static_cast<int>(rest / a.batch), lane);
+        n = min(seg.len - seg.first, 1 << shift);
         outside = seg.band < 0 || seg.band >= a.n_bands;
         several = seg.len > 1 << a.shift;
     }
@@ -213,7 +213,7 @@ __device__ inline float* decay_state_of(const DecayArgs& a, const DecayJob& j, c
     const int64_t size = static_cast<int64_t>(a.dim) * a.dim;
     there = true;
     if (p.several)
-        return j.part + ((p.b * slot_count(a.rows, a.shift) + slot_of(p.seg.start, p.seg.first >> a.shift, a.shift)) *
+        return j.part + ((p.b * slot_count(a.rows, a.fine) + slot_of(p.seg.start, p.seg.first >> a.fine, a.fine)) *
                              a.kv_heads + p.kv) * size;
     if (a.state) return a.state + ((p.b * a.n_bands + p.seg.band) * a.kv_heads + p.kv) * size;
     there = false;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
     __shared__ __align__(128) char ta[2][kDecayTile * RB], tb[2][kDecayTile * RB], tc[2][kDecayTile * RB];
     __shared__ float power[kDecayTile + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
-    const DecayPlace p(a, lane);
+    const DecayPlace p(a, a.shift, lane);
     if (!p.seg.live) return;
     const DecayJob& j = a.job[p.job];
     const bool reverse = j.reverse;
@@ -343,20 +343,20 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
     }
 }
 
-// What a segment adds to the state, sum_s g^(n - 1 - s) b_s c_s^T, into its
-// slot: for bands of several segments (the last one's only where a state is
-// kept). single: bands of one segment, whose state in `state` goes on. Three
-// pieces of w c: the states are 32-bit results.
+// What a part adds to the state, sum_s g^(n - 1 - s) b_s c_s^T, into its slot:
+// for bands of several segments, up to the last one's start (to the band's end
+// where a state is kept). single: bands of one segment, whose state in `state`
+// goes on. Three pieces of w c: the states are 32-bit results.
 template <class T, int DP, bool WIDE>
 __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
     constexpr int RB = row_bytes<T, DP>(), ND = DP / 32;
     __shared__ __align__(128) char tb[2][kDecayTile * RB], tc[2][kDecayTile * RB];
     __shared__ float power[kDecayTile + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
-    const DecayPlace p(a, lane);
+    const DecayPlace p(a, a.single ? a.shift : a.fine, lane);
     if (!p.seg.live || p.outside || p.several == a.single) return;
     const DecayJob& j = a.job[p.job];
-    if (!a.state && p.seg.first + p.n == p.seg.len) return;
+    if (!a.state && p.seg.first >> a.shift == (p.seg.len - 1) >> a.shift) return;
     const int count = (p.n + kDecayTile - 1) / kDecayTile, stages = count * j.many;
     DecayLoad<T, DP, WIDE> lb(a, j.b, p, p.kv * j.many, j.reverse, tid), lc(a, j.c, p, p.kv * j.many, j.reverse, tid);
     auto use = [&](int tile) {
@@ -424,9 +424,9 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
         }
 }
 
-// From what each segment adds to the state that each starts with, in place,
-// along the segments of every band of several; `state` goes to the band's end.
-// A thread takes V neighbouring elements.
+// From what each part adds to the state that each segment starts with, in
+// place, along every band of several; `state` goes to the band's end. A thread
+// takes V neighbouring elements.
 template <int V> constexpr int decay_scan_part() { return 256 * V; }   // elements of a workgroup
 template <int V> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
     typedef float vec __attribute__((ext_vector_type(V)));
@@ -441,28 +441,29 @@ template <int V> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a
     const int start = band_bound(a.off, a.n_bands, a.rows, band + 1), len = band_bound(a.off, a.n_bands, a.rows, band + 2) - start;
     if (len <= 1 << a.shift || e >= size) return;
     const double l2 = static_cast<double>(a.log_decay[kv]) * 1.4426950408889634;
-    const float across = decay_power(l2, int64_t(1) << a.shift);
-    const int count = (len + (1 << a.shift) - 1) >> a.shift;
+    const float across = decay_power(l2, int64_t(1) << a.fine);
+    const int count = (len + (1 << a.fine) - 1) >> a.fine, each = (1 << (a.shift - a.fine)) - 1;
+    const int last = (len - 1) >> a.shift << (a.shift - a.fine);   // the part that the last segment starts with
     const int64_t step = static_cast<int64_t>(a.kv_heads) * size;
-    float* x = a.job[job].part + ((b * slot_count(a.rows, a.shift) + slot_of(start, 0, a.shift)) * a.kv_heads + kv) * size + e;
+    float* x = a.job[job].part + ((b * slot_count(a.rows, a.fine) + slot_of(start, 0, a.fine)) * a.kv_heads + kv) * size + e;
     float* st = a.state ? a.state + ((b * a.n_bands + band) * a.kv_heads + kv) * size + e : nullptr;
     auto at = [&](int i) -> vec& { return *reinterpret_cast<vec*>(x + i * step); };
     vec s = st ? *reinterpret_cast<vec*>(st) : vec(0.f);
-    constexpr int kAhead = V == 1 ? 16 : 8;
-    for (int i = 0; i + 1 < count; i += kAhead) {
+    const int end = st ? count - 1 : last;   // (the band's last part may be a short one)
+    constexpr int kAhead = 16;
+    for (int i = 0; i < end; i += kAhead) {
         vec add[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) add[k] = i + k + 1 < count ? at(i + k) : vec(0.f);
+        for (int k = 0; k < kAhead; ++k) add[k] = i + k < end ? at(i + k) : vec(0.f);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (i + k + 1 < count) {
-                at(i + k) = s;
+            if (i + k < end) {
+                if (((i + k) & each) == 0) at(i + k) = s;
                 s = across * s + add[k];
             }
     }
-    const vec add = st ? at(count - 1) : vec(0.f);
-    at(count - 1) = s;
-    if (st) *reinterpret_cast<vec*>(st) = decay_power(l2, len - (static_cast<int64_t>(count - 1) << a.shift)) * s + add;
+    if (st) *reinterpret_cast<vec*>(st) = decay_power(l2, len - (static_cast<int64_t>(end) << a.fine)) * s + at(end);
+    if ((end & each) == 0) at(end) = s;
 }
 
 // ------------------------------------------------------------- single tokens

@@ -48,6 +48,14 @@ int gated_chunk_shift(int64_t batch, int64_t rows, int64_t n_out) {
     return shift;
 }
 
+// Rows of a workgroup of k_gated_kept: up to 1024 for each copy of W into LDS,
+// but not so many that fewer than 4 workgroups fall on a compute unit.
+int kept_rows_shift(int64_t batch, int64_t rows, int64_t cols) {
+    int shift = 10;
+    while (shift > 7 && ((batch * rows) >> shift) * cols < 1024) --shift;
+    return shift;
+}
+
 }  // namespace
 
 extern "C" {
@@ -68,7 +76,15 @@ int nsgcqt_band_gated(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x, con
         using T = decltype(t);
         auto go = [&](auto nb) -> int {
             constexpr int NB = decltype(nb)::value;
-            const int64_t blocks = tile_count(kRowShift, a.n_bands, a.batch, a.rows) * ((n_out + 32 * NB - 1) / (32 * NB));
+            const int64_t cols = (n_out + 32 * NB - 1) / (32 * NB);
+            if (n_in <= gated_inputs<T>()) {
+                a.chunk_shift = kept_rows_shift(a.batch, a.rows, cols);
+                const int64_t blocks = tile_count(a.chunk_shift, a.n_bands, a.batch, a.rows) * cols;
+                CHECK_TRY(check_grid(blocks));
+                LAUNCH_TRY((k_gated_kept<T, NB>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
+                return NSGCQT_OK;
+            }
+            const int64_t blocks = tile_count(kRowShift, a.n_bands, a.batch, a.rows) * cols;
             CHECK_TRY(check_grid(blocks));
             LAUNCH_TRY((k_gated<T, NB>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
             return NSGCQT_OK;
@@ -132,7 +148,7 @@ int nsgcqt_band_gated_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x
             constexpr bool kHeld = decltype(held)::value;
             if (inputs) LAUNCH_TRY((k_gated_dx<T, kHeld>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
             if (weights) {
-                LAUNCH_TRY((k_gated_dw<T, kHeld>), dim3(static_cast<unsigned>(items)), dim3(256), 0, st, a);
+                LAUNCH_TRY((k_gated_dw<T, kHeld>), dim3(static_cast<unsigned>(items)), dim3(512), 0, st, a);
                 const int64_t join = (2 * n_in * n_out + 2 * n_out + 255) / 256;
                 for (LinearArgs l = a.dw; l.first_band < l.n_bands; l.first_band += 65535)
                     LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64),
