@@ -6,74 +6,78 @@ namespace nsl {
 
 enum Act { kNone = 0, kSilu = 1, kGelu = 2, kSigmoid = 3 };
 
-// exp(-z). What the exponent's product loses in 32 bits is added to first
-// order: off by 2e-7 relative however large |z|.
-__device__ inline float exp_neg(float z) {
+// EXACT, for 32-bit results, makes up for what an exponent's product loses in
+// 32 bits; for 16-bit results that is left out (1e-6 at |z| = 10).
+
+// exp(-z). EXACT: what the exponent's product loses in 32 bits is added to
+// first order: off by 2e-7 relative however large |z|.
+template <bool EXACT> __device__ inline float exp_neg(float z) {
     constexpr float kHigh = -1.44269504f, kLow = -1.92596299e-8f;   // -log2(e)
-    const float y = z * kHigh, rest = fmaf(z, kLow, fmaf(z, kHigh, -y));
+    const float y = z * kHigh;
+    if (!EXACT) return __builtin_amdgcn_exp2f(y);
+    const float rest = fmaf(z, kLow, fmaf(z, kHigh, -y));
     return __builtin_amdgcn_exp2f(y) * fmaf(rest, 0.69314718f, 1.f);
 }
 
-// 1 / (1 + exp(-z)), and into `other` the same of -z (their sum is 1, but the
-// smaller one's last bits are not in the larger one).
-__device__ inline float logistic(float z, float& other) {
-    // (past 80 the correction would meet an infinity; 1 / (1 + e^80) is below what any result shows beside it)
-    const float e = exp_neg(fmaxf(z, -80.f)), s = __builtin_amdgcn_rcpf(1.f + e);
-    other = e * s;
+// 1 / (1 + exp(-z)), and into `other` the same of -z: their sum is 1, but the
+// smaller one's last bits are not in the larger one (and past 88 exp(-z) is
+// infinite where z is negative).
+template <bool EXACT> __device__ inline float logistic(float z, float& other) {
+    const float e = exp_neg<EXACT>(z), s = __builtin_amdgcn_rcpf(1.f + e);
+    other = z < 0.f ? 1.f - s : e * s;
     return s;
 }
-__device__ inline float logistic(float z) {
-    float other;
-    return logistic(z, other);
-}
+template <bool EXACT> __device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + exp_neg<EXACT>(z)); }
 
 // The normal distribution's Phi(z), and exp(-z^2 / 2) into `bell`. With w =
-// |z| / sqrt(2) and t = 1 / (1 + 0.3 w): erfc(w) = exp(-w^2) t Q(t), Q the
-// polynomial of degree 8 that fits exp(w^2) erfc(w) / t on (0, 1] with a
-// relative error of 2e-8; in 32 bits Phi is off by 4.5e-7 relative over |z| <= 9,
-// also where it is small. The square's rounding is made up for as above.
-__device__ inline float normal_cdf(float z, float& bell) {
+// |z| / sqrt(2) and t = 1 / (1 + 0.33 w): erfc(w) = exp(-w^2) t Q(t), Q the
+// polynomial of degree 7 that fits exp(w^2) erfc(w) / t on (0, 1], by least
+// squares with weights that even out the largest relative errors: 1e-7. EXACT:
+// Phi is off by 5e-7 relative over |z| <= 9, also where it is small.
+template <bool EXACT> __device__ inline float normal_cdf(float z, float& bell) {
     constexpr float kHigh = -0.721347520f, kLow = -9.62981497e-9f;   // -log2(e) / 2
-    z = fminf(fmaxf(z, -13.f), 13.f);   // (beyond, Phi is 0 or 1 in 32 bits)
-    const float s = z * z, e = fmaf(z, z, -s), y = s * kHigh, rest = fmaf(s, kLow, fmaf(s, kHigh, -y));
-    bell = __builtin_amdgcn_exp2f(y) * fmaf(e, -0.5f, fmaf(rest, 0.69314718f, 1.f));
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.212132034f, 1.f));
-    float q = -0.129540965f;
-    q = fmaf(q, t, 0.48565802f);
-    q = fmaf(q, t, -0.5124914f);
-    q = fmaf(q, t, 0.54798836f);
-    q = fmaf(q, t, -0.0948568061f);
-    q = fmaf(q, t, 0.215024844f);
-    q = fmaf(q, t, 0.148310348f);
-    q = fmaf(q, t, 0.170719892f);
-    q = fmaf(q, t, 0.16918768f);
-    const float tail = 0.5f * bell * t * q;
+    z = __builtin_amdgcn_fmed3f(z, -13.f, 13.f);   // (beyond, Phi is 0 or 1 in 32 bits)
+    const float s = z * z, y = s * kHigh;
+    bell = __builtin_amdgcn_exp2f(y);
+    if (EXACT) {
+        const float e = fmaf(z, z, -s), rest = fmaf(s, kLow, fmaf(s, kHigh, -y));
+        bell *= fmaf(e, -0.5f, fmaf(rest, 0.69314718f, 1.f));
+    }
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.23334524f, 1.f));
+    float q = fmaf(-0.134988993f, t, 0.458738714f);
+    q = fmaf(q, t, -0.348531395f);
+    q = fmaf(q, t, 0.406038553f);
+    q = fmaf(q, t, 0.0485620759f);
+    q = fmaf(q, t, 0.200800955f);
+    q = fmaf(q, t, 0.183027253f);
+    q = fmaf(q, t, 0.186352849f) * t;
+    const float tail = 0.5f * bell * q;
     return z < 0.f ? tail : 1.f - tail;
 }
 
-template <int ACT> __device__ inline float act_of(float z) {
+template <int ACT, bool EXACT> __device__ inline float act_of(float z) {
     float bell;
-    if constexpr (ACT == kSilu) return z * logistic(z);
-    if constexpr (ACT == kGelu) return z * normal_cdf(z, bell);
-    if constexpr (ACT == kSigmoid) return logistic(z);
+    if constexpr (ACT == kSilu) return z * logistic<EXACT>(z);
+    if constexpr (ACT == kGelu) return z * normal_cdf<EXACT>(z, bell);
+    if constexpr (ACT == kSigmoid) return logistic<EXACT>(z);
     return z;
 }
 
 // act(z), and its derivative into slope.
-template <int ACT> __device__ inline float act_of(float z, float& slope) {
+template <int ACT, bool EXACT> __device__ inline float act_of(float z, float& slope) {
     if constexpr (ACT == kSilu) {
         float other;
-        const float s = logistic(z, other);
+        const float s = logistic<EXACT>(z, other);
         slope = fmaf(z * s, other, s);
         return z * s;
     } else if constexpr (ACT == kGelu) {
         float bell;
-        const float phi = normal_cdf(z, bell);
+        const float phi = normal_cdf<EXACT>(z, bell);
         slope = fmaf(0.39894228f * z, bell, phi);
         return z * phi;
     } else if constexpr (ACT == kSigmoid) {
         float other;
-        const float s = logistic(z, other);
+        const float s = logistic<EXACT>(z, other);
         slope = s * other;
         return s;
     } else {

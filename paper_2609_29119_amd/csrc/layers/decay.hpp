@@ -88,8 +88,7 @@ template <class T, int RB> __device__ inline frag<T> read_turned_state(const cha
     }
 }
 
-// What a workgroup of either kernel works on. Blocks begin at the end of the
-// row: where bands grow along it, the longest segments come first.
+// What a workgroup of either kernel works on.
 struct DecayPlace {
     int job, head, kv;
     int64_t b;
@@ -98,7 +97,7 @@ struct DecayPlace {
     bool outside;   // tokens that no band holds
     bool several;   // the band has more than one segment
     __device__ DecayPlace(const DecayArgs& a, int shift, int lane) {
-        const unsigned id = gridDim.x - 1 - die_order(blockIdx.x, gridDim.x), rest = id / a.units;
+        const unsigned id = last_first(blockIdx.x, gridDim.x), rest = id / a.units;
         head = static_cast<int>(id - rest * a.units);
         job = 0;
         while (head >= a.job[job].heads) head -= a.job[job++].heads;

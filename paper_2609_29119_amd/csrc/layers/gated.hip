@@ -40,18 +40,21 @@ GatedArgs gated_args(const nsgcqt_rows* r, const void* w, const void* bias, int6
     return a;
 }
 
-// Rows of a chunk of the weights' gradient, 256 to 4096: the most that leave 400 workgroups.
+// Rows of a chunk of the weights' gradient, 256 to 4096: the most that leave
+// 800 workgroups of 512 threads. 446,932 rows, 128 -> 256: 1024 rows 373 us and
+// 40 for the join, 512 rows 434 and 64, 2048 rows 403 and 30.
 int gated_chunk_shift(int64_t batch, int64_t rows, int64_t n_out) {
     const int64_t tiles = (n_out + 127) / 128;
     int shift = 12;
-    while (shift > 8 && ((batch * rows) >> shift) * tiles < 400) --shift;
+    while (shift > 8 && ((batch * rows) >> shift) * tiles < 800) --shift;
     return shift;
 }
 
-// Rows of a workgroup of k_gated_kept: up to 1024 for each copy of W into LDS,
-// but not so many that fewer than 4 workgroups fall on a compute unit.
+// Rows of a workgroup of k_gated_kept: up to 2048 for each copy of W into LDS,
+// but not so many that fewer than 4 workgroups fall on a compute unit (446,932
+// rows, 128 -> 256: 2048 rows 165 us, 1024 rows 175, 512 rows 195).
 int kept_rows_shift(int64_t batch, int64_t rows, int64_t cols) {
-    int shift = 10;
+    int shift = 11;
     while (shift > 7 && ((batch * rows) >> shift) * cols < 1024) --shift;
     return shift;
 }

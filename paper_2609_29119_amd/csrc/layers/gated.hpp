@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedArgs a) {
     __shared__ __align__(16) float start[2 * BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int cols = (a.n_out + BN - 1) / BN;
-    const unsigned id = die_order(blockIdx.x, gridDim.x), p = id / cols;
+    const unsigned id = last_first(blockIdx.x, gridDim.x), p = id / cols;
     const int c0 = (id - p * cols) * BN;
     const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, kRowShift, p, lane);
     if (!t.live) return;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedArgs a) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) acc[nb][q] = act_of<act.value>(acc[nb][q]) * acc[NB + nb][q];
+            for (int q = 0; q < 16; ++q) acc[nb][q] = act_of<act.value, sizeof(T) == 4>(acc[nb][q]) * acc[NB + nb][q];
     });
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) store_column<T>(out, acc[nb], c0 + 32 * nb, a.n_out, a.y_wide, lane);
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_kept(GatedArgs a) {
     __shared__ __align__(16) float start[2 * BN];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int cols = (a.n_out + BN - 1) / BN;
-    const unsigned id = die_order(blockIdx.x, gridDim.x), p = id / cols;
+    const unsigned id = last_first(blockIdx.x, gridDim.x), p = id / cols;
     const int c0 = (id - p * cols) * BN;
     const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, a.chunk_shift, p, lane);
     if (!t.live) return;
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_kept(GatedArgs a) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int q = 0; q < 16; ++q) acc[nb][q] = act_of<act.value>(acc[nb][q]) * acc[NB + nb][q];
+                for (int q = 0; q < 16; ++q) acc[nb][q] = act_of<act.value, sizeof(T) == 4>(acc[nb][q]) * acc[NB + nb][q];
         });
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) store_column<T>(to, acc[nb], c0 + 32 * nb, a.n_out, a.y_wide, lane);
@@ -249,11 +249,11 @@ template <class T> __device__ inline quad<T> load4(const T* p, int n, bool wide)
 }
 
 // From a, u and dy: da and du, in their places.
-template <int ACT> __device__ inline void gated_slope(acc16& a, acc16& u, const float (&dy)[16]) {
+template <int ACT, bool EXACT> __device__ inline void gated_slope(acc16& a, acc16& u, const float (&dy)[16]) {
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
         float slope;
-        const float f = act_of<ACT>(a[q], slope);
+        const float f = act_of<ACT, EXACT>(a[q], slope);
         a[q] = dy[q] * u[q] * slope;
         u[q] = dy[q] * f;
     }
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedArgs a) {
     __shared__ __align__(16) float start[2][2][32];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int slabs = (a.n_in + BK - 1) / BK;
-    const unsigned id = die_order(blockIdx.x, gridDim.x), p = id / slabs;
+    const unsigned id = last_first(blockIdx.x, gridDim.x), p = id / slabs;
     const int my_slab = static_cast<int>(id - p * slabs), c0 = my_slab * BK;
     const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, kRowShift, p, lane);
     if (!t.live) return;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedArgs a) {
             float d[16];
 #pragma unroll
             for (int q = 0; q < 16; ++q) d[q] = static_cast<float>(dyq[q >> 2][q & 3]);
-            by_act(a.act, [&](auto act) __attribute__((always_inline)) { gated_slope<act.value>(za, zu, d); });
+            by_act(a.act, [&](auto act) __attribute__((always_inline)) { gated_slope<act.value, sizeof(T) == 4>(za, zu, d); });
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const auto da = sum_of<T, 2>(octet(za, x)), du = sum_of<T, 2>(octet(zu, x));
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_dw(GatedArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int wi = wave & 3, wj = wave >> 2;
     const int ot = (a.n_out + 127) / 128, it = max(1, (a.n_in + BK - 1) / BK);
-    const unsigned id = die_order(blockIdx.x, gridDim.x), p = id / (ot * it), at2 = id - p * (ot * it);
+    const unsigned id = last_first(blockIdx.x, gridDim.x), p = id / (ot * it), at2 = id - p * (ot * it);
     const int o0 = at2 / it * 128, i0 = at2 % it * BK;
     const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, a.dw.chunk_shift, p, lane);
     if (!t.live || t.band < 0 || t.band >= a.n_bands) return;
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(512, 2) void k_gated_dw(GatedArgs a) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         float slope;
-                        const float f = act_of<act.value>(za[8 * x + j], slope), dy = static_cast<float>(d[j]);
+                        const float f = act_of<act.value, sizeof(T) == 4>(za[8 * x + j], slope), dy = static_cast<float>(d[j]);
                         da[j] = dy * zu[8 * x + j] * slope;
                         du[j] = dy * f;
                     }

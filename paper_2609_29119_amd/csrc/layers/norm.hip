@@ -26,14 +26,24 @@ int check_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s) {
 }
 
 // Tokens of a chunk: what a workgroup's registers hold, `held` octets a thread
-// (64 KB a workgroup).
+// (64 KB a workgroup); and of a part, up to 8 chunks, but not so many that
+// fewer than 1024 workgroups are left.
 void set_chunk(NormArgs& a, int held) {
     a.octets = (a.channels + 7) / 8;
     a.together = kNormThreads / a.octets;
     a.shift = 0;
     while ((2 << a.shift) <= a.together * held) ++a.shift;
+    a.part_shift = a.shift + 3;
+    while (a.part_shift > a.shift && product(static_cast<int64_t>(a.batch), static_cast<int64_t>(a.rows >> a.part_shift)) < 1024) --a.part_shift;
     a.items = static_cast<unsigned>(tile_count(a.shift, a.n_bands, 1, a.rows));
+    a.parts = static_cast<unsigned>(tile_count(a.part_shift, a.n_bands, 1, a.rows));
+    a.octet_groups = a.cg % 8 == 0;
 }
+bool has_parts(const NormArgs& a) { return a.rows > 1 << a.shift; }
+
+// Whether each chunk and part leaves what it adds to dw and db: where these
+// have 16 tokens or more at the mean, that is little beside the data.
+bool chunks_sum(const NormArgs& a) { return a.rows >= 16 * static_cast<int64_t>(a.items); }
 
 // Rows of an item of the weights' gradient, 64 to 4096: the most that leave 1024 items.
 int weight_shift_of(int64_t batch, int64_t rows) {
@@ -70,9 +80,10 @@ NormSpace norm_space(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     if (a.channels == 0) return {0, 0};
     set_chunk(a, held_of(dtype, grad));
     NormSpace n{0, 0};
-    if (r->rows > int64_t(1) << a.shift) n.part = product(16, r->batch, slot_count(r->rows, a.shift), a.groups);
+    if (has_parts(a)) n.part = product(16, r->batch, static_cast<int64_t>(a.parts), a.groups);
     if (grad && weights)
-        n.sums = product(8, tile_count(weight_shift_of(r->batch, r->rows), r->n_bands, r->batch, r->rows), a.channels);
+        n.sums = product(8, chunks_sum(a) ? product(r->batch, r->n_bands + static_cast<int64_t>(a.parts))
+                                          : tile_count(weight_shift_of(r->batch, r->rows), r->n_bands, r->batch, r->rows), a.channels);
     return n;
 }
 int64_t norm_bytes(const NormSpace& n) {
@@ -90,10 +101,10 @@ int check_space(const void* ws, size_t have, int64_t need) {
     return NSGCQT_OK;
 }
 
-template <class K> int launch_all(K kernel, NormArgs a, int64_t threads, hipStream_t st) {
+template <class K, class... More> int launch_all(K kernel, NormArgs a, int64_t threads, hipStream_t st, More... more) {
     const int64_t blocks = (threads + 255) / 256;
     for (; a.first_block < blocks; a.first_block += kMaxGrid)
-        LAUNCH_TRY(kernel, dim3(static_cast<unsigned>(std::min(blocks - a.first_block, kMaxGrid))), dim3(256), 0, st, a);
+        LAUNCH_TRY(kernel, dim3(static_cast<unsigned>(std::min(blocks - a.first_block, kMaxGrid))), dim3(256), 0, st, a, more...);
     return NSGCQT_OK;
 }
 
@@ -131,7 +142,8 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     CHECK_TRY(check_grid(blocks));
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
-    const dim3 grid(static_cast<unsigned>(blocks)), block(kNormThreads);
+    CHECK_TRY(check_grid(product(r->batch, static_cast<int64_t>(a.parts))));
+    const dim3 grid(static_cast<unsigned>(blocks)), parts(static_cast<unsigned>(r->batch * a.parts)), block(kNormThreads);
     const size_t lds = sizeof(double) * 8 * a.octets * a.together;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
@@ -139,6 +151,7 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
         constexpr bool kWide = decltype(w)::value;
         LAUNCH_TRY((k_norm<T, kWide>), grid, block, lds, st, a);
         if (space.part) {
+            LAUNCH_TRY((k_norm_sum<T, kWide>), parts, block, lds, st, a);
             CHECK_TRY(launch_all(k_norm_join<false>, a, groups, st));
             LAUNCH_TRY((k_norm_apply<T, kWide>), grid, block, 0, st, a);
         }
@@ -171,14 +184,17 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     if (dx) a.y = view_of(dx);
     a.stats = reinterpret_cast<double2*>(const_cast<double*>(stats));
     a.part = static_cast<double2*>(ws);
-    a.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + space.part);
+    float* sums = weights ? reinterpret_cast<float*>(static_cast<char*>(ws) + space.part) : nullptr;
+    const bool by_chunk = weights && chunks_sum(a);
+    if (by_chunk) a.sums = sums;
     a.dw = dw;
     a.db = db;
     const int64_t blocks = product(r->batch, static_cast<int64_t>(a.items));
     const int64_t items = tile_count(a.weight_shift, r->n_bands, r->batch, r->rows);
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
-    if (dx) CHECK_TRY(check_grid(blocks));
-    if (weights) CHECK_TRY(check_grid(items));
+    const int64_t parts = product(r->batch, static_cast<int64_t>(a.parts));
+    if (dx || by_chunk) CHECK_TRY(check_grid(std::max(blocks, parts)));
+    if (weights && !by_chunk) CHECK_TRY(check_grid(items));
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
     const dim3 block(kNormThreads);
     const size_t lds = sizeof(double) * 8 * a.octets * a.together;
@@ -186,18 +202,22 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
         using T = decltype(t);
         constexpr bool kWide = decltype(w)::value;
-        if (dx && rows) {
+        if ((dx || by_chunk) && rows) {
             const dim3 grid(static_cast<unsigned>(blocks));
-            LAUNCH_TRY((k_norm_grad<T, kWide, false>), grid, block, lds, st, a);
+            LAUNCH_TRY((k_norm_grad<T, kWide>), grid, block, lds, st, a);
             if (space.part) {
-                CHECK_TRY(launch_all(k_norm_join<true>, a, groups, st));
-                LAUNCH_TRY((k_norm_grad<T, kWide, true>), grid, block, 0, st, a);
+                LAUNCH_TRY((k_norm_grad_sum<T, kWide>), dim3(static_cast<unsigned>(parts)), block, lds, st, a);
+                if (dx) {
+                    CHECK_TRY(launch_all(k_norm_join<true>, a, groups, st));
+                    LAUNCH_TRY((k_norm_grad_apply<T, kWide>), grid, block, 0, st, a);
+                }
             }
         }
         if (weights) {
-            if (rows)
+            a.sums = sums;
+            if (rows && !by_chunk)
                 LAUNCH_TRY((k_norm_weight<T, kWide>), dim3(static_cast<unsigned>(items)), block, lds, st, a);
-            CHECK_TRY(launch_all(k_norm_weight_join<T>, a, r->n_bands * s->channels, st));
+            CHECK_TRY(launch_all(k_norm_weight_join<T>, a, r->n_bands * s->channels, st, by_chunk));
         }
         return NSGCQT_OK;
     });

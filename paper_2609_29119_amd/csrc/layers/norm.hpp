@@ -6,11 +6,12 @@
 //   db = sum dz   dw = sum dz xh     over the band's tokens of all signals
 //
 // A workgroup takes a chunk of a band's tokens, all channels; a thread 8
-// channels of every n-th token, held in registers from the load to the store.
-// So a band of one chunk is read once; longer ones leave their chunks'
-// statistics in slots, which a second kernel joins and a third applies.
-// Statistics are means and sums of squared differences from them, never
-// differences of large sums, and are held in 64 bits.
+// channels of every n-th token. What a chunk holds stays in registers from the
+// load to the store: bands of one chunk are read once. Longer bands are read
+// twice: first in parts of several chunks for their sums, which a small kernel
+// joins, then chunk by chunk. Statistics are summed in 64 bits, where the square
+// of a mean of 10^6 deviations does not hide the variance; d's sums are those
+// that db and dw are made of, times w.
 #pragma once
 #include "act.hpp"
 
@@ -26,15 +27,18 @@ struct NormArgs {
     int64_t w_band, b_band;       // their strides from band to band
     void *dw, *db;
     double2* stats;               // [batch][n_bands][groups]: mean, rstd
-    double2* part;                // [batch][slots][groups]: of a chunk (mean, sum of squares) or (sum d, sum d xh)
-    float* sums;                  // weights' gradient: [items][2][channels]
+    double2* part;                // [batch][parts][groups]: a part's (sum x, sum x^2) or (sum d, sum d xh)
+    float* sums;                  // dw and db before they are joined, [2][channels] each (NULL: not wanted):
+                                  // [batch][n_bands] of bands of one chunk, then [batch][parts]; or of k_norm_weight's items
     const int64_t* off;
     int rows, n_bands, batch, channels, groups, cg;
     int octets, together;         // octets of a token's channels, tokens that a workgroup takes at once
-    int shift, weight_shift;      // of a chunk's tokens; of the weights' gradient's rows
-    unsigned items;               // work items of a signal
+    int shift, part_shift;        // of a chunk's tokens; of a part's
+    int weight_shift;             // of the rows of an item of k_norm_weight
+    unsigned items, parts;        // chunks and parts of a signal, the empty ones among them
     int64_t first_block;          // of a launch of a kernel whose blocks may pass a grid's limit
     int act;
+    bool octet_groups;            // a group is whole octets of channels
     double eps;
 };
 
@@ -42,38 +46,77 @@ template <class T> __device__ inline T* norm_row(const View& v, int64_t b, int64
     return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row;
 }
 
-// A thread's 8 channels: what is applied to them.
-struct NormOctet {
-    float high[8], low[8], rstd[8], w[8], b[8];   // the mean as two numbers
-    template <class T> __device__ void load_affine(const NormArgs& a, int band, int col) {
-        const T* wp = static_cast<const T*>(a.w) + band * a.w_band;
-        const T* bp = static_cast<const T*>(a.b) + band * a.b_band;
+// A thread's 8 channels: their groups, and what is applied to them. 32-bit data
+// are taken from the mean as two numbers; 16-bit data, whose mean is at most
+// some 2^11 of their smallest differences, by one multiply-add.
+template <class T> struct NormOctet {
+    static constexpr bool kExact = sizeof(T) == 4;
+    int group[8];
+    float high[kExact ? 8 : 1], low[8], rstd[8], w[8], b[8];   // (16 bits: low is -mean rstd)
+    __device__ NormOctet(const NormArgs& a, int col) {
+        int g = col / a.cg, r = col - g * a.cg;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bool there = col + i < a.channels;
-            w[i] = a.w && there ? static_cast<float>(wp[col + i]) : 1.f;
-            b[i] = a.b && there ? static_cast<float>(bp[col + i]) : 0.f;
+            group[i] = min(g, a.groups - 1);
+            if (++r == a.cg) {
+                r = 0;
+                ++g;
+            }
         }
     }
-    __device__ void set(int i, double mean, double r) {
-        high[i] = static_cast<float>(mean);
-        low[i] = static_cast<float>(mean - static_cast<double>(high[i]));
-        rstd[i] = static_cast<float>(r);
-    }
-    __device__ void load_stats(const NormArgs& a, const double2* st, int col) {
+    __device__ void load_affine(const NormArgs& a, int band, int col) {
+        const T* wp = static_cast<const T*>(a.w) + band * a.w_band + col;
+        const T* bp = static_cast<const T*>(a.b) + band * a.b_band + col;
+        const frag<T> fw = load8<T, false>(wp, a.w ? a.channels - col : 0), fb = load8<T, false>(bp, a.b ? a.channels - col : 0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const double2 v = st[min(col + i, a.channels - 1) / a.cg];
-            set(i, v.x, v.y);
+            w[i] = a.w ? static_cast<float>(fw[i]) : 1.f;
+            b[i] = static_cast<float>(fb[i]);
         }
     }
-    __device__ float hat(float x, int i) const { return ((x - high[i]) - low[i]) * rstd[i]; }
+    // f(group) gives its (mean, rstd)
+    template <class F> __device__ __attribute__((always_inline)) void set(const NormArgs& a, F f) {
+        auto put = [&](int i, double2 v) __attribute__((always_inline)) {
+            rstd[i] = static_cast<float>(v.y);
+            if constexpr (kExact) {
+                high[i] = static_cast<float>(v.x);
+                low[i] = static_cast<float>(v.x - static_cast<double>(high[i]));
+            } else {
+                low[i] = static_cast<float>(-v.x * v.y);
+            }
+        };
+        if (a.octet_groups) {
+            const double2 v = f(group[0]);
+            each<8>([&](auto i) __attribute__((always_inline)) { put(i.value, v); });
+        } else {
+            each<8>([&](auto i) __attribute__((always_inline)) { put(i.value, f(group[i.value])); });
+        }
+    }
+    __device__ float hat(T x, int i) const {
+        if constexpr (kExact)
+            return ((x - high[i]) - low[i]) * rstd[i];
+        else
+            return fmaf(static_cast<float>(x), rstd[i], low[i]);
+    }
+    template <int ACT> __device__ frag<T> out(frag<T> x) const {
+        frag<T> y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = static_cast<T>(act_of<ACT, kExact>(fmaf(hat(x[i], i), w[i], b[i])));
+        return y;
+    }
+    // xh and dz
+    template <int ACT> __device__ void slope(frag<T> x, frag<T> dy, float (&xh)[8], float (&dz)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            xh[i] = hat(x[i], i);
+            float d;
+            act_of<ACT, kExact>(fmaf(xh[i], w[i], b[i]), d);
+            dz[i] = static_cast<float>(dy[i]) * d;
+        }
+    }
 };
 
-template <class T> __device__ inline void store8(T* p, const float (&v)[8], int n, bool wide) {
-    frag<T> f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = static_cast<T>(v[i]);
+template <class T> __device__ inline void store8(T* p, frag<T> f, int n, bool wide) {
     if (wide) {
         *reinterpret_cast<frag<T>*>(p) = f;
     } else if (n >= 8) {
@@ -85,39 +128,47 @@ template <class T> __device__ inline void store8(T* p, const float (&v)[8], int 
     }
 }
 
-// Sums over a workgroup's tokens and a group's channels, in a fixed order.
-// `cells` holds a value of each of the tokens taken at once and each channel.
-__device__ inline void norm_put(const NormArgs& a, double* cells, int tr, int col, const float (&v)[8]) {
+// Sums over a workgroup's tokens and channels, in a fixed order. `cells` holds
+// a row of 8 octets values for each of the tokens taken at once, channel c at
+// norm_cell(c) of it, which spreads a wave's writes over the banks. norm_columns
+// leaves the sum of a channel in parts, [part * width + cell]: a thread adds
+// every parts-th row into its own first one. All threads; ends with a barrier.
+__device__ inline int norm_cell(const NormArgs& a, int c) { return (c & 7) * a.octets + (c >> 3); }
+__device__ inline int norm_parts(const NormArgs& a) { return min(a.together, max(1, kNormThreads / (8 * a.octets))); }
+template <class V> __device__ inline void norm_columns(const NormArgs& a, V* cells, bool works, int tr, int col, const V (&v)[8], int tid) {
+    const int width = 8 * a.octets, parts = norm_parts(a);
+    if (works) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) cells[tr * a.octets * 8 + col + i] = v[i];
-}
-__device__ inline void norm_put(const NormArgs& a, double* cells, int tr, int col, const double (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cells[tr * a.octets * 8 + col + i] = v[i];
-}
-// result: [groups], in LDS. All threads; begins and ends with a barrier.
-__device__ inline void norm_add_up(const NormArgs& a, double* cells, double* result, int tid) {
-    const int width = a.octets * 8;
-    __syncthreads();
-    if (a.together > 1) {
-        for (int c = tid; c < a.channels; c += kNormThreads) {
-            double s = cells[c];
-            for (int r = 1; r < a.together; ++r) s += cells[r * width + c];
-            cells[c] = s;
-        }
-        __syncthreads();
+        for (int i = 0; i < 8; ++i) cells[tr * width + norm_cell(a, col + i)] = v[i];
     }
-    if (a.cg <= 32) {
+    __syncthreads();
+    if (parts < a.together) {
+        for (int at = tid; at < width * parts; at += kNormThreads) {
+            V s = cells[at];
+            for (int r = at + width * parts; r < width * a.together; r += width * parts) s += cells[r];
+            cells[at] = s;
+        }
+    }
+    __syncthreads();
+}
+// result[g] = the sum of f(cell, channel) over a group's channels and the parts. Ends with a barrier.
+template <class F> __device__ __attribute__((always_inline)) inline void norm_groups(const NormArgs& a, double* result, int tid, F f) {
+    const int width = 8 * a.octets, parts = norm_parts(a), each_group = a.cg * parts;
+    if (each_group <= 8 || a.groups >= kNormThreads / 4) {
         for (int g = tid; g < a.groups; g += kNormThreads) {
             double s = 0.0;
-            for (int c = g * a.cg; c < (g + 1) * a.cg; ++c) s += cells[c];
+            for (int p = 0; p < parts; ++p)
+                for (int c = g * a.cg; c < (g + 1) * a.cg; ++c) s += f(p * width + norm_cell(a, c), c);
             result[g] = s;
         }
     } else {
         const int lane = tid & 63;
         for (int g = wave_number(); g < a.groups; g += kNormThreads / 64) {
             double s = 0.0;
-            for (int c = lane; c < a.cg; c += 64) s += cells[g * a.cg + c];
+            for (int i = lane; i < each_group; i += 64) {
+                const int p = i / a.cg, c = g * a.cg + i - p * a.cg;
+                s += f(p * width + norm_cell(a, c), c);
+            }
 #pragma unroll
             for (int x = 1; x < 64; x <<= 1) s += __shfl_xor(s, x);
             if (lane == 0) result[g] = s;
@@ -131,14 +182,16 @@ __device__ inline void norm_add_up(const NormArgs& a, double* cells, double* res
 struct NormPlace {
     int64_t b;
     Tile<int> t;
-    int all, n, tr, col;   // all: the chunk's tokens
+    int all, n, tr, col;   // all: the chunk's (or part's) tokens
+    unsigned item;
     bool outside, several;
-    __device__ explicit NormPlace(const NormArgs& a) {
-        const unsigned id = die_order(blockIdx.x, gridDim.x);
+    __device__ NormPlace(const NormArgs& a, unsigned items, int shift) {
+        const unsigned id = last_first(blockIdx.x, gridDim.x);
         const int tid = threadIdx.x;
-        b = id / a.items;
-        t = find_tile<int>(a.off, a.n_bands, a.rows, 1, a.shift, static_cast<int>(id % a.items), tid & 63);
-        all = min(t.len - t.first, 1 << a.shift);
+        b = id / items;
+        item = id - static_cast<unsigned>(b) * items;
+        t = find_tile<int>(a.off, a.n_bands, a.rows, 1, shift, static_cast<int>(item), tid & 63);
+        all = min(t.len - t.first, 1 << shift);
         outside = t.band < 0 || t.band >= a.n_bands;
         several = t.len > 1 << a.shift;
         tr = tid / a.octets;
@@ -147,20 +200,21 @@ struct NormPlace {
     }
     __device__ bool works(const NormArgs& a) const { return tr < a.together; }
     __device__ double2* stats(const NormArgs& a) const { return a.stats + (b * a.n_bands + t.band) * a.groups; }
-    __device__ double2* part(const NormArgs& a) const {
-        return a.part + (b * slot_count(a.rows, a.shift) + slot_of(t.start, t.first >> a.shift, a.shift)) * a.groups;
-    }
     template <class T> __device__ T* at(const View& v, int token) const {
         return norm_row<T>(v, b, t.start + t.first + token) + col;
     }
-    template <class T, int N, bool WIDE> __device__ void load(const NormArgs& a, const View& v, frag<T> (&f)[N]) const {
+    template <class T, int N, bool WIDE> __device__ void load(const NormArgs& a, const View& v, frag<T> (&f)[N], int from = 0) const {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int token = tr + a.together * k;
+            const int token = from + tr + a.together * k;
             f[k] = load8<T, WIDE>(at<T>(v, token < n ? token : 0), token < n ? a.channels - col : 0, col > 0);
         }
     }
 };
+// Where the parts of a band lie among a signal's.
+__device__ inline int64_t norm_part(const NormArgs& a, int64_t b, int band, int start) {
+    return b * a.parts + (start >> a.part_shift) + band + 1;
+}
 
 // f(k, token) for the thread's tokens that exist
 template <int N, class F> __device__ __attribute__((always_inline)) inline void norm_tokens(const NormArgs& a, const NormPlace& p, F f) {
@@ -171,66 +225,102 @@ template <int N, class F> __device__ __attribute__((always_inline)) inline void 
 }
 
 template <class T, bool WIDE> __device__ inline void norm_zero(const NormArgs& a, const NormPlace& p) {
-    const float zero[8] = {};
-    for (int token = p.tr; token < p.n; token += a.together) store8<T>(p.at<T>(a.y, token), zero, a.channels - p.col, WIDE);
+    for (int token = p.tr; token < p.n; token += a.together) store8<T>(p.at<T>(a.y, token), zero8<T>(), a.channels - p.col, WIDE);
 }
 
-// y of bands of one chunk; else the chunk's statistics.
+template <class T, int N, bool WIDE> __device__ inline void norm_out(const NormArgs& a, const NormPlace& p, const NormOctet<T>& o, const frag<T> (&x)[N]) {
+    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
+        norm_tokens<N>(a, p, [&](int k, int token) __attribute__((always_inline)) {
+            store8<T>(p.at<T>(a.y, token), o.template out<act.value>(x[k]), a.channels - p.col, WIDE);
+        });
+    });
+}
+
+// y of bands of one chunk, and zeros where no band is: the mean first, then the
+// squares of the differences from it.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     constexpr int N = norm_held<T>();
     extern __shared__ __align__(16) double norm_lds[];
     __shared__ double mean[kNormGroups], squares[kNormGroups];
     const int tid = threadIdx.x;
-    const NormPlace p(a);
+    const NormPlace p(a, a.items, a.shift);
     if (!p.t.live) return;
     if (p.outside) return norm_zero<T, WIDE>(a, p);
+    if (p.several) return;
     frag<T> x[N];
     p.load<T, N, WIDE>(a, a.x, x);
-    const double count = static_cast<double>(p.all) * a.cg;
+    const double count = static_cast<double>(p.all) * a.cg;   // (divided by: the mean of equal values is theirs)
+    auto cell = [&](int at, int) { return norm_lds[at]; };
     double s[8] = {};
     norm_tokens<N>(a, p, [&](int k, int) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += static_cast<double>(static_cast<float>(x[k][i]));
     });
-    if (p.works(a)) norm_put(a, norm_lds, p.tr, p.col, s);
-    norm_add_up(a, norm_lds, mean, tid);
-    NormOctet o;
-    float q[8] = {};
+    norm_columns(a, norm_lds, p.works(a), p.tr, p.col, s, tid);
+    norm_groups(a, mean, tid, cell);
+    NormOctet<T> o(a, p.col);
+    float m[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.set(i, mean[min(p.col + i, a.channels - 1) / a.cg] / count, 1.0);
+    for (int i = 0; i < 8; ++i) {
+        m[i] = static_cast<float>(mean[o.group[i]] / count);   // (what it is off by is made up for below)
+        s[i] = 0.0;
+    }
     norm_tokens<N>(a, p, [&](int k, int) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float d = o.hat(static_cast<float>(x[k][i]), i);
-            q[i] = fmaf(d, d, q[i]);
+            const float d = static_cast<float>(x[k][i]) - m[i];
+            s[i] = fma(static_cast<double>(d), static_cast<double>(d), s[i]);
         }
     });
-    if (p.works(a)) norm_put(a, norm_lds, p.tr, p.col, q);
-    norm_add_up(a, norm_lds, squares, tid);
-    double2* st = p.several ? p.part(a) : p.stats(a);
-    for (int g = tid; g < a.groups; g += kNormThreads)
-        st[g] = double2{mean[g] / count, p.several ? squares[g] : 1.0 / sqrt(squares[g] / count + a.eps)};
-    if (p.several || !p.works(a)) return;
-    o.load_affine<T>(a, p.t.band, p.col);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int g = min(p.col + i, a.channels - 1) / a.cg;
-        o.set(i, mean[g] / count, 1.0 / sqrt(squares[g] / count + a.eps));
-    }
-    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
-        norm_tokens<N>(a, p, [&](int k, int token) __attribute__((always_inline)) {
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = act_of<act.value>(fmaf(o.hat(static_cast<float>(x[k][i]), i), o.w[i], o.b[i]));
-            store8<T>(p.at<T>(a.y, token), v, a.channels - p.col, WIDE);
-        });
-    });
+    norm_columns(a, norm_lds, p.works(a), p.tr, p.col, s, tid);
+    norm_groups(a, squares, tid, cell);
+    // the mean of the squared differences from m is the variance and the square of the mean's own difference from m
+    auto stat = [&](int g) {
+        const double mu = mean[g] / count, off = mu - static_cast<double>(static_cast<float>(mu));
+        return double2{mu, 1.0 / sqrt(fmax(squares[g] / count - off * off, 0.0) + a.eps)};
+    };
+    double2* st = p.stats(a);
+    for (int g = tid; g < a.groups; g += kNormThreads) st[g] = stat(g);
+    if (!p.works(a)) return;
+    o.load_affine(a, p.t.band, p.col);
+    o.set(a, stat);
+    norm_out<T, N, WIDE>(a, p, o, x);
 }
 
-// Statistics of bands of several chunks: a thread joins one group's, in order.
-// GRAD: the sums of d and d xh, into the first chunk's slot.
+// The sums of x and x^2 of the parts of longer bands.
+template <class T, bool WIDE>
+__global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
+    constexpr int N = 4;
+    extern __shared__ __align__(16) double norm_lds[];
+    __shared__ double sum[kNormGroups], squares[kNormGroups];
+    const int tid = threadIdx.x;
+    const NormPlace p(a, a.parts, a.part_shift);
+    if (!p.t.live || p.outside || !p.several) return;
+    double s[8] = {}, q[8] = {};
+    for (int from = 0; from < p.all; from += N * a.together) {
+        frag<T> x[N];
+        p.load<T, N, WIDE>(a, a.x, x, from);   // (zeros past the end)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double v = static_cast<float>(x[k][i]);
+                s[i] += v;
+                q[i] = fma(v, v, q[i]);
+            }
+    }
+    auto cell = [&](int at, int) { return norm_lds[at]; };
+    norm_columns(a, norm_lds, p.works(a), p.tr, p.col, s, tid);
+    norm_groups(a, sum, tid, cell);
+    norm_columns(a, norm_lds, p.works(a), p.tr, p.col, q, tid);
+    norm_groups(a, squares, tid, cell);
+    double2* to = a.part + (p.b * a.parts + p.item) * a.groups;
+    for (int g = tid; g < a.groups; g += kNormThreads) to[g] = double2{sum[g], squares[g]};
+}
+
+// Joins the parts of longer bands, in order, a group a thread: into their
+// statistics, or (GRAD) their means of d and d xh into the first part's place.
 template <bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs a) {
     const int64_t id = (a.first_block + blockIdx.x) * 256 + threadIdx.x, place = id / a.groups;
     const int g = static_cast<int>(id % a.groups), band = static_cast<int>(place % a.n_bands);
@@ -238,138 +328,190 @@ template <bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs
     if (b >= a.batch) return;
     const int start = band_bound(a.off, a.n_bands, a.rows, band + 1), len = band_bound(a.off, a.n_bands, a.rows, band + 2) - start;
     if (len <= 1 << a.shift) return;
-    double2* part = a.part + (b * slot_count(a.rows, a.shift) + slot_of(start, 0, a.shift)) * a.groups + g;
-    double2 all = part[0];
-    double n = static_cast<double>(1 << a.shift) * a.cg;
-    for (int c = 1; c << a.shift < len; ++c) {
-        const double2 v = part[static_cast<int64_t>(c) * a.groups];
-        if (GRAD) {
-            all.x += v.x;
-            all.y += v.y;
-        } else {   // the mean and the squares of both together
-            const double m = static_cast<double>(min(len - (c << a.shift), 1 << a.shift)) * a.cg, d = v.x - all.x;
-            all.x += d * (m / (n + m));
-            all.y += v.y + d * d * (n * m / (n + m));
-            n += m;
-        }
-    }
+    double2* part = a.part + norm_part(a, b, band, start) * a.groups + g;
+    const int count = (len + (1 << a.part_shift) - 1) >> a.part_shift;
+    double2 all = {0.0, 0.0};
+#pragma unroll 8
+    for (int c = 0; c < count; ++c) all += part[static_cast<int64_t>(c) * a.groups];
+    all /= static_cast<double>(len) * a.cg;
     if (GRAD)
         part[0] = all;
     else
-        a.stats[place * a.groups + g] = double2{all.x, 1.0 / sqrt(all.y / n + a.eps)};
+        a.stats[place * a.groups + g] = double2{all.x, 1.0 / sqrt(fmax(all.y - all.x * all.x, 0.0) + a.eps)};
 }
 
-// y of bands of several chunks.
+// y of longer bands.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a) {
     constexpr int N = norm_held<T>();
-    const NormPlace p(a);
+    const NormPlace p(a, a.items, a.shift);
     if (!p.t.live || p.outside || !p.several || !p.works(a)) return;
     frag<T> x[N];
     p.load<T, N, WIDE>(a, a.x, x);
-    NormOctet o;
-    o.load_affine<T>(a, p.t.band, p.col);
-    o.load_stats(a, p.stats(a), p.col);
+    NormOctet<T> o(a, p.col);
+    const double2* st = p.stats(a);
+    o.load_affine(a, p.t.band, p.col);
+    o.set(a, [&](int g) { return st[g]; });
+    norm_out<T, N, WIDE>(a, p, o, x);
+}
+
+// From the sums of dz and dz xh of a thread's 8 channels: those of the
+// workgroup's channels, to `to` (NULL: not wanted), and times w, of its groups.
+template <class T>
+__device__ inline void norm_grad_sums(const NormArgs& a, const NormPlace& p, float2* cells, const float2 (&s)[8], float* to,
+                                      double* first, double* second, int tid) {
+    const int width = 8 * a.octets, parts = norm_parts(a);
+    norm_columns(a, cells, p.works(a), p.tr, p.col, s, tid);
+    if (to) {
+        for (int c = tid; c < a.channels; c += kNormThreads) {
+            float2 v = cells[norm_cell(a, c)];
+            for (int k = 1; k < parts; ++k) v += cells[k * width + norm_cell(a, c)];
+            to[c] = v.y;
+            to[a.channels + c] = v.x;
+        }
+    }
+    const T* wp = static_cast<const T*>(a.w) + p.t.band * a.w_band;
+    auto w = [&](int c) { return a.w ? static_cast<double>(static_cast<float>(wp[c])) : 1.0; };
+    norm_groups(a, first, tid, [&](int at, int c) { return cells[at].x * w(c); });
+    norm_groups(a, second, tid, [&](int at, int c) { return cells[at].y * w(c); });
+}
+
+template <class T, int N, bool WIDE, class M>
+__device__ inline void norm_grad_out(const NormArgs& a, const NormPlace& p, const NormOctet<T>& o, const frag<T> (&x)[N], const frag<T> (&dy)[N], M means) {
+    float m1[8], m2[8];
+    each<8>([&](auto i) __attribute__((always_inline)) {
+        if (i.value && a.octet_groups) {
+            m1[i.value] = m1[0];
+            m2[i.value] = m2[0];
+        } else {
+            const double2 v = means(o.group[i.value]);
+            m1[i.value] = static_cast<float>(v.x);
+            m2[i.value] = static_cast<float>(v.y);
+        }
+    });
     by_act(a.act, [&](auto act) __attribute__((always_inline)) {
         norm_tokens<N>(a, p, [&](int k, int token) __attribute__((always_inline)) {
-            float v[8];
+            float xh[8], dz[8];
+            o.template slope<act.value>(x[k], dy[k], xh, dz);
+            frag<T> f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = act_of<act.value>(fmaf(o.hat(static_cast<float>(x[k][i]), i), o.w[i], o.b[i]));
-            store8<T>(p.at<T>(a.y, token), v, a.channels - p.col, WIDE);
+            for (int i = 0; i < 8; ++i) f[i] = static_cast<T>(o.rstd[i] * (fmaf(dz[i], o.w[i], -m1[i]) - xh[i] * m2[i]));
+            store8<T>(p.at<T>(a.y, token), f, a.channels - p.col, WIDE);
         });
     });
 }
 
-// d and xh of 8 values
-template <int ACT, class T>
-__device__ inline void norm_slope(const NormOctet& o, const frag<T>& x, const frag<T>& dy, float (&hat)[8], float (&dz)[8]) {
+template <int ACT, class T> __device__ inline void norm_grad_add(const NormOctet<T>& o, frag<T> x, frag<T> dy, float2 (&s)[8]) {
+    float xh[8], dz[8];
+    o.template slope<ACT>(x, dy, xh, dz);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        hat[i] = o.hat(static_cast<float>(x[i]), i);
-        float slope;
-        act_of<ACT>(fmaf(hat[i], o.w[i], o.b[i]), slope);
-        dz[i] = static_cast<float>(dy[i]) * slope;
+        s[i].x += dz[i];
+        s[i].y = fmaf(dz[i], xh[i], s[i].y);
     }
 }
 
-// dx of bands of one chunk; else the chunk's sums of d and d xh. JOINED: dx of
-// bands of several chunks, whose sums are in the first one's slot.
-template <class T, bool WIDE, bool JOINED>
+// dx of bands of one chunk, and what they add to dw and db.
+template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad(NormArgs a) {
     constexpr int N = norm_held<T>() / 2;
     extern __shared__ __align__(16) double norm_lds[];
-    __shared__ double first[JOINED ? 1 : kNormGroups], second[JOINED ? 1 : kNormGroups];
+    __shared__ double first[kNormGroups], second[kNormGroups];
     const int tid = threadIdx.x;
-    const NormPlace p(a);
-    if (!p.t.live || (JOINED && (p.outside || !p.several))) return;
-    if (p.outside) return norm_zero<T, WIDE>(a, p);
+    const NormPlace p(a, a.items, a.shift);
+    if (!p.t.live) return;
+    if (p.outside) {
+        if (a.y.data) norm_zero<T, WIDE>(a, p);
+        return;
+    }
+    if (p.several) return;
     frag<T> x[N], dy[N];
     p.load<T, N, WIDE>(a, a.x, x);
     p.load<T, N, WIDE>(a, a.dy, dy);
-    NormOctet o;
+    NormOctet<T> o(a, p.col);
     if (p.works(a)) {
-        o.load_affine<T>(a, p.t.band, p.col);
-        o.load_stats(a, p.stats(a), p.col);
+        const double2* st = p.stats(a);
+        o.load_affine(a, p.t.band, p.col);
+        o.set(a, [&](int g) { return st[g]; });
     }
-    if constexpr (!JOINED) {
-        float s1[8] = {}, s2[8] = {};
-        by_act(a.act, [&](auto act) __attribute__((always_inline)) {
-            norm_tokens<N>(a, p, [&](int k, int) __attribute__((always_inline)) {
-                float hat[8], dz[8];
-                norm_slope<act.value, T>(o, x[k], dy[k], hat, dz);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    s1[i] = fmaf(dz[i], o.w[i], s1[i]);
-                    s2[i] = fmaf(dz[i] * o.w[i], hat[i], s2[i]);
-                }
-            });
-        });
-        if (p.works(a)) norm_put(a, norm_lds, p.tr, p.col, s1);
-        norm_add_up(a, norm_lds, first, tid);
-        if (p.works(a)) norm_put(a, norm_lds, p.tr, p.col, s2);
-        norm_add_up(a, norm_lds, second, tid);
-        if (p.several) {
-            double2* to = p.part(a);
-            for (int g = tid; g < a.groups; g += kNormThreads) to[g] = double2{first[g], second[g]};
-            return;
-        }
-    }
-    const double2* sums = JOINED ? p.part(a) - static_cast<int64_t>(p.t.first >> a.shift) * a.groups : nullptr;
-    const double share = 1.0 / (static_cast<double>(p.t.len) * a.cg);
-    float m1[8], m2[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int g = min(p.col + i, a.channels - 1) / a.cg;
-        m1[i] = static_cast<float>((JOINED ? sums[g].x : first[g]) * share);
-        m2[i] = static_cast<float>((JOINED ? sums[g].y : second[g]) * share);
-    }
+    float2 s[8] = {};
     by_act(a.act, [&](auto act) __attribute__((always_inline)) {
-        norm_tokens<N>(a, p, [&](int k, int token) __attribute__((always_inline)) {
-            float hat[8], dz[8], v[8];
-            norm_slope<act.value, T>(o, x[k], dy[k], hat, dz);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = o.rstd[i] * (fmaf(dz[i], o.w[i], -m1[i]) - hat[i] * m2[i]);
-            store8<T>(p.at<T>(a.y, token), v, a.channels - p.col, WIDE);
-        });
+        norm_tokens<N>(a, p, [&](int k, int) __attribute__((always_inline)) { norm_grad_add<act.value>(o, x[k], dy[k], s); });
     });
+    norm_grad_sums<T>(a, p, reinterpret_cast<float2*>(norm_lds), s,
+                      a.sums ? a.sums + (p.b * a.n_bands + p.t.band) * 2 * a.channels : nullptr, first, second, tid);
+    if (!a.y.data) return;
+    const double share = 1.0 / (static_cast<double>(p.t.len) * a.cg);
+    norm_grad_out<T, N, WIDE>(a, p, o, x, dy, [&](int g) { return double2{first[g] * share, second[g] * share}; });
 }
 
-// dw and db: sums over 2^weight_shift rows of a band, token r % len of signal
-// r / len, into the item's place.
+// The sums of d and d xh of the parts of longer bands, and what they add to dw and db.
+template <class T, bool WIDE>
+__global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
+    constexpr int N = 4;
+    extern __shared__ __align__(16) double norm_lds[];
+    __shared__ double first[kNormGroups], second[kNormGroups];
+    const int tid = threadIdx.x;
+    const NormPlace p(a, a.parts, a.part_shift);
+    if (!p.t.live || p.outside || !p.several) return;
+    NormOctet<T> o(a, p.col);
+    if (p.works(a)) {
+        const double2* st = p.stats(a);
+        o.load_affine(a, p.t.band, p.col);
+        o.set(a, [&](int g) { return st[g]; });
+    }
+    float2 s[8] = {};
+    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
+        for (int from = 0; from < p.all; from += N * a.together) {
+            frag<T> x[N], dy[N];
+            p.load<T, N, WIDE>(a, a.x, x, from);
+            p.load<T, N, WIDE>(a, a.dy, dy, from);
+#pragma unroll
+            for (int k = 0; k < N; ++k)   // (where a token is not there, dy is 0)
+                if (from + p.tr + a.together * k < p.n) norm_grad_add<act.value>(o, x[k], dy[k], s);
+        }
+    });
+    norm_grad_sums<T>(a, p, reinterpret_cast<float2*>(norm_lds), s,
+                      a.sums ? a.sums + (static_cast<int64_t>(a.batch) * a.n_bands + p.b * a.parts + p.item) * 2 * a.channels : nullptr,
+                      first, second, tid);
+    double2* to = a.part + (p.b * a.parts + p.item) * a.groups;
+    for (int g = tid; g < a.groups; g += kNormThreads) to[g] = double2{first[g], second[g]};
+}
+
+// dx of longer bands.
+template <class T, bool WIDE>
+__global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a) {
+    constexpr int N = norm_held<T>() / 2;
+    const NormPlace p(a, a.items, a.shift);
+    if (!p.t.live || p.outside || !p.several || !p.works(a)) return;
+    frag<T> x[N], dy[N];
+    p.load<T, N, WIDE>(a, a.x, x);
+    p.load<T, N, WIDE>(a, a.dy, dy);
+    NormOctet<T> o(a, p.col);
+    const double2 *st = p.stats(a), *means = a.part + norm_part(a, p.b, p.t.band, p.t.start) * a.groups;
+    o.load_affine(a, p.t.band, p.col);
+    o.set(a, [&](int g) { return st[g]; });
+    norm_grad_out<T, N, WIDE>(a, p, o, x, dy, [&](int g) { return means[g]; });
+}
+
+// dw and db where bands are so short that what each adds to them would be as
+// much as the data: sums over 2^weight_shift rows of a band, token r % len of
+// signal r / len.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads) void k_norm_weight(NormArgs a) {
-    extern __shared__ __align__(16) float norm_sums[];   // [together][2][8 octets]
+    extern __shared__ __align__(16) double norm_lds[];
+    float2* cells = reinterpret_cast<float2*>(norm_lds);
     const int tid = threadIdx.x, lane = tid & 63;
     const unsigned id = die_order(blockIdx.x, gridDim.x);
     const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, a.weight_shift, id, lane);
     if (!t.live || t.band < 0 || t.band >= a.n_bands) return;
     const int64_t end = min(t.first + (int64_t(1) << a.weight_shift), static_cast<int64_t>(t.len) * a.batch);
-    const int tr = tid / a.octets, col = 8 * (tid - tr * a.octets), width = 8 * a.octets;
-    if (tr < a.together) {
-        NormOctet o;
-        o.load_affine<T>(a, t.band, col);
-        float s1[8] = {}, s2[8] = {};
+    const int tr = tid / a.octets, col = 8 * (tid - tr * a.octets);
+    const bool works = tr < a.together;
+    float2 s[8] = {};
+    if (works) {
+        NormOctet<T> o(a, col);
+        o.load_affine(a, t.band, col);
         int64_t signal = -1;
         by_act(a.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll 2
@@ -377,47 +519,49 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_weight(NormArgs a) {
                 const int64_t b = r / t.len, row = t.start + (r - b * t.len);
                 const frag<T> x = load8<T, WIDE>(norm_row<T>(a.x, b, row) + col, a.channels - col, col > 0);
                 const frag<T> dy = load8<T, WIDE>(norm_row<T>(a.dy, b, row) + col, a.channels - col, col > 0);
-                if (b != signal) o.load_stats(a, a.stats + (b * a.n_bands + t.band) * a.groups, col);
-                signal = b;
-                float hat[8], dz[8];
-                norm_slope<act.value, T>(o, x, dy, hat, dz);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    s1[i] = fmaf(dz[i], hat[i], s1[i]);
-                    s2[i] += dz[i];
+                if (b != signal) {
+                    const double2* st = a.stats + (b * a.n_bands + t.band) * a.groups;
+                    o.set(a, [&](int g) { return st[g]; });
                 }
+                signal = b;
+                norm_grad_add<act.value>(o, x, dy, s);
             }
         });
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            norm_sums[2 * tr * width + col + i] = s1[i];
-            norm_sums[(2 * tr + 1) * width + col + i] = s2[i];
-        }
     }
-    __syncthreads();
+    norm_columns(a, cells, works, tr, col, s, tid);
     float* to = a.sums + static_cast<int64_t>(id) * 2 * a.channels;
-    for (int e = tid; e < 2 * a.channels; e += kNormThreads) {
-        const int which = e >= a.channels, c = e - which * a.channels;
-        float s = norm_sums[which * width + c];
-        for (int r = 1; r < a.together; ++r) s += norm_sums[(2 * r + which) * width + c];
-        to[e] = s;
+    for (int c = tid; c < a.channels; c += kNormThreads) {
+        float2 v = cells[norm_cell(a, c)];
+        for (int k = 1; k < norm_parts(a); ++k) v += cells[k * 8 * a.octets + norm_cell(a, c)];
+        to[c] = v.y;
+        to[a.channels + c] = v.x;
     }
 }
 
-// Adds up the items of each band, in order.
-template <class T> __global__ __launch_bounds__(256) void k_norm_weight_join(NormArgs a) {
+// Adds up what was left for dw and db of each band, in order: by k_norm_weight,
+// or with `by_chunk` by the other two.
+template <class T> __global__ __launch_bounds__(256) void k_norm_weight_join(NormArgs a, bool by_chunk) {
     const int64_t id = (a.first_block + blockIdx.x) * 256 + threadIdx.x;
     const int c = static_cast<int>(id % a.channels), band = static_cast<int>(id / a.channels);
     if (id >= static_cast<int64_t>(a.n_bands) * a.channels) return;
-    const int64_t b0 = band_bound(a.off, a.n_bands, a.rows, band + 1), b1 = band_bound(a.off, a.n_bands, a.rows, band + 2);
-    const int64_t n = b1 > b0 ? (b1 - b0) * a.batch : 0;
-    const int64_t count = (n + (int64_t(1) << a.weight_shift) - 1) >> a.weight_shift;
-    const float* s = a.sums + (((b0 * a.batch) >> a.weight_shift) + band + 1) * 2 * a.channels + c;
+    const int start = band_bound(a.off, a.n_bands, a.rows, band + 1), len = max(band_bound(a.off, a.n_bands, a.rows, band + 2) - start, 0);
+    const int64_t step = 2 * static_cast<int64_t>(a.channels);
     float dw = 0.f, db = 0.f;
-#pragma unroll 4
-    for (int64_t i = 0; i < count; ++i) {
-        dw += s[i * 2 * a.channels];
-        db += s[(2 * i + 1) * a.channels];
+    auto add = [&](int64_t from, int64_t count, int64_t by) {
+#pragma unroll 8
+        for (int64_t i = 0; i < count; ++i) {
+            dw += a.sums[(from + i * by) * step + c];
+            db += a.sums[(from + i * by) * step + a.channels + c];
+        }
+    };
+    if (!by_chunk) {
+        const int64_t n = static_cast<int64_t>(len) * a.batch;
+        add(((static_cast<int64_t>(start) * a.batch) >> a.weight_shift) + band + 1, (n + (int64_t(1) << a.weight_shift) - 1) >> a.weight_shift, 1);
+    } else if (len > 1 << a.shift) {
+        for (int64_t b = 0; b < a.batch; ++b)
+            add(static_cast<int64_t>(a.batch) * a.n_bands + norm_part(a, b, band, start), (len + (int64_t(1) << a.part_shift) - 1) >> a.part_shift, 1);
+    } else if (len > 0) {
+        add(band, a.batch, a.n_bands);
     }
     if (a.dw) static_cast<T*>(a.dw)[id] = static_cast<T>(dw);
     if (a.db) static_cast<T*>(a.db)[id] = static_cast<T>(db);
