@@ -188,8 +188,9 @@ __global__ __launch_bounds__(256, 2) void k_gated_kept(GatedArgs a) {
     fetch(row.of<T>(a.x, t), 32 * wave + m < n);
     const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(t.band) * 2 * a.n_out * a.n_in;
     by_width(a.w_wide, [&](auto wide) {
-#pragma unroll 4
-        for (int c = tid; c < 2 * BN * (BK / 8); c += 256) {
+#pragma unroll
+        for (int e = 0; e < 2 * BN * BK / 8 / 256; ++e) {
+            const int c = tid + 256 * e;
             const int i = c / (BK / 8), o = c0 + i % BN, col = c % (BK / 8) * 8;
             const T* from = w + (static_cast<int64_t>(i / BN) * a.n_out + o) * a.n_in + col;
             write8<T, RB>(ws, i, col / 8, load8<T, wide.value>(from, o < a.n_out ? a.n_in - col : 0, col > 0));

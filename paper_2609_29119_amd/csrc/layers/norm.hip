@@ -26,24 +26,25 @@ int check_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s) {
 }
 
 // Tokens of a chunk: what a workgroup's registers hold, `held` octets a thread
-// (64 KB a workgroup); and of a part, up to 8 chunks, but not so many that
+// (32 KB a workgroup of 256); and of a part, up to 8 chunks, but not so many that
 // fewer than 1024 workgroups are left.
 void set_chunk(NormArgs& a, int held) {
     a.octets = (a.channels + 7) / 8;
-    a.together = kNormThreads / a.octets;
+    a.threads = a.octets > 256 ? kNormThreads : 256;   // (of four waves three workgroups fit a compute unit, of eight one)
+    a.together = a.threads / a.octets;
     a.shift = 0;
     while ((2 << a.shift) <= a.together * held) ++a.shift;
     a.part_shift = a.shift + 3;
     while (a.part_shift > a.shift && product(static_cast<int64_t>(a.batch), static_cast<int64_t>(a.rows >> a.part_shift)) < 1024) --a.part_shift;
-    a.items = static_cast<unsigned>(tile_count(a.shift, a.n_bands, 1, a.rows));
+    a.zeros = static_cast<int>(std::min<int64_t>(64, (static_cast<int64_t>(a.rows) + 1023) >> 10));
     a.parts = static_cast<unsigned>(tile_count(a.part_shift, a.n_bands, 1, a.rows));
     a.octet_groups = a.cg % 8 == 0;
 }
 bool has_parts(const NormArgs& a) { return a.rows > 1 << a.shift; }
 
-// Whether each chunk and part leaves what it adds to dw and db: where these
-// have 16 tokens or more at the mean, that is little beside the data.
-bool chunks_sum(const NormArgs& a) { return a.rows >= 16 * static_cast<int64_t>(a.items); }
+// Whether each band of one chunk and each part leaves what it adds to dw and
+// db: where these have 16 tokens or more at the mean, that is little beside the data.
+bool chunks_sum(const NormArgs& a) { return a.rows >= 16 * static_cast<int64_t>(a.n_bands + 1); }
 
 // Rows of an item of the weights' gradient, 64 to 4096: the most that leave 1024 items.
 int weight_shift_of(int64_t batch, int64_t rows) {
@@ -138,12 +139,12 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     a.y = view_of(y);
     a.stats = reinterpret_cast<double2*>(stats);
     a.part = static_cast<double2*>(ws);
-    const int64_t blocks = product(r->batch, static_cast<int64_t>(a.items));
+    const int64_t blocks = product(r->batch, r->n_bands + a.zeros);
     CHECK_TRY(check_grid(blocks));
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
     CHECK_TRY(check_grid(product(r->batch, static_cast<int64_t>(a.parts))));
-    const dim3 grid(static_cast<unsigned>(blocks)), parts(static_cast<unsigned>(r->batch * a.parts)), block(kNormThreads);
+    const dim3 grid(static_cast<unsigned>(blocks)), parts(static_cast<unsigned>(r->batch * a.parts)), block(a.threads);
     const size_t lds = sizeof(double) * 8 * a.octets * a.together;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
@@ -153,7 +154,7 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
         if (space.part) {
             LAUNCH_TRY((k_norm_sum<T, kWide>), parts, block, lds, st, a);
             CHECK_TRY(launch_all(k_norm_join<false>, a, groups, st));
-            LAUNCH_TRY((k_norm_apply<T, kWide>), grid, block, 0, st, a);
+            LAUNCH_TRY((k_norm_apply<T, kWide>), parts, block, 0, st, a);
         }
         return NSGCQT_OK;
     });
@@ -189,14 +190,14 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     if (by_chunk) a.sums = sums;
     a.dw = dw;
     a.db = db;
-    const int64_t blocks = product(r->batch, static_cast<int64_t>(a.items));
+    const int64_t blocks = product(r->batch, r->n_bands + a.zeros);
     const int64_t items = tile_count(a.weight_shift, r->n_bands, r->batch, r->rows);
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
     const int64_t parts = product(r->batch, static_cast<int64_t>(a.parts));
     if (dx || by_chunk) CHECK_TRY(check_grid(std::max(blocks, parts)));
     if (weights && !by_chunk) CHECK_TRY(check_grid(items));
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
-    const dim3 block(kNormThreads);
+    const dim3 block(a.threads);
     const size_t lds = sizeof(double) * 8 * a.octets * a.together;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
@@ -209,7 +210,7 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
                 LAUNCH_TRY((k_norm_grad_sum<T, kWide>), dim3(static_cast<unsigned>(parts)), block, lds, st, a);
                 if (dx) {
                     CHECK_TRY(launch_all(k_norm_join<true>, a, groups, st));
-                    LAUNCH_TRY((k_norm_grad_apply<T, kWide>), grid, block, 0, st, a);
+                    LAUNCH_TRY((k_norm_grad_apply<T, kWide>), dim3(static_cast<unsigned>(parts)), block, 0, st, a);
                 }
             }
         }

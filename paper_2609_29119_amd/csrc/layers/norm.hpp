@@ -17,7 +17,7 @@
 
 namespace nsl {
 
-constexpr int kNormThreads = 512, kNormChannels = 8 * kNormThreads, kNormGroups = 1024;
+constexpr int kNormThreads = 512, kNormChannels = 8 * kNormThreads, kNormGroups = 1024;   // the most of each
 // Octets of x that a thread holds (half as many where dy is held beside it).
 template <class T> constexpr int norm_held() { return sizeof(T) == 4 ? 4 : 8; }
 
@@ -32,10 +32,12 @@ struct NormArgs {
                                   // [batch][n_bands] of bands of one chunk, then [batch][parts]; or of k_norm_weight's items
     const int64_t* off;
     int rows, n_bands, batch, channels, groups, cg;
+    int threads;                  // of a workgroup
     int octets, together;         // octets of a token's channels, tokens that a workgroup takes at once
     int shift, part_shift;        // of a chunk's tokens; of a part's
     int weight_shift;             // of the rows of an item of k_norm_weight
-    unsigned items, parts;        // chunks and parts of a signal, the empty ones among them
+    unsigned parts;               // of a signal, the empty ones among them
+    int zeros;                    // workgroups of a signal for the tokens that no band holds
     int64_t first_block;          // of a launch of a kernel whose blocks may pass a grid's limit
     int act;
     bool octet_groups;            // a group is whole octets of channels
@@ -134,7 +136,7 @@ template <class T> __device__ inline void store8(T* p, frag<T> f, int n, bool wi
 // leaves the sum of a channel in parts, [part * width + cell]: a thread adds
 // every parts-th row into its own first one. All threads; ends with a barrier.
 __device__ inline int norm_cell(const NormArgs& a, int c) { return (c & 7) * a.octets + (c >> 3); }
-__device__ inline int norm_parts(const NormArgs& a) { return min(a.together, max(1, kNormThreads / (8 * a.octets))); }
+__device__ inline int norm_parts(const NormArgs& a) { return min(a.together, max(1, a.threads / (8 * a.octets))); }
 template <class V> __device__ inline void norm_columns(const NormArgs& a, V* cells, bool works, int tr, int col, const V (&v)[8], int tid) {
     const int width = 8 * a.octets, parts = norm_parts(a);
     if (works) {
@@ -143,7 +145,7 @@ template <class V> __device__ inline void norm_columns(const NormArgs& a, V* cel
     }
     __syncthreads();
     if (parts < a.together) {
-        for (int at = tid; at < width * parts; at += kNormThreads) {
+        for (int at = tid; at < width * parts; at += a.threads) {
             V s = cells[at];
             for (int r = at + width * parts; r < width * a.together; r += width * parts) s += cells[r];
             cells[at] = s;
@@ -154,8 +156,8 @@ template <class V> __device__ inline void norm_columns(const NormArgs& a, V* cel
 // result[g] = the sum of f(cell, channel) over a group's channels and the parts. Ends with a barrier.
 template <class F> __device__ __attribute__((always_inline)) inline void norm_groups(const NormArgs& a, double* result, int tid, F f) {
     const int width = 8 * a.octets, parts = norm_parts(a), each_group = a.cg * parts;
-    if (each_group <= 8 || a.groups >= kNormThreads / 4) {
-        for (int g = tid; g < a.groups; g += kNormThreads) {
+    if (each_group <= 8 || a.groups >= a.threads / 4) {
+        for (int g = tid; g < a.groups; g += a.threads) {
             double s = 0.0;
             for (int p = 0; p < parts; ++p)
                 for (int c = g * a.cg; c < (g + 1) * a.cg; ++c) s += f(p * width + norm_cell(a, c), c);
@@ -163,7 +165,7 @@ template <class F> __device__ __attribute__((always_inline)) inline void norm_gr
         }
     } else {
         const int lane = tid & 63;
-        for (int g = wave_number(); g < a.groups; g += kNormThreads / 64) {
+        for (int g = wave_number(); g < a.groups; g += a.threads / 64) {
             double s = 0.0;
             for (int i = lane; i < each_group; i += 64) {
                 const int p = i / a.cg, c = g * a.cg + i - p * a.cg;
@@ -198,6 +200,26 @@ struct NormPlace {
         col = 8 * (tid - tr * a.octets);
         n = works(a) ? all : 0;
     }
+    // One workgroup a band: all of its tokens (several: more than a chunk); behind
+    // the bands a.zeros workgroups a signal, which share the tokens that no band holds.
+    __device__ explicit NormPlace(const NormArgs& a) {
+        const unsigned items = a.n_bands + a.zeros, id = gridDim.x - 1 - blockIdx.x;
+        const int tid = threadIdx.x;
+        b = id / items;
+        item = id - static_cast<unsigned>(b) * items;
+        t.band = static_cast<int>(item);
+        outside = t.band >= a.n_bands;
+        t.start = outside ? 0 : band_bound(a.off, a.n_bands, a.rows, t.band + 1);
+        const int end = outside ? 0 : band_bound(a.off, a.n_bands, a.rows, t.band + 2);
+        t.len = end > t.start ? end - t.start : 0;
+        t.first = 0;
+        t.live = outside || t.len > 0;
+        all = t.len;
+        several = t.len > 1 << a.shift;
+        tr = tid / a.octets;
+        col = 8 * (tid - tr * a.octets);
+        n = works(a) ? all : 0;
+    }
     __device__ bool works(const NormArgs& a) const { return tr < a.together; }
     __device__ double2* stats(const NormArgs& a) const { return a.stats + (b * a.n_bands + t.band) * a.groups; }
     template <class T> __device__ T* at(const View& v, int token) const {
@@ -225,7 +247,11 @@ template <int N, class F> __device__ __attribute__((always_inline)) inline void 
 }
 
 template <class T, bool WIDE> __device__ inline void norm_zero(const NormArgs& a, const NormPlace& p) {
-    for (int token = p.tr; token < p.n; token += a.together) store8<T>(p.at<T>(a.y, token), zero8<T>(), a.channels - p.col, WIDE);
+    const int first = band_bound(a.off, a.n_bands, a.rows, 1), last = band_bound(a.off, a.n_bands, a.rows, a.n_bands + 1);
+    const int step = a.zeros * a.together;
+    if (!p.works(a)) return;
+    for (int64_t row = (p.item - a.n_bands) * a.together + p.tr; row < a.rows; row += step)
+        if (row < first || row >= last) store8<T>(norm_row<T>(a.y, p.b, row) + p.col, zero8<T>(), a.channels - p.col, WIDE);
 }
 
 template <class T, int N, bool WIDE> __device__ inline void norm_out(const NormArgs& a, const NormPlace& p, const NormOctet<T>& o, const frag<T> (&x)[N]) {
@@ -244,7 +270,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     extern __shared__ __align__(16) double norm_lds[];
     __shared__ double mean[kNormGroups], squares[kNormGroups];
     const int tid = threadIdx.x;
-    const NormPlace p(a, a.items, a.shift);
+    const NormPlace p(a);
     if (!p.t.live) return;
     if (p.outside) return norm_zero<T, WIDE>(a, p);
     if (p.several) return;
@@ -259,11 +285,13 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     });
     norm_columns(a, norm_lds, p.works(a), p.tr, p.col, s, tid);
     norm_groups(a, mean, tid, cell);
+    for (int g = tid; g < a.groups; g += a.threads) mean[g] /= count;
+    __syncthreads();
     NormOctet<T> o(a, p.col);
     float m[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        m[i] = static_cast<float>(mean[o.group[i]] / count);   // (what it is off by is made up for below)
+        m[i] = static_cast<float>(mean[o.group[i]]);   // (what it is off by is made up for below)
         s[i] = 0.0;
     }
     norm_tokens<N>(a, p, [&](int k, int) __attribute__((always_inline)) {
@@ -276,15 +304,16 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     norm_columns(a, norm_lds, p.works(a), p.tr, p.col, s, tid);
     norm_groups(a, squares, tid, cell);
     // the mean of the squared differences from m is the variance and the square of the mean's own difference from m
-    auto stat = [&](int g) {
-        const double mu = mean[g] / count, off = mu - static_cast<double>(static_cast<float>(mu));
-        return double2{mu, 1.0 / sqrt(fmax(squares[g] / count - off * off, 0.0) + a.eps)};
-    };
     double2* st = p.stats(a);
-    for (int g = tid; g < a.groups; g += kNormThreads) st[g] = stat(g);
+    for (int g = tid; g < a.groups; g += a.threads) {
+        const double off = mean[g] - static_cast<double>(static_cast<float>(mean[g]));
+        squares[g] = 1.0 / sqrt(fmax(squares[g] / count - off * off, 0.0) + a.eps);
+        st[g] = double2{mean[g], squares[g]};
+    }
+    __syncthreads();
     if (!p.works(a)) return;
     o.load_affine(a, p.t.band, p.col);
-    o.set(a, stat);
+    o.set(a, [&](int g) { return double2{mean[g], squares[g]}; });
     norm_out<T, N, WIDE>(a, p, o, x);
 }
 
@@ -316,7 +345,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
     norm_columns(a, norm_lds, p.works(a), p.tr, p.col, q, tid);
     norm_groups(a, squares, tid, cell);
     double2* to = a.part + (p.b * a.parts + p.item) * a.groups;
-    for (int g = tid; g < a.groups; g += kNormThreads) to[g] = double2{sum[g], squares[g]};
+    for (int g = tid; g < a.groups; g += a.threads) to[g] = double2{sum[g], squares[g]};
 }
 
 // Joins the parts of longer bands, in order, a group a thread: into their
@@ -340,19 +369,29 @@ template <bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs
         a.stats[place * a.groups + g] = double2{all.x, 1.0 / sqrt(fmax(all.y - all.x * all.x, 0.0) + a.eps)};
 }
 
-// y of longer bands.
+// y of longer bands, a part a workgroup: the next tokens are on their way while these are computed.
 template <class T, bool WIDE>
-__global__ __launch_bounds__(kNormThreads) void k_norm_apply(NormArgs a) {
-    constexpr int N = norm_held<T>();
-    const NormPlace p(a, a.items, a.shift);
+__global__ __launch_bounds__(kNormThreads, 2) void k_norm_apply(NormArgs a) {
+    constexpr int N = norm_held<T>() / 2;
+    const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several || !p.works(a)) return;
-    frag<T> x[N];
-    p.load<T, N, WIDE>(a, a.x, x);
+    frag<T> x[N], next[N];
+    p.load<T, N, WIDE>(a, a.x, next);
     NormOctet<T> o(a, p.col);
     const double2* st = p.stats(a);
     o.load_affine(a, p.t.band, p.col);
     o.set(a, [&](int g) { return st[g]; });
-    norm_out<T, N, WIDE>(a, p, o, x);
+    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
+        for (int from = 0; from < p.n; from += N * a.together) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = next[k];
+            p.load<T, N, WIDE>(a, a.x, next, from + N * a.together);
+            each<N>([&](auto k) __attribute__((always_inline)) {
+                const int token = from + p.tr + a.together * k.value;
+                if (token < p.n) store8<T>(p.at<T>(a.y, token), o.template out<act.value>(x[k.value]), a.channels - p.col, WIDE);
+            });
+        }
+    });
 }
 
 // From the sums of dz and dz xh of a thread's 8 channels: those of the
@@ -363,7 +402,7 @@ __device__ inline void norm_grad_sums(const NormArgs& a, const NormPlace& p, flo
     const int width = 8 * a.octets, parts = norm_parts(a);
     norm_columns(a, cells, p.works(a), p.tr, p.col, s, tid);
     if (to) {
-        for (int c = tid; c < a.channels; c += kNormThreads) {
+        for (int c = tid; c < a.channels; c += a.threads) {
             float2 v = cells[norm_cell(a, c)];
             for (int k = 1; k < parts; ++k) v += cells[k * width + norm_cell(a, c)];
             to[c] = v.y;
@@ -376,30 +415,30 @@ __device__ inline void norm_grad_sums(const NormArgs& a, const NormPlace& p, flo
     norm_groups(a, second, tid, [&](int at, int c) { return cells[at].y * w(c); });
 }
 
-template <class T, int N, bool WIDE, class M>
-__device__ inline void norm_grad_out(const NormArgs& a, const NormPlace& p, const NormOctet<T>& o, const frag<T> (&x)[N], const frag<T> (&dy)[N], M means) {
-    float m1[8], m2[8];
-    each<8>([&](auto i) __attribute__((always_inline)) {
-        if (i.value && a.octet_groups) {
-            m1[i.value] = m1[0];
-            m2[i.value] = m2[0];
-        } else {
-            const double2 v = means(o.group[i.value]);
-            m1[i.value] = static_cast<float>(v.x);
-            m2[i.value] = static_cast<float>(v.y);
-        }
-    });
-    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
-        norm_tokens<N>(a, p, [&](int k, int token) __attribute__((always_inline)) {
-            float xh[8], dz[8];
-            o.template slope<act.value>(x[k], dy[k], xh, dz);
-            frag<T> f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = static_cast<T>(o.rstd[i] * (fmaf(dz[i], o.w[i], -m1[i]) - xh[i] * m2[i]));
-            store8<T>(p.at<T>(a.y, token), f, a.channels - p.col, WIDE);
+// The means of d and d xh of a thread's 8 channels' groups, and dx.
+template <class T> struct NormMeans {
+    float first[8], second[8];
+    template <class F> __device__ NormMeans(const NormArgs& a, const NormOctet<T>& o, F means) {
+        each<8>([&](auto i) __attribute__((always_inline)) {
+            if (i.value && a.octet_groups) {
+                first[i.value] = first[0];
+                second[i.value] = second[0];
+            } else {
+                const double2 v = means(o.group[i.value]);
+                first[i.value] = static_cast<float>(v.x);
+                second[i.value] = static_cast<float>(v.y);
+            }
         });
-    });
-}
+    }
+    template <int ACT> __device__ frag<T> dx(const NormOctet<T>& o, frag<T> x, frag<T> dy) const {
+        float xh[8], dz[8];
+        o.template slope<ACT>(x, dy, xh, dz);
+        frag<T> f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = static_cast<T>(o.rstd[i] * (fmaf(dz[i], o.w[i], -first[i]) - xh[i] * second[i]));
+        return f;
+    }
+};
 
 template <int ACT, class T> __device__ inline void norm_grad_add(const NormOctet<T>& o, frag<T> x, frag<T> dy, float2 (&s)[8]) {
     float xh[8], dz[8];
@@ -418,7 +457,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad(NormArgs a) {
     extern __shared__ __align__(16) double norm_lds[];
     __shared__ double first[kNormGroups], second[kNormGroups];
     const int tid = threadIdx.x;
-    const NormPlace p(a, a.items, a.shift);
+    const NormPlace p(a);
     if (!p.t.live) return;
     if (p.outside) {
         if (a.y.data) norm_zero<T, WIDE>(a, p);
@@ -442,18 +481,26 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad(NormArgs a) {
                       a.sums ? a.sums + (p.b * a.n_bands + p.t.band) * 2 * a.channels : nullptr, first, second, tid);
     if (!a.y.data) return;
     const double share = 1.0 / (static_cast<double>(p.t.len) * a.cg);
-    norm_grad_out<T, N, WIDE>(a, p, o, x, dy, [&](int g) { return double2{first[g] * share, second[g] * share}; });
+    const NormMeans<T> means(a, o, [&](int g) { return double2{first[g] * share, second[g] * share}; });
+    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
+        norm_tokens<N>(a, p, [&](int k, int token) __attribute__((always_inline)) {
+            store8<T>(p.at<T>(a.y, token), means.template dx<act.value>(o, x[k], dy[k]), a.channels - p.col, WIDE);
+        });
+    });
 }
 
 // The sums of d and d xh of the parts of longer bands, and what they add to dw and db.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
-    constexpr int N = 4;
+    constexpr int N = 2;
     extern __shared__ __align__(16) double norm_lds[];
     __shared__ double first[kNormGroups], second[kNormGroups];
     const int tid = threadIdx.x;
     const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several) return;
+    frag<T> x[N], dy[N], x_next[N], dy_next[N];
+    p.load<T, N, WIDE>(a, a.x, x_next);
+    p.load<T, N, WIDE>(a, a.dy, dy_next);
     NormOctet<T> o(a, p.col);
     if (p.works(a)) {
         const double2* st = p.stats(a);
@@ -463,11 +510,15 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
     float2 s[8] = {};
     by_act(a.act, [&](auto act) __attribute__((always_inline)) {
         for (int from = 0; from < p.all; from += N * a.together) {
-            frag<T> x[N], dy[N];
-            p.load<T, N, WIDE>(a, a.x, x, from);
-            p.load<T, N, WIDE>(a, a.dy, dy, from);
 #pragma unroll
-            for (int k = 0; k < N; ++k)   // (where a token is not there, dy is 0)
+            for (int k = 0; k < N; ++k) {
+                x[k] = x_next[k];
+                dy[k] = dy_next[k];
+            }
+            p.load<T, N, WIDE>(a, a.x, x_next, from + N * a.together);
+            p.load<T, N, WIDE>(a, a.dy, dy_next, from + N * a.together);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
                 if (from + p.tr + a.together * k < p.n) norm_grad_add<act.value>(o, x[k], dy[k], s);
         }
     });
@@ -475,30 +526,46 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
                       a.sums ? a.sums + (static_cast<int64_t>(a.batch) * a.n_bands + p.b * a.parts + p.item) * 2 * a.channels : nullptr,
                       first, second, tid);
     double2* to = a.part + (p.b * a.parts + p.item) * a.groups;
-    for (int g = tid; g < a.groups; g += kNormThreads) to[g] = double2{first[g], second[g]};
+    for (int g = tid; g < a.groups; g += a.threads) to[g] = double2{first[g], second[g]};
 }
 
-// dx of longer bands.
+// dx of longer bands, a part a workgroup.
 template <class T, bool WIDE>
-__global__ __launch_bounds__(kNormThreads) void k_norm_grad_apply(NormArgs a) {
-    constexpr int N = norm_held<T>() / 2;
-    const NormPlace p(a, a.items, a.shift);
+__global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_apply(NormArgs a) {
+    constexpr int N = 2;
+    const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several || !p.works(a)) return;
-    frag<T> x[N], dy[N];
-    p.load<T, N, WIDE>(a, a.x, x);
-    p.load<T, N, WIDE>(a, a.dy, dy);
+    frag<T> x[N], dy[N], x_next[N], dy_next[N];
+    p.load<T, N, WIDE>(a, a.x, x_next);
+    p.load<T, N, WIDE>(a, a.dy, dy_next);
     NormOctet<T> o(a, p.col);
-    const double2 *st = p.stats(a), *means = a.part + norm_part(a, p.b, p.t.band, p.t.start) * a.groups;
+    const double2 *st = p.stats(a), *sums = a.part + norm_part(a, p.b, p.t.band, p.t.start) * a.groups;
     o.load_affine(a, p.t.band, p.col);
     o.set(a, [&](int g) { return st[g]; });
-    norm_grad_out<T, N, WIDE>(a, p, o, x, dy, [&](int g) { return means[g]; });
+    const NormMeans<T> means(a, o, [&](int g) { return sums[g]; });
+    by_act(a.act, [&](auto act) __attribute__((always_inline)) {
+        for (int from = 0; from < p.n; from += N * a.together) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                x[k] = x_next[k];
+                dy[k] = dy_next[k];
+            }
+            p.load<T, N, WIDE>(a, a.x, x_next, from + N * a.together);
+            p.load<T, N, WIDE>(a, a.dy, dy_next, from + N * a.together);
+            each<N>([&](auto k) __attribute__((always_inline)) {
+                const int token = from + p.tr + a.together * k.value;
+                if (token < p.n)
+                    store8<T>(p.at<T>(a.y, token), means.template dx<act.value>(o, x[k.value], dy[k.value]), a.channels - p.col, WIDE);
+            });
+        }
+    });
 }
 
 // dw and db where bands are so short that what each adds to them would be as
 // much as the data: sums over 2^weight_shift rows of a band, token r % len of
 // signal r / len.
 template <class T, bool WIDE>
-__global__ __launch_bounds__(kNormThreads) void k_norm_weight(NormArgs a) {
+__global__ __launch_bounds__(kNormThreads, 2) void k_norm_weight(NormArgs a) {
     extern __shared__ __align__(16) double norm_lds[];
     float2* cells = reinterpret_cast<float2*>(norm_lds);
     const int tid = threadIdx.x, lane = tid & 63;
@@ -530,7 +597,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_weight(NormArgs a) {
     }
     norm_columns(a, cells, works, tr, col, s, tid);
     float* to = a.sums + static_cast<int64_t>(id) * 2 * a.channels;
-    for (int c = tid; c < a.channels; c += kNormThreads) {
+    for (int c = tid; c < a.channels; c += a.threads) {
         float2 v = cells[norm_cell(a, c)];
         for (int k = 1; k < norm_parts(a); ++k) v += cells[k * 8 * a.octets + norm_cell(a, c)];
         to[c] = v.y;
