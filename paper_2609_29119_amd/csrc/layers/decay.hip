@@ -30,7 +30,7 @@ int check_state(const float* p) {
     return NSGCQT_OK;
 }
 
-// Tokens of a segment, 128 to 4096 (2048 for the gradients, where some heads
+// Tokens of a segment, 64 to 4096 (2048 for the gradients, where some heads
 // walk through them several times): the most that leave 1536 workgroups of one
 // result head each; and of a part of it, at most 1024, as many of one key head
 // (few of a ragged row's tokens lie in bands of several segments). A part's
@@ -38,7 +38,7 @@ int check_state(const float* p) {
 // of less than 8 head_dim tokens only below 1024 workgroups. 131,072 tokens, 8
 // heads of 128, bfloat16: 1024 tokens 445 us, 512 tokens 480, 2048 560.
 int shift_of(int64_t batch, int64_t rows, int64_t heads, int64_t dim, int shift) {
-    while (shift > 7 && product(batch, rows >> shift, heads) < (1 << shift > 8 * dim ? 1536 : 1024)) --shift;
+    while (shift > 6 && product(batch, rows >> shift, heads) < (1 << shift > 8 * dim ? 1536 : 1024)) --shift;
     return shift;
 }
 struct DecayCut { int shift, fine; };

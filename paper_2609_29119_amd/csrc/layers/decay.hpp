@@ -49,16 +49,51 @@ template <class T> __device__ inline T* decay_row(const View& v, int64_t b, int6
     return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row + head * v.head;
 }
 
-// decay^n of a head, l2 the decay's base-2 logarithm. The product is formed in
-// 64 bits and only its fraction enters the exponential: the power is right to
-// the last bits of 32 however long the distance.
-__device__ inline float decay_power(double l2, int64_t n) {
-    if (n == 0) return 1.f;
-    const double x = fmin(fmax(l2 * static_cast<double>(n), -400.0), 400.0);
-    if (l2 != l2) return __builtin_nanf("");
-    const double whole = floor(x);
-    return ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), static_cast<int>(whole));
+// decay^n of a head, rounded once.
+__device__ inline float decay_power(double log_decay, int64_t n) {
+    return n == 0 ? 1.f : static_cast<float>(exp(log_decay * static_cast<double>(n)));
 }
+
+// A state decays by n tokens many times over; with the factor rounded, by the
+// same error each time: by 1e-5 after as many tiles as a slow head remembers. So
+// where it is near 1 it is kept as its difference from 1,
+struct DecayBy {
+    bool near;
+    float by;
+    __device__ DecayBy(double log_decay, int64_t n) {
+        const double less = expm1(log_decay * static_cast<double>(n));
+        near = less > -0.5;
+        by = near ? static_cast<float>(less) : decay_power(log_decay, n);
+    }
+    template <class V> __device__ V of(V s) const { return near ? s * by + s : s * by; }   // (one multiply-add)
+};
+// or, where a state's many values should take one multiplication each, its two
+// neighbours in 32 bits take turns, so that their product so far is right to one
+// rounding.
+struct DecayFactors {
+    float low, high, share, phase = 0.f;   // share: of the turns that are `high`'s
+    __device__ static float uniform(float x) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+    }
+    __device__ DecayFactors(double log_decay, int64_t n) {
+        const double factor = exp(log_decay * static_cast<double>(n));
+        const float near = static_cast<float>(factor);
+        const int bits = __builtin_bit_cast(int, near);
+        const bool normal = factor > 1e-30 && factor < 1e30;
+        const bool over = static_cast<double>(near) > factor;
+        const float below = normal && over ? __builtin_bit_cast(float, bits - 1) : near;
+        const float above = normal && !over ? __builtin_bit_cast(float, bits + 1) : near;
+        low = uniform(below);
+        high = uniform(above);
+        share = uniform(normal ? static_cast<float>((factor - below) / (static_cast<double>(above) - below)) : 0.f);
+    }
+    __device__ float next() {
+        phase += share;
+        const bool turn = phase >= 1.f;
+        phase = uniform(turn ? phase - 1.f : phase);
+        return turn ? high : low;
+    }
+};
 
 // As read_turned, with bits 2 and 3 of the column's number exchanged: a
 // product's result whose rows are these columns then holds, in registers
@@ -225,9 +260,9 @@ __device__ inline float* decay_state_of(const DecayArgs& a, const DecayJob& j, c
 // products are formed transposed, so that the scores, the state and the result
 // go from one to the next without a trip through LDS.
 template <class T, int DP, bool WIDE>
-__global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_decay(DecayArgs a) {
+__global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP >= 96 ? 1 : 2) void k_decay(DecayArgs a) {
     constexpr int RB = row_bytes<T, DP>(), ND = DP / 32, NK = DP / 16;
-    constexpr bool kEarly = WIDE || sizeof(T) == 2;   // the next tiles are on their way while these are computed
+    constexpr bool kEarly = WIDE || (sizeof(T) == 2 && DP <= 64);   // the next tiles are on their way while these are computed
     __shared__ __align__(128) char ta[2][kDecayTile * RB], tb[2][kDecayTile * RB], tc[2][kDecayTile * RB];
     __shared__ float power[kDecayTile + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
@@ -256,8 +291,9 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
     fetch_a(0, kept);
     fetch_bc(0, 0, 0, kept);
     if (count > 1) kept_next = kept_of(1);
-    const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
-    if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
+    const double log_decay = a.log_decay[p.kv];
+    DecayFactors across(log_decay, kDecayTile);
+    if (tid <= kDecayTile) power[tid] = decay_power(log_decay, tid);
     acc16 s[ND];
     bool some;
     const float* from = decay_state_of(a, j, p, some);
@@ -284,7 +320,7 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
         const int lag = m - (8 * (r >> 2) + 4 * h + (r & 3));
         fade[r] = lag < 0 ? 0.f : power[lag] * a.scale;
     }
-    const float up = power[m + 1] * a.scale, across = power[kDecayTile];
+    const float up = power[m + 1] * a.scale;
     T* to = decay_row<T>(j.out, p.b, p.token(m, reverse), p.head);   // (of the last tile, perhaps past the segment: not used)
     const int64_t to_step = (reverse ? -j.out.row : j.out.row) * kDecayTile;
     int stage = 0;
@@ -307,16 +343,18 @@ __global__ __launch_bounds__(2 * DP, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k
             if (end && tile + 2 < count) kept_next = kept_of(tile + 2);
             if (g == 0) {
                 each<NK>([&](auto x) __attribute__((always_inline)) {
+                    if (DP <= 64 && 16 * x.value >= a.dim) return;   // (wider heads: the branches cost more, 334 -> 368 us)
                     const auto af = data_of(read8<T, RB>(xa, m, 2 * x.value + h));
                     out = product(sum_of<T, 2>(octet(s[x.value / 2], x.value % 2)), af, out);
                 });
                 out *= up;
+                const float by = across.next();
 #pragma unroll
-                for (int d = 0; d < ND; ++d) s[d] *= across;
+                for (int d = 0; d < ND; ++d) s[d] *= by;
             }
             acc16 q = zero16();
             each<NK>([&](auto x) __attribute__((always_inline)) {
-                q = mma(read8<T, RB>(xb, m, 2 * x.value + h), read8<T, RB>(xa, m, 2 * x.value + h), q);
+                if (DP > 64 || 16 * x.value < a.dim) q = mma(read8<T, RB>(xb, m, 2 * x.value + h), read8<T, RB>(xa, m, 2 * x.value + h), q);
             });
 #pragma unroll
             for (int r = 0; r < 16; ++r) q[r] *= fade[r];
@@ -369,8 +407,9 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
     unsigned kept = use(0), kept_next = 0;
     fetch(0, 0, 0, kept);
     if (count > 1) kept_next = use(1);
-    const double l2 = static_cast<double>(a.log_decay[p.kv]) * 1.4426950408889634;
-    if (tid <= kDecayTile) power[tid] = decay_power(l2, tid);
+    const double log_decay = a.log_decay[p.kv];
+    DecayFactors across(log_decay, kDecayTile);
+    if (tid <= kDecayTile) power[tid] = decay_power(log_decay, tid);
     bool there;
     float* to = decay_state_of(a, j, p, there);
     const int col = 32 * wave + m;
@@ -394,9 +433,9 @@ __global__ __launch_bounds__(2 * DP, 2) void k_decay_sum(DecayArgs a) {
         if (more) fetch(stage + 1, end ? tile + 1 : tile, end ? 0 : g + 1, kept);
         if (end && tile + 2 < count) kept_next = use(tile + 2);
         if (g == 0) {
-            const float across = power[n];
+            const float by = n == kDecayTile ? across.next() : power[n];
 #pragma unroll
-            for (int d = 0; d < ND; ++d) s[d] *= across;
+            for (int d = 0; d < ND; ++d) s[d] *= by;
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -439,8 +478,8 @@ template <int V> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a
     const int64_t b = id / a.n_bands;
     const int start = band_bound(a.off, a.n_bands, a.rows, band + 1), len = band_bound(a.off, a.n_bands, a.rows, band + 2) - start;
     if (len <= 1 << a.shift || e >= size) return;
-    const double l2 = static_cast<double>(a.log_decay[kv]) * 1.4426950408889634;
-    const float across = decay_power(l2, int64_t(1) << a.fine);
+    const double log_decay = a.log_decay[kv];
+    const DecayBy across(log_decay, int64_t(1) << a.fine);
     const int count = (len + (1 << a.fine) - 1) >> a.fine, each = (1 << (a.shift - a.fine)) - 1;
     const int last = (len - 1) >> a.shift << (a.shift - a.fine);   // the part that the last segment starts with
     const int64_t step = static_cast<int64_t>(a.kv_heads) * size;
@@ -458,10 +497,10 @@ template <int V> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a
         for (int k = 0; k < kAhead; ++k)
             if (i + k < end) {
                 if (((i + k) & each) == 0) at(i + k) = s;
-                s = across * s + add[k];
+                s = across.of(s) + add[k];
             }
     }
-    if (st) *reinterpret_cast<vec*>(st) = decay_power(l2, len - (static_cast<int64_t>(end) << a.fine)) * s + at(end);
+    if (st) *reinterpret_cast<vec*>(st) = decay_power(log_decay, len - (static_cast<int64_t>(end) << a.fine)) * s + at(end);
     if ((end & each) == 0) at(end) = s;
 }
 
@@ -512,7 +551,7 @@ __global__ __launch_bounds__(256) void k_decay_step(DecayStepArgs a) {
     if (c0 < a.dim)
 #pragma unroll
         for (int x = 0; x < V; ++x) v[x] = static_cast<float>(vp[c0 + x]);
-    const float fade = decay_power(static_cast<double>(a.log_decay[kv]) * 1.4426950408889634, 1);
+    const DecayBy fade(a.log_decay[kv], 1);
     if (tid < DP) ks[tid] = tid < a.dim ? static_cast<float>(kp[tid]) : 0.f;
     __syncthreads();
 #pragma unroll
@@ -520,7 +559,7 @@ __global__ __launch_bounds__(256) void k_decay_step(DecayStepArgs a) {
         const int r = r0 + kRows * i;
         const float kr = ks[r];
 #pragma unroll
-        for (int x = 0; x < V; ++x) s[i][x] = fmaf(pos > 0 ? fade : 0.f, s[i][x], kr * v[x]);
+        for (int x = 0; x < V; ++x) s[i][x] = fmaf(kr, v[x], pos > 0 ? fade.of(s[i][x]) : 0.f);
         if (r < a.dim && c0 < a.dim) *reinterpret_cast<vec*>(st + r * a.dim + c0) = s[i];
     }
     for (int g0 = 0; g0 < a.group; g0 += kHeads) {

@@ -157,6 +157,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_kept(GatedArgs a) {
     constexpr int BK = gated_inputs<T>(), BN = 32 * NB, KS = BK / 16, RB = row_bytes<T, BK>();
     __shared__ __align__(128) char ws[2 * BN * RB];
     __shared__ __align__(16) float start[2 * BN];
+    __shared__ __align__(128) char slabs[4][4096];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_number(), m = lane & 31, h = lane >> 5;
     const int cols = (a.n_out + BN - 1) / BN;
     const unsigned id = last_first(blockIdx.x, gridDim.x), p = id / cols;
@@ -226,8 +227,13 @@ __global__ __launch_bounds__(256, 2) void k_gated_kept(GatedArgs a) {
 #pragma unroll
                 for (int q = 0; q < 16; ++q) acc[nb][q] = act_of<act.value, sizeof(T) == 4>(acc[nb][q]) * acc[NB + nb][q];
         });
+        T* row_out[4];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) store_column<T>(to, acc[nb], c0 + 32 * nb, a.n_out, a.y_wide, lane);
+        for (int e = 0; e < 4; ++e) row_out[e] = from_lane(to, lane / 8 + 8 * e);
+        acc16 y[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) y[nb] = acc[nb];
+        store_rows<T, NB>(slabs[wave], y, row_out, min(n - r, 32), c0, a.n_out, a.y_wide, lane);
     }
 }
 

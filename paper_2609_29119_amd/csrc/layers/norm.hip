@@ -75,13 +75,14 @@ int held_of(int dtype, bool grad) { return (dtype == NSGCQT_F32 ? norm_held<floa
 
 // Bytes of the workspace, whose parts begin at 16-byte boundaries: chunks'
 // statistics, then the weights' partial sums.
-struct NormSpace { int64_t part, sums; };
+struct NormSpace { int64_t part, sums; };   // (sums: without gradient, the statistics, for a call that does not ask for them)
 NormSpace norm_space(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, bool grad, bool weights) {
     NormArgs a = norm_args(r, s);
     if (a.channels == 0) return {0, 0};
     set_chunk(a, held_of(dtype, grad));
     NormSpace n{0, 0};
     if (has_parts(a)) n.part = product(16, r->batch, static_cast<int64_t>(a.parts), a.groups);
+    if (has_parts(a) && !grad) n.sums = product(16, r->batch, r->n_bands, a.groups);
     if (grad && weights)
         n.sums = product(8, chunks_sum(a) ? product(r->batch, r->n_bands + static_cast<int64_t>(a.parts))
                                           : tile_count(weight_shift_of(r->batch, r->rows), r->n_bands, r->batch, r->rows), a.channels);
@@ -130,15 +131,16 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     CHECK_TRY(check_view(x, "x", dtype, r->batch, r->rows, 1, s->channels, wide));
     CHECK_TRY(check_view(y, "y", dtype, r->batch, r->rows, 1, s->channels, wide));
     if (r->batch == 0 || r->rows == 0 || s->channels == 0) return NSGCQT_OK;
-    if (!stats || misaligned(stats, 16)) return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 16 bytes");
+    if (misaligned(stats, 16)) return set_err(NSGCQT_EINVAL, "stats is not aligned to 16 bytes");
     const NormSpace space = norm_space(dtype, r, s, false, false);
     CHECK_TRY(check_space(ws, ws_bytes, norm_bytes(space)));
     NormArgs a = norm_args(r, s);
     set_chunk(a, held_of(dtype, false));
     a.x = view_of(x);
     a.y = view_of(y);
-    a.stats = reinterpret_cast<double2*>(stats);
     a.part = static_cast<double2*>(ws);
+    a.stats = stats ? reinterpret_cast<double2*>(stats)
+                    : space.part ? reinterpret_cast<double2*>(static_cast<char*>(ws) + space.part) : nullptr;
     const int64_t blocks = product(r->batch, r->n_bands + a.zeros);
     CHECK_TRY(check_grid(blocks));
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
@@ -173,7 +175,7 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     const bool weights = dw || db;
     if (s->channels == 0 || (!dx && !weights)) return NSGCQT_OK;
     const bool rows = r->batch > 0 && r->rows > 0;
-    if (rows && (!stats || misaligned(stats, 16)))
+    if (rows && r->n_bands > 0 && (!stats || misaligned(stats, 16)))
         return set_err(NSGCQT_EINVAL, "stats is NULL or not aligned to 16 bytes");
     const NormSpace space = norm_space(dtype, r, s, true, weights);
     CHECK_TRY(check_space(ws, ws_bytes, norm_bytes(space)));

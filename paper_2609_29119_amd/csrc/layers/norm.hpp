@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     for (int g = tid; g < a.groups; g += a.threads) {
         const double off = mean[g] - static_cast<double>(static_cast<float>(mean[g]));
         squares[g] = 1.0 / sqrt(fmax(squares[g] / count - off * off, 0.0) + a.eps);
-        st[g] = double2{mean[g], squares[g]};
+        if (a.stats) st[g] = double2{mean[g], squares[g]};
     }
     __syncthreads();
     if (!p.works(a)) return;

@@ -604,16 +604,24 @@ def _decay_shape_of(q, k, log_decay, keep, scale):
                         0 if keep is None else keep.data_ptr(), 0 if keep is None else keep.stride(0))
 
 
-def _decay_workspace(r, shape, grad, like):
-    n = _bytes(_lib().nsgcqt_decay_attention_workspace(r, shape, grad))
-    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None, n
+@functools.lru_cache(maxsize=256)
+def _decay_bytes(bands, batch, rows, heads, kv_heads, dim, grad):
+    here = ctypes.c_int64(0)   # offsets and decays that are not read
+    at = ctypes.addressof(here)
+    return _bytes(_lib().nsgcqt_decay_attention_workspace(_rows(at, bands, batch, rows),
+                                                          _decay_shape(heads, kv_heads, dim, 1.0, at, 0, 0), grad))
+
+
+def _decay_workspace(q, kv_heads, offsets, grad):
+    n = _decay_bytes(offsets.shape[0] - 1, q.shape[0], q.shape[1], q.shape[2], kv_heads, q.shape[3], grad)
+    return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None, n
 
 
 def _decay_forward(q, k, v, offsets, log_decay, keep, state, scale):
     o = torch.empty_like(q, memory_format=torch.contiguous_format)
     shape, r = _decay_shape_of(q, k, log_decay, keep, scale), _ragged(offsets, q.shape[0], q.shape[1])
     with _on(q):
-        ws, n = _decay_workspace(r, shape, 0, q)
+        ws, n = _decay_workspace(q, k.shape[2], offsets, 0)
         _check(_lib().nsgcqt_decay_attention(
             _DTYPES[q.dtype], r, shape, _view4(q), _view4(k), _view4(v), _view4(o),
             None if state is None else state.data_ptr(), ws.data_ptr() if n else None, n, _stream(q)))
@@ -635,7 +643,7 @@ class _DecayAttention(torch.autograd.Function):
         dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
         shape, r = _decay_shape_of(q, k, log_decay, keep, ctx.scale), _ragged(offsets, q.shape[0], q.shape[1])
         with _on(q):
-            ws, n = _decay_workspace(r, shape, 1, q)
+            ws, n = _decay_workspace(q, k.shape[2], offsets, 1)
             _check(_lib().nsgcqt_decay_attention_grad(
                 _DTYPES[q.dtype], r, shape, _view4(q), _view4(k), _view4(v), _view4(do), _view4(dq), _view4(dk),
                 _view4(dv), ws.data_ptr() if n else None, n, _stream(q)))
@@ -752,31 +760,39 @@ def _norm_shape_of(x, weight, bias, groups, act, eps):
     return _norm_shape(x.shape[2], groups, eps, w[0], b[0], w[1], b[1], act)
 
 
-def _norm_workspace(x, r, shape, grad, weights):
-    n = _bytes(_lib().nsgcqt_band_norm_workspace(_DTYPES[x.dtype], r, shape, grad, weights))
+@functools.lru_cache(maxsize=256)
+def _norm_bytes(dtype, bands, batch, rows, channels, groups, act, eps, grad, weights):
+    here = ctypes.c_int64(0)   # offsets that are not read
+    return _bytes(_lib().nsgcqt_band_norm_workspace(dtype, _rows(ctypes.addressof(here), bands, batch, rows),
+                                                    _norm_shape(channels, groups, eps, 0, 0, 0, 0, act), grad, weights))
+
+
+def _norm_workspace(x, bands, groups, act, eps, grad, weights):
+    n = _norm_bytes(_DTYPES[x.dtype], bands, x.shape[0], x.shape[1], x.shape[2], groups, act, eps, grad, weights)
     return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None, n
 
 
-def _norm_call(x, offsets, weight, bias, groups, act, eps):
-    batch, rows, channels = x.shape
+def _norm_call(x, offsets, weight, bias, groups, act, eps, stats=None):
+    batch, rows, _ = x.shape
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    stats = torch.empty((batch, offsets.numel() - 1, groups, 2), dtype=torch.float64, device=x.device)
     shape, r = _norm_shape_of(x, weight, bias, groups, act, eps), _ragged(offsets, batch, rows)
     with _on(x):
-        ws, n = _norm_workspace(x, r, shape, 0, 0)
-        _check(_lib().nsgcqt_band_norm(_DTYPES[x.dtype], r, shape, _view3(x), _view3(y), stats.data_ptr(),
-                                       ws.data_ptr() if n else None, n, _stream(x)))
-    return y, stats
+        ws, n = _norm_workspace(x, offsets.shape[0] - 1, groups, act, eps, 0, 0)
+        _check(_lib().nsgcqt_band_norm(_DTYPES[x.dtype], r, shape, _view3(x), _view3(y),
+                                       None if stats is None else stats.data_ptr(), ws.data_ptr() if n else None, n,
+                                       _stream(x)))
+    return y
 
 
 def _norm_forward(x, weight, bias, offsets, groups, act, eps):
-    return _norm_call(x, offsets, weight, bias, groups, act, eps)[0]
+    return _norm_call(x, offsets, weight, bias, groups, act, eps)
 
 
 class _BandNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, offsets, groups, act, eps):
-        y, stats = _norm_call(x, offsets, weight, bias, groups, act, eps)
+        stats = torch.empty((x.shape[0], offsets.numel() - 1, groups, 2), dtype=torch.float64, device=x.device)
+        y = _norm_call(x, offsets, weight, bias, groups, act, eps, stats)
         ctx.save_for_backward(x, weight, bias, offsets, stats)
         ctx.how = groups, act, eps
         return y
@@ -792,7 +808,7 @@ class _BandNorm(torch.autograd.Function):
                   for t, n in ((weight, need[1]), (bias, need[2])))
         shape, r = _norm_shape_of(x, weight, bias, *ctx.how), _ragged(offsets, x.shape[0], x.shape[1])
         with _on(x):
-            ws, n = _norm_workspace(x, r, shape, 1, dw is not None or db is not None)
+            ws, n = _norm_workspace(x, offsets.shape[0] - 1, *ctx.how, 1, int(dw is not None or db is not None))
             _check(_lib().nsgcqt_band_norm_grad(
                 _DTYPES[x.dtype], r, shape, _view3(x), stats.data_ptr(), _view3(dy),
                 None if dx is None else _view3(dx), None if dw is None else dw.data_ptr(),
@@ -817,9 +833,11 @@ def band_norm(x, offsets, weight=None, bias=None, groups=1, activation=None, eps
     for t, name in ((weight, "weight"), (bias, "bias")):
         if t is not None:
             _tensor(t, name, x, (offsets.numel() - 1, x.shape[2]))
-    act = _act(activation)
+    act, groups = _act(activation), int(groups)
+    if groups < 1 or x.shape[2] % groups:
+        _bad("groups must divide channels, and be at least 1")
     call = _BandNorm.apply if _trains(x, weight, bias) else _norm_forward
-    return call(x, weight, bias, offsets, int(groups), act, float(eps))
+    return call(x, weight, bias, offsets, groups, act, float(eps))
 
 
 class BandNorm(torch.nn.Module):

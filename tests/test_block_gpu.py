@@ -419,3 +419,564 @@ def test_band_gated_strides_and_uncovered_tokens(dtype):
         close(dw, ref[2], size[2], "dw", sums_of(dtype), 2.0 ** -25)
         for t in (y, dx):
             assert t[:, :first].abs().max() == 0 and t[:, first + 167:].abs().max() == 0
+
+
+# ------------------------------------------------------- where it can go wrong
+
+
+def tiny_of(dtype):
+    return 2.0 ** -25 if dtype == torch.float16 else 1e-37
+
+
+def decay_by_blocks(q, k, v, n, log_decay, scale, state=None):
+    """One band from its first token, in 64 bits, a block of 256 tokens at a time; heads of q, k and v alike."""
+    q, k, v = (t.double() for t in (q, k, v))
+    lam = log_decay.double()[:, None, None]
+    s = torch.zeros(*q.shape[:1], q.shape[2], q.shape[3], q.shape[3], device="cuda").double() if state is None else state
+    o = torch.zeros_like(q)
+    for a in range(0, n, 256):
+        b = min(a + 256, n)
+        i = torch.arange(b - a, device="cuda", dtype=torch.float64)[:, None]
+        fade = torch.where(i >= i.T, ((i - i.T).clamp(min=0) * lam).exp(), 0.0)
+        x, y, z = (t[:, a:b].transpose(1, 2) for t in (q, k, v))
+        p = torch.matmul(x, y.mT.contiguous()) * fade
+        o[:, a:b] = ((torch.matmul(p, z) + torch.matmul(x, s) * (lam * (i + 1)).exp()) * scale).transpose(1, 2)
+        s = s * (lam * (b - a)).exp() + torch.matmul((y * (lam * (b - a - 1 - i)).exp()).mT.contiguous(), z)
+    return o, s
+
+
+@pytest.mark.parametrize("dtype,h,hk,d,lengths", [
+    (torch.bfloat16, 8, 2, 16, [131072]),          # segments of several parts
+    (torch.float32, 2, 2, 32, [20000, 7, 9000]),
+    (torch.float16, 4, 4, 64, [33000]),
+])
+def test_decay_attention_of_long_bands(dtype, h, hk, d, lengths):
+    """The quadratic form is too long here: the same by blocks, which the short cases' check covers in the kernels. The
+    2-norm: one rounding (at most u), and 2^-16 (2^-21) of sums whose terms are at most 16 times larger than they."""
+    rows, scale = sum(lengths), d ** -0.5
+    q, k, v, do = (randn(i, 1, rows, n, d, dtype=dtype).requires_grad_(i < 4) for i, n in ((1, h), (2, hk), (3, hk), (4, h)))
+    lam = -torch.logspace(-0.5, -4, hk).cuda()
+    off = offsets_of(lengths)
+    state = randn(9, len(lengths), hk, d, d, by=2.0)
+    with torch.no_grad():
+        last = state.clone()
+        carried = layers.decay_attention(q, k, v, off, lam, state=last)
+    o = layers.decay_attention(q, k, v, off, lam)
+    grads = torch.autograd.grad(o, [q, k, v], do)
+    lam_h, group, at = lam.repeat_interleave(h // hk), h // hk, 0
+    bound = U[dtype] + 16 * (2.0 ** -21 if dtype == torch.float32 else 2.0 ** -16)
+
+    def near(got, want, what, by=bound):
+        assert ((got.double() - want).norm() <= by * want.norm()).item(), what
+
+    for g, n in enumerate(lengths):
+        s = slice(at, at + n)
+        at += n
+        x, e = q[:, s].detach(), do[:, s]
+        y, z = (t[:, s].detach().repeat_interleave(group, 2) for t in (k, v))
+        back = lambda a, b, c: decay_by_blocks(a.flip(1), b.flip(1), c.flip(1), n, lam_h, scale)[0].flip(1)  # noqa: E731
+        near(o[:, s], decay_by_blocks(x, y, z, n, lam_h, scale)[0], "o")
+        near(grads[0][:, s], decay_by_blocks(e, z, y, n, lam_h, scale)[0], "dq")
+        near(grads[1][:, s], back(z, e, x).unflatten(2, (hk, group)).sum(3), "dk")
+        near(grads[2][:, s], back(y, x, e).unflatten(2, (hk, group)).sum(3), "dv")
+        want, after = decay_by_blocks(x, y, z, n, lam_h, scale, state[g:g + 1].double().repeat_interleave(group, 1))
+        near(carried[:, s], want, "o from a state")
+        near(last[g:g + 1], after[:, ::group], "state", 16 * 2.0 ** -21)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decay_attention_strides_scale_and_uncovered_tokens(dtype):
+    lengths, first, rows, d = [50, 140], 7, 200, 20
+    base = randn(1, 3, rows + 1, 6, d + 1, dtype=dtype)
+    q = base[::2, 1:, 1:5, 1:].detach().requires_grad_()        # odd strides, a base off by one
+    k = randn(2, rows, 2, 2, d, dtype=dtype).transpose(0, 1).detach().requires_grad_()
+    v = randn(3, 2, 2, rows, d, dtype=dtype).transpose(1, 2).detach().requires_grad_()
+    do = randn(4, 2, 4, rows, d, dtype=dtype).transpose(1, 2)
+    lam = decays_of(2, 5)
+    o = layers.decay_attention(q, k, v, offsets_of(lengths, first), lam, scale=-0.4)
+    got = (o, *torch.autograd.grad(o, [q, k, v], do))
+    ref, size = decay_reference(q, k, v, lengths, first, lam, -0.4, do=do)
+    for t, r, z, name in zip(got, ref, size, ("o", "dq", "dk", "dv")):
+        close(t, r, z, name, sums_of(dtype), tiny_of(dtype))
+        assert t[:, :first].abs().max() == 0 and t[:, first + 190:].abs().max() == 0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decay_attention_never_uses_what_is_not_kept(dtype):
+    lengths = [200, 90]
+    q, k, v, do = (randn(i, 2, 290, n, 32, dtype=dtype) for i, n in ((1, 4), (2, 2), (3, 2), (4, 4)))
+    keep = torch.rand(2, 290, generator=torch.Generator().manual_seed(0)) > 0.4
+    keep[:, 100:200] = False
+    keep, lam, off = keep.cuda(), decays_of(2), offsets_of(lengths)
+    state = torch.zeros(4, 2, 32, 32, device="cuda")
+    want = layers.decay_attention(q, k, v, off, lam, keep=keep, state=state)
+    for bad in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).min):
+        k2, v2 = (torch.where(keep[..., None, None], t, bad).to(dtype).requires_grad_() for t in (k, v))
+        q2 = q.detach().requires_grad_()
+        o = layers.decay_attention(q2, k2, v2, off, lam, keep=keep)
+        assert torch.equal(o, layers.decay_attention(q, k, v, off, lam, keep=keep))
+        dq, dk, dv = torch.autograd.grad(o, [q2, k2, v2], do)
+        assert torch.isfinite(dq).all() and not dk[~keep].any() and not dv[~keep].any()
+        s2 = torch.zeros_like(state)
+        with torch.no_grad():
+            assert torch.equal(layers.decay_attention(q, k2, v2, off, lam, keep=keep, state=s2), want)
+        assert torch.equal(s2, state)
+    # nothing kept: zeros, no gradient, and a state that only decays
+    none = torch.zeros_like(keep)
+    q2 = q.detach().requires_grad_()
+    o = layers.decay_attention(q2, k, v, off, lam, keep=none)
+    assert not o.any() and not torch.autograd.grad(o, [q2], do)[0].any()
+    s2 = randn(8, 4, 2, 32, 32)
+    before = s2.double()
+    layers.decay_attention(q, k, v, off, lam, keep=none, state=s2)
+    n = torch.tensor(lengths * 2, device="cuda").double()[:, None, None, None]
+    faded = before * (lam.double()[None, :, None, None] * n).exp()
+    # six tiles and a rest: a rounding of the state each, and two of the factors' product
+    assert ((s2 - faded).abs() <= 2.0 ** -20 * faded.abs() + 1e-37).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decays_at_their_ends(dtype):
+    """A head that keeps all, one that keeps nothing but the token itself, and ones beyond 32 bits of any power."""
+    lam = torch.tensor([0.0, -float("inf"), -200.0, -1e-30], device="cuda")
+    q, k, v, do = (randn(i, 1, 150, 4, 24, dtype=dtype).requires_grad_(i < 4) for i in (1, 2, 3, 4))
+    off = offsets_of([150])
+    o = layers.decay_attention(q, k, v, off, lam)
+    got = (o, *torch.autograd.grad(o, [q, k, v], do))
+    as_finite = torch.tensor([0.0, -1e4, -200.0, 0.0], device="cuda")
+    ref, size = decay_reference(q, k, v, [150], 0, as_finite, 24 ** -0.5, do=do)
+    for t, r, z, name in zip(got, ref, size, ("o", "dq", "dk", "dv")):
+        close(t, r, z, name, sums_of(dtype), tiny_of(dtype))
+
+
+def test_an_infinite_token_reaches_no_tile_before_it():
+    q, k, v = (randn(i, 1, 200, 2, 32, dtype=torch.bfloat16) for i in (1, 2, 3))
+    off, lam = offsets_of([200]), decays_of(2)
+    want = layers.decay_attention(q, k, v, off, lam)
+    k[:, 130], v[:, 131] = float("inf"), float("nan")
+    got = layers.decay_attention(q, k, v, off, lam)
+    assert torch.equal(got[:, :128], want[:, :128])
+
+
+@pytest.mark.parametrize("by", [2.0 ** -16, 2.0 ** 10])
+def test_float16_beyond_its_range_inside(by):
+    """Gradients of a loss scaled far down or up: what lies between, states among it, passes float16's range."""
+    lengths, off, lam = [300, 70], offsets_of([300, 70]), -torch.tensor([1e-3, 1e-2]).cuda()
+    q, k, v = (randn(i, 1, 370, 2, 32, dtype=torch.float16, by=8.0).requires_grad_() for i in (1, 2, 3))
+    do = (randn(4, 1, 370, 2, 32) * by * 2.0 ** -10).half()
+    o = layers.decay_attention(q, k, v, off, lam, scale=2.0 ** -9)
+    got = (o, *torch.autograd.grad(o, [q, k, v], do))
+    ref, size = decay_reference(q, k, v, lengths, 0, lam, 2.0 ** -9, do=do)
+    for t, r, z, name in zip(got, ref, size, ("o", "dq", "dk", "dv")):
+        close(t, r, z, name, 2.0 ** -14, 2.0 ** -25)
+    x = randn(6, 1, 370, 64, dtype=torch.float16).requires_grad_()
+    w = randn(7, 2, 2, 48, 64, dtype=torch.float16, by=0.3).requires_grad_()
+    dy = (randn(8, 1, 370, 48) * by * 2.0 ** -4).half()
+    y = layers.band_gated(x, w, off)
+    got = torch.autograd.grad(y, [x, w], dy)
+    ref, size = gated_reference(x, w, None, lengths, 0, "silu", dy)
+    for t, r, z, name in zip(got, ref[1:], size[1:], ("dx", "dw")):
+        close(t, r, z, name, 2.0 ** -14, 2.0 ** -25)
+
+
+@pytest.mark.parametrize("bands,batch", [(5000, 2), (3000, 1)])
+def test_thousands_of_bands(bands, batch):
+    g = torch.Generator().manual_seed(bands)
+    lengths = torch.randint(0, 4, (bands,), generator=g).tolist()
+    rows, off = sum(lengths), offsets_of(lengths)
+    q, k, v = (randn(i, batch, rows, 2, 8, dtype=torch.bfloat16) for i in (1, 2, 3))
+    lam = decays_of(2)
+    state = randn(4, batch * bands, 2, 8, 8)
+    ref, size = [], []
+    band = torch.arange(bands, device="cuda").repeat_interleave(torch.tensor(lengths, device="cuda"))
+    i = torch.arange(rows, device="cuda") - off[band]
+    # at most three tokens a band: shifted by one and two rows
+    qd, kd, vd, sd = (t.double() for t in (q, k, v, state.view(batch, bands, 2, 8, 8)))
+    want = torch.matmul(qd[:, :, :, None], sd[:, band])[:, :, :, 0] * (lam.double() * (i[:, None] + 1)).exp()[:, :, None]
+    for lag in range(3):
+        ok = (i >= lag)[None, :, None, None]
+        p = (qd * kd.roll(lag, 1)).sum(-1, keepdim=True) * (lam.double() * lag).exp()[:, None]
+        want = want + torch.where(ok, p * vd.roll(lag, 1), 0.0)
+    o = layers.decay_attention(q, k, v, off, lam, 1.0, state=state)
+    close(o, want, want.abs() + 60.0, "o", 2.0 ** -14, 1e-37)
+    x = randn(5, batch, rows, 24).requires_grad_()
+    w, b = randn(6, bands, 24).requires_grad_(), randn(7, bands, 24).requires_grad_()
+    dy = randn(8, batch, rows, 24)
+    got = layers.band_norm(x, off, w, b, 3, "silu")
+    grads = torch.autograd.grad(got, [x, w, b], dy)
+    ends = off.tolist()
+    pick = [n for n in range(0, bands, 97) if lengths[n]]
+    for n in pick:
+        s = slice(ends[n], ends[n + 1])
+        r, z = norm_reference(x[:, s], [lengths[n]], 0, w[n:n + 1], b[n:n + 1], 3, "silu", 1e-5, dy[:, s])
+        for t, e, y, name in zip((got[:, s], grads[0][:, s], grads[1][n:n + 1], grads[2][n:n + 1]), r, z, ("y", "dx", "dw", "db")):
+            close(t, e, y, name, 2.0 ** -20, 1e-37)
+    assert not grads[1][torch.tensor(lengths) == 0].any()
+
+
+def test_tokens_normalised_each_by_itself():
+    x = randn(1, 700, 1, 96, dtype=torch.bfloat16).requires_grad_()
+    w = randn(2, 1, 96, dtype=torch.bfloat16).requires_grad_()
+    off, dy = torch.tensor([0, 1], device="cuda"), randn(3, 700, 1, 96, dtype=torch.bfloat16)
+    y = layers.band_norm(x, off, w, groups=4, activation="gelu")
+    got = [y, *torch.autograd.grad(y, [x, w], dy)]
+    ref, size = norm_reference(x, [1], 0, w, None, 4, "gelu", 1e-5, dy)
+    for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw")):
+        close(t, r, z, name, 2.0 ** -20, 1e-37)
+
+
+def test_lone_and_broadcast_inputs():
+    """Axes of one element with any stride; expanded inputs, whose gradients autograd adds up."""
+    lam = decays_of(1)
+    off = offsets_of([40])
+    q = randn(1, 1, 40, 1, 16).requires_grad_()
+    k = randn(2, 1, 1, 1, 16).requires_grad_()     # one token for all
+    v = randn(3, 1, 40, 1, 16).as_strided((1, 40, 1, 16), (999, 16, 7, 1)).detach().requires_grad_()
+    do = randn(4, 1, 1, 1, 16).expand(1, 40, 1, 16)
+    o = layers.decay_attention(q, k.expand(1, 40, 1, 16), v, off, lam)
+    got = torch.autograd.grad(o, [q, k, v], do)
+    ref, size = decay_reference(q, k.expand(1, 40, 1, 16), v, [40], 0, lam, 0.25, do=do)
+    close(o, ref[0], size[0], "o", 2.0 ** -20)
+    close(got[0], ref[1], size[1], "dq", 2.0 ** -20)
+    close(got[1], ref[2].sum(1, True), size[2].sum(1, True), "dk", 2.0 ** -18)
+    x = randn(5, 1, 1, 24).requires_grad_()
+    w = randn(6, 1, 2, 8, 24).requires_grad_()
+    dy = randn(7, 1, 40, 8)
+    y = layers.band_gated(x.expand(1, 40, 24), w, off)
+    got = torch.autograd.grad(y, [x, w], dy)
+    ref, size = gated_reference(x.expand(1, 40, 24), w, None, [40], 0, "silu", dy)
+    close(got[0], ref[1].sum(1, True), size[1].sum(1, True), "dx", 2.0 ** -18)
+    close(got[1], ref[2], size[2], "dw", 2.0 ** -20)
+    y = layers.band_norm(x.expand(1, 40, 24), off, groups=2)
+    assert torch.isfinite(y).all()
+
+
+def test_gradients_against_differences():
+    """Central differences of a loss through all three in 32 bits: truncation is of the order of h^2 = 1e-4,
+    cancellation 2^-24 / h = 6e-6 of the loss' terms."""
+    off, lam, h = offsets_of([90, 40]), decays_of(2, 3), 1e-2
+    x, w, b = randn(1, 1, 130, 32).requires_grad_(), randn(2, 2, 32).requires_grad_(), randn(3, 2, 32).requires_grad_()
+    k, v = (randn(i, 1, 130, 2, 16, by=0.3).requires_grad_() for i in (4, 5))
+    wg = randn(6, 2, 2, 24, 32, by=0.2).requires_grad_()
+    do = randn(7, 1, 130, 24)
+
+    def loss(x, w, b, k, v, wg):
+        q = layers.band_norm(x, off, w, b, 4, "silu").unflatten(2, (2, 16))
+        o = layers.decay_attention(q, k, v, off, lam).flatten(2)
+        return (layers.band_gated(o, wg, off, activation="gelu").double() * do.double()).sum()
+
+    args = [x, w, b, k, v, wg]
+    grads = torch.autograd.grad(loss(*args), args)
+    for n, (t, g) in enumerate(zip(args, grads)):
+        u = randn(20 + n, *t.shape)
+        u /= u.norm() / t.numel() ** 0.25
+        with torch.no_grad():
+            hi, lo = (loss(*[a + s * h * u if m == n else a for m, a in enumerate(args)]) for s in (1, -1))
+        want, have = ((hi - lo) / (2 * h)).item(), (g.double() * u.double()).sum().item()
+        assert abs(have - want) <= 5e-3 * (g.norm() * u.norm()).item() / t.numel() ** 0.5 * 8 + 2e-3 * abs(want), n
+
+
+# ------------------------------------------------------------ a block of them
+
+
+class Block(torch.nn.Module):
+    """norm -> decayed attention -> norm -> gated product -> projection, with both residuals; each token is
+    normalised by itself, so that one token at a time gives what whole bands do."""
+
+    def __init__(self, bands, width, heads, kv_heads, dim, hidden, dtype=torch.float32):
+        super().__init__()
+        self.split, self.dim = [heads, kv_heads, kv_heads], dim
+        self.log_decay = -torch.logspace(-1, -3, kv_heads).cuda()
+        self.norm = torch.nn.ParameterList([randn(n, 1, width, dtype=dtype, by=0.2) + 1 for n in (1, 2)])
+        self.qkv = layers.BandLinear(bands, width, sum(self.split) * dim, dtype=dtype)
+        self.out = layers.BandLinear(bands, heads * dim, width, dtype=dtype)
+        self.gated = layers.BandGated(bands, width, hidden, dtype=dtype)
+        self.down = layers.BandLinear(bands, hidden, width, dtype=dtype)
+
+    def forward(self, x, off, mix):
+        one = torch.tensor([0, 1], device="cuda")
+        token = lambda x, w: layers.band_norm(x.reshape(-1, 1, x.shape[2]), one, w, groups=2).view(x.shape)  # noqa: E731
+        q, k, v = self.qkv(token(x, self.norm[0]), off).unflatten(-1, (-1, self.dim)).split(self.split, 2)
+        x = x + self.out(mix(q, k, v).flatten(2), off)
+        return x + self.down(self.gated(token(x, self.norm[1]), off), off)
+
+    def plain(self, x, lengths):
+        """The same in 64 bits, of elementary operations that autograd knows."""
+        band = torch.arange(len(lengths), device="cuda").repeat_interleave(torch.tensor(lengths, device="cuda"))
+
+        def token(x, w):
+            t = x.unflatten(2, (2, -1))
+            t = (t - t.mean(3, True)) / (t.var(3, correction=0, keepdim=True) + 1e-5).sqrt()
+            return t.flatten(2) * w.double()
+
+        def linear(x, m):
+            return (m.weight.double()[band] * x[:, :, None]).sum(3) + m.bias.double()[band]
+
+        q, k, v = linear(token(x, self.norm[0]), self.qkv).unflatten(-1, (-1, self.dim)).split(self.split, 2)
+        k, v = (t.repeat_interleave(q.shape[2] // k.shape[2], 2) for t in (k, v))
+        lam = self.log_decay.double().repeat_interleave(q.shape[2] // self.split[1])
+        i = torch.arange(len(band), device="cuda")
+        lag = i[:, None] - i
+        see = (lag >= 0) & (band[:, None] == band)
+        fade = torch.where(see, (lam[:, None, None] * lag.clamp(min=0)).exp(), 0.0) * self.dim ** -0.5
+        p = torch.matmul(q.transpose(1, 2), k.permute(0, 2, 3, 1).contiguous()) * fade
+        x = x + linear(torch.matmul(p, v.transpose(1, 2)).transpose(1, 2).flatten(2), self.out)
+        t = token(x, self.norm[1])[:, :, None, None]
+        a = (self.gated.weight.double()[band] * t).sum(4) + self.gated.bias.double()[band]
+        return x + linear(a[:, :, 0] * torch.sigmoid(a[:, :, 0]) * a[:, :, 1], self.down)
+
+
+def test_block_trains_and_streams():
+    """All of them as they are used together. Each of the nine operators is off by 2^-20 of its terms, which are at
+    most some 2^3 times what they add up to: 2^-13 of the 2-norm for all."""
+    torch.manual_seed(0)
+    lengths, width = [70, 3, 0, 41], 48
+    off = offsets_of(lengths)
+    block = Block(4, width, 4, 2, 16, 80)
+    x = randn(11, 2, 114, width).requires_grad_()
+    dy = randn(12, 2, 114, width)
+    y = block(x, off, lambda q, k, v: layers.decay_attention(q, k, v, off, block.log_decay))
+    params = [x, *block.parameters()]
+    want = block.plain(x.double(), lengths)
+    for a, b, p in zip((y, *torch.autograd.grad(y, params, dy)), (want, *torch.autograd.grad(want, params, dy.double())), [y] + params):
+        # (bands without tokens, and a shift that the next norm takes out, have no gradient)
+        assert ((a.double() - b.double()).norm() <= 2.0 ** -13 * b.double().norm() + 2.0 ** -16).item(), p.shape
+    # the first tokens of each band at once, then one token of every band at a time
+    with torch.no_grad():
+        streams = layers.DecayState(8, 2, 16)
+        cut, each = [40, 1, 0, 5], torch.arange(5, device="cuda")
+        at = torch.cat([torch.arange(a, a + n) for a, n in zip(off.tolist(), cut)]).cuda()
+        first = offsets_of(cut)
+        got = block(x[:, at], first, lambda q, k, v: streams.read(q, k, v, first, block.log_decay))
+        assert ((got - y[:, at]).norm() <= 2.0 ** -13 * y.norm()).item()
+        streams.pos.view(2, 4)[:, 2] = -1          # (a band without tokens)
+        for t in range(40):
+            pos = torch.tensor([c + t for c in cut], device="cuda")
+            here = (pos < torch.tensor(lengths, device="cuda")) & (pos >= 0)
+            streams.pos.copy_(torch.where(here, pos, -1).repeat(2))
+            rows = torch.where(here, off[:-1] + pos, 0)
+            if not here.any():
+                break
+            step = block(x[:, rows], each, lambda q, k, v: streams.step(
+                q.flatten(0, 1), k.flatten(0, 1), v.flatten(0, 1), block.log_decay).view(q.shape))
+            assert ((step - y[:, rows])[:, here].norm() <= 2.0 ** -13 * y[:, rows][:, here].norm()).item(), t
+
+
+def test_results_do_not_vary():
+    lengths = [1000, 70, 300, 2500]
+    off, rows, lam = offsets_of(lengths), 3870, decays_of(2)
+    q, k, v, do = (randn(i, 2, rows, n, 64, dtype=torch.bfloat16).requires_grad_(i < 4) for i, n in ((1, 4), (2, 2), (3, 2), (4, 4)))
+    x = randn(5, 2, rows, 64, dtype=torch.bfloat16).requires_grad_()
+    w = randn(6, 4, 2, 72, 64, dtype=torch.bfloat16).requires_grad_()
+    nw = randn(7, 4, 64, dtype=torch.bfloat16).requires_grad_()
+
+    def once():
+        o = layers.decay_attention(q, k, v, off, lam)
+        y, z = layers.band_gated(x, w, off), layers.band_norm(x, off, nw, groups=4, activation="silu")
+        return [o, y, z, *torch.autograd.grad(o, [q, k, v], do), *torch.autograd.grad(y, [x, w], torch.ones_like(y)),
+                *torch.autograd.grad(z, [x, nw], torch.ones_like(z))]
+
+    first = once()
+    for _ in range(3):
+        for a, b in zip(first, once()):
+            assert torch.equal(a, b)
+
+
+def test_in_graphs_and_on_another_stream():
+    """Two captured graphs that share a memory pool, the gradients in one of them, replayed among eager calls."""
+    lengths = [900, 33]
+    off, lam = offsets_of(lengths), decays_of(2)
+    x, w, nw = randn(1, 2, 933, 64), randn(2, 2, 2, 64, 64, by=0.2), randn(3, 2, 64)
+    state0 = randn(4, 4, 2, 16, 16)
+    state = state0.clone()
+    one = [randn(i, 4, n, 16) for i, n in ((5, 4), (6, 2), (7, 2))]
+    pos, out = torch.ones(4, dtype=torch.int64, device="cuda"), torch.empty(4, 4, 16, device="cuda")
+
+    def train(x):
+        x = x.detach().requires_grad_()
+        y = layers.band_norm(x, off, nw, groups=4, activation="silu")
+        q, k, v = layers.band_gated(y, w, off).unflatten(2, (4, 16)).split([2, 1, 1], 2)
+        o = layers.decay_attention(q, k, v, off, lam[:1])
+        return [o, *torch.autograd.grad(o.square().sum(), [x])]
+
+    def serve():
+        layers.decay_step(*one, state, pos, lam, out=out)
+
+    want = [t.clone() for t in train(x)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for a, b in zip(train(x), want):
+            assert torch.equal(a, b)
+        serve()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graphs, pool = [torch.cuda.CUDAGraph() for _ in range(2)], torch.cuda.graph_pool_handle()
+    fixed = x.clone()
+    with torch.cuda.graph(graphs[0], pool=pool):
+        held = train(fixed)
+    with torch.cuda.graph(graphs[1], pool=pool):
+        serve()
+    for turn in range(3):
+        now = randn(50 + turn, *x.shape)
+        fixed.copy_(now)
+        state.copy_(state0)
+        graphs[0].replay()
+        got = [t.clone() for t in held]
+        graphs[1].replay()
+        stepped, row = state.clone(), out.clone()
+        torch.cuda.synchronize()
+        for a, b in zip(got, train(now)):
+            assert torch.equal(a, b), turn
+        state.copy_(state0)
+        serve()
+        assert torch.equal(state, stepped) and torch.equal(out, row)
+
+
+def test_writes_to_states_are_seen_by_autograd():
+    q, k, v = (randn(i, 2, 2, 8) for i in (1, 2, 3))
+    state, pos, lam = randn(4, 2, 2, 8, 8), torch.ones(2, dtype=torch.int64, device="cuda"), decays_of(2)
+    w = torch.ones_like(state, requires_grad=True)
+    y = (state * w).sum()
+    with torch.no_grad():
+        layers.decay_step(q, k, v, state, pos, lam)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    y = (state * w).sum()
+    with torch.no_grad():
+        layers.decay_attention(q[None], k[None], v[None], torch.tensor([0, 2], device="cuda"), lam, state=state[:1])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_refusals():
+    off, lam = offsets_of([10]), decays_of(2)
+    q, k, v = randn(1, 1, 10, 4, 8), randn(2, 1, 10, 2, 8), randn(3, 1, 10, 2, 8)
+    state = torch.zeros(1, 2, 8, 8, device="cuda")
+    bad = pytest.raises(ValueError)
+    with bad:
+        layers.decay_attention(q, k, v, off, lam.double())
+    with bad:
+        layers.decay_attention(q, k, v, off, lam[:1])
+    with bad:
+        layers.decay_attention(q, k, v, off, lam.clone().requires_grad_())
+    with bad:
+        layers.decay_attention(q, k, v, off, lam, state=state.half())
+    with bad:
+        layers.decay_attention(q, k, v, off, lam, state=state[:, :, :4])
+    with bad:
+        layers.decay_attention(q.clone().requires_grad_(), k, v, off, lam, state=state)
+    with bad:
+        layers.decay_attention(q, k, v, off, lam, state=state.clone().requires_grad_())
+    with bad:
+        layers.decay_attention(q, k, v[:, :9], off, lam)
+    with bad:
+        layers.decay_attention(q, k, v, off.int(), lam)
+    with bad:
+        layers.decay_attention(q, k, v, off, lam, keep=torch.ones(1, 10, device="cuda"))
+    with bad:
+        layers.decay_attention(q[0], k, v, off, lam)
+    with bad:
+        layers.decay_attention(q.cpu(), k, v, off, lam)
+    with pytest.raises(nc.NsgcqtError):
+        layers.decay_attention(randn(1, 1, 10, 3, 8), k, v, off, lam)
+    with pytest.raises(nc.NsgcqtError):
+        layers.decay_attention(q, k, v, off, lam, scale=float("inf"))
+    with pytest.raises(nc.NsgcqtError):
+        layers.decay_attention(*(randn(1, 1, 10, 2, 129) for _ in range(3)), off, lam)
+    with pytest.raises(NotImplementedError):
+        with torch.autograd.forward_ad.dual_level():
+            layers.decay_attention(torch.autograd.forward_ad.make_dual(q, q), k, v, off, lam)
+    pos = torch.zeros(1, dtype=torch.int64, device="cuda")
+    one = q[0, :1], k[0, :1], v[0, :1]
+    layers.decay_step(*one, state, pos, lam)
+    with bad:
+        layers.decay_step(*one, state, pos.int(), lam)
+    with bad:
+        layers.decay_step(*one, state[:, :1], pos, lam)
+    with bad:
+        layers.decay_step(one[0].clone().requires_grad_(), *one[1:], state, pos, lam)
+    with bad:
+        layers.decay_step(*one, state, pos, lam, out=torch.empty(1, 4, 8, device="cuda").half())
+    x = randn(4, 1, 10, 12)
+    for call in (lambda: layers.band_norm(x, off, groups=5), lambda: layers.band_norm(x, off, groups=0),
+                 lambda: layers.band_norm(x, off, eps=0.0), lambda: layers.band_norm(x, off, eps=float("nan")),
+                 lambda: layers.band_norm(randn(5, 1, 10, 4104), off)):
+        with pytest.raises(nc.NsgcqtError):
+            call()
+    with bad:
+        layers.band_norm(x, off, activation="relu")
+    with bad:
+        layers.band_norm(x, off, torch.ones(2, 12, device="cuda"))
+    with bad:
+        layers.band_norm(x, off, torch.ones(1, 12, device="cuda").half())
+    with bad:
+        layers.band_norm(x.transpose(1, 2), off)
+    w = randn(6, 1, 2, 8, 12)
+    with bad:
+        layers.band_gated(x, w[:, 0], off)
+    with bad:
+        layers.band_gated(x, w[..., :6], off)
+    with bad:
+        layers.band_gated(x, w.transpose(2, 3).contiguous().transpose(2, 3), off)
+    with bad:
+        layers.band_gated(x, w, off, torch.zeros(1, 8, device="cuda"))
+    with bad:
+        layers.band_gated(x, w, off, activation="tanh")
+    for f in (lambda t: layers.band_norm(t, off), lambda t: layers.band_gated(t, w, off)):
+        with pytest.raises(NotImplementedError):
+            with torch.autograd.forward_ad.dual_level():
+                f(torch.autograd.forward_ad.make_dual(x, x))
+
+
+def test_empty_calls():
+    off, none = offsets_of([0]), torch.zeros(1, dtype=torch.int64, device="cuda")
+    for batch, rows, o in ((0, 5, offsets_of([5])), (2, 0, off), (2, 4, none)):
+        G = o.numel() - 1
+        q = randn(1, batch, rows, 2, 8).requires_grad_()
+        y = layers.decay_attention(q, q, q, o, decays_of(2))
+        assert y.shape == q.shape and not y.any()
+        assert not torch.autograd.grad(y, [q], torch.ones_like(y))[0].any()
+        x = randn(2, batch, rows, 8).requires_grad_()
+        w = randn(3, G, 2, 4, 8).requires_grad_()
+        y = layers.band_gated(x, w, o)
+        dx, dw = torch.autograd.grad(y, [x, w], torch.ones_like(y))
+        assert y.shape == (batch, rows, 4) and dw.shape == w.shape and not dx.any()
+        if batch == 0 or rows == 0:
+            assert not dw.any()
+        nw = randn(4, G, 8).requires_grad_()
+        y = layers.band_norm(x, o, nw, groups=2)
+        dx, dw = torch.autograd.grad(y, [x, nw], torch.ones_like(y))
+        assert y.shape == x.shape and not dx.any() and not dw.any()
+    assert layers.band_norm(randn(1, 2, 3, 0), offsets_of([3])).shape == (2, 3, 0)
+    layers.decay_step(*(torch.zeros(0, n, 8, device="cuda") for n in (2, 1, 1)), torch.zeros(0, 1, 8, 8, device="cuda"),
+                      torch.zeros(0, dtype=torch.int64, device="cuda"), decays_of(1))
+
+
+@pytest.mark.parametrize("group", [5, 9])
+def test_decay_step_of_large_groups(group):
+    q, k, v = randn(1, 3, 2 * group, 64), randn(2, 3, 2, 64), randn(3, 3, 2, 64)
+    state = randn(4, 3, 2, 64, 64)
+    before, lam = state.double(), decays_of(2)
+    pos = torch.tensor([4, 0, 7], device="cuda")
+    o = layers.decay_step(q, k, v, state, pos, lam)
+    old, new = before * lam.double().exp()[None, :, None, None] * (pos > 0)[:, None, None, None], k.double()[..., None] * v.double()[:, :, None]
+    s, z = old + new, old.abs() + new.abs()
+    want = torch.matmul(q.double().unflatten(1, (2, group)), s).flatten(1, 2) / 8
+    close(o, want, torch.matmul(q.double().abs().unflatten(1, (2, group)), z).flatten(1, 2) / 8, "o", 2.0 ** -20)
+    close(state, s, z, "state", 2.0 ** -20)
+
+
+def test_states_and_steps_of_odd_alignment():
+    """States that begin off a 16-byte boundary take element accesses."""
+    lam = decays_of(2)
+    q, k, v = (randn(i, 1, 300, n, 32) for i, n in ((1, 2), (2, 2), (3, 2)))
+    base = randn(4, 2 * 32 * 32 + 1)
+    state = base[1:].view(1, 2, 32, 32)
+    aligned = state.clone()
+    off = offsets_of([300])
+    assert torch.equal(layers.decay_attention(q, k, v, off, lam, state=state), layers.decay_attention(q, k, v, off, lam, state=aligned))
+    assert torch.equal(state, aligned)
+    pos = torch.tensor([3], device="cuda")
+    a, b = (layers.decay_step(q[:, 0], k[:, 0], v[:, 0], s, pos, lam) for s in (state, aligned))
+    assert ((a - b).abs() <= 2.0 ** -18 * b.abs().max()).all() and torch.equal(state, aligned)
