@@ -38,7 +38,7 @@ int check_state(const float* p) {
 // of less than 8 head_dim tokens only below 1024 workgroups. 131,072 tokens, 8
 // heads of 128, bfloat16: 1024 tokens 445 us, 512 tokens 480, 2048 560.
 int shift_of(int64_t batch, int64_t rows, int64_t heads, int64_t dim, int shift) {
-    while (shift > 6 && product(batch, rows >> shift, heads) < (1 << shift > 8 * dim ? 1536 : 1024)) --shift;
+    while (shift > 6 && product(batch, (rows + (int64_t(1) << shift) - 1) >> shift, heads) < (1 << shift > 8 * dim ? 1536 : 1024)) --shift;
     return shift;
 }
 struct DecayCut { int shift, fine; };
@@ -130,14 +130,22 @@ int run_decay(int dtype, const nsgcqt_rows* r, const DecayArgs& a, DecayArgs sum
     });
 }
 
+// The kernels go by strides from a tile's last token too: a row's stride that
+// was not checked, of rows of one token, is not used.
+View row_view(const nsgcqt_view* v, const DecayArgs& a) {
+    View w = view_of(v);
+    if (a.rows == 1) w.row = a.dim;
+    return w;
+}
+
 DecayJob job_of(const nsgcqt_view* a, const nsgcqt_view* b, const nsgcqt_view* c, const nsgcqt_view* out, float* part,
                 const DecayArgs& args, int64_t heads, bool reverse, bool turned) {
     const int group = static_cast<int>(heads / args.kv_heads);
     DecayJob j{};
-    j.a = view_of(a);
-    j.b = view_of(b);
-    j.c = view_of(c);
-    if (out) j.out = view_of(out);
+    j.a = row_view(a, args);
+    j.b = row_view(b, args);
+    j.c = row_view(c, args);
+    if (out) j.out = row_view(out, args);
     j.part = part;
     j.reverse = reverse;
     j.turned = turned;

@@ -166,7 +166,7 @@ template <class T, int DP, bool WIDE> struct DecayLoad {
     static constexpr unsigned kPast = 0x80000000u;   // past every tile, and less than 2^30 from its end
     const char* base;    // of the first tile's buffer
     int64_t step, head;  // bytes from tile to tile, from head to head
-    unsigned row;        // and from token to token
+    int64_t row;         // and from token to token (wide: below 2^23)
     bool reverse;
     unsigned at[WIDE ? kEach : 1];
     frag<T> f[WIDE ? 1 : 2];
@@ -176,7 +176,7 @@ template <class T, int DP, bool WIDE> struct DecayLoad {
     }
     __device__ DecayLoad(const DecayArgs& a, const View& v, const DecayPlace& p, int first_head, bool rev, int tid) {
         reverse = rev;
-        row = static_cast<unsigned>(v.row) * sizeof(T);
+        row = v.row * static_cast<int64_t>(sizeof(T));
         step = (rev ? -v.row : v.row) * static_cast<int64_t>(kDecayTile * sizeof(T));
         head = v.head * static_cast<int64_t>(sizeof(T));
         base = reinterpret_cast<const char*>(decay_row<T>(v, p.b, p.token(rev ? kDecayTile - 1 : 0, rev), first_head));
@@ -185,7 +185,7 @@ template <class T, int DP, bool WIDE> struct DecayLoad {
             for (int e = 0; e < kEach; ++e) {
                 const int byte = (wave_number() * kEach + e) * 1024 + (tid & 63) * 16, r = byte / RB;
                 const unsigned d = ((byte % RB / 16) ^ turn(r)) * 16;
-                at[e] = d < a.dim * sizeof(T) ? (rev ? kDecayTile - 1 - r : r) * row + d : kPast;
+                at[e] = d < a.dim * sizeof(T) ? (rev ? kDecayTile - 1 - r : r) * static_cast<unsigned>(row) + d : kPast;
             }
         }
     }
@@ -194,7 +194,7 @@ template <class T, int DP, bool WIDE> struct DecayLoad {
         const char* from = base + number * step + g * head;
         if constexpr (WIDE) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass does not know a buffer's type
-            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, kDecayTile * row, 0x00020000);
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, kDecayTile * static_cast<unsigned>(row), 0x00020000);
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 const int load = wave_number() * kEach + e;
@@ -208,7 +208,7 @@ template <class T, int DP, bool WIDE> struct DecayLoad {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r = token_of(e, tid), d = (tid + kThreads * e) % (DP / 8) * 8;
-                const T* p = reinterpret_cast<const T*>(from + static_cast<int64_t>(reverse ? kDecayTile - 1 - r : r) * row);
+                const T* p = reinterpret_cast<const T*>(from + (reverse ? kDecayTile - 1 - r : r) * row);
                 f[e] = load8<T, false>(p + d, kept >> r & 1 ? a.dim - d : 0, d > 0);
             }
         }

@@ -651,6 +651,28 @@ def test_lone_and_broadcast_inputs():
     assert torch.isfinite(y).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_one_token_with_any_stride(dtype):
+    """The stride of an axis of one element may be anything: it is not used, in the gradients either."""
+    base = [randn(i, 3, 1, n, 64, dtype=dtype) for i, n in ((1, 4), (2, 2), (3, 2), (4, 4))]
+    strange = lambda t, s: t.as_strided(t.shape, (t.stride(0), s, *t.stride()[2:]))  # noqa: E731
+    off, lam = torch.tensor([0, 1], device="cuda"), decays_of(2)
+    got = []
+    for s in (64 * 4, 0, 8, 1 << 40):
+        q, k, v, do = (strange(t.clone(), s) for t in base)
+        for t in (q, k, v):
+            t.requires_grad_()
+        o = layers.decay_attention(q, k, v, off, lam)
+        got.append((o, *torch.autograd.grad(o, [q, k, v], do)))
+        for a, b in zip(got[0], got[-1]):
+            assert torch.equal(a, b)
+    x, w = randn(5, 3, 1, 64, dtype=dtype), randn(6, 1, 2, 32, 64, dtype=dtype)
+    for s in (0, 8, 1 << 40):
+        y = x.as_strided(x.shape, (64, s, 1))
+        assert torch.equal(layers.band_norm(y, off, groups=2), layers.band_norm(x, off, groups=2))
+        assert torch.equal(layers.band_gated(y, w, off), layers.band_gated(x, w, off))
+
+
 def test_gradients_against_differences():
     """Central differences of a loss through all three in 32 bits: truncation is of the order of h^2 = 1e-4,
     cancellation 2^-24 / h = 6e-6 of the loss' terms."""
