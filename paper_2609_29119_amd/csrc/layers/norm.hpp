@@ -327,9 +327,12 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
     const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several) return;
     double s[8] = {}, q[8] = {};
+    frag<T> x[N], next[N];
+    p.load<T, N, WIDE>(a, a.x, next);   // (zeros past the end)
     for (int from = 0; from < p.all; from += N * a.together) {
-        frag<T> x[N];
-        p.load<T, N, WIDE>(a, a.x, x, from);   // (zeros past the end)
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = next[k];
+        p.load<T, N, WIDE>(a, a.x, next, from + N * a.together);
 #pragma unroll
         for (int k = 0; k < N; ++k)
 #pragma unroll
