@@ -36,7 +36,9 @@ int check_state(const float* p) {
 // (few of a ragged row's tokens lie in bands of several segments). A part's
 // state costs as much to write, join and read as 4 head_dim of its tokens: parts
 // of less than 8 head_dim tokens only below 1024 workgroups. 131,072 tokens, 8
-// heads of 128, bfloat16: 1024 tokens 445 us, 512 tokens 480, 2048 560.
+// heads of 128, bfloat16, all three kernels: 256 tokens 561 us, 512 497, 1024 500,
+// 2048 574; 446,932 tokens over 221 bands, 8 heads of 64 over 4: 512 tokens 607,
+// 1024 600, 2048 650.
 int shift_of(int64_t batch, int64_t rows, int64_t heads, int64_t dim, int shift) {
     while (shift > 6 && product(batch, (rows + (int64_t(1) << shift) - 1) >> shift, heads) < (1 << shift > 8 * dim ? 1536 : 1024)) --shift;
     return shift;

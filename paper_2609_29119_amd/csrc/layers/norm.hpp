@@ -263,7 +263,8 @@ template <class T, int N, bool WIDE> __device__ inline void norm_out(const NormA
 }
 
 // y of bands of one chunk, and zeros where no band is: the mean first, then the
-// squares of the differences from it.
+// squares of the differences from it. Bound by the chain of loads, sums and
+// barriers of a workgroup: 64 signals of one token of 128 channels 6.6 us.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     constexpr int N = norm_held<T>();
@@ -317,7 +318,9 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     norm_out<T, N, WIDE>(a, p, o, x);
 }
 
-// The sums of x and x^2 of the parts of longer bands.
+// The sums of x and x^2 of the parts of longer bands. 446,932 tokens of 128
+// channels, bfloat16, 221 bands: 28 us (4.1 TB/s); 710,680 of 77, float16: 48, as
+// loads at odd addresses take four accesses of the first cache each.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
     constexpr int N = 4;
@@ -372,7 +375,9 @@ template <bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs
         a.stats[place * a.groups + g] = double2{all.x, 1.0 / sqrt(fmax(all.y - all.x * all.x, 0.0) + a.eps)};
 }
 
-// y of longer bands, a part a workgroup: the next tokens are on their way while these are computed.
+// y of longer bands, a part a workgroup: the next tokens are on their way while
+// these are computed. The same two cases: 37 us, much of x coming from the
+// memory-side cache, and 83.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_apply(NormArgs a) {
     constexpr int N = norm_held<T>() / 2;
@@ -492,7 +497,8 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad(NormArgs a) {
     });
 }
 
-// The sums of d and d xh of the parts of longer bands, and what they add to dw and db.
+// The sums of d and d xh of the parts of longer bands, and what they add to dw
+// and db. 446,932 tokens of 128 channels, bfloat16: 56 us (4.1 TB/s).
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
     constexpr int N = 2;
@@ -532,7 +538,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
     for (int g = tid; g < a.groups; g += a.threads) to[g] = double2{first[g], second[g]};
 }
 
-// dx of longer bands, a part a workgroup.
+// dx of longer bands, a part a workgroup: 60 us (5.7 TB/s with the memory-side cache).
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_apply(NormArgs a) {
     constexpr int N = 2;

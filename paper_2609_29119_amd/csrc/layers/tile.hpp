@@ -367,9 +367,8 @@ __device__ inline unsigned die_order(unsigned id, unsigned n) {
     return (k / kStretch * 8 + die) * kStretch + k % kStretch;
 }
 
-// The same from the row's end: where bands grow along the row, short work comes
-// last and fills the dies evenly (decayed attention of the training case 620 ->
-// 556 us).
+// The same from the row's end: where bands grow along the row, the longest work
+// begins first and the shortest fills the end.
 __device__ inline unsigned last_first(unsigned id, unsigned n) { return n - 1 - die_order(id, n); }
 
 // I: int where a band's mult * len rows stay below 2^30, else int64_t.
