@@ -54,6 +54,10 @@
  *     s = 4, 2 or 1 heads a workgroup, the largest that divides n_heads /
  *     n_kv_heads, for the attention). The step takes a workgroup for each
  *     stream, kv head and 32 query heads of it, and one for each stream and head.
+ *     The decayed attention takes one for each segment (64 to 4,096 tokens)
+ *     of each band of each signal and head, its step for each stream and kv
+ *     head, the norm for each band (and part of a long one) of each signal,
+ *     the gated product for 128 tokens or more of a band and 64 outputs.
  */
 #ifndef NSGCQT_LAYERS_H
 #define NSGCQT_LAYERS_H
