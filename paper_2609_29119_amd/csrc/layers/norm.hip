@@ -25,13 +25,24 @@ int check_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s) {
     return NSGCQT_OK;
 }
 
+void set_threads(NormArgs& a, int threads) {
+    a.octets = (a.channels + 7) / 8;
+    a.threads = a.octets > 256 ? kNormThreads : threads;   // (of four waves three workgroups fit a compute unit, of eight one)
+    a.together = a.threads / a.octets;
+}
+size_t norm_lds(const NormArgs& a) { return sizeof(double) * (8 * a.octets * a.together + 2 * a.groups); }
+
 // Tokens of a chunk: what a workgroup's registers hold, `held` octets a thread
 // (32 KB a workgroup of 256); and of a part, up to 8 chunks, but not so many that
-// fewer than 1024 workgroups are left.
+// fewer than 1024 workgroups are left. A workgroup is one wave where the mean
+// band is at most an eighth of what a wave holds: more bands are then on their
+// way at once. 256 bands of 64 signals, 64 channels in bfloat16, of 8 tokens at the
+// mean: 61 us, and 115 with four waves; with gradients, of 4: 155 and 207. With 16
+// signals and bands twice as long, more of which take parts: 158 and 92.
 void set_chunk(NormArgs& a, int held) {
-    a.octets = (a.channels + 7) / 8;
-    a.threads = a.octets > 256 ? kNormThreads : 256;   // (of four waves three workgroups fit a compute unit, of eight one)
-    a.together = a.threads / a.octets;
+    set_threads(a, 256);
+    const int64_t wave = a.octets <= 64 ? 64 / a.octets * held : 0;   // tokens
+    if (8 * static_cast<int64_t>(a.rows) <= wave * a.n_bands) set_threads(a, 64);
     a.shift = 0;
     while ((2 << a.shift) <= a.together * held) ++a.shift;
     a.part_shift = a.shift + 3;
@@ -147,7 +158,7 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
     CHECK_TRY(check_grid(product(r->batch, static_cast<int64_t>(a.parts))));
     const dim3 grid(static_cast<unsigned>(blocks)), parts(static_cast<unsigned>(r->batch * a.parts)), block(a.threads);
-    const size_t lds = sizeof(double) * 8 * a.octets * a.together;
+    const size_t lds = norm_lds(a);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
         using T = decltype(t);
@@ -200,7 +211,7 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     if (weights && !by_chunk) CHECK_TRY(check_grid(items));
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
     const dim3 block(a.threads);
-    const size_t lds = sizeof(double) * 8 * a.octets * a.together;
+    const size_t lds = norm_lds(a);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
         using T = decltype(t);
@@ -218,8 +229,10 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
         }
         if (weights) {
             a.sums = sums;
-            if (rows && !by_chunk)
-                LAUNCH_TRY((k_norm_weight<T, kWide>), dim3(static_cast<unsigned>(items)), block, lds, st, a);
+            if (rows && !by_chunk) {
+                set_threads(a, 256);
+                LAUNCH_TRY((k_norm_weight<T, kWide>), dim3(static_cast<unsigned>(items)), dim3(a.threads), norm_lds(a), st, a);
+            }
             CHECK_TRY(launch_all(k_norm_weight_join<T>, a, r->n_bands * s->channels, st, by_chunk));
         }
         return NSGCQT_OK;

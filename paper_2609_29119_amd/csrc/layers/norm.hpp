@@ -269,7 +269,7 @@ template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     constexpr int N = norm_held<T>();
     extern __shared__ __align__(16) double norm_lds[];
-    __shared__ double mean[kNormGroups], squares[kNormGroups];
+    double *const mean = norm_lds + 8 * a.octets * a.together, *const squares = mean + a.groups;   // [groups]
     const int tid = threadIdx.x;
     const NormPlace p(a);
     if (!p.t.live) return;
@@ -325,7 +325,7 @@ template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
     constexpr int N = 4;
     extern __shared__ __align__(16) double norm_lds[];
-    __shared__ double sum[kNormGroups], squares[kNormGroups];
+    double *const sum = norm_lds + 8 * a.octets * a.together, *const squares = sum + a.groups;   // [groups]
     const int tid = threadIdx.x;
     const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several) return;
@@ -463,7 +463,7 @@ template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad(NormArgs a) {
     constexpr int N = norm_held<T>() / 2;
     extern __shared__ __align__(16) double norm_lds[];
-    __shared__ double first[kNormGroups], second[kNormGroups];
+    double *const first = norm_lds + 8 * a.octets * a.together, *const second = first + a.groups;   // [groups]
     const int tid = threadIdx.x;
     const NormPlace p(a);
     if (!p.t.live) return;
@@ -503,7 +503,7 @@ template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
     constexpr int N = 2;
     extern __shared__ __align__(16) double norm_lds[];
-    __shared__ double first[kNormGroups], second[kNormGroups];
+    double *const first = norm_lds + 8 * a.octets * a.together, *const second = first + a.groups;   // [groups]
     const int tid = threadIdx.x;
     const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several) return;

@@ -322,6 +322,23 @@ def test_band_norm_strides_uncovered_tokens_and_shared_weights(act, dtype):
             assert t[:, :first].abs().max() == 0 and t[:, first + 1167:].abs().max() == 0
 
 
+# Many short bands are a wave each; a long one among them passes what a wave holds.
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels, groups, bands, longest", [(3, 1, 700, 900), (64, 8, 800, 150), (121, 11, 700, 70), (512, 1, 900, 30)])
+def test_band_norm_many_short_bands_and_a_long_one(channels, groups, bands, longest, dtype):
+    lengths = [(1, 2, 0, 1)[n % 4] if channels < 512 else int(n % 9 == 0) for n in range(bands)]
+    lengths[bands // 3] = longest
+    rows = sum(lengths)
+    x = (randn(3, 3, rows, channels) + 2 * randn(4, channels)).to(dtype).requires_grad_()
+    w, b = ((randn(n, bands, channels, by=0.4) + 1).to(dtype).requires_grad_() for n in (5, 6))
+    dy = randn(7, 3, rows, channels, dtype=dtype)
+    y = layers.band_norm(x, offsets_of(lengths), w, b, groups, "silu", 1e-3)
+    got = [y, *torch.autograd.grad(y, (x, w, b), dy)]
+    ref, size = norm_reference(x, lengths, 0, w, b, groups, "silu", 1e-3, dy)
+    for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
+        close(t, r, z, name, 2.0 ** -20, 2.0 ** -25)
+
+
 def test_band_norm_far_from_zero():
     """A mean of 10^4 standard deviations: the statistics are differences from the mean, not of squares."""
     for n in (40, 5000):
