@@ -166,7 +166,7 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
         LAUNCH_TRY((k_norm<T, kWide>), grid, block, lds, st, a);
         if (space.part) {
             LAUNCH_TRY((k_norm_sum<T, kWide>), parts, block, lds, st, a);
-            CHECK_TRY(launch_all(k_norm_join<false>, a, groups, st));
+            CHECK_TRY(launch_all((k_norm_join<T, false>), a, groups, st));
             LAUNCH_TRY((k_norm_apply<T, kWide>), parts, block, 0, st, a);
         }
         return NSGCQT_OK;
@@ -222,7 +222,7 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
             if (space.part) {
                 LAUNCH_TRY((k_norm_grad_sum<T, kWide>), dim3(static_cast<unsigned>(parts)), block, lds, st, a);
                 if (dx) {
-                    CHECK_TRY(launch_all(k_norm_join<true>, a, groups, st));
+                    CHECK_TRY(launch_all((k_norm_join<T, true>), a, groups, st));
                     LAUNCH_TRY((k_norm_grad_apply<T, kWide>), dim3(static_cast<unsigned>(parts)), block, 0, st, a);
                 }
             }

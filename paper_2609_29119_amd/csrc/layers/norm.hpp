@@ -9,9 +9,9 @@
 // channels of every n-th token. What a chunk holds stays in registers from the
 // load to the store: bands of one chunk are read once. Longer bands are read
 // twice: first in parts of several chunks for their sums, which a small kernel
-// joins, then chunk by chunk. Statistics are summed in 64 bits, where the square
-// of a mean of 10^6 deviations does not hide the variance; d's sums are those
-// that db and dw are made of, times w.
+// joins, then chunk by chunk. Statistics are summed in 64 bits, of differences
+// from a value of the group itself, so that a level far above them does not hide
+// the variance; d's sums are those that db and dw are made of, times w.
 #pragma once
 #include "act.hpp"
 
@@ -27,7 +27,7 @@ struct NormArgs {
     int64_t w_band, b_band;       // their strides from band to band
     void *dw, *db;
     double2* stats;               // [batch][n_bands][groups]: mean, rstd
-    double2* part;                // [batch][parts][groups]: a part's (sum x, sum x^2) or (sum d, sum d xh)
+    double2* part;                // [batch][parts][groups]: a part's (sum v, sum v^2), v = x - norm_pivot, or (sum d, sum d xh)
     float* sums;                  // dw and db before they are joined, [2][channels] each (NULL: not wanted):
                                   // [batch][n_bands] of bands of one chunk, then [batch][parts]; or of k_norm_weight's items
     const int64_t* off;
@@ -318,7 +318,12 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     norm_out<T, N, WIDE>(a, p, o, x);
 }
 
-// The sums of x and x^2 of the parts of longer bands. 446,932 tokens of 128
+// What a group's values of a longer band are summed as differences from: its first one.
+template <class T> __device__ inline double norm_pivot(const NormArgs& a, int64_t b, int start, int group) {
+    return static_cast<double>(static_cast<float>(norm_row<const T>(a.x, b, start)[group * a.cg]));
+}
+
+// The sums of v and v^2, v = x - norm_pivot, of the parts of longer bands. 446,932 tokens of 128
 // channels, bfloat16, 221 bands: 28 us (4.1 TB/s); 710,680 of 77, float16: 48, as
 // loads at odd addresses take four accesses of the first cache each.
 template <class T, bool WIDE>
@@ -329,21 +334,27 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
     const int tid = threadIdx.x;
     const NormPlace p(a, a.parts, a.part_shift);
     if (!p.t.live || p.outside || !p.several) return;
-    double s[8] = {}, q[8] = {};
+    double s[8] = {}, q[8] = {}, pivot[8];
     frag<T> x[N], next[N];
-    p.load<T, N, WIDE>(a, a.x, next);   // (zeros past the end)
+    p.load<T, N, WIDE>(a, a.x, next);
+    const NormOctet<T> o(a, p.col);
+    each<8>([&](auto i) __attribute__((always_inline)) {
+        pivot[i.value] = i.value && a.octet_groups ? pivot[0] : norm_pivot<T>(a, p.b, p.t.start, o.group[i.value]);
+    });
     for (int from = 0; from < p.all; from += N * a.together) {
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] = next[k];
         p.load<T, N, WIDE>(a, a.x, next, from + N * a.together);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
+        for (int k = 0; k < N; ++k) {
+            if (from + p.tr + a.together * k >= p.n) break;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double v = static_cast<float>(x[k][i]);
+                const double v = static_cast<double>(static_cast<float>(x[k][i])) - pivot[i];
                 s[i] += v;
                 q[i] = fma(v, v, q[i]);
             }
+        }
     }
     auto cell = [&](int at, int) { return norm_lds[at]; };
     norm_columns(a, norm_lds, p.works(a), p.tr, p.col, s, tid);
@@ -356,7 +367,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
 
 // Joins the parts of longer bands, in order, a group a thread: into their
 // statistics, or (GRAD) their means of d and d xh into the first part's place.
-template <bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs a) {
+template <class T, bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs a) {
     const int64_t id = (a.first_block + blockIdx.x) * 256 + threadIdx.x, place = id / a.groups;
     const int g = static_cast<int>(id % a.groups), band = static_cast<int>(place % a.n_bands);
     const int64_t b = place / a.n_bands;
@@ -372,7 +383,7 @@ template <bool GRAD> __global__ __launch_bounds__(256) void k_norm_join(NormArgs
     if (GRAD)
         part[0] = all;
     else
-        a.stats[place * a.groups + g] = double2{all.x, 1.0 / sqrt(fmax(all.y - all.x * all.x, 0.0) + a.eps)};
+        a.stats[place * a.groups + g] = double2{norm_pivot<T>(a, b, start, g) + all.x, 1.0 / sqrt(fmax(all.y - all.x * all.x, 0.0) + a.eps)};
 }
 
 // y of longer bands, a part a workgroup: the next tokens are on their way while

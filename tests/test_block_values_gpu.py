@@ -1,0 +1,72 @@
+"""GPU tests of the streaming block's layers at values and sizes where their arithmetic can go wrong: groups of equal
+values, levels far above the differences, infinite and extreme arguments, very long sums, very many signals.
+
+Bounds, beside test_block_gpu's: what a norm makes of a value is off by 2^-20 of the normalised value and of 1 (the
+level's own rest, 2^-24 of a level of 10^6 deviations), however high the level is.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2609_29119_amd as nc  # noqa: E402
+from paper_2609_29119_amd import layers  # noqa: E402
+from test_block_gpu import act_reference, close, offsets_of, randn  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    nc.lib()
+
+
+def norm_of(x, lengths, w, b, groups, act, eps, dy):
+    """(y, dx, dw, db) in 64 bits, and the sizes of their terms: those of the normalised values, not of the level."""
+    x, dy, w, b = (t.detach().double() for t in (x, dy, w, b))
+    ref = [torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(w), torch.zeros_like(w)]
+    size = [torch.zeros_like(t) for t in ref]
+    at = 0
+    for g, n in enumerate(lengths):
+        s = slice(at, at + n)
+        at += n
+        split = lambda t: t.reshape(*t.shape[:-1], groups, -1)  # noqa: E731
+        mean2 = lambda v: v.mean((1, 3), keepdim=True)  # noqa: E731
+        t = split(x[:, s])
+        t = t - mean2(t)
+        t = t - mean2(t)                       # (what the level's own rounding left)
+        r = (mean2(t * t) + eps) ** -0.5
+        hat = t * r
+        hat_size = hat.abs() + 2.0
+        wg, bg = split(w[g]), split(b[g])
+        z, z_size = wg * hat + bg, wg.abs() * hat_size + bg.abs()
+        y, slope = act_reference(z, act)
+        ref[0][:, s], size[0][:, s] = y.flatten(2), (y.abs() + (slope.abs() + 0.4) * z_size).flatten(2)
+        d0 = split(dy[:, s])
+        dz, dz_size = d0 * slope, d0.abs() * (slope.abs() + z_size)
+        d, d_size = dz * wg, dz_size * wg.abs()
+        ref[1][:, s] = (r * (d - mean2(d) - hat * mean2(d * hat))).flatten(2)
+        size[1][:, s] = (r * (d_size + mean2(d_size) + hat_size * mean2(d_size * hat_size))).flatten(2)
+        ref[2][g], size[2][g] = (dz * hat).sum((0, 1)).flatten(), (dz_size * hat_size).sum((0, 1)).flatten()
+        ref[3][g], size[3][g] = dz.sum((0, 1)).flatten(), dz_size.sum((0, 1)).flatten()
+    return ref, size
+
+
+def norm_and_gradients(x, lengths, w, b, groups, act, eps, dy):
+    x, w, b = (t.detach().requires_grad_() for t in (x, w, b))
+    y = layers.band_norm(x, offsets_of(lengths), w, b, groups, act, eps)
+    return [y.detach(), *torch.autograd.grad(y, (x, w, b), dy)]
+
+
+# ----------------------------------------------------------------------------------------------- levels far from zero
+
+
+@pytest.mark.parametrize("tokens", [40, 5000])
+def test_band_norm_of_a_level_of_a_million_deviations(tokens):
+    """In 32 bits: squares of the values themselves would leave 2^-53 of 10^12 deviations."""
+    x, dy = 1e6 + randn(1, 2, tokens, 16), randn(2, 2, tokens, 16)
+    w, b = randn(3, 1, 16), randn(4, 1, 16)
+    got = norm_and_gradients(x, [tokens], w, b, 2, "silu", 1e-5, dy)
+    ref, size = norm_of(x, [tokens], w, b, 2, "silu", 1e-5, dy)
+    for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
+        close(t, r, z, name, 2.0 ** -20, 2.0 ** -25)
