@@ -48,13 +48,13 @@ template <class T> __device__ inline T* norm_row(const View& v, int64_t b, int64
     return reinterpret_cast<T*>(v.data) + b * v.batch + row * v.row;
 }
 
-// A thread's 8 channels: their groups, and what is applied to them. 32-bit data
-// are taken from the mean as two numbers; 16-bit data, whose mean is at most
-// some 2^11 of their smallest differences, by one multiply-add.
+// A thread's 8 channels: their groups, and what is applied to them. Values are
+// taken from the mean before they are scaled, and the mean's rest in 32 bits
+// after that: equal values give 0 at any level, also where eps alone is the scale.
 template <class T> struct NormOctet {
     static constexpr bool kExact = sizeof(T) == 4;
     int group[8];
-    float high[kExact ? 8 : 1], low[8], rstd[8], w[8], b[8];   // (16 bits: low is -mean rstd)
+    float high[8], low[8], rstd[8], w[8], b[8];   // (low: of the mean's rest, times -rstd)
     __device__ NormOctet(const NormArgs& a, int col) {
         int g = col / a.cg, r = col - g * a.cg;
 #pragma unroll
@@ -80,12 +80,8 @@ template <class T> struct NormOctet {
     template <class F> __device__ __attribute__((always_inline)) void set(const NormArgs& a, F f) {
         auto put = [&](int i, double2 v) __attribute__((always_inline)) {
             rstd[i] = static_cast<float>(v.y);
-            if constexpr (kExact) {
-                high[i] = static_cast<float>(v.x);
-                low[i] = static_cast<float>(v.x - static_cast<double>(high[i]));
-            } else {
-                low[i] = static_cast<float>(-v.x * v.y);
-            }
+            high[i] = static_cast<float>(v.x);
+            low[i] = static_cast<float>((static_cast<double>(high[i]) - v.x) * v.y);
         };
         if (a.octet_groups) {
             const double2 v = f(group[0]);
@@ -94,12 +90,7 @@ template <class T> struct NormOctet {
             each<8>([&](auto i) __attribute__((always_inline)) { put(i.value, f(group[i.value])); });
         }
     }
-    __device__ float hat(T x, int i) const {
-        if constexpr (kExact)
-            return ((x - high[i]) - low[i]) * rstd[i];
-        else
-            return fmaf(static_cast<float>(x), rstd[i], low[i]);
-    }
+    __device__ float hat(T x, int i) const { return fmaf(static_cast<float>(x) - high[i], rstd[i], low[i]); }
     template <int ACT> __device__ frag<T> out(frag<T> x) const {
         frag<T> y;
 #pragma unroll

@@ -9,7 +9,7 @@ import pytest
 torch = pytest.importorskip("torch")
 import paper_2609_29119_amd as nc  # noqa: E402
 from paper_2609_29119_amd import layers  # noqa: E402
-from test_block_gpu import act_reference, close, offsets_of, randn  # noqa: E402
+from test_block_gpu import ACTS, TYPES, U, act_reference, close, offsets_of, randn  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -56,6 +56,58 @@ def norm_and_gradients(x, lengths, w, b, groups, act, eps, dy):
     x, w, b = (t.detach().requires_grad_() for t in (x, w, b))
     y = layers.band_norm(x, offsets_of(lengths), w, b, groups, act, eps)
     return [y.detach(), *torch.autograd.grad(y, (x, w, b), dy)]
+
+
+LEVEL = {torch.float32: (1000.0, -3e6), torch.float16: (1000.0, 30000.0, -60000.0), torch.bfloat16: (1000.0, -1e6)}
+EQUAL = [
+    # lengths, batch, channels, groups
+    ([1], 40, 16, 16),        # single tokens, a group a channel
+    ([7, 1, 30], 2, 24, 4),
+    ([9000, 3], 1, 24, 3),    # parts
+    ([2500], 2, 5, 5),
+]
+
+
+# --------------------------------------------------------------------------------------------- groups of equal values
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(EQUAL)))
+def test_band_norm_of_equal_values(case, dtype):
+    """A group without differences: the normalised value is 0 at any level, y is act(b), and w has no gradient."""
+    lengths, batch, ch, groups = EQUAL[case]
+    rows, G = sum(lengths), len(lengths)
+    w, b = (randn(n, G, ch, dtype=dtype) for n in (case, case + 10))
+    dy = randn(case + 20, batch, rows, ch, dtype=dtype)
+    for level in LEVEL[dtype]:
+        each = level * (1 - torch.arange(groups, device="cuda") / (4 * groups))       # a level of its own for each group
+        x = each.repeat_interleave(ch // groups).to(dtype).expand(batch, rows, ch).contiguous()
+        for act in ACTS:
+            got = norm_and_gradients(x, lengths, w, b, groups, act, 1e-5, dy)
+            ref, size = norm_of(x, lengths, w, b, groups, act, 1e-5, dy)
+            if act is None:
+                assert torch.equal(got[0], b.repeat_interleave(torch.tensor(lengths, device="cuda"), 0).expand_as(got[0]))
+            assert not got[2].any(), (level, act)
+            for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
+                close(t, r, z, f"{name} at {level}, {act}", 2.0 ** -20, 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(EQUAL)))
+def test_band_norm_of_nearly_equal_values(case, dtype):
+    """One value in forty is a step of the type above the level: the others are next to the mean, not on it."""
+    lengths, batch, ch, groups = EQUAL[case]
+    rows, G = sum(lengths), len(lengths)
+    w, b = (randn(n, G, ch, dtype=dtype) for n in (case, case + 10))
+    dy = randn(case + 20, batch, rows, ch, dtype=dtype)
+    some = (torch.rand(batch, rows, ch, generator=torch.Generator().manual_seed(case)) < 1 / 40).cuda()
+    for level in LEVEL[dtype]:
+        level = torch.tensor(level).to(dtype).item()
+        x = torch.where(some, level + 2 * U[dtype] * abs(level), level).to(dtype)
+        got = norm_and_gradients(x, lengths, w, b, groups, "silu", 1e-5, dy)
+        ref, size = norm_of(x, lengths, w, b, groups, "silu", 1e-5, dy)
+        for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
+            close(t, r, z, f"{name} at {level}", 2.0 ** -20, 2.0 ** -25)
 
 
 # ----------------------------------------------------------------------------------------------- levels far from zero
