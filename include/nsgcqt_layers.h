@@ -250,7 +250,8 @@ typedef struct {
  * the channels of a group and all tokens of a band of one signal. x, y:
  * [batch][rows][channels]. stats: [batch][n_bands][groups][2] float64, 16-byte
  * aligned, receives mean and 1 / sqrt(var + eps) of bands that have tokens, for
- * the gradient; NULL: not wanted. y may be x itself. */
+ * the gradient; NULL: not wanted. y may be x itself. A group that holds an
+ * infinity or NaN in a band has no variance: its y (and dx) are NaN there. */
 int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s, const nsgcqt_view* x,
                      const nsgcqt_view* y, double* stats, void* ws, size_t ws_bytes, void* stream);
 

@@ -229,6 +229,10 @@ __device__ inline int64_t norm_part(const NormArgs& a, int64_t b, int band, int 
     return b * a.parts + (start >> a.part_shift) + band + 1;
 }
 
+// 1 / sqrt(var + eps). What rounding left below 0 is 0; a NaN, of a group that
+// holds an infinity or NaN, stays one.
+__device__ inline double norm_rstd(double var, double eps) { return 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps); }
+
 // f(k, token) for the thread's tokens that exist
 template <int N, class F> __device__ __attribute__((always_inline)) inline void norm_tokens(const NormArgs& a, const NormPlace& p, F f) {
     each<N>([&](auto k) __attribute__((always_inline)) {
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     double2* st = p.stats(a);
     for (int g = tid; g < a.groups; g += a.threads) {
         const double off = mean[g] - static_cast<double>(static_cast<float>(mean[g]));
-        squares[g] = 1.0 / sqrt(fmax(squares[g] / count - off * off, 0.0) + a.eps);
+        squares[g] = norm_rstd(squares[g] / count - off * off, a.eps);
         if (a.stats) st[g] = double2{mean[g], squares[g]};
     }
     __syncthreads();
@@ -374,7 +378,7 @@ template <class T, bool GRAD> __global__ __launch_bounds__(256) void k_norm_join
     if (GRAD)
         part[0] = all;
     else
-        a.stats[place * a.groups + g] = double2{norm_pivot<T>(a, b, start, g) + all.x, 1.0 / sqrt(fmax(all.y - all.x * all.x, 0.0) + a.eps)};
+        a.stats[place * a.groups + g] = double2{norm_pivot<T>(a, b, start, g) + all.x, norm_rstd(all.y - all.x * all.x, a.eps)};
 }
 
 // y of longer bands, a part a workgroup: the next tokens are on their way while

@@ -122,3 +122,30 @@ def test_band_norm_of_a_level_of_a_million_deviations(tokens):
     ref, size = norm_of(x, [tokens], w, b, 2, "silu", 1e-5, dy)
     for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
         close(t, r, z, name, 2.0 ** -20, 2.0 ** -25)
+
+
+# --------------------------------------------------------------------------------------------------------- infinities
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_a_group_with_an_infinity_has_no_norm(bad, act, dtype):
+    """No variance: the group's values in that band and signal are NaN, in y and dx; all others are as they were."""
+    lengths, batch, ch = [5, 9000, 3], 2, 24
+    x = randn(1, batch, 9008, ch, dtype=dtype)
+    w, b = (randn(n, 3, ch, dtype=dtype) for n in (2, 3))
+    dy = randn(4, batch, 9008, ch, dtype=dtype)
+    want = norm_and_gradients(x, lengths, w, b, 3, act, 1e-5, dy)
+    hit = torch.zeros_like(x, dtype=torch.bool)
+    for signal, band, token, channel in ((0, slice(0, 5), 4, 3), (1, slice(5, 9005), 5, 8), (0, slice(5, 9005), 7000, 20)):
+        x[signal, token, channel] = bad
+        hit[signal, band, channel // 8 * 8:channel // 8 * 8 + 8] = True
+    got = norm_and_gradients(x, lengths, w, b, 3, act, 1e-5, dy)
+    for a, e, name in zip(got[:2], want[:2], ("y", "dx")):
+        assert a[hit].isnan().all(), name
+        assert torch.equal(a[~hit], e[~hit]), name
+    for a, name in zip(got[2:], ("dw", "db")):
+        if name == "dw" or act is not None:
+            assert a[0, :8].isnan().all() and a[1, 8:].isnan().all(), name
+        assert torch.isfinite(a[2]).all() and torch.isfinite(a[0, 8:]).all() and torch.isfinite(a[1, :8]).all(), name
