@@ -57,10 +57,14 @@ bool has_parts(const NormArgs& a) { return a.rows > 1 << a.shift; }
 // db: where these have 16 tokens or more at the mean, that is little beside the data.
 bool chunks_sum(const NormArgs& a) { return a.rows >= 16 * static_cast<int64_t>(a.n_bands + 1); }
 
-// Rows of an item of the weights' gradient, 64 to 4096: the most that leave 1024 items.
-int weight_shift_of(int64_t batch, int64_t rows) {
+// Rows of an item of the weights' gradient, 64 to 4096: the most that leave 1024
+// items; but no more than 32 a thread, which adds them up one after another in 32
+// bits (n equal terms are then off by up to n 2^-25 of their sum).
+int weight_shift_of(const NormArgs& a) {
+    NormArgs w = a;
+    set_threads(w, 256);
     int shift = 12;
-    while (shift > 6 && product(batch, rows) >> shift < 1024) --shift;
+    while ((shift > 6 && product(static_cast<int64_t>(a.batch), static_cast<int64_t>(a.rows)) >> shift < 1024) || 1 << shift > 32 * w.together) --shift;
     return shift;
 }
 
@@ -96,7 +100,7 @@ NormSpace norm_space(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     if (has_parts(a) && !grad) n.sums = product(16, r->batch, r->n_bands, a.groups);
     if (grad && weights)
         n.sums = product(8, chunks_sum(a) ? product(r->batch, r->n_bands + static_cast<int64_t>(a.parts))
-                                          : tile_count(weight_shift_of(r->batch, r->rows), r->n_bands, r->batch, r->rows), a.channels);
+                                          : tile_count(weight_shift_of(a), r->n_bands, r->batch, r->rows), a.channels);
     return n;
 }
 int64_t norm_bytes(const NormSpace& n) {
@@ -192,7 +196,7 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     CHECK_TRY(check_space(ws, ws_bytes, norm_bytes(space)));
     NormArgs a = norm_args(r, s);
     set_chunk(a, held_of(dtype, true));
-    a.weight_shift = weight_shift_of(r->batch, r->rows);
+    a.weight_shift = weight_shift_of(a);
     a.x = view_of(x);
     a.dy = view_of(dy);
     if (dx) a.y = view_of(dx);

@@ -621,14 +621,15 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_weight(NormArgs a) {
 }
 
 // Adds up what was left for dw and db of each band, in order: by k_norm_weight,
-// or with `by_chunk` by the other two.
+// or with `by_chunk` by the other two. In 64 bits: long rows leave thousands, and
+// terms of one sign may all be rounded the same way.
 template <class T> __global__ __launch_bounds__(256) void k_norm_weight_join(NormArgs a, bool by_chunk) {
     const int64_t id = (a.first_block + blockIdx.x) * 256 + threadIdx.x;
     const int c = static_cast<int>(id % a.channels), band = static_cast<int>(id / a.channels);
     if (id >= static_cast<int64_t>(a.n_bands) * a.channels) return;
     const int start = band_bound(a.off, a.n_bands, a.rows, band + 1), len = max(band_bound(a.off, a.n_bands, a.rows, band + 2) - start, 0);
     const int64_t step = 2 * static_cast<int64_t>(a.channels);
-    float dw = 0.f, db = 0.f;
+    double dw = 0.0, db = 0.0;
     auto add = [&](int64_t from, int64_t count, int64_t by) {
 #pragma unroll 8
         for (int64_t i = 0; i < count; ++i) {
@@ -645,8 +646,8 @@ template <class T> __global__ __launch_bounds__(256) void k_norm_weight_join(Nor
     } else if (len > 0) {
         add(band, a.batch, a.n_bands);
     }
-    if (a.dw) static_cast<T*>(a.dw)[id] = static_cast<T>(dw);
-    if (a.db) static_cast<T*>(a.db)[id] = static_cast<T>(db);
+    if (a.dw) static_cast<T*>(a.dw)[id] = static_cast<T>(static_cast<float>(dw));
+    if (a.db) static_cast<T*>(a.db)[id] = static_cast<T>(static_cast<float>(db));
 }
 
 }  // namespace nsl

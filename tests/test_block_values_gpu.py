@@ -124,6 +124,26 @@ def test_band_norm_of_a_level_of_a_million_deviations(tokens):
         close(t, r, z, name, 2.0 ** -20, 2.0 ** -25)
 
 
+# ------------------------------------------------------------------------------- very long sums of the norm's weights
+
+
+@pytest.mark.parametrize("lengths,batch,channels", [
+    ([2_000_000], 1, 16),        # thousands of parts
+    ([1], 262_144, 1032),        # one token of many signals, a thread's sum over as many rows as an item has
+])
+def test_long_sums_of_a_norm_s_weights(lengths, batch, channels):
+    """Terms of one sign, whose additions may all round the same way: n equal terms added in turn are off by up to
+    n 2^-25 of their sum. The chains in 32 bits have 32 terms here, 8 + 8 + 16 (a thread, its columns, their sum) or 32 of
+    a thread; what follows is in 64 bits, and rounded once."""
+    rows = lengths[0]
+    x = torch.randn(batch, rows, channels, device="cuda")
+    dy = (0.5 + (torch.arange(channels, device="cuda") + 0.3) / (2 * channels)).expand(batch, rows, channels)
+    b = torch.zeros(1, channels, device="cuda").requires_grad_()
+    db = torch.autograd.grad(layers.band_norm(x, offsets_of(lengths), None, b), b, dy)[0].double()
+    want = dy[0, :1].double() * (batch * rows)
+    assert ((db - want).abs() <= (2.0 ** -20 + 2.0 ** -24) * want).all(), ((db / want - 1).abs().max() * 2 ** 20).item()
+
+
 # --------------------------------------------------------------------------------------------------------- infinities
 
 
