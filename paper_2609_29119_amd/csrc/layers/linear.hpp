@@ -402,7 +402,8 @@ __global__ __launch_bounds__(256, 2) void k_linear_dw(LinearArgs a) {
     }
 }
 
-// Adds the partial sums of bands of several chunks, and writes zeros for empty bands: bands first_band on.
+// Adds the partial sums of bands of several chunks, and writes zeros for empty bands: bands first_band on. In 64 bits:
+// long rows leave thousands, and terms of one sign may all be rounded the same way.
 template <class T>
 __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
     const int band = a.first_band + static_cast<int>(blockIdx.y);
@@ -413,9 +414,10 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
     const int64_t chunks = (n_rows + (int64_t(1) << a.chunk_shift) - 1) >> a.chunk_shift;
     const int64_t item = ((b0 * a.batch) >> a.chunk_shift) + band + 1;
     for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < n; e += 256 * gridDim.x) {
-        float s = 0.f;
+        double all = 0.0;
 #pragma unroll 8
-        for (int64_t c = 0; c < chunks; ++c) s += dw_part(a, item + c)[e];
+        for (int64_t c = 0; c < chunks; ++c) all += dw_part(a, item + c)[e];
+        const float s = static_cast<float>(all);
         if (e < n_w)
             static_cast<T*>(a.dw)[band * n_w + e] = static_cast<T>(s);
         else

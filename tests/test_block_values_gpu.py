@@ -144,6 +144,22 @@ def test_long_sums_of_a_norm_s_weights(lengths, batch, channels):
     assert ((db - want).abs() <= (2.0 ** -20 + 2.0 ** -24) * want).all(), ((db / want - 1).abs().max() * 2 ** 20).item()
 
 
+# ----------------------------------------------------------------------------------------- and of the gated product's
+
+
+def test_long_sums_of_a_gated_product_s_biases():
+    """As for the norm's weights: 4,000,000 rows of one band."""
+    rows, n_out = 4_000_000, 8
+    x = torch.zeros(1, rows, 1, device="cuda")
+    w = randn(1, 1, 2, n_out, 1)
+    b = randn(2, 1, 2, n_out).requires_grad_()
+    dy = (0.5 + (torch.arange(n_out, device="cuda") + 0.3) / 16).expand(1, rows, n_out)
+    y = layers.band_gated(x, w, offsets_of([rows]), b, None)
+    db = torch.autograd.grad(y, b, dy)[0].double()
+    want = dy[0, 0].double() * b.detach().double().flip(1) * rows
+    assert ((db - want).abs() <= 2.0 ** -20 * want.abs()).all(), ((db / want - 1).abs().max() * 2 ** 20).item()
+
+
 # --------------------------------------------------------------------------------------------------------- infinities
 
 
