@@ -543,6 +543,12 @@ __global__ __launch_bounds__(512, 2) void k_gated_dw(GatedArgs a) {
                         du[j] = dy * f;
                     }
                 });
+                if (!more) {   // (rows that are not there: x and dy are 0, but a bias may be infinite)
+                    const int left = n - (r0 + 32 * wj + 16 * x + 4 * h);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (8 * (j >> 2) + (j & 3) >= left) da[j] = du[j] = 0.f;
+                }
                 sa += sum8(da);
                 su += sum8(du);
                 put_pieces(ds[wave] + (2 * x) * kPieces, lane, sum_of<T, 2>(da));

@@ -160,6 +160,26 @@ def test_long_sums_of_a_gated_product_s_biases():
     assert ((db - want).abs() <= 2.0 ** -20 * want.abs()).all(), ((db / want - 1).abs().max() * 2 ** 20).item()
 
 
+# -------------------------------------------------------------------------------------------- rows that are not there
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, n_in", [(1, 8), (33, 8), (70, 130)])
+def test_rows_that_are_not_there_add_nothing_to_infinite_values(rows, n_in, dtype):
+    """A gate or a value that a bias makes infinite: its gradient is infinite or, by the other bias, a sum over its rows."""
+    x, dy = randn(1, 1, rows, n_in, dtype=dtype), randn(2, 1, rows, 4, dtype=dtype).abs() + 0.5
+    w = randn(3, 1, 2, 4, n_in, dtype=dtype, by=0.1)
+    bias = torch.tensor([[[float("inf"), 1.0, 1.0, 2.0], [1.0, float("inf"), 1.0, 2.0]]], device="cuda").to(dtype).requires_grad_()
+    y = layers.band_gated(x, w, offsets_of([rows]), bias, None)
+    db = torch.autograd.grad(y, bias, dy)[0][0].double()
+    a, u = (torch.matmul(x[0].double(), w[0, i].double().T.contiguous()) + bias.detach()[0, i].double() for i in (0, 1))
+    want = torch.stack([(dy[0].double() * t).sum(0) for t in (u, a)])
+    size = torch.stack([(dy[0].double() * (1 + x[0].double().abs().sum(1, keepdim=True) + t.abs())).sum(0) for t in (u, a)])
+    assert torch.equal(db.isinf(), want.isinf()) and (db[want.isinf()] > 0).all()
+    fine = want.isfinite()
+    assert ((db - want)[fine].abs() <= U[dtype] * want[fine].abs() + 2.0 ** -20 * size[fine]).all()
+
+
 # --------------------------------------------------------------------------------------------------------- infinities
 
 
