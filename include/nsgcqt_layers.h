@@ -232,7 +232,8 @@ int nsgcqt_decay_step(int dtype, int64_t n_streams, int64_t n_heads, int64_t n_k
                       float* state, const int64_t* pos, const float* log_decay, void* stream);
 
 /* none: z; silu: z / (1 + exp(-z)); gelu: z Phi(z), Phi the normal
- * distribution's; sigmoid: 1 / (1 + exp(-z)). */
+ * distribution's; sigmoid: 1 / (1 + exp(-z)). At infinite z these, and their
+ * derivatives, are their limits. */
 typedef enum {
     NSGCQT_ACT_NONE = 0, NSGCQT_ACT_SILU = 1, NSGCQT_ACT_GELU = 2, NSGCQT_ACT_SIGMOID = 3
 } nsgcqt_act;

@@ -9,12 +9,20 @@ enum Act { kNone = 0, kSilu = 1, kGelu = 2, kSigmoid = 3 };
 // EXACT, for 32-bit results, makes up for what an exponent's product loses in
 // 32 bits; for 16-bit results that is left out (1e-6 at |z| = 10).
 
+// At infinite arguments, and where a product passes 32 bits, results are the
+// limits: 0 wins over what it is multiplied by, and an exponent's argument is
+// held where the result no longer changes. A NaN stays one. (v_mul_legacy_f32 is
+// such a product, so that most of it costs nothing.)
+__device__ __attribute__((const, noconvergent)) float zero_wins(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+__device__ inline float at_most(float x, float most) { return __builtin_elementwise_minimum(x, most); }
+
 // exp(-z). EXACT: what the exponent's product loses in 32 bits is added to
 // first order: off by 2e-7 relative however large |z|.
 template <bool EXACT> __device__ inline float exp_neg(float z) {
     constexpr float kHigh = -1.44269504f, kLow = -1.92596299e-8f;   // -log2(e)
+    if (!EXACT) return __builtin_amdgcn_exp2f(z * kHigh);
+    z = at_most(__builtin_elementwise_maximum(z, -128.f), 128.f);   // (infinite, 0)
     const float y = z * kHigh;
-    if (!EXACT) return __builtin_amdgcn_exp2f(y);
     const float rest = fmaf(z, kLow, fmaf(z, kHigh, -y));
     return __builtin_amdgcn_exp2f(y) * fmaf(rest, 0.69314718f, 1.f);
 }
@@ -36,14 +44,14 @@ template <bool EXACT> __device__ inline float logistic(float z) { return __built
 // Phi is off by 5e-7 relative over |z| <= 9, also where it is small.
 template <bool EXACT> __device__ inline float normal_cdf(float z, float& bell) {
     constexpr float kHigh = -0.721347520f, kLow = -9.62981497e-9f;   // -log2(e) / 2
-    z = __builtin_amdgcn_fmed3f(z, -13.f, 13.f);   // (beyond, Phi is 0 or 1 in 32 bits)
-    const float s = z * z, y = s * kHigh;
+    const float far = at_most(fabsf(z), 16.f);   // (exp(-128) is 0 in 32 bits)
+    const float s = far * far, y = s * kHigh;
     bell = __builtin_amdgcn_exp2f(y);
     if (EXACT) {
-        const float e = fmaf(z, z, -s), rest = fmaf(s, kLow, fmaf(s, kHigh, -y));
+        const float e = fmaf(far, far, -s), rest = fmaf(s, kLow, fmaf(s, kHigh, -y));
         bell *= fmaf(e, -0.5f, fmaf(rest, 0.69314718f, 1.f));
     }
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.23334524f, 1.f));
+    const float t = __builtin_amdgcn_rcpf(fmaf(far, 0.23334524f, 1.f));
     float q = fmaf(-0.134988993f, t, 0.458738714f);
     q = fmaf(q, t, -0.348531395f);
     q = fmaf(q, t, 0.406038553f);
@@ -57,8 +65,8 @@ template <bool EXACT> __device__ inline float normal_cdf(float z, float& bell) {
 
 template <int ACT, bool EXACT> __device__ inline float act_of(float z) {
     float bell;
-    if constexpr (ACT == kSilu) return z * logistic<EXACT>(z);
-    if constexpr (ACT == kGelu) return z * normal_cdf<EXACT>(z, bell);
+    if constexpr (ACT == kSilu) return zero_wins(z, logistic<EXACT>(z));
+    if constexpr (ACT == kGelu) return zero_wins(z, normal_cdf<EXACT>(z, bell));
     if constexpr (ACT == kSigmoid) return logistic<EXACT>(z);
     return z;
 }
@@ -67,14 +75,14 @@ template <int ACT, bool EXACT> __device__ inline float act_of(float z) {
 template <int ACT, bool EXACT> __device__ inline float act_of(float z, float& slope) {
     if constexpr (ACT == kSilu) {
         float other;
-        const float s = logistic<EXACT>(z, other);
-        slope = fmaf(z * s, other, s);
-        return z * s;
+        const float s = logistic<EXACT>(z, other), value = zero_wins(z, s);
+        slope = zero_wins(value, other) + s;
+        return value;
     } else if constexpr (ACT == kGelu) {
         float bell;
         const float phi = normal_cdf<EXACT>(z, bell);
-        slope = fmaf(0.39894228f * z, bell, phi);
-        return z * phi;
+        slope = zero_wins(0.39894228f * z, bell) + phi;
+        return zero_wins(z, phi);
     } else if constexpr (ACT == kSigmoid) {
         float other;
         const float s = logistic<EXACT>(z, other);

@@ -180,6 +180,68 @@ def test_rows_that_are_not_there_add_nothing_to_infinite_values(rows, n_in, dtyp
     assert ((db - want)[fine].abs() <= U[dtype] * want[fine].abs() + 2.0 ** -20 * size[fine]).all()
 
 
+# -------------------------------------------------------------------------------------------------- activations' ends
+
+
+def act_limits(z, how):
+    """act_reference, with its limits at the infinities."""
+    far = z.isinf()
+    f, slope = act_reference(torch.where(far, 0.0, z), how)
+    up = (z > 0).double()
+    if how is None:
+        return z, torch.ones_like(z)
+    value = up if how == "sigmoid" else torch.where(z > 0, z, 0.0)
+    return torch.where(far, value, f), torch.where(far, 0.0 if how == "sigmoid" else up, slope)
+
+
+def extremes(dtype):
+    most = torch.finfo(dtype).max
+    z = [0.0, 1.0, 3.0, 10.0, 13.25, 14.5, 20.0, 88.0, 104.0, 127.0, 200.0, 1e4, 1e19, 1e30, 1e36, 1e38, 2.5e38, 3e38, most]
+    z = torch.tensor([v for v in z if v <= most] + [float("inf")], dtype=torch.float64)
+    return torch.cat([z, -z]).to(dtype).cuda()
+
+
+def check_act(got, want, z, what):
+    """Equal where infinite; else one rounding and 2^-20 of the value, times the argument where it is an exponent. An
+    exponential below 2^-126 may be taken for 0, and is multiplied by at most 1 + |z|, with |z| < 128 where it is not 0."""
+    got, want, z = got.double(), want.double(), z.detach()
+    by = 1 + z.double().abs().clamp(max=128)
+    tiny = 2.0 ** -25 if z.dtype == torch.float16 else by * 2.0 ** -126
+    fine = torch.where(want.isinf(), got == want, (got - want).abs() <= (U[z.dtype] + 2.0 ** -20 * by) * want.abs() + tiny)
+    assert fine.all(), f"{what}: {z[~fine].tolist()} give {got[~fine].tolist()}, not {want[~fine].tolist()}"
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_at_their_ends(act, dtype):
+    """Infinite and the largest arguments, as biases set them, in both operators; slopes as db has them."""
+    z = extremes(dtype)
+    n = z.numel()
+    want, slope = act_limits(z.double(), act)
+    off = offsets_of([1])
+    bias = torch.stack([z, torch.ones_like(z)])[None].requires_grad_()
+    x, w = randn(1, 1, 1, 8, dtype=dtype).requires_grad_(), torch.zeros(1, 2, n, 8, dtype=dtype, device="cuda")
+    y = layers.band_gated(x, w, off, bias, act)
+    dx, db = torch.autograd.grad(y, [x, bias], torch.ones_like(y))
+    check_act(y[0, 0], want, z, "gated")
+    check_act(db[0, 0], slope, z, "gated slope")
+    check_act(db[0, 1], want, z, "gated, other bias")
+    y = layers.band_gated(x.detach().expand(1, 1, 8), w, off, bias.detach(), act)
+    check_act(y[0, 0], want, z, "gated forward")
+    for rows in (1, 9000):
+        level = torch.full((1, rows, n), 3.0, dtype=dtype, device="cuda")
+        b = z[None].detach().requires_grad_()
+        y = layers.band_norm(level, offsets_of([rows]), torch.ones_like(b), b, 1, act)
+        dy = torch.zeros_like(y)
+        dy[:, rows // 2] = 1.0
+        db = torch.autograd.grad(y, b, dy)[0]
+        check_act(y[0, 0], want, z, "norm")
+        check_act(y[0, -1], want, z, "norm")
+        check_act(db[0], slope, z, "norm slope")
+    # a NaN stays one
+    assert layers.band_gated(x.detach(), w, off, torch.full_like(bias, float("nan")).detach(), act).isnan().all()
+
+
 # --------------------------------------------------------------------------------------------------------- infinities
 
 
