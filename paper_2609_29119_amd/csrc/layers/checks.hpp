@@ -10,7 +10,7 @@ using nsg::launch_kernel;
 using nsg::set_err;
 
 constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxCount = int64_t(1) << 30, kMaxBands = int64_t(1) << 24,
-                  kMaxWidth = 65536, kMaxGrid = 0xffffffffll / 256;   // a launch takes less than 2^32 threads
+                  kMaxWidth = 65536, kMaxGrid = 0xffffffffll / 256;   // a launch takes less than 2^32 threads, here of workgroups of 256
 
 inline int elem_bytes(int dtype) { return dtype == NSGCQT_F32 ? 4 : 2; }
 
@@ -68,8 +68,10 @@ template <class... N> inline int64_t product(int64_t a, N... rest) {
     return a;
 }
 
-inline int check_grid(int64_t blocks) {
-    if (blocks > kMaxGrid) return set_err(NSGCQT_EUNSUPPORTED, "more than 16,777,215 workgroups");
+// blocks of a launch, of at most `threads` each
+inline int check_grid(int64_t blocks, int threads = 256) {
+    const int64_t most = 0xffffffffll / threads;
+    if (blocks > most) return set_err(NSGCQT_EUNSUPPORTED, "more than " + std::to_string(most) + " workgroups");
     return NSGCQT_OK;
 }
 

@@ -143,7 +143,7 @@ int nsgcqt_band_gated_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x
         a.dw.chunk_shift = gated_chunk_shift(r->batch, r->rows, n_out);
         items = tile_count(a.dw.chunk_shift, r->n_bands, r->batch, r->rows) * ((n_out + 127) / 128) *
                 (slabs ? slabs : 1);
-        CHECK_TRY(check_grid(items));
+        CHECK_TRY(check_grid(items, kGatedThreads));
     }
     return by_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
@@ -151,7 +151,7 @@ int nsgcqt_band_gated_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_view* x
             constexpr bool kHeld = decltype(held)::value;
             if (inputs) LAUNCH_TRY((k_gated_dx<T, kHeld>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a);
             if (weights) {
-                LAUNCH_TRY((k_gated_dw<T, kHeld>), dim3(static_cast<unsigned>(items)), dim3(512), 0, st, a);
+                LAUNCH_TRY((k_gated_dw<T, kHeld>), dim3(static_cast<unsigned>(items)), dim3(kGatedThreads), 0, st, a);
                 const int64_t join = (2 * n_in * n_out + 2 * n_out + 255) / 256;
                 for (LinearArgs l = a.dw; l.first_band < l.n_bands; l.first_band += 65535)
                     LAUNCH_TRY(k_linear_join<T>, dim3(static_cast<unsigned>(join < 64 ? join : 64),

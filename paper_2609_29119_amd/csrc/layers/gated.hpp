@@ -428,8 +428,9 @@ template <class F, int N> __device__ inline Pieces<F, N> get_pieces(const char* 
 // registers, one wave a SIMD: 685); without the slope 325, without the second
 // product 317. Its two barriers a step keep a SIMD's waves in the same phase, so
 // that vector work and matrix cores take turns.
+constexpr int kGatedThreads = 512;
 template <class T, bool HELD>
-__global__ __launch_bounds__(512, 2) void k_gated_dw(GatedArgs a) {
+__global__ __launch_bounds__(kGatedThreads, 2) void k_gated_dw(GatedArgs a) {
     constexpr int BK = gated_inputs<T>(), NB = BK / 64, KS = BK / 16, RB = row_bytes<T, 128>(), RX = row_bytes<T, BK>();
     constexpr int kEach = 64 * 128 / 8 / 512, kEachX = 64 * BK / 8 / 512, NP = sizeof(T) == 4 ? 1 : 2;
     constexpr int kPieces = NP * static_cast<int>(sizeof(piece<T>)) * 64;   // bytes of a fragment's pieces

@@ -168,3 +168,12 @@ def test_no_kernel_spills(name, tmp_path):
     scratch = [int(v) for v in re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", r.stderr)]
     assert names and len(names) == len(scratch)
     assert not [(n, s) for n, s in zip(names, scratch) if s]
+
+
+def test_gated_gradients_of_more_workgroups_than_a_launch_takes(L):  # noqa: F811
+    """The weights' gradient has workgroups of 512: half as many as the other kernels' fit a launch."""
+    v = view()
+    grad = lambda bands: L.nsgcqt_band_gated_grad(  # noqa: E731
+        0, ref(rows(n=8, bands=bands)), ref(v), FAKE, None, ref(v), None, FAKE, None, 8, 8, 1, FAKE, 1 << 40, None)
+    refused(grad(9_000_000), nb.EUNSUPPORTED, "8388607 workgroups")
+    refused(grad(1 << 24), nb.EUNSUPPORTED, "workgroups")
