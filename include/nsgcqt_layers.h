@@ -56,8 +56,10 @@
  *     stream, kv head and 32 query heads of it, and one for each stream and head.
  *     The decayed attention takes one for each segment (64 to 4,096 tokens)
  *     of each band of each signal and head, its step for each stream and kv
- *     head, the norm for each band (and part of a long one) of each signal,
- *     the gated product for 128 tokens or more of a band and 64 outputs.
+ *     head, the gated product for 128 tokens or more of a band and 64 outputs
+ *     (256 and 128 for the weights' gradient, 8,388,607 of them a launch). The
+ *     norm takes one for each band (and part of a long one) of each signal, in
+ *     as many launches of whole signals as that needs, up to 2^34 in all.
  */
 #ifndef NSGCQT_LAYERS_H
 #define NSGCQT_LAYERS_H

@@ -118,10 +118,25 @@ int check_space(const void* ws, size_t have, int64_t need) {
     return NSGCQT_OK;
 }
 
-template <class K, class... More> int launch_all(K kernel, NormArgs a, int64_t threads, hipStream_t st, More... more) {
-    const int64_t blocks = (threads + 255) / 256;
-    for (; a.first_block < blocks; a.first_block += kMaxGrid)
-        LAUNCH_TRY(kernel, dim3(static_cast<unsigned>(std::min(blocks - a.first_block, kMaxGrid))), dim3(256), 0, st, a, more...);
+// A kernel's workgroups, `each` of every signal, in launches of whole signals.
+constexpr int64_t kMaxBlocks = int64_t(1) << 34;
+int check_signals(const NormArgs& a, int64_t each) {
+    CHECK_TRY(check_grid(each, a.threads));
+    if (product(static_cast<int64_t>(a.batch), each) > kMaxBlocks) return set_err(NSGCQT_EUNSUPPORTED, "more than 2^34 workgroups");
+    return NSGCQT_OK;
+}
+template <class K> int launch_signals(K kernel, NormArgs a, int64_t each, size_t lds, hipStream_t st) {
+    const int64_t most = 0xffffffffll / a.threads / each;   // signals a launch
+    for (; a.first_signal < a.batch; a.first_signal += most)
+        LAUNCH_TRY(kernel, dim3(static_cast<unsigned>(std::min(a.batch - a.first_signal, most) * each)), dim3(a.threads), lds, st, a);
+    return NSGCQT_OK;
+}
+
+// And `blocks` of all signals.
+template <class K, class... More> int launch_all(K kernel, NormArgs a, int64_t blocks, int threads, size_t lds, hipStream_t st, More... more) {
+    const int64_t most = 0xffffffffll / threads;
+    for (; a.first_block < blocks; a.first_block += most)
+        LAUNCH_TRY(kernel, dim3(static_cast<unsigned>(std::min(blocks - a.first_block, most))), dim3(threads), lds, st, a, more...);
     return NSGCQT_OK;
 }
 
@@ -156,22 +171,21 @@ int nsgcqt_band_norm(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_shape* s
     a.part = static_cast<double2*>(ws);
     a.stats = stats ? reinterpret_cast<double2*>(stats)
                     : space.part ? reinterpret_cast<double2*>(static_cast<char*>(ws) + space.part) : nullptr;
-    const int64_t blocks = product(r->batch, r->n_bands + a.zeros);
-    CHECK_TRY(check_grid(blocks));
+    const int64_t blocks = r->n_bands + a.zeros;
+    CHECK_TRY(check_signals(a, blocks));
+    if (space.part) CHECK_TRY(check_signals(a, a.parts));
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
-    CHECK_TRY(check_grid(product(r->batch, static_cast<int64_t>(a.parts))));
-    const dim3 grid(static_cast<unsigned>(blocks)), parts(static_cast<unsigned>(r->batch * a.parts)), block(a.threads);
     const size_t lds = norm_lds(a);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
         using T = decltype(t);
         constexpr bool kWide = decltype(w)::value;
-        LAUNCH_TRY((k_norm<T, kWide>), grid, block, lds, st, a);
+        CHECK_TRY(launch_signals(k_norm<T, kWide>, a, blocks, lds, st));
         if (space.part) {
-            LAUNCH_TRY((k_norm_sum<T, kWide>), parts, block, lds, st, a);
-            CHECK_TRY(launch_all((k_norm_join<T, false>), a, groups, st));
-            LAUNCH_TRY((k_norm_apply<T, kWide>), parts, block, 0, st, a);
+            CHECK_TRY(launch_signals(k_norm_sum<T, kWide>, a, a.parts, lds, st));
+            CHECK_TRY(launch_all(k_norm_join<T, false>, a, (groups + 255) / 256, 256, 0, st));
+            CHECK_TRY(launch_signals(k_norm_apply<T, kWide>, a, a.parts, 0, st));
         }
         return NSGCQT_OK;
     });
@@ -207,27 +221,25 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
     if (by_chunk) a.sums = sums;
     a.dw = dw;
     a.db = db;
-    const int64_t blocks = product(r->batch, r->n_bands + a.zeros);
+    const int64_t blocks = r->n_bands + a.zeros;
     const int64_t items = tile_count(a.weight_shift, r->n_bands, r->batch, r->rows);
     const int64_t groups = product(r->batch, r->n_bands, a.groups);
-    const int64_t parts = product(r->batch, static_cast<int64_t>(a.parts));
-    if (dx || by_chunk) CHECK_TRY(check_grid(std::max(blocks, parts)));
-    if (weights && !by_chunk) CHECK_TRY(check_grid(items));
+    const bool bands = (dx || by_chunk) && rows;
+    if (bands) CHECK_TRY(check_signals(a, blocks));
+    if (bands && space.part) CHECK_TRY(check_signals(a, a.parts));
     if (groups == INT64_MAX) return set_err(NSGCQT_EUNSUPPORTED, "more groups than 64 bits count");
-    const dim3 block(a.threads);
     const size_t lds = norm_lds(a);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return by_width_of(dtype, wide, [&](auto t, auto w) -> int {
         using T = decltype(t);
         constexpr bool kWide = decltype(w)::value;
-        if ((dx || by_chunk) && rows) {
-            const dim3 grid(static_cast<unsigned>(blocks));
-            LAUNCH_TRY((k_norm_grad<T, kWide>), grid, block, lds, st, a);
+        if (bands) {
+            CHECK_TRY(launch_signals(k_norm_grad<T, kWide>, a, blocks, lds, st));
             if (space.part) {
-                LAUNCH_TRY((k_norm_grad_sum<T, kWide>), dim3(static_cast<unsigned>(parts)), block, lds, st, a);
+                CHECK_TRY(launch_signals(k_norm_grad_sum<T, kWide>, a, a.parts, lds, st));
                 if (dx) {
-                    CHECK_TRY(launch_all((k_norm_join<T, true>), a, groups, st));
-                    LAUNCH_TRY((k_norm_grad_apply<T, kWide>), dim3(static_cast<unsigned>(parts)), block, 0, st, a);
+                    CHECK_TRY(launch_all(k_norm_join<T, true>, a, (groups + 255) / 256, 256, 0, st));
+                    CHECK_TRY(launch_signals(k_norm_grad_apply<T, kWide>, a, a.parts, 0, st));
                 }
             }
         }
@@ -235,9 +247,9 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
             a.sums = sums;
             if (rows && !by_chunk) {
                 set_threads(a, 256);
-                LAUNCH_TRY((k_norm_weight<T, kWide>), dim3(static_cast<unsigned>(items)), dim3(a.threads), norm_lds(a), st, a);
+                CHECK_TRY(launch_all(k_norm_weight<T, kWide>, a, items, a.threads, norm_lds(a), st));
             }
-            CHECK_TRY(launch_all(k_norm_weight_join<T>, a, r->n_bands * s->channels, st, by_chunk));
+            CHECK_TRY(launch_all(k_norm_weight_join<T>, a, (r->n_bands * s->channels + 255) / 256, 256, 0, st, by_chunk));
         }
         return NSGCQT_OK;
     });

@@ -38,7 +38,7 @@ struct NormArgs {
     int weight_shift;             // of the rows of an item of k_norm_weight
     unsigned parts;               // of a signal, the empty ones among them
     int zeros;                    // workgroups of a signal for the tokens that no band holds
-    int64_t first_block;          // of a launch of a kernel whose blocks may pass a grid's limit
+    int64_t first_block, first_signal;   // of a launch, where a call takes several
     int act;
     bool octet_groups;            // a group is whole octets of channels
     double eps;
@@ -181,8 +181,8 @@ struct NormPlace {
     __device__ NormPlace(const NormArgs& a, unsigned items, int shift) {
         const unsigned id = last_first(blockIdx.x, gridDim.x);
         const int tid = threadIdx.x;
-        b = id / items;
-        item = id - static_cast<unsigned>(b) * items;
+        item = id % items;
+        b = a.first_signal + id / items;
         t = find_tile<int>(a.off, a.n_bands, a.rows, 1, shift, static_cast<int>(item), tid & 63);
         all = min(t.len - t.first, 1 << shift);
         outside = t.band < 0 || t.band >= a.n_bands;
@@ -196,8 +196,8 @@ struct NormPlace {
     __device__ explicit NormPlace(const NormArgs& a) {
         const unsigned items = a.n_bands + a.zeros, id = gridDim.x - 1 - blockIdx.x;
         const int tid = threadIdx.x;
-        b = id / items;
-        item = id - static_cast<unsigned>(b) * items;
+        item = id % items;
+        b = a.first_signal + id / items;
         t.band = static_cast<int>(item);
         outside = t.band >= a.n_bands;
         t.start = outside ? 0 : band_bound(a.off, a.n_bands, a.rows, t.band + 1);
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_weight(NormArgs a) {
     extern __shared__ __align__(16) double norm_lds[];
     float2* cells = reinterpret_cast<float2*>(norm_lds);
     const int tid = threadIdx.x, lane = tid & 63;
-    const unsigned id = die_order(blockIdx.x, gridDim.x);
+    const int64_t id = a.first_block + die_order(blockIdx.x, gridDim.x);
     const Tile<int64_t> t = find_tile<int64_t>(a.off, a.n_bands, a.rows, a.batch, a.weight_shift, id, lane);
     if (!t.live || t.band < 0 || t.band >= a.n_bands) return;
     const int64_t end = min(t.first + (int64_t(1) << a.weight_shift), static_cast<int64_t>(t.len) * a.batch);
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_weight(NormArgs a) {
         });
     }
     norm_columns(a, cells, works, tr, col, s, tid);
-    float* to = a.sums + static_cast<int64_t>(id) * 2 * a.channels;
+    float* to = a.sums + id * 2 * a.channels;
     for (int c = tid; c < a.channels; c += a.threads) {
         float2 v = cells[norm_cell(a, c)];
         for (int k = 1; k < norm_parts(a); ++k) v += cells[k * 8 * a.octets + norm_cell(a, c)];

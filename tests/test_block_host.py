@@ -177,3 +177,10 @@ def test_gated_gradients_of_more_workgroups_than_a_launch_takes(L):  # noqa: F81
         0, ref(rows(n=8, bands=bands)), ref(v), FAKE, None, ref(v), None, FAKE, None, 8, 8, 1, FAKE, 1 << 40, None)
     refused(grad(9_000_000), nb.EUNSUPPORTED, "8388607 workgroups")
     refused(grad(1 << 24), nb.EUNSUPPORTED, "workgroups")
+
+
+def test_norms_of_more_workgroups_than_launches_take(L):  # noqa: F811
+    v = view()
+    call = lambda r, s=norm(): L.nsgcqt_band_norm(0, ref(r), ref(s), ref(v), ref(v), None, None, 0, None)  # noqa: E731
+    refused(call(rows(n=8, bands=1 << 23, batch=1 << 12)), nb.EUNSUPPORTED, "2^34")
+    refused(call(rows(n=1, bands=1 << 23), norm(channels=4096, groups=1)), nb.EUNSUPPORTED, "8388607 workgroups")

@@ -267,3 +267,37 @@ def test_a_group_with_an_infinity_has_no_norm(bad, act, dtype):
         if name == "dw" or act is not None:
             assert a[0, :8].isnan().all() and a[1, 8:].isnan().all(), name
         assert torch.isfinite(a[2]).all() and torch.isfinite(a[0, 8:]).all() and torch.isfinite(a[1, :8]).all(), name
+
+
+# ---------------------------------------------------------------------------------- more workgroups than a launch has
+
+
+def test_band_norm_of_more_signals_than_a_launch_has_workgroups():
+    """Single tokens of 33,554,435 signals: two launches of each kernel."""
+    n = (1 << 25) + 3
+    x = torch.randn(n, 1, 2, device="cuda").bfloat16().requires_grad_()
+    w = torch.tensor([[1.5, -2.0]], device="cuda").bfloat16().requires_grad_()
+    dy = torch.randn(n, 1, 2, device="cuda").bfloat16()
+    y = layers.band_norm(x, torch.tensor([0, 1], device="cuda"), w, eps=1e-3)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+    for at in (slice(0, 1 << 20), slice((1 << 25) - (1 << 20), n)):   # around the launches' border and at both ends
+        ref, size = zip(*[norm_of_pairs(t[at].detach(), d[at], w) for t, d in ((x, dy),)])
+        close(y[at], ref[0][0], size[0][0], "y", 2.0 ** -20, 1e-37)
+        close(dx[at], ref[0][1], size[0][1], "dx", 2.0 ** -20, 1e-37)
+    assert not (y == 0).all(2).logical_and((x[:, :, 0] != x[:, :, 1])).any()
+    want, terms = torch.zeros(2, device="cuda").double(), torch.zeros(2, device="cuda").double()
+    for i in range(0, n, 1 << 22):
+        t = x[i:i + (1 << 22), 0].detach().double()
+        h = (t - t.mean(1, keepdim=True)) * (t.var(1, correction=0, keepdim=True) + 1e-3) ** -0.5 * dy[i:i + (1 << 22), 0].double()
+        want, terms = want + h.sum(0), terms + h.abs().sum(0)
+    close(dw[0], want, terms, "dw", 2.0 ** -20)
+
+
+def norm_of_pairs(x, dy, w, eps=1e-3):
+    """(y, dx) of groups of two values, in 64 bits, and their sizes."""
+    x, dy, w = (t.detach().double() for t in (x, dy, w))
+    t = x - x.mean(2, keepdim=True)
+    r = ((t * t).mean(2, keepdim=True) + eps) ** -0.5
+    hat, d = t * r, dy * w
+    dx = r * (d - d.mean(2, keepdim=True) - hat * (d * hat).mean(2, keepdim=True))
+    return (hat * w, dx), ((hat.abs() + 2) * w.abs(), r * (d.abs() + d.abs().mean(2, keepdim=True)) * (2 + (hat.abs() + 2) ** 2))
