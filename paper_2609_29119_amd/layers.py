@@ -612,6 +612,12 @@ def _decay_bytes(bands, batch, rows, heads, kv_heads, dim, grad):
                                                           _decay_shape(heads, kv_heads, dim, 1.0, at, 0, 0), grad))
 
 
+def _decay_sizes(q, k, log_decay, keep, scale, offsets):
+    """Refuses a shape as the call itself does."""
+    _bytes(_lib().nsgcqt_decay_attention_workspace(_ragged(offsets, q.shape[0], q.shape[1]),
+                                                   _decay_shape_of(q, k, log_decay, keep, scale), 0))
+
+
 def _decay_workspace(q, kv_heads, offsets, grad):
     n = _decay_bytes(offsets.shape[0] - 1, q.shape[0], q.shape[1], q.shape[2], kv_heads, q.shape[3], grad)
     return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None, n
@@ -650,19 +656,8 @@ class _DecayAttention(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None
 
 
-def decay_attention(q, k, v, offsets, log_decay, scale=None, keep=None, state=None):
-    """Linear attention along each band, the past decaying by exp(log_decay) a token.
-
-    o_t = scale * sum over s <= t of exp(log_decay (t - s)) (q_t . k_s) v_s,
-    within token t's band. q [batch][rows][heads][D], k and v with kv_heads
-    heads, a divisor of heads (D at most 128); log_decay float32 [kv_heads], at
-    most 0. scale: D^-1/2 by default. keep (bool [batch][rows] or None): tokens
-    that add nothing, though they count as distance; what k and v hold there is
-    never used. state (float32 [batch * n_bands][kv_heads][D][D] or None): the
-    sum of exp(..) k_s v_s^T over what came before each band, row b * n_bands +
-    g for band g of signal b; it is replaced by that sum at the band's end.
-    Gradients for q, k and v, where no state is given; log_decay has none.
-    """
+def _decay_checks(q, k, v, offsets, log_decay, scale, keep, state):
+    """Checks a call's arguments; the function to call, and the scale."""
     _tensor(q, "q", dims="[batch][rows][heads][D]")
     if k.dim() != 4:
         raise ValueError("k has to be [batch][rows][kv_heads][D]")
@@ -680,8 +675,24 @@ def decay_attention(q, k, v, offsets, log_decay, scale=None, keep=None, state=No
         _states(state, q, batch * (offsets.numel() - 1), kv_heads, dim)
         if trains or _trains(state):
             raise ValueError("decay_attention has no gradient from or into a state: call it under torch.no_grad()")
-    o = (_DecayAttention.apply if trains else _decay_forward)(q, k, v, offsets, log_decay, keep, state,
-                                                              _scale(scale, dim))
+    return _DecayAttention.apply if trains else _decay_forward, _scale(scale, dim)
+
+
+def decay_attention(q, k, v, offsets, log_decay, scale=None, keep=None, state=None):
+    """Linear attention along each band, the past decaying by exp(log_decay) a token.
+
+    o_t = scale * sum over s <= t of exp(log_decay (t - s)) (q_t . k_s) v_s,
+    within token t's band. q [batch][rows][heads][D], k and v with kv_heads
+    heads, a divisor of heads (D at most 128); log_decay float32 [kv_heads], at
+    most 0. scale: D^-1/2 by default. keep (bool [batch][rows] or None): tokens
+    that add nothing, though they count as distance; what k and v hold there is
+    never used. state (float32 [batch * n_bands][kv_heads][D][D] or None): the
+    sum of exp(..) k_s v_s^T over what came before each band, row b * n_bands +
+    g for band g of signal b; it is replaced by that sum at the band's end.
+    Gradients for q, k and v, where no state is given; log_decay has none.
+    """
+    call, scale = _decay_checks(q, k, v, offsets, log_decay, scale, keep, state)
+    o = call(q, k, v, offsets, log_decay, keep, state, scale)
     if state is not None:
         _written(state)
     return o
@@ -722,7 +733,8 @@ class DecayState:
     """The states of many streams of `decay_attention`: one matrix a key head, however long a stream is.
 
     `pos` holds the number of each stream's next token; a stream whose pos is
-    below 0 is idle: its state and its pos stay as they are.
+    below 0 is idle: its state and its pos stay as they are, until `read` has
+    tokens for it.
     """
 
     def __init__(self, streams, kv_heads, head_dim, device="cuda"):
@@ -731,12 +743,14 @@ class DecayState:
 
     def read(self, q, k, v, offsets, log_decay, scale=None, keep=None):
         """`decay_attention` of whole bands: band g of signal b continues stream b * n_bands + g, or begins it where
-        its pos is 0 or below."""
-        self.pos.clamp_(min=0)
-        self.state.masked_fill_((self.pos == 0)[:, None, None, None], 0.0)
-        o = decay_attention(q, k, v, offsets, log_decay, scale, keep, self.state)
-        ends = offsets.clamp(0, k.shape[1])     # bands are cut to the row, as the kernels cut them
-        self.pos += (ends[1:] - ends[:-1]).repeat(k.shape[0])
+        its pos is 0, or below 0 and the band has tokens. A call that is refused leaves states and pos as they are."""
+        _, factor = _decay_checks(q, k, v, offsets, log_decay, scale, keep, self.state)
+        _decay_sizes(q, k, log_decay, keep, factor, offsets)
+        ends = offsets.clamp(0, q.shape[1])     # bands are cut to the row, as the kernels cut them
+        more = (ends[1:] - ends[:-1]).clamp_(min=0).repeat(q.shape[0])
+        self.state.masked_fill_(((self.pos == 0) | ((self.pos < 0) & (more > 0)))[:, None, None, None], 0.0)
+        o = decay_attention(q, k, v, offsets, log_decay, factor, keep, self.state)
+        self.pos.copy_(torch.where(more > 0, self.pos.clamp(min=0) + more, self.pos))
         return o
 
     def step(self, q, k, v, log_decay, scale=None):

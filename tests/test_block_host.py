@@ -184,3 +184,14 @@ def test_norms_of_more_workgroups_than_launches_take(L):  # noqa: F811
     call = lambda r, s=norm(): L.nsgcqt_band_norm(0, ref(r), ref(s), ref(v), ref(v), None, None, 0, None)  # noqa: E731
     refused(call(rows(n=8, bands=1 << 23, batch=1 << 12)), nb.EUNSUPPORTED, "2^34")
     refused(call(rows(n=1, bands=1 << 23), norm(channels=4096, groups=1)), nb.EUNSUPPORTED, "8388607 workgroups")
+
+
+def test_a_refused_read_leaves_the_streams_as_they_are():
+    torch = pytest.importorskip("torch")
+    held = layers.DecayState(2, 1, 8, device="cpu")
+    held.state.fill_(7.0)
+    held.pos.copy_(torch.tensor([-1, 0]))
+    q = torch.zeros(1, 4, 1, 8)
+    with pytest.raises(ValueError, match="cuda"):
+        held.read(q, q, q, torch.tensor([0, 2, 4]), torch.zeros(1))
+    assert held.pos.tolist() == [-1, 0] and (held.state == 7.0).all()

@@ -301,3 +301,28 @@ def norm_of_pairs(x, dy, w, eps=1e-3):
     hat, d = t * r, dy * w
     dx = r * (d - d.mean(2, keepdim=True) - hat * (d * hat).mean(2, keepdim=True))
     return (hat * w, dx), ((hat.abs() + 2) * w.abs(), r * (d.abs() + d.abs().mean(2, keepdim=True)) * (2 + (hat.abs() + 2) ** 2))
+
+
+# ------------------------------------------------------------------------------------------------------------ streams
+
+
+def test_streams_that_a_read_begins_continues_and_leaves_alone():
+    """Streams at 0, idle or going on, with and without tokens; a refused call changes nothing."""
+    lengths, off, lam = [5, 0, 7, 0, 3, 0], offsets_of([5, 0, 7, 0, 3, 0]), torch.tensor([-0.1, -0.01], device="cuda")
+    q, k, v = (randn(i, 1, 15, 2, 8) for i in (1, 2, 3))
+    held = layers.DecayState(6, 2, 8)
+    held.state.copy_(randn(4, 6, 2, 8, 8))
+    held.pos.copy_(torch.tensor([0, 0, -1, -2, 9, 4], device="cuda"))
+    state, pos = held.state.clone(), held.pos.clone()
+    for bad, error in ((dict(scale=float("inf")), nc.NsgcqtError), (dict(scale=1e300), nc.NsgcqtError),
+                       (dict(keep=torch.ones(1, 14, dtype=torch.bool, device="cuda")), ValueError)):
+        with pytest.raises(error):
+            held.read(q, k, v, off, lam, **bad)
+        assert torch.equal(held.state, state) and torch.equal(held.pos, pos)
+    start = state.clone()
+    start[[0, 2]] = 0.0          # those that begin
+    want = layers.decay_attention(q, k, v, off, lam, state=start)
+    assert torch.equal(held.read(q, k, v, off, lam), want)
+    assert held.pos.tolist() == [5, 0, 7, -2, 12, 4]
+    for n in (0, 2, 3, 4, 5):    # (what the state at pos 0 holds is not used)
+        assert torch.equal(held.state[n], start[n] if lengths[n] else state[n]), n
