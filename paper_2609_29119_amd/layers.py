@@ -690,6 +690,9 @@ def decay_attention(q, k, v, offsets, log_decay, scale=None, keep=None, state=No
     sum of exp(..) k_s v_s^T over what came before each band, row b * n_bands +
     g for band g of signal b; it is replaced by that sum at the band's end.
     Gradients for q, k and v, where no state is given; log_decay has none.
+    Tokens are taken 32 at a time: an infinity or NaN of a kept token, or a
+    product with it that passes 32 bits, may make the results of up to 31 tokens
+    before it NaN (in the gradients for k and v, of up to 31 after it).
     """
     call, scale = _decay_checks(q, k, v, offsets, log_decay, scale, keep, state)
     o = call(q, k, v, offsets, log_decay, keep, state, scale)

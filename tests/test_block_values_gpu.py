@@ -4,6 +4,8 @@ values, levels far above the differences, infinite and extreme arguments, very l
 Bounds, beside test_block_gpu's: what a norm makes of a value is off by 2^-20 of the normalised value and of 1 (the
 level's own rest, 2^-24 of a level of 10^6 deviations), however high the level is.
 """
+import ctypes
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -269,6 +271,20 @@ def test_a_group_with_an_infinity_has_no_norm(bad, act, dtype):
         assert torch.isfinite(a[2]).all() and torch.isfinite(a[0, 8:]).all() and torch.isfinite(a[1, :8]).all(), name
 
 
+# -------------------------------------------------------------------------------------------------- ends of the range
+
+
+@pytest.mark.parametrize("by", [1e30, 1e-30])
+@pytest.mark.parametrize("tokens", [40, 5000])
+def test_band_norm_of_values_near_the_ends_of_their_range(tokens, by):
+    x, dy = (randn(1, 2, tokens, 16) * by).float(), randn(2, 2, tokens, 16)
+    w, b = randn(3, 1, 16), randn(4, 1, 16)
+    got = norm_and_gradients(x, [tokens], w, b, 2, "silu", 1e-30, dy)
+    ref, size = norm_of(x, [tokens], w, b, 2, "silu", 1e-30, dy)
+    for t, r, z, name in zip(got, ref, size, ("y", "dx", "dw", "db")):
+        close(t, r, z, name, 2.0 ** -20, 1e-37)
+
+
 # ---------------------------------------------------------------------------------- more workgroups than a launch has
 
 
@@ -303,6 +319,27 @@ def norm_of_pairs(x, dy, w, eps=1e-3):
     return (hat * w, dx), ((hat.abs() + 2) * w.abs(), r * (d.abs() + d.abs().mean(2, keepdim=True)) * (2 + (hat.abs() + 2) ** 2))
 
 
+# -------------------------------------------------------------------------------------------------- an infinite token
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_an_infinite_token_reaches_the_tiles_it_lies_in_only(dtype):
+    """Tiles of 32 tokens from the band's start for o and dq, from its end for dk and dv (136 .. 167 is one)."""
+    q, k, v, do = (randn(i, 1, 200, 2, 32, dtype=dtype) for i in (1, 2, 3, 4))
+    off, lam = offsets_of([200]), torch.tensor([-0.1, -0.01], device="cuda")
+
+    def run(q, k, v, do):
+        q, k, v = (t.clone().requires_grad_() for t in (q, k, v))
+        o = layers.decay_attention(q, k, v, off, lam)
+        return (o, *torch.autograd.grad(o, [q, k, v], do))
+
+    want = run(q, k, v, do)
+    q[:, 130], k[:, 131], v[:, 132], do[:, 133] = float("inf"), float("nan"), float("inf"), -float("inf")
+    got = run(q, k, v, do)
+    for a, b, at in zip(got, want, (slice(0, 128), slice(0, 128), slice(136, 200), slice(136, 200))):
+        assert torch.equal(a[:, at], b[:, at])
+
+
 # ------------------------------------------------------------------------------------------------------------ streams
 
 
@@ -326,3 +363,36 @@ def test_streams_that_a_read_begins_continues_and_leaves_alone():
     assert held.pos.tolist() == [5, 0, 7, -2, 12, 4]
     for n in (0, 2, 3, 4, 5):    # (what the state at pos 0 holds is not used)
         assert torch.equal(held.state[n], start[n] if lengths[n] else state[n]), n
+
+
+# ----------------------------------------------------------------------------------------------- claims of the header
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels, odd", [(64, 0), (77, 0), (40, 1)])
+def test_band_norm_may_write_over_its_input(channels, odd, dtype):
+    """Through the C call, which takes one tensor as x and y: short bands, long ones and tokens of no band."""
+    lengths, first, rows = [9, 0, 9000, 40], 4, 9060
+    x = randn(1, 2, rows, channels + odd, dtype=dtype)[..., odd:]
+    want = layers.band_norm(x, offsets_of(lengths, first), activation="gelu")
+    L, off = layers._lib(), offsets_of(lengths, first)
+    r = layers._ragged(off, 2, rows)
+    shape = layers._norm_shape(channels, 1, 1e-5, 0, 0, 0, 0, 2)
+    n = L.nsgcqt_band_norm_workspace(layers._DTYPES[dtype], r, shape, 0, 0)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    assert L.nsgcqt_band_norm(layers._DTYPES[dtype], r, shape, layers._view3(x), layers._view3(x), None, ws.data_ptr(), n,
+                              ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == nc.OK
+    assert torch.equal(x, want)
+
+
+def test_the_norm_s_module():
+    m = layers.BandNorm(3, 24, groups=4, activation="silu", eps=1e-3)
+    x, off = randn(1, 2, 60, 24).requires_grad_(), offsets_of([20, 0, 40])
+    with torch.no_grad():
+        m.weight.copy_(randn(2, 3, 24))
+        m.bias.copy_(randn(3, 3, 24))
+    y = m(x, off)
+    assert torch.equal(y, layers.band_norm(x, off, m.weight, m.bias, 4, "silu", 1e-3))
+    got = torch.autograd.grad(y.square().sum(), [x, m.weight, m.bias])
+    assert all(torch.isfinite(g).all() and g.any() for g in got)
+    assert [n for n, _ in m.named_parameters()] == ["weight", "bias"]
