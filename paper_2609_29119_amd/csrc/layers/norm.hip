@@ -249,7 +249,10 @@ int nsgcqt_band_norm_grad(int dtype, const nsgcqt_rows* r, const nsgcqt_norm_sha
                 set_threads(a, 256);
                 CHECK_TRY(launch_all(k_norm_weight<T, kWide>, a, items, a.threads, norm_lds(a), st));
             }
-            CHECK_TRY(launch_all(k_norm_weight_join<T>, a, (r->n_bands * s->channels + 255) / 256, 256, 0, st, by_chunk));
+            if ((by_chunk ? product(static_cast<int64_t>(a.parts), r->batch) : items) >= 64 * r->n_bands)
+                CHECK_TRY(launch_all(k_norm_weight_join<T, 16>, a, r->n_bands * ((s->channels + 63) / 64), 1024, 0, st, by_chunk));
+            else
+                CHECK_TRY(launch_all(k_norm_weight_join<T, 1>, a, (r->n_bands * s->channels + 255) / 256, 256, 0, st, by_chunk));
         }
         return NSGCQT_OK;
     });

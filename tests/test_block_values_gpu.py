@@ -146,6 +146,24 @@ def test_long_sums_of_a_norm_s_weights(lengths, batch, channels):
     assert ((db - want).abs() <= (2.0 ** -20 + 2.0 ** -24) * want).all(), ((db / want - 1).abs().max() * 2 ** 20).item()
 
 
+# --------------------------------------------------------------------------------------------------------- many parts
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,batch", [([20000, 1, 0, 300], 5), ([1, 1], 5000)])
+def test_many_parts_of_a_norm_s_weights(lengths, batch, dtype):
+    """Parts of several signals, and items of short bands, so many that the waves of a workgroup share them; 70 channels."""
+    rows, G = sum(lengths), len(lengths)
+    x, dy = randn(1, batch, rows, 70, dtype=dtype), randn(2, batch, rows, 70, dtype=dtype)
+    w, b = (randn(n, G, 70, dtype=dtype) for n in (3, 4))
+    got = norm_and_gradients(x, lengths, w, b, 7, "silu", 1e-3, dy)
+    full = [n for n in range(G) if lengths[n]]
+    ref, size = norm_of(x, [lengths[n] for n in full], w[full], b[full], 7, "silu", 1e-3, dy)
+    for t, r, z, name in zip([*got[:2], got[2][full], got[3][full]], ref, size, ("y", "dx", "dw", "db")):
+        close(t, r, z, name, 2.0 ** -20, 2.0 ** -25)
+    assert not any(got[i][n].any() for i in (2, 3) for n in range(G) if not lengths[n])
+
+
 # ----------------------------------------------------------------------------------------- and of the gated product's
 
 
