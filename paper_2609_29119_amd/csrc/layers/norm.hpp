@@ -91,10 +91,16 @@ template <class T> struct NormOctet {
         }
     }
     __device__ float hat(T x, int i) const { return fmaf(static_cast<float>(x) - high[i], rstd[i], low[i]); }
+    // For `out` alone: the mean's rest goes into b, so that it takes no registers.
+    __device__ void fold() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = fmaf(low[i], w[i], b[i]);
+    }
     template <int ACT> __device__ frag<T> out(frag<T> x) const {
         frag<T> y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = static_cast<T>(act_of<ACT, kExact>(fmaf(hat(x[i], i), w[i], b[i])));
+        for (int i = 0; i < 8; ++i)
+            y[i] = static_cast<T>(act_of<ACT, kExact>(fmaf((static_cast<float>(x[i]) - high[i]) * rstd[i], w[i], b[i])));
         return y;
     }
     // xh and dz
@@ -310,6 +316,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     if (!p.works(a)) return;
     o.load_affine(a, p.t.band, p.col);
     o.set(a, [&](int g) { return double2{mean[g], squares[g]}; });
+    o.fold();
     norm_out<T, N, WIDE>(a, p, o, x);
 }
 
@@ -395,6 +402,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_apply(NormArgs a) {
     const double2* st = p.stats(a);
     o.load_affine(a, p.t.band, p.col);
     o.set(a, [&](int g) { return st[g]; });
+    o.fold();
     by_act(a.act, [&](auto act) __attribute__((always_inline)) {
         for (int from = 0; from < p.n; from += N * a.together) {
 #pragma unroll
