@@ -424,7 +424,7 @@ template <class F, int N> __device__ inline Pieces<F, N> get_pieces(const char* 
 // they are; through LDS they go to the wave that takes the other half of the
 // inputs. x is read both ways from one tile. HELD: the inputs are all there
 // are, and W stays on chip for the whole chunk, Wa in registers and Wu in LDS.
-// The same case: 365 us and 39 for the join (four waves of all inputs, W in
+// The same case: 365 us and 41 for the join (four waves of all inputs, W in
 // registers, one wave a SIMD: 685); without the slope 325, without the second
 // product 317. Its two barriers a step keep a SIMD's waves in the same phase, so
 // that vector work and matrix cores take turns.

@@ -37,7 +37,7 @@ size_t norm_lds(const NormArgs& a) { return sizeof(double) * (8 * a.octets * a.t
 // fewer than 1024 workgroups are left. A workgroup is one wave where the mean
 // band is at most an eighth of what a wave holds: more bands are then on their
 // way at once. 256 bands of 64 signals, 64 channels in bfloat16, of 8 tokens at the
-// mean: 61 us, and 115 with four waves; with gradients, of 4: 155 and 207. With 16
+// mean: 62 us, and 117 with four waves; with gradients, of 4: 165 and 213. With 16
 // signals and bands twice as long, more of which take parts: 158 and 92.
 void set_chunk(NormArgs& a, int held) {
     set_threads(a, 256);

@@ -265,7 +265,7 @@ template <class T, int N, bool WIDE> __device__ inline void norm_out(const NormA
 
 // y of bands of one chunk, and zeros where no band is: the mean first, then the
 // squares of the differences from it. Bound by the chain of loads, sums and
-// barriers of a workgroup: 64 signals of one token of 128 channels 6.6 us.
+// barriers of a workgroup: 64 signals of one token of 128 channels 8.3 us.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm(NormArgs a) {
     constexpr int N = norm_held<T>();
@@ -326,7 +326,7 @@ template <class T> __device__ inline double norm_pivot(const NormArgs& a, int64_
 }
 
 // The sums of v and v^2, v = x - norm_pivot, of the parts of longer bands. 446,932 tokens of 128
-// channels, bfloat16, 221 bands: 28 us (4.1 TB/s); 710,680 of 77, float16: 48, as
+// channels, bfloat16, 221 bands: 28 us (4.1 TB/s); 710,680 of 77, float16: 51, as
 // loads at odd addresses take four accesses of the first cache each.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_sum(NormArgs a) {
@@ -390,7 +390,7 @@ template <class T, bool GRAD> __global__ __launch_bounds__(256) void k_norm_join
 
 // y of longer bands, a part a workgroup: the next tokens are on their way while
 // these are computed. The same two cases: 37 us, much of x coming from the
-// memory-side cache, and 83.
+// memory-side cache, and 84.
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_apply(NormArgs a) {
     constexpr int N = norm_held<T>() / 2;
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad(NormArgs a) {
 }
 
 // The sums of d and d xh of the parts of longer bands, and what they add to dw
-// and db. 446,932 tokens of 128 channels, bfloat16: 56 us (4.1 TB/s).
+// and db. 446,932 tokens of 128 channels, bfloat16: 58 us (3.9 TB/s).
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
     constexpr int N = 2;
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_sum(NormArgs a) {
     for (int g = tid; g < a.groups; g += a.threads) to[g] = double2{first[g], second[g]};
 }
 
-// dx of longer bands, a part a workgroup: 60 us (5.7 TB/s with the memory-side cache).
+// dx of longer bands, a part a workgroup: 61 us (5.6 TB/s with the memory-side cache).
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kNormThreads, 2) void k_norm_grad_apply(NormArgs a) {
     constexpr int N = 2;
